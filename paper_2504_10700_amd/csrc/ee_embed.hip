@@ -1,0 +1,550 @@
+// Element embedding and the gradient of its table (include/ee.h).
+//
+// Forward: a row copy with a factor, bound by the rows that it writes.
+//
+// Gradient: dT[z] = scale * sum of the rows of dY with index z.  The rows are read once, which is what bounds it; everything else is there
+// to keep the sums in a fixed order without atomics.
+//   1. a stable counting sort of the indices, 10 bits a pass (one pass up to 1023 elements, two up to EE_MAX_ELEMENTS): workgroups count their
+//      stretches of the batch, then each sums the counts before its own and scatters its stretch;
+//   2. the sorted order is cut into pieces of kPiece rows; a wave sums the runs of equal indices of one piece, 64 lanes across the
+//      channels.  A run inside one piece is a finished row of dT; one that goes on beyond it leaves its sum in a slot of the
+//      piece (slot 0: the run came in from the piece before; slot 1: it starts here and goes on);
+//   3. for each element the slots of its pieces are added in order, or its row is zeroed if it is absent.
+// Small batches instead look through all indices for each element: one launch.
+#include <algorithm>
+#include <cmath>
+
+#include "sc_internal.h"
+#include "../../include/ee.h"
+
+namespace ee {
+namespace {
+
+using sc::align_up;
+using sc::DeviceGuard;
+using sc::kLanes;
+using sc::misaligned;
+using sc::set_error;
+
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / kLanes;
+constexpr int kDigitBits = 10;
+constexpr int kBins = 1 << kDigitBits;
+constexpr int kSortBlocks = 256;     // most workgroups of a sort pass
+constexpr int kSortChunk = 2048;     // rows of a workgroup below that
+constexpr int kPiece = 64;           // sorted rows a wave sums
+constexpr int kAhead = 8;            // rows requested before the first of them is used
+
+template <typename T, int N>
+struct Vec {
+  typedef T type __attribute__((ext_vector_type(N), aligned(sizeof(T))));   // wide accesses need element alignment only
+};
+template <typename T>
+struct Vec<T, 1> {
+  typedef T type __attribute__((ext_vector_type(1), aligned(sizeof(T))));
+};
+
+// ---- forward
+
+// `rows` rows per workgroup, vectors of V channels; magic = 2^32 / per_row rounded up: i / per_row for i below 65536.
+template <typename TS, typename TA, int V>
+__global__ __launch_bounds__(kThreads) void forward_kernel(int64_t n, int channels, int elements, TA scale, int rows, int per_row,
+                                                           unsigned magic, const int* __restrict__ z, const TA* __restrict__ T,
+                                                           TS* __restrict__ Y) {
+  typedef typename Vec<TA, V>::type VA;
+  typedef typename Vec<TS, V>::type VS;
+  const int64_t blocks = (n + rows - 1) / rows;
+  for (int64_t block = blockIdx.x; block < blocks; block += gridDim.x) {
+    const int64_t first = block * rows;
+    const int count = static_cast<int>(min(static_cast<int64_t>(rows), n - first)) * per_row;
+    for (int i = threadIdx.x; i < count; i += kThreads) {
+      const int r = per_row == 1 ? i : static_cast<int>(__umulhi(static_cast<unsigned>(i), magic)), c = (i - r * per_row) * V;
+      const int element = z[first + r];
+      VS y;
+      if (static_cast<unsigned>(element) < static_cast<unsigned>(elements)) {
+        const VA t = *reinterpret_cast<const VA*>(T + static_cast<int64_t>(element) * channels + c);
+#pragma unroll
+        for (int k = 0; k < V; ++k) y[k] = static_cast<TS>(scale * t[k]);
+      } else {
+#pragma unroll
+        for (int k = 0; k < V; ++k) y[k] = static_cast<TS>(0.f);
+      }
+      *reinterpret_cast<VS*>(Y + (first + r) * channels + c) = y;
+    }
+  }
+}
+
+// ---- sort
+
+// The key of a row: its index, or `elements` for one outside the table.
+__device__ __forceinline__ int key_of(int z, int elements) {
+  return static_cast<unsigned>(z) < static_cast<unsigned>(elements) ? z : elements;
+}
+
+struct Sort {
+  int64_t n, per_block;   // rows, rows of a workgroup (a multiple of kThreads)
+  int elements, shift, bins;
+  const int* z;
+  const int* order;   // rows in the order of the previous pass, or NULL: 0, 1, 2, ...
+};
+
+__device__ __forceinline__ int row_at(const Sort& s, int64_t i) { return s.order ? s.order[i] : static_cast<int>(i); }
+__device__ __forceinline__ int digit_of(const Sort& s, int row) { return (key_of(s.z[row], s.elements) >> s.shift) & (kBins - 1); }
+
+// counts[block][bin]; on the way first[element] = -1 (no row yet).
+__global__ __launch_bounds__(kThreads) void count_kernel(Sort s, int* __restrict__ counts, int* __restrict__ first) {
+  __shared__ int bin[kBins];
+  for (int i = threadIdx.x; i < s.bins; i += kThreads) bin[i] = 0;
+  __syncthreads();
+  const int64_t begin = blockIdx.x * s.per_block, end = min(s.n, begin + s.per_block);
+  for (int64_t i = begin + threadIdx.x; i < end; i += kThreads) atomicAdd(&bin[digit_of(s, row_at(s, i))], 1);   // whole numbers: any order
+  __syncthreads();
+  for (int i = threadIdx.x; i < s.bins; i += kThreads) counts[blockIdx.x * static_cast<int64_t>(s.bins) + i] = bin[i];
+  if (first)
+    for (int i = blockIdx.x * kThreads + threadIdx.x; i < s.elements; i += gridDim.x * kThreads) first[i] = -1;
+}
+
+// Rows to their places: bins in order, inside a bin the order of the pass before.
+__global__ __launch_bounds__(kThreads) void scatter_kernel(Sort s, int blocks, const int* __restrict__ counts, int* __restrict__ out) {
+  __shared__ int place[kWaves][kBins];   // next place of each bin for each wave
+  __shared__ int wave_total[kWaves];
+  const int lane = threadIdx.x & (kLanes - 1), wave = threadIdx.x / kLanes;
+  const int64_t begin = blockIdx.x * s.per_block, end = min(s.n, begin + s.per_block);
+  const int64_t per_wave = s.per_block / kWaves;
+  const int64_t w0 = min(end, begin + wave * per_wave), w1 = min(end, w0 + per_wave);
+  for (int i = threadIdx.x; i < kWaves * kBins; i += kThreads) (&place[0][0])[i] = 0;
+  __syncthreads();
+  for (int64_t i = w0 + lane; i < w1; i += kLanes) atomicAdd(&place[wave][digit_of(s, row_at(s, i))], 1);
+  __syncthreads();
+  // bins 4 t .. 4 t + 3 of thread t: all rows of the bin, and those of earlier workgroups
+  constexpr int kOwn = kBins / kThreads;
+  int total[kOwn] = {}, before[kOwn] = {};
+  const int b0 = threadIdx.x * kOwn;
+  if (b0 < s.bins) {
+    for (int b = 0; b < blocks; ++b) {
+      const int* row = counts + b * static_cast<int64_t>(s.bins) + b0;
+#pragma unroll
+      for (int k = 0; k < kOwn; ++k) {
+        const int v = b0 + k < s.bins ? row[k] : 0;
+        total[k] += v;
+        before[k] += b < static_cast<int>(blockIdx.x) ? v : 0;
+      }
+    }
+  }
+  int mine = 0;
+#pragma unroll
+  for (int k = 0; k < kOwn; ++k) mine += total[k];
+  int up = mine;   // inclusive sum over the lanes
+#pragma unroll
+  for (int d = 1; d < kLanes; d *= 2) {
+    const int v = __shfl_up(up, d);
+    if (lane >= d) up += v;
+  }
+  if (lane == kLanes - 1) wave_total[wave] = up;
+  __syncthreads();
+  int at = up - mine;
+  for (int w = 0; w < wave; ++w) at += wave_total[w];
+#pragma unroll
+  for (int k = 0; k < kOwn; ++k) {
+    if (b0 + k < s.bins) {
+      int next = at + before[k];
+      for (int w = 0; w < kWaves; ++w) {
+        const int c = place[w][b0 + k];
+        place[w][b0 + k] = next;
+        next += c;
+      }
+    }
+    at += total[k];
+  }
+  __syncthreads();
+  // 64 rows at a time: a row's rank among the earlier lanes with the same bin, then the first of them moves the bin on
+  volatile int* const next = place[wave];
+  for (int64_t i = w0; i < w1; i += kLanes) {
+    const bool live = i + lane < w1;
+    const int row = live ? row_at(s, i + lane) : 0;
+    const int d = live ? digit_of(s, row) : 0;
+    unsigned long long same = __ballot(live);
+#pragma unroll
+    for (int bit = 0; bit < kDigitBits; ++bit) {
+      const unsigned long long set = __ballot((d >> bit) & 1);
+      same &= (d >> bit) & 1 ? set : ~set;
+    }
+    const unsigned long long below = same & ((1ull << lane) - 1);
+    int start = 0;
+    if (live) {
+      start = next[d];
+      out[start + __popcll(below)] = row;
+    }
+    __builtin_amdgcn_wave_barrier();   // every lane has read the place before it moves
+    if (live && below == 0) next[d] = start + __popcll(same);
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// ---- sums
+
+template <typename TS, typename TA, int V>
+struct Row {
+  typedef typename Vec<TS, V>::type VS;
+  typedef typename Vec<TA, V>::type VA;
+  static __device__ __forceinline__ void add(TA (&acc)[V], const VS& v) {
+#pragma unroll
+    for (int k = 0; k < V; ++k) acc[k] += static_cast<TA>(v[k]);
+  }
+  static __device__ __forceinline__ void store(TA* p, const TA (&acc)[V], TA scale) {
+    VA v;
+#pragma unroll
+    for (int k = 0; k < V; ++k) v[k] = scale * acc[k];
+    *reinterpret_cast<VA*>(p) = v;
+  }
+};
+
+// A wave: one piece of the sorted order, 64 V channels.  first / last: sorted positions of an element's first and last row.
+template <typename TS, typename TA, int V>
+__global__ __launch_bounds__(kThreads) void piece_kernel(int64_t n, int64_t pieces, int col_blocks, int channels, int elements, TA scale,
+                                                         const int* __restrict__ z, const int* __restrict__ order,
+                                                         const TS* __restrict__ dY, TA* __restrict__ dT, TA* __restrict__ slots,
+                                                         int* __restrict__ first, int* __restrict__ last) {
+  typedef Row<TS, TA, V> R;
+  const int lane = threadIdx.x & (kLanes - 1);
+  const int64_t task = blockIdx.x * static_cast<int64_t>(kWaves) + __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
+  if (task >= pieces * col_blocks) return;
+  const int64_t piece = task / col_blocks;
+  const int c = (static_cast<int>(task % col_blocks) * kLanes + lane) * V;
+  const bool live = c < channels;
+  const int64_t p0 = piece * kPiece;
+  const int count = static_cast<int>(min(static_cast<int64_t>(kPiece), n - p0));
+  static_assert(kPiece == kLanes, "a lane holds the row and the key of one position");
+  const int row = lane < count ? order[p0 + lane] : 0;
+  const int key = lane < count ? key_of(z[row], elements) : -1;
+  const int before = p0 > 0 ? key_of(z[order[p0 - 1]], elements) : -1;             // keys of the neighbouring positions
+  const int after = p0 + count < n ? key_of(z[order[p0 + count]], elements) : -1;
+  const int up = __shfl_up(key, 1), down = __shfl_down(key, 1);   // with all lanes active
+  const int left = lane == 0 ? before : up, right = lane == count - 1 ? after : down;
+  if (c == lane * V && lane < count && key < elements) {      // the first column block writes the bounds
+    if (left != key) first[key] = static_cast<int>(p0) + lane;
+    if (right != key) last[key] = static_cast<int>(p0) + lane;
+  }
+  const unsigned long long ends = __ballot(lane < count && right != key || lane == count - 1);   // last positions of the runs of this piece
+  TA acc[V] = {};
+  typename R::VS v[kAhead];
+  int run_start = 0;
+  for (int i = 0; i < count; i += kAhead) {
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const int r = __builtin_amdgcn_readlane(row, min(i + k, count - 1));
+      if (live) v[k] = *reinterpret_cast<const typename R::VS*>(dY + static_cast<int64_t>(r) * channels + c);
+    }
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      if (i + k >= count) break;
+      if (live) R::add(acc, v[k]);
+      if ((ends >> (i + k)) & 1) {
+        const int e = __builtin_amdgcn_readlane(key, i + k);
+        if (e < elements && live) {
+          const bool came_in = run_start == 0 && before == e, goes_on = i + k == count - 1 && after == e;
+          if (came_in) R::store(slots + (piece * 2) * channels + c, acc, TA(1));
+          else if (goes_on) R::store(slots + (piece * 2 + 1) * channels + c, acc, TA(1));
+          else R::store(dT + static_cast<int64_t>(e) * channels + c, acc, scale);
+        }
+#pragma unroll
+        for (int q = 0; q < V; ++q) acc[q] = TA(0);
+        run_start = i + k + 1;
+      }
+    }
+  }
+}
+
+// Rows of dT whose rows span pieces, and those of absent elements.  A wave per element (four elements a workgroup); spans longer than
+// kLongSpan pieces are shared by the four waves.
+constexpr int kLongSpan = 16;
+
+template <typename TA, int V>
+__device__ __forceinline__ void add_slots(const TA* __restrict__ slots, int64_t p0, int64_t from, int64_t to, int channels, int c, TA (&acc)[V]) {
+  typedef typename Vec<TA, V>::type VA;
+  for (int64_t p = from; p < to; p += kAhead) {
+    VA v[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const int64_t q = min(p + k, to - 1);
+      v[k] = *reinterpret_cast<const VA*>(slots + (q * 2 + (q == p0)) * channels + c);
+    }
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+      if (p + k < to)
+#pragma unroll
+        for (int i = 0; i < V; ++i) acc[i] += v[k][i];
+  }
+}
+
+template <typename TA, int V>
+__global__ __launch_bounds__(kThreads) void join_kernel(int channels, int elements, TA scale, const TA* __restrict__ slots,
+                                                        const int* __restrict__ first, const int* __restrict__ last, TA* __restrict__ dT) {
+  typedef Row<TA, TA, V> R;
+  __shared__ TA part[kWaves][kLanes * V];
+  const int lane = threadIdx.x & (kLanes - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
+  for (int64_t e0 = static_cast<int64_t>(blockIdx.x) * kWaves; e0 < elements; e0 += static_cast<int64_t>(gridDim.x) * kWaves) {
+    for (int w = 0; w < kWaves; ++w) {
+      const int64_t e = e0 + w;
+      if (e >= elements) break;
+      const int a = first[e];
+      const int64_t p0 = a / kPiece, p1 = a < 0 ? 0 : last[e] / kPiece;
+      if (a >= 0 && p0 == p1) continue;                       // summed inside one piece
+      const bool is_long = a >= 0 && p1 - p0 >= kLongSpan;    // the same for all waves
+      if (!is_long && w != wave) continue;
+      for (int c0 = 0; c0 < channels; c0 += kLanes * V) {
+        const int c = c0 + lane * V;
+        TA acc[V] = {};
+        if (!is_long) {
+          if (c < channels) {
+            if (a >= 0) add_slots<TA, V>(slots, p0, p0, p1 + 1, channels, c, acc);
+            R::store(dT + e * channels + c, acc, a >= 0 ? scale : TA(0));
+          }
+        } else {
+          const int64_t per = (p1 + 1 - p0 + kWaves - 1) / kWaves, from = min(p1 + 1, p0 + wave * per), to = min(p1 + 1, from + per);
+          if (c < channels) add_slots<TA, V>(slots, p0, from, to, channels, c, acc);
+          __syncthreads();
+#pragma unroll
+          for (int k = 0; k < V; ++k) part[wave][lane * V + k] = acc[k];
+          __syncthreads();
+          if (wave == 0 && c < channels) {
+            for (int v = 1; v < kWaves; ++v)
+#pragma unroll
+              for (int k = 0; k < V; ++k) acc[k] += part[v][lane * V + k];
+            R::store(dT + e * channels + c, acc, scale);
+          }
+        }
+      }
+    }
+  }
+}
+
+// Small batches: a wave per (element, 64 V channels) looks through all indices and adds its rows in order.
+template <typename TS, typename TA, int V>
+__global__ __launch_bounds__(kThreads) void search_kernel(int n, int col_blocks, int channels, int elements, TA scale,
+                                                          const int* __restrict__ z, const TS* __restrict__ dY, TA* __restrict__ dT) {
+  typedef Row<TS, TA, V> R;
+  const int lane = threadIdx.x & (kLanes - 1);
+  const int64_t task = blockIdx.x * static_cast<int64_t>(kWaves) + __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
+  if (task >= static_cast<int64_t>(elements) * col_blocks) return;
+  const int element = static_cast<int>(task / col_blocks);
+  const int c = (static_cast<int>(task % col_blocks) * kLanes + lane) * V;
+  TA acc[V] = {};
+  for (int i = 0; i < n; i += kLanes) {
+    unsigned long long hits = __ballot(i + lane < n && z[min(i + lane, n - 1)] == element);
+    while (hits) {
+      const int r = i + __builtin_ctzll(hits);
+      hits &= hits - 1;
+      if (c < channels) R::add(acc, *reinterpret_cast<const typename R::VS*>(dY + static_cast<int64_t>(r) * channels + c));
+    }
+  }
+  if (c < channels) R::store(dT + static_cast<int64_t>(element) * channels + c, acc, scale);
+}
+
+// ---- host side
+
+size_t row_size(const ee_config* c) { return c->dtype == SC_F64 ? 8 : c->dtype == SC_F32 ? 4 : 2; }
+size_t table_size(const ee_config* c) { return c->dtype == SC_F64 ? 8 : 4; }
+
+sc_status check_config(const char* fn, const ee_config* cfg, int64_t n) {
+  auto bad = [&](sc_status st, const char* what) { return set_error(st, std::string(fn) + ": " + what); };
+  if (!cfg) return bad(SC_ERR_INVALID_ARG, "cfg is NULL");
+  if (cfg->struct_size != static_cast<int32_t>(sizeof(ee_config)))
+    return bad(SC_ERR_INVALID_ARG, "struct_size does not match this library's ee_config");
+  if (cfg->num_elements < 1 || cfg->num_channels < 1) return bad(SC_ERR_INVALID_ARG, "num_elements or num_channels < 1");
+  if (cfg->num_elements > EE_MAX_ELEMENTS || cfg->num_channels > EE_MAX_CHANNELS)
+    return bad(SC_ERR_UNSUPPORTED, "num_elements above EE_MAX_ELEMENTS or num_channels above EE_MAX_CHANNELS");
+  if (cfg->dtype != SC_F32 && cfg->dtype != SC_F64 && cfg->dtype != SC_BF16) return bad(SC_ERR_INVALID_ARG, "bad dtype");
+  if (!std::isfinite(cfg->scale)) return bad(SC_ERR_INVALID_ARG, "scale not finite");
+  if (n < 0 || n > (int64_t(1) << 30)) return bad(SC_ERR_INVALID_ARG, "n_nodes outside 0..2^30");
+  return SC_OK;
+}
+
+// Does the search take a batch?  Its waves each look through all indices, 64 at a time, and it saves three launches.
+bool searched(const ee_config* c, int64_t n) { return n <= 1024 && n * c->num_elements <= 1 << 20; }
+
+int64_t sort_rows_per_block(int64_t n) {
+  const int64_t per = std::max<int64_t>(kSortChunk, (n + kSortBlocks - 1) / kSortBlocks);
+  return (per + kThreads - 1) / kThreads * kThreads;
+}
+int sort_passes(const ee_config* c) { return c->num_elements < kBins ? 1 : 2; }
+int sort_bins(const ee_config* c, int pass) {
+  const int keys = c->num_elements + 1;
+  return sort_passes(c) == 1 ? keys : pass == 0 ? kBins : (keys - 1) / kBins + 1;
+}
+
+struct Workspace {
+  int *order, *order0, *counts, *first, *last;
+  void* slots;
+  size_t bytes;
+};
+
+Workspace carve(const ee_config* c, int64_t n, void* base) {
+  Workspace w{};
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    void* p = static_cast<char*>(base) + at;
+    at += align_up(bytes, 256);
+    return p;
+  };
+  if (!searched(c, n)) {
+    const int64_t blocks = (n + sort_rows_per_block(n) - 1) / sort_rows_per_block(n);
+    w.order = static_cast<int*>(take(n * 4));
+    w.order0 = sort_passes(c) == 2 ? static_cast<int*>(take(n * 4)) : nullptr;
+    w.counts = static_cast<int*>(take(blocks * kBins * 4));
+    w.first = static_cast<int*>(take(static_cast<size_t>(c->num_elements) * 4));
+    w.last = static_cast<int*>(take(static_cast<size_t>(c->num_elements) * 4));
+    w.slots = take((n + kPiece - 1) / kPiece * 2 * c->num_channels * table_size(c));
+  }
+  w.bytes = at + 256;
+  return w;
+}
+
+unsigned blocks_of(int64_t waves) { return static_cast<unsigned>((waves + kWaves - 1) / kWaves); }
+
+template <typename TS, typename TA>
+struct Calls {
+  const ee_config* c;
+  int64_t n;
+  hipStream_t stream;
+
+  template <int V>
+  hipError_t forward_v(const int32_t* z, const void* T, void* Y) const {
+    const int per_row = c->num_channels / V;
+    const int rows = std::min<int64_t>(std::max(1, 2048 / per_row), std::max<int64_t>(1, n));
+    const unsigned magic = per_row == 1 ? 0 : static_cast<unsigned>(((uint64_t(1) << 32) + per_row - 1) / per_row);
+    const int64_t blocks = std::min<int64_t>((n + rows - 1) / rows, 1 << 20);
+    hipLaunchKernelGGL((forward_kernel<TS, TA, V>), dim3(static_cast<unsigned>(blocks)), dim3(kThreads), 0, stream, n, c->num_channels,
+                       c->num_elements, static_cast<TA>(c->scale), rows, per_row, magic, z, static_cast<const TA*>(T),
+                       static_cast<TS*>(Y));
+    return hipGetLastError();
+  }
+
+  hipError_t forward(const int32_t* z, const void* T, void* Y) const {
+    if (c->num_channels % 4 == 0) return forward_v<4>(z, T, Y);
+    return c->num_channels % 2 == 0 ? forward_v<2>(z, T, Y) : forward_v<1>(z, T, Y);
+  }
+
+  hipError_t sort(const int32_t* z, const Workspace& w) const {
+    Sort s{n, sort_rows_per_block(n), c->num_elements, 0, 0, z, nullptr};
+    const int blocks = static_cast<int>((n + s.per_block - 1) / s.per_block);
+    const int passes = sort_passes(c);
+    for (int pass = 0; pass < passes; ++pass) {
+      s.shift = pass * kDigitBits;
+      s.bins = sort_bins(c, pass);
+      s.order = pass == 0 ? nullptr : w.order0;
+      hipLaunchKernelGGL(count_kernel, dim3(blocks), dim3(kThreads), 0, stream, s, w.counts, pass == 0 ? w.first : nullptr);
+      hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+      hipLaunchKernelGGL(scatter_kernel, dim3(blocks), dim3(kThreads), 0, stream, s, blocks, w.counts, pass + 1 < passes ? w.order0 : w.order);
+      e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+  }
+
+  template <int V>
+  hipError_t backward_v(const int32_t* z, const void* dY, void* dT, void* ws) const {
+    const int k = c->num_channels, elements = c->num_elements;
+    const int col_blocks = (k + kLanes * V - 1) / (kLanes * V);
+    const TA scale = static_cast<TA>(c->scale);
+    if (searched(c, n)) {
+      hipLaunchKernelGGL((search_kernel<TS, TA, V>), dim3(blocks_of(static_cast<int64_t>(elements) * col_blocks)), dim3(kThreads), 0, stream,
+                         static_cast<int>(n), col_blocks, k, elements, scale, z, static_cast<const TS*>(dY), static_cast<TA*>(dT));
+      return hipGetLastError();
+    }
+    const Workspace w = carve(c, n, ws);
+    hipError_t e = sort(z, w);
+    if (e != hipSuccess) return e;
+    const int64_t pieces = (n + kPiece - 1) / kPiece;
+    hipLaunchKernelGGL((piece_kernel<TS, TA, V>), dim3(blocks_of(pieces * col_blocks)), dim3(kThreads), 0, stream, n, pieces, col_blocks, k,
+                       elements, scale, z, w.order, static_cast<const TS*>(dY), static_cast<TA*>(dT), static_cast<TA*>(w.slots), w.first,
+                       w.last);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((join_kernel<TA, V>), dim3(blocks_of(elements)), dim3(kThreads), 0, stream, k, elements, scale,
+                       static_cast<const TA*>(w.slots), w.first, w.last, static_cast<TA*>(dT));
+    return hipGetLastError();
+  }
+
+  // channels of a lane: as many as leave no lane idle, four at most
+  hipError_t backward(const int32_t* z, const void* dY, void* dT, void* ws) const {
+    const int k = c->num_channels;
+    if (k % 4 == 0 && k >= 4 * kLanes) return backward_v<4>(z, dY, dT, ws);
+    if (k % 2 == 0 && k >= 2 * kLanes) return backward_v<2>(z, dY, dT, ws);
+    return backward_v<1>(z, dY, dT, ws);
+  }
+};
+
+__global__ void zero_kernel(unsigned* __restrict__ p, int64_t words) {
+  for (int64_t i = blockIdx.x * static_cast<int64_t>(kThreads) + threadIdx.x; i < words; i += static_cast<int64_t>(gridDim.x) * kThreads) p[i] = 0;
+}
+
+template <typename F>
+hipError_t by_type(const ee_config* c, int64_t n, hipStream_t stream, F&& f) {
+  switch (c->dtype) {
+    case SC_F64: return f(Calls<double, double>{c, n, stream});
+    case SC_BF16: return f(Calls<__bf16, float>{c, n, stream});
+    default: return f(Calls<float, float>{c, n, stream});
+  }
+}
+
+}  // namespace
+}  // namespace ee
+
+extern "C" {
+
+sc_status ee_forward(const ee_config* cfg, int64_t n_nodes, const int32_t* z, const void* T, void* Y, void* hip_stream) {
+  using namespace ee;
+  const sc_status st = check_config("ee_forward", cfg, n_nodes);
+  if (st != SC_OK || n_nodes == 0) return st;
+  if (!z || !T || !Y) return set_error(SC_ERR_INVALID_ARG, "ee_forward: NULL tensor argument");
+  if (misaligned(z, 16) || misaligned(T, 16) || misaligned(Y, 16))
+    return set_error(SC_ERR_INVALID_ARG, "ee_forward: tensor pointer not 16-byte aligned");
+  DeviceGuard guard(cfg->device);
+  if (!guard.ok) return set_error(SC_ERR_HIP, "ee_forward: cannot make cfg->device current");
+  const hipError_t e = by_type(cfg, n_nodes, static_cast<hipStream_t>(hip_stream), [&](const auto& calls) { return calls.forward(z, T, Y); });
+  if (e != hipSuccess) return set_error(SC_ERR_HIP, std::string("ee_forward: kernel launch: ") + hipGetErrorString(e));
+  return SC_OK;
+}
+
+sc_status ee_workspace_bytes(const ee_config* cfg, int64_t n_nodes, size_t* bytes) {
+  using namespace ee;
+  const sc_status st = check_config("ee_workspace_bytes", cfg, n_nodes);
+  if (st != SC_OK) return st;
+  if (!bytes) return set_error(SC_ERR_INVALID_ARG, "ee_workspace_bytes: bytes is NULL");
+  *bytes = n_nodes == 0 ? 256 : carve(cfg, n_nodes, nullptr).bytes;
+  return SC_OK;
+}
+
+sc_status ee_backward(const ee_config* cfg, int64_t n_nodes, const int32_t* z, const void* dY, void* dT, void* workspace,
+                      size_t workspace_bytes, void* hip_stream) {
+  using namespace ee;
+  const sc_status st = check_config("ee_backward", cfg, n_nodes);
+  if (st != SC_OK) return st;
+  if (!dT) return set_error(SC_ERR_INVALID_ARG, "ee_backward: dT is NULL");
+  if (misaligned(z, 16) || misaligned(dY, 16) || misaligned(dT, 16))
+    return set_error(SC_ERR_INVALID_ARG, "ee_backward: tensor pointer not 16-byte aligned");
+  if (n_nodes > 0) {
+    if (!z || !dY) return set_error(SC_ERR_INVALID_ARG, "ee_backward: NULL tensor argument");
+    if (!workspace || workspace_bytes < carve(cfg, n_nodes, nullptr).bytes)
+      return set_error(SC_ERR_WORKSPACE, "ee_backward: workspace missing or smaller than ee_workspace_bytes()");
+    if (misaligned(workspace, 256)) return set_error(SC_ERR_WORKSPACE, "ee_backward: workspace not 256-byte aligned");
+  }
+  DeviceGuard guard(cfg->device);
+  if (!guard.ok) return set_error(SC_ERR_HIP, "ee_backward: cannot make cfg->device current");
+  hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  hipError_t e;
+  if (n_nodes == 0) {
+    const int64_t words = static_cast<int64_t>(cfg->num_elements) * cfg->num_channels * (table_size(cfg) / 4);
+    hipLaunchKernelGGL(zero_kernel, dim3(static_cast<unsigned>(std::min<int64_t>((words + kThreads - 1) / kThreads, 2048))), dim3(kThreads), 0,
+                       stream, static_cast<unsigned*>(dT), words);
+    e = hipGetLastError();
+  } else {
+    e = by_type(cfg, n_nodes, stream, [&](const auto& calls) { return calls.backward(z, dY, dT, workspace); });
+  }
+  if (e != hipSuccess) return set_error(SC_ERR_HIP, std::string("ee_backward: kernel launch: ") + hipGetErrorString(e));
+  return SC_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,301 @@
+// Global gradient norm over a list of tensors, and clipping (include/gc.h).
+//
+// Both passes stream the tensors once and are bound by memory.  The list travels as kernel arguments, kItems tensors a launch; its
+// elements are cut into chunks of kChunk that the workgroups take in turn, so a list of many small tensors costs as few workgroups
+// as one large one.  First pass: a partial sum of squares per workgroup, in fp64 (a 4-byte element costs one conversion and one fp64
+// fused multiply-add, far below what the memory takes).  Second pass: with one launch's partials every workgroup of the scaling sums
+// them itself in a fixed order (at most kPartials, 8 KB from the caches) - cheaper than a launch between the two; longer lists
+// have one.
+#include <algorithm>
+#include <cmath>
+
+#include "sc_internal.h"
+#include "../../include/gc.h"
+
+namespace gc {
+namespace {
+
+using sc::DeviceGuard;
+using sc::misaligned;
+using sc::set_error;
+
+constexpr int kThreads = 256;
+constexpr int kItems = 96;          // tensors of one launch: 3.9 KB of kernel arguments
+constexpr int kChunk = 4096;        // elements a workgroup takes at a time
+constexpr int kPartials = 1024;     // workgroups of one launch of the first pass
+
+struct Item {
+  const void* src;
+  void* dst;
+  int64_t numel;
+  int64_t first_chunk;   // chunks of the launch's earlier tensors
+  int32_t dtype;
+  int32_t pad;
+};
+
+struct Batch {
+  int64_t chunks;
+  int32_t count;
+  int32_t pad;
+  Item item[kItems];
+};
+static_assert(sizeof(Batch) <= 4000, "the kernel arguments hold 4 KB");
+
+template <typename T>
+struct Vec {
+  static constexpr int kN = 16 / sizeof(T);
+  typedef T type __attribute__((ext_vector_type(kN), aligned(sizeof(T))));   // 16-byte accesses need element alignment only
+};
+
+__device__ __forceinline__ const Item& item_of(const Batch& b, int64_t chunk) {
+  int lo = 0, hi = b.count - 1;      // the last tensor whose first chunk is not beyond `chunk`; empty ones share it with the next
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) / 2;
+    if (b.item[mid].first_chunk <= chunk) lo = mid; else hi = mid - 1;
+  }
+  return b.item[lo];
+}
+
+// f(src, n) once per full vector of the chunk and per left-over element, all vectors of a thread requested before the first is used.
+template <typename T, typename F>
+__device__ __forceinline__ void each_vector(const T* __restrict__ src, int64_t n, F&& f) {
+  constexpr int N = Vec<T>::kN, kRounds = kChunk / (kThreads * N);
+  typedef typename Vec<T>::type V;
+  if (n >= kChunk) {
+    V v[kRounds];
+#pragma unroll
+    for (int i = 0; i < kRounds; ++i) v[i] = *reinterpret_cast<const V*>(src + (i * kThreads + threadIdx.x) * N);
+#pragma unroll
+    for (int i = 0; i < kRounds; ++i)
+#pragma unroll
+      for (int k = 0; k < N; ++k) f.element(v[i][k], (i * kThreads + threadIdx.x) * N + k, k, N);
+  } else {
+    for (int at = threadIdx.x; at < n; at += kThreads) f.element(src[at], at, 0, 1);
+  }
+}
+
+struct Square {
+  double sum = 0;
+  template <typename T>
+  __device__ __forceinline__ void element(T x, int, int, int) {
+    const double v = static_cast<double>(static_cast<std::conditional_t<sizeof(T) == 8, double, float>>(x));
+    sum = fma(v, v, sum);
+  }
+};
+
+template <typename T>
+__device__ __forceinline__ void scale_chunk(const T* __restrict__ src, T* __restrict__ dst, int64_t n, double coefficient) {
+  typedef std::conditional_t<sizeof(T) == 8, double, float> A;
+  constexpr int N = Vec<T>::kN, kRounds = kChunk / (kThreads * N);
+  typedef typename Vec<T>::type V;
+  const A c = static_cast<A>(coefficient);
+  if (n >= kChunk) {
+    V v[kRounds];
+#pragma unroll
+    for (int i = 0; i < kRounds; ++i) v[i] = *reinterpret_cast<const V*>(src + (i * kThreads + threadIdx.x) * N);
+#pragma unroll
+    for (int i = 0; i < kRounds; ++i) {
+#pragma unroll
+      for (int k = 0; k < N; ++k) v[i][k] = static_cast<T>(c * static_cast<A>(v[i][k]));
+      *reinterpret_cast<V*>(dst + (i * kThreads + threadIdx.x) * N) = v[i];
+    }
+  } else {
+    for (int at = threadIdx.x; at < n; at += kThreads) dst[at] = static_cast<T>(c * static_cast<A>(src[at]));
+  }
+}
+
+// The same sum in every workgroup and run: lanes, then waves in order.
+__device__ __forceinline__ double workgroup_sum(double v, double* slots) {
+#pragma unroll
+  for (int d = 32; d > 0; d /= 2) v += __shfl_xor(v, d);
+  if ((threadIdx.x & 63) == 0) slots[threadIdx.x / 64] = v;
+  __syncthreads();
+  double s = slots[0];
+#pragma unroll
+  for (int w = 1; w < kThreads / 64; ++w) s += slots[w];
+  __syncthreads();
+  return s;
+}
+
+__device__ __forceinline__ double sum_partials(const double* __restrict__ partial, int64_t n, double* slots) {
+  double s = 0;
+  for (int64_t i = threadIdx.x; i < n; i += kThreads) s += partial[i];
+  return workgroup_sum(s, slots);
+}
+
+__device__ __forceinline__ double coefficient_of(double norm, double max_norm, double eps) {
+  const double c = max_norm / (norm + eps);
+  return c < 1.0 ? c : norm != norm ? norm : 1.0;
+}
+
+__device__ __forceinline__ void store_result(void* out, int dtype, double norm, double coefficient) {
+  if (dtype == SC_F64) {
+    static_cast<double*>(out)[0] = norm;
+    static_cast<double*>(out)[1] = coefficient;
+  } else {
+    static_cast<float*>(out)[0] = static_cast<float>(norm);
+    static_cast<float*>(out)[1] = static_cast<float>(coefficient);
+  }
+}
+
+__global__ __launch_bounds__(kThreads) void square_kernel(const Batch b, double* __restrict__ partial) {
+  __shared__ double slots[kThreads / 64];
+  Square q;
+  for (int64_t chunk = blockIdx.x; chunk < b.chunks; chunk += gridDim.x) {
+    const Item& it = item_of(b, chunk);
+    const int64_t at = (chunk - it.first_chunk) * kChunk, n = it.numel - at;
+    if (it.dtype == SC_F64) each_vector(static_cast<const double*>(it.src) + at, n, q);
+    else if (it.dtype == SC_F32) each_vector(static_cast<const float*>(it.src) + at, n, q);
+    else each_vector(static_cast<const __bf16*>(it.src) + at, n, q);
+  }
+  const double s = workgroup_sum(q.sum, slots);
+  if (threadIdx.x == 0) partial[blockIdx.x] = s;
+}
+
+// Norm and coefficient of a list that took several launches, or of one that is not scaled.
+__global__ __launch_bounds__(kThreads) void finish_kernel(const double* __restrict__ partial, int64_t n, double max_norm, double eps,
+                                                          int dtype, void* out, double* __restrict__ kept) {
+  __shared__ double slots[kThreads / 64];
+  const double norm = sqrt(sum_partials(partial, n, slots));
+  if (threadIdx.x == 0) {
+    const double c = coefficient_of(norm, max_norm, eps);
+    store_result(out, dtype, norm, c);
+    *kept = c;
+  }
+}
+
+// kept: the coefficient, or NULL: it is made here from the partial sums.
+__global__ __launch_bounds__(kThreads) void scale_kernel(const Batch b, const double* __restrict__ partial, int64_t n, double max_norm,
+                                                         double eps, int dtype, void* out, const double* __restrict__ kept) {
+  __shared__ double slots[kThreads / 64];
+  double c;
+  if (kept) {
+    c = *kept;
+  } else {
+    const double norm = sqrt(sum_partials(partial, n, slots));
+    c = coefficient_of(norm, max_norm, eps);
+    if (blockIdx.x == 0 && threadIdx.x == 0) store_result(out, dtype, norm, c);
+  }
+  for (int64_t chunk = blockIdx.x; chunk < b.chunks; chunk += gridDim.x) {
+    const Item& it = item_of(b, chunk);
+    if (!it.dst || (it.dst == it.src && c == 1.0)) continue;
+    const int64_t at = (chunk - it.first_chunk) * kChunk, left = it.numel - at;
+    if (it.dtype == SC_F64) scale_chunk(static_cast<const double*>(it.src) + at, static_cast<double*>(it.dst) + at, left, c);
+    else if (it.dtype == SC_F32) scale_chunk(static_cast<const float*>(it.src) + at, static_cast<float*>(it.dst) + at, left, c);
+    else scale_chunk(static_cast<const __bf16*>(it.src) + at, static_cast<__bf16*>(it.dst) + at, left, c);
+  }
+}
+
+// ---- host side
+
+int64_t batches_of(int64_t n_tensors) { return std::max<int64_t>(1, (n_tensors + kItems - 1) / kItems); }
+
+// Workspace: [ coefficient ][ partial sums, kPartials per launch of the first pass ].
+size_t workspace_bytes(int64_t n_tensors) { return 256 + static_cast<size_t>(batches_of(n_tensors)) * kPartials * sizeof(double); }
+
+size_t elem_size(int dtype) { return dtype == SC_F64 ? 8 : dtype == SC_F32 ? 4 : 2; }
+
+Batch batch_of(int64_t n_tensors, const gc_tensor* tensors, int64_t index) {
+  Batch b;
+  b.chunks = 0;
+  b.pad = 0;
+  b.count = static_cast<int32_t>(std::min<int64_t>(kItems, n_tensors - index * kItems));
+  for (int i = 0; i < b.count; ++i) {
+    const gc_tensor& t = tensors[index * kItems + i];
+    b.item[i] = {t.src, t.dst, t.numel, b.chunks, t.dtype, 0};
+    b.chunks += (t.numel + kChunk - 1) / kChunk;
+  }
+  return b;
+}
+
+sc_status check(const char* fn, const gc_config* cfg, int64_t n, const gc_tensor* tensors) {
+  auto bad = [&](sc_status st, const std::string& what) { return set_error(st, std::string(fn) + ": " + what); };
+  if (!cfg) return bad(SC_ERR_INVALID_ARG, "cfg is NULL");
+  if (cfg->struct_size != static_cast<int32_t>(sizeof(gc_config)))
+    return bad(SC_ERR_INVALID_ARG, "struct_size does not match this library's gc_config");
+  if (cfg->dtype != SC_F32 && cfg->dtype != SC_F64) return bad(SC_ERR_INVALID_ARG, "bad dtype");
+  if (!(cfg->max_norm > 0)) return bad(SC_ERR_INVALID_ARG, "max_norm not above 0");
+  if (!(cfg->eps >= 0) || std::isinf(cfg->eps)) return bad(SC_ERR_INVALID_ARG, "eps negative or not finite");
+  if (n < 0) return bad(SC_ERR_INVALID_ARG, "n_tensors < 0");
+  if (n > GC_MAX_TENSORS) return bad(SC_ERR_UNSUPPORTED, "more than GC_MAX_TENSORS tensors");
+  if (n > 0 && !tensors) return bad(SC_ERR_INVALID_ARG, "tensors is NULL");
+  int scaled = -1;   // does the first tensor that is not empty have a dst?
+  for (int64_t i = 0; i < n; ++i) {
+    const gc_tensor& t = tensors[i];
+    const char* what = nullptr;
+    if (t.dtype != SC_F32 && t.dtype != SC_F64 && t.dtype != SC_BF16) what = "bad dtype";
+    else if (t.numel < 0 || t.numel > (int64_t(1) << 40)) what = "numel outside 0..2^40";
+    else if (t.numel > 0 && !t.src) what = "src is NULL";
+    else if (misaligned(t.src, elem_size(t.dtype)) || misaligned(t.dst, elem_size(t.dtype))) what = "pointer not aligned to its element";
+    else if (t.numel > 0 && scaled >= 0 && scaled != (t.dst != nullptr)) what = "dst is NULL for some tensors and not for others";
+    if (what) return bad(SC_ERR_INVALID_ARG, "tensor " + std::to_string(i) + ": " + what);
+    if (t.numel > 0) scaled = t.dst != nullptr;
+  }
+  return SC_OK;
+}
+
+hipError_t clip(const gc_config* cfg, int64_t n, const gc_tensor* tensors, void* out, void* workspace, hipStream_t stream) {
+  double* kept = static_cast<double*>(workspace);
+  double* partial = kept + 32;
+  const int64_t batches = batches_of(n);
+  bool scaled = false;
+  for (int64_t i = 0; i < n; ++i) scaled = scaled || (tensors[i].dst && tensors[i].numel > 0);
+  int64_t partials = 0;
+  for (int64_t i = 0; i < batches; ++i) {
+    const Batch b = batch_of(n, tensors, i);
+    if (b.chunks == 0) continue;
+    const unsigned grid = static_cast<unsigned>(std::min<int64_t>(b.chunks, kPartials));
+    hipLaunchKernelGGL(square_kernel, dim3(grid), dim3(kThreads), 0, stream, b, partial + partials);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    partials += grid;
+  }
+  const bool together = scaled && batches == 1;
+  if (!together) {
+    hipLaunchKernelGGL(finish_kernel, dim3(1), dim3(kThreads), 0, stream, partial, partials, cfg->max_norm, cfg->eps, cfg->dtype, out, kept);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !scaled) return e;
+  }
+  for (int64_t i = 0; i < batches; ++i) {
+    const Batch b = batch_of(n, tensors, i);
+    if (b.chunks == 0) continue;
+    hipLaunchKernelGGL(scale_kernel, dim3(static_cast<unsigned>(std::min<int64_t>(b.chunks, 2048))), dim3(kThreads), 0, stream, b, partial,
+                       partials, cfg->max_norm, cfg->eps, cfg->dtype, out, together ? nullptr : kept);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+}  // namespace
+}  // namespace gc
+
+extern "C" {
+
+sc_status gc_workspace_bytes(const gc_config* cfg, int64_t n_tensors, const gc_tensor* tensors, size_t* bytes) {
+  const sc_status st = gc::check("gc_workspace_bytes", cfg, n_tensors, tensors);
+  if (st != SC_OK) return st;
+  if (!bytes) return sc::set_error(SC_ERR_INVALID_ARG, "gc_workspace_bytes: bytes is NULL");
+  *bytes = gc::workspace_bytes(n_tensors);
+  return SC_OK;
+}
+
+sc_status gc_clip(const gc_config* cfg, int64_t n_tensors, const gc_tensor* tensors, void* norm_and_coefficient, void* workspace,
+                  size_t workspace_bytes, void* hip_stream) {
+  using namespace gc;
+  const sc_status st = check("gc_clip", cfg, n_tensors, tensors);
+  if (st != SC_OK) return st;
+  if (!norm_and_coefficient) return set_error(SC_ERR_INVALID_ARG, "gc_clip: norm_and_coefficient is NULL");
+  if (misaligned(norm_and_coefficient, cfg->dtype == SC_F64 ? 8 : 4))
+    return set_error(SC_ERR_INVALID_ARG, "gc_clip: norm_and_coefficient not aligned to its element");
+  if (!workspace || workspace_bytes < gc::workspace_bytes(n_tensors))
+    return set_error(SC_ERR_WORKSPACE, "gc_clip: workspace missing or smaller than gc_workspace_bytes()");
+  if (misaligned(workspace, 256)) return set_error(SC_ERR_WORKSPACE, "gc_clip: workspace not 256-byte aligned");
+  DeviceGuard guard(cfg->device);
+  if (!guard.ok) return set_error(SC_ERR_HIP, "gc_clip: cannot make cfg->device current");
+  const hipError_t e = clip(cfg, n_tensors, tensors, norm_and_coefficient, workspace, static_cast<hipStream_t>(hip_stream));
+  if (e != hipSuccess) return set_error(SC_ERR_HIP, std::string("gc_clip: kernel launch: ") + hipGetErrorString(e));
+  return SC_OK;
+}
+
+}  // extern "C"
