@@ -10,275 +10,348 @@
 //   X2        rows x k_in    A = S    B = W^T
 //   W2, b2    k_in x k_out   A = X^T  B = S, then A = HX^T  B = G on the same accumulators
 #include <algorithm>
-#include <cstring>
+#include <initializer_list>
+#include <string>
+#include <type_traits>
 
-#include "dl_gate.h"
-#include "el_tile.h"
+#include "dl_product.h"
 
 namespace dl {
 namespace {
 
-using el::Mma;
 using sc::align_up;
 using sc::DeviceGuard;
-using sc::kLanes;
 using sc::misaligned;
 using sc::set_error;
 
-constexpr int kThreads = 256;
-constexpr int kTile = 64;      // rows and columns of a workgroup's tile: four waves of 32 x 32
-constexpr int kDepth = 16;     // reduction index per staged step
-constexpr int kPad = kTile + 4;
 constexpr int kXcds = 8;
 
-// One row-major tensor as an operand: element (r, c) at p[r * ld + c].
-template <typename T>
-struct Matrix {
-  const T* p;
-  int64_t ld;
+// Waves that share one result where rows are few (the registers of an fp64 wave leave room for four).
+template <typename TA>
+__host__ __device__ constexpr int split_waves() { return sizeof(TA) == 8 ? 4 : 8; }
+template <bool kSplit, typename TA>
+constexpr int threads() { return kSplit ? split_waves<TA>() * kLanes : kThreads; }
+// LDS of a product of rows: the waves' corners, or their results where they share one.
+template <bool kSplit, int kRT, typename TA>
+constexpr int lds_elements() { return kSplit ? split_waves<TA>() * 16 * kLanes : kWaves * kRT * Corner<TA>::kBlock; }
+
+// How a workgroup's waves stand: wc side by side along the columns, the others along the rows.
+struct Shape {
+  int wc, wr;
 };
 
-enum Source { kPlain, kGated };   // kGated: dY act'(Z)
-
-template <typename T, typename TA>
-__device__ __forceinline__ void load4(const Matrix<T>& m, int64_t r, int64_t c, int64_t rows, int64_t cols, TA (&v)[4]) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = TA(0);
-  if (r >= rows || c >= cols) return;
-  const T* p = m.p + r * m.ld + c;
-  if (c + 4 <= cols) {
-    typedef T Vec __attribute__((ext_vector_type(4), aligned(sizeof(T))));   // wide accesses need element alignment only
-    const Vec x = *reinterpret_cast<const Vec*>(p);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = static_cast<TA>(x[i]);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (c + i < cols) v[i] = static_cast<TA>(p[i]);
-  }
-}
-
-template <typename TA, typename T, Source kSource>
-struct Operand {
-  Matrix<T> x, z;   // z: pre-activations beside x = dY (kGated)
-  int act;
-  __device__ __forceinline__ void load(int64_t r, int64_t c, int64_t rows, int64_t cols, TA (&v)[4]) const {
-    load4(x, r, c, rows, cols, v);
-    if constexpr (kSource == kGated) {
-      TA g[4];
-      load4(z, r, c, rows, cols, g);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] *= Gate<TA>::first(act, g[i]);
-    }
-  }
-};
-
-// Adds to acc the product over k in [k0, k1) of the 64 x 64 tile at (m0, n0).  kAlongM: A is stored [k][m], otherwise [m][k];
-// kAlongN: B is stored [k][n], otherwise [n][k].  sum: column sums of B, per staging thread, if wanted.
-template <typename TA, bool kAlongM, bool kAlongN, bool kSum, typename A, typename B>
-__device__ __forceinline__ void tile_product(const A& a, const B& b, int64_t m0, int64_t n0, int64_t m_end, int64_t n_end,
-                                             int64_t k0, int64_t k1, TA* as, TA* bs, typename Mma<TA>::acc_t (&acc)[2][2],
-                                             TA (&sum)[4]) {
-  const int t = threadIdx.x, lane = t & (kLanes - 1), wave = t / kLanes;
-  const int wm = (wave / 2) * 32, wn = (wave % 2) * 32;
-  TA va[4], vb[4];
-  auto fetch = [&](int64_t k) {
-    if constexpr (kAlongM)
-      a.load(k + t / 16, m0 + (t % 16) * 4, k1, m_end, va);
-    else
-      a.load(m0 + t / 4, k + (t % 4) * 4, m_end, k1, va);
-    if constexpr (kAlongN)
-      b.load(k + t / 16, n0 + (t % 16) * 4, k1, n_end, vb);
-    else
-      b.load(n0 + t / 4, k + (t % 4) * 4, n_end, k1, vb);
-  };
-  auto stage = [&]() {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if constexpr (kAlongM) as[(t / 16) * kPad + (t % 16) * 4 + i] = va[i];
-      else as[((t % 4) * 4 + i) * kPad + t / 4] = va[i];
-      if constexpr (kAlongN) bs[(t / 16) * kPad + (t % 16) * 4 + i] = vb[i];
-      else bs[((t % 4) * 4 + i) * kPad + t / 4] = vb[i];
-      if constexpr (kSum) sum[i] += vb[i];
-    }
-  };
-  if (k0 < k1) fetch(k0);
-  for (int64_t k = k0; k < k1; k += kDepth) {
-    __syncthreads();
-    stage();
-    __syncthreads();
-    if (k + kDepth < k1) fetch(k + kDepth);
-#pragma unroll
-    for (int s = 0; s < kDepth / 4; ++s) {
-      const int row = (s * 4 + lane / 16) * kPad + (lane & 15);
-      TA fa[2], fb[2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        fa[i] = as[row + wm + i * 16];
-        fb[i] = bs[row + wn + i * 16];
-      }
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) acc[i][j] = Mma<TA>::mma(fa[i], fb[j], acc[i][j]);
-    }
-  }
-}
-
-// Calls f(m, n, value) for the elements of the tile that lie inside the result.
-template <typename TA, typename F>
-__device__ __forceinline__ void each_result(int64_t m0, int64_t n0, int64_t m_end, int64_t n_end,
-                                            const typename Mma<TA>::acc_t (&acc)[2][2], F&& f) {
-  const int lane = threadIdx.x & (kLanes - 1), wave = threadIdx.x / kLanes;
-#pragma unroll
-  for (int i = 0; i < 2; ++i)
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int64_t m = m0 + (wave / 2) * 32 + i * 16 + Mma<TA>::row(lane, r);
-        const int64_t n = n0 + (wave % 2) * 32 + j * 16 + (lane & 15);
-        if (m < m_end && n < n_end) f(m, n, acc[i][j][r]);
-      }
-}
-
-// The tiles of a result with many rows: all column tiles of a row tile go to one XCD (workgroups are dealt out to the XCDs in turn), whose
+// Row groups x column groups of workgroups.  All column groups of a row group go to one XCD (workgroups are dealt out to the XCDs in turn), whose
 // L2 then holds the rows that they share.
-struct TileWalk {
-  int64_t row_tiles, col_tiles;
-  __host__ __device__ int64_t count() const { return (row_tiles + kXcds - 1) / kXcds * kXcds * col_tiles; }
-  __device__ bool at(int64_t t, int64_t* row, int64_t* col) const {
+struct Walk {
+  int64_t row_groups;
+  int col_groups;
+  __host__ __device__ int64_t count() const { return (row_groups + kXcds - 1) / kXcds * kXcds * col_groups; }
+  __device__ bool at(int64_t t, int64_t* row, int* col) const {
     const int64_t local = t / kXcds;
-    *row = local / col_tiles * kXcds + t % kXcds;
-    *col = local % col_tiles;
-    return *row < row_tiles;
+    *row = local / col_groups * kXcds + t % kXcds;
+    *col = static_cast<int>(local % col_groups);
+    return *row < row_groups;
   }
 };
 
-template <typename TA>
-struct Zero {
-  typename Mma<TA>::acc_t acc[2][2];
-  __device__ Zero() {
+// The results of 16 kRT rows and 64 columns, by this wave alone or (kSplit) by all waves of the workgroup, each over its part of the reduced
+// index, joined in LDS in the order of the waves.  f as in each_four.
+template <typename TA, int kRT, bool kSplit, bool kFours, typename Rows, typename Weights, typename T, int N, typename F>
+__device__ __forceinline__ void finish_rows(const Rows& a, const Weights& w, int64_t row0, int64_t rows, int n0, TA* lds,
+                                            const TA* __restrict__ bias, const Beside<T, N>& beside, F&& f) {
+  typename Mma<TA>::acc_t acc[kRT][4];
+  const int lane = threadIdx.x & (kLanes - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
+  TA* const corner = lds + wave * (kRT * Corner<TA>::kBlock);
+  if constexpr (!kSplit) {
+    rows_product<TA, kRT, kFours>(a, w, row0, rows, n0, 0, w.k_end, corner, acc);
+    each_four<TA, kRT, kFours>(row0, rows, n0, w.n_end, acc, bias, beside, f);
+  } else {
+    static_assert(kRT == 1, "one row tile");
+    constexpr int kN = split_waves<TA>();
+    const int per = ((w.k_end + kN - 1) / kN + kDepth - 1) / kDepth * kDepth;
+    const int from = min(w.k_end, wave * per), to = min(w.k_end, from + per);
+    if (from < to) {
+      rows_product<TA, 1, kFours>(a, w, row0, rows, n0, from, to, corner, acc);
+    } else {
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int j = 0; j < 2; ++j) acc[i][j] = typename Mma<TA>::acc_t{0, 0, 0, 0};
-  }
-};
-
-template <typename TS, typename TA>
-__global__ __launch_bounds__(kThreads) void forward_kernel(TileWalk walk, int64_t rows, int k_in, int k_out, int64_t ld_out, int act,
-                                                           Matrix<TS> X, Matrix<TA> W, const TA* __restrict__ bias,
-                                                           const TS* __restrict__ residual, TS* __restrict__ Y, TS* __restrict__ Z) {
-  __shared__ TA as[kDepth * kPad], bs[kDepth * kPad];
-  const Operand<TA, TS, kPlain> a{X, X, 0};
-  const Operand<TA, TA, kPlain> b{W, W, 0};
-  for (int64_t t = blockIdx.x; t < walk.count(); t += gridDim.x) {
-    int64_t row, col;
-    if (!walk.at(t, &row, &col)) continue;
-    Zero<TA> c;
-    TA none[4];
-    tile_product<TA, false, true, false>(a, b, row * kTile, col * kTile, rows, k_out, 0, k_in, as, bs, c.acc, none);
-    each_result<TA>(row * kTile, col * kTile, rows, k_out, c.acc, [&](int64_t m, int64_t n, TA z) {
-      const int64_t at = m * ld_out + n;
-      if (bias) z += bias[n];
-      if (Z) Z[at] = static_cast<TS>(z);
-      TA y = Gate<TA>::value(act, z);
-      if (residual) y += static_cast<TA>(residual[at]);
-      Y[at] = static_cast<TS>(y);
-    });
-  }
-}
-
-// dX (and X2, whose source is S): A = the source, B = W transposed.
-template <typename TS, typename TA, typename TG, Source kSource>
-__global__ __launch_bounds__(kThreads) void dx_kernel(TileWalk walk, int64_t rows, int k_in, int k_out, int64_t ld_in,
-                                                      Operand<TA, TG, kSource> g, Matrix<TA> W, TS* __restrict__ dX) {
-  __shared__ TA as[kDepth * kPad], bs[kDepth * kPad];
-  const Operand<TA, TA, kPlain> b{W, W, 0};
-  for (int64_t t = blockIdx.x; t < walk.count(); t += gridDim.x) {
-    int64_t row, col;
-    if (!walk.at(t, &row, &col)) continue;
-    Zero<TA> c;
-    TA none[4];
-    tile_product<TA, false, false, false>(g, b, row * kTile, col * kTile, rows, k_in, 0, k_out, as, bs, c.acc, none);
-    each_result<TA>(row * kTile, col * kTile, rows, k_in, c.acc,
-                    [&](int64_t m, int64_t n, TA v) { dX[m * ld_in + n] = static_cast<TS>(v); });
-  }
-}
-
-template <typename TS, typename TA>
-__global__ __launch_bounds__(kThreads) void v_kernel(TileWalk walk, int64_t rows, int k_in, int k_out, int64_t ld_out, int act,
-                                                     Matrix<TS> HX, Matrix<TA> W, const TS* __restrict__ Z, const TS* __restrict__ dY,
-                                                     TS* __restrict__ ddY, TA* __restrict__ S) {
-  __shared__ TA as[kDepth * kPad], bs[kDepth * kPad];
-  const Operand<TA, TS, kPlain> a{HX, HX, 0};
-  const Operand<TA, TA, kPlain> b{W, W, 0};
-  for (int64_t t = blockIdx.x; t < walk.count(); t += gridDim.x) {
-    int64_t row, col;
-    if (!walk.at(t, &row, &col)) continue;
-    Zero<TA> c;
-    TA none[4];
-    tile_product<TA, false, true, false>(a, b, row * kTile, col * kTile, rows, k_out, 0, k_in, as, bs, c.acc, none);
-    each_result<TA>(row * kTile, col * kTile, rows, k_out, c.acc, [&](int64_t m, int64_t n, TA v) {
-      const int64_t at = m * ld_out + n;
-      if (Z) {
-        TA first, second;
-        Gate<TA>::both(act, static_cast<TA>(Z[at]), &first, &second);
-        if (S) S[m * k_out + n] = v * static_cast<TA>(dY[at]) * second;
-        v *= first;
-      }
-      ddY[at] = static_cast<TS>(v);
-    });
-  }
-}
-
-// Partial dW (and db) of one range of rows per workgroup: tile (m, n) of the range's row of `part`, [k_in][k_out] then [k_out].
-// kTwo: A2, B2 are added on the same accumulators (the second-order pass); column sums are those of the first pair.
-template <typename TA, typename TX, typename TB, Source kB, typename TB2, Source kB2, bool kTwo>
-__global__ __launch_bounds__(kThreads) void dw_kernel(int64_t rows, int64_t per, int k_in, int k_out, int want_dw, int want_db,
-                                                      Matrix<TX> X, Operand<TA, TB, kB> B, Matrix<TX> X2, Operand<TA, TB2, kB2> B2,
-                                                      TA* __restrict__ dW, TA* __restrict__ db, int64_t stride) {
-  __shared__ TA as[kDepth * kPad], bs[kDepth * kPad];
-  __shared__ TA sums[16][kTile];
-  const int col_tiles = (k_out + kTile - 1) / kTile, row_tiles = (k_in + kTile - 1) / kTile;
-  const int64_t tiles = static_cast<int64_t>(col_tiles) * row_tiles;
-  const int64_t range = blockIdx.x / tiles, tile = blockIdx.x % tiles;
-  const int64_t m0 = tile / col_tiles * kTile, n0 = tile % col_tiles * kTile;
-  const int64_t k0 = range * per, k1 = min(rows, k0 + per);
-  const Operand<TA, TX, kPlain> a{X, X, 0}, a2{X2, X2, 0};
-  Zero<TA> c;
-  TA sum[4] = {0, 0, 0, 0}, none[4];
-  tile_product<TA, true, true, true>(a, B, m0, n0, k_in, k_out, k0, k1, as, bs, c.acc, sum);
-  if constexpr (kTwo) tile_product<TA, true, true, false>(a2, B2, m0, n0, k_in, k_out, k0, k1, as, bs, c.acc, none);
-  if (want_dw)
-    each_result<TA>(m0, n0, k_in, k_out, c.acc, [&](int64_t m, int64_t n, TA v) { dW[range * stride + m * k_out + n] = v; });
-  if (want_db && m0 == 0) {
-    const int t = threadIdx.x;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) sums[t / 16][(t % 16) * 4 + i] = sum[i];
+      for (int u = 0; u < 4; ++u) acc[0][u] = typename Mma<TA>::acc_t{0, 0, 0, 0};
+    }
     __syncthreads();
-    if (t < kTile && n0 + t < k_out) {
-      TA s = 0;
-      for (int i = 0; i < 16; ++i) s += sums[i][t];
-      db[range * stride + n0 + t] = s;
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int u = 0; u < 4; ++u) lds[((wave * 4 + r) * 4 + u) * kLanes + lane] = acc[0][u][r];
+    __syncthreads();
+    const int64_t row = row0 + Mma<TA>::row(lane, wave & 3);   // wave w < 4 finishes the lanes' result r = w
+    const int c = n0 + 4 * (lane & 15);
+    if (wave < 4 && row < rows && c < w.n_end) {
+      TA x[N > 0 ? N : 1][4], v[4] = {0, 0, 0, 0}, sum[4] = {0, 0, 0, 0};
+      if (bias) load4<kFours>(bias, c, w.n_end, v);
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (beside.m[e].p) load4<kFours>(beside.m[e].p + row * beside.m[e].ld, c, w.n_end, x[e]);
+      for (int p = 0; p < kN; ++p)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[i] += lds[((p * 4 + wave) * 4 + i) * kLanes + lane];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] += sum[i];
+      f(row, c, v, x);
+    }
+    __syncthreads();
+  }
+}
+
+// Calls f(first row, first column) for the tiles of this wave (kSplit: of the workgroup).
+template <int kRT, bool kSplit, typename F>
+__device__ __forceinline__ void each_tile(const Walk& walk, const Shape& shape, int64_t rows, int n_end, F&& f) {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
+  for (int64_t t = blockIdx.x; t < walk.count(); t += gridDim.x) {
+    int64_t rg;
+    int cg;
+    if (!walk.at(t, &rg, &cg)) continue;
+    const int64_t row0 = kSplit ? rg * 16 : (rg * shape.wr + wave / shape.wc) * (16 * kRT);
+    const int n0 = (kSplit ? cg : cg * shape.wc + wave % shape.wc) * kCols;
+    if (row0 < rows && n0 < n_end) f(row0, n0);
+  }
+}
+
+template <typename TS, typename TA, int kRT, bool kSplit, bool kFours>
+__global__ __launch_bounds__((threads<kSplit, TA>())) void forward_kernel(Walk walk, Shape shape, int64_t rows, Gate<TA> gate, int64_t ld_out,
+                                                                    Operand<TA, TS, kPlain> X, AlongRows<TA> W, const TA* __restrict__ bias,
+                                                                    const TS* __restrict__ residual, TS* __restrict__ Y,
+                                                                    TS* __restrict__ Z) {
+  __shared__ TA lds[lds_elements<kSplit, kRT, TA>()];
+  const int n_end = W.n_end;
+  const Beside<TS, 1> beside{{{residual, ld_out}}};
+  each_tile<kRT, kSplit>(walk, shape, rows, n_end, [&](int64_t row0, int n0) {
+    finish_rows<TA, kRT, kSplit, kFours>(X, W, row0, rows, n0, lds, bias, beside, [&](int64_t row, int c, const TA (&z)[4], const TA (&x)[1][4]) {
+      const int64_t at = row * ld_out;
+      TA y[4];
+      if (Z) store4<kFours>(Z + at, c, n_end, z);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[i] = z[i];
+      if (gate.on) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = gate.value(z[i]);
+      }
+      if (residual) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] += x[0][i];
+      }
+      store4<kFours>(Y + at, c, n_end, y);
+    });
+  });
+}
+
+// V = HX W, ddY = V act'(Z), S = V dY act''(Z).  Z NULL: no activation; S NULL: no curvature.
+template <typename TS, typename TA, int kRT, bool kSplit, bool kFours>
+__global__ __launch_bounds__((threads<kSplit, TA>())) void v_kernel(Walk walk, Shape shape, int64_t rows, Gate<TA> gate, int64_t ld_out,
+                                                              Operand<TA, TS, kPlain> HX, AlongRows<TA> W, const TS* __restrict__ Z,
+                                                              const TS* __restrict__ dY, TS* __restrict__ ddY, TA* __restrict__ S) {
+  __shared__ TA lds[lds_elements<kSplit, kRT, TA>()];
+  const int n_end = W.n_end;
+  const Beside<TS, 2> beside{{{Z, ld_out}, {S ? dY : nullptr, ld_out}}};
+  each_tile<kRT, kSplit>(walk, shape, rows, n_end, [&](int64_t row0, int n0) {
+    const TA* const none = nullptr;
+    finish_rows<TA, kRT, kSplit, kFours>(HX, W, row0, rows, n0, lds, none, beside, [&](int64_t row, int c, const TA (&v)[4], const TA (&x)[2][4]) {
+      TA out[4], s[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        TA first = TA(1), second = TA(0);
+        if (Z) gate.both(x[0][i], &first, &second);
+        out[i] = v[i] * first;
+        s[i] = v[i] * x[1][i] * second;
+      }
+      if (S) store4<kFours>(S + row * n_end, c, n_end, s);
+      store4<kFours>(ddY + row * ld_out, c, n_end, out);
+    });
+  });
+}
+
+// What a launch of the backward does: the rows in chunks, of each chunk first dx_groups workgroups of dX, then dw_groups of the chunk's partial dW and
+// db.  A chunk stays on one XCD and its two halves run at about the same time: the second reading of dY (and Z) comes from the caches.
+struct Plan {
+  int64_t rows, per;    // per: rows of a chunk, a multiple of 64
+  int64_t chunks;
+  int64_t dx_groups, dw_groups;   // workgroups of a chunk
+  int dx_col_groups, dw_col_groups;
+  Shape dx, dw;
+  int64_t stride;       // elements between the chunks' partial results
+};
+
+template <typename TA, int kRT, bool kSplit, bool kFours, typename TS, typename G, typename Weights>
+__device__ __forceinline__ void dx_role(const Plan& p, int64_t chunk, int64_t i, const G& g, const Weights& W, int64_t ld_in,
+                                        TS* __restrict__ dX, TA* lds) {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
+  const int64_t end = min(p.rows, (chunk + 1) * p.per);
+  const int64_t rg = i / p.dx_col_groups;
+  const int cg = static_cast<int>(i % p.dx_col_groups);
+  const int64_t row0 = chunk * p.per + (kSplit ? rg * 16 : (rg * p.dx.wr + wave / p.dx.wc) * (16 * kRT));
+  const int n0 = (kSplit ? cg : cg * p.dx.wc + wave % p.dx.wc) * kCols;
+  if (row0 >= end || n0 >= W.n_end) return;   // for kSplit the same in all waves
+  const TA* const none = nullptr;
+  finish_rows<TA, kRT, kSplit, kFours>(g, W, row0, end, n0, lds, none, Beside<TS, 0>{}, [&](int64_t row, int c, const TA (&v)[4], const TA (&)[1][4]) {
+    store4<kFours>(dX + row * ld_in, c, W.n_end, v);
+  });
+}
+
+// Partial dW of one 64 x 64 wc block: the chunk's rows are shared by dw.wr waves, joined in LDS in order.
+template <typename TA, bool kTwo, bool kFours, typename X, typename B, typename B2>
+__device__ __forceinline__ void dw_role(const Plan& p, int64_t chunk, int i, int k_in, int k_out, const X& x, const B& b, const X& x2,
+                                        const B2& b2, TA* __restrict__ dW, TA* __restrict__ db, TA* lds) {
+  const int lane = threadIdx.x & (kLanes - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
+  const int q = lane / 16, j = lane & 15;
+  const int wc = wave % p.dw.wc, wr = wave / p.dw.wc;
+  const int m0 = i / p.dw_col_groups * kCols, n0 = (i % p.dw_col_groups * p.dw.wc + wc) * kCols;
+  const int64_t begin = chunk * p.per, end = min(p.rows, begin + p.per);
+  const int64_t share = (p.per / p.dw.wr + 15) / 16 * 16;
+  const int64_t from = min(end, begin + wr * share), to = min(end, from + share);
+  typename Mma<TA>::acc_t acc[4][4];
+#pragma unroll
+  for (int t = 0; t < 4; ++t)
+#pragma unroll
+    for (int u = 0; u < 4; ++u) acc[t][u] = typename Mma<TA>::acc_t{0, 0, 0, 0};
+  TA sum[4] = {0, 0, 0, 0}, none[4];
+  if (n0 < k_out) {
+    outer_product<TA, kFours>(x, b, m0, k_in, n0, k_out, from, to, acc, sum);
+    if constexpr (kTwo) outer_product<TA, kFours>(x2, b2, m0, k_in, n0, k_out, from, to, acc, none);
+  }
+  TA* const to_dw = dW ? dW + chunk * p.stride : nullptr;
+  TA* const to_db = db && m0 == 0 ? db + chunk * p.stride : nullptr;
+  // column sums: over the four q of the wave, then over the waves
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    sum[u] += __shfl_xor(sum[u], 16);
+    sum[u] += __shfl_xor(sum[u], 32);
+  }
+  const int n = n0 + 4 * j;
+  if (p.dw.wr == 1) {
+    if (n0 >= k_out) return;
+    if (to_db && q == 0) store4<kFours>(to_db, n, k_out, sum);
+    if (to_dw) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int m = m0 + 4 * Mma<TA>::row(lane, r) + t;
+          const TA v[4] = {acc[t][0][r], acc[t][1][r], acc[t][2][r], acc[t][3][r]};
+          if (m < k_in && n < k_out) store4<kFours>(to_dw + static_cast<int64_t>(m) * k_out, n, k_out, v);
+        }
+    }
+    return;
+  }
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int u = 0; u < 4; ++u) lds[((wave * 4 + r) * 4 + u) * kLanes + lane] = acc[t][u][r];
+    __syncthreads();
+    if (to_dw && n < k_out) {
+      for (int r = wr; r < 4; r += p.dw.wr) {
+        const int m = m0 + 4 * Mma<TA>::row(lane, r) + t;
+        TA v[4] = {0, 0, 0, 0};
+        for (int w = 0; w < p.dw.wr; ++w)
+#pragma unroll
+          for (int u = 0; u < 4; ++u) v[u] += lds[(((w * p.dw.wc + wc) * 4 + r) * 4 + u) * kLanes + lane];
+        if (m < k_in) store4<kFours>(to_dw + static_cast<int64_t>(m) * k_out, n, k_out, v);
+      }
+    }
+  }
+  if (to_db) {
+    __syncthreads();
+    if (q == 0) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) lds[(wave * 4 + u) * 16 + j] = sum[u];
+    }
+    __syncthreads();
+    if (wr == 0 && q == 0 && n < k_out) {
+      TA v[4] = {0, 0, 0, 0};
+      for (int w = 0; w < p.dw.wr; ++w)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) v[u] += lds[((w * p.dw.wc + wc) * 4 + u) * 16 + j];
+      store4<kFours>(to_db, n, k_out, v);
     }
   }
 }
 
-// out[i] = sum over the ranges of part[range][i], in order: [0, n_dw) to dW, the rest to db.  No range at all: zeros.
+// G: the source of dX.  B, B2: those of dW (kTwo: the second-order pass, x2 B2 added to x B; the column sums are those of B).
+template <typename TS, typename TA, int kRT, bool kSplit, bool kFours, bool kTwo, typename G, typename B, typename B2, typename Weights>
+__global__ __launch_bounds__((threads<kSplit, TA>())) void backward_kernel(Plan p, int k_in, int k_out, int64_t ld_in, G g, Weights W,
+                                                                     TS* __restrict__ dX, Operand<TA, TS, kPlain> x, B b,
+                                                                     Operand<TA, TS, kPlain> x2, B2 b2, TA* __restrict__ dW,
+                                                                     TA* __restrict__ db) {
+  constexpr int kJoin = threads<kSplit, TA>() * 16, kRowsPart = lds_elements<kSplit, kRT, TA>();
+  __shared__ TA lds[kJoin > kRowsPart ? kJoin : kRowsPart];
+  const int64_t groups = p.dx_groups + p.dw_groups, total = (p.chunks + kXcds - 1) / kXcds * kXcds * groups;
+  for (int64_t t = blockIdx.x; t < total; t += gridDim.x) {
+    const int64_t local = t / kXcds, chunk = local / groups * kXcds + t % kXcds, i = local % groups;
+    if (chunk >= p.chunks) continue;
+    if (i < p.dx_groups)
+      dx_role<TA, kRT, kSplit, kFours>(p, chunk, i, g, W, ld_in, dX, lds);
+    else
+      dw_role<TA, kTwo, kFours>(p, chunk, static_cast<int>(i - p.dx_groups), k_in, k_out, x, b, x2, b2, dW, db, lds);
+    __syncthreads();   // LDS is the next tile's
+  }
+}
+
+// out[i] = sum over the chunks of part[chunk][i], each of 16 groups of lanes over a stretch of the chunks, joined in order: [0, n_dw) to
+// dW, the rest to db.  No chunk at all: zeros.
 template <typename TA>
-__global__ __launch_bounds__(kThreads) void sum_ranges_kernel(const TA* __restrict__ part, int64_t ranges, int64_t stride, int64_t n_dw,
+__global__ __launch_bounds__(kThreads) void sum_chunks_kernel(const TA* __restrict__ part, int64_t chunks, int64_t stride, int64_t n_dw,
                                                               int64_t n_db, TA* __restrict__ dW, TA* __restrict__ db) {
-  for (int64_t i = blockIdx.x * static_cast<int64_t>(kThreads) + threadIdx.x; i < n_dw + n_db; i += static_cast<int64_t>(gridDim.x) * kThreads) {
-    TA s = 0;
-    for (int64_t r = 0; r < ranges; ++r) s += part[r * stride + i];
-    if (i < n_dw) {
-      if (dW) dW[i] = s;
-    } else if (db) {
-      db[i - n_dw] = s;
+  constexpr int kGroups = 16, kAhead = 8;
+  __shared__ TA lds[kGroups][64];
+  const int group = threadIdx.x / 16, four = threadIdx.x % 16;
+  const int64_t per = (chunks + kGroups - 1) / kGroups, from = min(chunks, group * per), to = min(chunks, from + per);
+  const int64_t all = n_dw + n_db;
+  for (int64_t i0 = blockIdx.x * static_cast<int64_t>(64); i0 < all; i0 += static_cast<int64_t>(gridDim.x) * 64) {
+    const int64_t i = i0 + 4 * four;
+    const int cols = static_cast<int>(min(static_cast<int64_t>(64), all - i0));
+    TA s[4] = {0, 0, 0, 0};
+    if (i < all) {
+      for (int64_t c = from; c < to; c += kAhead) {
+        TA v[kAhead][4];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) load4<false>(part + min(c + k, to - 1) * stride + i0, 4 * four, cols, v[k]);
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+          if (c + k < to)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[e] += v[k][e];
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < 4; ++e) lds[group][4 * four + e] = s[e];
+    __syncthreads();
+    if (threadIdx.x < 64 && i0 + threadIdx.x < all) {
+      TA v = 0;
+      for (int k = 0; k < kGroups; ++k) v += lds[k][threadIdx.x];
+      const int64_t at = i0 + threadIdx.x;
+      if (at < n_dw) {
+        if (dW) dW[at] = v;
+      } else if (db) {
+        db[at - n_dw] = v;
+      }
     }
   }
+}
+
+// WT [k_out][k_in] = W transposed, 32 x 32 elements at a time through LDS.
+template <typename TA>
+__global__ __launch_bounds__(kThreads) void transpose_kernel(int k_in, int k_out, const TA* __restrict__ W, TA* __restrict__ WT) {
+  __shared__ TA tile[32][33];
+  const int across = (k_out + 31) / 32, r0 = blockIdx.x / across * 32, c0 = blockIdx.x % across * 32;
+  const int x = threadIdx.x % 32, y = threadIdx.x / 32;
+#pragma unroll
+  for (int i = 0; i < 32; i += kThreads / 32)
+    if (r0 + y + i < k_in && c0 + x < k_out) tile[y + i][x] = W[static_cast<int64_t>(r0 + y + i) * k_out + c0 + x];
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 32; i += kThreads / 32)
+    if (c0 + y + i < k_out && r0 + x < k_in) WT[static_cast<int64_t>(c0 + y + i) * k_in + r0 + x] = tile[x][y + i];
 }
 
 template <typename TS>
@@ -311,141 +384,209 @@ sc_status check_config(const char* fn, const dl_config* cfg, int64_t n) {
   return SC_OK;
 }
 
-int64_t tiles_of(int64_t n) { return (n + kTile - 1) / kTile; }
+int64_t blocks_of(int64_t n, int64_t size) { return (n + size - 1) / size; }
 
-// Rows per range of the dW launch: about four workgroups per CU together, no range below 256 rows.
-int64_t rows_per_range(const dl_config* c, int64_t n) {
-  const int64_t tiles = tiles_of(c->k_in) * tiles_of(c->k_out);
-  const int64_t ranges = std::max<int64_t>(1, 1024 / tiles);
-  const int64_t per = std::max<int64_t>(256, (n + ranges - 1) / ranges);
-  return (per + kDepth - 1) / kDepth * kDepth;
+// Waves side by side along the columns: as many as there are column blocks, up to four.
+Shape shape_of(int cols) {
+  const int64_t blocks = blocks_of(cols, kCols);
+  return blocks >= 3 ? Shape{4, 1} : blocks == 2 ? Shape{2, 2} : Shape{1, 4};
 }
 
-int64_t range_count(const dl_config* c, int64_t n) {
-  const int64_t per = rows_per_range(c, n);
-  return (n + per - 1) / per;
+// Row tiles of a wave: the fewer the rows the fewer, so that there are two waves for every SIMD of 256 CUs as long as possible.
+int row_tiles(int64_t rows, int cols, int most) {
+  const int64_t waves = blocks_of(rows, 16) * blocks_of(cols, kCols);
+  int rt = 1;
+  while (rt < most && waves / (2 * rt) >= 2048) rt *= 2;
+  return rt;
 }
 
-int64_t range_stride(const dl_config* c) { return static_cast<int64_t>(c->k_in) * c->k_out + c->k_out; }
+// Do all waves of a workgroup share one tile?  Where there is at most one row tile for every two SIMDs and the sum is long.
+bool split_sum(int64_t rows, int cols, int k) { return k >= 128 && blocks_of(rows, 16) * blocks_of(cols, kCols) <= 512; }
 
-// Workspace: [ S of the second-order pass ][ partial dW and db per range of rows ].
-size_t s_bytes(const dl_config* c, int64_t n) {
-  return c->activation == DL_NONE || c->activation == DL_RELU ? 0 : align_up(static_cast<size_t>(n) * c->k_out * weight_size(c), 256);
+Plan plan_of(const dl_config* c, int64_t n, bool want_dx, bool want_dw, bool split, int rt) {
+  const int split_waves = c->dtype == SC_F64 ? dl::split_waves<double>() : dl::split_waves<float>();
+  Plan p{};
+  p.rows = n;
+  p.dw = shape_of(c->k_out);
+  if (split) p.dw = {1, split_waves};
+  const int64_t blocks = blocks_of(c->k_in, kCols) * blocks_of(c->k_out, kCols);
+  // about 2048 waves of dW, none with less than 64 rows
+  const int64_t chunks = std::max<int64_t>(1, std::min(2048 / (blocks * p.dw.wr), n / (64 * p.dw.wr)));
+  p.per = blocks_of(n, chunks);
+  p.per = blocks_of(p.per, p.per < 256 ? 64 : 256) * (p.per < 256 ? 64 : 256);
+  p.chunks = blocks_of(n, p.per);
+  p.dx = split ? Shape{1, 1} : shape_of(c->k_in);
+  p.dx_col_groups = static_cast<int>(blocks_of(c->k_in, kCols * p.dx.wc));
+  p.dx_groups = want_dx ? blocks_of(p.per, split ? 16 : 16 * rt * p.dx.wr) * p.dx_col_groups : 0;
+  p.dw_col_groups = static_cast<int>(blocks_of(c->k_out, kCols * p.dw.wc));
+  p.dw_groups = want_dw ? blocks_of(c->k_in, kCols) * p.dw_col_groups : 0;
+  p.stride = static_cast<int64_t>(c->k_in) * c->k_out + c->k_out;
+  return p;
 }
+
+bool curved(const dl_config* c) { return c->activation == DL_SILU || c->activation == DL_GELU; }
+
+// Does dX take W transposed (a launch of its own, 2 us)?  Where the reading of W as it is, four times the accesses, would take longer.
+bool transposed(int64_t n, const dl_config* c, bool split) { return !split && n >= 4096; }
+
+size_t wt_bytes(int64_t n, const dl_config* c) {
+  return transposed(n, c, false) ? align_up(static_cast<size_t>(c->k_in) * c->k_out * weight_size(c), 256) : 0;
+}
+
+// Workspace: [ S of the second-order pass ][ W transposed ][ partial dW and db per chunk ].
+size_t s_bytes(const dl_config* c, int64_t n) { return curved(c) ? align_up(static_cast<size_t>(n) * c->k_out * weight_size(c), 256) : 0; }
 
 size_t workspace_bytes(const dl_config* c, int64_t n) {
   if (n == 0) return 256;
-  return s_bytes(c, n) + align_up(static_cast<size_t>(range_count(c, n)) * range_stride(c) * weight_size(c), 256) + 256;
+  size_t part = 0;
+  for (bool split : {false, true}) {
+    const Plan p = plan_of(c, n, true, true, split, 1);
+    part = std::max(part, static_cast<size_t>(p.chunks) * p.stride * weight_size(c));
+  }
+  return s_bytes(c, n) + wt_bytes(n, c) + align_up(part, 256) + 256;
 }
-
-template <typename T>
-Matrix<T> matrix(const void* p, int64_t ld) {
-  return {static_cast<const T*>(p), ld};
-}
-
-unsigned grid_of(int64_t n) { return static_cast<unsigned>(std::min<int64_t>(std::max<int64_t>(n, 1), 1 << 22)); }
 
 template <typename TS, typename TA>
 struct Calls {
   const dl_config* c;
   int64_t n;
   hipStream_t stream;
+  static constexpr int kMostTiles = sizeof(TA) == 8 ? 2 : 4;
+
+  template <typename T>
+  static Matrix<T> matrix(const void* p, int64_t ld) {
+    return {static_cast<const T*>(p), ld};
+  }
+  Operand<TA, TS, kPlain> rows_in(const void* X) const { return {matrix<TS>(X, ld_in(c)), {}, {}}; }
+  template <Source kSource>
+  Operand<TA, TS, kSource> g(const void* dY, const void* Z) const {
+    return {matrix<TS>(dY, ld_out(c)), matrix<TS>(Z, ld_out(c)), Gate<TA>::of(c->activation)};
+  }
+
+  // Launches a product of rows with W [k_in][k_out]: launch(row tiles, split, fours) with all three known at compile time.  Widths that are no
+  // multiple of four test every element and are bound by that: one row tile does for them.
+  template <typename F>
+  hipError_t by_shape(int cols, int k, F&& launch) const {
+    const std::integral_constant<int, 1> one{};
+    const std::true_type yes{};
+    const std::false_type no{};
+    const bool fours = c->k_in % 4 == 0 && c->k_out % 4 == 0, split = split_sum(n, cols, k);
+    if (!fours) return split ? launch(one, yes, no) : launch(one, no, no);
+    if (split) return launch(one, yes, yes);
+    const int rt = row_tiles(n, cols, kMostTiles);
+    if constexpr (kMostTiles == 4) {
+      if (rt == 4) return launch(std::integral_constant<int, 4>{}, no, yes);
+    }
+    if (rt >= 2) return launch(std::integral_constant<int, 2>{}, no, yes);
+    return launch(one, no, yes);
+  }
+
+  Walk walk_of(int rt, bool split, const Shape& shape) const {
+    if (split) return {blocks_of(n, 16), static_cast<int>(blocks_of(c->k_out, kCols))};
+    return {blocks_of(n, 16 * rt * shape.wr), static_cast<int>(blocks_of(c->k_out, kCols * shape.wc))};
+  }
+  static unsigned grid_of(int64_t groups) { return static_cast<unsigned>(std::min<int64_t>(groups, 1 << 22)); }
 
   hipError_t forward(const void* X, const void* W, const void* b, const void* residual, void* Y, void* Z) const {
-    const TileWalk walk{tiles_of(n), tiles_of(c->k_out)};
-    hipLaunchKernelGGL((forward_kernel<TS, TA>), dim3(grid_of(walk.count())), dim3(kThreads), 0, stream, walk, n, c->k_in, c->k_out,
-                       ld_out(c), c->activation, matrix<TS>(X, ld_in(c)), matrix<TA>(W, c->k_out), static_cast<const TA*>(b),
-                       static_cast<const TS*>(residual), static_cast<TS*>(Y), static_cast<TS*>(Z));
-    return hipGetLastError();
+    return by_shape(c->k_out, c->k_in, [&](auto rt, auto split, auto fours) {
+      const Shape shape = shape_of(c->k_out);
+      const Walk walk = walk_of(rt, split, shape);
+      hipLaunchKernelGGL((forward_kernel<TS, TA, rt.value, split.value, fours.value>), dim3(grid_of(walk.count())), dim3((threads<split.value, TA>())), 0, stream,
+                         walk, shape, n, Gate<TA>::of(c->activation), ld_out(c), rows_in(X),
+                         (AlongRows<TA>{static_cast<const TA*>(W), c->k_in, c->k_out}), static_cast<const TA*>(b),
+                         static_cast<const TS*>(residual), static_cast<TS*>(Y), static_cast<TS*>(Z));
+      return hipGetLastError();
+    });
   }
 
-  template <typename TG, Source kSource>
-  hipError_t dx(const Operand<TA, TG, kSource>& g, const void* W, void* dX) const {
-    const TileWalk walk{tiles_of(n), tiles_of(c->k_in)};
-    hipLaunchKernelGGL((dx_kernel<TS, TA, TG, kSource>), dim3(grid_of(walk.count())), dim3(kThreads), 0, stream, walk, n, c->k_in, c->k_out,
-                       ld_in(c), g, matrix<TA>(W, c->k_out), static_cast<TS*>(dX));
-    return hipGetLastError();
+  hipError_t v(const void* HX, const void* W, const void* Z, const void* dY, void* ddY, TA* S) const {
+    return by_shape(c->k_out, c->k_in, [&](auto rt, auto split, auto fours) {
+      const Shape shape = shape_of(c->k_out);
+      const Walk walk = walk_of(rt, split, shape);
+      hipLaunchKernelGGL((v_kernel<TS, TA, rt.value, split.value, fours.value>), dim3(grid_of(walk.count())), dim3((threads<split.value, TA>())), 0, stream, walk,
+                         shape, n, Gate<TA>::of(c->activation), ld_out(c), rows_in(HX), (AlongRows<TA>{static_cast<const TA*>(W), c->k_in, c->k_out}),
+                         c->activation == DL_NONE ? nullptr : static_cast<const TS*>(Z), static_cast<const TS*>(dY),
+                         static_cast<TS*>(ddY), S);
+      return hipGetLastError();
+    });
   }
 
-  template <bool kTwo, typename TB, Source kB, typename TB2, Source kB2>
-  hipError_t dw(const void* X, const Operand<TA, TB, kB>& B, const void* X2, const Operand<TA, TB2, kB2>& B2, void* dW, void* db,
-                void* partial) const {
-    const int64_t per = rows_per_range(c, n), ranges = range_count(c, n), stride = range_stride(c);
+  // ws: [ W transposed ][ partial results ].
+  template <bool kTwo, typename G, typename B, typename B2>
+  hipError_t gradients(const G& source, const void* W, void* dX, const void* X, const B& b, const void* X2, const B2& b2, void* dW,
+                       void* db, void* ws) const {
+    return by_shape(c->k_in, c->k_out, [&](auto rt, auto split, auto fours) {
+      const AlongColumns<TA> as_is{static_cast<const TA*>(W), c->k_out, c->k_in};
+      if constexpr (!split.value && fours.value) {
+        if (dX && transposed(n, c, split)) {
+          const int64_t tiles = blocks_of(c->k_in, 32) * blocks_of(c->k_out, 32);
+          hipLaunchKernelGGL((transpose_kernel<TA>), dim3(static_cast<unsigned>(tiles)), dim3(kThreads), 0, stream, c->k_in, c->k_out,
+                             static_cast<const TA*>(W), static_cast<TA*>(ws));
+          const hipError_t e = hipGetLastError();
+          if (e != hipSuccess) return e;
+          return gradients_with<kTwo>(rt, split, fours, source, AlongRows<TA>{static_cast<const TA*>(ws), c->k_out, c->k_in}, dX, X, b, X2,
+                                      b2, dW, db, ws);
+        }
+      }
+      return gradients_with<kTwo>(rt, split, fours, source, as_is, dX, X, b, X2, b2, dW, db, ws);
+    });
+  }
+
+  template <bool kTwo, typename RT, typename Split, typename Fours, typename G, typename Weights, typename B, typename B2>
+  hipError_t gradients_with(RT rt, Split split, Fours fours, const G& source, const Weights& w, void* dX, const void* X, const B& b,
+                            const void* X2, const B2& b2, void* dW, void* db, void* ws) const {
+    const Plan p = plan_of(c, n, dX != nullptr, dW || db, split, rt);
+    const bool whole = p.chunks == 1;
+    TA* part = reinterpret_cast<TA*>(static_cast<char*>(ws) + wt_bytes(n, c));
     const int64_t n_dw = static_cast<int64_t>(c->k_in) * c->k_out;
-    TA* part = static_cast<TA*>(partial);
-    TA* to_dw = ranges == 1 ? static_cast<TA*>(dW) : part;
-    TA* to_db = ranges == 1 ? static_cast<TA*>(db) : part + n_dw;
-    const int64_t tiles = (dW ? tiles_of(c->k_in) : 1) * tiles_of(c->k_out);
-    hipLaunchKernelGGL((dw_kernel<TA, TS, TB, kB, TB2, kB2, kTwo>), dim3(static_cast<unsigned>(tiles * ranges)), dim3(kThreads), 0, stream, n,
-                       per, dW ? c->k_in : std::min(c->k_in, kTile), c->k_out, dW != nullptr, db != nullptr, matrix<TS>(X, ld_in(c)), B,
-                       matrix<TS>(X2, ld_in(c)), B2, to_dw, to_db, stride);
+    TA* to_dw = !dW ? nullptr : whole ? static_cast<TA*>(dW) : part;
+    TA* to_db = !db ? nullptr : whole ? static_cast<TA*>(db) : part + n_dw;
+    const int64_t groups = blocks_of(p.chunks, kXcds) * kXcds * (p.dx_groups + p.dw_groups);
+    hipLaunchKernelGGL((backward_kernel<TS, TA, RT::value, Split::value, Fours::value, kTwo, G, B, B2, Weights>), dim3(grid_of(groups)),
+                       dim3((threads<Split::value, TA>())), 0, stream, p, c->k_in, c->k_out, ld_in(c), source, w, static_cast<TS*>(dX),
+                       rows_in(X), b, rows_in(X2), b2, to_dw, to_db);
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || ranges == 1) return e;
-    return sum_ranges(part, ranges, dW, db);
+    if (e != hipSuccess || whole || !(dW || db)) return e;
+    return sum_chunks(part, p.chunks, dW, db);
   }
 
-  hipError_t sum_ranges(const TA* part, int64_t ranges, void* dW, void* db) const {
+  hipError_t sum_chunks(const TA* part, int64_t chunks, void* dW, void* db) const {
     const int64_t n_dw = static_cast<int64_t>(c->k_in) * c->k_out;
-    hipLaunchKernelGGL((sum_ranges_kernel<TA>), dim3(grid_of(std::min<int64_t>((n_dw + c->k_out + kThreads - 1) / kThreads, 1 << 16))),
-                       dim3(kThreads), 0, stream, part, ranges, range_stride(c), n_dw, static_cast<int64_t>(c->k_out),
+    hipLaunchKernelGGL((sum_chunks_kernel<TA>), dim3(static_cast<unsigned>(std::min<int64_t>(blocks_of(n_dw + c->k_out, 64), 1 << 16))),
+                       dim3(kThreads), 0, stream, part, chunks, n_dw + c->k_out, n_dw, static_cast<int64_t>(c->k_out),
                        static_cast<TA*>(dW), static_cast<TA*>(db));
     return hipGetLastError();
   }
 
-  template <Source kSource>
-  Operand<TA, TS, kSource> g(const void* dY, const void* Z) const {
-    return {matrix<TS>(dY, ld_out(c)), matrix<TS>(Z, ld_out(c)), c->activation};
-  }
-
-  template <Source kSource>
-  hipError_t backward_as(const void* X, const void* W, const void* Z, const void* dY, void* dX, void* dW, void* db, void* ws) const {
-    const auto G = g<kSource>(dY, Z);
-    if (dX) {
-      const hipError_t e = dx(G, W, dX);
-      if (e != hipSuccess) return e;
-    }
-    return dW || db ? dw<false>(X, G, X, G, dW, db, ws) : hipSuccess;
-  }
-
   hipError_t backward(const void* X, const void* W, const void* Z, const void* dY, void* dX, void* dW, void* db, void* ws) const {
-    return c->activation == DL_NONE ? backward_as<kPlain>(X, W, Z, dY, dX, dW, db, ws) : backward_as<kGated>(X, W, Z, dY, dX, dW, db, ws);
+    if (c->activation == DL_NONE) return gradients<false>(g<kPlain>(dY, Z), W, dX, X, g<kPlain>(dY, Z), X, g<kPlain>(dY, Z), dW, db, ws);
+    return gradients<false>(g<kGated>(dY, Z), W, dX, X, g<kGated>(dY, Z), X, g<kGated>(dY, Z), dW, db, ws);
   }
 
   hipError_t zero_rows(void* p, int cols, int64_t ld) const {
     if (!p) return hipSuccess;
-    hipLaunchKernelGGL((zero_rows_kernel<TS>), dim3(grid_of(std::min<int64_t>((n * cols + kThreads - 1) / kThreads, 2048))), dim3(kThreads),
-                       0, stream, n, cols, ld, static_cast<TS*>(p));
+    hipLaunchKernelGGL((zero_rows_kernel<TS>), dim3(grid_of(std::min<int64_t>(blocks_of(n * cols, kThreads), 2048))), dim3(kThreads), 0, stream,
+                       n, cols, ld, static_cast<TS*>(p));
     return hipGetLastError();
   }
 
   hipError_t double_backward(const void* X, const void* W, const void* Z, const void* dY, const void* HX, void* ddY, void* X2, void* W2,
                              void* b2, void* ws) const {
-    const bool curved = s_bytes(c, n) != 0;
-    TA* S = curved ? static_cast<TA*>(ws) : nullptr;
+    TA* S = curved(c) ? static_cast<TA*>(ws) : nullptr;
     void* part = static_cast<char*>(ws) + s_bytes(c, n);
-    const TileWalk walk{tiles_of(n), tiles_of(c->k_out)};
-    hipLaunchKernelGGL((v_kernel<TS, TA>), dim3(grid_of(walk.count())), dim3(kThreads), 0, stream, walk, n, c->k_in, c->k_out, ld_out(c),
-                       c->activation, matrix<TS>(HX, ld_in(c)), matrix<TA>(W, c->k_out),
-                       c->activation == DL_NONE ? nullptr : static_cast<const TS*>(Z), static_cast<const TS*>(dY), static_cast<TS*>(ddY), S);
-    hipError_t e = hipGetLastError();
+    hipError_t e = v(HX, W, Z, dY, ddY, S);
     if (e != hipSuccess) return e;
-    if (!curved) {   // act'' = 0: W2 is dW of HX, X2 and b2 are zero
+    if (!S) {   // act'' = 0: W2 is dW of HX, X2 and b2 are zero
       e = zero_rows(X2, c->k_in, ld_in(c));
-      if (e != hipSuccess) return e;
-      if (b2) {
-        e = sum_ranges(nullptr, 0, nullptr, b2);
-        if (e != hipSuccess) return e;
-      }
-      if (!W2) return hipSuccess;
-      if (c->activation == DL_NONE) return dw<false>(HX, g<kPlain>(dY, Z), HX, g<kPlain>(dY, Z), W2, nullptr, part);
-      return dw<false>(HX, g<kGated>(dY, Z), HX, g<kGated>(dY, Z), W2, nullptr, part);
+      if (e == hipSuccess && b2) e = sum_chunks(nullptr, 0, nullptr, b2);
+      if (e != hipSuccess || !W2) return e;
+      if (c->activation == DL_NONE)
+        return gradients<false>(g<kPlain>(dY, Z), W, nullptr, HX, g<kPlain>(dY, Z), HX, g<kPlain>(dY, Z), W2, nullptr, part);
+      return gradients<false>(g<kGated>(dY, Z), W, nullptr, HX, g<kGated>(dY, Z), HX, g<kGated>(dY, Z), W2, nullptr, part);
     }
-    const Operand<TA, TA, kPlain> s{matrix<TA>(S, c->k_out), matrix<TA>(S, c->k_out), 0};
-    if (X2) {
-      e = dx(s, W, X2);
-      if (e != hipSuccess) return e;
-    }
-    return W2 || b2 ? dw<true>(X, s, HX, g<kGated>(dY, Z), W2, b2, part) : hipSuccess;
+    if (!X2 && !W2 && !b2) return hipSuccess;
+    const Operand<TA, TA, kPlain> s{{S, c->k_out}, {}, {}};
+    return gradients<true>(s, W, X2, X, s, HX, g<kGated>(dY, Z), W2, b2, part);
   }
 };
 
@@ -522,7 +663,7 @@ sc_status dl_backward(const dl_config* cfg, int64_t n_rows, const void* X, const
   DeviceGuard guard(cfg->device);
   if (!guard.ok) return set_error(SC_ERR_HIP, "dl_backward: cannot make cfg->device current");
   return launched("dl_backward", by_type(cfg, n_rows, static_cast<hipStream_t>(hip_stream), [&](const auto& calls) {
-                    if (n_rows == 0) return dW || db ? calls.sum_ranges(nullptr, 0, dW, db) : hipSuccess;
+                    if (n_rows == 0) return dW || db ? calls.sum_chunks(nullptr, 0, dW, db) : hipSuccess;
                     return calls.backward(X, W, Z, dY, dX, dW, db, workspace);
                   }));
 }
@@ -544,7 +685,7 @@ sc_status dl_double_backward(const dl_config* cfg, int64_t n_rows, const void* X
   DeviceGuard guard(cfg->device);
   if (!guard.ok) return set_error(SC_ERR_HIP, "dl_double_backward: cannot make cfg->device current");
   return launched("dl_double_backward", by_type(cfg, n_rows, static_cast<hipStream_t>(hip_stream), [&](const auto& calls) {
-                    if (n_rows == 0) return W2 || b2 ? calls.sum_ranges(nullptr, 0, W2, b2) : hipSuccess;
+                    if (n_rows == 0) return W2 || b2 ? calls.sum_chunks(nullptr, 0, W2, b2) : hipSuccess;
                     return calls.double_backward(X, W, Z, dY, HX, ddY, X2, W2, b2, workspace);
                   }));
 }

@@ -31,9 +31,9 @@ constexpr int kWaves = kThreads / kLanes;
 constexpr int kDigitBits = 10;
 constexpr int kBins = 1 << kDigitBits;
 constexpr int kSortBlocks = 256;     // most workgroups of a sort pass
-constexpr int kSortChunk = 2048;     // rows of a workgroup below that
-constexpr int kPiece = 64;           // sorted rows a wave sums
-constexpr int kAhead = 8;            // rows requested before the first of them is used
+constexpr int kSortChunk = 1024;     // rows of a workgroup below that
+constexpr int kPiece = 32;           // sorted rows a wave sums
+constexpr int kAhead = 8;            // rows (or slots) requested at a time
 
 template <typename T, int N>
 struct Vec {
@@ -91,13 +91,27 @@ struct Sort {
 __device__ __forceinline__ int row_at(const Sort& s, int64_t i) { return s.order ? s.order[i] : static_cast<int>(i); }
 __device__ __forceinline__ int digit_of(const Sort& s, int row) { return (key_of(s.z[row], s.elements) >> s.shift) & (kBins - 1); }
 
+// Adds the digits of rows i, i + step, .. below end to bin (whole numbers: any order); four requests at a time.
+__device__ __forceinline__ void count_digits(const Sort& s, int64_t i, int64_t end, int step, int* bin) {
+  for (; i < end; i += 4 * step) {
+    int row[4], digit[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) row[k] = row_at(s, min(i + k * step, end - 1));
+#pragma unroll
+    for (int k = 0; k < 4; ++k) digit[k] = digit_of(s, row[k]);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (i + k * step < end) atomicAdd(&bin[digit[k]], 1);
+  }
+}
+
 // counts[block][bin]; on the way first[element] = -1 (no row yet).
 __global__ __launch_bounds__(kThreads) void count_kernel(Sort s, int* __restrict__ counts, int* __restrict__ first) {
   __shared__ int bin[kBins];
   for (int i = threadIdx.x; i < s.bins; i += kThreads) bin[i] = 0;
   __syncthreads();
   const int64_t begin = blockIdx.x * s.per_block, end = min(s.n, begin + s.per_block);
-  for (int64_t i = begin + threadIdx.x; i < end; i += kThreads) atomicAdd(&bin[digit_of(s, row_at(s, i))], 1);   // whole numbers: any order
+  count_digits(s, begin + threadIdx.x, end, kThreads, bin);
   __syncthreads();
   for (int i = threadIdx.x; i < s.bins; i += kThreads) counts[blockIdx.x * static_cast<int64_t>(s.bins) + i] = bin[i];
   if (first)
@@ -107,6 +121,7 @@ __global__ __launch_bounds__(kThreads) void count_kernel(Sort s, int* __restrict
 // Rows to their places: bins in order, inside a bin the order of the pass before.
 __global__ __launch_bounds__(kThreads) void scatter_kernel(Sort s, int blocks, const int* __restrict__ counts, int* __restrict__ out) {
   __shared__ int place[kWaves][kBins];   // next place of each bin for each wave
+  __shared__ int4 all[kThreads], earlier[kThreads];   // of four bins, over a share of the workgroups
   __shared__ int wave_total[kWaves];
   const int lane = threadIdx.x & (kLanes - 1), wave = threadIdx.x / kLanes;
   const int64_t begin = blockIdx.x * s.per_block, end = min(s.n, begin + s.per_block);
@@ -114,26 +129,42 @@ __global__ __launch_bounds__(kThreads) void scatter_kernel(Sort s, int blocks, c
   const int64_t w0 = min(end, begin + wave * per_wave), w1 = min(end, w0 + per_wave);
   for (int i = threadIdx.x; i < kWaves * kBins; i += kThreads) (&place[0][0])[i] = 0;
   __syncthreads();
-  for (int64_t i = w0 + lane; i < w1; i += kLanes) atomicAdd(&place[wave][digit_of(s, row_at(s, i))], 1);
-  __syncthreads();
-  // bins 4 t .. 4 t + 3 of thread t: all rows of the bin, and those of earlier workgroups
-  constexpr int kOwn = kBins / kThreads;
-  int total[kOwn] = {}, before[kOwn] = {};
-  const int b0 = threadIdx.x * kOwn;
-  if (b0 < s.bins) {
-    for (int b = 0; b < blocks; ++b) {
-      const int* row = counts + b * static_cast<int64_t>(s.bins) + b0;
+  count_digits(s, w0 + lane, w1, kLanes, place[wave]);
+  // four bins a thread (the bins are a multiple of four), the workgroups shared by kThreads / width groups of threads
+  const int quads = s.bins / 4;
+  int width = 1;
+  while (width < quads) width *= 2;
+  const int group = threadIdx.x / width, quad = threadIdx.x % width, groups = kThreads / width;
+  int4 sum = {0, 0, 0, 0}, part = {0, 0, 0, 0};
+  if (quad < quads) {
+    const int per = (blocks + groups - 1) / groups, b0 = group * per, b1 = min(blocks, b0 + per);
+    for (int b = b0; b < b1; b += kAhead) {
+      int4 v[kAhead];
 #pragma unroll
-      for (int k = 0; k < kOwn; ++k) {
-        const int v = b0 + k < s.bins ? row[k] : 0;
-        total[k] += v;
-        before[k] += b < static_cast<int>(blockIdx.x) ? v : 0;
-      }
+      for (int k = 0; k < kAhead; ++k)
+        v[k] = reinterpret_cast<const int4*>(counts + min(b + k, b1 - 1) * static_cast<int64_t>(s.bins))[quad];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k)
+        if (b + k < b1) {
+          sum.x += v[k].x, sum.y += v[k].y, sum.z += v[k].z, sum.w += v[k].w;
+          if (b + k < static_cast<int>(blockIdx.x)) part.x += v[k].x, part.y += v[k].y, part.z += v[k].z, part.w += v[k].w;
+        }
     }
   }
-  int mine = 0;
-#pragma unroll
-  for (int k = 0; k < kOwn; ++k) mine += total[k];
+  all[threadIdx.x] = sum;
+  earlier[threadIdx.x] = part;
+  __syncthreads();
+  // thread t: bins 4 t .. 4 t + 3
+  constexpr int kOwn = 4;
+  int total[kOwn] = {}, before[kOwn] = {};
+  const int b0 = threadIdx.x * kOwn;
+  if (b0 < s.bins)
+    for (int g = 0; g < groups; ++g) {
+      const int4 a = all[g * width + threadIdx.x], e = earlier[g * width + threadIdx.x];
+      total[0] += a.x, total[1] += a.y, total[2] += a.z, total[3] += a.w;
+      before[0] += e.x, before[1] += e.y, before[2] += e.z, before[3] += e.w;
+    }
+  const int mine = total[0] + total[1] + total[2] + total[3];
   int up = mine;   // inclusive sum over the lanes
 #pragma unroll
   for (int d = 1; d < kLanes; d *= 2) {
@@ -144,25 +175,29 @@ __global__ __launch_bounds__(kThreads) void scatter_kernel(Sort s, int blocks, c
   __syncthreads();
   int at = up - mine;
   for (int w = 0; w < wave; ++w) at += wave_total[w];
+  if (b0 < s.bins) {
 #pragma unroll
-  for (int k = 0; k < kOwn; ++k) {
-    if (b0 + k < s.bins) {
+    for (int k = 0; k < kOwn; ++k) {
       int next = at + before[k];
       for (int w = 0; w < kWaves; ++w) {
         const int c = place[w][b0 + k];
         place[w][b0 + k] = next;
         next += c;
       }
+      at += total[k];
     }
-    at += total[k];
   }
   __syncthreads();
   // 64 rows at a time: a row's rank among the earlier lanes with the same bin, then the first of them moves the bin on
   volatile int* const next = place[wave];
+  int row = w0 < w1 ? row_at(s, min(w0 + lane, w1 - 1)) : 0, d = w0 < w1 ? digit_of(s, row) : 0;
   for (int64_t i = w0; i < w1; i += kLanes) {
     const bool live = i + lane < w1;
-    const int row = live ? row_at(s, i + lane) : 0;
-    const int d = live ? digit_of(s, row) : 0;
+    int row_next = 0, d_next = 0;
+    if (i + kLanes < w1) {
+      row_next = row_at(s, min(i + kLanes + lane, w1 - 1));
+      d_next = digit_of(s, row_next);
+    }
     unsigned long long same = __ballot(live);
 #pragma unroll
     for (int bit = 0; bit < kDigitBits; ++bit) {
@@ -178,6 +213,8 @@ __global__ __launch_bounds__(kThreads) void scatter_kernel(Sort s, int blocks, c
     __builtin_amdgcn_wave_barrier();   // every lane has read the place before it moves
     if (live && below == 0) next[d] = start + __popcll(same);
     __builtin_amdgcn_wave_barrier();
+    row = row_next;
+    d = d_next;
   }
 }
 
@@ -214,7 +251,7 @@ __global__ __launch_bounds__(kThreads) void piece_kernel(int64_t n, int64_t piec
   const bool live = c < channels;
   const int64_t p0 = piece * kPiece;
   const int count = static_cast<int>(min(static_cast<int64_t>(kPiece), n - p0));
-  static_assert(kPiece == kLanes, "a lane holds the row and the key of one position");
+  static_assert(kPiece <= kLanes, "a lane holds the row and the key of one position");
   const int row = lane < count ? order[p0 + lane] : 0;
   const int key = lane < count ? key_of(z[row], elements) : -1;
   const int before = p0 > 0 ? key_of(z[order[p0 - 1]], elements) : -1;             // keys of the neighbouring positions
@@ -227,14 +264,21 @@ __global__ __launch_bounds__(kThreads) void piece_kernel(int64_t n, int64_t piec
   }
   const unsigned long long ends = __ballot(lane < count && right != key || lane == count - 1);   // last positions of the runs of this piece
   TA acc[V] = {};
-  typename R::VS v[kAhead];
-  int run_start = 0;
-  for (int i = 0; i < count; i += kAhead) {
+  typename R::VS next[kAhead];
+  auto request = [&](int i) {
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
       const int r = __builtin_amdgcn_readlane(row, min(i + k, count - 1));
-      if (live) v[k] = *reinterpret_cast<const typename R::VS*>(dY + static_cast<int64_t>(r) * channels + c);
+      if (live) next[k] = *reinterpret_cast<const typename R::VS*>(dY + static_cast<int64_t>(r) * channels + c);
     }
+  };
+  int run_start = 0;
+  request(0);
+  for (int i = 0; i < count; i += kAhead) {
+    typename R::VS v[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) v[k] = next[k];
+    if (i + kAhead < count) request(i + kAhead);
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
       if (i + k >= count) break;
@@ -255,9 +299,10 @@ __global__ __launch_bounds__(kThreads) void piece_kernel(int64_t n, int64_t piec
   }
 }
 
-// Rows of dT whose rows span pieces, and those of absent elements.  A wave per element (four elements a workgroup); spans longer than
-// kLongSpan pieces are shared by the four waves.
+// Rows of dT whose rows span pieces, and those of absent elements.  A workgroup has `own` elements: kWaves of a long table, each a wave's, or
+// one of a table with fewer elements than the chip has places for workgroups.  Spans from kLongSpan pieces on are shared by all waves.
 constexpr int kLongSpan = 16;
+constexpr int kShortTable = 2048;
 
 template <typename TA, int V>
 __device__ __forceinline__ void add_slots(const TA* __restrict__ slots, int64_t p0, int64_t from, int64_t to, int channels, int c, TA (&acc)[V]) {
@@ -278,13 +323,13 @@ __device__ __forceinline__ void add_slots(const TA* __restrict__ slots, int64_t 
 }
 
 template <typename TA, int V>
-__global__ __launch_bounds__(kThreads) void join_kernel(int channels, int elements, TA scale, const TA* __restrict__ slots,
+__global__ __launch_bounds__(kThreads) void join_kernel(int own, int channels, int elements, TA scale, const TA* __restrict__ slots,
                                                         const int* __restrict__ first, const int* __restrict__ last, TA* __restrict__ dT) {
   typedef Row<TA, TA, V> R;
   __shared__ TA part[kWaves][kLanes * V];
   const int lane = threadIdx.x & (kLanes - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
-  for (int64_t e0 = static_cast<int64_t>(blockIdx.x) * kWaves; e0 < elements; e0 += static_cast<int64_t>(gridDim.x) * kWaves) {
-    for (int w = 0; w < kWaves; ++w) {
+  for (int64_t e0 = static_cast<int64_t>(blockIdx.x) * own; e0 < elements; e0 += static_cast<int64_t>(gridDim.x) * own) {
+    for (int w = 0; w < own; ++w) {
       const int64_t e = e0 + w;
       if (e >= elements) break;
       const int a = first[e];
@@ -370,7 +415,8 @@ int64_t sort_rows_per_block(int64_t n) {
 int sort_passes(const ee_config* c) { return c->num_elements < kBins ? 1 : 2; }
 int sort_bins(const ee_config* c, int pass) {
   const int keys = c->num_elements + 1;
-  return sort_passes(c) == 1 ? keys : pass == 0 ? kBins : (keys - 1) / kBins + 1;
+  const int bins = sort_passes(c) == 1 ? keys : pass == 0 ? kBins : (keys - 1) / kBins + 1;
+  return (bins + 3) / 4 * 4;
 }
 
 struct Workspace {
@@ -394,7 +440,7 @@ Workspace carve(const ee_config* c, int64_t n, void* base) {
     w.counts = static_cast<int*>(take(blocks * kBins * 4));
     w.first = static_cast<int*>(take(static_cast<size_t>(c->num_elements) * 4));
     w.last = static_cast<int*>(take(static_cast<size_t>(c->num_elements) * 4));
-    w.slots = take((n + kPiece - 1) / kPiece * 2 * c->num_channels * table_size(c));
+    w.slots = take(static_cast<size_t>((n + kPiece - 1) / kPiece) * 2 * c->num_channels * table_size(c));
   }
   w.bytes = at + 256;
   return w;
@@ -462,7 +508,8 @@ struct Calls {
                        w.last);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((join_kernel<TA, V>), dim3(blocks_of(elements)), dim3(kThreads), 0, stream, k, elements, scale,
+    const int own = elements <= kShortTable ? 1 : kWaves;
+    hipLaunchKernelGGL((join_kernel<TA, V>), dim3((elements + own - 1) / own), dim3(kThreads), 0, stream, own, k, elements, scale,
                        static_cast<const TA*>(w.slots), w.first, w.last, static_cast<TA*>(dT));
     return hipGetLastError();
   }
