@@ -14,7 +14,7 @@
 #include <string>
 #include <type_traits>
 
-#include "dl_product.h"
+#include "dl_parts.h"
 
 namespace dl {
 namespace {
@@ -53,6 +53,25 @@ struct Walk {
     return *row < row_groups;
   }
 };
+
+// Parts of the operands on the bfloat16 matrix cores (dl_parts.h): of X, of W, of the source of dX and of that of dW.
+template <typename TS>
+struct PartCount {
+  static constexpr int x = sizeof(TS) == 2 ? 1 : 3, w = sizeof(TS) == 2 ? 2 : 3;
+  template <typename T, Source kSource>
+  static constexpr int dx(const Operand<float, T, kSource>*) { return sizeof(TS) != 2 ? 3 : sizeof(T) == 2 && kSource == kPlain ? 1 : 2; }
+  template <typename T, Source kSource>
+  static constexpr int dw(const Operand<float, T, kSource>*) { return sizeof(T) == 2 && kSource == kPlain ? 1 : 3; }
+  // fp64: no parts
+  template <typename T, Source kSource>
+  static constexpr int dx(const Operand<double, T, kSource>*) { return 0; }
+  template <typename T, Source kSource>
+  static constexpr int dw(const Operand<double, T, kSource>*) { return 0; }
+};
+template <int kParts, typename T, Source kSource>
+__device__ __forceinline__ PartsRows<T, kSource, kParts> as_rows(const Operand<float, T, kSource>& o) { return {o}; }
+template <int kParts, typename T, Source kSource>
+__device__ __forceinline__ PartsColumns<T, kSource, kParts> as_columns(const Operand<float, T, kSource>& o) { return {o}; }
 
 // The results of 16 kRT rows and 64 columns, by this wave alone or (kSplit) by all waves of the workgroup, each over its part of the reduced
 // index, joined in LDS in the order of the waves.  f as in each_four.
@@ -115,57 +134,137 @@ __device__ __forceinline__ void each_tile(const Walk& walk, const Shape& shape, 
   }
 }
 
-template <typename TS, typename TA, int kRT, bool kSplit, bool kFours>
-__global__ __launch_bounds__((threads<kSplit, TA>())) void forward_kernel(Walk walk, Shape shape, int64_t rows, Gate<TA> gate, int64_t ld_out,
-                                                                    Operand<TA, TS, kPlain> X, AlongRows<TA> W, const TA* __restrict__ bias,
-                                                                    const TS* __restrict__ residual, TS* __restrict__ Y,
-                                                                    TS* __restrict__ Z) {
+// What becomes of four neighbouring results v of a row.  The constructor takes what is the same for a lane's column.
+template <typename TS, typename TA, bool kFours>
+struct ForwardEnd {   // Z = v (bias added), Y = act(Z) + residual
+  Gate<TA> gate;
+  int64_t ld_out;
+  int n_end;
+  const TS* residual;
+  TS *Y, *Z;
+  __device__ __forceinline__ Beside<TS, 1> beside() const { return {{{residual, ld_out}}}; }
+  __device__ __forceinline__ void operator()(int64_t row, int c, const TA (&z)[4], const TA (&x)[1][4]) const {
+    const int64_t at = row * ld_out;
+    TA y[4];
+    if (Z) store4<kFours>(Z + at, c, n_end, z);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = z[i];
+    if (gate.on) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[i] = gate.value(z[i]);
+    }
+    if (residual) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[i] += x[0][i];
+    }
+    store4<kFours>(Y + at, c, n_end, y);
+  }
+};
+
+template <typename TS, typename TA, bool kFours>
+struct SecondEnd {   // v = V: ddY = V act'(Z), S = V dY act''(Z).  Z NULL: no activation; S NULL: no curvature
+  Gate<TA> gate;
+  int64_t ld_out;
+  int n_end;
+  const TS *Z, *dY;
+  TS* ddY;
+  TA* S;
+  __device__ __forceinline__ Beside<TS, 2> beside() const { return {{{Z, ld_out}, {S ? dY : nullptr, ld_out}}}; }
+  __device__ __forceinline__ void operator()(int64_t row, int c, const TA (&v)[4], const TA (&x)[2][4]) const {
+    TA out[4], s[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      TA first = TA(1), second = TA(0);
+      if (Z) gate.both(x[0][i], &first, &second);
+      out[i] = v[i] * first;
+      s[i] = v[i] * x[1][i] * second;
+    }
+    if (S) store4<kFours>(S + row * n_end, c, n_end, s);
+    store4<kFours>(ddY + row * ld_out, c, n_end, out);
+  }
+};
+
+template <typename TS, typename TA, bool kFours>
+struct StoreEnd {
+  int64_t ld;
+  int n_end;
+  TS* out;
+  __device__ __forceinline__ Beside<TS, 0> beside() const { return {}; }
+  __device__ __forceinline__ void operator()(int64_t row, int c, const TA (&v)[4], const TA (&)[1][4]) const { store4<kFours>(out + row * ld, c, n_end, v); }
+};
+
+// Forward and V: rows x W.
+template <typename TS, typename TA, int kRT, bool kSplit, bool kFours, typename End>
+__global__ __launch_bounds__((threads<kSplit, TA>())) void rows_kernel(Walk walk, Shape shape, int64_t rows, Operand<TA, TS, kPlain> X, AlongRows<TA> W,
+                                                                       const TA* __restrict__ bias, End end) {
   __shared__ TA lds[lds_elements<kSplit, kRT, TA>()];
-  const int n_end = W.n_end;
-  const Beside<TS, 1> beside{{{residual, ld_out}}};
-  each_tile<kRT, kSplit>(walk, shape, rows, n_end, [&](int64_t row0, int n0) {
-    finish_rows<TA, kRT, kSplit, kFours>(X, W, row0, rows, n0, lds, bias, beside, [&](int64_t row, int c, const TA (&z)[4], const TA (&x)[1][4]) {
-      const int64_t at = row * ld_out;
-      TA y[4];
-      if (Z) store4<kFours>(Z + at, c, n_end, z);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) y[i] = z[i];
-      if (gate.on) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) y[i] = gate.value(z[i]);
-      }
-      if (residual) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) y[i] += x[0][i];
-      }
-      store4<kFours>(Y + at, c, n_end, y);
-    });
+  each_tile<kRT, kSplit>(walk, shape, rows, W.n_end, [&](int64_t row0, int n0) {
+    finish_rows<TA, kRT, kSplit, kFours>(X, W, row0, rows, n0, lds, bias, end.beside(), end);
   });
 }
 
-// V = HX W, ddY = V act'(Z), S = V dY act''(Z).  Z NULL: no activation; S NULL: no curvature.
-template <typename TS, typename TA, int kRT, bool kSplit, bool kFours>
-__global__ __launch_bounds__((threads<kSplit, TA>())) void v_kernel(Walk walk, Shape shape, int64_t rows, Gate<TA> gate, int64_t ld_out,
-                                                              Operand<TA, TS, kPlain> HX, AlongRows<TA> W, const TS* __restrict__ Z,
-                                                              const TS* __restrict__ dY, TS* __restrict__ ddY, TA* __restrict__ S) {
-  __shared__ TA lds[lds_elements<kSplit, kRT, TA>()];
-  const int n_end = W.n_end;
-  const Beside<TS, 2> beside{{{Z, ld_out}, {S ? dY : nullptr, ld_out}}};
-  each_tile<kRT, kSplit>(walk, shape, rows, n_end, [&](int64_t row0, int n0) {
-    const TA* const none = nullptr;
-    finish_rows<TA, kRT, kSplit, kFours>(HX, W, row0, rows, n0, lds, none, beside, [&](int64_t row, int c, const TA (&v)[4], const TA (&x)[2][4]) {
-      TA out[4], s[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        TA first = TA(1), second = TA(0);
-        if (Z) gate.both(x[0][i], &first, &second);
-        out[i] = v[i] * first;
-        s[i] = v[i] * x[1][i] * second;
-      }
-      if (S) store4<kFours>(S + row * n_end, c, n_end, s);
-      store4<kFours>(ddY + row * ld_out, c, n_end, out);
-    });
-  });
+// Parts of the operands on the bfloat16 matrix cores (dl_parts.h): of X, of W, of the source of dX and of that of dW.
+constexpr int kPartsTiles = 4;   // row tiles of a wave
+template <int kX, int kW>
+constexpr int rows_words() { return kWaves * kPartsTiles * kX * kPlane + shared_words<kW>(); }
+
+// The results of 64 kWaves rows from row0 and of 64 columns by a workgroup.
+template <int kX, int kW, typename Rows, typename T, int N, typename F>
+__device__ __forceinline__ void finish_rows_parts(const Rows& a, const AlongRows<float>& w, int64_t row0, int64_t rows, int n0, unsigned* lds,
+                                                  const float* __restrict__ bias, const Beside<T, N>& beside, F&& f) {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
+  Acc acc[kPartsTiles][4];
+  unsigned* const planes = lds + wave * (kPartsTiles * kX * kPlane);
+  const Operand<float, float, kPlain> matrix{{w.W, w.n_end}, {}, {}};
+  const int64_t first = row0 + wave * (16 * kPartsTiles);
+  if (!rows_parts<kPartsTiles, kX, kW>(as_rows<kX>(a), SharedColumns<float, kPlain, kW>{matrix}, first, rows, n0, w.n_end, w.k_end, planes,
+                                       lds + kWaves * kPartsTiles * kX * kPlane, acc))
+    rows_product<float, kPartsTiles, true>(a, w, first, rows, n0, 0, w.k_end, reinterpret_cast<float*>(planes), acc);
+  each_four<float, kPartsTiles, true>(first, rows, n0, w.n_end, acc, bias, beside, f);
+}
+
+template <typename TS, typename End>
+__global__ __launch_bounds__(kThreads, 2) void parts_rows_kernel(Walk walk, int64_t rows, Operand<float, TS, kPlain> X, AlongRows<float> W,
+                                                                 const float* __restrict__ bias, End end) {
+  constexpr int kX = PartCount<TS>::x, kW = PartCount<TS>::w;
+  __shared__ unsigned lds[rows_words<kX, kW>()];
+  for (int64_t t = blockIdx.x; t < walk.count(); t += gridDim.x) {
+    int64_t rg;
+    int cg;
+    if (!walk.at(t, &rg, &cg)) continue;
+    finish_rows_parts<kX, kW>(X, W, rg * (16 * kPartsTiles * kWaves), rows, cg * kCols, lds, bias, end.beside(), end);
+    __syncthreads();
+  }
+}
+
+// A product of rows with a matrix of at most 32 kRounds reduced indices that the waves keep (dl_parts.h).  Weights: W in place (forward, V) or
+// transposed (dX), with the same matrix for the fp32 instruction; kX: parts of the rows.
+template <typename TS, int kRounds, int kX, typename Rows, typename Weights, typename Plain, typename End>
+__global__ __launch_bounds__(kThreads, 2) void kept_kernel(Walk walk, Shape shape, int64_t rows, Rows from, Weights weights, Plain plain,
+                                                           const float* __restrict__ bias, End end) {
+  constexpr int kW = PartCount<TS>::w;
+  constexpr int kLds = kWaves * kRounds * kX * kPlane;
+  __shared__ float lds[kLds];
+  static_assert(kRounds * kX * kPlane >= Corner<float>::kBlock, "room for the fp32 product");
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes), lane = threadIdx.x & (kLanes - 1);
+  int64_t rg;
+  int cg;
+  if (!walk.at(blockIdx.x, &rg, &cg)) return;
+  const int n0 = (cg * shape.wc + wave % shape.wc) * kCols, n_end = plain.n_end, k_end = plain.k_end;
+  if (n0 >= n_end) return;
+  float* const corner = lds + wave * (kRounds * kX * kPlane);
+  Kept<kRounds, kW> kept;
+  keep(weights, n0, n_end, k_end, kept);
+  float b[4] = {0, 0, 0, 0};
+  if (bias) load4<true>(bias, n0 + 4 * (lane & 15), n_end, b);
+  walk_rows<kRounds, kX, kW>(
+      as_rows<kX>(from), kept, rg * shape.wr + wave / shape.wc, walk.row_groups * shape.wr, rows, n0, n_end, k_end,
+      reinterpret_cast<unsigned*>(corner), end.beside(),
+      [&](int64_t row0, Acc(&acc)[1][4]) { rows_product<float, 1, true>(from, plain, row0, rows, n0, 0, k_end, corner, acc); },
+      [&](int64_t row, int c, const float(&v)[4], const auto& x) {
+        const float z[4] = {v[0] + b[0], v[1] + b[1], v[2] + b[2], v[3] + b[3]};
+        end(row, c, z, x);
+      });
 }
 
 // What a launch of the backward does: the rows in chunks, of each chunk first dx_groups workgroups of dX, then dw_groups of the chunk's partial dW and
@@ -190,9 +289,7 @@ __device__ __forceinline__ void dx_role(const Plan& p, int64_t chunk, int64_t i,
   const int n0 = (kSplit ? cg : cg * p.dx.wc + wave % p.dx.wc) * kCols;
   if (row0 >= end || n0 >= W.n_end) return;   // for kSplit the same in all waves
   const TA* const none = nullptr;
-  finish_rows<TA, kRT, kSplit, kFours>(g, W, row0, end, n0, lds, none, Beside<TS, 0>{}, [&](int64_t row, int c, const TA (&v)[4], const TA (&)[1][4]) {
-    store4<kFours>(dX + row * ld_in, c, W.n_end, v);
-  });
+  finish_rows<TA, kRT, kSplit, kFours>(g, W, row0, end, n0, lds, none, Beside<TS, 0>{}, StoreEnd<TS, TA, kFours>{ld_in, W.n_end, dX});
 }
 
 // Partial dW of one 64 x 64 wc block: the chunk's rows are shared by dw.wr waves, joined in LDS in order.
@@ -278,10 +375,9 @@ __device__ __forceinline__ void dw_role(const Plan& p, int64_t chunk, int i, int
 
 // G: the source of dX.  B, B2: those of dW (kTwo: the second-order pass, x2 B2 added to x B; the column sums are those of B).
 template <typename TS, typename TA, int kRT, bool kSplit, bool kFours, bool kTwo, typename G, typename B, typename B2, typename Weights>
-__global__ __launch_bounds__((threads<kSplit, TA>())) void backward_kernel(Plan p, int k_in, int k_out, int64_t ld_in, G g, Weights W,
-                                                                     TS* __restrict__ dX, Operand<TA, TS, kPlain> x, B b,
-                                                                     Operand<TA, TS, kPlain> x2, B2 b2, TA* __restrict__ dW,
-                                                                     TA* __restrict__ db) {
+__global__ __launch_bounds__((threads<kSplit, TA>())) void backward_kernel(Plan p, int k_in, int k_out, int64_t ld_in, G g, Weights W, TS* __restrict__ dX,
+                                                                           Operand<TA, TS, kPlain> x, B b, Operand<TA, TS, kPlain> x2, B2 b2,
+                                                                           TA* __restrict__ dW, TA* __restrict__ db) {
   constexpr int kJoin = threads<kSplit, TA>() * 16, kRowsPart = lds_elements<kSplit, kRT, TA>();
   __shared__ TA lds[kJoin > kRowsPart ? kJoin : kRowsPart];
   const int64_t groups = p.dx_groups + p.dw_groups, total = (p.chunks + kXcds - 1) / kXcds * kXcds * groups;
@@ -293,6 +389,145 @@ __global__ __launch_bounds__((threads<kSplit, TA>())) void backward_kernel(Plan 
     else
       dw_role<TA, kTwo, kFours>(p, chunk, static_cast<int>(i - p.dx_groups), k_in, k_out, x, b, x2, b2, dW, db, lds);
     __syncthreads();   // LDS is the next tile's
+  }
+}
+
+template <int kParts, typename T, Source kSource>
+__device__ __forceinline__ SharedColumns<T, kSource, kParts> as_shared(const Operand<float, T, kSource>& o) { return {o}; }
+
+// Partial dW of the rows of a chunk on parts.  Wide: 64 x 256, a wave per 64 columns; otherwise 64 x 64, a wave per 16 rows of dW.
+template <bool kWide, bool kTwo, int kX, int kB, int kB2, typename X, typename B, typename B2>
+__device__ __forceinline__ void parts_dw_role(const Plan& p, int64_t chunk, int i, int k_in, int k_out, const X& x, const B& b, const X& x2,
+                                              const B2& b2, float* __restrict__ dW, float* __restrict__ db, unsigned* lds) {
+  constexpr int kT = kWide ? 4 : 1;   // tiles of 16 rows of dW a wave has
+  const int lane = threadIdx.x & (kLanes - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
+  const int j = lane & 15;
+  const int m0 = i / p.dw_col_groups * kCols, n0 = (i % p.dw_col_groups * p.dw.wc + (kWide ? wave : 0)) * kCols;
+  const int64_t from = chunk * p.per, to = min(p.rows, from + p.per);
+  unsigned* const shared_b = lds + shared_words<kX>();
+  Acc acc[kT][4];
+  float sum[4], none[4];
+  auto clear = [&]() {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      sum[u] = 0;
+#pragma unroll
+      for (int t = 0; t < kT; ++t) acc[t][u] = Acc{0, 0, 0, 0};
+    }
+  };
+  clear();
+  bool done;
+  if constexpr (kWide) {
+    done = outer_parts<kX, kB>(as_shared<kX>(x), as_columns<kB>(b), m0, k_in, n0, k_out, from, to, lds, acc, sum);
+    if constexpr (kTwo) done = outer_parts<kX, kB2>(as_shared<kX>(x2), as_columns<kB2>(b2), m0, k_in, n0, k_out, from, to, lds, acc, none) && done;
+  } else {
+    done = block_parts<kX, kB>(as_shared<kX>(x), as_shared<kB>(b), m0, k_in, n0, k_out, from, to, lds, shared_b, acc, sum);
+    if constexpr (kTwo)
+      done = block_parts<kX, kB2>(as_shared<kX>(x2), as_shared<kB2>(b2), m0, k_in, n0, k_out, from, to, lds, shared_b, acc, none) && done;
+  }
+  if (!done) {   // the same for all waves
+    clear();
+    if constexpr (kWide) {
+      outer_product<float, true>(x, b, m0, k_in, n0, k_out, from, to, acc, sum);
+      if constexpr (kTwo) outer_product<float, true>(x2, b2, m0, k_in, n0, k_out, from, to, acc, none);
+    } else {   // every wave computes the block and keeps its own rows; the column sums are all there in every wave
+      Acc whole[4][4];
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) whole[t][u] = Acc{0, 0, 0, 0};
+      outer_product<float, true>(x, b, m0, k_in, n0, k_out, from, to, whole, sum);
+      if constexpr (kTwo) outer_product<float, true>(x2, b2, m0, k_in, n0, k_out, from, to, whole, none);
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+        if (t == wave) {
+#pragma unroll
+          for (int u = 0; u < 4; ++u) acc[0][u] = whole[t][u];
+        }
+      if (wave != 0) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) sum[u] = 0;
+      }
+    }
+  }
+  const int n = n0 + 4 * j;
+  if (dW && n < k_out) {
+    float* const to_dw = dW + chunk * p.stride;
+#pragma unroll
+    for (int t = 0; t < kT; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int m = m0 + 4 * Mma<float>::row(lane, r) + (kWide ? t : wave);
+        const float v[4] = {acc[t][0][r], acc[t][1][r], acc[t][2][r], acc[t][3][r]};
+        if (m < k_in) store4<true>(to_dw + static_cast<int64_t>(m) * k_out, n, k_out, v);
+      }
+  }
+  if (db && m0 == 0) {   // column sums: over the four q of a wave, then over the waves that shared the rows
+    float* const to_db = db + chunk * p.stride;
+    float* const joined = reinterpret_cast<float*>(lds);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      sum[u] += __shfl_xor(sum[u], 16);
+      sum[u] += __shfl_xor(sum[u], 32);
+    }
+    if constexpr (!kWide) {
+      if (lane < 16) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) joined[(wave * 4 + u) * 16 + j] = sum[u];
+      }
+      __syncthreads();
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        sum[u] = 0;
+        for (int w = 0; w < kWaves; ++w) sum[u] += joined[(w * 4 + u) * 16 + j];
+      }
+    }
+    if (lane < 16 && n < k_out && (kWide || wave == 0)) store4<true>(to_db, n, k_out, sum);
+  }
+}
+
+// backward_kernel on parts.  WT: W transposed.
+template <typename TS, bool kWide, bool kTwo, typename G, typename B, typename B2>
+__global__ __launch_bounds__(kThreads, 2) void parts_backward_kernel(Plan p, int k_in, int k_out, int64_t ld_in, G g, AlongRows<float> WT,
+                                                                     TS* __restrict__ dX, Operand<float, TS, kPlain> x, B b,
+                                                                     Operand<float, TS, kPlain> x2, B2 b2, float* __restrict__ dW,
+                                                                     float* __restrict__ db) {
+  typedef PartCount<TS> Count;
+  constexpr int kG = Count::dx(static_cast<G*>(nullptr)), kB = Count::dw(static_cast<B*>(nullptr)), kB2 = Count::dw(static_cast<B2*>(nullptr));
+  constexpr int kDx = rows_words<kG, Count::w>();
+  constexpr int kDw = shared_words<Count::x>() + (kWide ? 0 : shared_words<(kB > kB2 ? kB : kB2)>());
+  __shared__ unsigned lds[kDx > kDw ? kDx : kDw];
+  const int64_t groups = p.dx_groups + p.dw_groups, total = (p.chunks + kXcds - 1) / kXcds * kXcds * groups;
+  for (int64_t t = blockIdx.x; t < total; t += gridDim.x) {
+    const int64_t local = t / kXcds, chunk = local / groups * kXcds + t % kXcds, i = local % groups;
+    if (chunk >= p.chunks) continue;
+    if (i < p.dx_groups) {
+      const int64_t row0 = chunk * p.per + i / p.dx_col_groups * (16 * kPartsTiles * kWaves), end = min(p.rows, (chunk + 1) * p.per);
+      const int n0 = static_cast<int>(i % p.dx_col_groups) * kCols;
+      const float* const none = nullptr;
+      if (row0 < end)
+        finish_rows_parts<kG, Count::w>(g, WT, row0, end, n0, lds, none, Beside<TS, 0>{}, StoreEnd<TS, float, true>{ld_in, k_in, dX});
+    } else {
+      parts_dw_role<kWide, kTwo, Count::x, kB, kB2>(p, chunk, static_cast<int>(i - p.dx_groups), k_in, k_out, x, b, x2, b2, dW, db, lds);
+    }
+    __syncthreads();
+  }
+}
+
+// G = dY act'(Z) as a tensor of its own, in the arithmetic type: where several column blocks of dX would each make it again.
+template <typename TS>
+__global__ __launch_bounds__(kThreads) void gate_kernel(int64_t rows, int cols, int64_t ld, Gate<float> gate, const TS* __restrict__ dY,
+                                                        const TS* __restrict__ Z, float* __restrict__ G) {
+  const int fours = cols / 4;
+  for (int64_t i = blockIdx.x * static_cast<int64_t>(kThreads) + threadIdx.x; i < rows * fours; i += static_cast<int64_t>(gridDim.x) * kThreads) {
+    const int64_t row = i / fours;
+    const int c = static_cast<int>(i - row * fours) * 4;
+    float g[4], z[4];
+    load4<true>(dY + row * ld, c, cols, g);
+    load4<true>(Z + row * ld, c, cols, z);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) g[k] *= gate.first(z[k]);
+    store4<true>(G + row * cols, c, cols, g);
   }
 }
 
@@ -426,24 +661,58 @@ Plan plan_of(const dl_config* c, int64_t n, bool want_dx, bool want_dw, bool spl
 
 bool curved(const dl_config* c) { return c->activation == DL_SILU || c->activation == DL_GELU; }
 
-// Does dX take W transposed (a launch of its own, 2 us)?  Where the reading of W as it is, four times the accesses, would take longer.
-bool transposed(int64_t n, const dl_config* c, bool split) { return !split && n >= 4096; }
-
-size_t wt_bytes(int64_t n, const dl_config* c) {
-  return transposed(n, c, false) ? align_up(static_cast<size_t>(c->k_in) * c->k_out * weight_size(c), 256) : 0;
+// Do the bfloat16 matrix cores serve a product of rows (dl_parts.h)?
+bool in_parts(const dl_config* c, int64_t n, int cols, int k) {
+  if (c->dtype == SC_F64 || c->k_in % 4 != 0 || c->k_out % 4 != 0 || k <= 16 || (c->dtype == SC_BF16 && k % 8 != 0)) return false;
+  return blocks_of(n, 64) * blocks_of(cols, kCols) >= 1024;
 }
 
-// Workspace: [ S of the second-order pass ][ W transposed ][ partial dW and db per chunk ].
-size_t s_bytes(const dl_config* c, int64_t n) { return curved(c) ? align_up(static_cast<size_t>(n) * c->k_out * weight_size(c), 256) : 0; }
+// Do the waves keep W (walk_rows)?  Its parts of up to 64 reduced indices fit the registers.
+bool kept_ok(const dl_config* c, int64_t n, int cols, int k) { return k <= 2 * kRound && in_parts(c, n, cols, k); }
+
+// Is a wave's share of dW 64 x 64 (parts_dw_role)?
+bool wide_parts(const dl_config* c) { return c->k_out > 2 * kCols; }
+
+Plan parts_plan(const dl_config* c, int64_t n, bool want_dx, bool want_dw) {
+  Plan p{};
+  p.rows = n;
+  const bool wide = wide_parts(c);
+  p.dw = {wide ? kWaves : 1, 1};
+  p.dw_col_groups = static_cast<int>(blocks_of(c->k_out, kCols * p.dw.wc));
+  const int64_t groups = blocks_of(c->k_in, kCols) * p.dw_col_groups;
+  // about two (64 x 64 blocks: three) workgroups a CU, none with less than 256 rows
+  const int64_t chunks = std::max<int64_t>(1, std::min<int64_t>((wide ? 512 : 768) / groups, n / 256));
+  p.per = blocks_of(blocks_of(n, chunks), 256) * 256;
+  p.chunks = blocks_of(n, p.per);
+  p.dx = {1, kWaves};
+  p.dx_col_groups = static_cast<int>(blocks_of(c->k_in, kCols));
+  p.dx_groups = want_dx ? blocks_of(p.per, 16 * kPartsTiles * kWaves) * p.dx_col_groups : 0;
+  p.dw_groups = want_dw ? groups : 0;
+  p.stride = static_cast<int64_t>(c->k_in) * c->k_out + c->k_out;
+  return p;
+}
+
+// Is G made first?  It would be made again for every column block of dX, which then takes longer than its writing and reading.
+bool g_first(const dl_config* c, int64_t n) { return c->activation != DL_NONE && c->k_in > kCols && in_parts(c, n, c->k_in, c->k_out); }
+
+// Workspace: [ S of the second-order pass, or G of the backward ][ W transposed ][ partial dW and db per chunk ].
+size_t s_bytes(const dl_config* c, int64_t n) {
+  return curved(c) || g_first(c, n) ? align_up(static_cast<size_t>(n) * c->k_out * weight_size(c), 256) : 0;
+}
+
+// Does dX take W transposed (a launch of its own, 2 us)?  Where the reading of W as it is, four times the accesses, would take longer.
+bool transposed(int64_t n, const dl_config* c) { return n >= 4096 || in_parts(c, n, c->k_in, c->k_out); }
+
+size_t wt_bytes(int64_t n, const dl_config* c) {
+  return transposed(n, c) ? align_up(static_cast<size_t>(c->k_in) * c->k_out * weight_size(c), 256) : 0;
+}
 
 size_t workspace_bytes(const dl_config* c, int64_t n) {
   if (n == 0) return 256;
-  size_t part = 0;
-  for (bool split : {false, true}) {
-    const Plan p = plan_of(c, n, true, true, split, 1);
-    part = std::max(part, static_cast<size_t>(p.chunks) * p.stride * weight_size(c));
-  }
-  return s_bytes(c, n) + wt_bytes(n, c) + align_up(part, 256) + 256;
+  int64_t chunks = parts_plan(c, n, true, true).chunks;
+  for (bool split : {false, true}) chunks = std::max(chunks, plan_of(c, n, true, true, split, 1).chunks);
+  return s_bytes(c, n) + wt_bytes(n, c) + align_up(static_cast<size_t>(chunks) * plan_of(c, n, true, true, false, 1).stride * weight_size(c), 256) +
+         256;
 }
 
 template <typename TS, typename TA>
@@ -463,8 +732,8 @@ struct Calls {
     return {matrix<TS>(dY, ld_out(c)), matrix<TS>(Z, ld_out(c)), Gate<TA>::of(c->activation)};
   }
 
-  // Launches a product of rows with W [k_in][k_out]: launch(row tiles, split, fours) with all three known at compile time.  Widths that are no
-  // multiple of four test every element and are bound by that: one row tile does for them.
+  // Launches a product of rows with W [k_in][k_out] on the fp32 or fp64 instruction: launch(row tiles, split, fours), all known at compile time.
+  // Widths that are no multiple of four test every element and are bound by that: one row tile does for them.
   template <typename F>
   hipError_t by_shape(int cols, int k, F&& launch) const {
     const std::integral_constant<int, 1> one{};
@@ -487,27 +756,63 @@ struct Calls {
   }
   static unsigned grid_of(int64_t groups) { return static_cast<unsigned>(std::min<int64_t>(groups, 1 << 22)); }
 
-  hipError_t forward(const void* X, const void* W, const void* b, const void* residual, void* Y, void* Z) const {
+  // rows x W with an epilogue: make(fours) gives it.
+  template <typename Make>
+  hipError_t rows_times_w(const void* X, const void* W, const void* b, Make&& make) const {
+    const AlongRows<TA> along{static_cast<const TA*>(W), c->k_in, c->k_out};
+    if constexpr (sizeof(TA) == 4) {
+      if (kept_ok(c, n, c->k_out, c->k_in)) {
+        const PartsColumns<float, kPlain, PartCount<TS>::w> weights{{{along.W, c->k_out}, {}, {}}};
+        return kept<PartCount<TS>::x>(c->k_out, c->k_in, rows_in(X), weights, along, b, make(std::true_type{}));
+      }
+    }
+    if constexpr (sizeof(TA) == 4) {
+      if (in_parts(c, n, c->k_out, c->k_in)) {
+        const Walk walk{blocks_of(n, 16 * kPartsTiles * kWaves), static_cast<int>(blocks_of(c->k_out, kCols))};
+        const auto end = make(std::true_type{});
+        hipLaunchKernelGGL((parts_rows_kernel<TS, std::decay_t<decltype(end)>>), dim3(grid_of(walk.count())), dim3(kThreads), 0, stream, walk, n,
+                           rows_in(X), along, static_cast<const float*>(b), end);
+        return hipGetLastError();
+      }
+    }
     return by_shape(c->k_out, c->k_in, [&](auto rt, auto split, auto fours) {
       const Shape shape = shape_of(c->k_out);
       const Walk walk = walk_of(rt, split, shape);
-      hipLaunchKernelGGL((forward_kernel<TS, TA, rt.value, split.value, fours.value>), dim3(grid_of(walk.count())), dim3((threads<split.value, TA>())), 0, stream,
-                         walk, shape, n, Gate<TA>::of(c->activation), ld_out(c), rows_in(X),
-                         (AlongRows<TA>{static_cast<const TA*>(W), c->k_in, c->k_out}), static_cast<const TA*>(b),
-                         static_cast<const TS*>(residual), static_cast<TS*>(Y), static_cast<TS*>(Z));
+      const auto end = make(fours);
+      hipLaunchKernelGGL((rows_kernel<TS, TA, rt.value, split.value, fours.value, std::decay_t<decltype(end)>>),
+                         dim3(grid_of(walk.count())), dim3((threads<split.value, TA>())), 0, stream, walk, shape, n, rows_in(X), along,
+                         static_cast<const TA*>(b), end);
       return hipGetLastError();
     });
   }
 
+  template <int kX, typename Rows, typename Weights, typename Plain, typename End>
+  hipError_t kept(int cols, int k, const Rows& rows, const Weights& weights, const Plain& plain, const void* b, const End& end) const {
+    const Shape shape = shape_of(cols);
+    const int col_groups = static_cast<int>(blocks_of(cols, kCols * shape.wc));
+    // two waves for every SIMD, all at once
+    const int64_t groups = std::max<int64_t>(kXcds, std::min<int64_t>(512 / col_groups, blocks_of(n, 16 * shape.wr)) / kXcds * kXcds);
+    const Walk walk{groups, col_groups};
+    if (k <= kRound)
+      hipLaunchKernelGGL((kept_kernel<TS, 1, kX, Rows, Weights, Plain, End>), dim3(grid_of(walk.count())), dim3(kThreads), 0, stream, walk, shape,
+                         n, rows, weights, plain, static_cast<const float*>(b), end);
+    else
+      hipLaunchKernelGGL((kept_kernel<TS, 2, kX, Rows, Weights, Plain, End>), dim3(grid_of(walk.count())), dim3(kThreads), 0, stream, walk, shape,
+                         n, rows, weights, plain, static_cast<const float*>(b), end);
+    return hipGetLastError();
+  }
+
+  hipError_t forward(const void* X, const void* W, const void* b, const void* residual, void* Y, void* Z) const {
+    return rows_times_w(X, W, b, [&](auto fours) {
+      return ForwardEnd<TS, TA, fours.value>{Gate<TA>::of(c->activation), ld_out(c), c->k_out, static_cast<const TS*>(residual), static_cast<TS*>(Y),
+                                             static_cast<TS*>(Z)};
+    });
+  }
+
   hipError_t v(const void* HX, const void* W, const void* Z, const void* dY, void* ddY, TA* S) const {
-    return by_shape(c->k_out, c->k_in, [&](auto rt, auto split, auto fours) {
-      const Shape shape = shape_of(c->k_out);
-      const Walk walk = walk_of(rt, split, shape);
-      hipLaunchKernelGGL((v_kernel<TS, TA, rt.value, split.value, fours.value>), dim3(grid_of(walk.count())), dim3((threads<split.value, TA>())), 0, stream, walk,
-                         shape, n, Gate<TA>::of(c->activation), ld_out(c), rows_in(HX), (AlongRows<TA>{static_cast<const TA*>(W), c->k_in, c->k_out}),
-                         c->activation == DL_NONE ? nullptr : static_cast<const TS*>(Z), static_cast<const TS*>(dY),
-                         static_cast<TS*>(ddY), S);
-      return hipGetLastError();
+    return rows_times_w(HX, W, nullptr, [&](auto fours) {
+      return SecondEnd<TS, TA, fours.value>{Gate<TA>::of(c->activation), ld_out(c), c->k_out, c->activation == DL_NONE ? nullptr : static_cast<const TS*>(Z),
+                                            static_cast<const TS*>(dY), static_cast<TS*>(ddY), S};
     });
   }
 
@@ -515,39 +820,82 @@ struct Calls {
   template <bool kTwo, typename G, typename B, typename B2>
   hipError_t gradients(const G& source, const void* W, void* dX, const void* X, const B& b, const void* X2, const B2& b2, void* dW,
                        void* db, void* ws) const {
-    return by_shape(c->k_in, c->k_out, [&](auto rt, auto split, auto fours) {
-      const AlongColumns<TA> as_is{static_cast<const TA*>(W), c->k_out, c->k_in};
-      if constexpr (!split.value && fours.value) {
-        if (dX && transposed(n, c, split)) {
-          const int64_t tiles = blocks_of(c->k_in, 32) * blocks_of(c->k_out, 32);
-          hipLaunchKernelGGL((transpose_kernel<TA>), dim3(static_cast<unsigned>(tiles)), dim3(kThreads), 0, stream, c->k_in, c->k_out,
-                             static_cast<const TA*>(W), static_cast<TA*>(ws));
-          const hipError_t e = hipGetLastError();
+    if constexpr (sizeof(TA) == 4) {
+      if (dX && kept_ok(c, n, c->k_in, c->k_out)) {   // dX by itself, then dW
+        const float* w = static_cast<const float*>(W);
+        const PartsTransposed<PartCount<TS>::w> weights{{w, c->k_out}};
+        const hipError_t e = kept<PartCount<TS>::dx(static_cast<G*>(nullptr))>(c->k_in, c->k_out, source, weights, AlongColumns<float>{w, c->k_out, c->k_in},
+                                                                                nullptr, StoreEnd<TS, float, true>{ld_in(c), c->k_in, static_cast<TS*>(dX)});
+        return e != hipSuccess || !(dW || db) ? e : gradients<kTwo>(source, W, nullptr, X, b, X2, b2, dW, db, ws);
+      }
+    }
+    if constexpr (sizeof(TA) == 4) {
+      if (in_parts(c, n, c->k_in, c->k_out)) {
+        if (dX) {
+          const hipError_t e = transpose(W, ws);
           if (e != hipSuccess) return e;
-          return gradients_with<kTwo>(rt, split, fours, source, AlongRows<TA>{static_cast<const TA*>(ws), c->k_out, c->k_in}, dX, X, b, X2,
-                                      b2, dW, db, ws);
+        }
+        if (wide_parts(c)) return parts_gradients<true, kTwo>(source, dX, X, b, X2, b2, dW, db, ws);
+        return parts_gradients<false, kTwo>(source, dX, X, b, X2, b2, dW, db, ws);
+      }
+    }
+    return by_shape(c->k_in, c->k_out, [&](auto rt, auto split, auto fours) {
+      if constexpr (!split.value && fours.value) {
+        if (dX && transposed(n, c)) {
+          const hipError_t e = transpose(W, ws);
+          if (e != hipSuccess) return e;
+          return gradients_with<kTwo>(rt, split, fours, source, AlongRows<TA>{static_cast<const TA*>(ws), c->k_out, c->k_in}, dX, X, b, X2, b2, dW,
+                                      db, ws);
         }
       }
-      return gradients_with<kTwo>(rt, split, fours, source, as_is, dX, X, b, X2, b2, dW, db, ws);
+      return gradients_with<kTwo>(rt, split, fours, source, AlongColumns<TA>{static_cast<const TA*>(W), c->k_out, c->k_in}, dX, X, b, X2, b2, dW, db,
+                                  ws);
     });
   }
 
-  template <bool kTwo, typename RT, typename Split, typename Fours, typename G, typename Weights, typename B, typename B2>
-  hipError_t gradients_with(RT rt, Split split, Fours fours, const G& source, const Weights& w, void* dX, const void* X, const B& b,
-                            const void* X2, const B2& b2, void* dW, void* db, void* ws) const {
-    const Plan p = plan_of(c, n, dX != nullptr, dW || db, split, rt);
-    const bool whole = p.chunks == 1;
+  hipError_t transpose(const void* W, void* wt) const {
+    const int64_t tiles = blocks_of(c->k_in, 32) * blocks_of(c->k_out, 32);
+    hipLaunchKernelGGL((transpose_kernel<TA>), dim3(static_cast<unsigned>(tiles)), dim3(kThreads), 0, stream, c->k_in, c->k_out,
+                       static_cast<const TA*>(W), static_cast<TA*>(wt));
+    return hipGetLastError();
+  }
+
+  // dW and db where a chunk's results go: the outputs themselves if there is one chunk.
+  struct Target {
+    TA *dw, *db, *part;
+  };
+  Target target(const Plan& p, void* dW, void* db, void* ws) const {
     TA* part = reinterpret_cast<TA*>(static_cast<char*>(ws) + wt_bytes(n, c));
-    const int64_t n_dw = static_cast<int64_t>(c->k_in) * c->k_out;
-    TA* to_dw = !dW ? nullptr : whole ? static_cast<TA*>(dW) : part;
-    TA* to_db = !db ? nullptr : whole ? static_cast<TA*>(db) : part + n_dw;
+    const bool whole = p.chunks == 1;
+    return {!dW ? nullptr : whole ? static_cast<TA*>(dW) : part,
+            !db ? nullptr : whole ? static_cast<TA*>(db) : part + static_cast<int64_t>(c->k_in) * c->k_out, part};
+  }
+  hipError_t join(const Plan& p, const Target& to, void* dW, void* db) const {
+    const hipError_t e = hipGetLastError();
+    return e != hipSuccess || p.chunks == 1 || !(dW || db) ? e : sum_chunks(to.part, p.chunks, dW, db);
+  }
+
+  template <bool kTwo, typename RT, typename Split, typename Fours, typename G, typename Weights, typename B, typename B2>
+  hipError_t gradients_with(RT rt, Split split, Fours, const G& source, const Weights& w, void* dX, const void* X, const B& b, const void* X2,
+                            const B2& b2, void* dW, void* db, void* ws) const {
+    const Plan p = plan_of(c, n, dX != nullptr, dW || db, split, rt);
+    const Target to = target(p, dW, db, ws);
     const int64_t groups = blocks_of(p.chunks, kXcds) * kXcds * (p.dx_groups + p.dw_groups);
     hipLaunchKernelGGL((backward_kernel<TS, TA, RT::value, Split::value, Fours::value, kTwo, G, B, B2, Weights>), dim3(grid_of(groups)),
-                       dim3((threads<Split::value, TA>())), 0, stream, p, c->k_in, c->k_out, ld_in(c), source, w, static_cast<TS*>(dX),
-                       rows_in(X), b, rows_in(X2), b2, to_dw, to_db);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || whole || !(dW || db)) return e;
-    return sum_chunks(part, p.chunks, dW, db);
+                       dim3((threads<Split::value, TA>())), 0, stream, p, c->k_in, c->k_out, ld_in(c), source, w, static_cast<TS*>(dX), rows_in(X), b,
+                       rows_in(X2), b2, to.dw, to.db);
+    return join(p, to, dW, db);
+  }
+
+  template <bool kWide, bool kTwo, typename G, typename B, typename B2>
+  hipError_t parts_gradients(const G& source, void* dX, const void* X, const B& b, const void* X2, const B2& b2, void* dW, void* db, void* ws) const {
+    const Plan p = parts_plan(c, n, dX != nullptr, dW || db);
+    const Target to = target(p, dW, db, ws);
+    const int64_t groups = blocks_of(p.chunks, kXcds) * kXcds * (p.dx_groups + p.dw_groups);
+    hipLaunchKernelGGL((parts_backward_kernel<TS, kWide, kTwo, G, B, B2>), dim3(grid_of(groups)), dim3(kThreads), 0, stream, p, c->k_in, c->k_out,
+                       ld_in(c), source, (AlongRows<float>{static_cast<const float*>(ws), c->k_out, c->k_in}), static_cast<TS*>(dX), rows_in(X), b,
+                       rows_in(X2), b2, to.dw, to.db);
+    return join(p, to, dW, db);
   }
 
   hipError_t sum_chunks(const TA* part, int64_t chunks, void* dW, void* db) const {
@@ -560,6 +908,17 @@ struct Calls {
 
   hipError_t backward(const void* X, const void* W, const void* Z, const void* dY, void* dX, void* dW, void* db, void* ws) const {
     if (c->activation == DL_NONE) return gradients<false>(g<kPlain>(dY, Z), W, dX, X, g<kPlain>(dY, Z), X, g<kPlain>(dY, Z), dW, db, ws);
+    if constexpr (sizeof(TA) == 4) {
+      if (g_first(c, n)) {
+        float* const G = static_cast<float*>(ws);
+        hipLaunchKernelGGL((gate_kernel<TS>), dim3(grid_of(std::min<int64_t>(blocks_of(n * c->k_out, 4 * kThreads), 8192))), dim3(kThreads), 0, stream, n,
+                           c->k_out, ld_out(c), Gate<float>::of(c->activation), static_cast<const TS*>(dY), static_cast<const TS*>(Z), G);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        const Operand<float, float, kPlain> made{{G, c->k_out}, {}, {}};
+        return gradients<false>(made, W, dX, X, made, X, made, dW, db, static_cast<char*>(ws) + s_bytes(c, n));
+      }
+    }
     return gradients<false>(g<kGated>(dY, Z), W, dX, X, g<kGated>(dY, Z), X, g<kGated>(dY, Z), dW, db, ws);
   }
 

@@ -1,20 +1,21 @@
 // The activations of the dense layer with their first two derivatives, in the arithmetic type.
 //
-// SiLU and the GELU are z s(u(z)) with the logistic s and u = c1 z + c3 z^3 (SiLU: c1 = 1, c3 = 0).  With p = s(u), q = 1 - p
-// (each from exp(-|u|), so neither is a difference of two numbers near 1):
+// SiLU and the GELU are z s(u(z)) with the logistic s and u = c1 z + c3 z^3 (SiLU: c1 = 1, c3 = 0).  With e = exp(-u), p = s(u) = 1 / (1 + e) and
+// q = 1 - p = e p (not the difference of two numbers near 1):
 //   value   z p
 //   first   p + z p q u'
 //   second  2 p q u' + z (p q (q - p) u'^2 + p q u'')
-// ReLU is the same with p = (z > 0) and p q = 0, so one straight line of code serves all three.  u is evaluated at z cut to +-kCut, where p
-// and q are 0 and 1 in both types: the cube would overflow for large z and 0 * infinity follow.
+// ReLU is the same with p = (z > 0) and p q = 0, so one straight line of code serves all three.  The polynomial is evaluated at z cut to +-kCut
+// (its cube would overflow for large z and 0 * infinity follow), and u from kLow on, where p would be the smallest number of the type and is taken
+// as 0: e stays finite, and a large z finds a true zero.
 #pragma once
 #include "sc_internal.h"
 #include "../../include/dl.h"
 
 namespace dl {
 
-// exp(x) for x <= 0 and 1 / x for x in [1, 2].  fp32: the hardware's 2^x and reciprocal, each good to a unit or two of the last place; x log2(e)
-// adds |x| units to the exponential, which by then is exp(x) small.  28 instructions less than the library's pair.
+// exp(x) and 1 / x for x from 1 to 1e38.  fp32: the hardware's 2^x and reciprocal, each good to a unit or two of the last place; x log2(e) adds
+// |x| units to the exponential, where p or q is exp(-|x|) small.  28 instructions less than the library's pair.
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896340736f); }
 __device__ __forceinline__ double exp_of(double x) { return exp(x); }
 __device__ __forceinline__ float inverse_of(float x) { return __builtin_amdgcn_rcpf(x); }
@@ -35,16 +36,17 @@ struct Gate {
   };
 
   __device__ __forceinline__ Point at(T z) const {
-    constexpr T kCut = T(700);
-    const T w = z > kCut ? kCut : z < -kCut ? -kCut : z;   // a NaN stays one
+    constexpr T kCut = T(700), kLow = sizeof(T) == 8 ? T(-700) : T(-87);
+    const T w = z > kCut ? kCut : z < -kCut ? -kCut : z;
     const T square = w * w;
-    const T u = w * (c1 + c3 * square);
-    const T e = exp_of(u > T(0) ? -u : u);   // in (0, 1]
-    const T large = inverse_of(T(1) + e), small = e * large;
+    T u = w * (c1 + c3 * square);
+    u = u < kLow ? kLow : u;   // a NaN stays one, and z carries it in any case
+    const T e = exp_of(-u);
     Point g;
-    g.p = u > T(0) ? large : small;
-    g.pq = large * small;
-    g.diff = u > T(0) ? small - large : large - small;
+    g.p = u > kLow ? inverse_of(T(1) + e) : T(0);
+    const T q = e * g.p;
+    g.pq = g.p * q;
+    g.diff = q - g.p;
     g.u1 = c1 + T(3) * c3 * square;
     g.u2 = T(6) * c3 * w;
     if (relu) {

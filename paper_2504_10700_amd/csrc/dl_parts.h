@@ -1,0 +1,560 @@
+// The products of dl_product.h on the bfloat16 matrix cores, every fp32 value as the sum of bfloat16 parts (el::split_pair: h + m + l, exact from
+// 2^-110 on).  A 16x16x32 instruction occupies the matrix core for 16 cycles, eight 16x16x4 ones for 256, so even six products of parts
+// take three eighths of the time.
+//
+//   fp32 rows       h h + (h m + m h + m m + h l + l h): what is left out is below 2^-24 of |x w|.  An instruction cuts its smaller products off at
+//                   the last bit of the largest and of the sum it adds to, so the five small products are summed by themselves and join
+//                   the sum of h h once per 32 reduced indices.
+//   bfloat16 rows   a row's elements are one part.  Results that are rounded to bfloat16 take two parts of W (2^-17 of a weight) and of
+//                   G = dY act' (one where there is no activation); dW and db are fp32 and take all three parts of G.
+//
+// A lane holds 8 consecutive reduced indices k = 8 q .. 8 q + 7 of index j.  Values that the parts do not stand for (not finite, beyond the largest
+// bfloat16, not zero and below 2^-110) are noted by the wave that meets them, which then computes its tile with the products of
+// dl_product.h.
+#pragma once
+#include "dl_product.h"
+
+namespace dl {
+
+using el::Bf8;
+using el::pack_bf16;
+using el::split_pair;
+using el::SplitPair;
+typedef unsigned U4 __attribute__((ext_vector_type(4)));
+typedef unsigned U2 __attribute__((ext_vector_type(2)));
+typedef Mma<float>::acc_t Acc;
+
+constexpr int kRound = 32;   // reduced indices per round
+
+__device__ __forceinline__ Acc mma_parts(const U4& a, const U4& b, const Acc& c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(Bf8, a), __builtin_bit_cast(Bf8, b), c, 0, 0, 0);
+}
+
+// Adds a b to sum.  NA, NB parts.
+template <int NA, int NB>
+__device__ __forceinline__ void multiply(const U4 (&a)[NA], const U4 (&b)[NB], Acc& sum) {
+  Acc small = {0, 0, 0, 0};
+  bool any = false;
+#pragma unroll
+  for (int order = NA + NB - 2; order > 0; --order)
+#pragma unroll
+    for (int p = NA - 1; p >= 0; --p)
+      if (order - p >= 0 && order - p < NB && order < (NA > NB ? NA : NB)) {
+        if (NA == 3 || NB == 3) small = mma_parts(a[p], b[order - p], small), any = true;
+        else sum = mma_parts(a[p], b[order - p], sum);
+      }
+  sum = mma_parts(a[0], b[0], sum);
+  if (any) sum += small;
+}
+
+// Pairs of values into parts, in the halves of a register each.  low: collects what the last part is rounded from (el::split_pair).
+template <int N>
+__device__ __forceinline__ void split(float x, float y, unsigned (&part)[N], unsigned& low) {
+  if constexpr (N == 3) {
+    const SplitPair s = split_pair(x, y, low);
+    part[0] = s.h, part[1] = s.m, part[2] = s.l;
+  } else {
+    part[0] = pack_bf16(x, y);
+    if constexpr (N == 2) part[1] = pack_bf16(x - el::low_half(part[0]), y - el::high_half(part[0]));
+  }
+}
+
+// Notes an element whose size the parts do not reach: not zero and below 2^-100 (for what is multiplied by act' afterwards: a product that
+// becomes small there does not count beside the others).
+__device__ __forceinline__ void note_tiny(float x, unsigned& low) {
+  const unsigned b = __builtin_bit_cast(unsigned, x) & 0x7fffffffu;
+  low |= b - 1u < 0x0d800000u - 1u ? 1u : 0u;
+}
+
+// Rows as an operand: 16 rows x 32 reduced indices in kParts planes of the wave's corner of LDS (16 rows of 64 bytes each, the four pieces of a
+// row at places that differ between groups of four rows).
+template <typename T, Source kSource, int kParts>
+struct PartsRows;
+
+constexpr int kPlane = 256;   // 32-bit words of a plane
+__device__ __forceinline__ int piece_at(int row, int piece) { return 16 * row + 4 * (piece ^ (row / 4)); }
+
+template <Source kSource, int kParts>
+struct PartsRows<float, kSource, kParts> {
+  Operand<float, float, kSource> from;
+  struct Raw {
+    typename Operand<float, float, kSource>::Raw half[2];   // rows 0..7 and 8..15: lane 8 row + piece of four elements
+  };
+  static __device__ __forceinline__ int column() { return 4 * (threadIdx.x % 8); }
+  __device__ __forceinline__ void request(int64_t row0, int64_t rows, int k, int k_end, Raw& raw) const {
+    const int lane = threadIdx.x & (kLanes - 1);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      from.template request<true>(min(row0 + 8 * h + lane / 8, rows - 1), k + column(), k_end, raw.half[h]);
+  }
+  __device__ __forceinline__ void put(const Raw& raw, int k, int k_end, unsigned* planes, unsigned& low) const {
+    const int lane = threadIdx.x & (kLanes - 1);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      float v[4];
+      from.template finish<true>(raw.half[h], k + column(), k_end, v);
+      unsigned ignored = 0, a[kParts], b[kParts];
+      split<kParts>(v[0], v[1], a, kSource == kGated ? ignored : low);
+      split<kParts>(v[2], v[3], b, kSource == kGated ? ignored : low);
+      if constexpr (kSource == kGated && kParts == 3) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) note_tiny(raw.half[h].v[i], low);
+      }
+      const int at = piece_at(8 * h + lane / 8, lane % 8 / 2) + 2 * (lane & 1);
+#pragma unroll
+      for (int p = 0; p < kParts; ++p) *reinterpret_cast<U2*>(planes + p * kPlane + at) = U2{a[p], b[p]};
+    }
+  }
+};
+
+template <Source kSource, int kParts>
+struct PartsRows<__bf16, kSource, kParts> {
+  static_assert(kSource == kGated || kParts == 1, "an element is one part");
+  Operand<float, __bf16, kSource> from;
+  struct Raw {
+    U4 v, z;   // lane 4 row + piece of eight elements
+  };
+  static __device__ __forceinline__ int column() { return 8 * (threadIdx.x % 4); }
+  static __device__ __forceinline__ U4 load(const Matrix<__bf16>& m, int64_t row, int c, int k_end) {
+    typedef U4 Loose __attribute__((aligned(2)));
+    return *reinterpret_cast<const Loose*>(m.p + row * m.ld + min(c, k_end - 8));
+  }
+  __device__ __forceinline__ void request(int64_t row0, int64_t rows, int k, int k_end, Raw& raw) const {
+    const int64_t row = min(row0 + (threadIdx.x & (kLanes - 1)) / 4, rows - 1);
+    raw.v = load(from.x, row, k + column(), k_end);
+    if constexpr (kSource == kGated) raw.z = load(from.z, row, k + column(), k_end);
+  }
+  __device__ __forceinline__ void put(const Raw& raw, int k, int k_end, unsigned* planes, unsigned& low) const {
+    const int lane = threadIdx.x & (kLanes - 1);
+    const bool inside = k + column() < k_end;
+    U4 part[kParts];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const unsigned pair = inside ? raw.v[i] : 0u;
+      if constexpr (kSource == kPlain) {
+        part[0][i] = pair;
+      } else {
+        const float x = el::low_half(pair) * from.gate.first(el::low_half(raw.z[i])), y = el::high_half(pair) * from.gate.first(el::high_half(raw.z[i]));
+        unsigned s[kParts], ignored = 0;
+        split<kParts>(inside ? x : 0.f, inside ? y : 0.f, s, ignored);
+#pragma unroll
+        for (int p = 0; p < kParts; ++p) part[p][i] = s[p];
+      }
+    }
+    (void)low;
+#pragma unroll
+    for (int p = 0; p < kParts; ++p) *reinterpret_cast<U4*>(planes + p * kPlane + piece_at(lane / 4, lane % 4)) = part[p];
+  }
+};
+
+// A round's operand of 16 rows from the planes.
+template <int kParts>
+__device__ __forceinline__ void get_parts(const unsigned* planes, U4 (&x)[kParts]) {
+  const int lane = threadIdx.x & (kLanes - 1);
+#pragma unroll
+  for (int p = 0; p < kParts; ++p) x[p] = *reinterpret_cast<const U4*>(planes + p * kPlane + piece_at(lane & 15, lane / 16));
+}
+
+// 32 rows x 64 columns of a matrix whose columns are not reduced (W [k][n], and both operands of dW) as an operand: tile u holds columns
+// c0 + 4 j + u.  Raw: rows k + 8 q + i, i = 0..7.
+template <typename T, Source kSource, int kParts>
+struct PartsColumns;
+
+template <Source kSource, int kParts>
+struct PartsColumns<float, kSource, kParts> {
+  Operand<float, float, kSource> from;
+  struct Raw {
+    typename Operand<float, float, kSource>::Raw row[8];
+  };
+  __device__ __forceinline__ void request(int64_t k, int64_t k_end, int c0, int c_end, Raw& raw) const {
+    const int lane = threadIdx.x & (kLanes - 1);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) from.template request<true>(min(k + 8 * (lane / 16) + i, k_end - 1), c0 + 4 * (lane & 15), c_end, raw.row[i]);
+  }
+  // tile u's operand; sum: adds the column's values
+  template <bool kSum>
+  __device__ __forceinline__ void operand(const Raw& raw, int u, int64_t k, int64_t k_end, int c0, int c_end, U4 (&part)[kParts], float& sum,
+                                          unsigned& low) const {
+    const int lane = threadIdx.x & (kLanes - 1);
+    const int64_t k0 = k + 8 * (lane / 16);
+    const bool inside = c0 + 4 * (lane & 15) < c_end;
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+      float v[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        v[h] = raw.row[i + h].v[u];
+        if constexpr (kSource == kGated) v[h] *= from.gate.first(raw.row[i + h].z[u]);
+        if constexpr (kSource == kGated && kParts == 3) note_tiny(raw.row[i + h].v[u], low);
+        v[h] = inside && k0 + i + h < k_end ? v[h] : 0.f;   // rows beyond the end have no part
+      }
+      unsigned s[kParts], ignored = 0;
+      split<kParts>(v[0], v[1], s, kSource == kGated ? ignored : low);
+      if constexpr (kSum) sum += v[0] + v[1];
+#pragma unroll
+      for (int p = 0; p < kParts; ++p) part[p][i / 2] = s[p];
+    }
+  }
+};
+
+template <Source kSource, int kParts>
+struct PartsColumns<__bf16, kSource, kParts> {
+  static_assert(kSource == kGated || kParts == 1, "an element is one part");
+  Operand<float, __bf16, kSource> from;
+  struct Raw {
+    U2 v[8], z[kSource == kGated ? 8 : 1];
+  };
+  static __device__ __forceinline__ U2 load(const Matrix<__bf16>& m, int64_t row, int c, int c_end) {
+    typedef U2 Loose __attribute__((aligned(2)));
+    return *reinterpret_cast<const Loose*>(m.p + row * m.ld + min(c, c_end - 4));
+  }
+  __device__ __forceinline__ void request(int64_t k, int64_t k_end, int c0, int c_end, Raw& raw) const {
+    const int lane = threadIdx.x & (kLanes - 1);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int64_t row = min(k + 8 * (lane / 16) + i, k_end - 1);
+      raw.v[i] = load(from.x, row, c0 + 4 * (lane & 15), c_end);
+      if constexpr (kSource == kGated) raw.z[i] = load(from.z, row, c0 + 4 * (lane & 15), c_end);
+    }
+  }
+  template <bool kSum>
+  __device__ __forceinline__ void operand(const Raw& raw, int u, int64_t k, int64_t k_end, int c0, int c_end, U4 (&part)[kParts], float& sum,
+                                          unsigned& low) const {
+    const int lane = threadIdx.x & (kLanes - 1), w = u / 2;
+    const int64_t k0 = k + 8 * (lane / 16);
+    const bool inside = c0 + 4 * (lane & 15) < c_end;
+    auto half = [&](unsigned x) { return u & 1 ? el::high_half(x) : el::low_half(x); };
+    (void)low;
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+      const bool live_a = inside && k0 + i < k_end, live_b = inside && k0 + i + 1 < k_end;
+      const unsigned a = live_a ? raw.v[i][w] : 0u, b = live_b ? raw.v[i + 1][w] : 0u;
+      if constexpr (kSource == kPlain) {
+        part[0][i / 2] = __builtin_amdgcn_perm(b, a, u & 1 ? 0x07060302 : 0x05040100);
+        if constexpr (kSum) sum += half(a) + half(b);
+      } else {
+        float ga = half(a) * from.gate.first(half(raw.z[i][w])), gb = half(b) * from.gate.first(half(raw.z[i + 1][w]));
+        ga = live_a ? ga : 0.f;
+        gb = live_b ? gb : 0.f;
+        unsigned s[kParts], ignored = 0;
+        split<kParts>(ga, gb, s, ignored);
+        if constexpr (kSum) sum += ga + gb;
+#pragma unroll
+        for (int p = 0; p < kParts; ++p) part[p][i / 2] = s[p];
+      }
+    }
+  }
+};
+
+// Did the wave meet a value that the parts do not stand for?  One that is not finite leaves a NaN in the sums.
+template <int kR, int kC>
+__device__ __forceinline__ bool unserved(const Acc (&acc)[kR][kC], unsigned low) {
+  float mark = 0;
+#pragma unroll
+  for (int i = 0; i < kR; ++i)
+#pragma unroll
+    for (int t = 0; t < kC; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) mark = fmaf(acc[i][t][r], 0.f, mark);
+  return __builtin_amdgcn_ballot_w64((low & 0xffffu) != 0 || mark != 0.f) != 0;   // mark is 0 or NaN
+}
+
+// 32 x 64 of an operand that all four waves of a workgroup use, as the instruction takes it: [part][tile u][lane][8 values] in LDS, two slots.  Wave
+// w makes the pairs of rows 2 w, 2 w + 1 of each eight.
+constexpr int kSharedPart = 4 * kLanes * 4;   // 32-bit words of a part
+template <int kParts>
+__host__ __device__ constexpr int shared_words() { return 2 * kParts * kSharedPart; }
+
+template <typename T, Source kSource, int kParts>
+struct SharedColumns {
+  Operand<float, T, kSource> from;
+  struct Raw {
+    typename Vec4<T>::type v[2], z[kSource == kGated ? 2 : 1];
+  };
+  __device__ __forceinline__ void request(int wave, int64_t k, int64_t k_end, int c0, int c_end, Raw& raw) const {
+    const int lane = threadIdx.x & (kLanes - 1), c = min(c0 + 4 * (lane & 15), c_end - 4);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int64_t row = min(k + 8 * (lane / 16) + 2 * wave + h, k_end - 1);
+      raw.v[h] = *reinterpret_cast<const typename Vec4<T>::type*>(from.x.p + row * from.x.ld + c);
+      if constexpr (kSource == kGated) raw.z[h] = *reinterpret_cast<const typename Vec4<T>::type*>(from.z.p + row * from.z.ld + c);
+    }
+  }
+  // sum: adds the columns' values
+  template <bool kSum>
+  __device__ __forceinline__ void put(int wave, const Raw& raw, int64_t k, int64_t k_end, int c0, int c_end, unsigned* slot, float (&sum)[4],
+                                      unsigned& low) const {
+    const int lane = threadIdx.x & (kLanes - 1);
+    const bool inside = c0 + 4 * (lane & 15) < c_end;
+    const int64_t row = k + 8 * (lane / 16) + 2 * wave;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      float v[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        v[h] = static_cast<float>(raw.v[h][u]);
+        if constexpr (kSource == kGated && kParts == 3) note_tiny(v[h], low);
+        if constexpr (kSource == kGated) v[h] *= from.gate.first(static_cast<float>(raw.z[h][u]));
+        v[h] = inside && row + h < k_end ? v[h] : 0.f;   // rows beyond the end have no part
+      }
+      if constexpr (kSum) sum[u] += v[0] + v[1];
+      unsigned s[kParts], ignored = 0;
+      split<kParts>(v[0], v[1], s, kSource == kGated ? ignored : low);
+#pragma unroll
+      for (int p = 0; p < kParts; ++p) slot[((p * 4 + u) * kLanes + lane) * 4 + wave] = s[p];
+    }
+  }
+};
+
+template <int kParts>
+__device__ __forceinline__ void get_shared(const unsigned* slot, int u, U4 (&part)[kParts]) {
+  const int lane = threadIdx.x & (kLanes - 1);
+#pragma unroll
+  for (int p = 0; p < kParts; ++p) part[p] = *reinterpret_cast<const U4*>(slot + ((p * 4 + u) * kLanes + lane) * 4);
+}
+
+// Is there a wave of the workgroup that met a value the parts do not stand for?  flag: a word of LDS per wave.
+__device__ __forceinline__ bool any_wave(bool mine, unsigned* flag) {
+  const int wave = threadIdx.x / kLanes;
+  __syncthreads();
+  flag[wave] = mine;
+  __syncthreads();
+  bool any = false;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) any = any || flag[w] != 0;
+  __syncthreads();
+  return any;
+}
+
+// rows_product on parts: acc[rt][u] of 16 kRT rows from row0 and the 64 columns from n0 that the workgroup's four waves share, over all reduced
+// indices.  planes: kRT * kX planes of this wave; shared: shared_words<kW>() of the workgroup.  All waves come here, the rows of some may lie
+// beyond the last.  false for all waves: a value that the parts do not stand for.
+template <int kRT, int kX, int kW, typename Rows, typename Weights>
+__device__ __forceinline__ bool rows_parts(const Rows& a, const Weights& w, int64_t row0, int64_t rows, int n0, int n_end, int k_end,
+                                           unsigned* planes, unsigned* shared, Acc (&acc)[kRT][4]) {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
+#pragma unroll
+  for (int i = 0; i < kRT; ++i)
+#pragma unroll
+    for (int t = 0; t < 4; ++t) acc[i][t] = Acc{0, 0, 0, 0};
+  typename Rows::Raw raw[kRT];
+  typename Weights::Raw next;
+  unsigned low = 0;
+  float none[4];
+  auto request_rows = [&](int k) {
+#pragma unroll
+    for (int i = 0; i < kRT; ++i) a.request(row0 + 16 * i, rows, k, k_end, raw[i]);
+  };
+  w.request(wave, 0, k_end, n0, n_end, next);
+  request_rows(0);
+  int at = 0;
+  for (int k = 0; k < k_end; k += kRound, at ^= kW * kSharedPart) {
+    w.template put<false>(wave, next, k, k_end, n0, n_end, shared + at, none, low);
+    if (k + kRound < k_end) w.request(wave, k + kRound, k_end, n0, n_end, next);
+#pragma unroll
+    for (int i = 0; i < kRT; ++i) a.put(raw[i], k, k_end, planes + i * kX * kPlane, low);
+    if (k + kRound < k_end) request_rows(k + kRound);
+    // (one barrier a round: a wave that runs ahead writes the other slot)
+    __syncthreads();
+    U4 x[kRT][kX];
+#pragma unroll
+    for (int i = 0; i < kRT; ++i) get_parts<kX>(planes + i * kX * kPlane, x[i]);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      U4 c[kW];
+      get_shared<kW>(shared + at, u, c);
+#pragma unroll
+      for (int i = 0; i < kRT; ++i) multiply<kX, kW>(x[i], c, acc[i][u]);
+    }
+    Corner<float>::sync();
+  }
+  return !any_wave(unserved<kRT, 4>(acc, low), shared);
+}
+
+// outer_product on parts: acc[t][u] of the wave's 64 columns from n0 and the 64 rows from m0 of dW that the four waves share.
+template <int kA, int kB, typename A, typename B>
+__device__ __forceinline__ bool outer_parts(const A& a, const B& b, int m0, int m_end, int n0, int n_end, int64_t from, int64_t to,
+                                            unsigned* shared, Acc (&acc)[4][4], float (&sum)[4]) {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
+  typename A::Raw ra;
+  typename B::Raw rb;
+  unsigned low = 0;
+  float none[4];
+  if (from < to) {
+    a.request(wave, from, to, m0, m_end, ra);
+    b.request(from, to, n0, n_end, rb);
+  }
+  int at = 0;
+  for (int64_t row = from; row < to; row += kRound, at ^= kA * kSharedPart) {
+    a.template put<false>(wave, ra, row, to, m0, m_end, shared + at, none, low);
+    if (row + kRound < to) a.request(wave, row + kRound, to, m0, m_end, ra);
+    U4 g[4][kB];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) b.template operand<true>(rb, u, row, to, n0, n_end, g[u], sum[u], low);
+    if (row + kRound < to) b.request(row + kRound, to, n0, n_end, rb);
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      U4 x[kA];
+      get_shared<kA>(shared + at, t, x);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) multiply<kA, kB>(x, g[u], acc[t][u]);
+    }
+  }
+  return !any_wave(unserved<4, 4>(acc, low), shared);
+}
+
+// The same of one 64 x 64 block by the whole workgroup, both operands shared: wave w computes the rows m0 + 4 j + w, acc[u].  For blocks that the memory
+// bounds: a quarter of the registers, so there are twice as many waves to wait for it.  sum: the shares of the wave's pairs of rows.
+template <int kA, int kB, typename A, typename B>
+__device__ __forceinline__ bool block_parts(const A& a, const B& b, int m0, int m_end, int n0, int n_end, int64_t from, int64_t to,
+                                            unsigned* shared_a, unsigned* shared_b, Acc (&acc)[1][4], float (&sum)[4]) {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
+  typename A::Raw ra;
+  typename B::Raw rb;
+  unsigned low = 0;
+  float none[4];
+  auto request = [&](int64_t row) {
+    a.request(wave, row, to, m0, m_end, ra);
+    b.request(wave, row, to, n0, n_end, rb);
+  };
+  if (from < to) request(from);
+  int slot = 0;
+  for (int64_t row = from; row < to; row += kRound, slot ^= 1) {
+    unsigned* const sa = shared_a + slot * kA * kSharedPart;
+    unsigned* const sb = shared_b + slot * kB * kSharedPart;
+    a.template put<false>(wave, ra, row, to, m0, m_end, sa, none, low);
+    b.template put<true>(wave, rb, row, to, n0, n_end, sb, sum, low);
+    if (row + kRound < to) request(row + kRound);
+    __syncthreads();
+    U4 x[kA];
+    get_shared<kA>(sa, wave, x);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      U4 g[kB];
+      get_shared<kB>(sb, u, g);
+      multiply<kA, kB>(x, g, acc[0][u]);
+    }
+  }
+  return !any_wave(unserved<1, 4>(acc, low), shared_a);
+}
+
+// The same operand of a matrix [n_end][k_end] whose second index is reduced (W in dX).
+template <int kParts>
+struct PartsTransposed {
+  Matrix<float> from;
+  struct Raw {
+    float v[4][2][4];   // row c0 + 4 j + u, columns k + 8 q + 4 h + e
+  };
+  __device__ __forceinline__ void request(int64_t k, int64_t k_end, int c0, int c_end, Raw& raw) const {
+    const int lane = threadIdx.x & (kLanes - 1);
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        load4<true>(from.p + min(c0 + 4 * (lane & 15) + u, c_end - 1) * from.ld, static_cast<int>(k) + 8 * (lane / 16) + 4 * h,
+                    static_cast<int>(k_end), raw.v[u][h]);
+  }
+  template <bool kSum>
+  __device__ __forceinline__ void operand(const Raw& raw, int u, int64_t k, int64_t k_end, int, int, U4 (&part)[kParts], float&, unsigned& low) const {
+    const int64_t k0 = k + 8 * ((threadIdx.x & (kLanes - 1)) / 16);
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+      const float a = k0 + i < k_end ? raw.v[u][i / 4][i % 4] : 0.f, b = k0 + i + 1 < k_end ? raw.v[u][i / 4][i % 4 + 1] : 0.f;
+      unsigned s[kParts];
+      split<kParts>(a, b, s, low);
+#pragma unroll
+      for (int p = 0; p < kParts; ++p) part[p][i / 2] = s[p];
+    }
+  }
+};
+
+// ---- products with a matrix of at most 64 reduced indices: a wave keeps its 64 columns of it in registers and walks over the rows
+
+template <int kRounds, int kW>
+struct Kept {
+  U4 c[kRounds][4][kW];
+  bool served;   // the parts stand for every value of the wave's columns
+};
+
+template <int kRounds, int kW, typename Weights>
+__device__ __forceinline__ void keep(const Weights& w, int n0, int n_end, int k_end, Kept<kRounds, kW>& kept) {
+  unsigned low = 0;
+  float none = 0, mark = 0;
+#pragma unroll
+  for (int r = 0; r < kRounds; ++r) {
+    typename Weights::Raw raw;
+    w.request(r * kRound, k_end, n0, n_end, raw);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      w.template operand<false>(raw, u, r * kRound, k_end, n0, n_end, kept.c[r][u], none, low);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)   // not finite (or beyond the largest bfloat16): 0 times the first part is a NaN
+        mark = fmaf(el::low_half(kept.c[r][u][0][i]), 0.f, fmaf(el::high_half(kept.c[r][u][0][i]), 0.f, mark));
+    }
+  }
+  kept.served = __builtin_amdgcn_ballot_w64((low & 0xffffu) != 0 || mark != 0.f) == 0;
+}
+
+// Row tiles tile, tile + step, .. of a wave: finish(row0, acc, beside) for each, the rows of the next tile and what its epilogue reads requested
+// before the present one is computed.  again: the product of a tile that the parts do not serve.
+template <int kRounds, int kX, int kW, typename Rows, typename T, int N, typename Again, typename F>
+__device__ __forceinline__ void walk_rows(const Rows& a, const Kept<kRounds, kW>& kept, int64_t tile, int64_t step, int64_t rows, int n0, int n_end,
+                                          int k_end, unsigned* planes, const Beside<T, N>& beside, Again&& again, F&& finish) {
+  const int lane = threadIdx.x & (kLanes - 1), c = n0 + 4 * (lane & 15);
+  constexpr int M = N > 0 ? N : 1;
+  typename Rows::Raw raw[kRounds];
+  typename Vec4<T>::type next[M][4];
+  auto request = [&](int64_t t) {
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r) a.request(16 * t, rows, r * kRound, k_end, raw[r]);
+  };
+  auto request_beside = [&](int64_t t) {
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      if (beside.m[e].p)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          next[e][r] = *reinterpret_cast<const typename Vec4<T>::type*>(beside.m[e].p + min(16 * t + Mma<float>::row(lane, r), rows - 1) * beside.m[e].ld +
+                                                                        min(c, n_end - 4));
+  };
+  if (16 * tile >= rows) return;
+  request(tile);
+  request_beside(tile);
+  for (; 16 * tile < rows; tile += step) {
+    unsigned low = 0;
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r) a.put(raw[r], r * kRound, k_end, planes + r * kX * kPlane, low);
+    const bool more = 16 * (tile + step) < rows;
+    if (more) request(tile + step);
+    Corner<float>::sync();
+    Acc acc[1][4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) acc[0][u] = Acc{0, 0, 0, 0};
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r) {
+      U4 x[kX];
+      get_parts<kX>(planes + r * kX * kPlane, x);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) multiply<kX, kW>(x, kept.c[r][u], acc[0][u]);
+    }
+    Corner<float>::sync();
+    if (!kept.served || unserved<1, 4>(acc, low)) again(16 * tile, acc);
+    float x[4][M][4];
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[r][e][i] = static_cast<float>(next[e][r][i]);
+    if (more) request_beside(tile + step);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int64_t row = 16 * tile + Mma<float>::row(lane, r);
+      const float v[4] = {acc[0][0][r], acc[0][1][r], acc[0][2][r], acc[0][3][r]};
+      if (row < rows && c < n_end) finish(row, c, v, x[r]);
+    }
+  }
+}
+
+}  // namespace dl
