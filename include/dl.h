@@ -38,7 +38,8 @@ extern "C" {
  * the hyperbolic tangent.  DL_RELU: max(z, 0), its derivative at 0 taken as 0. */
 typedef enum { DL_NONE = 0, DL_RELU = 1, DL_SILU = 2, DL_GELU = 3 } dl_activation;
 
-#define DL_MAX_WIDTH 65536 /* largest k_in and k_out */
+#define DL_MAX_WIDTH 65536     /* largest k_in and k_out   */
+#define DL_MAX_STRIDE 33554432 /* largest ld_in and ld_out */
 
 typedef struct {
   int32_t struct_size; /* = sizeof(dl_config), ABI guard        */

@@ -101,20 +101,20 @@ __device__ __forceinline__ void finish_rows(const Rows& a, const Weights& w, int
 #pragma unroll
       for (int u = 0; u < 4; ++u) lds[((wave * 4 + r) * 4 + u) * kLanes + lane] = acc[0][u][r];
     __syncthreads();
-    const int64_t row = row0 + Mma<TA>::row(lane, wave & 3);   // wave w < 4 finishes the lanes' result r = w
-    const int c = n0 + 4 * (lane & 15);
-    if (wave < 4 && row < rows && c < w.n_end) {
+    const int64_t row = row0 + base_row<TA>(wave & 3);   // wave w < 4 finishes the lanes' result r = w
+    const int c = n0 + 4 * (lane & 15), lr = lane_row<TA>();
+    if (wave < 4 && row + lr < rows && c < w.n_end) {
       TA x[N > 0 ? N : 1][4], v[4] = {0, 0, 0, 0}, sum[4] = {0, 0, 0, 0};
       if (bias) load4<kFours>(bias, c, w.n_end, v);
 #pragma unroll
       for (int e = 0; e < N; ++e)
-        if (beside.m[e].p) load4<kFours>(beside.m[e].p + row * beside.m[e].ld, c, w.n_end, x[e]);
+        if (beside.m[e].p) load4<kFours>(beside.m[e].p + (row + lr) * beside.m[e].ld, c, w.n_end, x[e]);
       for (int p = 0; p < kN; ++p)
 #pragma unroll
         for (int i = 0; i < 4; ++i) sum[i] += lds[((p * 4 + wave) * 4 + i) * kLanes + lane];
 #pragma unroll
       for (int i = 0; i < 4; ++i) v[i] += sum[i];
-      f(row, c, v, x);
+      f(row, lr, c, v, x);
     }
     __syncthreads();
   }
@@ -143,10 +143,10 @@ struct ForwardEnd {   // Z = v (bias added), Y = act(Z) + residual
   const TS* residual;
   TS *Y, *Z;
   __device__ __forceinline__ Beside<TS, 1> beside() const { return {{{residual, ld_out}}}; }
-  __device__ __forceinline__ void operator()(int64_t row, int c, const TA (&z)[4], const TA (&x)[1][4]) const {
-    const int64_t at = row * ld_out;
+  __device__ __forceinline__ void operator()(int64_t row, int lr, int c, const TA (&z)[4], const TA (&x)[1][4]) const {
+    const Spot spot{row * ld_out, static_cast<unsigned>(lr) * static_cast<unsigned>(ld_out) + c};
     TA y[4];
-    if (Z) store4<kFours>(Z + at, c, n_end, z);
+    if (Z) store4<kFours>(at(Z, spot), c, n_end, z);
 #pragma unroll
     for (int i = 0; i < 4; ++i) y[i] = z[i];
     if (gate.on) {
@@ -157,7 +157,7 @@ struct ForwardEnd {   // Z = v (bias added), Y = act(Z) + residual
 #pragma unroll
       for (int i = 0; i < 4; ++i) y[i] += x[0][i];
     }
-    store4<kFours>(Y + at, c, n_end, y);
+    store4<kFours>(at(Y, spot), c, n_end, y);
   }
 };
 
@@ -170,7 +170,7 @@ struct SecondEnd {   // v = V: ddY = V act'(Z), S = V dY act''(Z).  Z NULL: no a
   TS* ddY;
   TA* S;
   __device__ __forceinline__ Beside<TS, 2> beside() const { return {{{Z, ld_out}, {S ? dY : nullptr, ld_out}}}; }
-  __device__ __forceinline__ void operator()(int64_t row, int c, const TA (&v)[4], const TA (&x)[2][4]) const {
+  __device__ __forceinline__ void operator()(int64_t row, int lr, int c, const TA (&v)[4], const TA (&x)[2][4]) const {
     TA out[4], s[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -179,8 +179,8 @@ struct SecondEnd {   // v = V: ddY = V act'(Z), S = V dY act''(Z).  Z NULL: no a
       out[i] = v[i] * first;
       s[i] = v[i] * x[1][i] * second;
     }
-    if (S) store4<kFours>(S + row * n_end, c, n_end, s);
-    store4<kFours>(ddY + row * ld_out, c, n_end, out);
+    if (S) store4<kFours>(at(S, Spot{row * n_end, static_cast<unsigned>(lr * n_end + c)}), c, n_end, s);
+    store4<kFours>(at(ddY, Spot{row * ld_out, static_cast<unsigned>(lr) * static_cast<unsigned>(ld_out) + c}), c, n_end, out);
   }
 };
 
@@ -190,7 +190,9 @@ struct StoreEnd {
   int n_end;
   TS* out;
   __device__ __forceinline__ Beside<TS, 0> beside() const { return {}; }
-  __device__ __forceinline__ void operator()(int64_t row, int c, const TA (&v)[4], const TA (&)[1][4]) const { store4<kFours>(out + row * ld, c, n_end, v); }
+  __device__ __forceinline__ void operator()(int64_t row, int lr, int c, const TA (&v)[4], const TA (&)[1][4]) const {
+    store4<kFours>(at(out, Spot{row * ld, static_cast<unsigned>(lr) * static_cast<unsigned>(ld) + c}), c, n_end, v);
+  }
 };
 
 // Forward and V: rows x W.
@@ -239,31 +241,31 @@ __global__ __launch_bounds__(kThreads, 2) void parts_rows_kernel(Walk walk, int6
 
 // A product of rows with a matrix of at most 32 kRounds reduced indices that the waves keep (dl_parts.h).  Weights: W in place (forward, V) or
 // transposed (dX), with the same matrix for the fp32 instruction; kX: parts of the rows.
-template <typename TS, int kRounds, int kX, typename Rows, typename Weights, typename Plain, typename End>
-__global__ __launch_bounds__(kThreads, 2) void kept_kernel(Walk walk, Shape shape, int64_t rows, Rows from, Weights weights, Plain plain,
+template <typename TS, int kWc, int kRounds, int kX, typename Rows, typename Weights, typename Plain, typename End>
+__global__ __launch_bounds__(kThreads, 2) void kept_kernel(Walk walk, int64_t turns, int64_t rows, Rows from, Weights weights, Plain plain,
                                                            const float* __restrict__ bias, End end) {
-  constexpr int kW = PartCount<TS>::w;
-  constexpr int kLds = kWaves * kRounds * kX * kPlane;
-  __shared__ float lds[kLds];
-  static_assert(kRounds * kX * kPlane >= Corner<float>::kBlock, "room for the fp32 product");
+  constexpr int kW = PartCount<TS>::w, kWr = kWaves / kWc;
+  constexpr int kTile = kRounds * kX * kPlane, kSlots = kWc > 1 ? 2 : 1;
+  __shared__ unsigned lds[kWaves * kSlots * kTile];       // of each group of kWc waves: the planes of kWc tiles, a slot after the other
+  __shared__ float corners[kWaves][Corner<float>::kBlock];
+  __shared__ unsigned flags[kWr][2 * kWc];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes), lane = threadIdx.x & (kLanes - 1);
+  const int own = wave % kWc, group = wave / kWc;
   int64_t rg;
   int cg;
   if (!walk.at(blockIdx.x, &rg, &cg)) return;
-  const int n0 = (cg * shape.wc + wave % shape.wc) * kCols, n_end = plain.n_end, k_end = plain.k_end;
-  if (n0 >= n_end) return;
-  float* const corner = lds + wave * (kRounds * kX * kPlane);
+  const int n0 = (cg * kWc + own) * kCols, n_end = plain.n_end, k_end = plain.k_end;   // (columns beyond the last are computed and not stored)
   Kept<kRounds, kW> kept;
   keep(weights, n0, n_end, k_end, kept);
   float b[4] = {0, 0, 0, 0};
   if (bias) load4<true>(bias, n0 + 4 * (lane & 15), n_end, b);
-  walk_rows<kRounds, kX, kW>(
-      as_rows<kX>(from), kept, rg * shape.wr + wave / shape.wc, walk.row_groups * shape.wr, rows, n0, n_end, k_end,
-      reinterpret_cast<unsigned*>(corner), end.beside(),
-      [&](int64_t row0, Acc(&acc)[1][4]) { rows_product<float, 1, true>(from, plain, row0, rows, n0, 0, k_end, corner, acc); },
-      [&](int64_t row, int c, const float(&v)[4], const auto& x) {
+  walk_rows<kWc, kRounds, kX, kW>(
+      as_rows<kX>(from), kept, (rg * kWr + group) * kWc, walk.row_groups * kWaves, turns, own, rows, n0, n_end, k_end, lds + group * kWc * kSlots * kTile,
+      flags[group], end.beside(),
+      [&](int64_t row0, Acc(&acc)[1][4]) { rows_product<float, 1, true>(from, plain, row0, rows, n0, 0, k_end, corners[wave], acc); },
+      [&](int64_t row, int lr, int c, const float(&v)[4], const auto& x) {
         const float z[4] = {v[0] + b[0], v[1] + b[1], v[2] + b[2], v[3] + b[3]};
-        end(row, c, z, x);
+        end(row, lr, c, z, x);
       });
 }
 
@@ -324,7 +326,7 @@ __device__ __forceinline__ void dw_role(const Plan& p, int64_t chunk, int i, int
   const int n = n0 + 4 * j;
   if (p.dw.wr == 1) {
     if (n0 >= k_out) return;
-    if (to_db && q == 0) store4<kFours>(to_db, n, k_out, sum);
+    if (to_db && q == 0) store4<kFours>(to_db + n, n, k_out, sum);
     if (to_dw) {
 #pragma unroll
       for (int t = 0; t < 4; ++t)
@@ -332,7 +334,7 @@ __device__ __forceinline__ void dw_role(const Plan& p, int64_t chunk, int i, int
         for (int r = 0; r < 4; ++r) {
           const int m = m0 + 4 * Mma<TA>::row(lane, r) + t;
           const TA v[4] = {acc[t][0][r], acc[t][1][r], acc[t][2][r], acc[t][3][r]};
-          if (m < k_in && n < k_out) store4<kFours>(to_dw + static_cast<int64_t>(m) * k_out, n, k_out, v);
+          if (m < k_in && n < k_out) store4<kFours>(to_dw + static_cast<int64_t>(m) * k_out + n, n, k_out, v);
         }
     }
     return;
@@ -352,7 +354,7 @@ __device__ __forceinline__ void dw_role(const Plan& p, int64_t chunk, int i, int
         for (int w = 0; w < p.dw.wr; ++w)
 #pragma unroll
           for (int u = 0; u < 4; ++u) v[u] += lds[(((w * p.dw.wc + wc) * 4 + r) * 4 + u) * kLanes + lane];
-        if (m < k_in) store4<kFours>(to_dw + static_cast<int64_t>(m) * k_out, n, k_out, v);
+        if (m < k_in) store4<kFours>(to_dw + static_cast<int64_t>(m) * k_out + n, n, k_out, v);
       }
     }
   }
@@ -368,7 +370,7 @@ __device__ __forceinline__ void dw_role(const Plan& p, int64_t chunk, int i, int
       for (int w = 0; w < p.dw.wr; ++w)
 #pragma unroll
         for (int u = 0; u < 4; ++u) v[u] += lds[((w * p.dw.wc + wc) * 4 + u) * 16 + j];
-      store4<kFours>(to_db, n, k_out, v);
+      store4<kFours>(to_db + n, n, k_out, v);
     }
   }
 }
@@ -459,7 +461,7 @@ __device__ __forceinline__ void parts_dw_role(const Plan& p, int64_t chunk, int 
       for (int r = 0; r < 4; ++r) {
         const int m = m0 + 4 * Mma<float>::row(lane, r) + (kWide ? t : wave);
         const float v[4] = {acc[t][0][r], acc[t][1][r], acc[t][2][r], acc[t][3][r]};
-        if (m < k_in) store4<true>(to_dw + static_cast<int64_t>(m) * k_out, n, k_out, v);
+        if (m < k_in) store4<true>(to_dw + static_cast<int64_t>(m) * k_out + n, n, k_out, v);
       }
   }
   if (db && m0 == 0) {   // column sums: over the four q of a wave, then over the waves that shared the rows
@@ -482,31 +484,33 @@ __device__ __forceinline__ void parts_dw_role(const Plan& p, int64_t chunk, int 
         for (int w = 0; w < kWaves; ++w) sum[u] += joined[(w * 4 + u) * 16 + j];
       }
     }
-    if (lane < 16 && n < k_out && (kWide || wave == 0)) store4<true>(to_db, n, k_out, sum);
+    if (lane < 16 && n < k_out && (kWide || wave == 0)) store4<true>(to_db + n, n, k_out, sum);
   }
 }
 
-// backward_kernel on parts.  WT: W transposed.
-template <typename TS, bool kWide, bool kTwo, typename G, typename B, typename B2>
-__global__ __launch_bounds__(kThreads, 2) void parts_backward_kernel(Plan p, int k_in, int k_out, int64_t ld_in, G g, AlongRows<float> WT,
+// backward_kernel on parts.  WT: W transposed.  kDx: is there a dX here?  (Without it the 64 x 64 blocks leave room for more waves.)
+template <typename TS, bool kWide, bool kDx, bool kTwo, typename G, typename B, typename B2>
+__global__ __launch_bounds__(kThreads, kWide || kDx ? 2 : 3) void parts_backward_kernel(Plan p, int k_in, int k_out, int64_t ld_in, G g, AlongRows<float> WT,
                                                                      TS* __restrict__ dX, Operand<float, TS, kPlain> x, B b,
                                                                      Operand<float, TS, kPlain> x2, B2 b2, float* __restrict__ dW,
                                                                      float* __restrict__ db) {
   typedef PartCount<TS> Count;
   constexpr int kG = Count::dx(static_cast<G*>(nullptr)), kB = Count::dw(static_cast<B*>(nullptr)), kB2 = Count::dw(static_cast<B2*>(nullptr));
-  constexpr int kDx = rows_words<kG, Count::w>();
-  constexpr int kDw = shared_words<Count::x>() + (kWide ? 0 : shared_words<(kB > kB2 ? kB : kB2)>());
-  __shared__ unsigned lds[kDx > kDw ? kDx : kDw];
+  constexpr int kDxWords = kDx ? rows_words<kG, Count::w>() : 0;
+  constexpr int kDwWords = shared_words<Count::x>() + (kWide ? 0 : shared_words<(kB > kB2 ? kB : kB2)>());
+  __shared__ unsigned lds[kDxWords > kDwWords ? kDxWords : kDwWords];
   const int64_t groups = p.dx_groups + p.dw_groups, total = (p.chunks + kXcds - 1) / kXcds * kXcds * groups;
   for (int64_t t = blockIdx.x; t < total; t += gridDim.x) {
     const int64_t local = t / kXcds, chunk = local / groups * kXcds + t % kXcds, i = local % groups;
     if (chunk >= p.chunks) continue;
-    if (i < p.dx_groups) {
-      const int64_t row0 = chunk * p.per + i / p.dx_col_groups * (16 * kPartsTiles * kWaves), end = min(p.rows, (chunk + 1) * p.per);
-      const int n0 = static_cast<int>(i % p.dx_col_groups) * kCols;
-      const float* const none = nullptr;
-      if (row0 < end)
-        finish_rows_parts<kG, Count::w>(g, WT, row0, end, n0, lds, none, Beside<TS, 0>{}, StoreEnd<TS, float, true>{ld_in, k_in, dX});
+    if (kDx && i < p.dx_groups) {
+      if constexpr (kDx) {
+        const int64_t row0 = chunk * p.per + i / p.dx_col_groups * (16 * kPartsTiles * kWaves), end = min(p.rows, (chunk + 1) * p.per);
+        const int n0 = static_cast<int>(i % p.dx_col_groups) * kCols;
+        const float* const none = nullptr;
+        if (row0 < end)
+          finish_rows_parts<kG, Count::w>(g, WT, row0, end, n0, lds, none, Beside<TS, 0>{}, StoreEnd<TS, float, true>{ld_in, k_in, dX});
+      }
     } else {
       parts_dw_role<kWide, kTwo, Count::x, kB, kB2>(p, chunk, static_cast<int>(i - p.dx_groups), k_in, k_out, x, b, x2, b2, dW, db, lds);
     }
@@ -527,7 +531,7 @@ __global__ __launch_bounds__(kThreads) void gate_kernel(int64_t rows, int cols, 
     load4<true>(Z + row * ld, c, cols, z);
 #pragma unroll
     for (int k = 0; k < 4; ++k) g[k] *= gate.first(z[k]);
-    store4<true>(G + row * cols, c, cols, g);
+    store4<true>(G + row * cols + c, c, cols, g);
   }
 }
 
@@ -611,10 +615,9 @@ sc_status check_config(const char* fn, const dl_config* cfg, int64_t n) {
   if (cfg->k_in > DL_MAX_WIDTH || cfg->k_out > DL_MAX_WIDTH) return bad(SC_ERR_UNSUPPORTED, "k_in or k_out above DL_MAX_WIDTH");
   if (cfg->activation < DL_NONE || cfg->activation > DL_GELU) return bad(SC_ERR_INVALID_ARG, "bad activation");
   if (cfg->dtype != SC_F32 && cfg->dtype != SC_F64 && cfg->dtype != SC_BF16) return bad(SC_ERR_INVALID_ARG, "bad dtype");
-  const int64_t most = int64_t(1) << 32;
-  if (cfg->ld_in != 0 && (cfg->ld_in < cfg->k_in || cfg->ld_in > most)) return bad(SC_ERR_INVALID_ARG, "ld_in below k_in or above 2^32");
-  if (cfg->ld_out != 0 && (cfg->ld_out < cfg->k_out || cfg->ld_out > most))
-    return bad(SC_ERR_INVALID_ARG, "ld_out below k_out or above 2^32");
+  if (cfg->ld_in != 0 && cfg->ld_in < cfg->k_in) return bad(SC_ERR_INVALID_ARG, "ld_in below k_in");
+  if (cfg->ld_out != 0 && cfg->ld_out < cfg->k_out) return bad(SC_ERR_INVALID_ARG, "ld_out below k_out");
+  if (cfg->ld_in > DL_MAX_STRIDE || cfg->ld_out > DL_MAX_STRIDE) return bad(SC_ERR_UNSUPPORTED, "ld_in or ld_out above DL_MAX_STRIDE");
   if (n < 0 || n > (int64_t(1) << 30)) return bad(SC_ERR_INVALID_ARG, "n_rows outside 0..2^30");
   return SC_OK;
 }
@@ -663,6 +666,8 @@ bool curved(const dl_config* c) { return c->activation == DL_SILU || c->activati
 
 // Do the bfloat16 matrix cores serve a product of rows (dl_parts.h)?
 bool in_parts(const dl_config* c, int64_t n, int cols, int k) {
+  // (the lanes' places in 64 rows are 32-bit byte offsets)
+  if (ld_in(c) > (1 << 22) || ld_out(c) > (1 << 22)) return false;
   if (c->dtype == SC_F64 || c->k_in % 4 != 0 || c->k_out % 4 != 0 || k <= 16 || (c->dtype == SC_BF16 && k % 8 != 0)) return false;
   return blocks_of(n, 64) * blocks_of(cols, kCols) >= 1024;
 }
@@ -682,7 +687,8 @@ Plan parts_plan(const dl_config* c, int64_t n, bool want_dx, bool want_dw) {
   const int64_t groups = blocks_of(c->k_in, kCols) * p.dw_col_groups;
   // about two (64 x 64 blocks: three) workgroups a CU, none with less than 256 rows
   const int64_t chunks = std::max<int64_t>(1, std::min<int64_t>((wide ? 512 : 768) / groups, n / 256));
-  p.per = blocks_of(blocks_of(n, chunks), 256) * 256;
+  const int64_t unit = want_dx || wide ? 256 : 32;
+  p.per = blocks_of(blocks_of(n, chunks), unit) * unit;
   p.chunks = blocks_of(n, p.per);
   p.dx = {1, kWaves};
   p.dx_col_groups = static_cast<int>(blocks_of(c->k_in, kCols));
@@ -709,7 +715,7 @@ size_t wt_bytes(int64_t n, const dl_config* c) {
 
 size_t workspace_bytes(const dl_config* c, int64_t n) {
   if (n == 0) return 256;
-  int64_t chunks = parts_plan(c, n, true, true).chunks;
+  int64_t chunks = std::max(parts_plan(c, n, true, true).chunks, parts_plan(c, n, false, true).chunks);
   for (bool split : {false, true}) chunks = std::max(chunks, plan_of(c, n, true, true, split, 1).chunks);
   return s_bytes(c, n) + wt_bytes(n, c) + align_up(static_cast<size_t>(chunks) * plan_of(c, n, true, true, false, 1).stride * weight_size(c), 256) +
          256;
@@ -791,15 +797,19 @@ struct Calls {
     const Shape shape = shape_of(cols);
     const int col_groups = static_cast<int>(blocks_of(cols, kCols * shape.wc));
     // two waves for every SIMD, all at once
-    const int64_t groups = std::max<int64_t>(kXcds, std::min<int64_t>(512 / col_groups, blocks_of(n, 16 * shape.wr)) / kXcds * kXcds);
+    const int64_t groups = std::max<int64_t>(kXcds, std::min<int64_t>(512 / col_groups, blocks_of(n, 16 * kWaves)) / kXcds * kXcds);
     const Walk walk{groups, col_groups};
-    if (k <= kRound)
-      hipLaunchKernelGGL((kept_kernel<TS, 1, kX, Rows, Weights, Plain, End>), dim3(grid_of(walk.count())), dim3(kThreads), 0, stream, walk, shape,
-                         n, rows, weights, plain, static_cast<const float*>(b), end);
-    else
-      hipLaunchKernelGGL((kept_kernel<TS, 2, kX, Rows, Weights, Plain, End>), dim3(grid_of(walk.count())), dim3(kThreads), 0, stream, walk, shape,
-                         n, rows, weights, plain, static_cast<const float*>(b), end);
-    return hipGetLastError();
+    const int64_t turns = blocks_of(blocks_of(n, 16), groups * kWaves);
+    auto launch = [&](auto wc, auto rounds) {
+      hipLaunchKernelGGL((kept_kernel<TS, wc.value, rounds.value, kX, Rows, Weights, Plain, End>), dim3(grid_of(walk.count())), dim3(kThreads), 0,
+                         stream, walk, turns, n, rows, weights, plain, static_cast<const float*>(b), end);
+      return hipGetLastError();
+    };
+    const std::integral_constant<int, 1> one{};
+    const std::integral_constant<int, 2> two{};
+    const std::integral_constant<int, 4> four{};
+    if (k <= kRound) return shape.wc == 1 ? launch(one, one) : shape.wc == 2 ? launch(two, one) : launch(four, one);
+    return shape.wc == 1 ? launch(one, two) : shape.wc == 2 ? launch(two, two) : launch(four, two);
   }
 
   hipError_t forward(const void* X, const void* W, const void* b, const void* residual, void* Y, void* Z) const {
@@ -835,8 +845,10 @@ struct Calls {
           const hipError_t e = transpose(W, ws);
           if (e != hipSuccess) return e;
         }
-        if (wide_parts(c)) return parts_gradients<true, kTwo>(source, dX, X, b, X2, b2, dW, db, ws);
-        return parts_gradients<false, kTwo>(source, dX, X, b, X2, b2, dW, db, ws);
+        if (wide_parts(c)) return dX ? parts_gradients<true, true, kTwo>(source, dX, X, b, X2, b2, dW, db, ws)
+                                     : parts_gradients<true, false, kTwo>(source, dX, X, b, X2, b2, dW, db, ws);
+        return dX ? parts_gradients<false, true, kTwo>(source, dX, X, b, X2, b2, dW, db, ws)
+                  : parts_gradients<false, false, kTwo>(source, dX, X, b, X2, b2, dW, db, ws);
       }
     }
     return by_shape(c->k_in, c->k_out, [&](auto rt, auto split, auto fours) {
@@ -887,12 +899,12 @@ struct Calls {
     return join(p, to, dW, db);
   }
 
-  template <bool kWide, bool kTwo, typename G, typename B, typename B2>
+  template <bool kWide, bool kDx, bool kTwo, typename G, typename B, typename B2>
   hipError_t parts_gradients(const G& source, void* dX, const void* X, const B& b, const void* X2, const B2& b2, void* dW, void* db, void* ws) const {
     const Plan p = parts_plan(c, n, dX != nullptr, dW || db);
     const Target to = target(p, dW, db, ws);
     const int64_t groups = blocks_of(p.chunks, kXcds) * kXcds * (p.dx_groups + p.dw_groups);
-    hipLaunchKernelGGL((parts_backward_kernel<TS, kWide, kTwo, G, B, B2>), dim3(grid_of(groups)), dim3(kThreads), 0, stream, p, c->k_in, c->k_out,
+    hipLaunchKernelGGL((parts_backward_kernel<TS, kWide, kDx, kTwo, G, B, B2>), dim3(grid_of(groups)), dim3(kThreads), 0, stream, p, c->k_in, c->k_out,
                        ld_in(c), source, (AlongRows<float>{static_cast<const float*>(ws), c->k_out, c->k_in}), static_cast<TS*>(dX), rows_in(X), b,
                        rows_in(X2), b2, to.dw, to.db);
     return join(p, to, dW, db);

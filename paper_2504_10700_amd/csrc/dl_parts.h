@@ -30,21 +30,22 @@ __device__ __forceinline__ Acc mma_parts(const U4& a, const U4& b, const Acc& c)
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(Bf8, a), __builtin_bit_cast(Bf8, b), c, 0, 0, 0);
 }
 
-// Adds a b to sum.  NA, NB parts.
+// Adds a b: the product of the first parts to sum, the others to small (where no operand has three parts, all to sum).
 template <int NA, int NB>
-__device__ __forceinline__ void multiply(const U4 (&a)[NA], const U4 (&b)[NB], Acc& sum) {
-  Acc small = {0, 0, 0, 0};
-  bool any = false;
+__device__ __forceinline__ void multiply(const U4 (&a)[NA], const U4 (&b)[NB], Acc& sum, Acc& small) {
 #pragma unroll
   for (int order = NA + NB - 2; order > 0; --order)
 #pragma unroll
     for (int p = NA - 1; p >= 0; --p)
       if (order - p >= 0 && order - p < NB && order < (NA > NB ? NA : NB)) {
-        if (NA == 3 || NB == 3) small = mma_parts(a[p], b[order - p], small), any = true;
-        else sum = mma_parts(a[p], b[order - p], sum);
+        Acc& to = NA == 3 || NB == 3 ? small : sum;
+        to = mma_parts(a[p], b[order - p], to);
       }
   sum = mma_parts(a[0], b[0], sum);
-  if (any) sum += small;
+}
+template <int NA, int NB>
+__device__ __forceinline__ void join(Acc& sum, const Acc& small) {
+  if constexpr (NA == 3 || NB == 3) sum += small;
 }
 
 // Pairs of values into parts, in the halves of a register each.  low: collects what the last part is rounded from (el::split_pair).
@@ -74,35 +75,62 @@ struct PartsRows;
 constexpr int kPlane = 256;   // 32-bit words of a plane
 __device__ __forceinline__ int piece_at(int row, int piece) { return 16 * row + 4 * (piece ^ (row / 4)); }
 
+// Four or eight elements at (row0 + r) of a tensor, columns k + c .. of k_end: row0 and k are the same for the wave.  Beyond the end of the row the
+// address is that of its last elements.
+template <typename V, typename T>
+__device__ __forceinline__ V load_piece(const Matrix<T>& m, int64_t row0, int r, int k, int c, int k_end) {
+  constexpr int kN = sizeof(V) / sizeof(T);
+  typedef V Loose __attribute__((aligned(sizeof(T))));
+  unsigned lane = static_cast<unsigned>(r) * static_cast<unsigned>(m.ld) + c;
+  int64_t base = row0 * m.ld + k;
+  if (k + kRound > k_end) {   // the last round: what is left may end inside it
+    lane += min(k + c, k_end - kN) - c;
+    base = row0 * m.ld;
+  }
+  return *reinterpret_cast<const Loose*>(at(m.p, Spot{base, lane}));
+}
+
 template <Source kSource, int kParts>
 struct PartsRows<float, kSource, kParts> {
   Operand<float, float, kSource> from;
+  typedef float F4 __attribute__((ext_vector_type(4)));
   struct Raw {
-    typename Operand<float, float, kSource>::Raw half[2];   // rows 0..7 and 8..15: lane 8 row + piece of four elements
+    F4 v[2], z[kSource == kGated ? 2 : 1];   // rows 0..7 and 8..15: lane 8 row + piece of four elements
   };
   static __device__ __forceinline__ int column() { return 4 * (threadIdx.x % 8); }
-  __device__ __forceinline__ void request(int64_t row0, int64_t rows, int k, int k_end, Raw& raw) const {
-    const int lane = threadIdx.x & (kLanes - 1);
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-      from.template request<true>(min(row0 + 8 * h + lane / 8, rows - 1), k + column(), k_end, raw.half[h]);
-  }
-  __device__ __forceinline__ void put(const Raw& raw, int k, int k_end, unsigned* planes, unsigned& low) const {
+  __device__ __forceinline__ void request(int64_t start, int left, int k, int k_end, Raw& raw, int first) const {   // rows start + first on, of those that are left from start on
     const int lane = threadIdx.x & (kLanes - 1);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      float v[4];
-      from.template finish<true>(raw.half[h], k + column(), k_end, v);
+      const int r = min(first + 8 * h + lane / 8, left - 1);
+      raw.v[h] = load_piece<F4>(from.x, start, r, k, column(), k_end);
+      if constexpr (kSource == kGated) raw.z[h] = load_piece<F4>(from.z, start, r, k, column(), k_end);
+    }
+  }
+  __device__ __forceinline__ void put(Raw& raw, int k, int k_end, unsigned* planes, unsigned& low) const {
+    const int lane = threadIdx.x & (kLanes - 1);
+    if (k + kRound > k_end) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        if (k + column() >= k_end) raw.v[h] = F4{0, 0, 0, 0};
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      F4 v = raw.v[h];
+      if constexpr (kSource == kGated) {
+        const bool inside = k + column() < k_end;   // (0 times what stands beyond the end may be a NaN)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if constexpr (kParts == 3) note_tiny(v[i], low);
+          v[i] = inside ? v[i] * from.gate.first(raw.z[h][i]) : 0.f;
+        }
+      }
       unsigned ignored = 0, a[kParts], b[kParts];
       split<kParts>(v[0], v[1], a, kSource == kGated ? ignored : low);
       split<kParts>(v[2], v[3], b, kSource == kGated ? ignored : low);
-      if constexpr (kSource == kGated && kParts == 3) {
+      const int to = piece_at(8 * h + lane / 8, lane % 8 / 2) + 2 * (lane & 1);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) note_tiny(raw.half[h].v[i], low);
-      }
-      const int at = piece_at(8 * h + lane / 8, lane % 8 / 2) + 2 * (lane & 1);
-#pragma unroll
-      for (int p = 0; p < kParts; ++p) *reinterpret_cast<U2*>(planes + p * kPlane + at) = U2{a[p], b[p]};
+      for (int p = 0; p < kParts; ++p) *reinterpret_cast<U2*>(planes + p * kPlane + to) = U2{a[p], b[p]};
     }
   }
 };
@@ -115,33 +143,29 @@ struct PartsRows<__bf16, kSource, kParts> {
     U4 v, z;   // lane 4 row + piece of eight elements
   };
   static __device__ __forceinline__ int column() { return 8 * (threadIdx.x % 4); }
-  static __device__ __forceinline__ U4 load(const Matrix<__bf16>& m, int64_t row, int c, int k_end) {
-    typedef U4 Loose __attribute__((aligned(2)));
-    return *reinterpret_cast<const Loose*>(m.p + row * m.ld + min(c, k_end - 8));
+  __device__ __forceinline__ void request(int64_t start, int left, int k, int k_end, Raw& raw, int first) const {
+    const int r = min(first + static_cast<int>(threadIdx.x & (kLanes - 1)) / 4, left - 1);
+    raw.v = load_piece<U4>(from.x, start, r, k, column(), k_end);
+    if constexpr (kSource == kGated) raw.z = load_piece<U4>(from.z, start, r, k, column(), k_end);
   }
-  __device__ __forceinline__ void request(int64_t row0, int64_t rows, int k, int k_end, Raw& raw) const {
-    const int64_t row = min(row0 + (threadIdx.x & (kLanes - 1)) / 4, rows - 1);
-    raw.v = load(from.x, row, k + column(), k_end);
-    if constexpr (kSource == kGated) raw.z = load(from.z, row, k + column(), k_end);
-  }
-  __device__ __forceinline__ void put(const Raw& raw, int k, int k_end, unsigned* planes, unsigned& low) const {
+  __device__ __forceinline__ void put(Raw& raw, int k, int k_end, unsigned* planes, unsigned&) const {
     const int lane = threadIdx.x & (kLanes - 1);
     const bool inside = k + column() < k_end;
     U4 part[kParts];
+    if constexpr (kSource == kPlain) {
+      if (k + kRound > k_end && !inside) raw.v = U4{0, 0, 0, 0};
+      part[0] = raw.v;
+    } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const unsigned pair = inside ? raw.v[i] : 0u;
-      if constexpr (kSource == kPlain) {
-        part[0][i] = pair;
-      } else {
-        const float x = el::low_half(pair) * from.gate.first(el::low_half(raw.z[i])), y = el::high_half(pair) * from.gate.first(el::high_half(raw.z[i]));
+      for (int i = 0; i < 4; ++i) {
+        const float x = el::low_half(raw.v[i]) * from.gate.first(el::low_half(raw.z[i]));
+        const float y = el::high_half(raw.v[i]) * from.gate.first(el::high_half(raw.z[i]));
         unsigned s[kParts], ignored = 0;
         split<kParts>(inside ? x : 0.f, inside ? y : 0.f, s, ignored);
 #pragma unroll
         for (int p = 0; p < kParts; ++p) part[p][i] = s[p];
       }
     }
-    (void)low;
 #pragma unroll
     for (int p = 0; p < kParts; ++p) *reinterpret_cast<U4*>(planes + p * kPlane + piece_at(lane / 4, lane % 4)) = part[p];
   }
@@ -156,92 +180,81 @@ __device__ __forceinline__ void get_parts(const unsigned* planes, U4 (&x)[kParts
 }
 
 // 32 rows x 64 columns of a matrix whose columns are not reduced (W [k][n], and both operands of dW) as an operand: tile u holds columns
-// c0 + 4 j + u.  Raw: rows k + 8 q + i, i = 0..7.
-template <typename T, Source kSource, int kParts>
-struct PartsColumns;
+// c0 + 4 j + u.  Of the rows k + 8 q + i a lane requests kCount from kFirst on.
+template <typename T, Source kSource, int kCount>
+struct ColumnsRaw {
+  typename Vec4<T>::type v[kCount], z[kSource == kGated ? kCount : 1];
 
-template <Source kSource, int kParts>
-struct PartsColumns<float, kSource, kParts> {
-  Operand<float, float, kSource> from;
-  struct Raw {
-    typename Operand<float, float, kSource>::Raw row[8];
-  };
-  __device__ __forceinline__ void request(int64_t k, int64_t k_end, int c0, int c_end, Raw& raw) const {
-    const int lane = threadIdx.x & (kLanes - 1);
+  __device__ __forceinline__ void request(const Operand<float, T, kSource>& from, int first, int64_t k, int64_t k_end, int c0, int c_end) {
+    const int lane = threadIdx.x & (kLanes - 1), q8 = 8 * (lane / 16);
+    const int c = min(c0 + 4 * (lane & 15), c_end - 4);
+    const unsigned ld = static_cast<unsigned>(from.x.ld);
+    if (k + kRound <= k_end) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) from.template request<true>(min(k + 8 * (lane / 16) + i, k_end - 1), c0 + 4 * (lane & 15), c_end, raw.row[i]);
+      for (int i = 0; i < kCount; ++i) get(from, i, Spot{(k + first + i) * from.x.ld, q8 * ld + c});
+    } else {   // rows beyond the last: the last one again
+      const int left = static_cast<int>(k_end - k);
+#pragma unroll
+      for (int i = 0; i < kCount; ++i) get(from, i, Spot{k * from.x.ld, static_cast<unsigned>(min(q8 + first + i, left - 1)) * ld + c});
+    }
   }
-  // tile u's operand; sum: adds the column's values
-  template <bool kSum>
-  __device__ __forceinline__ void operand(const Raw& raw, int u, int64_t k, int64_t k_end, int c0, int c_end, U4 (&part)[kParts], float& sum,
-                                          unsigned& low) const {
+  __device__ __forceinline__ void get(const Operand<float, T, kSource>& from, int i, const Spot& spot) {
+    v[i] = *reinterpret_cast<const typename Vec4<T>::type*>(at(from.x.p, spot));
+    if constexpr (kSource == kGated) z[i] = *reinterpret_cast<const typename Vec4<T>::type*>(at(from.z.p, spot));
+  }
+  // what lies beyond the ends: zero (and act'(0) beside it)
+  __device__ __forceinline__ void clear_outside(int first, int64_t k, int64_t k_end, int c0, int c_end) {
+    if (k + kRound <= k_end && c0 + kCols <= c_end) return;
     const int lane = threadIdx.x & (kLanes - 1);
-    const int64_t k0 = k + 8 * (lane / 16);
-    const bool inside = c0 + 4 * (lane & 15) < c_end;
 #pragma unroll
-    for (int i = 0; i < 8; i += 2) {
-      float v[2];
+    for (int i = 0; i < kCount; ++i)
+      if (c0 + 4 * (lane & 15) >= c_end || k + 8 * (lane / 16) + first + i >= k_end) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        v[h] = raw.row[i + h].v[u];
-        if constexpr (kSource == kGated) v[h] *= from.gate.first(raw.row[i + h].z[u]);
-        if constexpr (kSource == kGated && kParts == 3) note_tiny(raw.row[i + h].v[u], low);
-        v[h] = inside && k0 + i + h < k_end ? v[h] : 0.f;   // rows beyond the end have no part
+        for (int u = 0; u < 4; ++u) {
+          v[i][u] = T(0.f);
+          if constexpr (kSource == kGated) z[i][u] = T(0.f);
+        }
       }
-      unsigned s[kParts], ignored = 0;
-      split<kParts>(v[0], v[1], s, kSource == kGated ? ignored : low);
-      if constexpr (kSum) sum += v[0] + v[1];
-#pragma unroll
-      for (int p = 0; p < kParts; ++p) part[p][i / 2] = s[p];
+  }
+  // the parts of rows first + i and first + i + 1 of tile u
+  template <int kParts, bool kSum>
+  __device__ __forceinline__ void pair(const Operand<float, T, kSource>& from, int i, int u, unsigned (&s)[kParts], float& sum, unsigned& low) const {
+    if constexpr (sizeof(T) == 2 && kSource == kPlain) {
+      static_assert(kParts == 1, "an element is one part");
+      const U2 a = __builtin_bit_cast(U2, v[i]), b = __builtin_bit_cast(U2, v[i + 1]);
+      s[0] = __builtin_amdgcn_perm(b[u / 2], a[u / 2], u & 1 ? 0x07060302 : 0x05040100);
+      if constexpr (kSum) sum += static_cast<float>(v[i][u]) + static_cast<float>(v[i + 1][u]);
+    } else {
+      float a = static_cast<float>(v[i][u]), b = static_cast<float>(v[i + 1][u]);
+      unsigned ignored = 0;
+      if constexpr (kSource == kGated) {
+        if constexpr (kParts == 3) note_tiny(a, low), note_tiny(b, low);
+        a *= from.gate.first(static_cast<float>(z[i][u]));
+        b *= from.gate.first(static_cast<float>(z[i + 1][u]));
+      }
+      if constexpr (kSum) sum += a + b;
+      split<kParts>(a, b, s, kSource == kGated ? ignored : low);
     }
   }
 };
 
-template <Source kSource, int kParts>
-struct PartsColumns<__bf16, kSource, kParts> {
-  static_assert(kSource == kGated || kParts == 1, "an element is one part");
-  Operand<float, __bf16, kSource> from;
-  struct Raw {
-    U2 v[8], z[kSource == kGated ? 8 : 1];
-  };
-  static __device__ __forceinline__ U2 load(const Matrix<__bf16>& m, int64_t row, int c, int c_end) {
-    typedef U2 Loose __attribute__((aligned(2)));
-    return *reinterpret_cast<const Loose*>(m.p + row * m.ld + min(c, c_end - 4));
+template <typename T, Source kSource, int kParts>
+struct PartsColumns {
+  Operand<float, T, kSource> from;
+  typedef ColumnsRaw<T, kSource, 8> Raw;
+  __device__ __forceinline__ void request(int64_t k, int64_t k_end, int c0, int c_end, Raw& raw) const { raw.request(from, 0, k, k_end, c0, c_end); }
+  __device__ __forceinline__ void clear_outside(int64_t k, int64_t k_end, int c0, int c_end, Raw& raw) const {
+    raw.clear_outside(0, k, k_end, c0, c_end);
   }
-  __device__ __forceinline__ void request(int64_t k, int64_t k_end, int c0, int c_end, Raw& raw) const {
-    const int lane = threadIdx.x & (kLanes - 1);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int64_t row = min(k + 8 * (lane / 16) + i, k_end - 1);
-      raw.v[i] = load(from.x, row, c0 + 4 * (lane & 15), c_end);
-      if constexpr (kSource == kGated) raw.z[i] = load(from.z, row, c0 + 4 * (lane & 15), c_end);
-    }
-  }
+  // tile u's operand; sum: adds the column's values
   template <bool kSum>
-  __device__ __forceinline__ void operand(const Raw& raw, int u, int64_t k, int64_t k_end, int c0, int c_end, U4 (&part)[kParts], float& sum,
-                                          unsigned& low) const {
-    const int lane = threadIdx.x & (kLanes - 1), w = u / 2;
-    const int64_t k0 = k + 8 * (lane / 16);
-    const bool inside = c0 + 4 * (lane & 15) < c_end;
-    auto half = [&](unsigned x) { return u & 1 ? el::high_half(x) : el::low_half(x); };
-    (void)low;
+  __device__ __forceinline__ void operand(const Raw& raw, int u, U4 (&part)[kParts], float& sum, unsigned& low) const {
 #pragma unroll
     for (int i = 0; i < 8; i += 2) {
-      const bool live_a = inside && k0 + i < k_end, live_b = inside && k0 + i + 1 < k_end;
-      const unsigned a = live_a ? raw.v[i][w] : 0u, b = live_b ? raw.v[i + 1][w] : 0u;
-      if constexpr (kSource == kPlain) {
-        part[0][i / 2] = __builtin_amdgcn_perm(b, a, u & 1 ? 0x07060302 : 0x05040100);
-        if constexpr (kSum) sum += half(a) + half(b);
-      } else {
-        float ga = half(a) * from.gate.first(half(raw.z[i][w])), gb = half(b) * from.gate.first(half(raw.z[i + 1][w]));
-        ga = live_a ? ga : 0.f;
-        gb = live_b ? gb : 0.f;
-        unsigned s[kParts], ignored = 0;
-        split<kParts>(ga, gb, s, ignored);
-        if constexpr (kSum) sum += ga + gb;
+      unsigned s[kParts];
+      raw.template pair<kParts, kSum>(from, i, u, s, sum, low);
 #pragma unroll
-        for (int p = 0; p < kParts; ++p) part[p][i / 2] = s[p];
-      }
+      for (int p = 0; p < kParts; ++p) part[p][i / 2] = s[p];
     }
   }
 };
@@ -268,38 +281,20 @@ __host__ __device__ constexpr int shared_words() { return 2 * kParts * kSharedPa
 template <typename T, Source kSource, int kParts>
 struct SharedColumns {
   Operand<float, T, kSource> from;
-  struct Raw {
-    typename Vec4<T>::type v[2], z[kSource == kGated ? 2 : 1];
-  };
+  typedef ColumnsRaw<T, kSource, 2> Raw;
   __device__ __forceinline__ void request(int wave, int64_t k, int64_t k_end, int c0, int c_end, Raw& raw) const {
-    const int lane = threadIdx.x & (kLanes - 1), c = min(c0 + 4 * (lane & 15), c_end - 4);
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int64_t row = min(k + 8 * (lane / 16) + 2 * wave + h, k_end - 1);
-      raw.v[h] = *reinterpret_cast<const typename Vec4<T>::type*>(from.x.p + row * from.x.ld + c);
-      if constexpr (kSource == kGated) raw.z[h] = *reinterpret_cast<const typename Vec4<T>::type*>(from.z.p + row * from.z.ld + c);
-    }
+    raw.request(from, 2 * wave, k, k_end, c0, c_end);
   }
   // sum: adds the columns' values
   template <bool kSum>
-  __device__ __forceinline__ void put(int wave, const Raw& raw, int64_t k, int64_t k_end, int c0, int c_end, unsigned* slot, float (&sum)[4],
+  __device__ __forceinline__ void put(int wave, Raw& raw, int64_t k, int64_t k_end, int c0, int c_end, unsigned* slot, float (&sum)[4],
                                       unsigned& low) const {
     const int lane = threadIdx.x & (kLanes - 1);
-    const bool inside = c0 + 4 * (lane & 15) < c_end;
-    const int64_t row = k + 8 * (lane / 16) + 2 * wave;
+    raw.clear_outside(2 * wave, k, k_end, c0, c_end);
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      float v[2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        v[h] = static_cast<float>(raw.v[h][u]);
-        if constexpr (kSource == kGated && kParts == 3) note_tiny(v[h], low);
-        if constexpr (kSource == kGated) v[h] *= from.gate.first(static_cast<float>(raw.z[h][u]));
-        v[h] = inside && row + h < k_end ? v[h] : 0.f;   // rows beyond the end have no part
-      }
-      if constexpr (kSum) sum[u] += v[0] + v[1];
-      unsigned s[kParts], ignored = 0;
-      split<kParts>(v[0], v[1], s, kSource == kGated ? ignored : low);
+      unsigned s[kParts];
+      raw.template pair<kParts, kSum>(from, 0, u, s, sum[u], low);
 #pragma unroll
       for (int p = 0; p < kParts; ++p) slot[((p * 4 + u) * kLanes + lane) * 4 + wave] = s[p];
     }
@@ -341,9 +336,11 @@ __device__ __forceinline__ bool rows_parts(const Rows& a, const Weights& w, int6
   typename Weights::Raw next;
   unsigned low = 0;
   float none[4];
+  const int64_t start = min(row0, rows - 1);   // (all rows beyond the last: the last one again)
+  const int left = static_cast<int>(min(rows - start, static_cast<int64_t>(16 * kRT)));
   auto request_rows = [&](int k) {
 #pragma unroll
-    for (int i = 0; i < kRT; ++i) a.request(row0 + 16 * i, rows, k, k_end, raw[i]);
+    for (int i = 0; i < kRT; ++i) a.request(start, left, k, k_end, raw[i], 16 * i);
   };
   w.request(wave, 0, k_end, n0, n_end, next);
   request_rows(0);
@@ -364,7 +361,11 @@ __device__ __forceinline__ bool rows_parts(const Rows& a, const Weights& w, int6
       U4 c[kW];
       get_shared<kW>(shared + at, u, c);
 #pragma unroll
-      for (int i = 0; i < kRT; ++i) multiply<kX, kW>(x[i], c, acc[i][u]);
+      for (int i = 0; i < kRT; ++i) {
+        Acc small = {0, 0, 0, 0};
+        multiply<kX, kW>(x[i], c, acc[i][u], small);
+        join<kX, kW>(acc[i][u], small);
+      }
     }
     Corner<float>::sync();
   }
@@ -389,8 +390,9 @@ __device__ __forceinline__ bool outer_parts(const A& a, const B& b, int m0, int 
     a.template put<false>(wave, ra, row, to, m0, m_end, shared + at, none, low);
     if (row + kRound < to) a.request(wave, row + kRound, to, m0, m_end, ra);
     U4 g[4][kB];
+    b.clear_outside(row, to, n0, n_end, rb);
 #pragma unroll
-    for (int u = 0; u < 4; ++u) b.template operand<true>(rb, u, row, to, n0, n_end, g[u], sum[u], low);
+    for (int u = 0; u < 4; ++u) b.template operand<true>(rb, u, g[u], sum[u], low);
     if (row + kRound < to) b.request(row + kRound, to, n0, n_end, rb);
     __syncthreads();
 #pragma unroll
@@ -398,7 +400,11 @@ __device__ __forceinline__ bool outer_parts(const A& a, const B& b, int m0, int 
       U4 x[kA];
       get_shared<kA>(shared + at, t, x);
 #pragma unroll
-      for (int u = 0; u < 4; ++u) multiply<kA, kB>(x, g[u], acc[t][u]);
+      for (int u = 0; u < 4; ++u) {
+        Acc small = {0, 0, 0, 0};
+        multiply<kA, kB>(x, g[u], acc[t][u], small);
+        join<kA, kB>(acc[t][u], small);
+      }
     }
   }
   return !any_wave(unserved<4, 4>(acc, low), shared);
@@ -433,7 +439,9 @@ __device__ __forceinline__ bool block_parts(const A& a, const B& b, int m0, int 
     for (int u = 0; u < 4; ++u) {
       U4 g[kB];
       get_shared<kB>(sb, u, g);
-      multiply<kA, kB>(x, g, acc[0][u]);
+      Acc small = {0, 0, 0, 0};
+      multiply<kA, kB>(x, g, acc[0][u], small);
+      join<kA, kB>(acc[0][u], small);
     }
   }
   return !any_wave(unserved<1, 4>(acc, low), shared_a);
@@ -455,14 +463,19 @@ struct PartsTransposed {
         load4<true>(from.p + min(c0 + 4 * (lane & 15) + u, c_end - 1) * from.ld, static_cast<int>(k) + 8 * (lane / 16) + 4 * h,
                     static_cast<int>(k_end), raw.v[u][h]);
   }
-  template <bool kSum>
-  __device__ __forceinline__ void operand(const Raw& raw, int u, int64_t k, int64_t k_end, int, int, U4 (&part)[kParts], float&, unsigned& low) const {
+  __device__ __forceinline__ void clear_outside(int64_t k, int64_t k_end, int, int, Raw& raw) const {
     const int64_t k0 = k + 8 * ((threadIdx.x & (kLanes - 1)) / 16);
 #pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) zero_unless(k0 + 4 * h < k_end, raw.v[u][h]);
+  }
+  template <bool kSum>
+  __device__ __forceinline__ void operand(const Raw& raw, int u, U4 (&part)[kParts], float&, unsigned& low) const {
+#pragma unroll
     for (int i = 0; i < 8; i += 2) {
-      const float a = k0 + i < k_end ? raw.v[u][i / 4][i % 4] : 0.f, b = k0 + i + 1 < k_end ? raw.v[u][i / 4][i % 4 + 1] : 0.f;
       unsigned s[kParts];
-      split<kParts>(a, b, s, low);
+      split<kParts>(raw.v[u][i / 4][i % 4], raw.v[u][i / 4][i % 4 + 1], s, low);
 #pragma unroll
       for (int p = 0; p < kParts; ++p) part[p][i / 2] = s[p];
     }
@@ -485,9 +498,10 @@ __device__ __forceinline__ void keep(const Weights& w, int n0, int n_end, int k_
   for (int r = 0; r < kRounds; ++r) {
     typename Weights::Raw raw;
     w.request(r * kRound, k_end, n0, n_end, raw);
+    w.clear_outside(r * kRound, k_end, n0, n_end, raw);
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      w.template operand<false>(raw, u, r * kRound, k_end, n0, n_end, kept.c[r][u], none, low);
+      w.template operand<false>(raw, u, kept.c[r][u], none, low);
 #pragma unroll
       for (int i = 0; i < 4; ++i)   // not finite (or beyond the largest bfloat16): 0 times the first part is a NaN
         mark = fmaf(el::low_half(kept.c[r][u][0][i]), 0.f, fmaf(el::high_half(kept.c[r][u][0][i]), 0.f, mark));
@@ -496,64 +510,92 @@ __device__ __forceinline__ void keep(const Weights& w, int n0, int n_end, int k_
   kept.served = __builtin_amdgcn_ballot_w64((low & 0xffffu) != 0 || mark != 0.f) == 0;
 }
 
-// Row tiles tile, tile + step, .. of a wave: finish(row0, acc, beside) for each, the rows of the next tile and what its epilogue reads requested
-// before the present one is computed.  again: the product of a tile that the parts do not serve.
-template <int kRounds, int kX, int kW, typename Rows, typename T, int N, typename Again, typename F>
-__device__ __forceinline__ void walk_rows(const Rows& a, const Kept<kRounds, kW>& kept, int64_t tile, int64_t step, int64_t rows, int n0, int n_end,
-                                          int k_end, unsigned* planes, const Beside<T, N>& beside, Again&& again, F&& finish) {
-  const int lane = threadIdx.x & (kLanes - 1), c = n0 + 4 * (lane & 15);
+// The row tiles of a wave, kWc at a time: finish(row, column, results, beside) for the rows of each.  kWc waves stand side by side along the columns and
+// share their rows: each puts the parts of one of the kWc tiles into LDS (two slots where they share: one barrier a turn, a wave that runs ahead
+// writes the other slot).  The rows of the next turn, and what the epilogue reads of the next tile, are requested before the present ones are
+// computed.  first: the group's first tile, step: from turn to turn, turns: the same for all waves of the workgroup; own: the wave's place among
+// the kWc.  again: the product of a tile that the parts do not serve.
+template <int kWc, int kRounds, int kX, int kW, typename Rows, typename T, int N, typename Again, typename F>
+__device__ __forceinline__ void walk_rows(const Rows& a, const Kept<kRounds, kW>& kept, int64_t first, int64_t step, int64_t turns, int own, int64_t rows,
+                                          int n0, int n_end, int k_end, unsigned* planes, unsigned* flags, const Beside<T, N>& beside, Again&& again,
+                                          F&& finish) {
+  constexpr int kTile = kRounds * kX * kPlane;   // words of a tile's planes
   constexpr int M = N > 0 ? N : 1;
+  const int lane = threadIdx.x & (kLanes - 1), c = n0 + 4 * (lane & 15);
   typename Rows::Raw raw[kRounds];
   typename Vec4<T>::type next[M][4];
-  auto request = [&](int64_t t) {
+  auto request = [&](int64_t tile) {
 #pragma unroll
-    for (int r = 0; r < kRounds; ++r) a.request(16 * t, rows, r * kRound, k_end, raw[r]);
+    for (int r = 0; r < kRounds; ++r) {
+      const int64_t row0 = min(16 * tile, rows - 1);
+      a.request(row0, static_cast<int>(min(rows - row0, static_cast<int64_t>(16))), r * kRound, k_end, raw[r], 0);
+    }
   };
-  auto request_beside = [&](int64_t t) {
+  auto request_beside = [&](int64_t tile) {
 #pragma unroll
     for (int e = 0; e < N; ++e)
       if (beside.m[e].p)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-          next[e][r] = *reinterpret_cast<const typename Vec4<T>::type*>(beside.m[e].p + min(16 * t + Mma<float>::row(lane, r), rows - 1) * beside.m[e].ld +
-                                                                        min(c, n_end - 4));
+        {
+          const int64_t row = min(16 * tile + r, rows - 1);
+          const unsigned lr = static_cast<unsigned>(min(static_cast<int64_t>(lane_row<float>()), rows - 1 - row));
+          next[e][r] = *reinterpret_cast<const typename Vec4<T>::type*>(
+              at(beside.m[e].p, Spot{row * beside.m[e].ld, lr * static_cast<unsigned>(beside.m[e].ld) + min(c, n_end - 4)}));
+        }
   };
-  if (16 * tile >= rows) return;
-  request(tile);
-  request_beside(tile);
-  for (; 16 * tile < rows; tile += step) {
+  request(first + own);
+  request_beside(first);
+  int slot = 0;
+  for (int64_t turn = 0; turn < turns; ++turn, first += step, slot = kWc > 1 ? slot ^ 1 : 0) {
+    unsigned* const here = planes + slot * kWc * kTile;
     unsigned low = 0;
 #pragma unroll
-    for (int r = 0; r < kRounds; ++r) a.put(raw[r], r * kRound, k_end, planes + r * kX * kPlane, low);
-    const bool more = 16 * (tile + step) < rows;
-    if (more) request(tile + step);
-    Corner<float>::sync();
-    Acc acc[1][4];
-#pragma unroll
-    for (int u = 0; u < 4; ++u) acc[0][u] = Acc{0, 0, 0, 0};
-#pragma unroll
-    for (int r = 0; r < kRounds; ++r) {
-      U4 x[kX];
-      get_parts<kX>(planes + r * kX * kPlane, x);
-#pragma unroll
-      for (int u = 0; u < 4; ++u) multiply<kX, kW>(x, kept.c[r][u], acc[0][u]);
+    for (int r = 0; r < kRounds; ++r) a.put(raw[r], r * kRound, k_end, here + own * kTile + r * kX * kPlane, low);
+    if constexpr (kWc > 1) {
+      const bool missed = __builtin_amdgcn_ballot_w64((low & 0xffffu) != 0) != 0;
+      if (lane == 0) flags[slot * kWc + own] = missed;
     }
-    Corner<float>::sync();
-    if (!kept.served || unserved<1, 4>(acc, low)) again(16 * tile, acc);
-    float x[4][M][4];
+    request(first + step + own);   // (beyond the last row the last one is read again)
+    if constexpr (kWc > 1) __syncthreads();
+    else Corner<float>::sync();
+#pragma unroll 1
+    for (int i = 0; i < kWc; ++i) {
+      const int64_t tile = first + i;
+      Acc acc[1][4], small[4];
 #pragma unroll
-    for (int e = 0; e < N; ++e)
+      for (int u = 0; u < 4; ++u) acc[0][u] = small[u] = Acc{0, 0, 0, 0};
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
+      for (int r = 0; r < kRounds; ++r) {
+        U4 x[kX];
+        get_parts<kX>(here + i * kTile + r * kX * kPlane, x);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[r][e][i] = static_cast<float>(next[e][r][i]);
-    if (more) request_beside(tile + step);
+        for (int u = 0; u < 4; ++u) multiply<kX, kW>(x, kept.c[r][u], acc[0][u], small[u]);
+      }
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int64_t row = 16 * tile + Mma<float>::row(lane, r);
-      const float v[4] = {acc[0][0][r], acc[0][1][r], acc[0][2][r], acc[0][3][r]};
-      if (row < rows && c < n_end) finish(row, c, v, x[r]);
+      for (int u = 0; u < 4; ++u) join<kX, kW>(acc[0][u], small[u]);
+      if constexpr (kWc > 1) low = flags[slot * kWc + i];
+      // (a row with a value that is not finite has a NaN in every column: the first tile's will do)
+      const Acc(&one)[1][1] = reinterpret_cast<const Acc(&)[1][1]>(acc[0][0]);
+      const bool served = kept.served && !unserved<1, 1>(one, low);
+      float x[4][M][4];
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) x[r][e][k] = static_cast<float>(next[e][r][k]);
+      request_beside(i + 1 < kWc ? tile + 1 : first + step);
+      if (!served && 16 * tile < rows) again(16 * tile, acc);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int64_t row = 16 * tile + r;
+        const int lr = lane_row<float>();
+        const float v[4] = {acc[0][0][r], acc[0][1][r], acc[0][2][r], acc[0][3][r]};
+        if (row + lr < rows && c < n_end) finish(row, lr, c, v, x[r]);
+      }
     }
+    if constexpr (kWc == 1) Corner<float>::sync();
   }
 }
 

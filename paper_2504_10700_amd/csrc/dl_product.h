@@ -12,6 +12,8 @@
 // An fp32 instruction of this shape occupies the matrix core for 32 cycles and an fp64 one for 64, so a wave that holds 64 x 32 or more results
 // needs less than 32 bytes a cycle and CU from the L1 cache: sharing the operands of several waves through LDS would save nothing.
 #pragma once
+#include <type_traits>
+
 #include "dl_gate.h"
 #include "el_tile.h"
 
@@ -37,6 +39,18 @@ struct Matrix {
   int64_t ld;
 };
 
+// Where a lane's elements lie: `base` elements from the start, the same for the whole wave, and `lane` further on.  Kept apart, the first is scalar
+// arithmetic and the second one register that does not change (the strides are limited so that it fits: DL_MAX_STRIDE).
+struct Spot {
+  int64_t base;
+  unsigned lane;
+};
+template <typename T>
+__device__ __forceinline__ T* at(T* p, const Spot& s) {
+  typedef std::conditional_t<std::is_const<T>::value, const char, char> Byte;
+  return reinterpret_cast<T*>(reinterpret_cast<Byte*>(p + s.base) + static_cast<size_t>(s.lane * static_cast<unsigned>(sizeof(T))));
+}
+
 // Four elements of a row from column c on.  kFours: the row's length is a multiple of four, so four elements are all inside or all
 // beyond the end; then the address is clamped and zeros are put in when the values are used, without a branch (requests behind branches
 // wait for each other).  Otherwise every element is tested.
@@ -58,17 +72,18 @@ __device__ __forceinline__ void zero_unless(bool inside, TA (&v)[4]) {
   for (int i = 0; i < 4; ++i) v[i] = inside ? v[i] : TA(0);
 }
 
+// p: where the first of them goes, column c of a row of `cols`.
 template <bool kFours, typename T, typename TA>
 __device__ __forceinline__ void store4(T* __restrict__ p, int c, int cols, const TA (&v)[4]) {
   if (kFours || c + 4 <= cols) {
     typename Vec4<T>::type x;
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[i] = static_cast<T>(v[i]);
-    *reinterpret_cast<typename Vec4<T>::type*>(p + c) = x;
+    *reinterpret_cast<typename Vec4<T>::type*>(p) = x;
   } else {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      if (c + i < cols) p[c + i] = static_cast<T>(v[i]);
+      if (c + i < cols) p[i] = static_cast<T>(v[i]);
   }
 }
 
@@ -218,11 +233,21 @@ struct Beside {
   Matrix<T> m[N > 0 ? N : 1];
 };
 
-// f(row, column, values of four neighbouring columns plus their bias, the same elements of the tensors beside) for a wave's results.
+// Rows row0 + base + lane of a tile's results r: fp32 lane 4 q, base r; fp64 lane q, base 4 r.
+template <typename TA>
+__device__ __forceinline__ int lane_row() {
+  const int q = (threadIdx.x & (kLanes - 1)) / 16;
+  return sizeof(TA) == 8 ? q : 4 * q;
+}
+template <typename TA>
+__device__ __forceinline__ constexpr int base_row(int r) { return sizeof(TA) == 8 ? 4 * r : r; }
+
+// f(base row, lane row, column, values of four neighbouring columns plus their bias, the same elements of the tensors beside) for a wave's
+// results.
 template <typename TA, int kRT, bool kFours, typename T, int N, typename F>
 __device__ __forceinline__ void each_four(int64_t row0, int64_t rows, int n0, int n_end, const typename Mma<TA>::acc_t (&acc)[kRT][4],
                                           const TA* __restrict__ bias, const Beside<T, N>& beside, F&& f) {
-  const int lane = threadIdx.x & (kLanes - 1), c = n0 + 4 * (lane & 15);
+  const int lane = threadIdx.x & (kLanes - 1), c = n0 + 4 * (lane & 15), lr = lane_row<TA>();
   constexpr int M = N > 0 ? N : 1;
   TA next[4][M][4];
   auto request = [&](int i) {
@@ -231,7 +256,7 @@ __device__ __forceinline__ void each_four(int64_t row0, int64_t rows, int n0, in
       if (beside.m[e].p)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-          load4<kFours>(beside.m[e].p + min(row0 + 16 * i + Mma<TA>::row(lane, r), rows - 1) * beside.m[e].ld, c, n_end, next[r][e]);
+          load4<kFours>(beside.m[e].p + min(row0 + 16 * i + base_row<TA>(r) + lr, rows - 1) * beside.m[e].ld, c, n_end, next[r][e]);
   };
   request(0);
   TA b[4] = {0, 0, 0, 0};
@@ -248,11 +273,11 @@ __device__ __forceinline__ void each_four(int64_t row0, int64_t rows, int n0, in
     if (i + 1 < kRT) request(i + 1);
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const int64_t row = row0 + 16 * i + Mma<TA>::row(lane, r);
+      const int64_t row = row0 + 16 * i + base_row<TA>(r);
       TA v[4];
 #pragma unroll
       for (int u = 0; u < 4; ++u) v[u] = acc[i][u][r] + b[u];
-      if (row < rows && c < n_end) f(row, c, v, x[r]);
+      if (row + lr < rows && c < n_end) f(row, lr, c, v, x[r]);
     }
   }
 }

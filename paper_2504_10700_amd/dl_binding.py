@@ -6,7 +6,7 @@ import ctypes as C
 from .binding import SC_BF16, SC_F32, SC_F64, ScError, _check, _ptr, _stream, lib  # noqa: F401
 
 DL_NONE, DL_RELU, DL_SILU, DL_GELU = 0, 1, 2, 3
-DL_MAX_WIDTH = 65536
+DL_MAX_WIDTH, DL_MAX_STRIDE = 65536, 33554432
 
 EXPORTS = ("dl_forward", "dl_workspace_bytes", "dl_backward", "dl_double_backward")
 

@@ -43,6 +43,8 @@ def test_dense_layer_refusals():
         refused(INVALID, dl.dl_workspace_bytes, bad, 10)
         refused(INVALID, dl.dl_forward, bad, 10, 16, 16, None, None, 16, None, stream=0)
     refused(UNSUPPORTED, dl.dl_workspace_bytes, dl.make_config(dl.DL_MAX_WIDTH + 1, 8), 10)
+    refused(UNSUPPORTED, dl.dl_workspace_bytes, dl.make_config(8, 8, ld_in=dl.DL_MAX_STRIDE + 1), 10)
+    refused(UNSUPPORTED, dl.dl_workspace_bytes, dl.make_config(8, 8, ld_out=dl.DL_MAX_STRIDE + 1), 10)
     refused(INVALID, dl.dl_workspace_bytes, good, -1)
     refused(INVALID, dl.dl_workspace_bytes, good, (1 << 30) + 1)
     short = dl.make_config(8, 64)
