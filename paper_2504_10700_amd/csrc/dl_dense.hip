@@ -108,7 +108,7 @@ __device__ __forceinline__ void finish_rows(const Rows& a, const Weights& w, int
       if (bias) load4<kFours>(bias, c, w.n_end, v);
 #pragma unroll
       for (int e = 0; e < N; ++e)
-        if (beside.m[e].p) load4<kFours>(beside.m[e].p + (row + lr) * beside.m[e].ld, c, w.n_end, x[e]);
+        load4<kFours>(beside.m[e].p + (row + lr) * beside.m[e].ld, c, w.n_end, x[e]);
       for (int p = 0; p < kN; ++p)
 #pragma unroll
         for (int i = 0; i < 4; ++i) sum[i] += lds[((p * 4 + wave) * 4 + i) * kLanes + lane];
@@ -135,14 +135,14 @@ __device__ __forceinline__ void each_tile(const Walk& walk, const Shape& shape, 
 }
 
 // What becomes of four neighbouring results v of a row.  The constructor takes what is the same for a lane's column.
-template <typename TS, typename TA, bool kFours>
+template <typename TS, typename TA, bool kFours, int kResidual>
 struct ForwardEnd {   // Z = v (bias added), Y = act(Z) + residual
   Gate<TA> gate;
   int64_t ld_out;
   int n_end;
   const TS* residual;
   TS *Y, *Z;
-  __device__ __forceinline__ Beside<TS, 1> beside() const { return {{{residual, ld_out}}}; }
+  __device__ __forceinline__ Beside<TS, kResidual> beside() const { return {{{residual, ld_out}}}; }
   __device__ __forceinline__ void operator()(int64_t row, int lr, int c, const TA (&z)[4], const TA (&x)[1][4]) const {
     const Spot spot{row * ld_out, static_cast<unsigned>(lr) * static_cast<unsigned>(ld_out) + c};
     TA y[4];
@@ -153,7 +153,7 @@ struct ForwardEnd {   // Z = v (bias added), Y = act(Z) + residual
 #pragma unroll
       for (int i = 0; i < 4; ++i) y[i] = gate.value(z[i]);
     }
-    if (residual) {
+    if constexpr (kResidual) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) y[i] += x[0][i];
     }
@@ -161,25 +161,29 @@ struct ForwardEnd {   // Z = v (bias added), Y = act(Z) + residual
   }
 };
 
-template <typename TS, typename TA, bool kFours>
-struct SecondEnd {   // v = V: ddY = V act'(Z), S = V dY act''(Z).  Z NULL: no activation; S NULL: no curvature
+// v = V: ddY = V act'(Z), S = V dY act''(Z).  kBeside 0: no activation; 1: no curvature (Z alone is read, no S); 2: Z and dY.
+template <typename TS, typename TA, bool kFours, int kBeside>
+struct SecondEnd {
   Gate<TA> gate;
   int64_t ld_out;
   int n_end;
   const TS *Z, *dY;
   TS* ddY;
   TA* S;
-  __device__ __forceinline__ Beside<TS, 2> beside() const { return {{{Z, ld_out}, {S ? dY : nullptr, ld_out}}}; }
-  __device__ __forceinline__ void operator()(int64_t row, int lr, int c, const TA (&v)[4], const TA (&x)[2][4]) const {
+  __device__ __forceinline__ Beside<TS, kBeside> beside() const {
+    if constexpr (kBeside == 2) return {{{Z, ld_out}, {dY, ld_out}}};
+    else return {{{Z, ld_out}}};
+  }
+  __device__ __forceinline__ void operator()(int64_t row, int lr, int c, const TA (&v)[4], const TA (&x)[kBeside > 0 ? kBeside : 1][4]) const {
     TA out[4], s[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       TA first = TA(1), second = TA(0);
-      if (Z) gate.both(x[0][i], &first, &second);
+      if constexpr (kBeside > 0) gate.both(x[0][i], &first, &second);
       out[i] = v[i] * first;
-      s[i] = v[i] * x[1][i] * second;
+      if constexpr (kBeside == 2) s[i] = v[i] * x[1][i] * second;
     }
-    if (S) store4<kFours>(at(S, Spot{row * n_end, static_cast<unsigned>(lr * n_end + c)}), c, n_end, s);
+    if constexpr (kBeside == 2) store4<kFours>(at(S, Spot{row * n_end, static_cast<unsigned>(lr * n_end + c)}), c, n_end, s);
     store4<kFours>(at(ddY, Spot{row * ld_out, static_cast<unsigned>(lr) * static_cast<unsigned>(ld_out) + c}), c, n_end, out);
   }
 };
@@ -812,18 +816,26 @@ struct Calls {
     return shape.wc == 1 ? launch(one, two) : shape.wc == 2 ? launch(two, two) : launch(four, two);
   }
 
-  hipError_t forward(const void* X, const void* W, const void* b, const void* residual, void* Y, void* Z) const {
+  template <int kResidual>
+  hipError_t forward_with(const void* X, const void* W, const void* b, const void* residual, void* Y, void* Z) const {
     return rows_times_w(X, W, b, [&](auto fours) {
-      return ForwardEnd<TS, TA, fours.value>{Gate<TA>::of(c->activation), ld_out(c), c->k_out, static_cast<const TS*>(residual), static_cast<TS*>(Y),
-                                             static_cast<TS*>(Z)};
+      return ForwardEnd<TS, TA, fours.value, kResidual>{Gate<TA>::of(c->activation), ld_out(c), c->k_out, static_cast<const TS*>(residual),
+                                                        static_cast<TS*>(Y), static_cast<TS*>(Z)};
     });
   }
+  hipError_t forward(const void* X, const void* W, const void* b, const void* residual, void* Y, void* Z) const {
+    return residual ? forward_with<1>(X, W, b, residual, Y, Z) : forward_with<0>(X, W, b, residual, Y, Z);
+  }
 
-  hipError_t v(const void* HX, const void* W, const void* Z, const void* dY, void* ddY, TA* S) const {
+  template <int kBeside>
+  hipError_t v_with(const void* HX, const void* W, const void* Z, const void* dY, void* ddY, TA* S) const {
     return rows_times_w(HX, W, nullptr, [&](auto fours) {
-      return SecondEnd<TS, TA, fours.value>{Gate<TA>::of(c->activation), ld_out(c), c->k_out, c->activation == DL_NONE ? nullptr : static_cast<const TS*>(Z),
-                                            static_cast<const TS*>(dY), static_cast<TS*>(ddY), S};
+      return SecondEnd<TS, TA, fours.value, kBeside>{Gate<TA>::of(c->activation), ld_out(c), c->k_out, static_cast<const TS*>(Z),
+                                                     static_cast<const TS*>(dY), static_cast<TS*>(ddY), S};
     });
+  }
+  hipError_t v(const void* HX, const void* W, const void* Z, const void* dY, void* ddY, TA* S) const {
+    return S ? v_with<2>(HX, W, Z, dY, ddY, S) : c->activation == DL_NONE ? v_with<0>(HX, W, Z, dY, ddY, S) : v_with<1>(HX, W, Z, dY, ddY, S);
   }
 
   // ws: [ W transposed ][ partial results ].

@@ -30,22 +30,30 @@ __device__ __forceinline__ Acc mma_parts(const U4& a, const U4& b, const Acc& c)
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(Bf8, a), __builtin_bit_cast(Bf8, b), c, 0, 0, 0);
 }
 
-// Adds a b: the product of the first parts to sum, the others to small (where no operand has three parts, all to sum).
-template <int NA, int NB>
-__device__ __forceinline__ void multiply(const U4 (&a)[NA], const U4 (&b)[NB], Acc& sum, Acc& small) {
+// Adds a(i) b(i) to sum[i], i = 0..3: the products of the first parts to sum, the others to small (where no operand has three parts, all to sum).
+// Product by product over the four, as each instruction waits for the one before it on the same sum.
+template <int NA, int NB, typename A, typename B>
+__device__ __forceinline__ void multiply4(A&& a, B&& b, Acc (&sum)[4], Acc (&small)[4]) {
 #pragma unroll
   for (int order = NA + NB - 2; order > 0; --order)
 #pragma unroll
     for (int p = NA - 1; p >= 0; --p)
       if (order - p >= 0 && order - p < NB && order < (NA > NB ? NA : NB)) {
-        Acc& to = NA == 3 || NB == 3 ? small : sum;
-        to = mma_parts(a[p], b[order - p], to);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          Acc& to = NA == 3 || NB == 3 ? small[i] : sum[i];
+          to = mma_parts(a(i)[p], b(i)[order - p], to);
+        }
       }
-  sum = mma_parts(a[0], b[0], sum);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) sum[i] = mma_parts(a(i)[0], b(i)[0], sum[i]);
 }
 template <int NA, int NB>
-__device__ __forceinline__ void join(Acc& sum, const Acc& small) {
-  if constexpr (NA == 3 || NB == 3) sum += small;
+__device__ __forceinline__ void join4(Acc (&sum)[4], const Acc (&small)[4]) {
+  if constexpr (NA == 3 || NB == 3) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum[i] += small[i];
+  }
 }
 
 // Pairs of values into parts, in the halves of a register each.  low: collects what the last part is rounded from (el::split_pair).
@@ -360,12 +368,12 @@ __device__ __forceinline__ bool rows_parts(const Rows& a, const Weights& w, int6
     for (int u = 0; u < 4; ++u) {
       U4 c[kW];
       get_shared<kW>(shared + at, u, c);
+      static_assert(kRT == 4, "four sums at a time");
+      Acc sum[4] = {acc[0][u], acc[1][u], acc[2][u], acc[3][u]}, small[4] = {};
+      multiply4<kX, kW>([&](int i) -> const U4(&)[kX] { return x[i]; }, [&](int) -> const U4(&)[kW] { return c; }, sum, small);
+      join4<kX, kW>(sum, small);
 #pragma unroll
-      for (int i = 0; i < kRT; ++i) {
-        Acc small = {0, 0, 0, 0};
-        multiply<kX, kW>(x[i], c, acc[i][u], small);
-        join<kX, kW>(acc[i][u], small);
-      }
+      for (int i = 0; i < kRT; ++i) acc[i][u] = sum[i];
     }
     Corner<float>::sync();
   }
@@ -399,12 +407,9 @@ __device__ __forceinline__ bool outer_parts(const A& a, const B& b, int m0, int 
     for (int t = 0; t < 4; ++t) {
       U4 x[kA];
       get_shared<kA>(shared + at, t, x);
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        Acc small = {0, 0, 0, 0};
-        multiply<kA, kB>(x, g[u], acc[t][u], small);
-        join<kA, kB>(acc[t][u], small);
-      }
+      Acc small[4] = {};
+      multiply4<kA, kB>([&](int) -> const U4(&)[kA] { return x; }, [&](int u) -> const U4(&)[kB] { return g[u]; }, acc[t], small);
+      join4<kA, kB>(acc[t], small);
     }
   }
   return !any_wave(unserved<4, 4>(acc, low), shared);
@@ -435,14 +440,12 @@ __device__ __forceinline__ bool block_parts(const A& a, const B& b, int m0, int 
     __syncthreads();
     U4 x[kA];
     get_shared<kA>(sa, wave, x);
+    U4 g[4][kB];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      U4 g[kB];
-      get_shared<kB>(sb, u, g);
-      Acc small = {0, 0, 0, 0};
-      multiply<kA, kB>(x, g, acc[0][u], small);
-      join<kA, kB>(acc[0][u], small);
-    }
+    for (int u = 0; u < 4; ++u) get_shared<kB>(sb, u, g[u]);
+    Acc small[4] = {};
+    multiply4<kA, kB>([&](int) -> const U4(&)[kA] { return x; }, [&](int u) -> const U4(&)[kB] { return g[u]; }, acc[0], small);
+    join4<kA, kB>(acc[0], small);
   }
   return !any_wave(unserved<1, 4>(acc, low), shared_a);
 }
@@ -460,7 +463,7 @@ struct PartsTransposed {
     for (int u = 0; u < 4; ++u)
 #pragma unroll
       for (int h = 0; h < 2; ++h)
-        load4<true>(from.p + min(c0 + 4 * (lane & 15) + u, c_end - 1) * from.ld, static_cast<int>(k) + 8 * (lane / 16) + 4 * h,
+        load4<true>(from.p + (min(c0 + 4 * (lane & 15), c_end - 4) + u) * from.ld, static_cast<int>(k) + 8 * (lane / 16) + 4 * h,
                     static_cast<int>(k_end), raw.v[u][h]);
   }
   __device__ __forceinline__ void clear_outside(int64_t k, int64_t k_end, int, int, Raw& raw) const {
@@ -498,7 +501,7 @@ __device__ __forceinline__ void keep(const Weights& w, int n0, int n_end, int k_
   for (int r = 0; r < kRounds; ++r) {
     typename Weights::Raw raw;
     w.request(r * kRound, k_end, n0, n_end, raw);
-    w.clear_outside(r * kRound, k_end, n0, n_end, raw);
+    w.clear_outside(r * kRound, k_end, 0, kCols, raw);   // (of the reduced indices; lanes beyond the last column hold its four again)
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       w.template operand<false>(raw, u, kept.c[r][u], none, low);
@@ -534,10 +537,8 @@ __device__ __forceinline__ void walk_rows(const Rows& a, const Kept<kRounds, kW>
   auto request_beside = [&](int64_t tile) {
 #pragma unroll
     for (int e = 0; e < N; ++e)
-      if (beside.m[e].p)
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-        {
+        for (int r = 0; r < 4; ++r) {
           const int64_t row = min(16 * tile + r, rows - 1);
           const unsigned lr = static_cast<unsigned>(min(static_cast<int64_t>(lane_row<float>()), rows - 1 - row));
           next[e][r] = *reinterpret_cast<const typename Vec4<T>::type*>(
@@ -547,7 +548,10 @@ __device__ __forceinline__ void walk_rows(const Rows& a, const Kept<kRounds, kW>
   request(first + own);
   request_beside(first);
   int slot = 0;
-  for (int64_t turn = 0; turn < turns; ++turn, first += step, slot = kWc > 1 ? slot ^ 1 : 0) {
+  // The last turn alone can meet rows beyond the last.  In the others nothing is written conditionally: where a store may be left out, the next
+  // request's arrival is only known once all stores are done.
+  auto turn = [&](auto last, auto live) {   // live: the wave has columns
+    constexpr bool kLast = decltype(last)::value;
     unsigned* const here = planes + slot * kWc * kTile;
     unsigned low = 0;
 #pragma unroll
@@ -556,10 +560,11 @@ __device__ __forceinline__ void walk_rows(const Rows& a, const Kept<kRounds, kW>
       const bool missed = __builtin_amdgcn_ballot_w64((low & 0xffffu) != 0) != 0;
       if (lane == 0) flags[slot * kWc + own] = missed;
     }
-    request(first + step + own);   // (beyond the last row the last one is read again)
+    if constexpr (!kLast) request(first + step + own);
     if constexpr (kWc > 1) __syncthreads();
     else Corner<float>::sync();
-#pragma unroll 1
+    if constexpr (!decltype(live)::value) return;
+#pragma unroll
     for (int i = 0; i < kWc; ++i) {
       const int64_t tile = first + i;
       Acc acc[1][4], small[4];
@@ -569,11 +574,9 @@ __device__ __forceinline__ void walk_rows(const Rows& a, const Kept<kRounds, kW>
       for (int r = 0; r < kRounds; ++r) {
         U4 x[kX];
         get_parts<kX>(here + i * kTile + r * kX * kPlane, x);
-#pragma unroll
-        for (int u = 0; u < 4; ++u) multiply<kX, kW>(x, kept.c[r][u], acc[0][u], small[u]);
+        multiply4<kX, kW>([&](int) -> const U4(&)[kX] { return x; }, [&](int u) -> const U4(&)[kW] { return kept.c[r][u]; }, acc[0], small);
       }
-#pragma unroll
-      for (int u = 0; u < 4; ++u) join<kX, kW>(acc[0][u], small[u]);
+      join4<kX, kW>(acc[0], small);
       if constexpr (kWc > 1) low = flags[slot * kWc + i];
       // (a row with a value that is not finite has a NaN in every column: the first tile's will do)
       const Acc(&one)[1][1] = reinterpret_cast<const Acc(&)[1][1]>(acc[0][0]);
@@ -585,18 +588,24 @@ __device__ __forceinline__ void walk_rows(const Rows& a, const Kept<kRounds, kW>
         for (int r = 0; r < 4; ++r)
 #pragma unroll
           for (int k = 0; k < 4; ++k) x[r][e][k] = static_cast<float>(next[e][r][k]);
-      request_beside(i + 1 < kWc ? tile + 1 : first + step);
+      if (!kLast || i + 1 < kWc) request_beside(i + 1 < kWc ? tile + 1 : first + step);
       if (!served && 16 * tile < rows) again(16 * tile, acc);
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int64_t row = 16 * tile + r;
         const int lr = lane_row<float>();
         const float v[4] = {acc[0][0][r], acc[0][1][r], acc[0][2][r], acc[0][3][r]};
-        if (row + lr < rows && c < n_end) finish(row, lr, c, v, x[r]);
+        if (!kLast || row + lr < rows) finish(row, lr, min(c, n_end - 4), v, x[r]);   // lanes beyond the last column repeat its four
       }
     }
     if constexpr (kWc == 1) Corner<float>::sync();
-  }
+  };
+  auto all = [&](auto live) {
+    for (int64_t t = 1; t < turns; ++t, first += step, slot = kWc > 1 ? slot ^ 1 : 0) turn(std::false_type{}, live);
+    turn(std::true_type{}, live);
+  };
+  if (kWc == 1 || n0 < n_end) all(std::true_type{});
+  else if constexpr (kWc > 1) all(std::false_type{});
 }
 
 }  // namespace dl

@@ -227,7 +227,7 @@ __device__ __forceinline__ void rows_product(const Rows& a, const Weights& w, in
   }
 }
 
-// Tensors with a row per result row that the epilogue reads (residual; Z and dY): requested a row tile ahead.  p NULL: not there.
+// Tensors with a row per result row that the epilogue reads (residual; Z and dY): requested a row tile ahead.
 template <typename T, int N>
 struct Beside {
   Matrix<T> m[N > 0 ? N : 1];
@@ -253,10 +253,9 @@ __device__ __forceinline__ void each_four(int64_t row0, int64_t rows, int n0, in
   auto request = [&](int i) {
 #pragma unroll
     for (int e = 0; e < N; ++e)
-      if (beside.m[e].p)
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-          load4<kFours>(beside.m[e].p + min(row0 + 16 * i + base_row<TA>(r) + lr, rows - 1) * beside.m[e].ld, c, n_end, next[r][e]);
+      for (int r = 0; r < 4; ++r)
+        load4<kFours>(beside.m[e].p + min(row0 + 16 * i + base_row<TA>(r) + lr, rows - 1) * beside.m[e].ld, c, n_end, next[r][e]);
   };
   request(0);
   TA b[4] = {0, 0, 0, 0};
