@@ -56,6 +56,14 @@ __device__ __forceinline__ void join4(Acc (&sum)[4], const Acc (&small)[4]) {
   }
 }
 
+// dY act'(z), rounded to fp32 as a value of its own: contracted with the subtraction of its first part it would be one with more bits than three
+// parts hold.
+__device__ __forceinline__ float gated(const Gate<float>& gate, float x, float z) {
+#pragma clang fp contract(off)
+  const float g = x * Gate<float>::cut(gate.first(z));
+  return g;
+}
+
 // Pairs of values into parts, in the halves of a register each.  low: collects what the last part is rounded from (el::split_pair).
 template <int N>
 __device__ __forceinline__ void split(float x, float y, unsigned (&part)[N], unsigned& low) {
@@ -66,13 +74,6 @@ __device__ __forceinline__ void split(float x, float y, unsigned (&part)[N], uns
     part[0] = pack_bf16(x, y);
     if constexpr (N == 2) part[1] = pack_bf16(x - el::low_half(part[0]), y - el::high_half(part[0]));
   }
-}
-
-// Notes an element whose size the parts do not reach: not zero and below 2^-100 (for what is multiplied by act' afterwards: a product that
-// becomes small there does not count beside the others).
-__device__ __forceinline__ void note_tiny(float x, unsigned& low) {
-  const unsigned b = __builtin_bit_cast(unsigned, x) & 0x7fffffffu;
-  low |= b - 1u < 0x0d800000u - 1u ? 1u : 0u;
 }
 
 // Rows as an operand: 16 rows x 32 reduced indices in kParts planes of the wave's corner of LDS (16 rows of 64 bytes each, the four pieces of a
@@ -128,14 +129,11 @@ struct PartsRows<float, kSource, kParts> {
       if constexpr (kSource == kGated) {
         const bool inside = k + column() < k_end;   // (0 times what stands beyond the end may be a NaN)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if constexpr (kParts == 3) note_tiny(v[i], low);
-          v[i] = inside ? v[i] * from.gate.first(raw.z[h][i]) : 0.f;
-        }
+        for (int i = 0; i < 4; ++i) v[i] = inside ? gated(from.gate, v[i], raw.z[h][i]) : 0.f;
       }
-      unsigned ignored = 0, a[kParts], b[kParts];
-      split<kParts>(v[0], v[1], a, kSource == kGated ? ignored : low);
-      split<kParts>(v[2], v[3], b, kSource == kGated ? ignored : low);
+      unsigned a[kParts], b[kParts];
+      split<kParts>(v[0], v[1], a, low);
+      split<kParts>(v[2], v[3], b, low);
       const int to = piece_at(8 * h + lane / 8, lane % 8 / 2) + 2 * (lane & 1);
 #pragma unroll
       for (int p = 0; p < kParts; ++p) *reinterpret_cast<U2*>(planes + p * kPlane + to) = U2{a[p], b[p]};
@@ -166,8 +164,8 @@ struct PartsRows<__bf16, kSource, kParts> {
     } else {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float x = el::low_half(raw.v[i]) * from.gate.first(el::low_half(raw.z[i]));
-        const float y = el::high_half(raw.v[i]) * from.gate.first(el::high_half(raw.z[i]));
+        const float x = gated(from.gate, el::low_half(raw.v[i]), el::low_half(raw.z[i]));
+        const float y = gated(from.gate, el::high_half(raw.v[i]), el::high_half(raw.z[i]));
         unsigned s[kParts], ignored = 0;
         split<kParts>(inside ? x : 0.f, inside ? y : 0.f, s, ignored);
 #pragma unroll
@@ -234,14 +232,12 @@ struct ColumnsRaw {
       if constexpr (kSum) sum += static_cast<float>(v[i][u]) + static_cast<float>(v[i + 1][u]);
     } else {
       float a = static_cast<float>(v[i][u]), b = static_cast<float>(v[i + 1][u]);
-      unsigned ignored = 0;
       if constexpr (kSource == kGated) {
-        if constexpr (kParts == 3) note_tiny(a, low), note_tiny(b, low);
-        a *= from.gate.first(static_cast<float>(z[i][u]));
-        b *= from.gate.first(static_cast<float>(z[i + 1][u]));
+        a = gated(from.gate, a, static_cast<float>(z[i][u]));
+        b = gated(from.gate, b, static_cast<float>(z[i + 1][u]));
       }
       if constexpr (kSum) sum += a + b;
-      split<kParts>(a, b, s, kSource == kGated ? ignored : low);
+      split<kParts>(a, b, s, low);
     }
   }
 };
@@ -381,7 +377,7 @@ __device__ __forceinline__ bool rows_parts(const Rows& a, const Weights& w, int6
 }
 
 // outer_product on parts: acc[t][u] of the wave's 64 columns from n0 and the 64 rows from m0 of dW that the four waves share.
-template <int kA, int kB, typename A, typename B>
+template <int kA, int kB, bool kSum, typename A, typename B>
 __device__ __forceinline__ bool outer_parts(const A& a, const B& b, int m0, int m_end, int n0, int n_end, int64_t from, int64_t to,
                                             unsigned* shared, Acc (&acc)[4][4], float (&sum)[4]) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
@@ -400,7 +396,7 @@ __device__ __forceinline__ bool outer_parts(const A& a, const B& b, int m0, int 
     U4 g[4][kB];
     b.clear_outside(row, to, n0, n_end, rb);
 #pragma unroll
-    for (int u = 0; u < 4; ++u) b.template operand<true>(rb, u, g[u], sum[u], low);
+    for (int u = 0; u < 4; ++u) b.template operand<kSum>(rb, u, g[u], sum[u], low);
     if (row + kRound < to) b.request(row + kRound, to, n0, n_end, rb);
     __syncthreads();
 #pragma unroll

@@ -1,0 +1,186 @@
+// How the dense layer's work is cut: what launches, workspace and kernels agree on.
+#pragma once
+#include <algorithm>
+
+#include "dl_parts.h"
+
+namespace dl {
+
+using sc::align_up;
+
+constexpr int kXcds = 8;
+
+// Waves that share one result where rows are few (the registers of an fp64 wave leave room for four).
+template <typename TA>
+__host__ __device__ constexpr int split_waves() { return sizeof(TA) == 8 ? 4 : 8; }
+template <bool kSplit, typename TA>
+constexpr int threads() { return kSplit ? split_waves<TA>() * kLanes : kThreads; }
+// LDS of a product of rows: the waves' corners, or their results where they share one.
+template <bool kSplit, int kRT, typename TA>
+constexpr int lds_elements() { return kSplit ? split_waves<TA>() * 16 * kLanes : kWaves * kRT * Corner<TA>::kBlock; }
+
+// How a workgroup's waves stand: wc side by side along the columns, the others along the rows.
+struct Shape {
+  int wc, wr;
+};
+
+// Row groups x column groups of workgroups.  All column groups of a row group go to one XCD (workgroups are dealt out to the XCDs in turn), whose
+// L2 then holds the rows that they share.
+struct Walk {
+  int64_t row_groups;
+  int col_groups;
+  __host__ __device__ int64_t count() const { return (row_groups + kXcds - 1) / kXcds * kXcds * col_groups; }
+  __device__ bool at(int64_t t, int64_t* row, int* col) const {
+    const int64_t local = t / kXcds;
+    *row = local / col_groups * kXcds + t % kXcds;
+    *col = static_cast<int>(local % col_groups);
+    return *row < row_groups;
+  }
+};
+
+
+constexpr int kPartsTiles = 4;   // row tiles of a wave
+
+// What a launch of the backward does: the rows in chunks, of each chunk first dx_groups workgroups of dX, then dw_groups of the chunk's partial dW and
+// db.  A chunk stays on one XCD and its two halves run at about the same time: the second reading of dY (and Z) comes from the caches.
+struct Plan {
+  int64_t rows, per;    // per: rows of a chunk, a multiple of 64
+  int64_t chunks;
+  int64_t dx_groups, dw_groups;   // workgroups of a chunk
+  int dx_col_groups, dw_col_groups;
+  Shape dx, dw;
+  int64_t stride;       // elements between the chunks' partial results
+};
+
+// ---- host side
+
+inline size_t row_size(const dl_config* c) { return c->dtype == SC_F64 ? 8 : c->dtype == SC_F32 ? 4 : 2; }
+inline size_t weight_size(const dl_config* c) { return c->dtype == SC_F64 ? 8 : 4; }
+inline int64_t ld_in(const dl_config* c) { return c->ld_in ? c->ld_in : c->k_in; }
+inline int64_t ld_out(const dl_config* c) { return c->ld_out ? c->ld_out : c->k_out; }
+
+inline int64_t blocks_of(int64_t n, int64_t size) { return (n + size - 1) / size; }
+
+// Waves side by side along the columns: as many as there are column blocks, up to four.
+inline Shape shape_of(int cols) {
+  const int64_t blocks = blocks_of(cols, kCols);
+  return blocks >= 3 ? Shape{4, 1} : blocks == 2 ? Shape{2, 2} : Shape{1, 4};
+}
+
+// Row tiles of a wave: the fewer the rows the fewer, so that there are two waves for every SIMD of 256 CUs as long as possible.
+inline int row_tiles(int64_t rows, int cols, int most) {
+  const int64_t waves = blocks_of(rows, 16) * blocks_of(cols, kCols);
+  int rt = 1;
+  while (rt < most && waves / (2 * rt) >= 2048) rt *= 2;
+  return rt;
+}
+
+// Do all waves of a workgroup share one tile?  Where there is at most one row tile for every SIMD and the sum is long.
+inline bool split_sum(int64_t rows, int cols, int k) { return k >= 128 && blocks_of(rows, 16) * blocks_of(cols, kCols) <= 1024; }
+
+inline Plan plan_of(const dl_config* c, int64_t n, bool want_dx, bool want_dw, bool split, int rt) {
+  const int split_waves = c->dtype == SC_F64 ? dl::split_waves<double>() : dl::split_waves<float>();
+  Plan p{};
+  p.rows = n;
+  p.dw = shape_of(c->k_out);
+  if (split) p.dw = {1, split_waves};
+  const int64_t blocks = blocks_of(c->k_in, kCols) * blocks_of(c->k_out, kCols);
+  // about 2048 waves of dW, none with less than 32 rows
+  const int64_t chunks = std::max<int64_t>(1, std::min(2048 / (blocks * p.dw.wr), n / (32 * p.dw.wr)));
+  p.per = blocks_of(n, chunks);
+  p.per = blocks_of(p.per, p.per < 256 ? 64 : 256) * (p.per < 256 ? 64 : 256);
+  p.chunks = blocks_of(n, p.per);
+  p.dx = split ? Shape{1, 1} : shape_of(c->k_in);
+  p.dx_col_groups = static_cast<int>(blocks_of(c->k_in, kCols * p.dx.wc));
+  p.dx_groups = want_dx ? blocks_of(p.per, split ? 16 : 16 * rt * p.dx.wr) * p.dx_col_groups : 0;
+  p.dw_col_groups = static_cast<int>(blocks_of(c->k_out, kCols * p.dw.wc));
+  p.dw_groups = want_dw ? blocks_of(c->k_in, kCols) * p.dw_col_groups : 0;
+  p.stride = static_cast<int64_t>(c->k_in) * c->k_out + c->k_out;
+  return p;
+}
+
+inline bool curved(const dl_config* c) { return c->activation == DL_SILU || c->activation == DL_GELU; }
+
+// Do the bfloat16 matrix cores serve a product of rows (dl_parts.h)?
+inline bool in_parts(const dl_config* c, int64_t n, int cols, int k) {
+  // (the lanes' places in 64 rows are 32-bit byte offsets)
+  if (ld_in(c) > (1 << 22) || ld_out(c) > (1 << 22)) return false;
+  if (c->dtype == SC_F64 || c->k_in % 4 != 0 || c->k_out % 4 != 0 || k <= 16 || (c->dtype == SC_BF16 && k % 8 != 0)) return false;
+  return blocks_of(n, 64) * blocks_of(cols, kCols) >= 1024;
+}
+
+// Do the waves keep W (walk_rows)?  Its parts of up to 64 reduced indices fit the registers.
+inline bool kept_ok(const dl_config* c, int64_t n, int cols, int k) { return k <= 2 * kRound && in_parts(c, n, cols, k); }
+
+// Is a wave's share of dW 64 x 64 (parts_dw_role)?
+inline bool wide_parts(const dl_config* c) { return c->k_out > 2 * kCols; }
+
+inline Plan parts_plan(const dl_config* c, int64_t n, bool want_dx, bool want_dw) {
+  Plan p{};
+  p.rows = n;
+  const bool wide = wide_parts(c);
+  p.dw = {wide ? kWaves : 1, 1};
+  p.dw_col_groups = static_cast<int>(blocks_of(c->k_out, kCols * p.dw.wc));
+  const int64_t groups = blocks_of(c->k_in, kCols) * p.dw_col_groups;
+  // Of dW alone as many workgroups as the chip has places for, two a CU (64 x 64 blocks: three) and the same for every XCD: one more would run when
+  // the others are done.  None with less than 256 rows.  (990 001 rows, 64 -> 1280: 65 workgroups on an XCD with 64 places 1640 us, 60 1190.)
+  const int64_t places = wide ? 64 : 96;
+  int64_t chunks = groups <= places ? places / groups * kXcds : kXcds * blocks_of(places, groups);
+  chunks = std::max<int64_t>(1, std::min<int64_t>(chunks, n / 256));
+  // With dX beside it no more than 4 MB of dY, so that what the workgroups of the chip read twice at a time stays in the caches: 990 001 rows of
+  // bfloat16, 64 -> 1280, 1325 us with 26 MB, 1120 with 10, 1017 with 4.
+  if (want_dx && want_dw) chunks = std::max(chunks, blocks_of(n * c->k_out * static_cast<int64_t>(row_size(c)), 4 << 20));
+  const int64_t unit = want_dx ? 256 : 32;
+  p.per = blocks_of(blocks_of(n, chunks), unit) * unit;
+  p.chunks = blocks_of(n, p.per);
+  p.dx = {1, kWaves};
+  p.dx_col_groups = static_cast<int>(blocks_of(c->k_in, kCols));
+  p.dx_groups = want_dx ? blocks_of(p.per, 16 * kPartsTiles * kWaves) * p.dx_col_groups : 0;
+  p.dw_groups = want_dw ? groups : 0;
+  p.stride = static_cast<int64_t>(c->k_in) * c->k_out + c->k_out;
+  return p;
+}
+
+// Is G made first?  It would be made again for every column block of dX, which then takes longer than its writing and reading; in fp64, whose
+// exponential is some sixty instructions of half the rate, always but for the smallest batches.
+inline bool g_first(const dl_config* c, int64_t n) {
+  if (c->activation == DL_NONE) return false;
+  return c->dtype == SC_F64 ? n >= 1024 : c->k_in > kCols && in_parts(c, n, c->k_in, c->k_out);
+}
+
+// Workspace: [ S of the second-order pass, or G of the backward ][ G of the second-order pass ][ W transposed ][ partial dW and db per chunk ].
+inline size_t s_bytes(const dl_config* c, int64_t n) {
+  return curved(c) || g_first(c, n) ? align_up(static_cast<size_t>(n) * c->k_out * weight_size(c), 256) : 0;
+}
+
+// Does dX take W transposed (a launch of its own, 2 us)?  Where the reading of W as it is, four times the accesses, would take longer.
+inline bool transposed(int64_t n, const dl_config* c) { return n >= 4096 || in_parts(c, n, c->k_in, c->k_out); }
+
+inline size_t wt_bytes(int64_t n, const dl_config* c) {
+  return transposed(n, c) ? align_up(static_cast<size_t>(c->k_in) * c->k_out * weight_size(c), 256) : 0;
+}
+
+inline size_t workspace_bytes(const dl_config* c, int64_t n) {
+  if (n == 0) return 256;
+  int64_t chunks = std::max(parts_plan(c, n, true, true).chunks, parts_plan(c, n, false, true).chunks);
+  for (bool split : {false, true}) chunks = std::max(chunks, plan_of(c, n, true, true, split, 1).chunks);
+  return (curved(c) && g_first(c, n) ? 2 : 1) * s_bytes(c, n) + wt_bytes(n, c) + align_up(static_cast<size_t>(chunks) * plan_of(c, n, true, true, false, 1).stride * weight_size(c), 256) +
+         256;
+}
+
+
+// The calls of one type (dl_calls.h).  c and the tensors have been checked; sum_chunks without chunks writes zeros.
+struct Entries {
+  hipError_t (*forward)(const dl_config* c, int64_t n, hipStream_t stream, const void* X, const void* W, const void* b, const void* residual, void* Y,
+                        void* Z);
+  hipError_t (*backward)(const dl_config* c, int64_t n, hipStream_t stream, const void* X, const void* W, const void* Z, const void* dY, void* dX,
+                         void* dW, void* db, void* ws);
+  hipError_t (*double_backward)(const dl_config* c, int64_t n, hipStream_t stream, const void* X, const void* W, const void* Z, const void* dY,
+                                const void* HX, void* ddY, void* X2, void* W2, void* b2, void* ws);
+  hipError_t (*zero)(const dl_config* c, hipStream_t stream, void* dW, void* db);
+};
+Entries entries_f32();
+Entries entries_f64();
+Entries entries_bf16();
+
+}  // namespace dl
