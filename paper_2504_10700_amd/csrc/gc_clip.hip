@@ -1,11 +1,13 @@
 // Global gradient norm over a list of tensors, and clipping (include/gc.h).
 //
 // Both passes stream the tensors once and are bound by memory.  The list travels as kernel arguments, kItems tensors a launch; its
-// elements are cut into chunks of kChunk that the workgroups take in turn, so a list of many small tensors costs as few workgroups
+// elements are cut into chunks that the workgroups take in turn, so a list of many small tensors costs as few workgroups
 // as one large one.  First pass: a partial sum of squares per workgroup, in fp64 (a 4-byte element costs one conversion and one fp64
 // fused multiply-add, far below what the memory takes).  Second pass: with one launch's partials every workgroup of the scaling sums
 // them itself in a fixed order (at most kPartials, 8 KB from the caches) - cheaper than a launch between the two; longer lists
-// have one.
+// have one.  The second pass goes through the list from its end, where the first has just been, and its results pass by the caches, so what
+// is still in them is read from there.  Measured: 1.5 M elements of a two-layer model 13 us; 85 M of 24 layers 297 us, 3.4 TB/s over both passes
+// and the writes (325 us in list order with ordinary stores).
 #include <algorithm>
 #include <cmath>
 
@@ -21,7 +23,8 @@ using sc::set_error;
 
 constexpr int kThreads = 256;
 constexpr int kItems = 96;          // tensors of one launch: 3.9 KB of kernel arguments
-constexpr int kChunk = 4096;        // elements a workgroup takes at a time
+constexpr int kLongChunk = 8192;    // elements a workgroup takes at a time from long lists ...
+constexpr int kShortChunk = 2048;   // ... and from lists that would leave places empty (1.5 M elements: 18.2 us with the long ones, 13.1 with these)
 constexpr int kPartials = 1024;     // workgroups of one launch of the first pass
 
 struct Item {
@@ -57,7 +60,7 @@ __device__ __forceinline__ const Item& item_of(const Batch& b, int64_t chunk) {
 }
 
 // f(src, n) once per full vector of the chunk and per left-over element, all vectors of a thread requested before the first is used.
-template <typename T, typename F>
+template <int kChunk, typename T, typename F>
 __device__ __forceinline__ void each_vector(const T* __restrict__ src, int64_t n, F&& f) {
   constexpr int N = Vec<T>::kN, kRounds = kChunk / (kThreads * N);
   typedef typename Vec<T>::type V;
@@ -83,8 +86,9 @@ struct Square {
   }
 };
 
-template <typename T>
-__device__ __forceinline__ void scale_chunk(const T* __restrict__ src, T* __restrict__ dst, int64_t n, double coefficient) {
+// (The results go past the caches, which hold the end of what the first pass read.)
+template <int kChunk, typename T>
+__device__ __forceinline__ void scale_chunk(const T* src, T* dst, int64_t n, double coefficient) {
   typedef std::conditional_t<sizeof(T) == 8, double, float> A;
   constexpr int N = Vec<T>::kN, kRounds = kChunk / (kThreads * N);
   typedef typename Vec<T>::type V;
@@ -97,7 +101,7 @@ __device__ __forceinline__ void scale_chunk(const T* __restrict__ src, T* __rest
     for (int i = 0; i < kRounds; ++i) {
 #pragma unroll
       for (int k = 0; k < N; ++k) v[i][k] = static_cast<T>(c * static_cast<A>(v[i][k]));
-      *reinterpret_cast<V*>(dst + (i * kThreads + threadIdx.x) * N) = v[i];
+      __builtin_nontemporal_store(v[i], reinterpret_cast<V*>(dst + (i * kThreads + threadIdx.x) * N));
     }
   } else {
     for (int at = threadIdx.x; at < n; at += kThreads) dst[at] = static_cast<T>(c * static_cast<A>(src[at]));
@@ -138,15 +142,16 @@ __device__ __forceinline__ void store_result(void* out, int dtype, double norm, 
   }
 }
 
+template <int kChunk>
 __global__ __launch_bounds__(kThreads) void square_kernel(const Batch b, double* __restrict__ partial) {
   __shared__ double slots[kThreads / 64];
   Square q;
   for (int64_t chunk = blockIdx.x; chunk < b.chunks; chunk += gridDim.x) {
     const Item& it = item_of(b, chunk);
     const int64_t at = (chunk - it.first_chunk) * kChunk, n = it.numel - at;
-    if (it.dtype == SC_F64) each_vector(static_cast<const double*>(it.src) + at, n, q);
-    else if (it.dtype == SC_F32) each_vector(static_cast<const float*>(it.src) + at, n, q);
-    else each_vector(static_cast<const __bf16*>(it.src) + at, n, q);
+    if (it.dtype == SC_F64) each_vector<kChunk>(static_cast<const double*>(it.src) + at, n, q);
+    else if (it.dtype == SC_F32) each_vector<kChunk>(static_cast<const float*>(it.src) + at, n, q);
+    else each_vector<kChunk>(static_cast<const __bf16*>(it.src) + at, n, q);
   }
   const double s = workgroup_sum(q.sum, slots);
   if (threadIdx.x == 0) partial[blockIdx.x] = s;
@@ -165,6 +170,7 @@ __global__ __launch_bounds__(kThreads) void finish_kernel(const double* __restri
 }
 
 // kept: the coefficient, or NULL: it is made here from the partial sums.
+template <int kChunk>
 __global__ __launch_bounds__(kThreads) void scale_kernel(const Batch b, const double* __restrict__ partial, int64_t n, double max_norm,
                                                          double eps, int dtype, void* out, const double* __restrict__ kept) {
   __shared__ double slots[kThreads / 64];
@@ -176,13 +182,14 @@ __global__ __launch_bounds__(kThreads) void scale_kernel(const Batch b, const do
     c = coefficient_of(norm, max_norm, eps);
     if (blockIdx.x == 0 && threadIdx.x == 0) store_result(out, dtype, norm, c);
   }
-  for (int64_t chunk = blockIdx.x; chunk < b.chunks; chunk += gridDim.x) {
+  for (int64_t left_over = blockIdx.x; left_over < b.chunks; left_over += gridDim.x) {
+    const int64_t chunk = b.chunks - 1 - left_over;   // what the first pass read last is still in the caches
     const Item& it = item_of(b, chunk);
     if (!it.dst || (it.dst == it.src && c == 1.0)) continue;
     const int64_t at = (chunk - it.first_chunk) * kChunk, left = it.numel - at;
-    if (it.dtype == SC_F64) scale_chunk(static_cast<const double*>(it.src) + at, static_cast<double*>(it.dst) + at, left, c);
-    else if (it.dtype == SC_F32) scale_chunk(static_cast<const float*>(it.src) + at, static_cast<float*>(it.dst) + at, left, c);
-    else scale_chunk(static_cast<const __bf16*>(it.src) + at, static_cast<__bf16*>(it.dst) + at, left, c);
+    if (it.dtype == SC_F64) scale_chunk<kChunk>(static_cast<const double*>(it.src) + at, static_cast<double*>(it.dst) + at, left, c);
+    else if (it.dtype == SC_F32) scale_chunk<kChunk>(static_cast<const float*>(it.src) + at, static_cast<float*>(it.dst) + at, left, c);
+    else scale_chunk<kChunk>(static_cast<const __bf16*>(it.src) + at, static_cast<__bf16*>(it.dst) + at, left, c);
   }
 }
 
@@ -195,7 +202,7 @@ size_t workspace_bytes(int64_t n_tensors) { return 256 + static_cast<size_t>(bat
 
 size_t elem_size(int dtype) { return dtype == SC_F64 ? 8 : dtype == SC_F32 ? 4 : 2; }
 
-Batch batch_of(int64_t n_tensors, const gc_tensor* tensors, int64_t index) {
+Batch batch_of(int64_t n_tensors, const gc_tensor* tensors, int64_t index, int chunk) {
   Batch b;
   b.chunks = 0;
   b.pad = 0;
@@ -203,7 +210,7 @@ Batch batch_of(int64_t n_tensors, const gc_tensor* tensors, int64_t index) {
   for (int i = 0; i < b.count; ++i) {
     const gc_tensor& t = tensors[index * kItems + i];
     b.item[i] = {t.src, t.dst, t.numel, b.chunks, t.dtype, 0};
-    b.chunks += (t.numel + kChunk - 1) / kChunk;
+    b.chunks += (t.numel + chunk - 1) / chunk;
   }
   return b;
 }
@@ -234,6 +241,7 @@ sc_status check(const char* fn, const gc_config* cfg, int64_t n, const gc_tensor
   return SC_OK;
 }
 
+template <int kChunk>
 hipError_t clip(const gc_config* cfg, int64_t n, const gc_tensor* tensors, void* out, void* workspace, hipStream_t stream) {
   double* kept = static_cast<double*>(workspace);
   double* partial = kept + 32;
@@ -242,10 +250,10 @@ hipError_t clip(const gc_config* cfg, int64_t n, const gc_tensor* tensors, void*
   for (int64_t i = 0; i < n; ++i) scaled = scaled || (tensors[i].dst && tensors[i].numel > 0);
   int64_t partials = 0;
   for (int64_t i = 0; i < batches; ++i) {
-    const Batch b = batch_of(n, tensors, i);
+    const Batch b = batch_of(n, tensors, i, kChunk);
     if (b.chunks == 0) continue;
     const unsigned grid = static_cast<unsigned>(std::min<int64_t>(b.chunks, kPartials));
-    hipLaunchKernelGGL(square_kernel, dim3(grid), dim3(kThreads), 0, stream, b, partial + partials);
+    hipLaunchKernelGGL((square_kernel<kChunk>), dim3(grid), dim3(kThreads), 0, stream, b, partial + partials);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     partials += grid;
@@ -256,10 +264,10 @@ hipError_t clip(const gc_config* cfg, int64_t n, const gc_tensor* tensors, void*
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !scaled) return e;
   }
-  for (int64_t i = 0; i < batches; ++i) {
-    const Batch b = batch_of(n, tensors, i);
+  for (int64_t i = batches - 1; i >= 0; --i) {
+    const Batch b = batch_of(n, tensors, i, kChunk);
     if (b.chunks == 0) continue;
-    hipLaunchKernelGGL(scale_kernel, dim3(static_cast<unsigned>(std::min<int64_t>(b.chunks, 2048))), dim3(kThreads), 0, stream, b, partial,
+    hipLaunchKernelGGL((scale_kernel<kChunk>), dim3(static_cast<unsigned>(std::min<int64_t>(b.chunks, 2048))), dim3(kThreads), 0, stream, b, partial,
                        partials, cfg->max_norm, cfg->eps, cfg->dtype, out, together ? nullptr : kept);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
@@ -293,7 +301,11 @@ sc_status gc_clip(const gc_config* cfg, int64_t n_tensors, const gc_tensor* tens
   if (misaligned(workspace, 256)) return set_error(SC_ERR_WORKSPACE, "gc_clip: workspace not 256-byte aligned");
   DeviceGuard guard(cfg->device);
   if (!guard.ok) return set_error(SC_ERR_HIP, "gc_clip: cannot make cfg->device current");
-  const hipError_t e = clip(cfg, n_tensors, tensors, norm_and_coefficient, workspace, static_cast<hipStream_t>(hip_stream));
+  int64_t total = 0;
+  for (int64_t i = 0; i < n_tensors; ++i) total += std::min<int64_t>(tensors[i].numel, int64_t(1) << 30);
+  hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  const hipError_t e = total > static_cast<int64_t>(kLongChunk) * kPartials ? clip<kLongChunk>(cfg, n_tensors, tensors, norm_and_coefficient, workspace, stream)
+                                                                             : clip<kShortChunk>(cfg, n_tensors, tensors, norm_and_coefficient, workspace, stream);
   if (e != hipSuccess) return set_error(SC_ERR_HIP, std::string("gc_clip: kernel launch: ") + hipGetErrorString(e));
   return SC_OK;
 }
