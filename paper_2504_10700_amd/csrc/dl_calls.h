@@ -285,7 +285,7 @@ __device__ __forceinline__ void dw_role(const Plan& p, int64_t chunk, int i, int
   const int n = n0 + 4 * j;
   if (p.dw.wr == 1) {
     if (n0 >= k_out) return;
-    if (to_db && q == 0) store4<kFours>(to_db + n, n, k_out, sum);
+    if (to_db && q == 0 && n < k_out) store4<kFours>(to_db + n, n, k_out, sum);
     if (to_dw) {
 #pragma unroll
       for (int t = 0; t < 4; ++t)

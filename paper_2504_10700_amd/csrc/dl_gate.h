@@ -32,7 +32,7 @@ struct Gate {
   }
 
   struct Point {
-    T p, pq, diff, u1, u2;   // diff = q - p
+    T z, p, pq, diff, u1, u2;   // diff = q - p
   };
 
   __device__ __forceinline__ Point at(T z) const {
@@ -43,6 +43,7 @@ struct Gate {
     u = u < kLow ? kLow : u;   // a NaN stays one, and z carries it in any case
     const T e = exp_of(-u);
     Point g;
+    g.z = relu ? w : z;   // (0 times minus infinity is no value of max(z, 0))
     g.p = u > kLow ? inverse_of(T(1) + e) : T(0);
     const T q = e * g.p;
     g.pq = g.p * q;
@@ -56,11 +57,14 @@ struct Gate {
     return g;
   }
 
-  __device__ __forceinline__ T value(T z) const { return z * at(z).p; }
+  __device__ __forceinline__ T value(T z) const {
+    const Point g = at(z);
+    return (z > T(0) ? z : g.z) * g.p;
+  }
 
   __device__ __forceinline__ T first(T z) const {
     const Point g = at(z);
-    return g.p + z * g.pq * g.u1;
+    return g.p + g.z * g.pq * g.u1;
   }
 
   // Derivatives below 2^-60 as zero.  For the products on parts: beside what they multiply they are far below the last bit of any sum, and the
@@ -69,8 +73,8 @@ struct Gate {
 
   __device__ __forceinline__ void both(T z, T* first_out, T* second) const {
     const Point g = at(z);
-    *first_out = g.p + z * g.pq * g.u1;
-    *second = T(2) * g.pq * g.u1 + (z * g.pq) * (g.diff * g.u1 * g.u1 + g.u2);   // z * p q first: 0 for large z
+    *first_out = g.p + g.z * g.pq * g.u1;
+    *second = T(2) * g.pq * g.u1 + (g.z * g.pq) * (g.diff * g.u1 * g.u1 + g.u2);   // z * p q first: 0 for large z
   }
 };
 

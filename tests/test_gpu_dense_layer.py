@@ -397,3 +397,228 @@ def test_other_stream_and_graph_replay(lib):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(out, ref)), f"replay {replay}"
+
+
+# ---- many rows: the results of whole rows on the bfloat16 matrix cores, where an fp32 number is the sum of three bfloat16 ones
+
+MANY = 66_001
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("k_in,k_out,act", [(72, 36, "gelu"), (20, 192, "silu"), (24, 72, "relu"), (100, 324, "silu"), (64, 132, "none"), (132, 64, "relu"),
+                                            (40, 4, "silu"), (8, 64, "gelu"), (192, 200, "silu"), (63, 64, "silu"), (64, 65, "none")])
+def test_many_rows_of_odd_widths(lib, k_in, k_out, act, dtype):
+    print(f"dense layer {MANY} x {k_in} -> {k_out} {dtype} {act}", flush=True)
+    check_layer(Layer(lib, MANY, k_in, k_out, act, dtype))
+
+
+EXACT = SHAPES + [(300, 20, 132), (700, 64, 260), (3000, 64, 260), (5000, 128, 192), (5000, 192, 320), (9000, 33, 195), (2100, 1280, 4), (2100, 4, 1280),
+                  (MANY, 64, 64), (MANY, 24, 192), (MANY, 64, 260), (MANY, 100, 324), (MANY, 192, 136), (MANY, 65, 67), (20_011, 64, 1280)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f64", "bf16"])
+@pytest.mark.parametrize("shape", EXACT, ids=lambda s: "x".join(map(str, s)))
+def test_small_integers_are_exact(lib, shape, dtype):
+    """Sums of products of small integers are exact in any order: no term may be missing, wrong or counted twice.  (Results in bfloat16 rows: rounded once.)"""
+    torch = lib.torch
+    act = ("none", "relu")[sum(shape) % 2]
+    print(f"dense layer {shape} {dtype} {act}, integers", flush=True)
+    layer = Layer(lib, *shape, act, dtype)
+    for t in (layer.X, layer.W, layer.b, layer.R, layer.dY, layer.HX):
+        t.copy_(t.clamp(-3, 3).round() if t is not layer.W else (t * shape[1] ** 0.5).clamp(-3, 3).round())
+    X, W, b, R, dY, HX = (t.double() for t in (layer.X, layer.W, layer.b, layer.R, layer.dY, layer.HX))
+
+    def same(name, got, ref):
+        assert torch.equal(got, ref.to(got.dtype)), f"{name}: {int((got != ref.to(got.dtype)).sum())} elements differ"
+
+    Y, Z = layer.forward()
+    z = X @ W + b
+    same("Z", Z, z)
+    same("Y", Y, (z.clamp(min=0) if act == "relu" else z) + R)
+    gate = (Z.double() > 0).double() if act == "relu" else torch.ones_like(z)
+    G = dY * gate
+    dX, dW, db = layer.backward(Z if act == "relu" else None)
+    same("dX", dX, G @ W.T.contiguous())
+    same("dW", dW, X.T.contiguous() @ G)
+    same("db", db, G.sum(0))
+    ddY, X2, W2, b2 = layer.double_backward(Z if act == "relu" else None)
+    same("ddY", ddY, (HX @ W) * gate)
+    assert not X2.any() and not b2.any()
+    same("W2", W2, HX.T.contiguous() @ G)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("spread", [(4, 1), (1, 3), (3, 2)], ids=str)
+@pytest.mark.parametrize("k_in,k_out", [(64, 64), (68, 140)])
+def test_many_strided_rows(lib, k_in, k_out, spread, dtype):
+    print(f"dense layer {MANY} x {k_in} -> {k_out} strides {spread} {dtype}", flush=True)
+    check_layer(Layer(lib, MANY, k_in, k_out, "silu", dtype, spread=spread))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("act", ["relu", "silu", "gelu"])
+@pytest.mark.parametrize("k_in,k_out", [(64, 64), (128, 192)])
+def test_many_rows_far_out(lib, k_in, k_out, act, dtype):
+    """Pre-activations of several tens: most derivatives are 0 or 1, many too small for their own parts."""
+    print(f"dense layer {MANY} x {k_in} -> {k_out} {dtype} {act}, wide rows", flush=True)
+    check_layer(Layer(lib, MANY, k_in, k_out, act, dtype, scale=30.0))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("k_in,k_out", [(64, 64), (24, 192), (64, 260)])
+def test_many_rows_with_values_that_are_not_finite(lib, dtype, value, k_in, k_out):
+    torch = lib.torch
+    print(f"dense layer {MANY} rows with {value} {dtype} {k_in} {k_out}", flush=True)
+    layer = Layer(lib, MANY, k_in, k_out, "none", dtype)
+    u = 2.0 ** -24
+    absolute = lambda t: t.double().abs()  # noqa: E731
+    part = 2.0 ** -16 if dtype == "bf16" else 0.0
+    slack_y = 2 * ((k_in + 4) * u + part) * (absolute(layer.X) @ absolute(layer.W) + absolute(layer.b) + absolute(layer.R))
+    slack_x = 2 * ((k_out + 4) * u + part) * (absolute(layer.dY) @ absolute(layer.W).T.contiguous())
+    Y0, _ = layer.forward()
+    dX0 = layer.backward(None)[0]
+    for row, column in ((77, 3), (40_000, 17), (MANY - 1, 0)):
+        layer.X[row, column] = value
+        layer.dY[row - 30, column + 2] = value
+    Y, _ = layer.forward()
+    dX, dW, db = layer.backward(None)
+    last = 2.0 ** -7 if dtype == "bf16" else 2 * u
+    keep = torch.ones(MANY, dtype=torch.bool, device="cuda")
+    keep_x = keep.clone()
+    keep_k, keep_n = torch.ones(k_in, dtype=torch.bool, device="cuda"), torch.ones(k_out, dtype=torch.bool, device="cuda")
+    for row, column in ((77, 3), (40_000, 17), (MANY - 1, 0)):
+        keep[row] = keep_x[row - 30] = False
+        keep_k[column] = keep_n[column + 2] = False
+        for got, r, w in ((Y, row, layer.W[column]), (dX, row - 30, layer.W[:, column + 2])):
+            want = value * w.double()
+            assert torch.equal(torch.isnan(got[r]), torch.isnan(want))
+            assert torch.equal(got[r].double()[~torch.isnan(want)], want[~torch.isnan(want)])
+    assert ((Y.double() - Y0.double()).abs() <= slack_y + last * absolute(Y0))[keep].all()
+    assert ((dX.double() - dX0.double()).abs() <= slack_x + last * absolute(dX0))[keep_x].all()
+    assert not torch.isfinite(dW[~keep_k]).any() and not torch.isfinite(dW[:, ~keep_n]).any() and not torch.isfinite(db[~keep_n]).any()
+    X, dY = layer.X.double(), layer.dY.double()
+    X[~keep], dY[~keep_x] = 0, 0                       # (those rows touch other columns too)
+    finite = (layer.X.double()[~keep][:, keep_k].T @ layer.dY.double()[~keep][:, keep_n] +
+              layer.X.double()[~keep_x][:, keep_k].T @ layer.dY.double()[~keep_x][:, keep_n])
+    ref = X[:, keep_k].T @ dY[:, keep_n] + finite
+    magnitude = absolute(layer.X)[:, keep_k].T @ absolute(layer.dY)[:, keep_n]
+    assert ((dW[keep_k][:, keep_n].double() - ref).abs() <= 2 * (MANY + 4) * u * magnitude).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), 3e38, 1e-42])
+@pytest.mark.parametrize("k_in,k_out", [(64, 64), (24, 260)])
+def test_many_rows_with_an_unusual_weight(lib, dtype, value, k_in, k_out):
+    """One weight that is not finite, close to the largest number, or below the smallest normal one: its column of Y and of dX show it, no other."""
+    torch = lib.torch
+    print(f"dense layer {MANY} rows, a weight of {value} {dtype} {k_in} {k_out}", flush=True)
+    layer = Layer(lib, MANY, k_in, k_out, "none", dtype, bias=False, residual=False)
+    layer.X.clamp_(-1, 1)
+    layer.dY.clamp_(-1, 1)
+    layer.W[5, 9] = value
+    Y, _ = layer.forward()
+    dX = layer.backward(None, "X")[0]
+    u, part, last = 2.0 ** -24, 2.0 ** -16 if dtype == "bf16" else 0.0, 2.0 ** -8 if dtype == "bf16" else 0.0
+    X, W, dY = layer.X.double(), layer.W.double(), layer.dY.double()
+    for got, a, b, column, k in ((Y, X, W, 9, k_in), (dX, dY, W.T.contiguous(), 5, k_out)):
+        keep = torch.arange(got.shape[1], device="cuda") != column
+        ref, magnitude = a @ b[:, keep], a.abs() @ b[:, keep].abs()
+        assert ((got[:, keep].double() - ref).abs() <= 1.01 * ((k + 2) * u + part) * magnitude + last * ref.abs()).all()
+        factor = a[:, 5 if column == 9 else 9] * W[5, 9]
+        if np.isfinite(value):
+            ref, magnitude = (a @ b[:, ~keep])[:, 0], (a.abs() @ b[:, ~keep].abs())[:, 0]
+            assert ((got[:, column].double() - ref).abs() <= 1.01 * ((k + 2) * u + part) * magnitude + last * ref.abs()).all()
+        else:
+            assert torch.equal(torch.isnan(got[:, column]), torch.isnan(factor))
+            assert torch.equal(got[:, column].double()[~torch.isnan(factor)], factor[~torch.isnan(factor)])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("size", [1e-36, 1e-30, 1e-25, 1e18, 3e37])
+def test_many_rows_of_every_size(lib, dtype, size):
+    """A third of the rows and of the entries of other rows far from 1 in size."""
+    torch = lib.torch
+    print(f"dense layer {MANY} rows, values of size {size} {dtype}", flush=True)
+    layer = Layer(lib, MANY, 64, 64, "none", dtype, bias=False, residual=False)
+    x = layer.X.double().clamp(-3, 3)
+    x[MANY // 3:2 * MANY // 3] *= size
+    x[2 * MANY // 3::50, ::7] *= size
+    layer.X.copy_(x.to(layer.X.dtype))
+    layer.W.copy_(layer.W.clamp(-0.1, 0.1))
+    X, W = host(layer.X), host(layer.W)
+    Y, _ = layer.forward()
+    ref, magnitude = X @ W, np.abs(X) @ np.abs(W)
+    slack = (66 * 2.0 ** -24 + (2.0 ** -8 + 2.0 ** -16 if dtype == "bf16" else 0)) * magnitude + 2.0 ** -125 * 2.0 ** -8
+    assert (np.abs(host(Y) - ref) <= slack).all()
+    layer.dY.copy_(layer.dY.clamp(-3, 3) * 1e-3)
+    dW = layer.backward(None)[1]
+    dY = host(layer.dY)
+    assert (np.abs(host(dW) - X.T @ dY) <= (MANY + 40) * 2.0 ** -24 * (np.abs(X).T @ np.abs(dY)) + 2.0 ** -125).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("k_in,k_out", [(64, 64), (128, 192)])
+def test_many_rows_optional_outputs_and_repetition(lib, dtype, k_in, k_out):
+    torch = lib.torch
+    print(f"dense layer optional outputs {MANY} {k_in} {k_out} {dtype}", flush=True)
+    for act in ("silu", "relu", "none"):
+        layer = Layer(lib, MANY, k_in, k_out, act, dtype)
+        Y, Z = layer.forward()
+        assert torch.equal(layer.forward(want_z=False)[0], Y) and torch.equal(layer.forward()[1], Z)
+        Zd = None if act == "none" else Z
+        for call in (layer.backward, layer.double_backward):
+            whole = call(Zd)
+            layer.ws.fill_(255)
+            assert all(torch.equal(a, b) for a, b in zip(whole, call(Zd)))
+            for want in ("X", "W", "b", "Xb", "Wb", "XW"):
+                for full, part in zip(whole, call(Zd, want)):
+                    # (a product may be cut differently where fewer results are wanted: equal up to the bound of its sums)
+                    if part is not None:
+                        d = (full.double() - part.double()).abs().max().item()
+                        assert d <= (2.0 ** -7 if dtype == "bf16" else 1e-4) * full.double().abs().max().item()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_many_rows_offsets_beyond_32_bits(lib, dtype):
+    torch = lib.torch
+    ld, k = 40_000, 64
+    print(f"dense layer, {MANY} rows {ld} elements apart, {dtype}", flush=True)
+    full = torch.empty(MANY * ld, dtype=lib.row[dtype], device="cuda").view(MANY, ld)
+    layer = Layer(lib, MANY, k, k, "silu", dtype)
+    Y0, Z0 = layer.forward()
+    dX0, dW0, db0 = layer.backward(Z0)
+    cfg = lib.dl.make_config(k, k, lib.dl.DL_SILU, lib.kind[dtype], ld_in=ld, ld_out=ld)
+    x, dy, r, y, z, dx = (full[:, 1000 * i:1000 * i + k] for i in range(6))
+    for wide, dense in ((x, layer.X), (dy, layer.dY), (r, layer.R)):
+        wide.copy_(dense)
+    dW, db = torch.empty_like(dW0), torch.empty_like(db0)
+    nbytes = lib.dl.dl_workspace_bytes(cfg, MANY)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+    lib.dl.dl_forward(cfg, MANY, x, layer.W, layer.b, r, y, z)
+    lib.dl.dl_backward(cfg, MANY, x, layer.W, z, dy, dx, dW, db, ws, nbytes)
+    for a, b in ((y, Y0), (z, Z0), (dx, dX0), (dW, dW0), (db, db0)):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f64", "bf16"])
+@pytest.mark.parametrize("rows", [5, 2000, MANY])
+def test_relu_of_infinities(lib, dtype, rows):
+    """max(z, 0) and its derivative are 0 at minus infinity; infinity stays."""
+    layer = Layer(lib, rows, 32, 32, "relu", dtype, bias=False, residual=False)
+    layer.W.zero_()
+    layer.W.fill_diagonal_(1.0)
+    layer.X.zero_()
+    layer.X[rows // 2] = 1.0
+    layer.X[3, :] = 0.0
+    layer.X[3, 4], layer.X[4, 5] = -float("inf"), float("inf")
+    Y, Z = layer.forward()
+    Z[3, :], Z[4, :] = -float("inf"), float("inf")     # (0 times infinity beside the diagonal: put the pre-activations in by hand)
+    dX, dW, db = layer.backward(Z, "X")
+    assert not dX[3].any()
+    assert lib.torch.equal(dX[4], layer.dY[4])
+    layer.X.zero_()
+    layer.b = layer.W[0].clone().zero_()
+    layer.b[7], layer.b[8] = -float("inf"), float("inf")
+    Y, Z = layer.forward()
+    assert not Y[:, :8].any() and lib.torch.isinf(Y[:, 8]).all() and (Z[:, 7] == -float("inf")).all()
