@@ -187,3 +187,24 @@ def test_other_stream_and_graph_replay(ee):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(Y, ref[0]) and torch.equal(dT, ref[1]), f"replay {replay}"
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f64", "bf16"])
+@pytest.mark.parametrize("n,elements,channels", [(61, 89, 128), (1500, 89, 128), (4097, 1024, 20), (33_001, 1025, 64), (200_003, 89, 128), (32_768, 50_000, 72),
+                                                 (70_001, 1, 64), (90_001, 700, 33)])
+def test_sums_of_small_integers_are_exact(ee, n, elements, channels, dtype):
+    """No row may be missing or counted twice, however many it is summed with."""
+    import torch
+    print(f"embedding of integers {n} {elements} {channels} {dtype}", flush=True)
+    row = {"f32": torch.float32, "f64": torch.float64, "bf16": torch.bfloat16}[dtype]
+    table = torch.float64 if dtype == "f64" else torch.float32
+    g = torch.Generator(device="cuda").manual_seed(n)
+    z = (elements * torch.rand(n, generator=g, device="cuda") ** 2 * 1.01).to(torch.int32)       # some beyond the table
+    dY = torch.randint(-5, 6, (n, channels), generator=g, device="cuda").to(row)
+    dT = torch.full((elements, channels), float("nan"), dtype=table, device="cuda")
+    cfg = ee.make_config(elements, channels, 0.5, {"f32": ee.SC_F32, "f64": ee.SC_F64, "bf16": ee.SC_BF16}[dtype])
+    nbytes = ee.ee_workspace_bytes(cfg, n)
+    ee.ee_backward(cfg, n, z, dY, dT, torch.full((nbytes,), 255, dtype=torch.uint8, device="cuda"), nbytes)
+    inside = z < elements
+    want = torch.zeros(elements, channels, dtype=torch.float64, device="cuda").index_add_(0, z[inside].long(), dY[inside].double()) * 0.5
+    assert torch.equal(dT, want.to(table))

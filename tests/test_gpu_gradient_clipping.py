@@ -167,3 +167,22 @@ def test_other_stream_and_graph_replay(gc):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip([out] + dst, ref)), f"replay {replay}"
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+def test_long_lists_of_every_type(gc, in_place):
+    """Beyond eight million elements, tensors of every type and of odd lengths, several kernel arguments' worth of them.  The elements against the product
+    with the coefficient that the call returns: sums of 74 million squares in different orders differ in more than the last bit."""
+    import torch
+    lengths = [3_000_001, 8193, 1, 0, 2047, 700_007] * 20
+    print(f"clip {sum(lengths)} elements, in place {in_place}", flush=True)
+    src = make(lengths, [getattr(torch, TYPES[i % 3]) for i in range(len(lengths))])
+    was = [x.clone() for x in src]
+    dst = src if in_place else [torch.full_like(x, float("nan")) for x in src]
+    norm, coefficient = clip(gc, src, dst, 0.5).tolist()
+    want = torch.sqrt(sum((x.double() ** 2).sum() for x in was)).item()
+    assert abs(norm - want) <= 1e-13 * norm and abs(coefficient - 0.5 / (want + 1e-6)) <= 1e-12 * coefficient
+    for x, w in zip(dst, was):
+        u = {torch.float32: 2.0 ** -23, torch.float64: 2.0 ** -51, torch.bfloat16: 2.0 ** -8 + 2.0 ** -23}[x.dtype]
+        w = w.double() * coefficient
+        assert ((x.double() - w).abs() <= u * w.abs()).all()
