@@ -177,34 +177,34 @@ __global__ __launch_bounds__((threads<kSplit, TA>())) void rows_kernel(Walk walk
 }
 
 // Parts of the operands on the bfloat16 matrix cores (dl_parts.h): of X, of W, of the source of dX and of that of dW.
-template <int kX, int kW>
-constexpr int rows_words() { return kWaves * kPartsTiles * kX * kPlane + shared_words<kW>(); }
+template <int kRT, int kX, int kW>
+constexpr int rows_words() { return kWaves * kRT * kX * kPlane + shared_words<kW>(); }
 
-// The results of 64 kWaves rows from row0 and of 64 columns by a workgroup.
-template <int kX, int kW, typename Rows, typename T, int N, typename F>
+// The results of 16 kRT kWaves rows from row0 and of 64 columns by a workgroup.
+template <int kRT, int kX, int kW, typename Rows, typename T, int N, typename F>
 __device__ __forceinline__ void finish_rows_parts(const Rows& a, const AlongRows<float>& w, int64_t row0, int64_t rows, int n0, unsigned* lds,
                                                   const float* __restrict__ bias, const Beside<T, N>& beside, F&& f) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
-  Acc acc[kPartsTiles][4];
-  unsigned* const planes = lds + wave * (kPartsTiles * kX * kPlane);
+  Acc acc[kRT][4];
+  unsigned* const planes = lds + wave * (kRT * kX * kPlane);
   const Operand<float, float, kPlain> matrix{{w.W, w.n_end}, {}, {}};
-  const int64_t first = row0 + wave * (16 * kPartsTiles);
-  if (!rows_parts<kPartsTiles, kX, kW>(as_rows<kX>(a), SharedColumns<float, kPlain, kW>{matrix}, first, rows, n0, w.n_end, w.k_end, planes,
-                                       lds + kWaves * kPartsTiles * kX * kPlane, acc))
-    rows_product<float, kPartsTiles, true>(a, w, first, rows, n0, 0, w.k_end, reinterpret_cast<float*>(planes), acc);
-  each_four<float, kPartsTiles, true>(first, rows, n0, w.n_end, acc, bias, beside, f);
+  const int64_t first = row0 + wave * (16 * kRT);
+  if (!rows_parts<kRT, kX, kW>(as_rows<kX>(a), SharedColumns<float, kPlain, kW>{matrix}, first, rows, n0, w.n_end, w.k_end, planes,
+                               lds + kWaves * kRT * kX * kPlane, acc))
+    rows_product<float, kRT, true>(a, w, first, rows, n0, 0, w.k_end, reinterpret_cast<float*>(planes), acc);
+  each_four<float, kRT, true>(first, rows, n0, w.n_end, acc, bias, beside, f);
 }
 
-template <typename TS, typename End>
+template <typename TS, int kRT, typename End>
 __global__ __launch_bounds__(kThreads, 2) void parts_rows_kernel(Walk walk, int64_t rows, Operand<float, TS, kPlain> X, AlongRows<float> W,
                                                                  const float* __restrict__ bias, End end) {
   constexpr int kX = PartCount<TS>::x, kW = PartCount<TS>::w;
-  __shared__ unsigned lds[rows_words<kX, kW>()];
+  __shared__ unsigned lds[rows_words<kRT, kX, kW>()];
   for (int64_t t = blockIdx.x; t < walk.count(); t += gridDim.x) {
     int64_t rg;
     int cg;
     if (!walk.at(t, &rg, &cg)) continue;
-    finish_rows_parts<kX, kW>(X, W, rg * (16 * kPartsTiles * kWaves), rows, cg * kCols, lds, bias, end.beside(), end);
+    finish_rows_parts<kRT, kX, kW>(X, W, rg * (16 * kRT * kWaves), rows, cg * kCols, lds, bias, end.beside(), end);
     __syncthreads();
   }
 }
@@ -341,10 +341,11 @@ __global__ __launch_bounds__((threads<kSplit, TA>())) void backward_kernel(Plan 
                                                                            TA* __restrict__ dW, TA* __restrict__ db) {
   constexpr int kJoin = threads<kSplit, TA>() * 16, kRowsPart = lds_elements<kSplit, kRT, TA>();
   __shared__ TA lds[kJoin > kRowsPart ? kJoin : kRowsPart];
-  const int64_t groups = p.dx_groups + p.dw_groups, total = (p.chunks + kXcds - 1) / kXcds * kXcds * groups;
+  const Deal deal = p.deal();
+  const int64_t total = deal.count();
   for (int64_t t = blockIdx.x; t < total; t += gridDim.x) {
-    const int64_t local = t / kXcds, chunk = local / groups * kXcds + t % kXcds, i = local % groups;
-    if (chunk >= p.chunks) continue;
+    int64_t chunk, i;
+    if (!deal.at(t, &chunk, &i)) continue;
     if (i < p.dx_groups)
       dx_role<TA, kRT, kSplit, kFours>(p, chunk, i, g, W, ld_in, dX, lds);
     else
@@ -449,27 +450,28 @@ __device__ __forceinline__ void parts_dw_role(const Plan& p, int64_t chunk, int 
 }
 
 // backward_kernel on parts.  WT: W transposed.  kDx: is there a dX here?  (Without it the 64 x 64 blocks leave room for more waves.)
-template <typename TS, bool kWide, bool kDx, bool kTwo, typename G, typename B, typename B2>
+template <typename TS, int kRT, bool kWide, bool kDx, bool kTwo, typename G, typename B, typename B2>
 __global__ __launch_bounds__(kThreads, kWide || kDx ? 2 : 3) void parts_backward_kernel(Plan p, int k_in, int k_out, int64_t ld_in, G g, AlongRows<float> WT,
                                                                      TS* __restrict__ dX, Operand<float, TS, kPlain> x, B b,
                                                                      Operand<float, TS, kPlain> x2, B2 b2, float* __restrict__ dW,
                                                                      float* __restrict__ db) {
   typedef PartCount<TS> Count;
   constexpr int kG = Count::dx(static_cast<G*>(nullptr)), kB = Count::dw(static_cast<B*>(nullptr)), kB2 = Count::dw(static_cast<B2*>(nullptr));
-  constexpr int kDxWords = kDx ? rows_words<kG, Count::w>() : 0;
+  constexpr int kDxWords = kDx ? rows_words<kRT, kG, Count::w>() : 0;
   constexpr int kDwWords = shared_words<Count::x>() + (kWide ? 0 : shared_words<(kB > kB2 ? kB : kB2)>());
   __shared__ unsigned lds[kDxWords > kDwWords ? kDxWords : kDwWords];
-  const int64_t groups = p.dx_groups + p.dw_groups, total = (p.chunks + kXcds - 1) / kXcds * kXcds * groups;
+  const Deal deal = p.deal();
+  const int64_t total = deal.count();
   for (int64_t t = blockIdx.x; t < total; t += gridDim.x) {
-    const int64_t local = t / kXcds, chunk = local / groups * kXcds + t % kXcds, i = local % groups;
-    if (chunk >= p.chunks) continue;
+    int64_t chunk, i;
+    if (!deal.at(t, &chunk, &i)) continue;
     if (kDx && i < p.dx_groups) {
       if constexpr (kDx) {
-        const int64_t row0 = chunk * p.per + i / p.dx_col_groups * (16 * kPartsTiles * kWaves), end = min(p.rows, (chunk + 1) * p.per);
+        const int64_t row0 = chunk * p.per + i / p.dx_col_groups * (16 * kRT * kWaves), end = min(p.rows, (chunk + 1) * p.per);
         const int n0 = static_cast<int>(i % p.dx_col_groups) * kCols;
         const float* const none = nullptr;
         if (row0 < end)
-          finish_rows_parts<kG, Count::w>(g, WT, row0, end, n0, lds, none, Beside<TS, 0>{}, StoreEnd<TS, float, true>{ld_in, k_in, dX});
+          finish_rows_parts<kRT, kG, Count::w>(g, WT, row0, end, n0, lds, none, Beside<TS, 0>{}, StoreEnd<TS, float, true>{ld_in, k_in, dX});
       }
     } else {
       parts_dw_role<kWide, kTwo, Count::x, kB, kB2>(p, chunk, static_cast<int>(i - p.dx_groups), k_in, k_out, x, b, x2, b2, dW, db, lds);
@@ -611,12 +613,16 @@ struct Calls {
       }
     }
     if constexpr (sizeof(TA) == 4) {
-      if (in_parts(c, n, c->k_out, c->k_in)) {
-        const Walk walk{blocks_of(n, 16 * kPartsTiles * kWaves), static_cast<int>(blocks_of(c->k_out, kCols))};
+      if (in_parts(c, n, c->k_out, c->k_in, sizeof(TS) == 4 ? 2 * kFewBlocks : kFewBlocks)) {
+        const int rt = parts_tiles(n, c->k_out);
+        const Walk walk{blocks_of(n, 16 * rt * kWaves), static_cast<int>(blocks_of(c->k_out, kCols))};
         const auto end = make(std::true_type{});
-        hipLaunchKernelGGL((parts_rows_kernel<TS, std::decay_t<decltype(end)>>), dim3(grid_of(walk.count())), dim3(kThreads), 0, stream, walk, n,
-                           rows_in(X), along, static_cast<const float*>(b), end);
-        return hipGetLastError();
+        auto launch = [&](auto tiles) {
+          hipLaunchKernelGGL((parts_rows_kernel<TS, tiles.value, std::decay_t<decltype(end)>>), dim3(grid_of(walk.count())), dim3(kThreads), 0, stream,
+                             walk, n, rows_in(X), along, static_cast<const float*>(b), end);
+          return hipGetLastError();
+        };
+        return rt == kPartsTiles ? launch(std::integral_constant<int, kPartsTiles>{}) : launch(std::integral_constant<int, 1>{});
       }
     }
     return by_shape(c->k_out, c->k_in, [&](auto rt, auto split, auto fours) {
@@ -692,10 +698,13 @@ struct Calls {
           const hipError_t e = transpose(W, ws);
           if (e != hipSuccess) return e;
         }
-        if (wide_parts(c)) return dX ? parts_gradients<true, true, kTwo>(source, dX, X, b, X2, b2, dW, db, ws)
-                                     : parts_gradients<true, false, kTwo>(source, dX, X, b, X2, b2, dW, db, ws);
-        return dX ? parts_gradients<false, true, kTwo>(source, dX, X, b, X2, b2, dW, db, ws)
-                  : parts_gradients<false, false, kTwo>(source, dX, X, b, X2, b2, dW, db, ws);
+        auto with_tiles = [&](auto tiles) {
+          if (wide_parts(c)) return parts_gradients<tiles.value, true, true, kTwo>(source, dX, X, b, X2, b2, dW, db, ws);
+          return parts_gradients<tiles.value, false, true, kTwo>(source, dX, X, b, X2, b2, dW, db, ws);
+        };
+        if (dX) return parts_tiles(n, c->k_in) == kPartsTiles ? with_tiles(std::integral_constant<int, kPartsTiles>{}) : with_tiles(std::integral_constant<int, 1>{});
+        return wide_parts(c) ? parts_gradients<1, true, false, kTwo>(source, dX, X, b, X2, b2, dW, db, ws)
+                             : parts_gradients<1, false, false, kTwo>(source, dX, X, b, X2, b2, dW, db, ws);
       }
     }
     return by_shape(c->k_in, c->k_out, [&](auto rt, auto split, auto fours) {
@@ -739,19 +748,18 @@ struct Calls {
                             const B2& b2, void* dW, void* db, void* ws) const {
     const Plan p = plan_of(c, n, dX != nullptr, dW || db, split, rt);
     const Target to = target(p, dW, db, ws);
-    const int64_t groups = blocks_of(p.chunks, kXcds) * kXcds * (p.dx_groups + p.dw_groups);
-    hipLaunchKernelGGL((backward_kernel<TS, TA, RT::value, Split::value, Fours::value, kTwo, G, B, B2, Weights>), dim3(grid_of(groups)),
+    hipLaunchKernelGGL((backward_kernel<TS, TA, RT::value, Split::value, Fours::value, kTwo, G, B, B2, Weights>), dim3(grid_of(p.deal().count())),
                        dim3((threads<Split::value, TA>())), 0, stream, p, c->k_in, c->k_out, ld_in(c), source, w, static_cast<TS*>(dX), rows_in(X), b,
                        rows_in(X2), b2, to.dw, to.db);
     return join(p, to, dW, db);
   }
 
-  template <bool kWide, bool kDx, bool kTwo, typename G, typename B, typename B2>
+  // kRT: row tiles of a wave of dX
+  template <int kRT, bool kWide, bool kDx, bool kTwo, typename G, typename B, typename B2>
   hipError_t parts_gradients(const G& source, void* dX, const void* X, const B& b, const void* X2, const B2& b2, void* dW, void* db, void* ws) const {
     const Plan p = parts_plan(c, n, dX != nullptr, dW || db);
     const Target to = target(p, dW, db, ws);
-    const int64_t groups = blocks_of(p.chunks, kXcds) * kXcds * (p.dx_groups + p.dw_groups);
-    hipLaunchKernelGGL((parts_backward_kernel<TS, kWide, kDx, kTwo, G, B, B2>), dim3(grid_of(groups)), dim3(kThreads), 0, stream, p, c->k_in, c->k_out,
+    hipLaunchKernelGGL((parts_backward_kernel<TS, kRT, kWide, kDx, kTwo, G, B, B2>), dim3(grid_of(p.deal().count())), dim3(kThreads), 0, stream, p, c->k_in, c->k_out,
                        ld_in(c), source, (AlongRows<float>{static_cast<const float*>(ws), c->k_out, c->k_in}), static_cast<TS*>(dX), rows_in(X), b,
                        rows_in(X2), b2, to.dw, to.db);
     return join(p, to, dW, db);

@@ -360,16 +360,25 @@ __device__ __forceinline__ bool rows_parts(const Rows& a, const Weights& w, int6
     U4 x[kRT][kX];
 #pragma unroll
     for (int i = 0; i < kRT; ++i) get_parts<kX>(planes + i * kX * kPlane, x[i]);
+    static_assert(kRT == 4 || kRT == 1, "four sums at a time");
+    if constexpr (kRT == 4) {
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      U4 c[kW];
-      get_shared<kW>(shared + at, u, c);
-      static_assert(kRT == 4, "four sums at a time");
-      Acc sum[4] = {acc[0][u], acc[1][u], acc[2][u], acc[3][u]}, small[4] = {};
-      multiply4<kX, kW>([&](int i) -> const U4(&)[kX] { return x[i]; }, [&](int) -> const U4(&)[kW] { return c; }, sum, small);
-      join4<kX, kW>(sum, small);
+      for (int u = 0; u < 4; ++u) {
+        U4 c[kW];
+        get_shared<kW>(shared + at, u, c);
+        Acc sum[4] = {acc[0][u], acc[1][u], acc[2][u], acc[3][u]}, small[4] = {};
+        multiply4<kX, kW>([&](int i) -> const U4(&)[kX] { return x[i]; }, [&](int) -> const U4(&)[kW] { return c; }, sum, small);
+        join4<kX, kW>(sum, small);
 #pragma unroll
-      for (int i = 0; i < kRT; ++i) acc[i][u] = sum[i];
+        for (int i = 0; i < kRT; ++i) acc[i][u] = sum[i];
+      }
+    } else {
+      U4 c[4][kW];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) get_shared<kW>(shared + at, u, c[u]);
+      Acc small[4] = {};
+      multiply4<kX, kW>([&](int) -> const U4(&)[kX] { return x[0]; }, [&](int u) -> const U4(&)[kW] { return c[u]; }, acc[0], small);
+      join4<kX, kW>(acc[0], small);
     }
     Corner<float>::sync();
   }

@@ -24,22 +24,38 @@ struct Shape {
   int wc, wr;
 };
 
-// Row groups x column groups of workgroups.  All column groups of a row group go to one XCD (workgroups are dealt out to the XCDs in turn), whose
-// L2 then holds the rows that they share.
-struct Walk {
-  int64_t row_groups;
-  int col_groups;
-  __host__ __device__ int64_t count() const { return (row_groups + kXcds - 1) / kXcds * kXcds * col_groups; }
-  __device__ bool at(int64_t t, int64_t* row, int* col) const {
-    const int64_t local = t / kXcds;
-    *row = local / col_groups * kXcds + t % kXcds;
-    *col = static_cast<int>(local % col_groups);
-    return *row < row_groups;
+// Workgroups that share rows, `shared` of them for each of `groups` groups of rows.  All of a group go to one XCD (workgroups are dealt out to the
+// XCDs in turn), whose L2 then holds the rows - where the groups come out even to a quarter.  Where they are few the XCDs take them as they come
+// (250 rows, 1024 -> 1024: all of one group on one XCD 104 us for dX, 16 on all).
+struct Deal {
+  int64_t groups, shared;
+  __host__ __device__ int64_t rounded() const { return (groups + kXcds - 1) / kXcds * kXcds; }
+  __host__ __device__ bool by_xcd() const { return 4 * rounded() <= 5 * groups; }
+  __host__ __device__ int64_t count() const { return (by_xcd() ? rounded() : groups) * shared; }
+  __device__ bool at(int64_t t, int64_t* group, int64_t* i) const {
+    const bool even = by_xcd();
+    const int64_t local = even ? t / kXcds : t;
+    *group = even ? local / shared * kXcds + t % kXcds : local / shared;
+    *i = local % shared;
+    return *group < groups;
   }
 };
 
+// Row groups x column groups of workgroups.
+struct Walk {
+  int64_t row_groups;
+  int col_groups;
+  __host__ __device__ Deal deal() const { return {row_groups, col_groups}; }
+  __host__ __device__ int64_t count() const { return deal().count(); }
+  __device__ bool at(int64_t t, int64_t* row, int* col) const {
+    int64_t i;
+    const bool inside = deal().at(t, row, &i);
+    *col = static_cast<int>(i);
+    return inside;
+  }
+};
 
-constexpr int kPartsTiles = 4;   // row tiles of a wave
+constexpr int kPartsTiles = 4;   // row tiles of a wave, where there are rows enough (parts_tiles)
 
 // What a launch of the backward does: the rows in chunks, of each chunk first dx_groups workgroups of dX, then dw_groups of the chunk's partial dW and
 // db.  A chunk stays on one XCD and its two halves run at about the same time: the second reading of dY (and Z) comes from the caches.
@@ -50,6 +66,7 @@ struct Plan {
   int dx_col_groups, dw_col_groups;
   Shape dx, dw;
   int64_t stride;       // elements between the chunks' partial results
+  __host__ __device__ Deal deal() const { return {chunks, dx_groups + dw_groups}; }
 };
 
 // ---- host side
@@ -85,8 +102,9 @@ inline Plan plan_of(const dl_config* c, int64_t n, bool want_dx, bool want_dw, b
   p.dw = shape_of(c->k_out);
   if (split) p.dw = {1, split_waves};
   const int64_t blocks = blocks_of(c->k_in, kCols) * blocks_of(c->k_out, kCols);
-  // about 2048 waves of dW, none with less than 32 rows
-  const int64_t chunks = std::max<int64_t>(1, std::min(2048 / (blocks * p.dw.wr), n / (32 * p.dw.wr)));
+  constexpr int kMinShare = 16;
+  // about 2048 waves of dW, none with less than 16 rows (1000 rows, 256 -> 256 in fp32: dW 21 us so, 28 with 32; 10 000, 128 -> 16 in fp64: 22, 25)
+  const int64_t chunks = std::max<int64_t>(1, std::min(2048 / (blocks * p.dw.wr), n / (kMinShare * p.dw.wr)));
   p.per = blocks_of(n, chunks);
   p.per = blocks_of(p.per, p.per < 256 ? 64 : 256) * (p.per < 256 ? 64 : 256);
   p.chunks = blocks_of(n, p.per);
@@ -101,13 +119,22 @@ inline Plan plan_of(const dl_config* c, int64_t n, bool want_dx, bool want_dw, b
 
 inline bool curved(const dl_config* c) { return c->activation == DL_SILU || c->activation == DL_GELU; }
 
-// Do the bfloat16 matrix cores serve a product of rows (dl_parts.h)?
-inline bool in_parts(const dl_config* c, int64_t n, int cols, int k) {
+// Do the bfloat16 matrix cores serve a product of rows (dl_parts.h)?  From 1024 blocks of 64 x 64 results on, and where the sum is long and there is a
+// block for every second CU; of the forward, whose launch does nothing else, with three parts a block for every CU.  (dX, dW and db together, fp32
+// instruction -> parts: 1000 rows, 1024 -> 1024 94 -> 83 us, 2100 rows 198 -> 120, 8000 rows, 128 -> 128 40 -> 25, 6000 rows, 128 -> 1240 110 -> 77;
+// 500 rows, 1024 -> 1024 54 -> 61.  Shorter sums: 25 000 rows, 64 -> 64, second order 41 -> 56.)
+constexpr int64_t kFewBlocks = 128;
+constexpr int kLongSum = 128;
+inline bool in_parts(const dl_config* c, int64_t n, int cols, int k, int64_t few = kFewBlocks) {
   // (the lanes' places in 64 rows are 32-bit byte offsets)
   if (ld_in(c) > (1 << 22) || ld_out(c) > (1 << 22)) return false;
   if (c->dtype == SC_F64 || c->k_in % 4 != 0 || c->k_out % 4 != 0 || k <= 16 || (c->dtype == SC_BF16 && k % 8 != 0)) return false;
-  return blocks_of(n, 64) * blocks_of(cols, kCols) >= 1024;
+  const int64_t blocks = blocks_of(n, 64) * blocks_of(cols, kCols);
+  return blocks >= 1024 || (blocks >= few && k >= kLongSum);
 }
+
+// Row tiles of a wave: one where four would leave CUs without a workgroup (2100 rows, 1024 -> 1024, dX 90 us with four, 83 with one; forward 86, 59).
+inline int parts_tiles(int64_t n, int cols) { return blocks_of(n, 64) * blocks_of(cols, kCols) >= 1024 ? kPartsTiles : 1; }
 
 // Do the waves keep W (walk_rows)?  Its parts of up to 64 reduced indices fit the registers.
 inline bool kept_ok(const dl_config* c, int64_t n, int cols, int k) { return k <= 2 * kRound && in_parts(c, n, cols, k); }
@@ -126,16 +153,17 @@ inline Plan parts_plan(const dl_config* c, int64_t n, bool want_dx, bool want_dw
   // the others are done.  None with less than 256 rows.  (990 001 rows, 64 -> 1280: 65 workgroups on an XCD with 64 places 1640 us, 60 1190.)
   const int64_t places = wide ? 64 : 96;
   int64_t chunks = groups <= places ? places / groups * kXcds : kXcds * blocks_of(places, groups);
-  chunks = std::max<int64_t>(1, std::min<int64_t>(chunks, n / 256));
+  const int rt = parts_tiles(n, c->k_in);
+  chunks = std::max<int64_t>(1, std::min<int64_t>(chunks, n / (rt == 1 ? 128 : 256)));
   // With dX beside it no more than 4 MB of dY, so that what the workgroups of the chip read twice at a time stays in the caches: 990 001 rows of
   // bfloat16, 64 -> 1280, 1325 us with 26 MB, 1120 with 10, 1017 with 4.
   if (want_dx && want_dw) chunks = std::max(chunks, blocks_of(n * c->k_out * static_cast<int64_t>(row_size(c)), 4 << 20));
-  const int64_t unit = want_dx ? 256 : 32;
+  const int64_t unit = want_dx ? 16 * rt * kWaves : 32;
   p.per = blocks_of(blocks_of(n, chunks), unit) * unit;
   p.chunks = blocks_of(n, p.per);
   p.dx = {1, kWaves};
   p.dx_col_groups = static_cast<int>(blocks_of(c->k_in, kCols));
-  p.dx_groups = want_dx ? blocks_of(p.per, 16 * kPartsTiles * kWaves) * p.dx_col_groups : 0;
+  p.dx_groups = want_dx ? blocks_of(p.per, 16 * rt * kWaves) * p.dx_col_groups : 0;
   p.dw_groups = want_dw ? groups : 0;
   p.stride = static_cast<int64_t>(c->k_in) * c->k_out + c->k_out;
   return p;

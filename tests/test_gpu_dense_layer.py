@@ -413,6 +413,7 @@ def test_many_rows_of_odd_widths(lib, k_in, k_out, act, dtype):
 
 
 EXACT = SHAPES + [(300, 20, 132), (700, 64, 260), (3000, 64, 260), (5000, 128, 192), (5000, 192, 320), (9000, 33, 195), (2100, 1280, 4), (2100, 4, 1280),
+                  (250, 1024, 1024), (600, 1000, 1024), (2100, 1024, 1028), (6000, 128, 1240), (3000, 256, 512), (8003, 128, 128), (5000, 200, 200),
                   (MANY, 64, 64), (MANY, 24, 192), (MANY, 64, 260), (MANY, 100, 324), (MANY, 192, 136), (MANY, 65, 67), (20_011, 64, 1280)]
 
 
@@ -622,3 +623,31 @@ def test_relu_of_infinities(lib, dtype, rows):
     layer.b[7], layer.b[8] = -float("inf"), float("inf")
     Y, Z = layer.forward()
     assert not Y[:, :8].any() and lib.torch.isinf(Y[:, 8]).all() and (Z[:, 7] == -float("inf")).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape,act", [((600, 1000, 1024), "gelu"), ((8003, 128, 128), "silu"), ((3001, 256, 512), "relu"), ((6000, 128, 1240), "silu"),
+                                       ((5000, 200, 200), "gelu")], ids=str)
+def test_long_sums_of_fewer_rows(lib, shape, act, dtype):
+    print(f"dense layer {shape} {dtype} {act}", flush=True)
+    check_layer(Layer(lib, *shape, act, dtype))
+    check_layer(Layer(lib, *shape, act, dtype, spread=(2, 3), scale=20.0))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(600, 1000, 1024), (8003, 128, 128)], ids=str)
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_long_sums_with_values_that_are_not_finite(lib, shape, value, dtype):
+    torch = lib.torch
+    rows, k_in, k_out = shape
+    print(f"dense layer {shape} with {value} {dtype}", flush=True)
+    layer = Layer(lib, *shape, "none", dtype)
+    layer.X[rows - 1, 3], layer.dY[70, k_out - 1] = value, value
+    Y, _ = layer.forward()
+    dX, dW, db = layer.backward(None)
+    for got, row in ((Y, rows - 1), (dX, 70)):
+        keep = torch.arange(rows, device="cuda") != row
+        assert torch.isfinite(got[keep]).all() and not torch.isfinite(got[row]).any()
+    assert not torch.isfinite(dW[3]).any() and not torch.isfinite(dW[:, -1]).any()
+    keep = torch.arange(k_in, device="cuda") != 3
+    assert torch.isfinite(dW[keep][:, :-1]).all() and torch.isfinite(db[:-1]).all() and not torch.isfinite(db[-1])
