@@ -30,6 +30,9 @@ struct PartCount {
   template <typename T, Source kSource>
   static constexpr int dw(const Operand<double, T, kSource>*) { return 0; }
 };
+// Parts of W in a product of rows with an epilogue.
+template <typename TS, typename End>
+constexpr int weight_parts() { return End::kExact ? 3 : PartCount<TS>::w; }
 template <int kParts, typename T, Source kSource>
 __device__ __forceinline__ PartsRows<T, kSource, kParts> as_rows(const Operand<float, T, kSource>& o) { return {o}; }
 template <int kParts, typename T, Source kSource>
@@ -99,6 +102,7 @@ __device__ __forceinline__ void each_tile(const Walk& walk, const Shape& shape, 
 // What becomes of four neighbouring results v of a row.  The constructor takes what is the same for a lane's column.
 template <typename TS, typename TA, bool kFours, int kResidual>
 struct ForwardEnd {   // Z = v (bias added), Y = act(Z) + residual
+  static constexpr bool kExact = false;   // nothing goes further than to results in the type of the rows
   Gate<TA> gate;
   int64_t ld_out;
   int n_end;
@@ -126,6 +130,7 @@ struct ForwardEnd {   // Z = v (bias added), Y = act(Z) + residual
 // v = V: ddY = V act'(Z), S = V dY act''(Z).  kBeside 0: no activation; 1: no curvature (Z alone is read, no S); 2: Z and dY.
 template <typename TS, typename TA, bool kFours, int kBeside>
 struct SecondEnd {
+  static constexpr bool kExact = kBeside == 2;   // S goes into sums that stay fp32
   Gate<TA> gate;
   int64_t ld_out;
   int n_end;
@@ -157,6 +162,7 @@ struct SecondEnd {
 
 template <typename TS, typename TA, bool kFours>
 struct StoreEnd {
+  static constexpr bool kExact = false;
   int64_t ld;
   int n_end;
   TS* out;
@@ -198,7 +204,7 @@ __device__ __forceinline__ void finish_rows_parts(const Rows& a, const AlongRows
 template <typename TS, int kRT, typename End>
 __global__ __launch_bounds__(kThreads, 2) void parts_rows_kernel(Walk walk, int64_t rows, Operand<float, TS, kPlain> X, AlongRows<float> W,
                                                                  const float* __restrict__ bias, End end) {
-  constexpr int kX = PartCount<TS>::x, kW = PartCount<TS>::w;
+  constexpr int kX = PartCount<TS>::x, kW = weight_parts<TS, End>();
   __shared__ unsigned lds[rows_words<kRT, kX, kW>()];
   for (int64_t t = blockIdx.x; t < walk.count(); t += gridDim.x) {
     int64_t rg;
@@ -214,7 +220,7 @@ __global__ __launch_bounds__(kThreads, 2) void parts_rows_kernel(Walk walk, int6
 template <typename TS, int kWc, int kRounds, int kX, typename Rows, typename Weights, typename Plain, typename End>
 __global__ __launch_bounds__(kThreads, 2) void kept_kernel(Walk walk, int64_t turns, int64_t rows, Rows from, Weights weights, Plain plain,
                                                            const float* __restrict__ bias, End end) {
-  constexpr int kW = PartCount<TS>::w, kWr = kWaves / kWc;
+  constexpr int kW = weight_parts<TS, End>(), kWr = kWaves / kWc;
   constexpr int kTile = kRounds * kX * kPlane, kSlots = kWc > 1 ? 2 : 1;
   __shared__ unsigned lds[kWaves * kSlots * kTile];       // of each group of kWc waves: the planes of kWc tiles, a slot after the other
   __shared__ float corners[kWaves][Corner<float>::kBlock];
@@ -608,8 +614,9 @@ struct Calls {
     const AlongRows<TA> along{static_cast<const TA*>(W), c->k_in, c->k_out};
     if constexpr (sizeof(TA) == 4) {
       if (kept_ok(c, n, c->k_out, c->k_in)) {
-        const PartsColumns<float, kPlain, PartCount<TS>::w> weights{{{along.W, c->k_out}, {}, {}}};
-        return kept<PartCount<TS>::x>(c->k_out, c->k_in, rows_in(X), weights, along, b, make(std::true_type{}));
+        const auto end = make(std::true_type{});
+        const PartsColumns<float, kPlain, weight_parts<TS, std::decay_t<decltype(end)>>()> weights{{{along.W, c->k_out}, {}, {}}};
+        return kept<PartCount<TS>::x>(c->k_out, c->k_in, rows_in(X), weights, along, b, end);
       }
     }
     if constexpr (sizeof(TA) == 4) {

@@ -6,7 +6,8 @@
 //                   the last bit of the largest and of the sum it adds to, so the five small products are summed by themselves and join
 //                   the sum of h h once per 32 reduced indices.
 //   bfloat16 rows   a row's elements are one part.  Results that are rounded to bfloat16 take two parts of W (2^-17 of a weight) and of
-//                   G = dY act' (one where there is no activation); dW and db are fp32 and take all three parts of G.
+//                   G = dY act' (one where there is no activation); dW, db, W2 and b2 are fp32 and take all three parts of G and, for S = V dY act'', of the W
+//                   in V.
 //
 // A lane holds 8 consecutive reduced indices k = 8 q .. 8 q + 7 of index j.  Values that the parts do not stand for (not finite, beyond the largest
 // bfloat16, not zero and below 2^-110) are noted by the wave that meets them, which then computes its tile with the products of

@@ -651,3 +651,30 @@ def test_long_sums_with_values_that_are_not_finite(lib, shape, value, dtype):
     assert not torch.isfinite(dW[3]).any() and not torch.isfinite(dW[:, -1]).any()
     keep = torch.arange(k_in, device="cuda") != 3
     assert torch.isfinite(dW[keep][:, :-1]).all() and torch.isfinite(db[:-1]).all() and not torch.isfinite(db[-1])
+
+
+@pytest.mark.parametrize("k_in,k_out", [(64, 1024), (64, 64), (128, 192), (1000, 72)])
+@pytest.mark.parametrize("rows", [800, 22_985, MANY])
+def test_weight_gradients_of_bfloat16_rows_are_those_of_fp32(lib, rows, k_in, k_out):
+    """dW, db, W2 and b2 are fp32 whatever the rows are.  Values of one sign, so that no sum is small beside its terms: each relative to its own
+    size, (64 + sqrt(n)) u for sums whose roundings are independent, 32 u (1 + |z|) + 256 u for what enters them; on average 64 u = 2^-18, which weights
+    cut to two bfloat16 numbers would pass by half."""
+    torch = lib.torch
+    print(f"dense layer weight gradients {rows} {k_in} {k_out}", flush=True)
+    layer = Layer(lib, rows, k_in, k_out, "silu", "bf16", bias=False, residual=False)
+    for t in (layer.X, layer.dY, layer.HX, layer.W):
+        t.abs_()
+    # weights that lose 1.5 2^-18 of themselves with their third bfloat16 number
+    layer.W.copy_((layer.W.bfloat16().float().clamp(min=2.0 ** -8)) * (1 + 2.0 ** -9 + 2.0 ** -18 + 2.0 ** -19))
+    Z = (torch.rand(rows, k_out, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda") - 0.5).to(torch.bfloat16)   # act'' > 0
+    z, X, W, dY, HX = (t.double() for t in (Z, layer.X, layer.W, layer.dY, layer.HX))
+    p = torch.sigmoid(z)
+    first, second = p + z * p * (1 - p), p * (1 - p) * (2 + z * (1 - 2 * p))
+    G, S = dY * first, (HX @ W) * dY * second
+    _, dW, db = layer.backward(Z)
+    _, _, W2, b2 = layer.double_backward(Z)
+    bound = (64 + rows ** 0.5 + 32 * 1.5 + 256 + k_in ** 0.5) * 2.0 ** -24
+    mean = lambda got, want: ((got.double() - want) / want).mean().abs().item()  # noqa: E731
+    for name, got, want in (("dW", dW, X.T.contiguous() @ G), ("db", db, G.sum(0)), ("W2", W2, X.T.contiguous() @ S + HX.T.contiguous() @ G), ("b2", b2, S.sum(0))):
+        assert ((got.double() - want) / want).abs().max() <= bound, name
+        assert mean(got, want) <= 2.0 ** -18, name
