@@ -1,7 +1,8 @@
 // The dense layer of include/dl.h: products with bias, activation and residual, their gradients and the second-order pass.
 //
 // Every step is a product C[m][n] = sum_k A[m][k] B[k][n] whose operands are made while they are staged
-// (G = dY act'(Z) never exists in memory) and whose result is finished where it stands in the accumulators:
+// (G = dY act'(Z) exists in memory only where several column blocks of dX would each make it again) and whose result is finished where it stands
+// in the accumulators:
 //
 //   forward   rows x k_out   A = X    B = W      epilogue + b, act, + residual -> Y, Z
 //   dX        rows x k_in    A = G    B = W^T
@@ -10,6 +11,16 @@
 //   X2        rows x k_in    A = S    B = W^T
 //   W2, b2    k_in x k_out   A = X^T  B = S, then A = HX^T  B = G on the same accumulators
 // Kernels and launches, instantiated for one type by each of dl_f32.hip, dl_f64.hip and dl_bf16.hip.
+//
+// Which kernel serves a product is a matter of its type and sizes (dl_plan.h):
+//   rows_kernel, backward_kernel              the fp32 and fp64 instruction: fp64, small batches, widths that are no multiple of four.  Few rows and a long
+//                                             sum: all waves of a workgroup share a tile, each a part of the sum.  Bound by the latency of the launch and of
+//                                             a few dependent loads (380 rows, 8 -> 64: 4.9 us), fp64 also by act' (10 000 rows, 128 -> 16: 13 and 24 us).
+//   kept_kernel                               sums of at most 64, many rows: W's parts in registers, the rows once through.  Bound by memory: 199 003 rows, 64 -> 64
+//                                             fp32, forward 41 us and V 50 us at 4.9 and 5.1 TB/s, dX 34 us and X2 22 at 4.5 and 4.7, 64 -> 1280 221 us at 4.8.
+//   parts_rows_kernel, parts_backward_kernel  the other products of many rows or long sums.  64 x 64 blocks of dW: memory (64 -> 64 as above: 32 us at 4.8
+//                                             TB/s, W2 61 us at 4.2).  Wide: the matrix cores and the splitting that feeds them (64 -> 1280 fp32 backward 512
+//                                             us, the products of its parts alone 366; 8191 rows, 1024 -> 1024 bfloat16 146 us, 97).
 #pragma once
 #include "dl_plan.h"
 

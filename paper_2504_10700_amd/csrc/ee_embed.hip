@@ -11,6 +11,9 @@
 //      piece (slot 0: the run came in from the piece before; slot 1: it starts here and goes on);
 //   3. for each element the slots of its pieces are added in order, or its row is zeroed if it is absent.
 // Small batches instead look through all indices for each element: one launch.
+//
+// Measured: 200 000 rows of 128 fp32 channels, 89 elements: forward 18.5 us (5.6 TB/s), count 3.5, scatter 9.2, pieces 30 (3.4 TB/s of dY), join 9.8; 32 768 rows of 512
+// bfloat16 channels, 50 000 elements: forward 16 us, two sort passes 22, pieces 17, join (102 MB of dT, most of it zeros) 25.  61 rows: 2.4 and 3 us.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -316,7 +319,7 @@ __global__ __launch_bounds__(kThreads) void piece_kernel(int64_t n, int64_t piec
 
 // Rows of dT whose rows span pieces, and those of absent elements.  A workgroup has `own` elements: kWaves of a long table, each a wave's, or
 // one of a table with fewer elements than the chip has places for workgroups, which then have kJoinWaves.  Spans from kLongSpan pieces on are
-// shared by all waves (625 pieces of an element with a tenth of 200 000 rows: 19 us by 4 waves, 8 by 16).
+// shared by all waves (625 pieces of an element with a tenth of 200 000 rows: 19 us by 4 waves, 10 by 16).
 constexpr int kLongSpan = 16;
 constexpr int kShortTable = 1024;
 constexpr int kJoinWaves = 16;
