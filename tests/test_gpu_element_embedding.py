@@ -208,3 +208,10 @@ def test_sums_of_small_integers_are_exact(ee, n, elements, channels, dtype):
     inside = z < elements
     want = torch.zeros(elements, channels, dtype=torch.float64, device="cuda").index_add_(0, z[inside].long(), dY[inside].double()) * 0.5
     assert torch.equal(dT, want.to(table))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f64", "bf16"])
+@pytest.mark.parametrize("n,elements,channels", [(838, 10_000, 64), (839, 10_000, 64), (128, 65_536, 33), (8, 999_999, 4), (67, 999_999, 4), (70, 999_999, 4), (1024, 65_536, 33), (1024, 65_537, 33), (1024, 8192, 130), (1024, 8193, 130)])
+def test_few_rows_of_long_tables(ee, n, elements, channels, dtype):
+    print(f"embedding {n} {elements} {channels} {dtype}", flush=True)
+    check(ee, n, elements, channels, dtype, "outside")
