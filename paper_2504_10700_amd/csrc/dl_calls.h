@@ -27,23 +27,17 @@
 namespace dl {
 namespace {
 
-// Parts of the operands on the bfloat16 matrix cores (dl_parts.h): of X, of W, of the source of dX and of that of dW.
+// Parts of an operand on the bfloat16 matrix cores (dl_parts.h): an element that is stored in bfloat16 is one, whatever is computed or stored in fp32 three.
+// (fp64: no parts.)
+constexpr int kWeightParts = 3;
+template <typename T, Source kSource>
+constexpr int parts_of(const Operand<float, T, kSource>*) { return sizeof(T) == 2 && kSource == kPlain ? 1 : 3; }
+template <typename T, Source kSource>
+constexpr int parts_of(const Operand<double, T, kSource>*) { return 0; }
+template <typename O>
+constexpr int kPartsOf = parts_of(static_cast<O*>(nullptr));
 template <typename TS>
-struct PartCount {
-  static constexpr int x = sizeof(TS) == 2 ? 1 : 3, w = sizeof(TS) == 2 ? 2 : 3;
-  template <typename T, Source kSource>
-  static constexpr int dx(const Operand<float, T, kSource>*) { return sizeof(TS) != 2 ? 3 : sizeof(T) == 2 && kSource == kPlain ? 1 : 2; }
-  template <typename T, Source kSource>
-  static constexpr int dw(const Operand<float, T, kSource>*) { return sizeof(T) == 2 && kSource == kPlain ? 1 : 3; }
-  // fp64: no parts
-  template <typename T, Source kSource>
-  static constexpr int dx(const Operand<double, T, kSource>*) { return 0; }
-  template <typename T, Source kSource>
-  static constexpr int dw(const Operand<double, T, kSource>*) { return 0; }
-};
-// Parts of W in a product of rows with an epilogue.
-template <typename TS, typename End>
-constexpr int weight_parts() { return End::kExact ? 3 : PartCount<TS>::w; }
+constexpr int kRowParts = sizeof(TS) == 2 ? 1 : 3;
 template <int kParts, typename T, Source kSource>
 __device__ __forceinline__ PartsRows<T, kSource, kParts> as_rows(const Operand<float, T, kSource>& o) { return {o}; }
 template <int kParts, typename T, Source kSource>
@@ -113,7 +107,6 @@ __device__ __forceinline__ void each_tile(const Walk& walk, const Shape& shape, 
 // What becomes of four neighbouring results v of a row.  The constructor takes what is the same for a lane's column.
 template <typename TS, typename TA, bool kFours, int kResidual>
 struct ForwardEnd {   // Z = v (bias added), Y = act(Z) + residual
-  static constexpr bool kExact = false;   // nothing goes further than to results in the type of the rows
   Gate<TA> gate;
   int64_t ld_out;
   int n_end;
@@ -141,7 +134,6 @@ struct ForwardEnd {   // Z = v (bias added), Y = act(Z) + residual
 // v = V: ddY = V act'(Z), S = V dY act''(Z).  kBeside 0: no activation; 1: no curvature (Z alone is read, no S); 2: Z and dY.
 template <typename TS, typename TA, bool kFours, int kBeside>
 struct SecondEnd {
-  static constexpr bool kExact = kBeside == 2;   // S goes into sums that stay fp32
   Gate<TA> gate;
   int64_t ld_out;
   int n_end;
@@ -173,7 +165,6 @@ struct SecondEnd {
 
 template <typename TS, typename TA, bool kFours>
 struct StoreEnd {
-  static constexpr bool kExact = false;
   int64_t ld;
   int n_end;
   TS* out;
@@ -193,7 +184,7 @@ __global__ __launch_bounds__((threads<kSplit, TA>())) void rows_kernel(Walk walk
   });
 }
 
-// Parts of the operands on the bfloat16 matrix cores (dl_parts.h): of X, of W, of the source of dX and of that of dW.
+// Words of LDS of a product of rows on parts.
 template <int kRT, int kX, int kW>
 constexpr int rows_words() { return kWaves * kRT * kX * kPlane + shared_words<kW>(); }
 
@@ -215,7 +206,7 @@ __device__ __forceinline__ void finish_rows_parts(const Rows& a, const AlongRows
 template <typename TS, int kRT, typename End>
 __global__ __launch_bounds__(kThreads, 2) void parts_rows_kernel(Walk walk, int64_t rows, Operand<float, TS, kPlain> X, AlongRows<float> W,
                                                                  const float* __restrict__ bias, End end) {
-  constexpr int kX = PartCount<TS>::x, kW = weight_parts<TS, End>();
+  constexpr int kX = kRowParts<TS>, kW = kWeightParts;
   __shared__ unsigned lds[rows_words<kRT, kX, kW>()];
   for (int64_t t = blockIdx.x; t < walk.count(); t += gridDim.x) {
     int64_t rg;
@@ -231,7 +222,7 @@ __global__ __launch_bounds__(kThreads, 2) void parts_rows_kernel(Walk walk, int6
 template <typename TS, int kWc, int kRounds, int kX, typename Rows, typename Weights, typename Plain, typename End>
 __global__ __launch_bounds__(kThreads, 2) void kept_kernel(Walk walk, int64_t turns, int64_t rows, Rows from, Weights weights, Plain plain,
                                                            const float* __restrict__ bias, End end) {
-  constexpr int kW = weight_parts<TS, End>(), kWr = kWaves / kWc;
+  constexpr int kW = kWeightParts, kWr = kWaves / kWc;
   constexpr int kTile = kRounds * kX * kPlane, kSlots = kWc > 1 ? 2 : 1;
   __shared__ unsigned lds[kWaves * kSlots * kTile];       // of each group of kWc waves: the planes of kWc tiles, a slot after the other
   __shared__ float corners[kWaves][Corner<float>::kBlock];
@@ -472,10 +463,9 @@ __global__ __launch_bounds__(kThreads, kWide || kDx ? 2 : 3) void parts_backward
                                                                      TS* __restrict__ dX, Operand<float, TS, kPlain> x, B b,
                                                                      Operand<float, TS, kPlain> x2, B2 b2, float* __restrict__ dW,
                                                                      float* __restrict__ db) {
-  typedef PartCount<TS> Count;
-  constexpr int kG = Count::dx(static_cast<G*>(nullptr)), kB = Count::dw(static_cast<B*>(nullptr)), kB2 = Count::dw(static_cast<B2*>(nullptr));
-  constexpr int kDxWords = kDx ? rows_words<kRT, kG, Count::w>() : 0;
-  constexpr int kDwWords = shared_words<Count::x>() + (kWide ? 0 : shared_words<(kB > kB2 ? kB : kB2)>());
+  constexpr int kX = kRowParts<TS>, kG = kPartsOf<G>, kB = kPartsOf<B>, kB2 = kPartsOf<B2>;
+  constexpr int kDxWords = kDx ? rows_words<kRT, kG, kWeightParts>() : 0;
+  constexpr int kDwWords = shared_words<kX>() + (kWide ? 0 : shared_words<(kB > kB2 ? kB : kB2)>());
   __shared__ unsigned lds[kDxWords > kDwWords ? kDxWords : kDwWords];
   const Deal deal = p.deal();
   const int64_t total = deal.count();
@@ -488,10 +478,10 @@ __global__ __launch_bounds__(kThreads, kWide || kDx ? 2 : 3) void parts_backward
         const int n0 = static_cast<int>(i % p.dx_col_groups) * kCols;
         const float* const none = nullptr;
         if (row0 < end)
-          finish_rows_parts<kRT, kG, Count::w>(g, WT, row0, end, n0, lds, none, Beside<TS, 0>{}, StoreEnd<TS, float, true>{ld_in, k_in, dX});
+          finish_rows_parts<kRT, kG, kWeightParts>(g, WT, row0, end, n0, lds, none, Beside<TS, 0>{}, StoreEnd<TS, float, true>{ld_in, k_in, dX});
       }
     } else {
-      parts_dw_role<kWide, kTwo, Count::x, kB, kB2>(p, chunk, static_cast<int>(i - p.dx_groups), k_in, k_out, x, b, x2, b2, dW, db, lds);
+      parts_dw_role<kWide, kTwo, kX, kB, kB2>(p, chunk, static_cast<int>(i - p.dx_groups), k_in, k_out, x, b, x2, b2, dW, db, lds);
     }
     __syncthreads();
   }
@@ -626,8 +616,8 @@ struct Calls {
     if constexpr (sizeof(TA) == 4) {
       if (kept_ok(c, n, c->k_out, c->k_in)) {
         const auto end = make(std::true_type{});
-        const PartsColumns<float, kPlain, weight_parts<TS, std::decay_t<decltype(end)>>()> weights{{{along.W, c->k_out}, {}, {}}};
-        return kept<PartCount<TS>::x>(c->k_out, c->k_in, rows_in(X), weights, along, b, end);
+        const PartsColumns<float, kPlain, kWeightParts> weights{{{along.W, c->k_out}, {}, {}}};
+        return kept<kRowParts<TS>>(c->k_out, c->k_in, rows_in(X), weights, along, b, end);
       }
     }
     if constexpr (sizeof(TA) == 4) {
@@ -704,8 +694,8 @@ struct Calls {
     if constexpr (sizeof(TA) == 4) {
       if (dX && kept_ok(c, n, c->k_in, c->k_out)) {   // dX by itself, then dW
         const float* w = static_cast<const float*>(W);
-        const PartsTransposed<PartCount<TS>::w> weights{{w, c->k_out}};
-        const hipError_t e = kept<PartCount<TS>::dx(static_cast<G*>(nullptr))>(c->k_in, c->k_out, source, weights, AlongColumns<float>{w, c->k_out, c->k_in},
+        const PartsTransposed<kWeightParts> weights{{w, c->k_out}};
+        const hipError_t e = kept<kPartsOf<G>>(c->k_in, c->k_out, source, weights, AlongColumns<float>{w, c->k_out, c->k_in},
                                                                                 nullptr, StoreEnd<TS, float, true>{ld_in(c), c->k_in, static_cast<TS*>(dX)});
         return e != hipSuccess || !(dW || db) ? e : gradients<kTwo>(source, W, nullptr, X, b, X2, b2, dW, db, ws);
       }

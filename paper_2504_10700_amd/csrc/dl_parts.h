@@ -5,9 +5,7 @@
 //   fp32 rows       h h + (h m + m h + m m + h l + l h): what is left out is below 2^-24 of |x w|.  An instruction cuts its smaller products off at
 //                   the last bit of the largest and of the sum it adds to, so the five small products are summed by themselves and join
 //                   the sum of h h once per 32 reduced indices.
-//   bfloat16 rows   a row's elements are one part.  Results that are rounded to bfloat16 take two parts of W (2^-17 of a weight) and of
-//                   G = dY act' (one where there is no activation); dW, db, W2 and b2 are fp32 and take all three parts of G and, for S = V dY act'', of the W
-//                   in V.
+//   bfloat16 rows   an element of them is one part; W, G = dY act' and S = V dY act'' are fp32 values and keep their three.
 //
 // A lane holds 8 consecutive reduced indices k = 8 q .. 8 q + 7 of index j.  Values that the parts do not stand for (not finite, beyond the largest
 // bfloat16, not zero and below 2^-110) are noted by the wave that meets them, which then computes its tile with the products of
@@ -65,16 +63,10 @@ __device__ __forceinline__ float gated(const Gate<float>& gate, float x, float z
   return g;
 }
 
-// Pairs of values into parts, in the halves of a register each.  low: collects what the last part is rounded from (el::split_pair).
-template <int N>
-__device__ __forceinline__ void split(float x, float y, unsigned (&part)[N], unsigned& low) {
-  if constexpr (N == 3) {
-    const SplitPair s = split_pair(x, y, low);
-    part[0] = s.h, part[1] = s.m, part[2] = s.l;
-  } else {
-    part[0] = pack_bf16(x, y);
-    if constexpr (N == 2) part[1] = pack_bf16(x - el::low_half(part[0]), y - el::high_half(part[0]));
-  }
+// Pairs of values into three parts, in the halves of a register each.  low: collects what the last part is rounded from (el::split_pair).
+__device__ __forceinline__ void split(float x, float y, unsigned (&part)[3], unsigned& low) {
+  const SplitPair s = split_pair(x, y, low);
+  part[0] = s.h, part[1] = s.m, part[2] = s.l;
 }
 
 // Rows as an operand: 16 rows x 32 reduced indices in kParts planes of the wave's corner of LDS (16 rows of 64 bytes each, the four pieces of a
@@ -133,8 +125,8 @@ struct PartsRows<float, kSource, kParts> {
         for (int i = 0; i < 4; ++i) v[i] = inside ? gated(from.gate, v[i], raw.z[h][i]) : 0.f;
       }
       unsigned a[kParts], b[kParts];
-      split<kParts>(v[0], v[1], a, low);
-      split<kParts>(v[2], v[3], b, low);
+      split(v[0], v[1], a, low);
+      split(v[2], v[3], b, low);
       const int to = piece_at(8 * h + lane / 8, lane % 8 / 2) + 2 * (lane & 1);
 #pragma unroll
       for (int p = 0; p < kParts; ++p) *reinterpret_cast<U2*>(planes + p * kPlane + to) = U2{a[p], b[p]};
@@ -155,7 +147,7 @@ struct PartsRows<__bf16, kSource, kParts> {
     raw.v = load_piece<U4>(from.x, start, r, k, column(), k_end);
     if constexpr (kSource == kGated) raw.z = load_piece<U4>(from.z, start, r, k, column(), k_end);
   }
-  __device__ __forceinline__ void put(Raw& raw, int k, int k_end, unsigned* planes, unsigned&) const {
+  __device__ __forceinline__ void put(Raw& raw, int k, int k_end, unsigned* planes, unsigned& low) const {
     const int lane = threadIdx.x & (kLanes - 1);
     const bool inside = k + column() < k_end;
     U4 part[kParts];
@@ -167,8 +159,8 @@ struct PartsRows<__bf16, kSource, kParts> {
       for (int i = 0; i < 4; ++i) {
         const float x = gated(from.gate, el::low_half(raw.v[i]), el::low_half(raw.z[i]));
         const float y = gated(from.gate, el::high_half(raw.v[i]), el::high_half(raw.z[i]));
-        unsigned s[kParts], ignored = 0;
-        split<kParts>(inside ? x : 0.f, inside ? y : 0.f, s, ignored);
+        unsigned s[kParts];
+        split(inside ? x : 0.f, inside ? y : 0.f, s, low);
 #pragma unroll
         for (int p = 0; p < kParts; ++p) part[p][i] = s[p];
       }
@@ -238,7 +230,7 @@ struct ColumnsRaw {
         b = gated(from.gate, b, static_cast<float>(z[i + 1][u]));
       }
       if constexpr (kSum) sum += a + b;
-      split<kParts>(a, b, s, low);
+      split(a, b, s, low);
     }
   }
 };
@@ -484,7 +476,7 @@ struct PartsTransposed {
 #pragma unroll
     for (int i = 0; i < 8; i += 2) {
       unsigned s[kParts];
-      split<kParts>(raw.v[u][i / 4][i % 4], raw.v[u][i / 4][i % 4 + 1], s, low);
+      split(raw.v[u][i / 4][i % 4], raw.v[u][i / 4][i % 4 + 1], s, low);
 #pragma unroll
       for (int p = 0; p < kParts; ++p) part[p][i / 2] = s[p];
     }

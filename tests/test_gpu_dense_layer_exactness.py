@@ -1,0 +1,114 @@
+"""The dense layer (include/dl.h) where a wrong last bit shows: results far smaller than their terms, derivatives far below 1, overflow.
+
+Tolerances stand with each test; u = 2^-24.
+"""
+import numpy as np
+import pytest
+
+from oracle import dense_layer as od
+from test_gpu_dense_layer import MANY, Layer, host, lib  # noqa: F401  (lib: the fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+def signs(n):
+    """1, -1, 1, -1, ... and the index of the pair."""
+    i = np.arange(n)
+    return 1.0 - 2.0 * (i % 2), i // 2
+
+
+def sparse(rng, rows, k):
+    """Rows of zeros but for up to four pairs of equal neighbours, +1 or -1 each."""
+    x = np.zeros((rows, k))
+    pairs = rng.random((rows, k // 2)).argsort(axis=1)[:, :4] if rows <= 4000 else rng.integers(0, k // 2, (rows, 4))
+    sign = rng.choice([-1.0, 1.0], pairs.shape)
+    for c in range(pairs.shape[1]):
+        for odd in (0, 1):
+            x[np.arange(rows), 2 * pairs[:, c] + odd] = sign[:, c]
+    return x
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("act", ["none", "relu"])
+@pytest.mark.parametrize("rows,k_in,k_out", [(40, 10, 14), (300, 64, 64), (MANY, 64, 64), (MANY, 32, 200), (20_011, 64, 1280), (8003, 128, 128), (600, 1000, 1024),
+                                             (2100, 1024, 260), (6000, 264, 128)])
+def test_every_bit_of_a_weight_counts(lib, rows, k_in, k_out, act, dtype):
+    """W[k][n] = +-(2 + c 2^-12) + j 2^-19, neighbours of opposite sign: their equal partners in a row cancel all but the j.  At most eight terms below 4 in
+    size, all multiples of 2^-19: exact in fp32 in any order, so a result in fp32 is exact and one in bfloat16 rounded once."""
+    torch = lib.torch
+    print(f"dense layer, bits of W, {rows} {k_in} {k_out} {act} {dtype}", flush=True)
+    rng = np.random.default_rng(rows + k_in)
+    (s_k, p_k), (s_n, p_n) = signs(k_in), signs(k_out)
+    common = 2 + (2 * rng.integers(0, 1024, (k_in // 2 + 1, k_out // 2 + 1)) + 1) * 2.0 ** -12
+    W = s_k[:, None] * s_n[None] * common[np.ix_(p_k, p_n)] + rng.integers(-31, 32, (k_in, k_out)) * 2.0 ** -19
+    layer = Layer(lib, rows, k_in, k_out, act, dtype, bias=False, residual=False)
+    layer.W.copy_(torch.tensor(W))
+    for t, k in ((layer.X, k_in), (layer.HX, k_in), (layer.dY, k_out)):
+        t.copy_(torch.tensor(sparse(rng, rows, k)))
+    X, Wd, dY, HX = (t.double() for t in (layer.X, layer.W, layer.dY, layer.HX))
+    assert torch.equal(layer.W.double().cpu(), torch.tensor(W))
+
+    def same(name, got, ref):
+        wrong = int((got != ref.to(got.dtype)).sum())
+        assert wrong == 0, f"{name}: {wrong} of {got.numel()} elements differ"
+
+    Y, Z = layer.forward()
+    z = torch.matmul(X, Wd)
+    assert 0 < z.abs().max() < 2.0 ** -10
+    same("Z", Z, z)
+    same("Y", Y, z.clamp(min=0) if act == "relu" else z)
+    gate = layer.wide(1, torch.where(torch.rand(rows, 1, device="cuda") < 0.9, 1.0, -1.0).expand(rows, k_out))
+    on = (gate.double() > 0).double() if act == "relu" else torch.ones_like(z)
+    given = gate if act == "relu" else None
+    same("dX", layer.backward(given, "X")[0], torch.matmul(dY * on, Wd.t().contiguous()))
+    same("dX beside dW", layer.backward(given)[0], torch.matmul(dY * on, Wd.t().contiguous()))
+    same("ddY", layer.double_backward(given)[0], torch.matmul(HX, Wd) * on)
+
+
+def near_pairs(order, act, count):
+    """Pairs of pre-activations (bfloat16 numbers) whose derivatives of that order agree to 2^-14 while the first 16 bits of the derivatives differ most from them."""
+    import torch
+    bf16 = lambda x: torch.tensor(x, dtype=torch.float32).bfloat16().double().numpy()  # noqa: E731
+    z = np.unique(bf16(np.linspace(-4, 4, 200_001)))
+    z = z[np.abs(z) >= 2.0 ** -6]
+    d = od.activation(act, z)[order]
+    whole = d.astype(np.float32).astype(np.float64)
+    rest = whole - bf16(whole)
+    rest -= bf16(rest)
+    i = np.argsort(d)
+    gap = np.abs(rest[i[1:]] - rest[i[:-1]]) * (np.abs(d[i[1:]] - d[i[:-1]]) <= 2.0 ** -14)
+    best = np.argsort(gap)[::-1][:count]
+    assert gap[best].min() > 40 * 2.0 ** -24
+    return z[i[best]], z[i[best + 1]]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("rows,k_in", [(48, 8), (MANY, 64), (MANY, 132), (20_003, 260)])
+def test_every_bit_of_a_derivative_counts(lib, rows, k_in, act, dtype):
+    """dX = w (act'(z) - act'(z~)) and X2 = w (act''(z) - act''(z~)) for pairs that nearly cancel.  Each derivative in fp32 is within 4 u (act') and 8 u (act'') of its
+    value for |z| <= 4 (u of the exponential, the reciprocal and six to ten operations on values below 1): 8 u and 16 u of the pair, and the result's last rounding."""
+    torch, u = lib.torch, 2.0 ** -24
+    print(f"dense layer, bits of derivatives, {rows} {k_in} {act} {dtype}", flush=True)
+    pairs = 16
+    layer = Layer(lib, rows, k_in, 2 * pairs, act, dtype, bias=False, residual=False)
+    w = torch.tensor([1.0, -2.0, 0.5, 4.0], device="cuda").repeat(k_in // 4)
+    layer.W.copy_(w[:, None] * torch.tensor(signs(2 * pairs)[0], device="cuda")[None])
+    mine = torch.arange(rows, device="cuda") % pairs
+    own_pair = (torch.arange(2 * pairs, device="cuda") // 2)[None] == mine[:, None]
+    layer.HX.zero_()
+    layer.HX[:, 0] = 1.0                                    # V = W[0] = +-1
+    for order, bound in ((1, 8 * u), (2, 16 * u)):
+        a, b = near_pairs(order, act, pairs)
+        Z = layer.wide(1, torch.tensor(np.stack([a, b], 1).reshape(-1), device="cuda")[None].expand(rows, 2 * pairs))
+        if order == 1:
+            layer.dY.copy_(own_pair.double())
+            got = (layer.backward(Z, "X")[0], layer.backward(Z)[0])
+        else:
+            layer.dY.copy_(own_pair.double() * torch.tensor(signs(2 * pairs)[0], device="cuda")[None])
+            got = (layer.double_backward(Z, "X")[1], layer.double_backward(Z)[1])
+        d = od.activation(act, host(Z)[0])[order]
+        want = torch.tensor(d[0::2] - d[1::2], device="cuda")[mine][:, None] * w.double()
+        slack = bound * w.abs().double() + 2.0 ** -8 * want.abs()
+        for g in got:
+            assert ((g.double() - want).abs() <= slack).all(), f"order {order}: {(((g.double() - want).abs() - slack) / w.abs()).max().item() / u:.1f} u beyond"
