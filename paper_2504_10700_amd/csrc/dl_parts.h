@@ -576,9 +576,8 @@ __device__ __forceinline__ void walk_rows(const Rows& a, const Kept<kRounds, kW>
       }
       join4<kX, kW>(acc[0], small);
       if constexpr (kWc > 1) low = flags[slot * kWc + i];
-      // (a row with a value that is not finite has a NaN in every column: the first tile's will do)
-      const Acc(&one)[1][1] = reinterpret_cast<const Acc(&)[1][1]>(acc[0][0]);
-      const bool served = kept.served && !unserved<1, 1>(one, low);
+      // (all four tiles: a row that is not finite shows in each of them, a product beyond the largest number in its own only)
+      const bool served = kept.served && !unserved<1, 4>(acc, low);
       float x[4][M][4];
 #pragma unroll
       for (int e = 0; e < N; ++e)

@@ -112,3 +112,27 @@ def test_every_bit_of_a_derivative_counts(lib, rows, k_in, act, dtype):
         slack = bound * w.abs().double() + 2.0 ** -8 * want.abs()
         for g in got:
             assert ((g.double() - want).abs() <= slack).all(), f"order {order}: {(((g.double() - want).abs() - slack) / w.abs()).max().item() / u:.1f} u beyond"
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("column", [4, 5, 6, 7])
+@pytest.mark.parametrize("rows,k_in,k_out", [(MANY, 64, 64), (MANY, 32, 128), (MANY, 64, 260), (MANY, 100, 100), (50, 64, 64)])
+def test_a_product_beyond_the_largest_number_is_infinite(lib, rows, k_in, k_out, column, dtype):
+    """1.5 2^127 times 2^17 (1 - 2^-10), which is 2^17 in eight bits and -2^7 beside it: infinity, not the difference of two infinities; everything else of the row
+    is an exact product."""
+    torch = lib.torch
+    print(f"dense layer, overflow in column {column}, {rows} {k_in} {k_out} {dtype}", flush=True)
+    layer = Layer(lib, rows, k_in, k_out, "none", dtype, bias=False, residual=False)
+    large, factor, row = 1.5 * 2.0 ** 127, 2.0 ** 17 * (1 - 2.0 ** -10), rows // 2
+    layer.W.fill_(0.5)
+    layer.W[column, column] = factor
+    layer.X[row] = 0
+    layer.X[row, column] = large
+    layer.dY[row] = 0
+    layer.dY[row, column] = -large
+    Y, _ = layer.forward()
+    for got, k, value in ((Y, k_out, large), (layer.backward(None, "X")[0], k_in, -large)):
+        want = torch.full((k,), 0.5 * value, dtype=torch.float64, device="cuda")
+        want[column] = float("inf") if value > 0 else -float("inf")
+        assert torch.equal(got[row].double(), want)
+        assert torch.isfinite(got[:row]).all() and torch.isfinite(got[row + 1:]).all()
