@@ -14,8 +14,7 @@
  * Types.  SC_F32: everything fp32; SC_F64: everything fp64; SC_BF16: the tensors with a row
  * per edge or atom (X, Y, Z, residual, dY, dX, HX, ddY, X2) bfloat16, the weights and their
  * gradients (W, b, dW, db, W2, b2) fp32.  Products and sums in fp64 for SC_F64; otherwise sums are
- * fp32 and products have the exactness of fp32 ones: rows of bfloat16 are rounded once, at the end.  A derivative
- * act' or act'' below 2^-60 in size may count as zero in fp32 sums.
+ * fp32 and products have the exactness of fp32 ones: rows of bfloat16 are rounded once, at the end.
  *
  * Strides.  Rows of X, dX, HX, X2 are ld_in elements apart, rows of Y, Z, residual, dY, ddY ld_out
  * (0: dense, k_in and k_out), so that a layer can read the invariant channels of features laid

@@ -151,8 +151,8 @@ struct SecondEnd {
       TA first = TA(1), second = TA(0);
       if constexpr (kBeside > 0) gate.both(x[0][i], &first, &second);
       out[i] = v[i] * first;
-      if constexpr (kBeside == 2) g[i] = x[1][i] * (sizeof(TA) == 4 ? Gate<TA>::cut(first) : first);
-      if constexpr (kBeside == 2) s[i] = v[i] * x[1][i] * (sizeof(TA) == 4 ? Gate<TA>::cut(second) : second);
+      if constexpr (kBeside == 2) g[i] = x[1][i] * first;
+      if constexpr (kBeside == 2) s[i] = v[i] * x[1][i] * second;
     }
     if constexpr (kBeside == 2) {
       const Spot spot{row * n_end, static_cast<unsigned>(lr * n_end + c)};
@@ -197,9 +197,10 @@ __device__ __forceinline__ void finish_rows_parts(const Rows& a, const AlongRows
   unsigned* const planes = lds + wave * (kRT * kX * kPlane);
   const Operand<float, float, kPlain> matrix{{w.W, w.n_end}, {}, {}};
   const int64_t first = row0 + wave * (16 * kRT);
-  if (!rows_parts<kRT, kX, kW>(as_rows<kX>(a), SharedColumns<float, kPlain, kW>{matrix}, first, rows, n0, w.n_end, w.k_end, planes,
-                               lds + kWaves * kRT * kX * kPlane, acc))
-    rows_product<float, kRT, true>(a, w, first, rows, n0, 0, w.k_end, reinterpret_cast<float*>(planes), acc);
+  const bool done = rows_parts<kRT, kX, kW>(as_rows<kX>(a), SharedColumns<float, kPlain, kW>{matrix}, first, rows, n0, w.n_end, w.k_end, planes,
+                                            lds + kWaves * kRT * kX * kPlane, acc);
+  if (!done) rows_product<float, kRT, true>(a, w, first, rows, n0, 0, w.k_end, reinterpret_cast<float*>(planes), acc);
+  unscale<Rows::source>(acc, done);
   each_four<float, kRT, true>(first, rows, n0, w.n_end, acc, bias, beside, f);
 }
 
@@ -421,6 +422,8 @@ __device__ __forceinline__ void parts_dw_role(const Plan& p, int64_t chunk, int 
       }
     }
   }
+  static_assert(!kTwo || kScale<B::source> == kScale<B2::source>, "both are in the same sums");
+  unscale<B::source>(acc, done);
   const int n = n0 + 4 * j;
   if (dW && n < k_out) {
     float* const to_dw = dW + chunk * p.stride;
@@ -499,7 +502,7 @@ __global__ __launch_bounds__(kThreads) void gate_kernel(int64_t rows, int cols, 
     load4<kFours>(dY + row * ld, c, cols, g);
     load4<kFours>(Z + row * ld, c, cols, z);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) g[k] *= sizeof(TA) == 4 ? Gate<TA>::cut(gate.first(z[k])) : gate.first(z[k]);
+    for (int k = 0; k < 4; ++k) g[k] *= gate.first(z[k]);
     store4<kFours>(G + row * cols + c, c, cols, g);
   }
 }
@@ -786,7 +789,7 @@ struct Calls {
     if (g_first(c, n)) {
       const hipError_t e = make_g(dY, Z, static_cast<TA*>(ws));
       if (e != hipSuccess) return e;
-      const Operand<TA, TA, kPlain> made{{static_cast<const TA*>(ws), c->k_out}, {}, {}};
+      const Operand<TA, TA, kMade> made{{static_cast<const TA*>(ws), c->k_out}, {}, {}};
       return gradients<false>(made, W, dX, X, made, X, made, dW, db, static_cast<char*>(ws) + s_bytes(c, n));
     }
     return gradients<false>(g<kGated>(dY, Z), W, dX, X, g<kGated>(dY, Z), X, g<kGated>(dY, Z), dW, db, ws);
@@ -827,7 +830,7 @@ struct Calls {
       return gradients<false>(g<kGated>(dY, Z), W, nullptr, HX, g<kGated>(dY, Z), HX, g<kGated>(dY, Z), W2, nullptr, part);
     }
     if (!X2 && !W2 && !b2) return hipSuccess;
-    const Operand<TA, TA, kPlain> s{{S, c->k_out}, {}, {}}, made{{G, c->k_out}, {}, {}};
+    const Operand<TA, TA, kMade> s{{S, c->k_out}, {}, {}}, made{{G, c->k_out}, {}, {}};
     if (G) return gradients<true>(s, W, X2, X, s, HX, made, W2, b2, part);
     return gradients<true>(s, W, X2, X, s, HX, g<kGated>(dY, Z), W2, b2, part);
   }

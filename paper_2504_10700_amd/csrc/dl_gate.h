@@ -67,10 +67,6 @@ struct Gate {
     return g.p + g.z * g.pq * g.u1;
   }
 
-  // Derivatives below 2^-60 as zero.  For the products on parts: beside what they multiply they are far below the last bit of any sum, and the
-  // parts of products that small would not stand for them.
-  static __device__ __forceinline__ T cut(T d) { return d < T(8.67e-19) && d > T(-8.67e-19) ? T(0) : d; }
-
   __device__ __forceinline__ void both(T z, T* first_out, T* second) const {
     const Point g = at(z);
     *first_out = g.p + g.z * g.pq * g.u1;

@@ -7,6 +7,10 @@
 //                   the sum of h h once per 32 reduced indices.
 //   bfloat16 rows   an element of them is one part; W, G = dY act' and S = V dY act'' are fp32 values and keep their three.
 //
+// G and S hold derivatives of the activations, which fall to nothing far out: a GELU layer whose pre-activations have a deviation of 2 has some below
+// 2^-110 in every tile.  Their parts are those of 2^16 times the value, which stand for every fp32 number below 2^111, and the sums are divided by 2^16
+// at the end.
+//
 // A lane holds 8 consecutive reduced indices k = 8 q .. 8 q + 7 of index j.  Values that the parts do not stand for (not finite, beyond the largest
 // bfloat16, not zero and below 2^-110) are noted by the wave that meets them, which then computes its tile with the products of
 // dl_product.h.
@@ -24,6 +28,21 @@ typedef unsigned U2 __attribute__((ext_vector_type(2)));
 typedef Mma<float>::acc_t Acc;
 
 constexpr int kRound = 32;   // reduced indices per round
+
+// What an operand's values are multiplied by.
+template <Source kSource>
+constexpr float kScale = kSource == kPlain ? 1.f : 65536.f;
+// Sums of such an operand's parts to sums of its values.  done: false for those that were made without parts.
+template <Source kSource, int kR, int kC>
+__device__ __forceinline__ void unscale(Acc (&acc)[kR][kC], bool done) {
+  if constexpr (kScale<kSource> != 1.f) {
+    const float down = done ? 1 / kScale<kSource> : 1.f;
+#pragma unroll
+    for (int i = 0; i < kR; ++i)
+#pragma unroll
+      for (int t = 0; t < kC; ++t) acc[i][t] *= down;
+  }
+}
 
 __device__ __forceinline__ Acc mma_parts(const U4& a, const U4& b, const Acc& c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(Bf8, a), __builtin_bit_cast(Bf8, b), c, 0, 0, 0);
@@ -59,13 +78,14 @@ __device__ __forceinline__ void join4(Acc (&sum)[4], const Acc (&small)[4]) {
 // parts hold.
 __device__ __forceinline__ float gated(const Gate<float>& gate, float x, float z) {
 #pragma clang fp contract(off)
-  const float g = x * Gate<float>::cut(gate.first(z));
+  const float g = x * gate.first(z);
   return g;
 }
 
 // Pairs of values into three parts, in the halves of a register each.  low: collects what the last part is rounded from (el::split_pair).
+template <Source kSource>
 __device__ __forceinline__ void split(float x, float y, unsigned (&part)[3], unsigned& low) {
-  const SplitPair s = split_pair(x, y, low);
+  const SplitPair s = split_pair(x * kScale<kSource>, y * kScale<kSource>, low);
   part[0] = s.h, part[1] = s.m, part[2] = s.l;
 }
 
@@ -94,6 +114,7 @@ __device__ __forceinline__ V load_piece(const Matrix<T>& m, int64_t row0, int r,
 
 template <Source kSource, int kParts>
 struct PartsRows<float, kSource, kParts> {
+  static constexpr Source source = kSource;
   Operand<float, float, kSource> from;
   typedef float F4 __attribute__((ext_vector_type(4)));
   struct Raw {
@@ -125,8 +146,8 @@ struct PartsRows<float, kSource, kParts> {
         for (int i = 0; i < 4; ++i) v[i] = inside ? gated(from.gate, v[i], raw.z[h][i]) : 0.f;
       }
       unsigned a[kParts], b[kParts];
-      split(v[0], v[1], a, low);
-      split(v[2], v[3], b, low);
+      split<kSource>(v[0], v[1], a, low);
+      split<kSource>(v[2], v[3], b, low);
       const int to = piece_at(8 * h + lane / 8, lane % 8 / 2) + 2 * (lane & 1);
 #pragma unroll
       for (int p = 0; p < kParts; ++p) *reinterpret_cast<U2*>(planes + p * kPlane + to) = U2{a[p], b[p]};
@@ -136,7 +157,8 @@ struct PartsRows<float, kSource, kParts> {
 
 template <Source kSource, int kParts>
 struct PartsRows<__bf16, kSource, kParts> {
-  static_assert(kSource == kGated || kParts == 1, "an element is one part");
+  static_assert(kSource != kPlain || kParts == 1, "an element is one part");
+  static constexpr Source source = kSource;
   Operand<float, __bf16, kSource> from;
   struct Raw {
     U4 v, z;   // lane 4 row + piece of eight elements
@@ -160,7 +182,7 @@ struct PartsRows<__bf16, kSource, kParts> {
         const float x = gated(from.gate, el::low_half(raw.v[i]), el::low_half(raw.z[i]));
         const float y = gated(from.gate, el::high_half(raw.v[i]), el::high_half(raw.z[i]));
         unsigned s[kParts];
-        split(inside ? x : 0.f, inside ? y : 0.f, s, low);
+        split<kSource>(inside ? x : 0.f, inside ? y : 0.f, s, low);
 #pragma unroll
         for (int p = 0; p < kParts; ++p) part[p][i] = s[p];
       }
@@ -230,7 +252,7 @@ struct ColumnsRaw {
         b = gated(from.gate, b, static_cast<float>(z[i + 1][u]));
       }
       if constexpr (kSum) sum += a + b;
-      split(a, b, s, low);
+      split<kSource>(a, b, s, low);
     }
   }
 };
@@ -476,7 +498,7 @@ struct PartsTransposed {
 #pragma unroll
     for (int i = 0; i < 8; i += 2) {
       unsigned s[kParts];
-      split(raw.v[u][i / 4][i % 4], raw.v[u][i / 4][i % 4 + 1], s, low);
+      split<kPlain>(raw.v[u][i / 4][i % 4], raw.v[u][i / 4][i % 4 + 1], s, low);
 #pragma unroll
       for (int p = 0; p < kParts; ++p) part[p][i / 2] = s[p];
     }
@@ -587,6 +609,7 @@ __device__ __forceinline__ void walk_rows(const Rows& a, const Kept<kRounds, kW>
           for (int k = 0; k < 4; ++k) x[r][e][k] = static_cast<float>(next[e][r][k]);
       if (!kLast || i + 1 < kWc) request_beside(i + 1 < kWc ? tile + 1 : first + step);
       if (!served && 16 * tile < rows) again(16 * tile, acc);
+      unscale<Rows::source>(acc, served);
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int64_t row = 16 * tile + r;

@@ -87,11 +87,12 @@ __device__ __forceinline__ void store4(T* __restrict__ p, int c, int cols, const
   }
 }
 
-// Rows of X, dY, S as an operand.  kGated: dY act'(Z), z beside x.
-enum Source { kPlain, kGated };
+// Rows as an operand.  kPlain: a tensor of the caller (X, HX, dY).  kMade: G or S as a tensor of its own.  kGated: dY act'(Z), z beside x.
+enum Source { kPlain, kMade, kGated };
 
 template <typename TA, typename T, Source kSource>
 struct Operand {
+  static constexpr Source source = kSource;
   Matrix<T> x, z;
   Gate<TA> gate;   // kGated
   // raw elements first (so that many requests can be under way), arithmetic later

@@ -136,3 +136,28 @@ def test_a_product_beyond_the_largest_number_is_infinite(lib, rows, k_in, k_out,
         want[column] = float("inf") if value > 0 else -float("inf")
         assert torch.equal(got[row].double(), want)
         assert torch.isfinite(got[:row]).all() and torch.isfinite(got[row + 1:]).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("size", [1.0, 1e15])
+@pytest.mark.parametrize("z", [-40.0, -48.0, -60.0, -74.0, -80.0])
+@pytest.mark.parametrize("rows,k_in,k_out", [(20, 64, 64), (MANY, 64, 64), (MANY, 132, 72), (3000, 512, 256)])
+def test_small_derivatives_are_not_zero(lib, rows, k_in, k_out, z, size, dtype):
+    """SiLU far left: act' and act'' are some z exp(z), 1e-16 to 1e-33, and all that the gradients are made of.  One sign, so each result is relative to
+    itself: 2^-15 for the exponential (|z| u = 5e-6 and a few u), the sums of the parts and 3 sqrt(n) u for a sum over the rows; bfloat16 rows 2^-8."""
+    torch = lib.torch
+    print(f"dense layer, pre-activations of {z}, dY {size}, {rows} {k_in} {k_out} {dtype}", flush=True)
+    layer = Layer(lib, rows, k_in, k_out, "silu", dtype, bias=False, residual=False)
+    for t in (layer.X, layer.W, layer.HX, layer.dY):
+        t.abs_().add_(0.5)
+    layer.dY.mul_(size)
+    Z = layer.wide(1, torch.full((rows, k_out), z, device="cuda"))
+    first, second = np.exp(z) * (1 + z), np.exp(z) * (2 + z)       # (the rest is some exp(2 z))
+    X, W, dY, HX = (t.double() for t in (layer.X, layer.W, layer.dY, layer.HX))
+    G, S = dY * first, torch.matmul(HX, W) * dY * second
+    Wt, Xt, Ht = W.t().contiguous(), X.t().contiguous(), HX.t().contiguous()
+    slack = 2.0 ** -15 + 3 * rows ** 0.5 * 2.0 ** -24
+    for name, got, want in zip(("dX", "dW", "db"), layer.backward(Z), (G @ Wt, Xt @ G, G.sum(0))):
+        assert ((got.double() / want - 1).abs() <= slack + (2.0 ** -8 if name == "dX" and dtype == "bf16" else 0)).all(), name
+    for name, got, want in zip(("ddY", "X2", "W2", "b2"), layer.double_backward(Z), (torch.matmul(HX, W) * first, S @ Wt, Xt @ S + Ht @ G, S.sum(0))):
+        assert ((got.double() / want - 1).abs() <= slack + (2.0 ** -8 if name in ("ddY", "X2") and dtype == "bf16" else 0)).all(), name
