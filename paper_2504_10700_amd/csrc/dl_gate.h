@@ -14,9 +14,17 @@
 
 namespace dl {
 
-// exp(x) and 1 / x for x from 1 to 1e38.  fp32: the hardware's 2^x and reciprocal, each good to a unit or two of the last place; x log2(e) adds
-// |x| units to the exponential, where p or q is exp(-|x|) small.  28 instructions less than the library's pair.
-__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896340736f); }
+// exp(x) and 1 / x for x from 1 to 1e38.  fp32: the hardware's 2^x and reciprocal, each good to a unit or two of the last place.  x log2(e) is rounded to
+// |x| units of the exponential; what the rounding left, and the rest of log2(e) beyond its first 24 bits, is the small t below, and 2^t is 1 + t ln 2 to within
+// t^2.  24 instructions less than the library's pair.
+__device__ __forceinline__ float exp_of(float x) {
+  constexpr double kLog2e = 1.4426950408889634073599246810019;
+  constexpr float kFirst = static_cast<float>(kLog2e), kRest = static_cast<float>(kLog2e - static_cast<double>(kFirst));
+  const float y = x * kFirst;
+  const float t = fmaf(x, kRest, fmaf(x, kFirst, -y));
+  const float e = __builtin_amdgcn_exp2f(y);
+  return fmaf(e, t * 0.693147180559945309417f, e);
+}
 __device__ __forceinline__ double exp_of(double x) { return exp(x); }
 __device__ __forceinline__ float inverse_of(float x) { return __builtin_amdgcn_rcpf(x); }
 __device__ __forceinline__ double inverse_of(double x) { return 1.0 / x; }

@@ -161,3 +161,28 @@ def test_small_derivatives_are_not_zero(lib, rows, k_in, k_out, z, size, dtype):
         assert ((got.double() / want - 1).abs() <= slack + (2.0 ** -8 if name == "dX" and dtype == "bf16" else 0)).all(), name
     for name, got, want in zip(("ddY", "X2", "W2", "b2"), layer.double_backward(Z), (torch.matmul(HX, W) * first, S @ Wt, Xt @ S + Ht @ G, S.sum(0))):
         assert ((got.double() / want - 1).abs() <= slack + (2.0 ** -8 if name in ("ddY", "X2") and dtype == "bf16" else 0)).all(), name
+
+
+@pytest.mark.parametrize("rows,k", [(7000, 1), (7000, 4), (70_000, 20)])
+def test_exponentials_far_out(lib, rows, k):
+    """SiLU in fp32 relative to itself, far left too.  The logistic p = 1 / (1 + e): 3 u of the exponential (the hardware's unit of 2 u, the correction), u of the
+    sum, 2 u of the reciprocal; z p one more: 8 u with the stored z exact.  act' = p + z p q for z <= -3: 8 u of p, 16 u of z p q, which is up to 1.6
+    times the sum there: 40 u, and the sum of k equal terms."""
+    torch, u = lib.torch, 2.0 ** -24
+    print(f"dense layer, exponentials {rows} {k}", flush=True)
+    layer = Layer(lib, rows, k, k, "silu", "f32", bias=False, residual=False)
+    layer.W.zero_()
+    layer.W.fill_diagonal_(1.0)
+    layer.X.copy_(torch.linspace(-86.0, 20.0, rows, device="cuda")[:, None].expand(rows, k))
+    Y, Z = layer.forward()
+    z = host(Z)
+    e = np.exp(-z)
+    want = z / (1 + e)
+    off = np.abs(host(Y) / want - 1)
+    assert off.max() <= 8 * u, f"{off.max() / u:.1f} u at {z.flat[off.argmax()]}"
+    layer.dY.fill_(1.0)
+    left = z[:, 0] <= -3
+    p = 1 / (1 + e[left])
+    want = p + z[left] * p * (1 - p)
+    off = np.abs(host(layer.backward(Z, "X")[0])[left] / want - 1)
+    assert off.max() <= 40 * u, f"{off.max() / u:.1f} u at {z[left].flat[off.argmax()]}"
