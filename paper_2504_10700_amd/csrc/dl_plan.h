@@ -151,14 +151,25 @@ inline Plan parts_plan(const dl_config* c, int64_t n, bool want_dx, bool want_dw
   p.dw_col_groups = static_cast<int>(blocks_of(c->k_out, kCols * p.dw.wc));
   const int64_t groups = blocks_of(c->k_in, kCols) * p.dw_col_groups;
   // Of dW alone as many workgroups as the chip has places for, two a CU (64 x 64 blocks: three) and the same for every XCD: one more would run when
-  // the others are done.  None with less than 256 rows.  (990 001 rows, 64 -> 1280: 65 workgroups on an XCD with 64 places 1640 us, 60 1190.)
-  const int64_t places = wide ? 64 : 96;
-  int64_t chunks = groups <= places ? places / groups * kXcds : kXcds * blocks_of(places, groups);
+  // the others are done.  None with less than 256 rows.  (990 001 rows, 64 -> 1280: 65 workgroups on an XCD with 64 places 1640 us, 60 1190.)  Wider layers
+  // a chunk for every XCD; where one chunk has workgroups for all places, the fewest chunks that leave a quarter of the places idle at most, as every chunk writes a
+  // dW that is read again (2048 rows, 4096 -> 4096 bfloat16, dW 464 us with eight, 135 with one; 8192 rows, 4096 -> 2560, 513 and 404 with two).
+  const int64_t places = wide ? 64 : 96, all = places * kXcds;
+  int64_t chunks = kXcds;
+  if (groups <= places) {
+    chunks = places / groups * kXcds;
+  } else if (groups >= all) {
+    chunks = 1;
+    while (chunks < kXcds && 4 * chunks * groups < 3 * all * blocks_of(chunks * groups, all)) ++chunks;
+  }
   const int rt = parts_tiles(n, c->k_in);
   chunks = std::max<int64_t>(1, std::min<int64_t>(chunks, n / (rt == 1 ? 128 : 256)));
   // With dX beside it no more than 4 MB of dY, so that what the workgroups of the chip read twice at a time stays in the caches: 990 001 rows of
-  // bfloat16, 64 -> 1280, 1325 us with 26 MB, 1120 with 10, 1017 with 4.
-  if (want_dx && want_dw) chunks = std::max(chunks, blocks_of(n * c->k_out * static_cast<int64_t>(row_size(c)), 4 << 20));
+  // bfloat16, 64 -> 1280, 1325 us with 26 MB, 1120 with 10, 1017 with 4.  But no chunk of less than four times as many rows as dW has, or the partial results
+  // would outweigh dY (dX and dW of 16 384 rows, 4096 -> 4096 bfloat16, 3560 us and 2.2 GB of workspace with 32 chunks, 2685 and 0.13 with one; 60 000 rows,
+  // 1280 -> 1280, 1211 with 37, 1109 with 11).
+  if (want_dx && want_dw)
+    chunks = std::max(chunks, std::min(blocks_of(n * c->k_out * static_cast<int64_t>(row_size(c)), 4 << 20), n / (4 * static_cast<int64_t>(c->k_in))));
   const int64_t unit = want_dx ? 16 * rt * kWaves : 32;
   p.per = blocks_of(blocks_of(n, chunks), unit) * unit;
   p.chunks = blocks_of(n, p.per);
@@ -191,12 +202,16 @@ inline size_t wt_bytes(int64_t n, const dl_config* c) {
   return transposed(n, c) ? align_up(static_cast<size_t>(c->k_in) * c->k_out * weight_size(c), 256) : 0;
 }
 
+// Partial results: none where a single chunk writes the outputs themselves.
+inline size_t partial_bytes(const dl_config* c, int64_t n) {
+  const int64_t chunks = in_parts(c, n, c->k_in, c->k_out) ? std::max(parts_plan(c, n, true, true).chunks, parts_plan(c, n, false, true).chunks)
+                                                           : plan_of(c, n, true, true, split_sum(n, c->k_in, c->k_out), 1).chunks;
+  return chunks == 1 ? 0 : static_cast<size_t>(chunks) * (static_cast<int64_t>(c->k_in) * c->k_out + c->k_out) * weight_size(c);
+}
+
 inline size_t workspace_bytes(const dl_config* c, int64_t n) {
   if (n == 0) return 256;
-  int64_t chunks = std::max(parts_plan(c, n, true, true).chunks, parts_plan(c, n, false, true).chunks);
-  for (bool split : {false, true}) chunks = std::max(chunks, plan_of(c, n, true, true, split, 1).chunks);
-  return (curved(c) && g_first(c, n) ? 2 : 1) * s_bytes(c, n) + wt_bytes(n, c) + align_up(static_cast<size_t>(chunks) * plan_of(c, n, true, true, false, 1).stride * weight_size(c), 256) +
-         256;
+  return (curved(c) && g_first(c, n) ? 2 : 1) * s_bytes(c, n) + wt_bytes(n, c) + align_up(partial_bytes(c, n), 256) + 256;
 }
 
 

@@ -5,6 +5,7 @@ Tolerances stand with each test; u = 2^-24.
 import numpy as np
 import pytest
 
+import test_gpu_dense_layer as base
 from oracle import dense_layer as od
 from test_gpu_dense_layer import MANY, Layer, host, lib  # noqa: F401  (lib: the fixture)
 
@@ -186,3 +187,11 @@ def test_exponentials_far_out(lib, rows, k):
     want = p + z[left] * p * (1 - p)
     off = np.abs(host(layer.backward(Z, "X")[0])[left] / want - 1)
     assert off.max() <= 40 * u, f"{off.max() / u:.1f} u at {z[left].flat[off.argmax()]}"
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(2500, 4096, 2304), (2048, 2560, 4096), (20_000, 1280, 1280), (6000, 1280, 1280), (700, 24_576, 128), (1500, 2048, 2560)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_wide_layers_in_few_chunks(lib, shape, dtype):
+    """Small integers: every sum exact, whatever the number of chunks."""
+    base.test_small_integers_are_exact(lib, shape, dtype)

@@ -105,3 +105,17 @@ def test_clipping_refusals():
     for src, dst in (([x.half()], None), ([x.t()[1:]], None), ([x], [x.double()]), ([x], [x[:2]]), ([x], [])):
         with pytest.raises(ValueError):
             gc.make_tensors(src, dst)
+
+
+@pytest.mark.parametrize("dtype", [dl.SC_F32, dl.SC_F64, dl.SC_BF16])
+def test_dense_layer_workspace_of_wide_layers(dtype):
+    """Without an activation: W transposed and partial results, which stay a small part of dY, or below three times W where that is large, or below 270 MB."""
+    row, weight = {dl.SC_F32: 4, dl.SC_F64: 8, dl.SC_BF16: 2}[dtype], 8 if dtype == dl.SC_F64 else 4
+    for rows in (1, 100, 2500, 8192, 24_414, 65_536, 1_000_000):
+        for k_in, k_out in ((64, 64), (64, 1280), (1280, 64), (1280, 1280), (2048, 2048), (2560, 2560), (4096, 2304), (4096, 4096), (16_384, 16_384),
+                            (dl.DL_MAX_WIDTH, 128), (dl.DL_MAX_WIDTH, dl.DL_MAX_WIDTH), (1279, 4097)):
+            n, w = dl.dl_workspace_bytes(dl.make_config(k_in, k_out, dl.DL_NONE, dtype), rows), k_in * k_out * weight
+            assert n - w <= max(rows * k_out * weight / 4, 3 * w if k_in * k_out > 8 << 20 else 0, 270e6) * 1.01 + 1024, (rows, k_in, k_out)
+    # one chunk needs no partial results
+    assert dl.dl_workspace_bytes(dl.make_config(4096, 4096, dl.DL_NONE, dl.SC_F64), 20_000) <= 4096 * 4096 * 8 + 1024
+    assert dl.dl_workspace_bytes(dl.make_config(dl.DL_MAX_WIDTH, dl.DL_MAX_WIDTH, dl.DL_NONE, dl.SC_F32), 8192) <= dl.DL_MAX_WIDTH ** 2 * 4 + 1024
