@@ -283,8 +283,8 @@ __device__ __forceinline__ void dw_role(const Plan& p, int64_t chunk, int i, int
     outer_product<TA, kFours>(x, b, m0, k_in, n0, k_out, from, to, acc, sum);
     if constexpr (kTwo) outer_product<TA, kFours>(x2, b2, m0, k_in, n0, k_out, from, to, acc, none);
   }
-  TA* const to_dw = dW ? dW + chunk * p.stride : nullptr;
-  TA* const to_db = db && m0 == 0 ? db + chunk * p.stride : nullptr;
+  TA* const to_dw = dW ? dW + chunk * p.stride() : nullptr;
+  TA* const to_db = db && m0 == 0 ? db + chunk * p.stride() : nullptr;
   // column sums: over the four q of the wave, then over the waves
 #pragma unroll
   for (int u = 0; u < 4; ++u) {
@@ -426,7 +426,7 @@ __device__ __forceinline__ void parts_dw_role(const Plan& p, int64_t chunk, int 
   unscale<B::source>(acc, done);
   const int n = n0 + 4 * j;
   if (dW && n < k_out) {
-    float* const to_dw = dW + chunk * p.stride;
+    float* const to_dw = dW + chunk * p.stride();
 #pragma unroll
     for (int t = 0; t < kT; ++t)
 #pragma unroll
@@ -437,7 +437,7 @@ __device__ __forceinline__ void parts_dw_role(const Plan& p, int64_t chunk, int 
       }
   }
   if (db && m0 == 0) {   // column sums: over the four q of a wave, then over the waves that shared the rows
-    float* const to_db = db + chunk * p.stride;
+    float* const to_db = db + chunk * p.stride();
     float* const joined = reinterpret_cast<float*>(lds);
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
@@ -541,11 +541,8 @@ __global__ __launch_bounds__(kThreads) void sum_chunks_kernel(const TA* __restri
       TA v = 0;
       for (int k = 0; k < kGroups; ++k) v += lds[k][threadIdx.x];
       const int64_t at = i0 + threadIdx.x;
-      if (at < n_dw) {
-        if (dW) dW[at] = v;
-      } else if (db) {
-        db[at - n_dw] = v;
-      }
+      if (at < n_dw) dW[at] = v;
+      else db[at - n_dw] = v;
     }
   }
 }
@@ -747,17 +744,17 @@ struct Calls {
     TA* part = reinterpret_cast<TA*>(static_cast<char*>(ws) + wt_bytes(n, c));
     const bool whole = p.chunks == 1;
     return {!dW ? nullptr : whole ? static_cast<TA*>(dW) : part,
-            !db ? nullptr : whole ? static_cast<TA*>(db) : part + static_cast<int64_t>(c->k_in) * c->k_out, part};
+            !db ? nullptr : whole ? static_cast<TA*>(db) : part + p.n_dw, part};
   }
   hipError_t join(const Plan& p, const Target& to, void* dW, void* db) const {
     const hipError_t e = hipGetLastError();
-    return e != hipSuccess || p.chunks == 1 || !(dW || db) ? e : sum_chunks(to.part, p.chunks, dW, db);
+    return e != hipSuccess || p.chunks == 1 || !(dW || db) ? e : sum_chunks(to.part, p.chunks, p.n_dw, dW, p.n_db, db);
   }
 
   template <bool kTwo, typename RT, typename Split, typename Fours, typename G, typename Weights, typename B, typename B2>
   hipError_t gradients_with(RT rt, Split split, Fours, const G& source, const Weights& w, void* dX, const void* X, const B& b, const void* X2,
                             const B2& b2, void* dW, void* db, void* ws) const {
-    const Plan p = plan_of(c, n, dX != nullptr, dW || db, split, rt);
+    const Plan p = plan_of(c, n, Wanted{dX != nullptr, dW != nullptr, db != nullptr}, split, rt);
     const Target to = target(p, dW, db, ws);
     hipLaunchKernelGGL((backward_kernel<TS, TA, RT::value, Split::value, Fours::value, kTwo, G, B, B2, Weights>), dim3(grid_of(p.deal().count())),
                        dim3((threads<Split::value, TA>())), 0, stream, p, c->k_in, c->k_out, ld_in(c), source, w, static_cast<TS*>(dX), rows_in(X), b,
@@ -768,7 +765,7 @@ struct Calls {
   // kRT: row tiles of a wave of dX
   template <int kRT, bool kWide, bool kDx, bool kTwo, typename G, typename B, typename B2>
   hipError_t parts_gradients(const G& source, void* dX, const void* X, const B& b, const void* X2, const B2& b2, void* dW, void* db, void* ws) const {
-    const Plan p = parts_plan(c, n, dX != nullptr, dW || db);
+    const Plan p = parts_plan(c, n, Wanted{dX != nullptr, dW != nullptr, db != nullptr});
     const Target to = target(p, dW, db, ws);
     hipLaunchKernelGGL((parts_backward_kernel<TS, kRT, kWide, kDx, kTwo, G, B, B2>), dim3(grid_of(p.deal().count())), dim3(kThreads), 0, stream, p, c->k_in, c->k_out,
                        ld_in(c), source, (AlongRows<float>{static_cast<const float*>(ws), c->k_out, c->k_in}), static_cast<TS*>(dX), rows_in(X), b,
@@ -776,12 +773,15 @@ struct Calls {
     return join(p, to, dW, db);
   }
 
-  hipError_t sum_chunks(const TA* part, int64_t chunks, void* dW, void* db) const {
-    const int64_t n_dw = static_cast<int64_t>(c->k_in) * c->k_out;
-    hipLaunchKernelGGL((sum_chunks_kernel<TA>), dim3(static_cast<unsigned>(std::min<int64_t>(blocks_of(n_dw + c->k_out, 64), 1 << 16))),
-                       dim3(kThreads), 0, stream, part, chunks, n_dw + c->k_out, n_dw, static_cast<int64_t>(c->k_out),
-                       static_cast<TA*>(dW), static_cast<TA*>(db));
+  // n_dw, n_db: what a chunk holds of each
+  hipError_t sum_chunks(const TA* part, int64_t chunks, int64_t n_dw, void* dW, int64_t n_db, void* db) const {
+    hipLaunchKernelGGL((sum_chunks_kernel<TA>), dim3(static_cast<unsigned>(std::min<int64_t>(blocks_of(n_dw + n_db, 64), 1 << 16))), dim3(kThreads), 0,
+                       stream, part, chunks, n_dw + n_db, n_dw, n_db, static_cast<TA*>(dW), static_cast<TA*>(db));
     return hipGetLastError();
+  }
+  hipError_t zero(void* dW, void* db) const {
+    if (!dW && !db) return hipSuccess;
+    return sum_chunks(nullptr, 0, dW ? static_cast<int64_t>(c->k_in) * c->k_out : 0, dW, db ? c->k_out : 0, db);
   }
 
   hipError_t backward(const void* X, const void* W, const void* Z, const void* dY, void* dX, void* dW, void* db, void* ws) const {
@@ -823,7 +823,7 @@ struct Calls {
     if (e != hipSuccess) return e;
     if (!S) {   // act'' = 0: W2 is dW of HX, X2 and b2 are zero
       e = zero_rows(X2, c->k_in, ld_in(c));
-      if (e == hipSuccess && b2) e = sum_chunks(nullptr, 0, nullptr, b2);
+      if (e == hipSuccess) e = zero(nullptr, b2);
       if (e != hipSuccess || !W2) return e;
       if (c->activation == DL_NONE)
         return gradients<false>(g<kPlain>(dY, Z), W, nullptr, HX, g<kPlain>(dY, Z), HX, g<kPlain>(dY, Z), W2, nullptr, part);
@@ -852,7 +852,7 @@ struct EntryOf {
     return C{c, n, stream}.double_backward(X, W, Z, dY, HX, ddY, X2, W2, b2, ws);
   }
   static hipError_t zero(const dl_config* c, hipStream_t stream, void* dW, void* db) {
-    return dW || db ? C{c, 0, stream}.sum_chunks(nullptr, 0, dW, db) : hipSuccess;
+    return C{c, 0, stream}.zero(dW, db);
   }
 };
 

@@ -57,6 +57,11 @@ struct Walk {
 
 constexpr int kPartsTiles = 4;   // row tiles of a wave, where there are rows enough (parts_tiles)
 
+// Which results a call wants.
+struct Wanted {
+  bool dx, dw, db;
+};
+
 // What a launch of the backward does: the rows in chunks, of each chunk first dx_groups workgroups of dX, then dw_groups of the chunk's partial dW and
 // db.  A chunk stays on one XCD and its two halves run at about the same time: the second reading of dY (and Z) comes from the caches.
 struct Plan {
@@ -65,7 +70,8 @@ struct Plan {
   int64_t dx_groups, dw_groups;   // workgroups of a chunk
   int dx_col_groups, dw_col_groups;
   Shape dx, dw;
-  int64_t stride;       // elements between the chunks' partial results
+  int64_t n_dw, n_db;   // elements of dW and of db that a chunk's partial results hold, dW first: 0 for one that is not wanted
+  __host__ __device__ int64_t stride() const { return n_dw + n_db; }
   __host__ __device__ Deal deal() const { return {chunks, dx_groups + dw_groups}; }
 };
 
@@ -96,25 +102,34 @@ inline int row_tiles(int64_t rows, int cols, int most) {
 // 200 rows, 256 -> 64 fp32 15.2 -> 7.7 us, 100 rows, 1024 -> 1024 44 -> 13.5; 10 000 rows, 128 -> 16 fp64 16.7 -> 14.6).
 inline bool split_sum(int64_t rows, int cols, int k) { return k >= 128 && blocks_of(rows, 16) * blocks_of(cols, kCols) <= 1024; }
 
-inline Plan plan_of(const dl_config* c, int64_t n, bool want_dx, bool want_dw, bool split, int rt) {
+inline void set_partials(const dl_config* c, const Wanted& want, Plan* p) {
+  p->n_dw = want.dw ? static_cast<int64_t>(c->k_in) * c->k_out : 0;
+  p->n_db = want.db ? c->k_out : 0;
+}
+// db without dW takes the blocks of the first 64 rows of dW only, in more chunks: as many as find room where the partial dW of this plan would be.
+inline int64_t room_for_db(const dl_config* c, const Plan& with_dw) { return with_dw.chunks > 1 ? with_dw.chunks * (c->k_in + 1) : 1; }
+
+inline Plan plan_of(const dl_config* c, int64_t n, const Wanted& want, bool split, int rt) {
   const int split_waves = c->dtype == SC_F64 ? dl::split_waves<double>() : dl::split_waves<float>();
   Plan p{};
   p.rows = n;
   p.dw = shape_of(c->k_out);
   if (split) p.dw = {1, split_waves};
-  const int64_t blocks = blocks_of(c->k_in, kCols) * blocks_of(c->k_out, kCols);
+  const bool only_db = want.db && !want.dw;
+  const int64_t dw_rows = only_db ? 1 : blocks_of(c->k_in, kCols), blocks = dw_rows * blocks_of(c->k_out, kCols);
   constexpr int kMinShare = 16;
   // about 2048 waves of dW, none with less than 16 rows (1000 rows, 256 -> 256 in fp32: dW 21 us so, 28 with 32; 10 000, 128 -> 16 in fp64: 22, 25)
-  const int64_t chunks = std::max<int64_t>(1, std::min(2048 / (blocks * p.dw.wr), n / (kMinShare * p.dw.wr)));
+  int64_t chunks = std::max<int64_t>(1, std::min(2048 / (blocks * p.dw.wr), n / (kMinShare * p.dw.wr)));
+  if (only_db) chunks = std::min(chunks, room_for_db(c, plan_of(c, n, {want.dx, true, true}, split, rt)));
   p.per = blocks_of(n, chunks);
   p.per = blocks_of(p.per, p.per < 256 ? 64 : 256) * (p.per < 256 ? 64 : 256);
   p.chunks = blocks_of(n, p.per);
   p.dx = split ? Shape{1, 1} : shape_of(c->k_in);
   p.dx_col_groups = static_cast<int>(blocks_of(c->k_in, kCols * p.dx.wc));
-  p.dx_groups = want_dx ? blocks_of(p.per, split ? 16 : 16 * rt * p.dx.wr) * p.dx_col_groups : 0;
+  p.dx_groups = want.dx ? blocks_of(p.per, split ? 16 : 16 * rt * p.dx.wr) * p.dx_col_groups : 0;
   p.dw_col_groups = static_cast<int>(blocks_of(c->k_out, kCols * p.dw.wc));
-  p.dw_groups = want_dw ? blocks_of(c->k_in, kCols) * p.dw_col_groups : 0;
-  p.stride = static_cast<int64_t>(c->k_in) * c->k_out + c->k_out;
+  p.dw_groups = want.dw || want.db ? dw_rows * p.dw_col_groups : 0;
+  set_partials(c, want, &p);
   return p;
 }
 
@@ -143,13 +158,14 @@ inline bool kept_ok(const dl_config* c, int64_t n, int cols, int k) { return k <
 // Is a wave's share of dW 64 x 64 (parts_dw_role)?
 inline bool wide_parts(const dl_config* c) { return c->k_out > 2 * kCols; }
 
-inline Plan parts_plan(const dl_config* c, int64_t n, bool want_dx, bool want_dw) {
+inline Plan parts_plan(const dl_config* c, int64_t n, const Wanted& want) {
   Plan p{};
   p.rows = n;
   const bool wide = wide_parts(c);
   p.dw = {wide ? kWaves : 1, 1};
   p.dw_col_groups = static_cast<int>(blocks_of(c->k_out, kCols * p.dw.wc));
-  const int64_t groups = blocks_of(c->k_in, kCols) * p.dw_col_groups;
+  const bool only_db = want.db && !want.dw;
+  const int64_t groups = (only_db ? 1 : blocks_of(c->k_in, kCols)) * p.dw_col_groups;
   // Of dW alone as many workgroups as the chip has places for, two a CU (64 x 64 blocks: three) and the same for every XCD: one more would run when
   // the others are done.  None with less than 256 rows.  (990 001 rows, 64 -> 1280: 65 workgroups on an XCD with 64 places 1640 us, 60 1190.)  Wider layers
   // a chunk for every XCD; where one chunk has workgroups for all places, the fewest chunks that leave a quarter of the places idle at most, as every chunk writes a
@@ -168,16 +184,17 @@ inline Plan parts_plan(const dl_config* c, int64_t n, bool want_dx, bool want_dw
   // bfloat16, 64 -> 1280, 1325 us with 26 MB, 1120 with 10, 1017 with 4.  But no chunk of less than four times as many rows as dW has, or the partial results
   // would outweigh dY (dX and dW of 16 384 rows, 4096 -> 4096 bfloat16, 3560 us and 2.2 GB of workspace with 32 chunks, 2685 and 0.13 with one; 60 000 rows,
   // 1280 -> 1280, 1211 with 37, 1109 with 11).
-  if (want_dx && want_dw)
+  if (want.dx && want.dw)
     chunks = std::max(chunks, std::min(blocks_of(n * c->k_out * static_cast<int64_t>(row_size(c)), 4 << 20), n / (4 * static_cast<int64_t>(c->k_in))));
-  const int64_t unit = want_dx ? 16 * rt * kWaves : 32;
+  if (only_db) chunks = std::min(chunks, room_for_db(c, parts_plan(c, n, {want.dx, true, true})));
+  const int64_t unit = want.dx ? 16 * rt * kWaves : 32;
   p.per = blocks_of(blocks_of(n, chunks), unit) * unit;
   p.chunks = blocks_of(n, p.per);
   p.dx = {1, kWaves};
   p.dx_col_groups = static_cast<int>(blocks_of(c->k_in, kCols));
-  p.dx_groups = want_dx ? blocks_of(p.per, 16 * rt * kWaves) * p.dx_col_groups : 0;
-  p.dw_groups = want_dw ? groups : 0;
-  p.stride = static_cast<int64_t>(c->k_in) * c->k_out + c->k_out;
+  p.dx_groups = want.dx ? blocks_of(p.per, 16 * rt * kWaves) * p.dx_col_groups : 0;
+  p.dw_groups = want.dw || want.db ? groups : 0;
+  set_partials(c, want, &p);
   return p;
 }
 
@@ -204,9 +221,13 @@ inline size_t wt_bytes(int64_t n, const dl_config* c) {
 
 // Partial results: none where a single chunk writes the outputs themselves.
 inline size_t partial_bytes(const dl_config* c, int64_t n) {
-  const int64_t chunks = in_parts(c, n, c->k_in, c->k_out) ? std::max(parts_plan(c, n, true, true).chunks, parts_plan(c, n, false, true).chunks)
-                                                           : plan_of(c, n, true, true, split_sum(n, c->k_in, c->k_out), 1).chunks;
-  return chunks == 1 ? 0 : static_cast<size_t>(chunks) * (static_cast<int64_t>(c->k_in) * c->k_out + c->k_out) * weight_size(c);
+  int64_t most = 0;
+  for (bool dx : {false, true}) {
+    const Wanted want{dx, true, true};
+    const Plan p = in_parts(c, n, c->k_in, c->k_out) ? parts_plan(c, n, want) : plan_of(c, n, want, split_sum(n, c->k_in, c->k_out), 1);
+    if (p.chunks > 1) most = std::max(most, p.chunks * p.stride());
+  }
+  return static_cast<size_t>(most) * weight_size(c);
 }
 
 inline size_t workspace_bytes(const dl_config* c, int64_t n) {
@@ -215,7 +236,7 @@ inline size_t workspace_bytes(const dl_config* c, int64_t n) {
 }
 
 
-// The calls of one type (dl_calls.h).  c and the tensors have been checked; sum_chunks without chunks writes zeros.
+// The calls of one type (dl_calls.h).  c and the tensors have been checked.
 struct Entries {
   hipError_t (*forward)(const dl_config* c, int64_t n, hipStream_t stream, const void* X, const void* W, const void* b, const void* residual, void* Y,
                         void* Z);

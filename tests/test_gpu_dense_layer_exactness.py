@@ -195,3 +195,53 @@ def test_exponentials_far_out(lib, rows, k):
 def test_wide_layers_in_few_chunks(lib, shape, dtype):
     """Small integers: every sum exact, whatever the number of chunks."""
     base.test_small_integers_are_exact(lib, shape, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f64", "bf16"])
+@pytest.mark.parametrize("rows,k_in,k_out", [(1, 8, 8), (777, 256, 48), (3000, 65, 67), (20_000, 128, 16), (MANY, 64, 64), (20_000, 1280, 1280), (2500, 2560, 4096),
+                                             (8003, 1024, 72)])
+def test_column_sums_by_themselves(lib, rows, k_in, k_out, dtype):
+    """db and b2 without dW and W2: small integers, exact; with and without dX; the workspace holds NaN."""
+    torch = lib.torch
+    print(f"dense layer, db alone {rows} {k_in} {k_out} {dtype}", flush=True)
+    for act in ("none", "relu"):
+        layer = Layer(lib, rows, k_in, k_out, act, dtype)
+        layer.dY.copy_(layer.dY.clamp(-3, 3).round())
+        Z = layer.wide(1, layer.R)
+        want = (layer.dY.double() * (Z.double() > 0 if act == "relu" else 1)).sum(0)
+        for wanted in ("b", "Xb"):
+            layer.ws.fill_(255)
+            assert torch.equal(layer.backward(Z, wanted)[2].double(), want)
+    layer = Layer(lib, rows, k_in, k_out, "silu", dtype)
+    Z = layer.wide(1, layer.R)
+    whole = layer.double_backward(Z)[3].double()
+    for wanted in ("b", "Xb"):
+        layer.ws.fill_(255)
+        got = layer.double_backward(Z, wanted)[3].double()
+        # |S| is below 8 for some 64 terms of unit size in V; sums of n in two orders differ by sqrt(n) units of it
+        assert (got - whole).abs().max() <= 64 * rows ** 0.5 * (2.0 ** -52 if dtype == "f64" else 2.0 ** -23) + 1e-30
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,k_in,k_out", [(66_001, 1024, 64), (20_000, 1280, 1280)])
+def test_column_sums_do_not_cost_a_whole_dw(lib, rows, k_in, k_out, dtype):
+    """Their operands are a sixteenth of those of dW (or the products a twentieth): below half of its time with room for noise."""
+    torch = lib.torch
+    print(f"dense layer, time of db alone {rows} {k_in} {k_out} {dtype}", flush=True)
+    layer = Layer(lib, rows, k_in, k_out, "none", dtype)
+
+    def microseconds(want):
+        times = []
+        for _ in range(25):
+            start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            start.record()
+            for _ in range(4):
+                lib.dl.dl_backward(layer.cfg, rows, layer.X, layer.W, None, layer.dY, None, dW if "W" in want else None, db, layer.ws, layer.nbytes)
+            end.record()
+            torch.cuda.synchronize()
+            times.append(start.elapsed_time(end) * 250)
+        return sorted(times)[12]
+    dW, db = layer.weights(layer.W), layer.weights(layer.b)
+    both, alone = microseconds("Wb"), microseconds("b")
+    print(f"dW and db {both:.1f} us, db {alone:.1f} us", flush=True)
+    assert alone < 0.5 * both
