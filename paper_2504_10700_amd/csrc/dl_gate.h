@@ -7,7 +7,7 @@
 //   second  2 p q u' + z (p q (q - p) u'^2 + p q u'')
 // ReLU is the same with p = (z > 0) and p q = 0, so one straight line of code serves all three.  The polynomial is evaluated at z cut to +-kCut
 // (its cube would overflow for large z and 0 * infinity follow), and u from kLow on, where p would be the smallest number of the type and is taken
-// as 0: e stays finite, and a large z finds a true zero.
+// as 0: e stays finite, and a large z finds a true zero; exp(-kCut) is below every number of the type, and a large positive z finds one too.
 #pragma once
 #include "sc_internal.h"
 #include "../../include/dl.h"
@@ -44,7 +44,7 @@ struct Gate {
   };
 
   __device__ __forceinline__ Point at(T z) const {
-    constexpr T kCut = T(700), kLow = sizeof(T) == 8 ? T(-700) : T(-87);
+    constexpr T kCut = T(800), kLow = sizeof(T) == 8 ? T(-700) : T(-87);
     const T w = z > kCut ? kCut : z < -kCut ? -kCut : z;
     const T square = w * w;
     T u = w * (c1 + c3 * square);

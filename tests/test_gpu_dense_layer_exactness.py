@@ -245,3 +245,19 @@ def test_column_sums_do_not_cost_a_whole_dw(lib, rows, k_in, k_out, dtype):
     both, alone = microseconds("Wb"), microseconds("b")
     print(f"dW and db {both:.1f} us, db {alone:.1f} us", flush=True)
     assert alone < 0.5 * both
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+def test_the_largest_preactivations_in_fp64(lib, act):
+    """act' is 1 or 0 and act'' 0 to the last bit from some 800 on, up to the largest numbers."""
+    torch = lib.torch
+    z = torch.tensor([s * x for x in (800.0, 1e5, 1e100, 1e289, 1e300, 1e308) for s in (1, -1)], device="cuda", dtype=torch.float64)[:, None]
+    layer = Layer(lib, len(z), 1, 1, act, "f64", bias=False, residual=False)
+    for t in (layer.W, layer.dY, layer.HX):
+        t.fill_(1.0)
+    layer.X.copy_(z)
+    Y, Z = layer.forward()
+    on = (z > 0).double()
+    assert torch.equal(Z, z) and torch.equal(Y, z.clamp(min=0)) and torch.equal(layer.backward(Z)[0], on)
+    ddY, X2, W2, _ = layer.double_backward(Z)
+    assert torch.equal(ddY, on) and not X2.any()
