@@ -254,18 +254,14 @@ struct Row {
   }
 };
 
-// A wave: one piece of the sorted order, 64 V channels.  first / last: sorted positions of an element's first and last row.
+// One piece of the sorted order, 64 V channels, by a wave.  first / last: sorted positions of an element's first and last row.
 template <typename TS, typename TA, int V>
-__global__ __launch_bounds__(kThreads) void piece_kernel(int64_t n, int64_t pieces, int col_blocks, int channels, int elements, TA scale,
-                                                         const int* __restrict__ keys, const int* __restrict__ order,
-                                                         const TS* __restrict__ dY, TA* __restrict__ dT, TA* __restrict__ slots,
-                                                         int* __restrict__ first, int* __restrict__ last) {
+__device__ __forceinline__ void sum_piece(int64_t piece, int col_block, int64_t n, int channels, int elements, TA scale, const int* __restrict__ keys,
+                                          const int* __restrict__ order, const TS* __restrict__ dY, TA* __restrict__ dT, TA* __restrict__ slots,
+                                          int* __restrict__ first, int* __restrict__ last) {
   typedef Row<TS, TA, V> R;
   const int lane = threadIdx.x & (kLanes - 1);
-  const int64_t task = blockIdx.x * static_cast<int64_t>(kWaves) + __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
-  if (task >= pieces * col_blocks) return;
-  const int64_t piece = task / col_blocks;
-  const int c = (static_cast<int>(task % col_blocks) * kLanes + lane) * V;
+  const int c = (col_block * kLanes + lane) * V;
   const bool live = c < channels;
   const int64_t p0 = piece * kPiece;
   const int count = static_cast<int>(min(static_cast<int64_t>(kPiece), n - p0));
@@ -315,6 +311,16 @@ __global__ __launch_bounds__(kThreads) void piece_kernel(int64_t n, int64_t piec
       }
     }
   }
+}
+
+template <typename TS, typename TA, int V>
+__global__ __launch_bounds__(kThreads) void piece_kernel(int64_t n, int64_t pieces, int col_blocks, int channels, int elements, TA scale,
+                                                         const int* __restrict__ keys, const int* __restrict__ order,
+                                                         const TS* __restrict__ dY, TA* __restrict__ dT, TA* __restrict__ slots,
+                                                         int* __restrict__ first, int* __restrict__ last) {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
+  for (int64_t task = blockIdx.x * static_cast<int64_t>(kWaves) + wave; task < pieces * col_blocks; task += gridDim.x * static_cast<int64_t>(kWaves))
+    sum_piece<TS, TA, V>(task / col_blocks, static_cast<int>(task % col_blocks), n, channels, elements, scale, keys, order, dY, dT, slots, first, last);
 }
 
 // Rows of dT whose rows span pieces, and those of absent elements.  A workgroup has `own` elements: kWaves of a long table, each a wave's, or
@@ -389,21 +395,22 @@ template <typename TS, typename TA, int V>
 __global__ __launch_bounds__(kThreads) void search_kernel(int n, int col_blocks, int channels, int elements, TA scale,
                                                           const int* __restrict__ z, const TS* __restrict__ dY, TA* __restrict__ dT) {
   typedef Row<TS, TA, V> R;
-  const int lane = threadIdx.x & (kLanes - 1);
-  const int64_t task = blockIdx.x * static_cast<int64_t>(kWaves) + __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
-  if (task >= static_cast<int64_t>(elements) * col_blocks) return;
-  const int element = static_cast<int>(task / col_blocks);
-  const int c = (static_cast<int>(task % col_blocks) * kLanes + lane) * V;
-  TA acc[V] = {};
-  for (int i = 0; i < n; i += kLanes) {
-    unsigned long long hits = __ballot(i + lane < n && z[min(i + lane, n - 1)] == element);
-    while (hits) {
-      const int r = i + __builtin_ctzll(hits);
-      hits &= hits - 1;
-      if (c < channels) R::add(acc, *reinterpret_cast<const typename R::VS*>(dY + static_cast<int64_t>(r) * channels + c));
+  const int lane = threadIdx.x & (kLanes - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
+  for (int64_t task = blockIdx.x * static_cast<int64_t>(kWaves) + wave; task < static_cast<int64_t>(elements) * col_blocks;
+       task += gridDim.x * static_cast<int64_t>(kWaves)) {
+    const int element = static_cast<int>(task / col_blocks);
+    const int c = (static_cast<int>(task % col_blocks) * kLanes + lane) * V;
+    TA acc[V] = {};
+    for (int i = 0; i < n; i += kLanes) {
+      unsigned long long hits = __ballot(i + lane < n && z[min(i + lane, n - 1)] == element);
+      while (hits) {
+        const int r = i + __builtin_ctzll(hits);
+        hits &= hits - 1;
+        if (c < channels) R::add(acc, *reinterpret_cast<const typename R::VS*>(dY + static_cast<int64_t>(r) * channels + c));
+      }
     }
+    if (c < channels) R::store(dT + static_cast<int64_t>(element) * channels + c, acc, scale);
   }
-  if (c < channels) R::store(dT + static_cast<int64_t>(element) * channels + c, acc, scale);
 }
 
 // ---- host side
@@ -469,7 +476,8 @@ Workspace carve(const ee_config* c, int64_t n, void* base) {
   return w;
 }
 
-unsigned blocks_of(int64_t waves) { return static_cast<unsigned>((waves + kWaves - 1) / kWaves); }
+// Workgroups for so many waves' tasks.  A launch has fewer than 2^32 threads: beyond 2^22 workgroups a wave takes several tasks.
+unsigned blocks_of(int64_t waves) { return static_cast<unsigned>(std::min<int64_t>((waves + kWaves - 1) / kWaves, 1 << 22)); }
 
 template <typename TS, typename TA>
 struct Calls {

@@ -215,3 +215,23 @@ def test_sums_of_small_integers_are_exact(ee, n, elements, channels, dtype):
 def test_few_rows_of_long_tables(ee, n, elements, channels, dtype):
     print(f"embedding {n} {elements} {channels} {dtype}", flush=True)
     check(ee, n, elements, channels, dtype, "outside")
+
+
+@pytest.mark.parametrize("elements,channels", [(1_000_000, 4301), (999_999, 1025)])
+def test_tables_of_more_waves_than_a_launch_has(ee, elements, channels):
+    """Three rows of a table of 4.3 (1.0) thousand million numbers: 68 (17) million waves' worth of dT, every element of it written."""
+    import torch
+    print(f"embedding 3 {elements} {channels}", flush=True)
+    cfg = ee.make_config(elements, channels, 2.0)
+    z = torch.tensor([elements - 1, 7, elements - 1], device="cuda", dtype=torch.int32)
+    dY = torch.arange(3 * channels, device="cuda", dtype=torch.float32).view(3, channels)
+    dT = torch.full((elements, channels), float("nan"), device="cuda")
+    nbytes = ee.ee_workspace_bytes(cfg, 3)
+    ee.ee_backward(cfg, 3, z, dY, dT, torch.empty(nbytes, dtype=torch.uint8, device="cuda"), nbytes)
+    assert torch.equal(dT[-1], 2 * (dY[0] + dY[2])) and torch.equal(dT[7], 2 * dY[1])
+    dT[-1], dT[7] = 0, 0
+    assert all(not part.any() for part in dT.split(50_000))
+    Y = torch.empty_like(dY)
+    dT[7] = dY[1]
+    ee.ee_forward(cfg, 3, z, dT, Y)
+    assert not Y[0].any() and torch.equal(Y[1], 2 * dY[1])
