@@ -10,7 +10,7 @@
 //      channels.  A run inside one piece is a finished row of dT; one that goes on beyond it leaves its sum in a slot of the
 //      piece (slot 0: the run came in from the piece before; slot 1: it starts here and goes on);
 //   3. for each element the slots of its pieces are added in order, or its row is zeroed if it is absent.
-// Small batches instead look through all indices for each element: one launch.
+// Small batches instead look through all indices for each element: one launch.  (Rules and times at search_few_kernel and searched.)
 //
 // Measured: 200 000 rows of 128 fp32 channels, 89 elements: forward 18.5 us (5.6 TB/s), count 3.5, scatter 9.2, pieces 30 (3.4 TB/s of dY), join 9.8; 32 768 rows of 512
 // bfloat16 channels, 50 000 elements: forward 16 us, two sort passes 22, pieces 17, join (102 MB of dT, most of it zeros) 25.  61 rows: 2.4 and 3 us.
@@ -390,26 +390,117 @@ __global__ __launch_bounds__(kW * kLanes) void join_kernel(int own, int channels
   }
 }
 
-// Small batches: a wave per (element, 64 V channels) looks through all indices and adds its rows in order.
+// Adds the rows list[from], .. list[to - 1], not none, in order, a batch of kAhead requested while the one before is added.
 template <typename TS, typename TA, int V>
-__global__ __launch_bounds__(kThreads) void search_kernel(int n, int col_blocks, int channels, int elements, TA scale,
+__device__ __forceinline__ void add_rows(const unsigned short* list, int from, int to, const TS* __restrict__ dY, int channels, int c, TA (&acc)[V]) {
+  typedef Row<TS, TA, V> R;
+  typename R::VS next[kAhead];
+  auto request = [&](int i) {
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+      next[k] = *reinterpret_cast<const typename R::VS*>(dY + static_cast<int64_t>(list[min(i + k, to - 1)]) * channels + c);
+  };
+  request(from);
+  for (int i = from; i < to; i += kAhead) {
+    typename R::VS v[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) v[k] = next[k];
+    if (i + kAhead < to) request(i + kAhead);
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+      if (i + k < to) R::add(acc, v[k]);
+  }
+}
+
+// Small batches, by search: a wave looks through all indices for the rows of its element.  A workgroup has kWaves elements.
+//
+// Up to kFewRows rows: the wave adds what it finds among 64 indices, kAhead at a time.  (One at a time 0.14 us a row, 19 us for 128 rows of one element; so 10.)
+constexpr int kFewRows = 128;
+
+template <typename TS, typename TA, int V>
+__global__ __launch_bounds__(kThreads) void search_few_kernel(int n, int channels, int elements, TA scale, const int* __restrict__ z,
+                                                              const TS* __restrict__ dY, TA* __restrict__ dT) {
+  typedef Row<TS, TA, V> R;
+  const int lane = threadIdx.x & (kLanes - 1), element = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
+  if (element >= elements) return;
+  const int c = (blockIdx.y * kLanes + lane) * V;
+  TA acc[V] = {};
+  for (int i = 0; i < n; i += kLanes) {
+    unsigned long long hits = __ballot(i + lane < n && z[min(i + lane, n - 1)] == element);
+    while (hits) {
+      const int count = __popcll(hits);
+      int row = 0;
+      typename R::VS v[kAhead];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {   // beyond the last one that one again
+        if (hits) row = i + __builtin_ctzll(hits);
+        hits &= hits - 1;
+        if (c < channels) v[k] = *reinterpret_cast<const typename R::VS*>(dY + static_cast<int64_t>(row) * channels + c);
+      }
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k)
+        if (k < count && c < channels) R::add(acc, v[k]);
+    }
+  }
+  if (c < channels) R::store(dT + static_cast<int64_t>(element) * channels + c, acc, scale);
+}
+
+// Up to kSearchRows rows: the wave lists them first.  Up to kLongList of them it adds itself; of an element with more every wave of the workgroup adds a
+// share, joined in order.  (1024 rows of one element by one wave, one after the other, 148 us; so 16, and sorted 24.)  x of the grid: elements; y: col_step blocks of
+// 64 V channels.
+constexpr int kSearchRows = 1024;
+constexpr int kLongList = 32;
+constexpr int kManyGroups = 4096;   // workgroups of elements
+
+template <typename TS, typename TA, int V>
+__global__ __launch_bounds__(kThreads) void search_kernel(int n, int col_blocks, int col_step, int channels, int elements, TA scale,
                                                           const int* __restrict__ z, const TS* __restrict__ dY, TA* __restrict__ dT) {
   typedef Row<TS, TA, V> R;
+  __shared__ unsigned short list[kWaves][kSearchRows];
+  __shared__ int4 found;
+  __shared__ TA part[kWaves][kLanes * V];
+  static_assert(kWaves == 4, "a component of `found` for each wave");
   const int lane = threadIdx.x & (kLanes - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
-  for (int64_t task = blockIdx.x * static_cast<int64_t>(kWaves) + wave; task < static_cast<int64_t>(elements) * col_blocks;
-       task += gridDim.x * static_cast<int64_t>(kWaves)) {
-    const int element = static_cast<int>(task / col_blocks);
-    const int c = (static_cast<int>(task % col_blocks) * kLanes + lane) * V;
-    TA acc[V] = {};
-    for (int i = 0; i < n; i += kLanes) {
-      unsigned long long hits = __ballot(i + lane < n && z[min(i + lane, n - 1)] == element);
-      while (hits) {
-        const int r = i + __builtin_ctzll(hits);
-        hits &= hits - 1;
-        if (c < channels) R::add(acc, *reinterpret_cast<const typename R::VS*>(dY + static_cast<int64_t>(r) * channels + c));
-      }
+  const int first = blockIdx.x * kWaves, element = first + wave;   // (beyond the table: no row has that index)
+  const int cb0 = blockIdx.y * col_step, cb1 = min(col_blocks, cb0 + col_step);
+  int count = 0;
+  for (int i = 0; i < n; i += kLanes) {
+    const bool hit = i + lane < n && element < elements && z[min(i + lane, n - 1)] == element;
+    const unsigned long long hits = __ballot(hit);
+    if (hit) list[wave][count + __popcll(hits & ((1ull << lane) - 1))] = static_cast<unsigned short>(i + lane);
+    count += __popcll(hits);
+  }
+  if (lane == 0) reinterpret_cast<int*>(&found)[wave] = count;
+  __syncthreads();
+  if (element < elements && count <= kLongList)
+    for (int cb = cb0; cb < cb1; ++cb) {
+      const int c = (cb * kLanes + lane) * V;
+      if (c >= channels) break;
+      TA acc[V] = {};
+      if (count > 0) add_rows<TS, TA, V>(list[wave], 0, count, dY, channels, c, acc);
+      R::store(dT + static_cast<int64_t>(element) * channels + c, acc, scale);
     }
-    if (c < channels) R::store(dT + static_cast<int64_t>(element) * channels + c, acc, scale);
+  const int4 all = found;
+  if (max(max(all.x, all.y), max(all.z, all.w)) <= kLongList) return;   // the same for all waves
+  for (int w = 0; w < kWaves; ++w) {
+    const int rows = w == 0 ? all.x : w == 1 ? all.y : w == 2 ? all.z : all.w;
+    if (rows <= kLongList) continue;
+    const int per = (rows + kWaves - 1) / kWaves, from = min(rows, wave * per), to = min(rows, from + per);
+    for (int cb = cb0; cb < cb1; ++cb) {
+      const int c = (cb * kLanes + lane) * V;
+      TA acc[V] = {};
+      if (c < channels && from < to) add_rows<TS, TA, V>(list[w], from, to, dY, channels, c, acc);
+#pragma unroll
+      for (int k = 0; k < V; ++k) part[wave][lane * V + k] = acc[k];
+      __syncthreads();
+      if (wave == 0 && c < channels) {
+        for (int v = 1; v < kWaves; ++v)
+#pragma unroll
+          for (int k = 0; k < V; ++k) acc[k] += part[v][lane * V + k];
+        R::store(dT + static_cast<int64_t>(first + w) * channels + c, acc, scale);
+      }
+      __syncthreads();   // part is the next block's
+    }
   }
 }
 
@@ -432,10 +523,10 @@ sc_status check_config(const char* fn, const ee_config* cfg, int64_t n) {
   return SC_OK;
 }
 
-// Does the search take a batch?  Its waves each look through all indices, 64 at a time, and add the rows of their element one by one; it saves three
-// launches, six for long tables.  512 rows of 89 elements 7.4 us, sorted 20.9, of 10 000 elements 8.0 and 42; 1024 rows of 65 536 33.5 and 63, 67 of a
-// million 115 and 523.  But 1024 rows of 10 elements 22 and 21, as of any table whose rows are that unevenly used.
-bool searched(const ee_config* c, int64_t n) { return n <= 1024 && n * c->num_elements <= 1 << 26; }
+// Does the search take a batch?  It is one launch instead of four, for long tables six, and no slower than those however the rows are spread over the elements
+// (search, sort; 128 and 512 channels): 64 rows of one element 6 and 6 us, 18 and 20; 1024 rows of one element 15 and 20, 24 and 28, of 10 elements 12 and 15, 18 and 22, of
+// 10 000 elements 9 and 17, 34 and 39, of 65 536 39 and 49, 62 and 68, of one of those 39 and 50, 60 and 65; 67 rows of a million elements of 4 channels 84 and 517.
+bool searched(const ee_config* c, int64_t n) { return n <= kSearchRows && n * c->num_elements <= 1 << 26; }
 
 int64_t sort_rows_per_block(int64_t n) {
   const int64_t per = std::max<int64_t>(kSortChunk, (n + kSortBlocks - 1) / kSortBlocks);
@@ -527,8 +618,17 @@ struct Calls {
     const int col_blocks = (k + kLanes * V - 1) / (kLanes * V);
     const TA scale = static_cast<TA>(c->scale);
     if (searched(c, n)) {
-      hipLaunchKernelGGL((search_kernel<TS, TA, V>), dim3(blocks_of(static_cast<int64_t>(elements) * col_blocks)), dim3(kThreads), 0, stream,
-                         static_cast<int>(n), col_blocks, k, elements, scale, z, static_cast<const TS*>(dY), static_cast<TA*>(dT));
+      const int groups = (elements + kWaves - 1) / kWaves;
+      if (n <= kFewRows) {
+        hipLaunchKernelGGL((search_few_kernel<TS, TA, V>), dim3(groups, col_blocks), dim3(kThreads), 0, stream, static_cast<int>(n), k, elements, scale, z,
+                           static_cast<const TS*>(dY), static_cast<TA*>(dT));
+        return hipGetLastError();
+      }
+      // A workgroup does one block of channels, or all where the elements alone make more workgroups than the chip holds: the indices are looked through
+      // once (1024 rows of 65 536 elements, 512 channels, 92 us and 49).
+      const int col_step = groups >= kManyGroups ? col_blocks : 1;
+      hipLaunchKernelGGL((search_kernel<TS, TA, V>), dim3(groups, (col_blocks + col_step - 1) / col_step), dim3(kThreads), 0, stream, static_cast<int>(n),
+                         col_blocks, col_step, k, elements, scale, z, static_cast<const TS*>(dY), static_cast<TA*>(dT));
       return hipGetLastError();
     }
     const Workspace w = carve(c, n, ws);

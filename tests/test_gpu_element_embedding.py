@@ -235,3 +235,52 @@ def test_tables_of_more_waves_than_a_launch_has(ee, elements, channels):
     dT[7] = dY[1]
     ee.ee_forward(cfg, 3, z, dT, Y)
     assert not Y[0].any() and torch.equal(Y[1], 2 * dY[1])
+
+
+@pytest.mark.parametrize("n", [31, 32, 33, 64, 65, 127, 130, 257, 512, 1023, 1024])
+@pytest.mark.parametrize("dtype", ["f32", "f64", "bf16"])
+@pytest.mark.parametrize("elements,used,channels", [(1, 1, 64), (2, 2, 130), (89, 1, 128), (89, 2, 257), (6, 6, 1024), (1001, 3, 33), (65_536, 1, 66)])
+def test_few_rows_of_few_elements(ee, n, dtype, elements, used, channels):
+    """Small integers, exact: rows that several waves share, the last one of a workgroup's elements beyond the table, indices outside it between them."""
+    import torch
+    print(f"embedding {n} rows of {used} of {elements} elements {channels} {dtype}", flush=True)
+    row = {"f32": torch.float32, "f64": torch.float64, "bf16": torch.bfloat16}[dtype]
+    table = torch.float64 if dtype == "f64" else torch.float32
+    g = torch.Generator(device="cuda").manual_seed(n)
+    which = torch.randperm(elements, generator=g, device="cuda")[:used]
+    z = which[torch.randint(0, used, (n,), generator=g, device="cuda")].int()
+    z[5::11] = elements
+    z[7::13] = -1
+    dY = torch.randint(-9, 10, (n, channels), generator=g, device="cuda").to(row)
+    dT = torch.full((elements, channels), float("nan"), dtype=table, device="cuda")
+    cfg = ee.make_config(elements, channels, 0.25, {"f32": ee.SC_F32, "f64": ee.SC_F64, "bf16": ee.SC_BF16}[dtype])
+    nbytes = ee.ee_workspace_bytes(cfg, n)
+    ee.ee_backward(cfg, n, z, dY, dT, torch.full((nbytes,), 255, dtype=torch.uint8, device="cuda"), nbytes)
+    inside = (z >= 0) & (z < elements)
+    want = torch.zeros(elements, channels, dtype=torch.float64, device="cuda").index_add_(0, z[inside].long(), dY[inside].double()) * 0.25
+    assert torch.equal(dT, want.to(table))
+
+
+@pytest.mark.parametrize("elements", [2, 89, 10_000])
+def test_a_small_batch_of_one_element_is_no_slower_than_a_larger_one(ee, elements):
+    """1024 rows are searched, 1025 sorted: the same work but for one row, however unevenly the elements are used (half as much again for noise)."""
+    import torch
+    print(f"embedding, time of 1024 rows of one of {elements} elements", flush=True)
+
+    def microseconds(n):
+        cfg = ee.make_config(elements, 128, 1.0)
+        z, dY = torch.full((n,), elements // 2, device="cuda", dtype=torch.int32), torch.randn(n, 128, device="cuda")
+        dT, nbytes = torch.empty(elements, 128, device="cuda"), ee.ee_workspace_bytes(cfg, n)
+        ws, times = torch.empty(nbytes, dtype=torch.uint8, device="cuda"), []
+        for _ in range(25):
+            start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            start.record()
+            for _ in range(4):
+                ee.ee_backward(cfg, n, z, dY, dT, ws, nbytes)
+            end.record()
+            torch.cuda.synchronize()
+            times.append(start.elapsed_time(end) * 250)
+        return sorted(times)[12]
+    few, more = microseconds(1024), microseconds(1025)
+    print(f"1024 rows {few:.1f} us, 1025 rows {more:.1f} us", flush=True)
+    assert few < 1.5 * more
