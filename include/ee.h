@@ -37,7 +37,7 @@ typedef struct {
   int32_t dtype;        /* sc_dtype                             */
   int32_t device;       /* HIP device ordinal                   */
   int32_t reserved;     /* 0                                    */
-  double scale;         /* finite                               */
+  double scale;         /* finite, in fp32 too but for SC_F64   */
 } ee_config;
 
 /* z [n_nodes] int32, T [num_elements][num_channels], Y [n_nodes][num_channels].  n_nodes == 0 does nothing. */

@@ -119,3 +119,12 @@ def test_dense_layer_workspace_of_wide_layers(dtype):
     # one chunk needs no partial results
     assert dl.dl_workspace_bytes(dl.make_config(4096, 4096, dl.DL_NONE, dl.SC_F64), 20_000) <= 4096 * 4096 * 8 + 1024
     assert dl.dl_workspace_bytes(dl.make_config(dl.DL_MAX_WIDTH, dl.DL_MAX_WIDTH, dl.DL_NONE, dl.SC_F32), 8192) <= dl.DL_MAX_WIDTH ** 2 * 4 + 1024
+
+
+def test_embedding_refuses_a_scale_that_its_type_does_not_hold():
+    for dtype in (dl.SC_F32, dl.SC_BF16):
+        refused(INVALID, ee.ee_workspace_bytes, ee.make_config(89, 128, 1e39, dtype), 10)
+        refused(INVALID, ee.ee_workspace_bytes, ee.make_config(89, 128, -1e39, dtype), 10)
+        refused(INVALID, ee.ee_forward, ee.make_config(89, 128, 1e39, dtype), 10, 16, 16, 16, stream=0)
+        ee.ee_workspace_bytes(ee.make_config(89, 128, 3e38, dtype), 10)
+    ee.ee_workspace_bytes(ee.make_config(89, 128, 1e300, dl.SC_F64), 10)
