@@ -8,7 +8,8 @@
  *   dst_j = coefficient * src_j
  *
  * Sums in fp64 in a fixed order: bitwise reproducible, and fp32 gradients of any finite size neither
- * overflow nor vanish in the square (fp64 gradients beyond 1e154 do overflow).  An infinite element gives the norm infinity and the coefficient 0 (so
+ * overflow nor vanish in the square (fp64 gradients beyond 1e154 do overflow).  fp32 and bfloat16 elements are multiplied in
+ * fp32, in fp64 where the coefficient is below 1e-30.  An infinite element gives the norm infinity and the coefficient 0 (so
  * the infinite element becomes NaN, the others 0); a NaN makes norm, coefficient and every result NaN: a training
  * loop tests the norm before it takes the step.
  *

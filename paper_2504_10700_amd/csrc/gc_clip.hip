@@ -89,12 +89,10 @@ struct Square {
 };
 
 // (The results go past the caches, which hold the end of what the first pass read.)
-template <int kChunk, typename T>
-__device__ __forceinline__ void scale_chunk(const T* src, T* dst, int64_t n, double coefficient) {
-  typedef std::conditional_t<sizeof(T) == 8, double, float> A;
+template <int kChunk, typename A, typename T>
+__device__ __forceinline__ void scale_by(const T* src, T* dst, int64_t n, A c) {
   constexpr int N = Vec<T>::kN, kRounds = kChunk / (kThreads * N);
   typedef typename Vec<T>::type V;
-  const A c = static_cast<A>(coefficient);
   if (n >= kChunk) {
     V v[kRounds];
 #pragma unroll
@@ -108,6 +106,15 @@ __device__ __forceinline__ void scale_chunk(const T* src, T* dst, int64_t n, dou
   } else {
     for (int at = threadIdx.x; at < n; at += kThreads) dst[at] = static_cast<T>(c * static_cast<A>(src[at]));
   }
+}
+
+// Below this a coefficient soon has fewer than 24 bits in fp32, or none, while its product with elements near the largest numbers has them all.
+constexpr double kSmallCoefficient = 1e-30;
+
+template <int kChunk, typename T>
+__device__ __forceinline__ void scale_chunk(const T* src, T* dst, int64_t n, double coefficient) {
+  if (sizeof(T) == 8 || coefficient < kSmallCoefficient) scale_by<kChunk, double>(src, dst, n, coefficient);
+  else if constexpr (sizeof(T) != 8) scale_by<kChunk, float>(src, dst, n, static_cast<float>(coefficient));
 }
 
 // The same sum in every workgroup and run: lanes, then waves in order.

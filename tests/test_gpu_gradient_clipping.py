@@ -186,3 +186,16 @@ def test_long_lists_of_every_type(gc, in_place):
         u = {torch.float32: 2.0 ** -23, torch.float64: 2.0 ** -51, torch.bfloat16: 2.0 ** -8 + 2.0 ** -23}[x.dtype]
         w = w.double() * coefficient
         assert ((x.double() - w).abs() <= u * w.abs()).all()
+
+
+@pytest.mark.parametrize("max_norm", [1e3, 1.0, 1e-9])
+@pytest.mark.parametrize("several", [1, 120])
+@pytest.mark.parametrize("kind", ["float32", "bfloat16", "mixed"])
+def test_gradients_near_the_largest_numbers(gc, kind, several, max_norm):
+    """Norms of 1e40 and more: the coefficient, 1e-37 to 1e-50, is no number of 24 bits in fp32, the elements are some 1e-2 to 1e-12 all the same."""
+    import torch
+    types = [torch.float32 if kind == "mixed" and i % 2 else torch.bfloat16 if kind != "float32" else torch.float32 for i in range(several)]
+    src = [x.clamp(-3, 3).mul_(1e38) for x in make([20_011] * several, types)]
+    print(f"clip {several} tensors near 1e38, {kind}, to {max_norm}", flush=True)
+    check(gc, src, max_norm)
+    check(gc, src, max_norm, in_place=True)
