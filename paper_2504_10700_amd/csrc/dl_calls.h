@@ -107,6 +107,7 @@ __device__ __forceinline__ void each_tile(const Walk& walk, const Shape& shape, 
 // What becomes of four neighbouring results v of a row.  The constructor takes what is the same for a lane's column.
 template <typename TS, typename TA, bool kFours, int kResidual>
 struct ForwardEnd {   // Z = v (bias added), Y = act(Z) + residual
+  static constexpr bool kRounded = sizeof(TS) == 2;   // results go to bfloat16 and nowhere else
   Gate<TA> gate;
   int64_t ld_out;
   int n_end;
@@ -134,6 +135,7 @@ struct ForwardEnd {   // Z = v (bias added), Y = act(Z) + residual
 // v = V: ddY = V act'(Z), S = V dY act''(Z).  kBeside 0: no activation; 1: no curvature (Z alone is read, no S); 2: Z and dY.
 template <typename TS, typename TA, bool kFours, int kBeside>
 struct SecondEnd {
+  static constexpr bool kRounded = sizeof(TS) == 2 && kBeside < 2;   // (S goes into sums that stay fp32)
   Gate<TA> gate;
   int64_t ld_out;
   int n_end;
@@ -165,6 +167,7 @@ struct SecondEnd {
 
 template <typename TS, typename TA, bool kFours>
 struct StoreEnd {
+  static constexpr bool kRounded = sizeof(TS) == 2;
   int64_t ld;
   int n_end;
   TS* out;
@@ -189,19 +192,19 @@ template <int kRT, int kX, int kW>
 constexpr int rows_words() { return kWaves * kRT * kX * kPlane + shared_words<kW>(); }
 
 // The results of 16 kRT kWaves rows from row0 and of 64 columns by a workgroup.
-template <int kRT, int kX, int kW, typename Rows, typename T, int N, typename F>
+template <int kRT, int kX, int kW, typename Rows, typename T, int N, typename End>
 __device__ __forceinline__ void finish_rows_parts(const Rows& a, const AlongRows<float>& w, int64_t row0, int64_t rows, int n0, unsigned* lds,
-                                                  const float* __restrict__ bias, const Beside<T, N>& beside, F&& f) {
+                                                  const float* __restrict__ bias, const Beside<T, N>& beside, const End& end) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
   Acc acc[kRT][4];
   unsigned* const planes = lds + wave * (kRT * kX * kPlane);
   const Operand<float, float, kPlain> matrix{{w.W, w.n_end}, {}, {}};
   const int64_t first = row0 + wave * (16 * kRT);
-  const bool done = rows_parts<kRT, kX, kW>(as_rows<kX>(a), SharedColumns<float, kPlain, kW>{matrix}, first, rows, n0, w.n_end, w.k_end, planes,
-                                            lds + kWaves * kRT * kX * kPlane, acc);
+  const bool done = rows_parts<kRT, kX, kW, kX == 1 && End::kRounded>(as_rows<kX>(a), SharedColumns<float, kPlain, kW>{matrix}, first, rows, n0, w.n_end,
+                                                                      w.k_end, planes, lds + kWaves * kRT * kX * kPlane, acc);
   if (!done) rows_product<float, kRT, true>(a, w, first, rows, n0, 0, w.k_end, reinterpret_cast<float*>(planes), acc);
   unscale<Rows::source>(acc, done);
-  each_four<float, kRT, true>(first, rows, n0, w.n_end, acc, bias, beside, f);
+  each_four<float, kRT, true>(first, rows, n0, w.n_end, acc, bias, beside, end);
 }
 
 template <typename TS, int kRT, typename End>
@@ -238,7 +241,7 @@ __global__ __launch_bounds__(kThreads, 2) void kept_kernel(Walk walk, int64_t tu
   keep(weights, n0, n_end, k_end, kept);
   float b[4] = {0, 0, 0, 0};
   if (bias) load4<true>(bias, n0 + 4 * (lane & 15), n_end, b);
-  walk_rows<kWc, kRounds, kX, kW>(
+  walk_rows<kWc, kRounds, kX, kW, kX == 1 && End::kRounded>(
       as_rows<kX>(from), kept, (rg * kWr + group) * kWc, walk.row_groups * kWaves, turns, own, rows, n0, n_end, k_end, lds + group * kWc * kSlots * kTile,
       flags[group], end.beside(),
       [&](int64_t row0, Acc(&acc)[1][4]) { rows_product<float, 1, true>(from, plain, row0, rows, n0, 0, k_end, corners[wave], acc); },

@@ -5,7 +5,9 @@
 //   fp32 rows       h h + (h m + m h + m m + h l + l h): what is left out is below 2^-24 of |x w|.  An instruction cuts its smaller products off at
 //                   the last bit of the largest and of the sum it adds to, so the five small products are summed by themselves and join
 //                   the sum of h h once per 32 reduced indices.
-//   bfloat16 rows   an element of them is one part; W, G = dY act' and S = V dY act'' are fp32 values and keep their three.
+//   bfloat16 rows   an element of them is one part; W, G = dY act' and S = V dY act'' are fp32 values and keep their three.  Results that are rounded to
+//                   bfloat16 and nothing else, of rows that are one part, take the three products into one sum, smallest first: two more
+//                   cuts at its last bit per 32 reduced indices (990 001 rows, 64 -> 1280, forward 815 us with two sums, 685 with one).
 //
 // G and S hold derivatives of the activations, which fall to nothing far out: a GELU layer whose pre-activations have a deviation of 2 has some below
 // 2^-110 in every tile.  Their parts are those of 2^16 times the value, which stand for every fp32 number below 2^111, and the sums are divided by 2^16
@@ -48,9 +50,9 @@ __device__ __forceinline__ Acc mma_parts(const U4& a, const U4& b, const Acc& c)
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(Bf8, a), __builtin_bit_cast(Bf8, b), c, 0, 0, 0);
 }
 
-// Adds a(i) b(i) to sum[i], i = 0..3: the products of the first parts to sum, the others to small (where no operand has three parts, all to sum).
+// Adds a(i) b(i) to sum[i], i = 0..3: the products of the first parts to sum, the others to small (kOneSum: all to sum, the smallest first).
 // Product by product over the four, as each instruction waits for the one before it on the same sum.
-template <int NA, int NB, typename A, typename B>
+template <int NA, int NB, bool kOneSum, typename A, typename B>
 __device__ __forceinline__ void multiply4(A&& a, B&& b, Acc (&sum)[4], Acc (&small)[4]) {
 #pragma unroll
   for (int order = NA + NB - 2; order > 0; --order)
@@ -59,16 +61,16 @@ __device__ __forceinline__ void multiply4(A&& a, B&& b, Acc (&sum)[4], Acc (&sma
       if (order - p >= 0 && order - p < NB && order < (NA > NB ? NA : NB)) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          Acc& to = NA == 3 || NB == 3 ? small[i] : sum[i];
+          Acc& to = kOneSum ? sum[i] : small[i];
           to = mma_parts(a(i)[p], b(i)[order - p], to);
         }
       }
 #pragma unroll
   for (int i = 0; i < 4; ++i) sum[i] = mma_parts(a(i)[0], b(i)[0], sum[i]);
 }
-template <int NA, int NB>
+template <bool kOneSum>
 __device__ __forceinline__ void join4(Acc (&sum)[4], const Acc (&small)[4]) {
-  if constexpr (NA == 3 || NB == 3) {
+  if constexpr (!kOneSum) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) sum[i] += small[i];
   }
@@ -343,7 +345,7 @@ __device__ __forceinline__ bool any_wave(bool mine, unsigned* flag) {
 // rows_product on parts: acc[rt][u] of 16 kRT rows from row0 and the 64 columns from n0 that the workgroup's four waves share, over all reduced
 // indices.  planes: kRT * kX planes of this wave; shared: shared_words<kW>() of the workgroup.  All waves come here, the rows of some may lie
 // beyond the last.  false for all waves: a value that the parts do not stand for.
-template <int kRT, int kX, int kW, typename Rows, typename Weights>
+template <int kRT, int kX, int kW, bool kOneSum, typename Rows, typename Weights>
 __device__ __forceinline__ bool rows_parts(const Rows& a, const Weights& w, int64_t row0, int64_t rows, int n0, int n_end, int k_end,
                                            unsigned* planes, unsigned* shared, Acc (&acc)[kRT][4]) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
@@ -382,8 +384,8 @@ __device__ __forceinline__ bool rows_parts(const Rows& a, const Weights& w, int6
         U4 c[kW];
         get_shared<kW>(shared + at, u, c);
         Acc sum[4] = {acc[0][u], acc[1][u], acc[2][u], acc[3][u]}, small[4] = {};
-        multiply4<kX, kW>([&](int i) -> const U4(&)[kX] { return x[i]; }, [&](int) -> const U4(&)[kW] { return c; }, sum, small);
-        join4<kX, kW>(sum, small);
+        multiply4<kX, kW, kOneSum>([&](int i) -> const U4(&)[kX] { return x[i]; }, [&](int) -> const U4(&)[kW] { return c; }, sum, small);
+        join4<kOneSum>(sum, small);
 #pragma unroll
         for (int i = 0; i < kRT; ++i) acc[i][u] = sum[i];
       }
@@ -392,8 +394,8 @@ __device__ __forceinline__ bool rows_parts(const Rows& a, const Weights& w, int6
 #pragma unroll
       for (int u = 0; u < 4; ++u) get_shared<kW>(shared + at, u, c[u]);
       Acc small[4] = {};
-      multiply4<kX, kW>([&](int) -> const U4(&)[kX] { return x[0]; }, [&](int u) -> const U4(&)[kW] { return c[u]; }, acc[0], small);
-      join4<kX, kW>(acc[0], small);
+      multiply4<kX, kW, kOneSum>([&](int) -> const U4(&)[kX] { return x[0]; }, [&](int u) -> const U4(&)[kW] { return c[u]; }, acc[0], small);
+      join4<kOneSum>(acc[0], small);
     }
     Corner<float>::sync();
   }
@@ -428,8 +430,8 @@ __device__ __forceinline__ bool outer_parts(const A& a, const B& b, int m0, int 
       U4 x[kA];
       get_shared<kA>(shared + at, t, x);
       Acc small[4] = {};
-      multiply4<kA, kB>([&](int) -> const U4(&)[kA] { return x; }, [&](int u) -> const U4(&)[kB] { return g[u]; }, acc[t], small);
-      join4<kA, kB>(acc[t], small);
+      multiply4<kA, kB, kA == 1 && kB == 1>([&](int) -> const U4(&)[kA] { return x; }, [&](int u) -> const U4(&)[kB] { return g[u]; }, acc[t], small);
+      join4<kA == 1 && kB == 1>(acc[t], small);
     }
   }
   return !any_wave(unserved<4, 4>(acc, low), shared);
@@ -464,8 +466,8 @@ __device__ __forceinline__ bool block_parts(const A& a, const B& b, int m0, int 
 #pragma unroll
     for (int u = 0; u < 4; ++u) get_shared<kB>(sb, u, g[u]);
     Acc small[4] = {};
-    multiply4<kA, kB>([&](int) -> const U4(&)[kA] { return x; }, [&](int u) -> const U4(&)[kB] { return g[u]; }, acc[0], small);
-    join4<kA, kB>(acc[0], small);
+    multiply4<kA, kB, kA == 1 && kB == 1>([&](int) -> const U4(&)[kA] { return x; }, [&](int u) -> const U4(&)[kB] { return g[u]; }, acc[0], small);
+    join4<kA == 1 && kB == 1>(acc[0], small);
   }
   return !any_wave(unserved<1, 4>(acc, low), shared_a);
 }
@@ -538,7 +540,7 @@ __device__ __forceinline__ void keep(const Weights& w, int n0, int n_end, int k_
 // writes the other slot).  The rows of the next turn, and what the epilogue reads of the next tile, are requested before the present ones are
 // computed.  first: the group's first tile, step: from turn to turn, turns: the same for all waves of the workgroup; own: the wave's place among
 // the kWc.  again: the product of a tile that the parts do not serve.
-template <int kWc, int kRounds, int kX, int kW, typename Rows, typename T, int N, typename Again, typename F>
+template <int kWc, int kRounds, int kX, int kW, bool kOneSum, typename Rows, typename T, int N, typename Again, typename F>
 __device__ __forceinline__ void walk_rows(const Rows& a, const Kept<kRounds, kW>& kept, int64_t first, int64_t step, int64_t turns, int own, int64_t rows,
                                           int n0, int n_end, int k_end, unsigned* planes, unsigned* flags, const Beside<T, N>& beside, Again&& again,
                                           F&& finish) {
@@ -594,9 +596,9 @@ __device__ __forceinline__ void walk_rows(const Rows& a, const Kept<kRounds, kW>
       for (int r = 0; r < kRounds; ++r) {
         U4 x[kX];
         get_parts<kX>(here + i * kTile + r * kX * kPlane, x);
-        multiply4<kX, kW>([&](int) -> const U4(&)[kX] { return x; }, [&](int u) -> const U4(&)[kW] { return kept.c[r][u]; }, acc[0], small);
+        multiply4<kX, kW, kOneSum>([&](int) -> const U4(&)[kX] { return x; }, [&](int u) -> const U4(&)[kW] { return kept.c[r][u]; }, acc[0], small);
       }
-      join4<kX, kW>(acc[0], small);
+      join4<kOneSum>(acc[0], small);
       if constexpr (kWc > 1) low = flags[slot * kWc + i];
       // (all four tiles: a row that is not finite shows in each of them, a product beyond the largest number in its own only)
       const bool served = kept.served && !unserved<1, 4>(acc, low);
