@@ -261,3 +261,31 @@ def test_the_largest_preactivations_in_fp64(lib, act):
     assert torch.equal(Z, z) and torch.equal(Y, z.clamp(min=0)) and torch.equal(layer.backward(Z)[0], on)
     ddY, X2, W2, _ = layer.double_backward(Z)
     assert torch.equal(ddY, on) and not X2.any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("size", [1e30, 1e34])
+@pytest.mark.parametrize("rows,k_in,k_out", [(20, 64, 64), (MANY, 64, 64), (MANY, 132, 72), (MANY, 64, 260), (3000, 512, 256)])
+def test_large_gradients(lib, rows, k_in, k_out, size, dtype):
+    """SiLU with an upstream gradient near the largest numbers in a few rows; the others are as they would be without.  All of one sign: relative, 2^-16 for the sums
+    of 66 001 rows and less elsewhere, bfloat16 rows 2^-8."""
+    torch = lib.torch
+    print(f"dense layer, some dY of {size}, {rows} {k_in} {k_out} {dtype}", flush=True)
+    layer = Layer(lib, rows, k_in, k_out, "silu", dtype, bias=False, residual=False)
+    for t in (layer.X, layer.W, layer.HX, layer.dY):
+        t.abs_().add_(0.5)
+    layer.W.mul_(0.125)
+    layer.dY[3::1000] *= size
+    Z = layer.wide(1, torch.rand(rows, k_out, generator=torch.Generator(device="cuda").manual_seed(2), device="cuda") - 0.5)
+    X, W, dY, HX, z = (t.double() for t in (layer.X, layer.W, layer.dY, layer.HX, Z))
+    p = torch.sigmoid(z)
+    first, second = p + z * p * (1 - p), p * (1 - p) * (2 + z * (1 - 2 * p))
+    V = torch.matmul(HX, W)
+    G, S = dY * first, V * dY * second
+    Wt, Xt, Ht = W.t().contiguous(), X.t().contiguous(), HX.t().contiguous()
+    want = dict(dX=torch.matmul(G, Wt), dW=torch.matmul(Xt, G), db=G.sum(0), ddY=V * first, X2=torch.matmul(S, Wt), W2=torch.matmul(Xt, S) + torch.matmul(Ht, G), b2=S.sum(0))
+    assert all(w.max() < 3e38 for w in want.values())
+    got = dict(zip(("dX", "dW", "db", "ddY", "X2", "W2", "b2"), layer.backward(Z) + layer.double_backward(Z)))
+    for name, w in want.items():
+        off = (got[name].double() / w - 1).abs().max().item()
+        assert off <= 2.0 ** -16 + (2.0 ** -8 if dtype == "bf16" and name in ("dX", "ddY", "X2") else 0), f"{name}: {off}"
