@@ -17,10 +17,11 @@
 //                                             sum: all waves of a workgroup share a tile, each a part of the sum.  Bound by the latency of the launch and of
 //                                             a few dependent loads (380 rows, 8 -> 64: 4.9 us), fp64 also by act' (10 000 rows, 128 -> 16: 13 and 24 us).
 //   kept_kernel                               sums of at most 64, many rows: W's parts in registers, the rows once through.  Bound by memory: 199 003 rows, 64 -> 64
-//                                             fp32, forward 41 us and V 50 us at 4.9 and 5.1 TB/s, dX 34 us and X2 22 at 4.5 and 4.7, 64 -> 1280 221 us at 4.8.
-//   parts_rows_kernel, parts_backward_kernel  the other products of many rows or long sums.  64 x 64 blocks of dW: memory (64 -> 64 as above: 32 us at 4.8
-//                                             TB/s, W2 61 us at 4.2).  Wide: the matrix cores and the splitting that feeds them (64 -> 1280 fp32 backward 512
-//                                             us, the products of its parts alone 366; 8191 rows, 1024 -> 1024 bfloat16 146 us, 97).
+//                                             fp32, forward 41 us and V 50 us at 4.9 and 5.1 TB/s, dX 35 us and X2 22 at 4.4 and 4.7, 64 -> 1280 215 to 262 us;
+//                                             990 001 bfloat16 rows, 64 -> 1280, 630 to 665 us at 4 TB/s.
+//   parts_rows_kernel, parts_backward_kernel  the other products of many rows or long sums.  64 x 64 blocks of dW: memory (64 -> 64 as above: 33 us at 4.7
+//                                             TB/s, W2 60 us at 4.3).  Wide: the matrix cores and the splitting that feeds them (64 -> 1280 fp32 backward 520
+//                                             us, the products of its parts alone 366; 8191 rows, 1024 -> 1024 bfloat16 197 us, 145).
 #pragma once
 #include "dl_plan.h"
 

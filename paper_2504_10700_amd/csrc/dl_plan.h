@@ -136,9 +136,10 @@ inline Plan plan_of(const dl_config* c, int64_t n, const Wanted& want, bool spli
 inline bool curved(const dl_config* c) { return c->activation == DL_SILU || c->activation == DL_GELU; }
 
 // Do the bfloat16 matrix cores serve a product of rows (dl_parts.h)?  From 1024 blocks of 64 x 64 results on, and where the sum is long and there is a
-// block for every second CU; of the forward, whose launch does nothing else, with three parts a block for every CU.  (dX, dW and db together, fp32
-// instruction -> parts: 1000 rows, 1024 -> 1024 94 -> 83 us, 2100 rows 198 -> 120, 8000 rows, 128 -> 128 40 -> 25, 6000 rows, 128 -> 1240 110 -> 77;
-// 500 rows, 1024 -> 1024 54 -> 61.  Shorter sums: 25 000 rows, 64 -> 64, second order 41 -> 56.)
+// block for every second CU; of the forward, whose launch does nothing else, on fp32 rows a block for every CU.  (dX, dW and db together, GELU, fp32
+// instruction -> parts, us.  bfloat16 rows: 512 rows, 1024 -> 1024 59 -> 66, 640 rows 75 -> 65, 1000 rows 102 -> 78, 2100 rows 245 -> 103, 8000 rows, 128 -> 128
+// 40 -> 23, 6000 rows, 128 -> 1240 127 -> 75; fp32 rows: 512 rows, 1024 -> 1024 57 -> 65, 640 rows 69 -> 66, 1280 rows 142 -> 81, 2000 rows, 512 -> 512 72 -> 45,
+// 8000 rows, 128 -> 128 41 -> 26.  Shorter sums: 25 000 rows, 64 -> 64, second order 41 -> 56.)
 constexpr int64_t kFewBlocks = 128;
 constexpr int kLongSum = 128;
 inline bool in_parts(const dl_config* c, int64_t n, int cols, int k, int64_t few = kFewBlocks) {

@@ -13,7 +13,7 @@
 // Small batches instead look through all indices for each element: one launch.  (Rules and times at search_few_kernel and searched.)
 //
 // Measured: 200 000 rows of 128 fp32 channels, 89 elements: forward 18.5 us (5.6 TB/s), count 3.5, scatter 9.2, pieces 30 (3.4 TB/s of dY), join 9.8; 32 768 rows of 512
-// bfloat16 channels, 50 000 elements: forward 16 us, two sort passes 22, pieces 17, join (102 MB of dT, most of it zeros) 25.  61 rows: 2.4 and 3 us.
+// bfloat16 channels, 50 000 elements: forward 16 us, two sort passes 22, pieces 17, join (102 MB of dT, most of it zeros) 25.  61 rows: 2.5 and 2.7 us.
 #include <algorithm>
 #include <cmath>
 #include <limits>
