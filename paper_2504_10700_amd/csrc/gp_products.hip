@@ -1,0 +1,448 @@
+// The products by element of include/gp.h: arguments, entry points, and the kernels that serve every case.
+//
+// Rows (Y, dX): a workgroup computes 64 rows of one bucket x 64 columns; the rows are gathered by the grouping's order, the reduced index goes
+// through LDS 16 at a time.  dW: a workgroup computes 64 x 64 of one element's matrix over a chunk of the element's rows; elements with several chunks leave
+// partial matrices that a second launch adds in order.  Batches without a grouping: an atom is a bucket of its own.
+// fp32 and fp64 matrix instructions (el_tile.h has their operand layout).
+#include <algorithm>
+#include <initializer_list>
+#include <string>
+
+#include "el_tile.h"
+#include "gp_internal.h"
+
+namespace gp {
+namespace {
+
+using el::Mma;
+using sc::DeviceGuard;
+using sc::misaligned;
+using sc::set_error;
+
+constexpr int kTile = 64;
+constexpr int kDepth = 16;
+constexpr int kPitch = kTile + 4;
+
+struct Rows {
+  int64_t n;            // atoms
+  int64_t ld_src, ld_dst;
+  const int32_t* z;
+  Grouping group;       // offsets NULL: none
+  int elements, components;
+  int reduced, columns;
+  const void* src;
+  const void* W;        // [elements][k_in][k_out]
+  const void* residual;
+  void* dst;
+};
+
+// The row r of a bucket: its atom, and where the row begins.
+template <typename T>
+__device__ __forceinline__ T* row_at(T* p, const int32_t* order, int64_t n, int begin, int r, int components, int64_t ld, int width) {
+  const int a = components == 1 ? r : r / components;
+  const int64_t atom = order ? min(static_cast<unsigned>(order[begin + a]), static_cast<unsigned>(n - 1)) : begin + a;
+  return p + atom * ld + static_cast<int64_t>(r - a * components) * width;
+}
+
+// kBack: dX, where W is read transposed.
+template <typename T, typename TA, bool kBack>
+__global__ __launch_bounds__(kThreads) void rows_kernel(const Rows a) {
+  __shared__ TA xs[kDepth][kPitch], ws[kDepth][kPitch];
+  typedef typename Mma<TA>::acc_t Acc;
+  const int lane = threadIdx.x & (kLanes - 1), wave = threadIdx.x / kLanes;
+  int bucket, begin, rows, first;
+  if (a.group.offsets) {
+    const Place p = place_of(a.group.offsets, a.elements + 1, a.n, blockIdx.x, [&](int atoms) { return (atoms * a.components + kTile - 1) / kTile; });
+    if (p.bucket < 0) return;
+    bucket = p.bucket;
+    begin = p.begin;
+    rows = p.atoms * a.components;
+    first = p.local * kTile;
+  } else {
+    const int z = a.z[blockIdx.x];
+    bucket = static_cast<unsigned>(z) < static_cast<unsigned>(a.elements) ? z : a.elements;
+    begin = blockIdx.x;
+    rows = a.components;
+    first = 0;
+  }
+  const int c0 = blockIdx.y * kTile;
+  Acc acc[4];
+#pragma unroll
+  for (int t = 0; t < 4; ++t) acc[t] = Acc{0, 0, 0, 0};
+  if (bucket < a.elements) {
+    const TA* const W = static_cast<const TA*>(a.W) + static_cast<int64_t>(bucket) * a.reduced * a.columns;
+    const int xr = threadIdx.x / 4, xk = threadIdx.x % 4 * 4;   // 64 rows x 4 pieces of 4
+    const T* const x = row_at(static_cast<const T*>(a.src), a.group.order, a.n, begin, min(first + xr, rows - 1), a.components, a.ld_src, a.reduced);
+    for (int k = 0; k < a.reduced; k += kDepth) {
+      TA xv[4], wv[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) xv[i] = k + xk + i < a.reduced ? static_cast<TA>(x[k + xk + i]) : TA(0);
+      if constexpr (kBack) {   // W [column][reduced]
+        const int c = min(c0 + threadIdx.x / 4, a.columns - 1);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) wv[i] = k + xk + i < a.reduced ? W[static_cast<int64_t>(c) * a.reduced + k + xk + i] : TA(0);
+      } else {                 // W [reduced][column]
+        const int r = k + threadIdx.x / 16, c = c0 + threadIdx.x % 16 * 4;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) wv[i] = r < a.reduced && c + i < a.columns ? W[static_cast<int64_t>(r) * a.columns + c + i] : TA(0);
+      }
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < 4; ++i) xs[xk + i][xr] = xv[i];
+      if constexpr (kBack) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) ws[xk + i][threadIdx.x / 4] = wv[i];
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) ws[threadIdx.x / 16][threadIdx.x % 16 * 4 + i] = wv[i];
+      }
+      __syncthreads();
+#pragma unroll
+      for (int s = 0; s < kDepth / 4; ++s) {
+        const TA xo = xs[4 * s + lane / 16][16 * wave + (lane & 15)];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) acc[t] = Mma<TA>::mma(xo, ws[4 * s + lane / 16][16 * t + (lane & 15)], acc[t]);
+      }
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const int row = first + 16 * wave + Mma<TA>::row(lane, r);
+    if (row >= rows) continue;
+    T* const y = row_at(static_cast<T*>(a.dst), a.group.order, a.n, begin, row, a.components, a.ld_dst, a.columns);
+    const T* const base = a.residual ? static_cast<const T*>(a.residual) + (y - static_cast<T*>(a.dst)) : nullptr;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const int c = c0 + 16 * t + (lane & 15);
+      if (c < a.columns) y[c] = static_cast<T>(base ? acc[t][r] + static_cast<TA>(base[c]) : acc[t][r]);
+    }
+  }
+}
+
+struct Outer {
+  int64_t n;
+  int64_t ld_in, ld_out;
+  const int32_t* z;
+  Grouping group;
+  int elements, components;
+  int k_in, k_out;
+  int per;              // rows of a chunk
+  const void* X;
+  const void* dY;
+  void* dW;
+  void* partial;        // [slots][k_in][k_out]
+};
+
+// An element without rows has a chunk too, which zeroes its matrix.
+__device__ __forceinline__ int chunks_of(int rows, int per) { return max(1, static_cast<int>((static_cast<unsigned>(rows) + per - 1) / static_cast<unsigned>(per))); }
+
+template <typename T, typename TA>
+__global__ __launch_bounds__(kThreads) void outer_kernel(const Outer a) {
+  __shared__ TA xs[kDepth][kPitch], gs[kDepth][kPitch];
+  __shared__ int32_t list[GP_UNGROUPED];
+  typedef typename Mma<TA>::acc_t Acc;
+  const int lane = threadIdx.x & (kLanes - 1), wave = threadIdx.x / kLanes;
+  const int32_t* order = a.group.order;
+  int element, begin, first, last;
+  TA* out;
+  const int64_t size = static_cast<int64_t>(a.k_in) * a.k_out;
+  if (a.group.offsets) {
+    const Place p = place_of(a.group.offsets, a.elements, a.n, blockIdx.x, [&](int atoms) { return chunks_of(atoms * a.components, a.per); });
+    if (p.bucket < 0) return;
+    element = p.bucket;
+    begin = p.begin;
+    first = p.local * a.per;
+    last = min(p.atoms * a.components, first + a.per);
+    const bool several = p.units > 1;
+    out = static_cast<TA*>(several ? a.partial : a.dW) + (several ? p.slots + p.local : element) * size;
+  } else {   // the atoms of the element, found here
+    element = blockIdx.x;
+    const unsigned long long mine = __builtin_amdgcn_ballot_w64(lane < a.n && a.z[min(static_cast<int64_t>(lane), a.n - 1)] == element);
+    if (wave == 0 && (mine >> lane) & 1) list[__popcll(mine & ((1ull << lane) - 1))] = lane;
+    __syncthreads();
+    order = list;
+    begin = 0;
+    first = 0;
+    last = __popcll(mine) * a.components;
+    out = static_cast<TA*>(a.dW) + element * size;
+  }
+  const int col_tiles = (a.k_out + kTile - 1) / kTile;
+  const int tiles = (a.k_in + kTile - 1) / kTile * col_tiles;
+  for (int tile = blockIdx.y; tile < tiles; tile += gridDim.y) {
+  const int k0 = tile / col_tiles * kTile, c0 = tile % col_tiles * kTile;
+  Acc acc[4];
+#pragma unroll
+  for (int t = 0; t < 4; ++t) acc[t] = Acc{0, 0, 0, 0};
+  const int lr = threadIdx.x / 16, lc = threadIdx.x % 16 * 4;
+  for (int r = first; r < last; r += kDepth) {
+    const int row = min(r + lr, last - 1);
+    const bool inside = r + lr < last;
+    const T* const x = row_at(static_cast<const T*>(a.X), order, a.n, begin, row, a.components, a.ld_in, a.k_in);
+    const T* const g = row_at(static_cast<const T*>(a.dY), order, a.n, begin, row, a.components, a.ld_out, a.k_out);
+    TA xv[4], gv[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      xv[i] = inside && k0 + lc + i < a.k_in ? static_cast<TA>(x[k0 + lc + i]) : TA(0);
+      gv[i] = inside && c0 + lc + i < a.k_out ? static_cast<TA>(g[c0 + lc + i]) : TA(0);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      xs[lr][lc + i] = xv[i];
+      gs[lr][lc + i] = gv[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int s = 0; s < kDepth / 4; ++s) {
+      const TA xo = xs[4 * s + lane / 16][16 * wave + (lane & 15)];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) acc[t] = Mma<TA>::mma(xo, gs[4 * s + lane / 16][16 * t + (lane & 15)], acc[t]);
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const int k = k0 + 16 * wave + Mma<TA>::row(lane, r);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const int c = c0 + 16 * t + (lane & 15);
+      if (k < a.k_in && c < a.k_out) out[static_cast<int64_t>(k) * a.k_out + c] = acc[t][r];
+    }
+  }
+  }
+}
+
+// Slots of the elements before this one: the lanes of a wave add up theirs.
+__device__ __forceinline__ int slots_before(const Outer& a, int element) {
+  const int most = static_cast<int>(a.n);
+  int sum = 0;
+  for (int e = threadIdx.x & (kLanes - 1); e < element; e += kLanes) {
+    const int atoms = max(min(a.group.offsets[e + 1], most) - min(a.group.offsets[e], most), 0);
+    const int k = chunks_of(atoms * a.components, a.per);
+    sum += k > 1 ? k : 0;
+  }
+#pragma unroll
+  for (int d = 32; d > 0; d /= 2) sum += __shfl_xor(sum, d);
+  return __builtin_amdgcn_readfirstlane(sum);
+}
+
+// The matrices of elements with several chunks: their partial ones in order.
+template <typename TA>
+__global__ __launch_bounds__(kThreads) void join_kernel(const Outer a) {
+  const int64_t size = static_cast<int64_t>(a.k_in) * a.k_out;
+  const int element = blockIdx.x;
+  const int n_slots = slots_before(a, element);
+  const int atoms = max(min(a.group.offsets[element + 1], static_cast<int>(a.n)) - min(a.group.offsets[element], static_cast<int>(a.n)), 0);
+  const int n = chunks_of(atoms * a.components, a.per);
+  if (n < 2) return;
+  const TA* const from = static_cast<const TA*>(a.partial) + n_slots * size;
+  TA* const to = static_cast<TA*>(a.dW) + element * size;
+  for (int64_t i = static_cast<int64_t>(blockIdx.y) * kThreads + threadIdx.x; i < size; i += static_cast<int64_t>(gridDim.y) * kThreads) {
+    TA sum = 0;
+    for (int c = 0; c < n; ++c) sum += from[c * size + i];
+    to[i] = sum;
+  }
+}
+
+template <typename TA>
+__global__ __launch_bounds__(kThreads) void zero_kernel(TA* p, int64_t n) {
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; i < n; i += static_cast<int64_t>(gridDim.x) * kThreads) p[i] = 0;
+}
+
+// ---- host side
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Rows of a chunk of dW: enough chunks for the chip where the matrices alone do not fill it.
+int chunk_rows(const gp_config* c, int64_t n) {
+  const int64_t rows = n * c->components, tiles = ceil_div(c->k_in, kTile) * ceil_div(c->k_out, kTile);
+  const int64_t wanted = std::max<int64_t>(1, std::min<int64_t>(512, 2048 / tiles));
+  return static_cast<int>(std::min<int64_t>(std::max<int64_t>(512, ceil_div(ceil_div(rows, wanted), kTile) * kTile), int64_t(1) << 30));
+}
+// Chunks of the elements that have several, at most.
+int64_t slots_of(const gp_config* c, int64_t n) {
+  const int64_t rows = n * c->components, per = chunk_rows(c, n);
+  return n <= GP_UNGROUPED || rows <= per ? 0 : 2 * ceil_div(rows, per);
+}
+size_t element_size(const gp_config* c) { return c->dtype == SC_F64 ? 8 : c->dtype == SC_F32 ? 4 : 2; }
+size_t weight_size(const gp_config* c) { return c->dtype == SC_F64 ? 8 : 4; }
+size_t workspace_bytes(const gp_config* c, int64_t n) {
+  return align_up(std::max<size_t>(256, static_cast<size_t>(slots_of(c, n)) * c->k_in * c->k_out * weight_size(c)), 256);
+}
+
+sc_status check_config(const char* fn, const gp_config* cfg, int64_t n) {
+  auto bad = [&](sc_status st, const char* what) { return set_error(st, std::string(fn) + ": " + what); };
+  if (!cfg) return bad(SC_ERR_INVALID_ARG, "cfg is NULL");
+  if (cfg->struct_size != static_cast<int32_t>(sizeof(gp_config)))
+    return bad(SC_ERR_INVALID_ARG, "struct_size does not match this library's gp_config");
+  if (cfg->num_elements < 1 || cfg->k_in < 1 || cfg->k_out < 1 || cfg->components < 1)
+    return bad(SC_ERR_INVALID_ARG, "num_elements, k_in, k_out or components < 1");
+  if (cfg->num_elements > GP_MAX_ELEMENTS) return bad(SC_ERR_UNSUPPORTED, "num_elements above GP_MAX_ELEMENTS");
+  if (cfg->k_in > GP_MAX_WIDTH || cfg->k_out > GP_MAX_WIDTH) return bad(SC_ERR_UNSUPPORTED, "k_in or k_out above GP_MAX_WIDTH");
+  if (cfg->components > GP_MAX_COMPONENTS) return bad(SC_ERR_UNSUPPORTED, "components above GP_MAX_COMPONENTS");
+  if (cfg->dtype != SC_F32 && cfg->dtype != SC_F64 && cfg->dtype != SC_BF16) return bad(SC_ERR_INVALID_ARG, "bad dtype");
+  if (cfg->reserved != 0) return bad(SC_ERR_INVALID_ARG, "reserved is not 0");
+  if (cfg->ld_in != 0 && cfg->ld_in < static_cast<int64_t>(cfg->components) * cfg->k_in)
+    return bad(SC_ERR_INVALID_ARG, "ld_in below components * k_in");
+  if (cfg->ld_out != 0 && cfg->ld_out < static_cast<int64_t>(cfg->components) * cfg->k_out)
+    return bad(SC_ERR_INVALID_ARG, "ld_out below components * k_out");
+  if (cfg->ld_in > GP_MAX_STRIDE || cfg->ld_out > GP_MAX_STRIDE) return bad(SC_ERR_UNSUPPORTED, "ld_in or ld_out above GP_MAX_STRIDE");
+  if (n < 0) return bad(SC_ERR_INVALID_ARG, "n_nodes < 0");
+  if (n > GP_MAX_ROWS / cfg->components) return bad(SC_ERR_UNSUPPORTED, "n_nodes * components above GP_MAX_ROWS");
+  return SC_OK;
+}
+
+sc_status check_tensors(const char* fn, size_t align, std::initializer_list<const void*> needed, std::initializer_list<const void*> optional) {
+  for (const void* p : needed)
+    if (!p) return set_error(SC_ERR_INVALID_ARG, std::string(fn) + ": NULL tensor argument");
+  for (auto list : {needed, optional})
+    for (const void* p : list)
+      if (misaligned(p, align)) return set_error(SC_ERR_INVALID_ARG, std::string(fn) + ": tensor pointer not aligned to its element");
+  return SC_OK;
+}
+
+sc_status check_grouping(const char* fn, const gp_config* cfg, int64_t n, const void* grouping) {
+  if (n > GP_UNGROUPED && !grouping) return set_error(SC_ERR_INVALID_ARG, std::string(fn) + ": grouping is NULL");
+  if (misaligned(grouping, 256)) return set_error(SC_ERR_INVALID_ARG, std::string(fn) + ": grouping not 256-byte aligned");
+  return SC_OK;
+}
+
+sc_status check_workspace(const char* fn, const gp_config* cfg, int64_t n, const void* workspace, size_t given) {
+  if (!workspace || given < workspace_bytes(cfg, n))
+    return set_error(SC_ERR_WORKSPACE, std::string(fn) + ": workspace missing or smaller than gp_workspace_bytes()");
+  if (misaligned(workspace, 256)) return set_error(SC_ERR_WORKSPACE, std::string(fn) + ": workspace not 256-byte aligned");
+  return SC_OK;
+}
+
+sc_status launched(const char* fn, hipError_t e) {
+  return e == hipSuccess ? SC_OK : set_error(SC_ERR_HIP, std::string(fn) + ": kernel launch: " + hipGetErrorString(e));
+}
+
+int64_t ld_in_of(const gp_config* c) { return c->ld_in ? c->ld_in : static_cast<int64_t>(c->components) * c->k_in; }
+int64_t ld_out_of(const gp_config* c) { return c->ld_out ? c->ld_out : static_cast<int64_t>(c->components) * c->k_out; }
+Grouping grouping_for(const gp_config* c, int64_t n, const void* grouping) {
+  return n <= GP_UNGROUPED ? Grouping{nullptr, nullptr} : grouping_of(grouping, c->num_elements);
+}
+
+template <bool kBack>
+hipError_t launch_rows(const gp_config* c, const Rows& a, hipStream_t stream) {
+  const int64_t rows = a.n * c->components;
+  const int64_t tiles = a.group.offsets ? ceil_div(rows, kTile) + std::min<int64_t>(c->num_elements + 1, a.n) : a.n;
+  const dim3 grid(static_cast<unsigned>(tiles), static_cast<unsigned>(ceil_div(a.columns, kTile)));
+  if (c->dtype == SC_F64) hipLaunchKernelGGL((rows_kernel<double, double, kBack>), grid, dim3(kThreads), 0, stream, a);
+  else if (c->dtype == SC_F32) hipLaunchKernelGGL((rows_kernel<float, float, kBack>), grid, dim3(kThreads), 0, stream, a);
+  else hipLaunchKernelGGL((rows_kernel<__bf16, float, kBack>), grid, dim3(kThreads), 0, stream, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_outer(const gp_config* c, const Outer& a, hipStream_t stream) {
+  const int64_t rows = a.n * c->components, col_tiles = ceil_div(c->k_out, kTile), tiles = ceil_div(c->k_in, kTile) * col_tiles;
+  const int64_t chunks = a.group.offsets ? c->num_elements + rows / a.per : c->num_elements;
+  const dim3 grid(static_cast<unsigned>(chunks), static_cast<unsigned>(std::min<int64_t>(tiles, 32768)));
+  if (c->dtype == SC_F64) hipLaunchKernelGGL((outer_kernel<double, double>), grid, dim3(kThreads), 0, stream, a);
+  else if (c->dtype == SC_F32) hipLaunchKernelGGL((outer_kernel<float, float>), grid, dim3(kThreads), 0, stream, a);
+  else hipLaunchKernelGGL((outer_kernel<__bf16, float>), grid, dim3(kThreads), 0, stream, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || slots_of(c, a.n) == 0) return e;
+  const int64_t size = static_cast<int64_t>(c->k_in) * c->k_out;
+  const dim3 join(static_cast<unsigned>(c->num_elements), static_cast<unsigned>(std::min<int64_t>(ceil_div(size, kThreads), 1024)));
+  if (c->dtype == SC_F64) hipLaunchKernelGGL(join_kernel<double>, join, dim3(kThreads), 0, stream, a);
+  else hipLaunchKernelGGL(join_kernel<float>, join, dim3(kThreads), 0, stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+}  // namespace gp
+
+extern "C" {
+
+sc_status gp_grouping_bytes(const gp_config* cfg, int64_t n_nodes, size_t* bytes) {
+  const sc_status st = gp::check_config("gp_grouping_bytes", cfg, n_nodes);
+  if (st != SC_OK) return st;
+  if (!bytes) return sc::set_error(SC_ERR_INVALID_ARG, "gp_grouping_bytes: bytes is NULL");
+  *bytes = gp::grouping_bytes(cfg->num_elements, n_nodes);
+  return SC_OK;
+}
+
+sc_status gp_group(const gp_config* cfg, int64_t n_nodes, const int32_t* z, void* grouping, size_t grouping_bytes_given, void* hip_stream) {
+  using namespace gp;
+  sc_status st = check_config("gp_group", cfg, n_nodes);
+  if (st != SC_OK || n_nodes <= GP_UNGROUPED) return st;
+  st = check_tensors("gp_group", 4, {z}, {});
+  if (st == SC_OK) st = check_grouping("gp_group", cfg, n_nodes, grouping);
+  if (st != SC_OK) return st;
+  if (grouping_bytes_given < grouping_bytes(cfg->num_elements, n_nodes))
+    return set_error(SC_ERR_WORKSPACE, "gp_group: grouping smaller than gp_grouping_bytes()");
+  DeviceGuard guard(cfg->device);
+  if (!guard.ok) return set_error(SC_ERR_HIP, "gp_group: cannot make cfg->device current");
+  return launched("gp_group", launch_group(cfg, n_nodes, z, grouping, static_cast<hipStream_t>(hip_stream)));
+}
+
+sc_status gp_workspace_bytes(const gp_config* cfg, int64_t n_nodes, size_t* bytes) {
+  const sc_status st = gp::check_config("gp_workspace_bytes", cfg, n_nodes);
+  if (st != SC_OK) return st;
+  if (!bytes) return sc::set_error(SC_ERR_INVALID_ARG, "gp_workspace_bytes: bytes is NULL");
+  *bytes = gp::workspace_bytes(cfg, n_nodes);
+  return SC_OK;
+}
+
+sc_status gp_forward(const gp_config* cfg, int64_t n_nodes, const int32_t* z, const void* grouping, const void* X, const void* W,
+                     const void* residual, void* Y, void* workspace, size_t workspace_bytes_given, void* hip_stream) {
+  using namespace gp;
+  sc_status st = check_config("gp_forward", cfg, n_nodes);
+  if (st != SC_OK || n_nodes == 0) return st;
+  st = check_tensors("gp_forward", 4, {z}, {});
+  if (st == SC_OK) st = check_tensors("gp_forward", element_size(cfg), {X, Y}, {residual});
+  if (st == SC_OK) st = check_tensors("gp_forward", weight_size(cfg), {W}, {});
+  if (st == SC_OK) st = check_grouping("gp_forward", cfg, n_nodes, grouping);
+  if (st == SC_OK) st = check_workspace("gp_forward", cfg, n_nodes, workspace, workspace_bytes_given);
+  if (st != SC_OK) return st;
+  DeviceGuard guard(cfg->device);
+  if (!guard.ok) return set_error(SC_ERR_HIP, "gp_forward: cannot make cfg->device current");
+  const Rows a{n_nodes, ld_in_of(cfg), ld_out_of(cfg), z, grouping_for(cfg, n_nodes, grouping), cfg->num_elements, cfg->components,
+               cfg->k_in, cfg->k_out, X, W, residual, Y};
+  return launched("gp_forward", launch_rows<false>(cfg, a, static_cast<hipStream_t>(hip_stream)));
+}
+
+sc_status gp_backward(const gp_config* cfg, int64_t n_nodes, const int32_t* z, const void* grouping, const void* X, const void* W,
+                      const void* dY, void* dX, void* dW, void* workspace, size_t workspace_bytes_given, void* hip_stream) {
+  using namespace gp;
+  sc_status st = check_config("gp_backward", cfg, n_nodes);
+  if (st != SC_OK) return st;
+  if (!dX && !dW) return set_error(SC_ERR_INVALID_ARG, "gp_backward: dX and dW are both NULL");
+  st = check_tensors("gp_backward", element_size(cfg), {}, {X, dY, dX});
+  if (st == SC_OK) st = check_tensors("gp_backward", weight_size(cfg), {}, {W, dW});
+  if (st != SC_OK) return st;
+  if (n_nodes > 0) {
+    st = check_tensors("gp_backward", 4, {z}, {});
+    if (st == SC_OK) st = check_tensors("gp_backward", 1, {dY}, {});
+    if (st == SC_OK && dX) st = check_tensors("gp_backward", 1, {W}, {});
+    if (st == SC_OK && dW) st = check_tensors("gp_backward", 1, {X}, {});
+    if (st == SC_OK) st = check_grouping("gp_backward", cfg, n_nodes, grouping);
+    if (st == SC_OK) st = check_workspace("gp_backward", cfg, n_nodes, workspace, workspace_bytes_given);
+    if (st != SC_OK) return st;
+  } else if (!dW) {
+    return SC_OK;
+  }
+  DeviceGuard guard(cfg->device);
+  if (!guard.ok) return set_error(SC_ERR_HIP, "gp_backward: cannot make cfg->device current");
+  hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  if (n_nodes == 0) {
+    const int64_t size = static_cast<int64_t>(cfg->num_elements) * cfg->k_in * cfg->k_out;
+    const dim3 grid(static_cast<unsigned>(std::min<int64_t>(ceil_div(size, kThreads), 4096)));
+    if (cfg->dtype == SC_F64) hipLaunchKernelGGL(zero_kernel<double>, grid, dim3(kThreads), 0, stream, static_cast<double*>(dW), size);
+    else hipLaunchKernelGGL(zero_kernel<float>, grid, dim3(kThreads), 0, stream, static_cast<float*>(dW), size);
+    return launched("gp_backward", hipGetLastError());
+  }
+  const Grouping group = grouping_for(cfg, n_nodes, grouping);
+  if (dX) {
+    const Rows a{n_nodes, ld_out_of(cfg), ld_in_of(cfg), z, group, cfg->num_elements, cfg->components, cfg->k_out, cfg->k_in, dY, W, nullptr, dX};
+    const hipError_t e = launch_rows<true>(cfg, a, stream);
+    if (e != hipSuccess) return launched("gp_backward", e);
+  }
+  if (!dW) return SC_OK;
+  const Outer a{n_nodes, ld_in_of(cfg), ld_out_of(cfg), z, group, cfg->num_elements, cfg->components, cfg->k_in, cfg->k_out,
+                chunk_rows(cfg, n_nodes), X, dY, dW, workspace};
+  return launched("gp_backward", launch_outer(cfg, a, stream));
+}
+
+}  // extern "C"

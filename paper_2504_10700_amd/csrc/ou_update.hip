@@ -1,0 +1,410 @@
+// The orthogonalised update of include/ou.h: arguments, entry points, and the kernels that serve every case.
+//
+// The list goes to the workspace once.  Then, each for all tensors of one arithmetic type together: momentum and sums of squares; X = U / norm; per
+// step S = X X^T, P = b S + c S S, X = a X + P X; the last step's results go straight into the update and the weights.
+#include <algorithm>
+#include <cmath>
+#include <string>
+#include <vector>
+
+#include "el_tile.h"
+#include "ou_internal.h"
+
+namespace ou {
+namespace {
+
+using el::Mma;
+using sc::DeviceGuard;
+using sc::misaligned;
+using sc::set_error;
+
+constexpr int kTile = 64, kDepth = 16, kPitch = kTile + 4;
+constexpr int kChunk = 4096;   // elements of a chunk
+
+struct Step {
+  double a, b, c, mu, rate, keep, eps;   // keep: 1 - rate * decay
+  int nesterov;
+};
+
+__global__ __launch_bounds__(kLanes) void send_kernel(const Sent sent, Item* __restrict__ items) {
+  const int i = threadIdx.x;
+  if (i < sent.count) items[sent.first + i] = sent.item[i];
+}
+
+__device__ __forceinline__ int64_t chunks_of(int64_t elements) { return (elements + kChunk - 1) / kChunk; }
+
+__device__ __forceinline__ double workgroup_sum(double v, double* slots) {
+#pragma unroll
+  for (int d = 32; d > 0; d /= 2) v += __shfl_xor(v, d);
+  if ((threadIdx.x & 63) == 0) slots[threadIdx.x / 64] = v;
+  __syncthreads();
+  double s = slots[0];
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) s += slots[w];
+  __syncthreads();
+  return s;
+}
+
+// T: of the gradient; TA: of everything else.
+template <typename T, typename TA>
+__device__ __forceinline__ double momentum_chunk(const Item& it, const Step& st, int64_t at, int n, TA* __restrict__ x) {
+  const T* const g = static_cast<const T*>(it.grad) + at;
+  TA* const m = it.momentum ? static_cast<TA*>(it.momentum) + at : nullptr;
+  const TA mu = static_cast<TA>(st.mu);
+  double sum = 0;
+  for (int i = threadIdx.x; i < n; i += kThreads) {
+    TA u = static_cast<TA>(g[i]);
+    if (m) {
+      const TA v = mu * m[i] + u;
+      m[i] = v;
+      u = st.nesterov ? u + mu * v : v;
+    }
+    x[at + i] = u;
+    sum = fma(static_cast<double>(u), static_cast<double>(u), sum);
+  }
+  return sum;
+}
+
+template <typename TA>
+__global__ __launch_bounds__(kThreads) void momentum_kernel(const Item* __restrict__ items, int n, const Step st, TA* __restrict__ X, double* __restrict__ partial) {
+  __shared__ double slots[kWaves];
+  const Item& it = items[item_of(items, n, kChunks, blockIdx.x)];
+  const int64_t size = static_cast<int64_t>(it.rows) * it.cols, per = chunks_of(size), unit = blockIdx.x - it.unit[kChunks];
+  const int64_t matrix = unit / per, at = unit % per * kChunk;
+  const int count = static_cast<int>(min(size - at, static_cast<int64_t>(kChunk)));
+  TA* const x = X + it.x;
+  double sum;
+  if constexpr (sizeof(TA) == 8) sum = momentum_chunk<double, double>(it, st, matrix * size + at, count, x);
+  else if (it.dtype == SC_F32) sum = momentum_chunk<float, float>(it, st, matrix * size + at, count, x);
+  else sum = momentum_chunk<__bf16, float>(it, st, matrix * size + at, count, x);
+  sum = workgroup_sum(sum, slots);
+  if (threadIdx.x == 0) partial[blockIdx.x] = sum;
+}
+
+// A finished element of X: into the update and the weight.
+template <typename TA>
+__device__ __forceinline__ void finish(const Item& it, const Step& st, int64_t at, TA x) {
+  if (it.update) {
+    if (sizeof(TA) == 4 && it.dtype == SC_BF16) static_cast<__bf16*>(it.update)[at] = static_cast<__bf16>(static_cast<float>(x));
+    else static_cast<TA*>(it.update)[at] = x;
+  }
+  if (it.weight) {
+    TA* const w = static_cast<TA*>(it.weight) + at;
+    *w = static_cast<TA>(st.keep) * *w - static_cast<TA>(st.rate * it.scale) * x;
+  }
+}
+
+// X = U / (norm + eps); last: no steps follow.
+template <typename TA>
+__global__ __launch_bounds__(kThreads) void normalise_kernel(const Item* __restrict__ items, int n, const Step st, bool last, TA* __restrict__ X,
+                                                             const double* __restrict__ partial) {
+  __shared__ double slots[kWaves];
+  const Item& it = items[item_of(items, n, kChunks, blockIdx.x)];
+  const int64_t size = static_cast<int64_t>(it.rows) * it.cols, per = chunks_of(size), unit = blockIdx.x - it.unit[kChunks];
+  const int64_t matrix = unit / per, at = unit % per * kChunk;
+  const int count = static_cast<int>(min(size - at, static_cast<int64_t>(kChunk)));
+  double sum = 0;
+  for (int64_t i = threadIdx.x; i < per; i += kThreads) sum += partial[it.unit[kChunks] + matrix * per + i];
+  const double down = 1.0 / (sqrt(workgroup_sum(sum, slots)) + st.eps);
+  for (int i = threadIdx.x; i < count; i += kThreads) {
+    const int64_t e = matrix * size + at + i;
+    const TA x = static_cast<TA>(static_cast<double>(X[it.x + e]) * down);
+    if (last) finish(it, st, e, x); else X[it.x + e] = x;
+  }
+}
+
+// Element (i, k) of a matrix at p[i * ld + k * step].
+template <typename TA>
+struct View {
+  const TA* p;
+  int64_t ld, step;
+  int rows, depth;
+};
+
+// acc[t] of wave's 16 rows and 64 columns: sum over k of P(i, k) Q(j, k).
+template <typename TA>
+__device__ __forceinline__ void product(const View<TA>& p, const View<TA>& q, int i0, int j0, TA (&ps)[kDepth][kPitch], TA (&qs)[kDepth][kPitch],
+                                        typename Mma<TA>::acc_t (&acc)[4]) {
+  const int lane = threadIdx.x & (kLanes - 1), wave = threadIdx.x / kLanes;
+  const int depth = p.depth;
+  auto load = [&](const View<TA>& v, int r0, int k, TA (&to)[kDepth][kPitch], TA (&x)[4]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int kk = v.step == 1 ? k + threadIdx.x % 16 : k + threadIdx.x / 64 + 4 * e;
+      const int r = r0 + (v.step == 1 ? static_cast<int>(threadIdx.x) / 16 + 16 * e : static_cast<int>(threadIdx.x) % 64);
+      x[e] = kk < depth && r < v.rows ? v.p[r * v.ld + kk * v.step] : TA(0);
+    }
+  };
+  auto put = [&](const View<TA>& v, TA (&to)[kDepth][kPitch], const TA (&x)[4]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (v.step == 1) to[threadIdx.x % 16][threadIdx.x / 16 + 16 * e] = x[e];
+      else to[threadIdx.x / 64 + 4 * e][threadIdx.x % 64] = x[e];
+    }
+  };
+#pragma unroll
+  for (int t = 0; t < 4; ++t) acc[t] = typename Mma<TA>::acc_t{0, 0, 0, 0};
+  for (int k = 0; k < depth; k += kDepth) {
+    TA x[4], y[4];
+    load(p, i0, k, ps, x);
+    load(q, j0, k, qs, y);
+    __syncthreads();
+    put(p, ps, x);
+    put(q, qs, y);
+    __syncthreads();
+#pragma unroll
+    for (int s = 0; s < kDepth / 4; ++s) {
+      const TA a = ps[4 * s + lane / 16][16 * wave + (lane & 15)];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) acc[t] = Mma<TA>::mma(a, qs[4 * s + lane / 16][16 * t + (lane & 15)], acc[t]);
+    }
+  }
+}
+
+enum Phase { kS, kP, kX };
+
+// The three products of a step: S from X; P from S; the next X from P and X (last: into the results).
+template <typename TA, int kPhase>
+__global__ __launch_bounds__(kThreads) void product_kernel(const Item* __restrict__ items, int n, const Step st, bool last, const TA* __restrict__ X,
+                                                           TA* __restrict__ next, TA* __restrict__ S, TA* __restrict__ P) {
+  __shared__ TA ps[kDepth][kPitch], qs[kDepth][kPitch];
+  constexpr int kind = kPhase == kX ? kProduct : kGram;
+  const int lane = threadIdx.x & (kLanes - 1), wave = threadIdx.x / kLanes;
+  const Item& it = items[item_of(items, n, kind, blockIdx.x)];
+  const bool turned = it.rows > it.cols;
+  const int m = turned ? it.cols : it.rows, l = turned ? it.rows : it.cols;   // X as m x l: element (i, k) at i * si + k * sk
+  const int64_t si = turned ? 1 : it.cols, sk = turned ? it.cols : 1;
+  const int columns = kPhase == kX ? l : m;
+  const int row_tiles = (m + kTile - 1) / kTile, col_tiles = (columns + kTile - 1) / kTile;
+  const int64_t unit = blockIdx.x - it.unit[kind], per = static_cast<int64_t>(row_tiles) * col_tiles, matrix = unit / per;
+  const int tile = static_cast<int>(unit % per), i0 = tile / col_tiles * kTile, j0 = tile % col_tiles * kTile;
+  const int64_t x0 = it.x + matrix * m * l, s0 = it.s + matrix * m * m;
+  typename Mma<TA>::acc_t acc[4];
+  if constexpr (kPhase == kS) {
+    const View<TA> v{X + x0, si, sk, m, l};
+    product<TA>(v, v, i0, j0, ps, qs, acc);
+  } else if constexpr (kPhase == kP) {
+    const View<TA> v{S + s0, m, 1, m, m};
+    product<TA>(v, v, i0, j0, ps, qs, acc);
+  } else {
+    const View<TA> p{P + s0, m, 1, m, m}, x{X + x0, sk, si, l, m};
+    product<TA>(p, x, i0, j0, ps, qs, acc);
+  }
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const int i = i0 + 16 * wave + Mma<TA>::row(lane, r);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const int j = j0 + 16 * t + (lane & 15);
+      if (i >= m || j >= columns) continue;
+      if constexpr (kPhase == kS) {
+        S[s0 + static_cast<int64_t>(i) * m + j] = acc[t][r];
+      } else if constexpr (kPhase == kP) {
+        const int64_t at = s0 + static_cast<int64_t>(i) * m + j;
+        P[at] = static_cast<TA>(st.b) * S[at] + static_cast<TA>(st.c) * acc[t][r];
+      } else {
+        const int64_t at = i * si + j * sk;
+        const TA x = static_cast<TA>(st.a) * X[x0 + at] + acc[t][r];
+        if (last) finish(it, st, matrix * m * l + at, x); else next[x0 + at] = x;
+      }
+    }
+  }
+}
+
+// ---- host side
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// The list in two parts, fp32 (and bfloat16) tensors and fp64 ones, and where everything lies in the workspace.
+struct Part {
+  std::vector<Item> items;
+  int64_t units[kKinds] = {0, 0, 0};
+  int64_t x = 0, s = 0;            // elements of X and of S
+  size_t elem = 4;
+  size_t at_items = 0, at_partial = 0, at_x[2] = {0, 0}, at_s = 0, at_p = 0;
+};
+struct Layout {
+  Part part[2];
+  size_t bytes = 0;
+};
+
+Layout layout_of(int64_t n, const ou_tensor* tensors, int steps) {
+  Layout l;
+  l.part[1].elem = 8;
+  for (int64_t i = 0; i < n; ++i) {
+    const ou_tensor& t = tensors[i];
+    if (t.count == 0) continue;
+    Part& p = l.part[t.dtype == SC_F64];
+    const int64_t m = std::min(t.rows, t.cols), k = std::max(t.rows, t.cols);
+    Item it{t.grad, t.momentum, t.weight, t.update, t.scale, t.count, p.x, p.s, {p.units[0], p.units[1], p.units[2]}, t.rows, t.cols, t.dtype, 0};
+    p.items.push_back(it);
+    p.units[kChunks] += t.count * ceil_div(m * k, kChunk);
+    p.units[kGram] += t.count * ceil_div(m, kTile) * ceil_div(m, kTile);
+    p.units[kProduct] += t.count * ceil_div(m, kTile) * ceil_div(k, kTile);
+    p.x += t.count * m * k;
+    p.s += t.count * m * m;
+  }
+  size_t at = 0;
+  auto room = [&](size_t bytes) {
+    const size_t from = at;
+    at += align_up(bytes, 256);
+    return from;
+  };
+  for (Part& p : l.part) {
+    if (p.items.empty()) continue;
+    p.at_items = room(p.items.size() * sizeof(Item));
+    p.at_partial = room(p.units[kChunks] * sizeof(double));
+    p.at_x[0] = room(p.x * p.elem);
+    if (steps > 0) {
+      p.at_x[1] = room(p.x * p.elem);
+      p.at_s = room(p.s * p.elem);
+      p.at_p = room(p.s * p.elem);
+    }
+  }
+  l.bytes = std::max<size_t>(at, 256);
+  return l;
+}
+
+// The largest |a x + b x^3 + c x^5| of 0 <= x <= top.
+double growth(const ou_config* c, double top) {
+  auto f = [&](double x) { return std::fabs(x * (c->a + x * x * (c->b + x * x * c->c))); };
+  double most = f(top);
+  // where the derivative a + 3 b y + 5 c y^2, y = x^2, is zero
+  const double q = 5 * c->c, p = 3 * c->b, d = p * p - 4 * q * c->a;
+  double roots[3] = {-1, -1, -1};
+  if (q != 0 && d >= 0) {
+    roots[0] = (-p + std::sqrt(d)) / (2 * q);
+    roots[1] = (-p - std::sqrt(d)) / (2 * q);
+  }
+  if (p != 0) roots[2] = -c->a / p;   // (without c; with it an ordinary point inside, which does no harm)
+  for (double y : roots)
+    if (y > 0 && y < top * top) most = std::max(most, f(std::sqrt(y)));
+  return most;
+}
+
+sc_status check(const char* fn, const ou_config* cfg, int64_t n, const ou_tensor* tensors) {
+  auto bad = [&](sc_status st, const std::string& what) { return set_error(st, std::string(fn) + ": " + what); };
+  if (!cfg) return bad(SC_ERR_INVALID_ARG, "cfg is NULL");
+  if (cfg->struct_size != static_cast<int32_t>(sizeof(ou_config)))
+    return bad(SC_ERR_INVALID_ARG, "struct_size does not match this library's ou_config");
+  if (cfg->steps < 0) return bad(SC_ERR_INVALID_ARG, "steps < 0");
+  if (cfg->steps > OU_MAX_STEPS) return bad(SC_ERR_UNSUPPORTED, "steps above OU_MAX_STEPS");
+  if (cfg->flags & ~static_cast<uint32_t>(OU_NESTEROV)) return bad(SC_ERR_INVALID_ARG, "unknown flags");
+  for (double v : {cfg->a, cfg->b, cfg->c, cfg->momentum, cfg->rate, cfg->decay})
+    if (!std::isfinite(v)) return bad(SC_ERR_INVALID_ARG, "a coefficient, momentum, rate or decay is not finite");
+  if (!(cfg->eps > 0) || !std::isfinite(cfg->eps)) return bad(SC_ERR_INVALID_ARG, "eps not above 0 or not finite");
+  double top = 1;
+  for (int i = 0; i < cfg->steps; ++i) {
+    top = growth(cfg, top);
+    if (!(top <= OU_MAX_GROWTH)) return bad(SC_ERR_UNSUPPORTED, "with these coefficients the iteration grows beyond OU_MAX_GROWTH");
+  }
+  if (n < 0) return bad(SC_ERR_INVALID_ARG, "n_tensors < 0");
+  if (n > OU_MAX_TENSORS) return bad(SC_ERR_UNSUPPORTED, "more than OU_MAX_TENSORS tensors");
+  if (n > 0 && !tensors) return bad(SC_ERR_INVALID_ARG, "tensors is NULL");
+  int64_t total = 0;
+  for (int64_t i = 0; i < n; ++i) {
+    const ou_tensor& t = tensors[i];
+    const char* what = nullptr;
+    if (t.dtype != SC_F32 && t.dtype != SC_F64 && t.dtype != SC_BF16) what = "bad dtype";
+    else if (t.reserved != 0) what = "reserved is not 0";
+    else if (t.rows < 1 || t.cols < 1) what = "rows or cols < 1";
+    else if (t.count < 0) what = "count < 0";
+    else if (!std::isfinite(t.scale)) what = "scale is not finite";
+    else if (t.count > 0 && !t.grad) what = "grad is NULL";
+    else if (t.count > 0 && !t.weight && !t.update) what = "weight and update are both NULL";
+    const size_t narrow = t.dtype == SC_F64 ? 8 : t.dtype == SC_F32 ? 4 : 2, wide = t.dtype == SC_F64 ? 8 : 4;
+    if (!what && (misaligned(t.grad, narrow) || misaligned(t.update, narrow) || misaligned(t.momentum, wide) || misaligned(t.weight, wide)))
+      what = "pointer not aligned to its element";
+    if (what) return bad(SC_ERR_INVALID_ARG, "tensor " + std::to_string(i) + ": " + what);
+    if (t.rows > OU_MAX_SIDE || t.cols > OU_MAX_SIDE) return bad(SC_ERR_UNSUPPORTED, "tensor " + std::to_string(i) + ": rows or cols above OU_MAX_SIDE");
+    const int64_t tiles = ceil_div(t.rows, kTile) * ceil_div(t.cols, kTile);
+    if (t.count > (OU_MAX_TILES - total) / tiles) return bad(SC_ERR_UNSUPPORTED, "more than OU_MAX_TILES tiles");
+    total += t.count * tiles;
+  }
+  return SC_OK;
+}
+
+template <typename TA>
+hipError_t run(const Part& p, const ou_config* cfg, const Step& st, char* base, hipStream_t stream) {
+  const int n = static_cast<int>(p.items.size());
+  if (n == 0) return hipSuccess;
+  Item* const items = reinterpret_cast<Item*>(base + p.at_items);
+  for (int first = 0; first < n; first += kSent) {
+    Sent sent{};
+    sent.first = first;
+    sent.count = std::min(kSent, n - first);
+    std::copy_n(p.items.begin() + first, sent.count, sent.item);
+    hipLaunchKernelGGL(send_kernel, dim3(1), dim3(kLanes), 0, stream, sent, items);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  double* const partial = reinterpret_cast<double*>(base + p.at_partial);
+  TA* X[2] = {reinterpret_cast<TA*>(base + p.at_x[0]), reinterpret_cast<TA*>(base + p.at_x[1])};
+  TA* const S = reinterpret_cast<TA*>(base + p.at_s);
+  TA* const P = reinterpret_cast<TA*>(base + p.at_p);
+  auto grid = [&](Kind k) { return dim3(static_cast<unsigned>(p.units[k])); };
+  hipLaunchKernelGGL(momentum_kernel<TA>, grid(kChunks), dim3(kThreads), 0, stream, items, n, st, X[0], partial);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(normalise_kernel<TA>, grid(kChunks), dim3(kThreads), 0, stream, items, n, st, cfg->steps == 0, X[0], partial);
+  e = hipGetLastError();
+  for (int i = 0; i < cfg->steps && e == hipSuccess; ++i) {
+    const bool last = i + 1 == cfg->steps;
+    const TA* const x = X[i & 1];
+    TA* const next = X[(i + 1) & 1];
+    hipLaunchKernelGGL((product_kernel<TA, kS>), grid(kGram), dim3(kThreads), 0, stream, items, n, st, last, x, next, S, P);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((product_kernel<TA, kP>), grid(kGram), dim3(kThreads), 0, stream, items, n, st, last, x, next, S, P);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((product_kernel<TA, kX>), grid(kProduct), dim3(kThreads), 0, stream, items, n, st, last, x, next, S, P);
+    e = hipGetLastError();
+  }
+  return e;
+}
+
+}  // namespace
+}  // namespace ou
+
+extern "C" {
+
+sc_status ou_workspace_bytes(const ou_config* cfg, int64_t n_tensors, const ou_tensor* tensors, size_t* bytes) {
+  using namespace ou;
+  const sc_status st = check("ou_workspace_bytes", cfg, n_tensors, tensors);
+  if (st != SC_OK) return st;
+  if (!bytes) return set_error(SC_ERR_INVALID_ARG, "ou_workspace_bytes: bytes is NULL");
+  try {
+    *bytes = layout_of(n_tensors, tensors, cfg->steps).bytes;
+  } catch (const std::bad_alloc&) {
+    return set_error(SC_ERR_ALLOC, "ou_workspace_bytes: out of host memory");
+  }
+  return SC_OK;
+}
+
+sc_status ou_step(const ou_config* cfg, int64_t n_tensors, const ou_tensor* tensors, void* workspace, size_t workspace_bytes,
+                  void* hip_stream) {
+  using namespace ou;
+  const sc_status st = check("ou_step", cfg, n_tensors, tensors);
+  if (st != SC_OK) return st;
+  try {
+    const Layout l = layout_of(n_tensors, tensors, cfg->steps);
+    if (l.part[0].items.empty() && l.part[1].items.empty()) return SC_OK;
+    if (!workspace || workspace_bytes < l.bytes)
+      return set_error(SC_ERR_WORKSPACE, "ou_step: workspace missing or smaller than ou_workspace_bytes()");
+    if (misaligned(workspace, 256)) return set_error(SC_ERR_WORKSPACE, "ou_step: workspace not 256-byte aligned");
+    DeviceGuard guard(cfg->device);
+    if (!guard.ok) return set_error(SC_ERR_HIP, "ou_step: cannot make cfg->device current");
+    const Step step{cfg->a, cfg->b, cfg->c, cfg->momentum, cfg->rate, 1 - cfg->rate * cfg->decay, cfg->eps, (cfg->flags & OU_NESTEROV) != 0};
+    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    char* const base = static_cast<char*>(workspace);
+    hipError_t e = run<float>(l.part[0], cfg, step, base, stream);
+    if (e == hipSuccess) e = run<double>(l.part[1], cfg, step, base, stream);
+    if (e != hipSuccess) return set_error(SC_ERR_HIP, std::string("ou_step: kernel launch: ") + hipGetErrorString(e));
+  } catch (const std::bad_alloc&) {
+    return set_error(SC_ERR_ALLOC, "ou_step: out of host memory");
+  }
+  return SC_OK;
+}
+
+}  // extern "C"
