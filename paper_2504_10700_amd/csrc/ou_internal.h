@@ -1,6 +1,8 @@
-// What the kernels of the orthogonalised update (include/ou.h) share: the list of tensors as the device has it.
+// What the kernels of the orthogonalised update (include/ou.h) share: the list of tensors as the device has it, the operations on elements.
 #pragma once
 #include <hip/hip_runtime.h>
+
+#include <vector>
 
 #include "sc_internal.h"
 #include "../../include/ou.h"
@@ -12,10 +14,11 @@ using sc::kLanes;
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kLanes;
+constexpr int kChunk = 4096;   // elements of a chunk of the first pass
 
-// A tensor of the list.  Work is dealt out in units (chunks of elements, tiles of a product); `unit[k]` is the number of units of kind k in the tensors
-// before this one.
-enum Kind { kChunks, kGram, kProduct, kKinds };
+// A matrix as the iteration sees it is m x l, m <= l: the tensor's matrix, or its transpose where rows > cols.  Work is dealt out in units; `unit[k]` is
+// the number of units of kind k in the tensors before this one.
+enum Kind { kChunks, kBlocks, kGram, kProduct, kKinds };
 
 struct Item {
   const void* grad;
@@ -23,17 +26,43 @@ struct Item {
   void* weight;
   void* update;
   double scale;
-  int64_t count;
-  int64_t x, s;            // where X and S begin in their buffers, in elements
   int64_t unit[kKinds];
+  int64_t x, s;            // where the tensor's X and S begin in their buffers, in elements
+  int64_t px, pt, ps;      // and the parts of X, of X transposed, of S and P
   int32_t rows, cols, dtype, pad;
 };
-constexpr int kSent = 36;  // items of one launch's kernel arguments
+constexpr int kSent = 31;  // items of one launch's kernel arguments
 struct Sent {
   int32_t first, count;
   Item item[kSent];
 };
 static_assert(sizeof(Sent) <= 4000, "the kernel arguments hold 4 KB");
+
+struct Step {
+  double a, b, c, mu, rate, keep, eps;   // keep: 1 - rate * decay
+  int nesterov;
+};
+
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Tensors of one way through the kernels.
+struct Part {
+  std::vector<Item> items;
+  int64_t units[kKinds] = {0, 0, 0, 0};
+  int64_t x = 0, s = 0, px = 0, pt = 0, ps = 0;
+  size_t at_items = 0, at_partial = 0, at_x = 0;
+  size_t at[6] = {};   // the way's other buffers
+};
+
+// What workspace there is: room(bytes) is the offset of the next piece.
+struct Room {
+  size_t bytes = 0;
+  size_t operator()(size_t n) {
+    const size_t from = bytes;
+    bytes += align_up(n, 256);
+    return from;
+  }
+};
 
 // The last of items[0..n) whose first unit of that kind is not beyond `unit` (tensors without units share it with the next one).
 __device__ __forceinline__ int item_of(const Item* __restrict__ items, int n, int kind, int64_t unit) {
@@ -44,5 +73,58 @@ __device__ __forceinline__ int item_of(const Item* __restrict__ items, int n, in
   }
   return lo;
 }
+
+__device__ __forceinline__ int64_t chunks_of(int64_t elements) { return (elements + kChunk - 1) / kChunk; }
+
+// U of an element from its gradient and the momentum that the step leaves.
+template <typename TA>
+__device__ __forceinline__ TA direction(TA g, TA m, TA mu, bool nesterov) { return nesterov ? g + mu * m : m; }
+
+// G of an element in the arithmetic type.
+template <typename TA>
+__device__ __forceinline__ TA gradient(const Item& it, int64_t at) {
+  if constexpr (sizeof(TA) == 8) return static_cast<const double*>(it.grad)[at];
+  else return it.dtype == SC_BF16 ? static_cast<float>(static_cast<const __bf16*>(it.grad)[at]) : static_cast<const float*>(it.grad)[at];
+}
+
+// A finished element of X: into the update and the weight.
+template <typename TA>
+__device__ __forceinline__ void finish(const Item& it, const Step& st, int64_t at, TA x) {
+  if (it.update) {
+    if (sizeof(TA) == 4 && it.dtype == SC_BF16) static_cast<__bf16*>(it.update)[at] = static_cast<__bf16>(static_cast<float>(x));
+    else static_cast<TA*>(it.update)[at] = x;
+  }
+  if (it.weight) {
+    TA* const w = static_cast<TA*>(it.weight) + at;
+    *w = static_cast<TA>(st.keep) * *w - static_cast<TA>(st.rate * it.scale) * x;
+  }
+}
+
+__device__ __forceinline__ double workgroup_sum(double v, double* slots) {
+#pragma unroll
+  for (int d = 32; d > 0; d /= 2) v += __shfl_xor(v, d);
+  if ((threadIdx.x & 63) == 0) slots[threadIdx.x / 64] = v;
+  __syncthreads();
+  double s = slots[0];
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) s += slots[w];
+  __syncthreads();
+  return s;
+}
+
+// 1 / (|U| + eps) of a matrix whose chunks left their sums of squares in partial[0..n).
+__device__ __forceinline__ double down_of(const double* __restrict__ partial, int64_t n, double eps, double* slots) {
+  double sum = 0;
+  for (int64_t i = threadIdx.x; i < n; i += kThreads) sum += partial[i];
+  return 1.0 / (sqrt(workgroup_sum(sum, slots)) + eps);
+}
+
+// The largest |a x + b x^3 + c x^5| of 0 <= x <= top: what the largest singular value can be after a step that began with top.
+double growth(const ou_config* c, double top);
+
+// fp32 matrices of any size, on parts (ou_parts.hip).  place: the units and places of a tensor's matrices; layout: the buffers; run: from the sums of squares on.
+void parts_place(Part& p, Item& it, int64_t count);
+void parts_layout(Part& p, Room& room, int steps);
+hipError_t parts_run(const Part& p, const ou_config* cfg, const Step& st, char* base, hipStream_t stream);
 
 }  // namespace ou

@@ -1,0 +1,437 @@
+// The products of the orthogonalised update on the fp16 matrix cores, for matrices of any size.
+//
+// No element of X, S = X X^T or P = b S + c S S is larger than the largest singular value can be, which the host knows for every step.
+// So an fp32 value v, times a power of two that brings that bound to at most 2^14, is the sum of two fp16 values h + l (h rounded from it, l from what is
+// left): 22 bits of it down to 2^-16 of the bound, and an error of 2^-39 of the bound below, where it is lost in the matrix's norm.  A product is
+// h h' + h l' + l h' (l l' is below 2^-22 of it): three instructions where bfloat16 parts take six and fp32 instructions the time of 16.
+// An instruction cuts off what is below the last bit of the sum it adds to, so a sum goes no further than kFlush indices and then joins an fp32 sum.
+//
+// Every product is one of rows with rows, sum over k of A[i][k] B[j][k], both operands contiguous in k: S from X and X, P from S and S (symmetric), the
+// next X from P and X transposed.  So the epilogues leave X in both orientations, split once where it is made and not where it is used.  Of S and P the
+// tiles on and below the diagonal are computed and mirrored.
+//
+// A workgroup: 128 x 128, four waves of 64 x 64; 32 reduced indices of both operands' parts (32 KB) go from memory to LDS without passing registers while
+// the 32 before are multiplied.  A row's four pieces of 16 bytes stand at places that differ between rows (swizzle), against bank conflicts.
+#include <algorithm>
+#include <cmath>
+
+#include "ou_internal.h"
+
+namespace ou {
+namespace {
+
+typedef _Float16 H8 __attribute__((ext_vector_type(8)));
+typedef float F16 __attribute__((ext_vector_type(16)));
+typedef float F4 __attribute__((ext_vector_type(4)));
+typedef float F4Loose __attribute__((ext_vector_type(4), aligned(4)));
+
+constexpr int kTile = 128, kDepth = 32, kFlush = 128;
+constexpr int kPad = 32;                  // rows of the parts in memory are multiples of this
+constexpr int kPlane = kTile * kDepth;    // elements of one part of one operand in LDS
+constexpr int kStage = 4 * kPlane;        // A h, A l, B h, B l
+constexpr int kPitch = 36;                // floats of a row of a wave's 32 x 32 in LDS
+constexpr int kXcds = 8;
+
+__host__ __device__ constexpr int64_t padded(int64_t n) { return (n + kPad - 1) / kPad * kPad; }
+
+// Buffers.  Parts: [h, l][rows][padded columns] of each matrix.
+struct Buffers {
+  float* X;             // [m][l]
+  float* S;             // [m][padded(m)], the tiles on and below the diagonal
+  _Float16* x;          // X
+  _Float16* t;          // X transposed
+  _Float16* next;       // the next X transposed
+  _Float16* s;
+  _Float16* p;
+};
+
+// Powers of two of a step.
+struct Scales {
+  float up;      // values that the phase makes to parts
+  float down;    // sums of parts to values
+};
+
+__device__ __forceinline__ void split(float v, _Float16& h, _Float16& l) {
+  h = static_cast<_Float16>(v);
+  l = static_cast<_Float16>(v - static_cast<float>(h));
+}
+
+// Sixteen consecutive values of a row, times `up`, to both parts; those from `inside` on are zeros.  (`to` is a multiple of 16 in a row of a multiple of 32.)
+__device__ __forceinline__ void put_parts(const float (&v)[16], float up, int inside, _Float16* to, int64_t part) {
+#pragma unroll
+  for (int b = 0; b < 16; b += 8) {
+    H8 h, l;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      _Float16 x, y;
+      split(b + i < inside ? v[b + i] * up : 0.f, x, y);
+      h[i] = x;
+      l[i] = y;
+    }
+    *reinterpret_cast<H8*>(to + b) = h;
+    *reinterpret_cast<H8*>(to + part + b) = l;
+  }
+}
+
+// A 64 x 64 block of X = U / (norm + eps): X, and its parts in both orientations.  last: no steps follow.
+__global__ __launch_bounds__(kThreads) void normalise_kernel(const Item* __restrict__ items, int n, const Step st, bool last, const Buffers buf, float up,
+                                                             const double* __restrict__ partial) {
+  __shared__ double slots[kWaves];
+  __shared__ float block[64][65];
+  const Item& it = items[item_of(items, n, kBlocks, blockIdx.x)];
+  const bool turned = it.rows > it.cols;
+  const int m = turned ? it.cols : it.rows, l = turned ? it.rows : it.cols;
+  const int64_t size = static_cast<int64_t>(m) * l, per = chunks_of(size);
+  const int col_blocks = (it.cols + 63) / 64, row_blocks = (it.rows + 63) / 64;
+  const int64_t unit = blockIdx.x - it.unit[kBlocks], blocks = static_cast<int64_t>(col_blocks) * row_blocks, matrix = unit / blocks;
+  const int b = static_cast<int>(unit % blocks), r0 = b / col_blocks * 64, c0 = b % col_blocks * 64;
+  const double down = down_of(partial + it.unit[kChunks] + matrix * per, per, st.eps, slots);
+  const float mu = static_cast<float>(st.mu);
+  for (int i = threadIdx.x; i < 64 * 64; i += kThreads) {
+    const int r = i / 64, c = i % 64;
+    float x = 0;
+    if (r0 + r < it.rows && c0 + c < it.cols) {
+      const int64_t at = matrix * size + static_cast<int64_t>(r0 + r) * it.cols + c0 + c;
+      float u = gradient<float>(it, at);
+      if (it.momentum) u = direction(u, static_cast<const float*>(it.momentum)[at], mu, st.nesterov);
+      x = static_cast<float>(static_cast<double>(u) * down);
+      if (last) finish(it, st, at, x);
+    }
+    if (turned) block[c][r] = x; else block[r][c] = x;
+  }
+  if (last) return;
+  __syncthreads();
+  const int i0 = turned ? c0 : r0, j0 = turned ? r0 : c0;   // of the m x l matrix
+  for (int i = threadIdx.x; i < 64 * 64; i += kThreads)
+    if (i0 + i / 64 < m && j0 + i % 64 < l) buf.X[it.x + matrix * size + static_cast<int64_t>(i0 + i / 64) * l + j0 + i % 64] = block[i / 64][i % 64];
+  const int64_t lp = padded(l), mp = padded(m);
+  const int row = threadIdx.x / 4, from = threadIdx.x % 4 * 16;
+  float v[16];
+  if (i0 + row < m && j0 + from < lp) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = block[row][from + i];
+    put_parts(v, up, l - j0 - from, buf.x + it.px + 2 * matrix * m * lp + (i0 + row) * lp + j0 + from, m * lp);
+  }
+  if (j0 + row < l && i0 + from < mp) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = block[from + i][row];
+    put_parts(v, up, m - i0 - from, buf.t + it.pt + 2 * matrix * l * mp + (j0 + row) * mp + i0 + from, l * mp);
+  }
+}
+
+// Tile t of those on and below the diagonal of rows x rows tiles.  Eight rows of tiles at a time, column after column, so that what runs at the same time on
+// an XCD shares its operands.
+constexpr int kGroup = 8;
+__device__ __forceinline__ void lower_tile(int t, int rows, int& i, int& j) {
+  int g = static_cast<int>((sqrtf(16.f + 128.f * t) - 4.f) / 64.f);
+  while (32 * (g + 1) * (g + 1) + 4 * (g + 1) <= t) ++g;
+  while (32 * g * g + 4 * g > t) --g;
+  t -= 32 * g * g + 4 * g;
+  const int first = kGroup * g, high = min(kGroup, rows - first);
+  if (t < first * high) {
+    j = t / high;
+    i = first + t % high;
+    return;
+  }
+  t -= first * high;
+  int r = 0;
+  while ((r + 1) * (r + 2) / 2 <= t) ++r;
+  i = first + r;
+  j = first + t - r * (r + 1) / 2;
+}
+__device__ __forceinline__ void any_tile(int t, int rows, int cols, int& i, int& j) {
+  const int g = t / (kGroup * cols), first = kGroup * g, high = min(kGroup, rows - first);
+  t -= kGroup * cols * g;
+  j = t / high;
+  i = first + t % high;
+}
+
+__device__ __forceinline__ int swizzle(int row) { return ((row >> 1) & 3) ^ ((row >> 3) & 1); }
+
+// 128 rows (clamped to the last) of one part, 32 reduced indices, to LDS: eight requests of a wave, 16 rows each.
+__device__ __forceinline__ void load_plane(const _Float16* __restrict__ from, const unsigned (&offset)[8], _Float16* to) {
+#pragma unroll
+  for (int q = 0; q < 8; ++q) {
+    const auto* const g = reinterpret_cast<const __attribute__((address_space(1))) unsigned*>(
+        reinterpret_cast<uintptr_t>(reinterpret_cast<const char*>(from) + offset[q]));
+    __builtin_amdgcn_global_load_lds(g, reinterpret_cast<__attribute__((address_space(3))) unsigned*>(reinterpret_cast<uintptr_t>(to + q * 16 * kDepth)), 16, 0, 0);
+  }
+}
+
+__device__ __forceinline__ void wave_sync() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+enum Phase { kS, kP, kX };
+
+template <int kPhase>
+__global__ __launch_bounds__(kThreads, 2) void product_kernel(const Item* __restrict__ items, int n, const Step st, bool last, const Buffers buf, const Scales sc,
+                                                              int total) {
+  __shared__ __attribute__((aligned(16))) _Float16 lds[2 * kStage];
+  constexpr int kind = kPhase == kX ? kProduct : kGram;
+  const int per_xcd = (total + kXcds - 1) / kXcds;
+  const int u = static_cast<int>(blockIdx.x) % kXcds * per_xcd + blockIdx.x / kXcds;
+  if (u >= total) return;
+  const Item& it = items[item_of(items, n, kind, u)];
+  const bool turned = it.rows > it.cols;
+  const int m = turned ? it.cols : it.rows, l = turned ? it.rows : it.cols;
+  const int64_t mp = padded(m), lp = padded(l);
+  const int tiles_m = (m + kTile - 1) / kTile, tiles_l = (l + kTile - 1) / kTile;
+  const int per = kPhase == kX ? tiles_m * tiles_l : tiles_m * (tiles_m + 1) / 2;
+  const int unit = static_cast<int>(u - it.unit[kind]), matrix = unit / per;
+  int ti, tj;
+  if constexpr (kPhase == kX) any_tile(unit % per, tiles_m, tiles_l, ti, tj);
+  else lower_tile(unit % per, tiles_m, ti, tj);
+  const int i0 = ti * kTile, j0 = tj * kTile;
+  const int lane = threadIdx.x & (kLanes - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
+
+  // operands: rows of A and of B
+  const int64_t ld = kPhase == kS ? lp : mp;
+  const _Float16* a;
+  const _Float16* b;
+  int64_t a_part, b_part;
+  int b_rows;
+  if constexpr (kPhase == kS) {
+    a = b = buf.x + it.px + 2 * matrix * m * lp;
+    a_part = b_part = m * lp;
+    b_rows = m;
+  } else if constexpr (kPhase == kP) {
+    a = b = buf.s + it.ps + 2 * matrix * m * mp;
+    a_part = b_part = m * mp;
+    b_rows = m;
+  } else {
+    a = buf.p + it.ps + 2 * matrix * m * mp;
+    a_part = m * mp;
+    b = buf.t + it.pt + 2 * matrix * l * mp;
+    b_part = l * mp;
+    b_rows = l;
+  }
+  const bool of_b = wave & 2;
+  const int row0 = of_b ? j0 : i0, left = (of_b ? b_rows : m) - row0;
+  const _Float16* from = (of_b ? b + (wave & 1) * b_part : a + (wave & 1) * a_part) + row0 * ld;
+  unsigned offset[8];
+#pragma unroll
+  for (int q = 0; q < 8; ++q)
+    offset[q] = 2u * (static_cast<unsigned>(min(16 * q + lane / 4, left - 1)) * static_cast<unsigned>(ld) + 8u * ((lane % 4) ^ swizzle(lane / 4)));
+  const int stages = static_cast<int>(ld / kDepth);
+  _Float16* const mine = lds + wave * kPlane;
+  const int wi = wave / 2 * 64, wj = wave % 2 * 64;
+
+  F16 sum[2][2], part[2][2];
+#pragma unroll
+  for (int x = 0; x < 2; ++x)
+#pragma unroll
+    for (int y = 0; y < 2; ++y)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sum[x][y][r] = part[x][y][r] = 0;
+
+  load_plane(from, offset, mine);
+  for (int t = 0; t < stages; ++t) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (t + 1 < stages) {
+      from += kDepth;
+      load_plane(from, offset, mine + ((t + 1) & 1) * kStage);
+    }
+    const _Float16* const here = lds + (t & 1) * kStage;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      H8 x[2][2], y[2][2];   // [tile][part]
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          const int r = e * 32 + (lane & 31), piece = ((2 * s + lane / 32) ^ swizzle(r)) * 8;
+          x[e][q] = *reinterpret_cast<const H8*>(here + q * kPlane + (wi + r) * kDepth + piece);
+          y[e][q] = *reinterpret_cast<const H8*>(here + (2 + q) * kPlane + (wj + r) * kDepth + piece);
+        }
+#pragma unroll
+      for (int q = 0; q < 3; ++q)   // l h, h l, h h
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+          for (int f = 0; f < 2; ++f) part[e][f] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[e][q == 0], y[f][q == 1], part[e][f], 0, 0, 0);
+    }
+    if ((t + 1) % (kFlush / kDepth) == 0 || t + 1 == stages) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int f = 0; f < 2; ++f) {
+          sum[e][f] += part[e][f];
+#pragma unroll
+          for (int r = 0; r < 16; ++r) part[e][f][r] = 0;
+        }
+    }
+  }
+
+  // results, 32 x 32 at a time through the wave's corner of LDS: row by row, then column by column
+  __syncthreads();
+  float* const corner = reinterpret_cast<float*>(lds) + wave * 32 * kPitch;
+  const int row = lane / 2, begin = lane % 2 * 16;
+  const bool mirrored = kPhase != kX && ti != tj;
+  const int columns = kPhase == kX ? l : m;
+#pragma unroll
+  for (int e = 0; e < 2; ++e)
+#pragma unroll
+    for (int f = 0; f < 2; ++f) {
+      const int ib = i0 + wi + 32 * e, jb = j0 + wj + 32 * f;
+      if (ib >= m || jb >= columns) continue;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) corner[(8 * (r / 4) + 4 * (lane / 32) + r % 4) * kPitch + (lane & 31)] = sum[e][f][r] * sc.down;
+      wave_sync();
+      float v[16];
+#pragma unroll
+      for (int r = 0; r < 16; r += 4) {
+        const F4 x = *reinterpret_cast<const F4*>(corner + row * kPitch + begin + r);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[r + k] = x[k];
+      }
+      const int i = ib + row, j = jb + begin;
+      if (i < m) {
+        if constexpr (kPhase == kX) {
+          const int64_t x0 = it.x + (static_cast<int64_t>(matrix) * m + i) * l + j;
+          float x[16];
+          if (j + 16 <= l) {
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+              const F4 w = *reinterpret_cast<const F4Loose*>(buf.X + x0 + r);
+#pragma unroll
+              for (int k = 0; k < 4; ++k) x[r + k] = w[k];
+            }
+          } else {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) x[r] = j + r < l ? buf.X[x0 + r] : 0.f;
+          }
+          const float ca = static_cast<float>(st.a);
+#pragma unroll
+          for (int r = 0; r < 16; ++r) v[r] = ca * x[r] + v[r];
+          if (last) {
+            if (!turned) {
+#pragma unroll
+              for (int r = 0; r < 16; ++r)
+                if (j + r < l) finish(it, st, (static_cast<int64_t>(matrix) * m + i) * l + j + r, v[r]);
+            }
+          } else {
+            if (j + 16 <= l) {
+#pragma unroll
+              for (int r = 0; r < 16; r += 4) *reinterpret_cast<F4Loose*>(buf.X + x0 + r) = F4{v[r], v[r + 1], v[r + 2], v[r + 3]};
+            } else {
+#pragma unroll
+              for (int r = 0; r < 16; ++r)
+                if (j + r < l) buf.X[x0 + r] = v[r];
+            }
+            put_parts(v, sc.up, l - j, buf.x + it.px + 2 * matrix * m * lp + i * lp + j, m * lp);
+          }
+        } else {
+          float* const S = buf.S + it.s + (matrix * m + i) * mp + j;
+          if constexpr (kPhase == kS) {
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) *reinterpret_cast<F4*>(S + r) = F4{v[r], v[r + 1], v[r + 2], v[r + 3]};
+          } else {
+            const float cb = static_cast<float>(st.b), cc = static_cast<float>(st.c);
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+              const F4 x = *reinterpret_cast<const F4*>(S + r);
+#pragma unroll
+              for (int k = 0; k < 4; ++k) v[r + k] = cb * x[k] + cc * v[r + k];
+            }
+          }
+          put_parts(v, sc.up, m - j, (kPhase == kS ? buf.s : buf.p) + it.ps + 2 * matrix * m * mp + i * mp + j, m * mp);
+        }
+      }
+      if (kPhase == kX || mirrored) {
+        if constexpr (kPhase != kS) {   // what the row pass made of the sums
+          wave_sync();
+#pragma unroll
+          for (int r = 0; r < 16; r += 4) *reinterpret_cast<F4*>(corner + row * kPitch + begin + r) = F4{v[r], v[r + 1], v[r + 2], v[r + 3]};
+          wave_sync();
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) v[r] = corner[(begin + r) * kPitch + row];
+        const int jc = jb + row, ic = ib + begin;
+        if (jc < columns) {
+          if constexpr (kPhase == kX) {
+            if (last) {
+              if (turned) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                  if (ic + r < m) finish(it, st, (static_cast<int64_t>(matrix) * l + jc) * m + ic + r, v[r]);
+              }
+            } else {
+              put_parts(v, sc.up, m - ic, buf.next + it.pt + 2 * matrix * l * mp + jc * mp + ic, l * mp);
+            }
+          } else {
+            put_parts(v, sc.up, m - ic, (kPhase == kS ? buf.s : buf.p) + it.ps + 2 * matrix * m * mp + jc * mp + ic, m * mp);
+          }
+        }
+      }
+      wave_sync();
+    }
+}
+
+// The power of two that brings `top` to at most 2^14.
+int exponent_of(double top) { return 14 - static_cast<int>(std::ceil(std::log2(std::max(top, 1e-3)))); }
+
+}  // namespace
+
+void parts_place(Part& p, Item& it, int64_t count) {
+  const int64_t m = std::min(it.rows, it.cols), l = std::max(it.rows, it.cols), tm = ceil_div(m, kTile), tl = ceil_div(l, kTile);
+  it.x = p.x;
+  it.s = p.s;
+  it.px = p.px;
+  it.pt = p.pt;
+  it.ps = p.ps;
+  p.units[kBlocks] += count * ceil_div(m, 64) * ceil_div(l, 64);
+  p.units[kGram] += count * tm * (tm + 1) / 2;
+  p.units[kProduct] += count * tm * tl;
+  p.x += count * m * l;
+  p.x = (p.x + 3) / 4 * 4;
+  p.s += count * m * padded(m);
+  p.px += 2 * count * m * padded(l);
+  p.pt += 2 * count * l * padded(m);
+  p.ps += 2 * count * m * padded(m);
+}
+
+void parts_layout(Part& p, Room& room, int steps) {
+  if (steps == 0) return;
+  p.at_x = room(p.x * sizeof(float));
+  p.at[0] = room(p.s * sizeof(float));
+  p.at[1] = room(p.px * sizeof(_Float16));
+  p.at[2] = room(p.pt * sizeof(_Float16));
+  p.at[3] = room(p.pt * sizeof(_Float16));
+  p.at[4] = room(p.ps * sizeof(_Float16));
+  p.at[5] = room(p.ps * sizeof(_Float16));
+}
+
+hipError_t parts_run(const Part& p, const ou_config* cfg, const Step& st, char* base, hipStream_t stream) {
+  const int n = static_cast<int>(p.items.size());
+  const Item* const items = reinterpret_cast<const Item*>(base + p.at_items);
+  const double* const partial = reinterpret_cast<const double*>(base + p.at_partial);
+  auto halfs = [&](int i) { return reinterpret_cast<_Float16*>(base + p.at[i]); };
+  Buffers buf{reinterpret_cast<float*>(base + p.at_x), reinterpret_cast<float*>(base + p.at[0]), halfs(1), halfs(2), halfs(3), halfs(4), halfs(5)};
+  double top = 1;
+  int ex = exponent_of(top);
+  hipLaunchKernelGGL(normalise_kernel, dim3(static_cast<unsigned>(p.units[kBlocks])), dim3(kThreads), 0, stream, items, n, st, cfg->steps == 0, buf,
+                     std::ldexp(1.f, ex), partial);
+  hipError_t e = hipGetLastError();
+  auto grid = [&](Kind k) { return dim3(static_cast<unsigned>(ceil_div(p.units[k], kXcds) * kXcds)); };
+  const int gram = static_cast<int>(p.units[kGram]), product = static_cast<int>(p.units[kProduct]);
+  for (int i = 0; i < cfg->steps && e == hipSuccess; ++i) {
+    const bool last = i + 1 == cfg->steps;
+    const double square = top * top;
+    const int es = exponent_of(square), ep = exponent_of(std::fabs(cfg->b) * square + std::fabs(cfg->c) * square * square);
+    top = growth(cfg, top);
+    const int next = exponent_of(top);
+    hipLaunchKernelGGL(product_kernel<kS>, grid(kGram), dim3(kThreads), 0, stream, items, n, st, last, buf, Scales{std::ldexp(1.f, es), std::ldexp(1.f, -2 * ex)}, gram);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(product_kernel<kP>, grid(kGram), dim3(kThreads), 0, stream, items, n, st, last, buf, Scales{std::ldexp(1.f, ep), std::ldexp(1.f, -2 * es)}, gram);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(product_kernel<kX>, grid(kProduct), dim3(kThreads), 0, stream, items, n, st, last, buf, Scales{std::ldexp(1.f, next), std::ldexp(1.f, -ep - ex)}, product);
+    e = hipGetLastError();
+    ex = next;
+    std::swap(buf.t, buf.next);
+  }
+  return e;
+}
+
+}  // namespace ou

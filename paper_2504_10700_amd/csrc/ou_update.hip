@@ -5,7 +5,6 @@
 #include <algorithm>
 #include <cmath>
 #include <string>
-#include <vector>
 
 #include "el_tile.h"
 #include "ou_internal.h"
@@ -19,97 +18,51 @@ using sc::misaligned;
 using sc::set_error;
 
 constexpr int kTile = 64, kDepth = 16, kPitch = kTile + 4;
-constexpr int kChunk = 4096;   // elements of a chunk
-
-struct Step {
-  double a, b, c, mu, rate, keep, eps;   // keep: 1 - rate * decay
-  int nesterov;
-};
 
 __global__ __launch_bounds__(kLanes) void send_kernel(const Sent sent, Item* __restrict__ items) {
   const int i = threadIdx.x;
   if (i < sent.count) items[sent.first + i] = sent.item[i];
 }
 
-__device__ __forceinline__ int64_t chunks_of(int64_t elements) { return (elements + kChunk - 1) / kChunk; }
-
-__device__ __forceinline__ double workgroup_sum(double v, double* slots) {
-#pragma unroll
-  for (int d = 32; d > 0; d /= 2) v += __shfl_xor(v, d);
-  if ((threadIdx.x & 63) == 0) slots[threadIdx.x / 64] = v;
-  __syncthreads();
-  double s = slots[0];
-#pragma unroll
-  for (int w = 1; w < kWaves; ++w) s += slots[w];
-  __syncthreads();
-  return s;
-}
-
-// T: of the gradient; TA: of everything else.
-template <typename T, typename TA>
-__device__ __forceinline__ double momentum_chunk(const Item& it, const Step& st, int64_t at, int n, TA* __restrict__ x) {
-  const T* const g = static_cast<const T*>(it.grad) + at;
-  TA* const m = it.momentum ? static_cast<TA*>(it.momentum) + at : nullptr;
-  const TA mu = static_cast<TA>(st.mu);
-  double sum = 0;
-  for (int i = threadIdx.x; i < n; i += kThreads) {
-    TA u = static_cast<TA>(g[i]);
-    if (m) {
-      const TA v = mu * m[i] + u;
-      m[i] = v;
-      u = st.nesterov ? u + mu * v : v;
-    }
-    x[at + i] = u;
-    sum = fma(static_cast<double>(u), static_cast<double>(u), sum);
-  }
-  return sum;
-}
-
+// Momentum of a chunk of elements, and the sum of their U's squares.  A matrix's sum is that of its chunks.
 template <typename TA>
-__global__ __launch_bounds__(kThreads) void momentum_kernel(const Item* __restrict__ items, int n, const Step st, TA* __restrict__ X, double* __restrict__ partial) {
+__global__ __launch_bounds__(kThreads) void momentum_kernel(const Item* __restrict__ items, int n, const Step st, double* __restrict__ partial) {
   __shared__ double slots[kWaves];
   const Item& it = items[item_of(items, n, kChunks, blockIdx.x)];
   const int64_t size = static_cast<int64_t>(it.rows) * it.cols, per = chunks_of(size), unit = blockIdx.x - it.unit[kChunks];
-  const int64_t matrix = unit / per, at = unit % per * kChunk;
-  const int count = static_cast<int>(min(size - at, static_cast<int64_t>(kChunk)));
-  TA* const x = X + it.x;
-  double sum;
-  if constexpr (sizeof(TA) == 8) sum = momentum_chunk<double, double>(it, st, matrix * size + at, count, x);
-  else if (it.dtype == SC_F32) sum = momentum_chunk<float, float>(it, st, matrix * size + at, count, x);
-  else sum = momentum_chunk<__bf16, float>(it, st, matrix * size + at, count, x);
+  const int64_t matrix = unit / per, first = unit % per * kChunk, at = matrix * size + first;
+  const int count = static_cast<int>(min(size - first, static_cast<int64_t>(kChunk)));
+  const TA mu = static_cast<TA>(st.mu);
+  double sum = 0;
+  for (int i = threadIdx.x; i < count; i += kThreads) {
+    TA u = gradient<TA>(it, at + i);
+    if (it.momentum) {
+      TA* const m = static_cast<TA*>(it.momentum) + at + i;
+      const TA v = mu * *m + u;
+      *m = v;
+      u = direction(u, v, mu, st.nesterov);
+    }
+    sum = fma(static_cast<double>(u), static_cast<double>(u), sum);
+  }
   sum = workgroup_sum(sum, slots);
   if (threadIdx.x == 0) partial[blockIdx.x] = sum;
 }
 
-// A finished element of X: into the update and the weight.
-template <typename TA>
-__device__ __forceinline__ void finish(const Item& it, const Step& st, int64_t at, TA x) {
-  if (it.update) {
-    if (sizeof(TA) == 4 && it.dtype == SC_BF16) static_cast<__bf16*>(it.update)[at] = static_cast<__bf16>(static_cast<float>(x));
-    else static_cast<TA*>(it.update)[at] = x;
-  }
-  if (it.weight) {
-    TA* const w = static_cast<TA*>(it.weight) + at;
-    *w = static_cast<TA>(st.keep) * *w - static_cast<TA>(st.rate * it.scale) * x;
-  }
-}
+// ---- fp64: X = U / (norm + eps), in the tensor's own orientation; last: no steps follow
 
-// X = U / (norm + eps); last: no steps follow.
-template <typename TA>
-__global__ __launch_bounds__(kThreads) void normalise_kernel(const Item* __restrict__ items, int n, const Step st, bool last, TA* __restrict__ X,
+__global__ __launch_bounds__(kThreads) void normalise_kernel(const Item* __restrict__ items, int n, const Step st, bool last, double* __restrict__ X,
                                                              const double* __restrict__ partial) {
   __shared__ double slots[kWaves];
   const Item& it = items[item_of(items, n, kChunks, blockIdx.x)];
   const int64_t size = static_cast<int64_t>(it.rows) * it.cols, per = chunks_of(size), unit = blockIdx.x - it.unit[kChunks];
-  const int64_t matrix = unit / per, at = unit % per * kChunk;
-  const int count = static_cast<int>(min(size - at, static_cast<int64_t>(kChunk)));
-  double sum = 0;
-  for (int64_t i = threadIdx.x; i < per; i += kThreads) sum += partial[it.unit[kChunks] + matrix * per + i];
-  const double down = 1.0 / (sqrt(workgroup_sum(sum, slots)) + st.eps);
+  const int64_t matrix = unit / per, first = unit % per * kChunk;
+  const int count = static_cast<int>(min(size - first, static_cast<int64_t>(kChunk)));
+  const double down = down_of(partial + it.unit[kChunks] + matrix * per, per, st.eps, slots);
   for (int i = threadIdx.x; i < count; i += kThreads) {
-    const int64_t e = matrix * size + at + i;
-    const TA x = static_cast<TA>(static_cast<double>(X[it.x + e]) * down);
-    if (last) finish(it, st, e, x); else X[it.x + e] = x;
+    const int64_t e = matrix * size + first + i;
+    double u = gradient<double>(it, e);
+    if (it.momentum) u = direction(u, static_cast<const double*>(it.momentum)[e], st.mu, st.nesterov);
+    if (last) finish(it, st, e, u * down); else X[it.x + e] = u * down;
   }
 }
 
@@ -213,73 +166,67 @@ __global__ __launch_bounds__(kThreads) void product_kernel(const Item* __restric
 
 // ---- host side
 
-int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+enum Way { kDouble, kParts, kWays };
 
-// The list in two parts, fp32 (and bfloat16) tensors and fp64 ones, and where everything lies in the workspace.
-struct Part {
-  std::vector<Item> items;
-  int64_t units[kKinds] = {0, 0, 0};
-  int64_t x = 0, s = 0;            // elements of X and of S
-  size_t elem = 4;
-  size_t at_items = 0, at_partial = 0, at_x[2] = {0, 0}, at_s = 0, at_p = 0;
-};
+// The tensors by the way that their matrices take, and where everything lies in the workspace.
 struct Layout {
-  Part part[2];
+  Part part[kWays];
   size_t bytes = 0;
 };
 
+Way way_of(const ou_tensor& t) { return t.dtype == SC_F64 ? kDouble : kParts; }
+
+void double_place(Part& p, Item& it, int64_t count) {
+  const int64_t m = std::min(it.rows, it.cols), l = std::max(it.rows, it.cols);
+  it.x = p.x;
+  it.s = p.s;
+  p.units[kGram] += count * ceil_div(m, kTile) * ceil_div(m, kTile);
+  p.units[kProduct] += count * ceil_div(m, kTile) * ceil_div(l, kTile);
+  p.x += count * m * l;
+  p.s += count * m * m;
+}
+
+void double_layout(Part& p, Room& room, int steps) {
+  if (steps == 0) return;
+  p.at_x = room(p.x * sizeof(double));
+  p.at[0] = room(p.x * sizeof(double));
+  p.at[1] = room(p.s * sizeof(double));
+  p.at[2] = room(p.s * sizeof(double));
+}
+
 Layout layout_of(int64_t n, const ou_tensor* tensors, int steps) {
   Layout l;
-  l.part[1].elem = 8;
   for (int64_t i = 0; i < n; ++i) {
     const ou_tensor& t = tensors[i];
     if (t.count == 0) continue;
-    Part& p = l.part[t.dtype == SC_F64];
-    const int64_t m = std::min(t.rows, t.cols), k = std::max(t.rows, t.cols);
-    Item it{t.grad, t.momentum, t.weight, t.update, t.scale, t.count, p.x, p.s, {p.units[0], p.units[1], p.units[2]}, t.rows, t.cols, t.dtype, 0};
+    const Way way = way_of(t);
+    Part& p = l.part[way];
+    Item it{};
+    it.grad = t.grad;
+    it.momentum = t.momentum;
+    it.weight = t.weight;
+    it.update = t.update;
+    it.scale = t.scale;
+    std::copy_n(p.units, static_cast<int>(kKinds), it.unit);
+    it.rows = t.rows;
+    it.cols = t.cols;
+    it.dtype = t.dtype;
+    p.units[kChunks] += t.count * ceil_div(static_cast<int64_t>(t.rows) * t.cols, kChunk);
+    if (way == kDouble) double_place(p, it, t.count);
+    else parts_place(p, it, t.count);
     p.items.push_back(it);
-    p.units[kChunks] += t.count * ceil_div(m * k, kChunk);
-    p.units[kGram] += t.count * ceil_div(m, kTile) * ceil_div(m, kTile);
-    p.units[kProduct] += t.count * ceil_div(m, kTile) * ceil_div(k, kTile);
-    p.x += t.count * m * k;
-    p.s += t.count * m * m;
   }
-  size_t at = 0;
-  auto room = [&](size_t bytes) {
-    const size_t from = at;
-    at += align_up(bytes, 256);
-    return from;
-  };
-  for (Part& p : l.part) {
+  Room room;
+  for (int way = 0; way < kWays; ++way) {
+    Part& p = l.part[way];
     if (p.items.empty()) continue;
     p.at_items = room(p.items.size() * sizeof(Item));
     p.at_partial = room(p.units[kChunks] * sizeof(double));
-    p.at_x[0] = room(p.x * p.elem);
-    if (steps > 0) {
-      p.at_x[1] = room(p.x * p.elem);
-      p.at_s = room(p.s * p.elem);
-      p.at_p = room(p.s * p.elem);
-    }
+    if (way == kDouble) double_layout(p, room, steps);
+    else parts_layout(p, room, steps);
   }
-  l.bytes = std::max<size_t>(at, 256);
+  l.bytes = std::max<size_t>(room.bytes, 256);
   return l;
-}
-
-// The largest |a x + b x^3 + c x^5| of 0 <= x <= top.
-double growth(const ou_config* c, double top) {
-  auto f = [&](double x) { return std::fabs(x * (c->a + x * x * (c->b + x * x * c->c))); };
-  double most = f(top);
-  // where the derivative a + 3 b y + 5 c y^2, y = x^2, is zero
-  const double q = 5 * c->c, p = 3 * c->b, d = p * p - 4 * q * c->a;
-  double roots[3] = {-1, -1, -1};
-  if (q != 0 && d >= 0) {
-    roots[0] = (-p + std::sqrt(d)) / (2 * q);
-    roots[1] = (-p - std::sqrt(d)) / (2 * q);
-  }
-  if (p != 0) roots[2] = -c->a / p;   // (without c; with it an ordinary point inside, which does no harm)
-  for (double y : roots)
-    if (y > 0 && y < top * top) most = std::max(most, f(std::sqrt(y)));
-  return most;
 }
 
 sc_status check(const char* fn, const ou_config* cfg, int64_t n, const ou_tensor* tensors) {
@@ -324,10 +271,10 @@ sc_status check(const char* fn, const ou_config* cfg, int64_t n, const ou_tensor
   return SC_OK;
 }
 
+// The items to the workspace, momentum and sums of squares.
 template <typename TA>
-hipError_t run(const Part& p, const ou_config* cfg, const Step& st, char* base, hipStream_t stream) {
+hipError_t begin(const Part& p, const Step& st, char* base, hipStream_t stream) {
   const int n = static_cast<int>(p.items.size());
-  if (n == 0) return hipSuccess;
   Item* const items = reinterpret_cast<Item*>(base + p.at_items);
   for (int first = 0; first < n; first += kSent) {
     Sent sent{};
@@ -338,33 +285,55 @@ hipError_t run(const Part& p, const ou_config* cfg, const Step& st, char* base, 
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  double* const partial = reinterpret_cast<double*>(base + p.at_partial);
-  TA* X[2] = {reinterpret_cast<TA*>(base + p.at_x[0]), reinterpret_cast<TA*>(base + p.at_x[1])};
-  TA* const S = reinterpret_cast<TA*>(base + p.at_s);
-  TA* const P = reinterpret_cast<TA*>(base + p.at_p);
+  hipLaunchKernelGGL(momentum_kernel<TA>, dim3(static_cast<unsigned>(p.units[kChunks])), dim3(kThreads), 0, stream, items, n, st,
+                     reinterpret_cast<double*>(base + p.at_partial));
+  return hipGetLastError();
+}
+
+hipError_t double_run(const Part& p, const ou_config* cfg, const Step& st, char* base, hipStream_t stream) {
+  const int n = static_cast<int>(p.items.size());
+  const Item* const items = reinterpret_cast<const Item*>(base + p.at_items);
+  const double* const partial = reinterpret_cast<const double*>(base + p.at_partial);
+  double* const X[2] = {reinterpret_cast<double*>(base + p.at_x), reinterpret_cast<double*>(base + p.at[0])};
+  double* const S = reinterpret_cast<double*>(base + p.at[1]);
+  double* const P = reinterpret_cast<double*>(base + p.at[2]);
   auto grid = [&](Kind k) { return dim3(static_cast<unsigned>(p.units[k])); };
-  hipLaunchKernelGGL(momentum_kernel<TA>, grid(kChunks), dim3(kThreads), 0, stream, items, n, st, X[0], partial);
+  hipLaunchKernelGGL(normalise_kernel, grid(kChunks), dim3(kThreads), 0, stream, items, n, st, cfg->steps == 0, X[0], partial);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(normalise_kernel<TA>, grid(kChunks), dim3(kThreads), 0, stream, items, n, st, cfg->steps == 0, X[0], partial);
-  e = hipGetLastError();
   for (int i = 0; i < cfg->steps && e == hipSuccess; ++i) {
     const bool last = i + 1 == cfg->steps;
-    const TA* const x = X[i & 1];
-    TA* const next = X[(i + 1) & 1];
-    hipLaunchKernelGGL((product_kernel<TA, kS>), grid(kGram), dim3(kThreads), 0, stream, items, n, st, last, x, next, S, P);
+    const double* const x = X[i & 1];
+    double* const next = X[(i + 1) & 1];
+    hipLaunchKernelGGL((product_kernel<double, kS>), grid(kGram), dim3(kThreads), 0, stream, items, n, st, last, x, next, S, P);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((product_kernel<TA, kP>), grid(kGram), dim3(kThreads), 0, stream, items, n, st, last, x, next, S, P);
+    hipLaunchKernelGGL((product_kernel<double, kP>), grid(kGram), dim3(kThreads), 0, stream, items, n, st, last, x, next, S, P);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((product_kernel<TA, kX>), grid(kProduct), dim3(kThreads), 0, stream, items, n, st, last, x, next, S, P);
+    hipLaunchKernelGGL((product_kernel<double, kX>), grid(kProduct), dim3(kThreads), 0, stream, items, n, st, last, x, next, S, P);
     e = hipGetLastError();
   }
   return e;
 }
 
 }  // namespace
+
+double growth(const ou_config* c, double top) {
+  auto f = [&](double x) { return std::fabs(x * (c->a + x * x * (c->b + x * x * c->c))); };
+  double most = f(top);
+  // where the derivative a + 3 b y + 5 c y^2, y = x^2, is zero
+  const double q = 5 * c->c, p = 3 * c->b, d = p * p - 4 * q * c->a;
+  double roots[3] = {-1, -1, -1};
+  if (q != 0 && d >= 0) {
+    roots[0] = (-p + std::sqrt(d)) / (2 * q);
+    roots[1] = (-p - std::sqrt(d)) / (2 * q);
+  }
+  if (p != 0) roots[2] = -c->a / p;   // (without c; with it an ordinary point inside, which does no harm)
+  for (double y : roots)
+    if (y > 0 && y < top * top) most = std::max(most, f(std::sqrt(y)));
+  return most;
+}
+
 }  // namespace ou
 
 extern "C" {
@@ -389,7 +358,9 @@ sc_status ou_step(const ou_config* cfg, int64_t n_tensors, const ou_tensor* tens
   if (st != SC_OK) return st;
   try {
     const Layout l = layout_of(n_tensors, tensors, cfg->steps);
-    if (l.part[0].items.empty() && l.part[1].items.empty()) return SC_OK;
+    bool any = false;
+    for (const Part& p : l.part) any = any || !p.items.empty();
+    if (!any) return SC_OK;
     if (!workspace || workspace_bytes < l.bytes)
       return set_error(SC_ERR_WORKSPACE, "ou_step: workspace missing or smaller than ou_workspace_bytes()");
     if (misaligned(workspace, 256)) return set_error(SC_ERR_WORKSPACE, "ou_step: workspace not 256-byte aligned");
@@ -398,8 +369,15 @@ sc_status ou_step(const ou_config* cfg, int64_t n_tensors, const ou_tensor* tens
     const Step step{cfg->a, cfg->b, cfg->c, cfg->momentum, cfg->rate, 1 - cfg->rate * cfg->decay, cfg->eps, (cfg->flags & OU_NESTEROV) != 0};
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     char* const base = static_cast<char*>(workspace);
-    hipError_t e = run<float>(l.part[0], cfg, step, base, stream);
-    if (e == hipSuccess) e = run<double>(l.part[1], cfg, step, base, stream);
+    hipError_t e = hipSuccess;
+    if (!l.part[kParts].items.empty()) {
+      e = begin<float>(l.part[kParts], step, base, stream);
+      if (e == hipSuccess) e = parts_run(l.part[kParts], cfg, step, base, stream);
+    }
+    if (e == hipSuccess && !l.part[kDouble].items.empty()) {
+      e = begin<double>(l.part[kDouble], step, base, stream);
+      if (e == hipSuccess) e = double_run(l.part[kDouble], cfg, step, base, stream);
+    }
     if (e != hipSuccess) return set_error(SC_ERR_HIP, std::string("ou_step: kernel launch: ") + hipGetErrorString(e));
   } catch (const std::bad_alloc&) {
     return set_error(SC_ERR_ALLOC, "ou_step: out of host memory");
