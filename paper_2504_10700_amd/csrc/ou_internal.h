@@ -76,6 +76,12 @@ __device__ __forceinline__ int item_of(const Item* __restrict__ items, int n, in
 
 __device__ __forceinline__ int64_t chunks_of(int64_t elements) { return (elements + kChunk - 1) / kChunk; }
 
+// fp32 values as two fp16 parts, v = h + l.
+__device__ __forceinline__ void split(float v, _Float16& h, _Float16& l) {
+  h = static_cast<_Float16>(v);
+  l = static_cast<_Float16>(v - static_cast<float>(h));
+}
+
 // U of an element from its gradient and the momentum that the step leaves.
 template <typename TA>
 __device__ __forceinline__ TA direction(TA g, TA m, TA mu, bool nesterov) { return nesterov ? g + mu * m : m; }
@@ -126,5 +132,11 @@ double growth(const ou_config* c, double top);
 void parts_place(Part& p, Item& it, int64_t count);
 void parts_layout(Part& p, Room& room, int steps);
 hipError_t parts_run(const Part& p, const ou_config* cfg, const Step& st, char* base, hipStream_t stream);
+
+// fp32 matrices of at most 64 x 64 and 128 x 128, a workgroup each from the gradient to the weight (ou_small.hip).
+hipError_t small_run(const Part& p, const ou_config* cfg, const Step& st, bool wide, const Item* items, hipStream_t stream);
+
+// The power of two that brings `top` to at most 2^14 (fp16 parts).
+int exponent_of(double top);
 
 }  // namespace ou

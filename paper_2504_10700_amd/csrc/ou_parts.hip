@@ -51,11 +51,6 @@ struct Scales {
   float down;    // sums of parts to values
 };
 
-__device__ __forceinline__ void split(float v, _Float16& h, _Float16& l) {
-  h = static_cast<_Float16>(v);
-  l = static_cast<_Float16>(v - static_cast<float>(h));
-}
-
 // Sixteen consecutive values of a row, times `up`, to both parts; those from `inside` on are zeros.  (`to` is a multiple of 16 in a row of a multiple of 32.)
 __device__ __forceinline__ void put_parts(const float (&v)[16], float up, int inside, _Float16* to, int64_t part) {
 #pragma unroll
@@ -367,10 +362,9 @@ __global__ __launch_bounds__(kThreads, 2) void product_kernel(const Item* __rest
     }
 }
 
-// The power of two that brings `top` to at most 2^14.
-int exponent_of(double top) { return 14 - static_cast<int>(std::ceil(std::log2(std::max(top, 1e-3)))); }
-
 }  // namespace
+
+int exponent_of(double top) { return 14 - static_cast<int>(std::ceil(std::log2(std::max(top, 1e-3)))); }
 
 void parts_place(Part& p, Item& it, int64_t count) {
   const int64_t m = std::min(it.rows, it.cols), l = std::max(it.rows, it.cols), tm = ceil_div(m, kTile), tl = ceil_div(l, kTile);

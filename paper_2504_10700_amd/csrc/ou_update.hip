@@ -166,7 +166,7 @@ __global__ __launch_bounds__(kThreads) void product_kernel(const Item* __restric
 
 // ---- host side
 
-enum Way { kDouble, kParts, kWays };
+enum Way { kDouble, kParts, kSmall, kMiddle, kWays };
 
 // The tensors by the way that their matrices take, and where everything lies in the workspace.
 struct Layout {
@@ -174,7 +174,11 @@ struct Layout {
   size_t bytes = 0;
 };
 
-Way way_of(const ou_tensor& t) { return t.dtype == SC_F64 ? kDouble : kParts; }
+// A matrix that one workgroup can hold takes one launch instead of three a step.
+Way way_of(const ou_tensor& t) {
+  const int l = std::max(t.rows, t.cols);
+  return t.dtype == SC_F64 ? kDouble : l <= 64 ? kSmall : l <= 128 ? kMiddle : kParts;
+}
 
 void double_place(Part& p, Item& it, int64_t count) {
   const int64_t m = std::min(it.rows, it.cols), l = std::max(it.rows, it.cols);
@@ -211,9 +215,10 @@ Layout layout_of(int64_t n, const ou_tensor* tensors, int steps) {
     it.rows = t.rows;
     it.cols = t.cols;
     it.dtype = t.dtype;
-    p.units[kChunks] += t.count * ceil_div(static_cast<int64_t>(t.rows) * t.cols, kChunk);
+    if (way == kDouble || way == kParts) p.units[kChunks] += t.count * ceil_div(static_cast<int64_t>(t.rows) * t.cols, kChunk);
     if (way == kDouble) double_place(p, it, t.count);
-    else parts_place(p, it, t.count);
+    else if (way == kParts) parts_place(p, it, t.count);
+    else p.units[kBlocks] += t.count;
     p.items.push_back(it);
   }
   Room room;
@@ -223,7 +228,7 @@ Layout layout_of(int64_t n, const ou_tensor* tensors, int steps) {
     p.at_items = room(p.items.size() * sizeof(Item));
     p.at_partial = room(p.units[kChunks] * sizeof(double));
     if (way == kDouble) double_layout(p, room, steps);
-    else parts_layout(p, room, steps);
+    else if (way == kParts) parts_layout(p, room, steps);
   }
   l.bytes = std::max<size_t>(room.bytes, 256);
   return l;
@@ -271,9 +276,7 @@ sc_status check(const char* fn, const ou_config* cfg, int64_t n, const ou_tensor
   return SC_OK;
 }
 
-// The items to the workspace, momentum and sums of squares.
-template <typename TA>
-hipError_t begin(const Part& p, const Step& st, char* base, hipStream_t stream) {
+hipError_t send(const Part& p, char* base, hipStream_t stream) {
   const int n = static_cast<int>(p.items.size());
   Item* const items = reinterpret_cast<Item*>(base + p.at_items);
   for (int first = 0; first < n; first += kSent) {
@@ -285,6 +288,16 @@ hipError_t begin(const Part& p, const Step& st, char* base, hipStream_t stream) 
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
+  return hipSuccess;
+}
+
+// The items to the workspace, momentum and sums of squares.
+template <typename TA>
+hipError_t begin(const Part& p, const Step& st, char* base, hipStream_t stream) {
+  const hipError_t e = send(p, base, stream);
+  if (e != hipSuccess) return e;
+  const int n = static_cast<int>(p.items.size());
+  const Item* const items = reinterpret_cast<const Item*>(base + p.at_items);
   hipLaunchKernelGGL(momentum_kernel<TA>, dim3(static_cast<unsigned>(p.units[kChunks])), dim3(kThreads), 0, stream, items, n, st,
                      reinterpret_cast<double*>(base + p.at_partial));
   return hipGetLastError();
@@ -370,7 +383,13 @@ sc_status ou_step(const ou_config* cfg, int64_t n_tensors, const ou_tensor* tens
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     char* const base = static_cast<char*>(workspace);
     hipError_t e = hipSuccess;
-    if (!l.part[kParts].items.empty()) {
+    for (const Way way : {kMiddle, kSmall}) {
+      const Part& p = l.part[way];
+      if (e != hipSuccess || p.items.empty()) continue;
+      e = send(p, base, stream);
+      if (e == hipSuccess) e = small_run(p, cfg, step, way == kMiddle, reinterpret_cast<const Item*>(base + p.at_items), stream);
+    }
+    if (e == hipSuccess && !l.part[kParts].items.empty()) {
       e = begin<float>(l.part[kParts], step, base, stream);
       if (e == hipSuccess) e = parts_run(l.part[kParts], cfg, step, base, stream);
     }
