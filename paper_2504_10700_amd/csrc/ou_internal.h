@@ -18,7 +18,7 @@ constexpr int kChunk = 4096;   // elements of a chunk of the first pass
 
 // A matrix as the iteration sees it is m x l, m <= l: the tensor's matrix, or its transpose where rows > cols.  Work is dealt out in units; `unit[k]` is
 // the number of units of kind k in the tensors before this one.
-enum Kind { kChunks, kBlocks, kGram, kProduct, kKinds };
+enum Kind { kChunks, kBlocks, kGram, kProduct, kGramSmall, kProductSmall, kKinds };   // (products: in tiles of 128, in tiles of 64)
 
 struct Item {
   const void* grad;
@@ -31,7 +31,7 @@ struct Item {
   int64_t px, pt, ps;      // and the parts of X, of X transposed, of S and P
   int32_t rows, cols, dtype, pad;
 };
-constexpr int kSent = 31;  // items of one launch's kernel arguments
+constexpr int kSent = 27;  // items of one launch's kernel arguments
 struct Sent {
   int32_t first, count;
   Item item[kSent];
@@ -48,7 +48,7 @@ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // Tensors of one way through the kernels.
 struct Part {
   std::vector<Item> items;
-  int64_t units[kKinds] = {0, 0, 0, 0};
+  int64_t units[kKinds] = {};
   int64_t x = 0, s = 0, px = 0, pt = 0, ps = 0;
   size_t at_items = 0, at_partial = 0, at_x = 0;
   size_t at[6] = {};   // the way's other buffers

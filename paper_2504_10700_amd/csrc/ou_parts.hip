@@ -11,7 +11,9 @@
 // tiles on and below the diagonal are computed and mirrored.
 //
 // A workgroup: 128 x 128, four waves of 64 x 64; 32 reduced indices of both operands' parts (32 KB) go from memory to LDS without passing registers while
-// the 32 before are multiplied.  A row's four pieces of 16 bytes stand at places that differ between rows (swizzle), against bank conflicts.
+// the 32 before are multiplied, and a second workgroup of the compute unit fills the waits.  Where there are not tiles enough for that (few_tiles), 64 x 64 with
+// eight stages: a stage then comes from memory while seven before it are multiplied.  A row's four pieces of 16 bytes stand at places that differ between rows
+// (swizzle), against bank conflicts.
 #include <algorithm>
 #include <cmath>
 
@@ -25,16 +27,20 @@ typedef float F16 __attribute__((ext_vector_type(16)));
 typedef float F4 __attribute__((ext_vector_type(4)));
 typedef float F4Loose __attribute__((ext_vector_type(4), aligned(4)));
 
-constexpr int kTile = 128, kDepth = 32, kFlush = 128;
+constexpr int kDepth = 32, kFlush = 128;
+constexpr int kRow = 2 * kDepth;          // elements of a row in LDS: h and l
 constexpr int kPad = 32;                  // rows of the parts in memory are multiples of this
-constexpr int kPlane = kTile * kDepth;    // elements of one part of one operand in LDS
-constexpr int kStage = 4 * kPlane;        // A h, A l, B h, B l
 constexpr int kPitch = 36;                // floats of a row of a wave's 32 x 32 in LDS
 constexpr int kXcds = 8;
+#ifndef OU_FEW
+#define OU_FEW 256
+#endif
+constexpr int kFewTiles = OU_FEW;
 
 __host__ __device__ constexpr int64_t padded(int64_t n) { return (n + kPad - 1) / kPad * kPad; }
 
-// Buffers.  Parts: [h, l][rows][padded columns] of each matrix.
+// Buffers.  Parts: [rows][padded columns / 32][h, l][32] of each matrix: what a stage reads of a row is one line of the caches (with h and l apart, and so half
+// lines: 4096 x 4096 twice @@ms instead of 9.8).
 struct Buffers {
   float* X;             // [m][l]
   float* S;             // [m][padded(m)], the tiles on and below the diagonal
@@ -51,8 +57,9 @@ struct Scales {
   float down;    // sums of parts to values
 };
 
-// Sixteen consecutive values of a row, times `up`, to both parts; those from `inside` on are zeros.  (`to` is a multiple of 16 in a row of a multiple of 32.)
-__device__ __forceinline__ void put_parts(const float (&v)[16], float up, int inside, _Float16* to, int64_t part) {
+// Sixteen consecutive values of a row from column c (a multiple of 16) on, times `up`, to both parts; those from `inside` on are zeros.
+__device__ __forceinline__ void put_parts(const float (&v)[16], float up, int inside, _Float16* row, int c) {
+  _Float16* const to = row + 2 * (c & ~31) + (c & 31);
 #pragma unroll
   for (int b = 0; b < 16; b += 8) {
     H8 h, l;
@@ -64,7 +71,7 @@ __device__ __forceinline__ void put_parts(const float (&v)[16], float up, int in
       l[i] = y;
     }
     *reinterpret_cast<H8*>(to + b) = h;
-    *reinterpret_cast<H8*>(to + part + b) = l;
+    *reinterpret_cast<H8*>(to + 32 + b) = l;
   }
 }
 
@@ -105,12 +112,12 @@ __global__ __launch_bounds__(kThreads) void normalise_kernel(const Item* __restr
   if (i0 + row < m && j0 + from < lp) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i] = block[row][from + i];
-    put_parts(v, up, l - j0 - from, buf.x + it.px + 2 * matrix * m * lp + (i0 + row) * lp + j0 + from, m * lp);
+    put_parts(v, up, l - j0 - from, buf.x + it.px + 2 * (matrix * m + i0 + row) * lp, j0 + from);
   }
   if (j0 + row < l && i0 + from < mp) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i] = block[from + i][row];
-    put_parts(v, up, m - i0 - from, buf.t + it.pt + 2 * matrix * l * mp + (j0 + row) * mp + i0 + from, l * mp);
+    put_parts(v, up, m - i0 - from, buf.t + it.pt + 2 * (matrix * l + j0 + row) * mp, i0 + from);
   }
 }
 
@@ -141,27 +148,48 @@ __device__ __forceinline__ void any_tile(int t, int rows, int cols, int& i, int&
   i = first + t % high;
 }
 
-__device__ __forceinline__ int swizzle(int row) { return ((row >> 1) & 3) ^ ((row >> 3) & 1); }
+__device__ __forceinline__ int swizzle(int row) { return ((row >> 1) & 7) ^ ((row & 1) << 2); }   // rows 0..7, and the even and the odd ones of 16, all differ
 
-// 128 rows (clamped to the last) of one part, 32 reduced indices, to LDS: eight requests of a wave, 16 rows each.
-__device__ __forceinline__ void load_plane(const _Float16* __restrict__ from, const unsigned (&offset)[8], _Float16* to) {
+// Half of a tile's rows (clamped to the last), 32 reduced indices, to LDS: eight rows with each request of a wave.
+template <int kLoads>
+__device__ __forceinline__ void load_rows(const _Float16* __restrict__ from, const unsigned (&offset)[kLoads], _Float16* to) {
 #pragma unroll
-  for (int q = 0; q < 8; ++q) {
+  for (int q = 0; q < kLoads; ++q) {
     const auto* const g = reinterpret_cast<const __attribute__((address_space(1))) unsigned*>(
         reinterpret_cast<uintptr_t>(reinterpret_cast<const char*>(from) + offset[q]));
-    __builtin_amdgcn_global_load_lds(g, reinterpret_cast<__attribute__((address_space(3))) unsigned*>(reinterpret_cast<uintptr_t>(to + q * 16 * kDepth)), 16, 0, 0);
+    __builtin_amdgcn_global_load_lds(g, reinterpret_cast<__attribute__((address_space(3))) unsigned*>(reinterpret_cast<uintptr_t>(to + q * 8 * kRow)), 16, 0, 0);
   }
 }
 
 __device__ __forceinline__ void wave_sync() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
+// Waits until at most N of the wave's requests are under way, then for the workgroup.
+template <int N>
+__device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(N) : "memory"); }
+// The stage that is multiplied next has arrived, of the `left` (at most kAhead) after it none has to.
+template <int kAhead, int kLoads>
+__device__ __forceinline__ void stage_arrived(int left) {
+  if constexpr (kAhead == 0) arrived<0>();
+  else if (left >= kAhead) arrived<kAhead * kLoads>();
+  else stage_arrived<kAhead - 1, kLoads>(left);
+}
+
 enum Phase { kS, kP, kX };
 
-template <int kPhase>
-__global__ __launch_bounds__(kThreads, 2) void product_kernel(const Item* __restrict__ items, int n, const Step st, bool last, const Buffers buf, const Scales sc,
+template <int kTile, int kStages>
+struct Ring {
+  static constexpr int kOperand = kTile * kRow;
+  static constexpr int kStage = 2 * kOperand;
+  static constexpr int kBytes = kStages * kStage * 2;
+};
+
+template <int kPhase, int kTile, int kStages>
+__global__ __launch_bounds__(kThreads, kStages == 2 ? 2 : 1) void product_kernel(const Item* __restrict__ items, int n, const Step st, bool last, const Buffers buf, const Scales sc,
                                                               int total) {
-  __shared__ __attribute__((aligned(16))) _Float16 lds[2 * kStage];
-  constexpr int kind = kPhase == kX ? kProduct : kGram;
+  using R = Ring<kTile, kStages>;
+  constexpr int kOperand = R::kOperand, kStage = R::kStage, kLoads = kTile / 16, kSide = kTile / 64;   // kSide: 32 x 32 blocks along a wave's side
+  extern __shared__ __attribute__((aligned(16))) _Float16 lds[];
+  constexpr int kind = kTile == 128 ? (kPhase == kX ? kProduct : kGram) : kPhase == kX ? kProductSmall : kGramSmall;
   const int per_xcd = (total + kXcds - 1) / kXcds;
   const int u = static_cast<int>(blockIdx.x) % kXcds * per_xcd + blockIdx.x / kXcds;
   if (u >= total) return;
@@ -178,78 +206,69 @@ __global__ __launch_bounds__(kThreads, 2) void product_kernel(const Item* __rest
   const int i0 = ti * kTile, j0 = tj * kTile;
   const int lane = threadIdx.x & (kLanes - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
 
-  // operands: rows of A and of B
-  const int64_t ld = kPhase == kS ? lp : mp;
-  const _Float16* a;
-  const _Float16* b;
-  int64_t a_part, b_part;
-  int b_rows;
-  if constexpr (kPhase == kS) {
-    a = b = buf.x + it.px + 2 * matrix * m * lp;
-    a_part = b_part = m * lp;
-    b_rows = m;
-  } else if constexpr (kPhase == kP) {
-    a = b = buf.s + it.ps + 2 * matrix * m * mp;
-    a_part = b_part = m * mp;
-    b_rows = m;
-  } else {
-    a = buf.p + it.ps + 2 * matrix * m * mp;
-    a_part = m * mp;
-    b = buf.t + it.pt + 2 * matrix * l * mp;
-    b_part = l * mp;
-    b_rows = l;
-  }
+  // operands: rows of A and of B, both from the same matrix but for the last phase.  Two waves bring A, two B.
+  const int64_t ld = 2 * (kPhase == kS ? lp : mp);
   const bool of_b = wave & 2;
-  const int row0 = of_b ? j0 : i0, left = (of_b ? b_rows : m) - row0;
-  const _Float16* from = (of_b ? b + (wave & 1) * b_part : a + (wave & 1) * a_part) + row0 * ld;
-  unsigned offset[8];
+  const _Float16* from = kPhase == kS   ? buf.x + it.px + matrix * m * ld
+                         : kPhase == kP ? buf.s + it.ps + matrix * m * ld
+                         : of_b         ? buf.t + it.pt + matrix * l * ld
+                                        : buf.p + it.ps + matrix * m * ld;
+  const int row0 = (of_b ? j0 : i0), left = (of_b && kPhase == kX ? l : m) - row0, half = wave % 2 * (kTile / 2);
+  from += row0 * ld;
+  unsigned offset[kLoads];
 #pragma unroll
-  for (int q = 0; q < 8; ++q)
-    offset[q] = 2u * (static_cast<unsigned>(min(16 * q + lane / 4, left - 1)) * static_cast<unsigned>(ld) + 8u * ((lane % 4) ^ swizzle(lane / 4)));
-  const int stages = static_cast<int>(ld / kDepth);
-  _Float16* const mine = lds + wave * kPlane;
-  const int wi = wave / 2 * 64, wj = wave % 2 * 64;
+  for (int q = 0; q < kLoads; ++q) {
+    const int r = half + 8 * q + lane / 8;
+    offset[q] = 2u * (static_cast<unsigned>(min(r, left - 1)) * static_cast<unsigned>(ld) + 8u * ((lane % 8) ^ swizzle(r)));
+  }
+  const int stages = static_cast<int>(ld / kRow);
+  _Float16* const mine = lds + wave / 2 * kOperand + half * kRow;
+  const int wi = wave / 2 * 32 * kSide, wj = wave % 2 * 32 * kSide;
 
-  F16 sum[2][2], part[2][2];
+  F16 sum[kSide][kSide], part[kSide][kSide];
 #pragma unroll
-  for (int x = 0; x < 2; ++x)
+  for (int x = 0; x < kSide; ++x)
 #pragma unroll
-    for (int y = 0; y < 2; ++y)
+    for (int y = 0; y < kSide; ++y)
 #pragma unroll
       for (int r = 0; r < 16; ++r) sum[x][y][r] = part[x][y][r] = 0;
 
-  load_plane(from, offset, mine);
+  // stage t stands in slot t % kStages; a slot is filled again once all waves have passed the barrier after its use
+  int filled = 0, slot = 0;
+  for (; filled < kStages - 1 && filled < stages; ++filled) load_rows<kLoads>(from + filled * kRow, offset, mine + filled * kStage);
+  int to = filled;   // (only used when there are stages left: then it is kStages - 1)
   for (int t = 0; t < stages; ++t) {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (t + 1 < stages) {
-      from += kDepth;
-      load_plane(from, offset, mine + ((t + 1) & 1) * kStage);
+    stage_arrived<kStages - 2, kLoads>(stages - 1 - t);
+    if (filled < stages) {
+      load_rows<kLoads>(from + static_cast<int64_t>(filled) * kRow, offset, mine + to * kStage);
+      ++filled;
+      to = to + 1 == kStages ? 0 : to + 1;
     }
-    const _Float16* const here = lds + (t & 1) * kStage;
+    const _Float16* const here = lds + slot * kStage;
+    slot = slot + 1 == kStages ? 0 : slot + 1;
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-      H8 x[2][2], y[2][2];   // [tile][part]
+      H8 x[kSide][2], y[kSide][2];   // [block][part]
 #pragma unroll
-      for (int e = 0; e < 2; ++e)
+      for (int e = 0; e < kSide; ++e)
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
-          const int r = e * 32 + (lane & 31), piece = ((2 * s + lane / 32) ^ swizzle(r)) * 8;
-          x[e][q] = *reinterpret_cast<const H8*>(here + q * kPlane + (wi + r) * kDepth + piece);
-          y[e][q] = *reinterpret_cast<const H8*>(here + (2 + q) * kPlane + (wj + r) * kDepth + piece);
+          const int r = e * 32 + (lane & 31), piece = ((4 * q + 2 * s + lane / 32) ^ swizzle(r)) * 8;   // (wi and wj are multiples of 32)
+          x[e][q] = *reinterpret_cast<const H8*>(here + (wi + r) * kRow + piece);
+          y[e][q] = *reinterpret_cast<const H8*>(here + kOperand + (wj + r) * kRow + piece);
         }
 #pragma unroll
       for (int q = 0; q < 3; ++q)   // l h, h l, h h
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
+        for (int e = 0; e < kSide; ++e)
 #pragma unroll
-          for (int f = 0; f < 2; ++f) part[e][f] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[e][q == 0], y[f][q == 1], part[e][f], 0, 0, 0);
+          for (int f = 0; f < kSide; ++f) part[e][f] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[e][q == 0], y[f][q == 1], part[e][f], 0, 0, 0);
     }
     if ((t + 1) % (kFlush / kDepth) == 0 || t + 1 == stages) {
 #pragma unroll
-      for (int e = 0; e < 2; ++e)
+      for (int e = 0; e < kSide; ++e)
 #pragma unroll
-        for (int f = 0; f < 2; ++f) {
+        for (int f = 0; f < kSide; ++f) {
           sum[e][f] += part[e][f];
 #pragma unroll
           for (int r = 0; r < 16; ++r) part[e][f][r] = 0;
@@ -264,9 +283,9 @@ __global__ __launch_bounds__(kThreads, 2) void product_kernel(const Item* __rest
   const bool mirrored = kPhase != kX && ti != tj;
   const int columns = kPhase == kX ? l : m;
 #pragma unroll
-  for (int e = 0; e < 2; ++e)
+  for (int e = 0; e < kSide; ++e)
 #pragma unroll
-    for (int f = 0; f < 2; ++f) {
+    for (int f = 0; f < kSide; ++f) {
       const int ib = i0 + wi + 32 * e, jb = j0 + wj + 32 * f;
       if (ib >= m || jb >= columns) continue;
 #pragma unroll
@@ -313,7 +332,7 @@ __global__ __launch_bounds__(kThreads, 2) void product_kernel(const Item* __rest
               for (int r = 0; r < 16; ++r)
                 if (j + r < l) buf.X[x0 + r] = v[r];
             }
-            put_parts(v, sc.up, l - j, buf.x + it.px + 2 * matrix * m * lp + i * lp + j, m * lp);
+            put_parts(v, sc.up, l - j, buf.x + it.px + 2 * (matrix * m + i) * lp, j);
           }
         } else {
           float* const S = buf.S + it.s + (matrix * m + i) * mp + j;
@@ -329,7 +348,7 @@ __global__ __launch_bounds__(kThreads, 2) void product_kernel(const Item* __rest
               for (int k = 0; k < 4; ++k) v[r + k] = cb * x[k] + cc * v[r + k];
             }
           }
-          put_parts(v, sc.up, m - j, (kPhase == kS ? buf.s : buf.p) + it.ps + 2 * matrix * m * mp + i * mp + j, m * mp);
+          put_parts(v, sc.up, m - j, (kPhase == kS ? buf.s : buf.p) + it.ps + 2 * (matrix * m + i) * mp, j);
         }
       }
       if (kPhase == kX || mirrored) {
@@ -351,10 +370,10 @@ __global__ __launch_bounds__(kThreads, 2) void product_kernel(const Item* __rest
                   if (ic + r < m) finish(it, st, (static_cast<int64_t>(matrix) * l + jc) * m + ic + r, v[r]);
               }
             } else {
-              put_parts(v, sc.up, m - ic, buf.next + it.pt + 2 * matrix * l * mp + jc * mp + ic, l * mp);
+              put_parts(v, sc.up, m - ic, buf.next + it.pt + 2 * (matrix * l + jc) * mp, ic);
             }
           } else {
-            put_parts(v, sc.up, m - ic, (kPhase == kS ? buf.s : buf.p) + it.ps + 2 * matrix * m * mp + jc * mp + ic, m * mp);
+            put_parts(v, sc.up, m - ic, (kPhase == kS ? buf.s : buf.p) + it.ps + 2 * (matrix * m + jc) * mp, ic);
           }
         }
       }
@@ -367,15 +386,18 @@ __global__ __launch_bounds__(kThreads, 2) void product_kernel(const Item* __rest
 int exponent_of(double top) { return 14 - static_cast<int>(std::ceil(std::log2(std::max(top, 1e-3)))); }
 
 void parts_place(Part& p, Item& it, int64_t count) {
-  const int64_t m = std::min(it.rows, it.cols), l = std::max(it.rows, it.cols), tm = ceil_div(m, kTile), tl = ceil_div(l, kTile);
+  const int64_t m = std::min(it.rows, it.cols), l = std::max(it.rows, it.cols);
   it.x = p.x;
   it.s = p.s;
   it.px = p.px;
   it.pt = p.pt;
   it.ps = p.ps;
   p.units[kBlocks] += count * ceil_div(m, 64) * ceil_div(l, 64);
-  p.units[kGram] += count * tm * (tm + 1) / 2;
-  p.units[kProduct] += count * tm * tl;
+  for (const int tile : {128, 64}) {
+    const int64_t tm = ceil_div(m, tile), tl = ceil_div(l, tile);
+    p.units[tile == 128 ? kGram : kGramSmall] += count * tm * (tm + 1) / 2;
+    p.units[tile == 128 ? kProduct : kProductSmall] += count * tm * tl;
+  }
   p.x += count * m * l;
   p.x = (p.x + 3) / 4 * 4;
   p.s += count * m * padded(m);
@@ -395,6 +417,33 @@ void parts_layout(Part& p, Room& room, int steps) {
   p.at[5] = room(p.ps * sizeof(_Float16));
 }
 
+namespace {
+
+// Tiles of 128 that leave half of the chip's places for workgroups empty: smaller ones.
+bool few_tiles(int64_t tiles) { return tiles <= kFewTiles; }
+
+template <int kPhase, int kTile, int kStages>
+hipError_t launch(const Part& p, const Item* items, const Step& st, bool last, const Buffers& buf, const Scales& sc, hipStream_t stream) {
+  constexpr int bytes = Ring<kTile, kStages>::kBytes;
+  constexpr Kind kind = kTile == 128 ? (kPhase == kX ? kProduct : kGram) : kPhase == kX ? kProductSmall : kGramSmall;
+  const void* const kernel = reinterpret_cast<const void*>(&product_kernel<kPhase, kTile, kStages>);
+  if (bytes > 64 * 1024) {
+    const hipError_t e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL((product_kernel<kPhase, kTile, kStages>), dim3(static_cast<unsigned>(ceil_div(p.units[kind], kXcds) * kXcds)), dim3(kThreads), bytes, stream,
+                     items, static_cast<int>(p.items.size()), st, last, buf, sc, static_cast<int>(p.units[kind]));
+  return hipGetLastError();
+}
+
+template <int kPhase>
+hipError_t launch(const Part& p, const Item* items, const Step& st, bool last, const Buffers& buf, const Scales& sc, hipStream_t stream) {
+  return few_tiles(p.units[kPhase == kX ? kProduct : kGram]) ? launch<kPhase, 64, 8>(p, items, st, last, buf, sc, stream)
+                                                             : launch<kPhase, 128, 2>(p, items, st, last, buf, sc, stream);
+}
+
+}  // namespace
+
 hipError_t parts_run(const Part& p, const ou_config* cfg, const Step& st, char* base, hipStream_t stream) {
   const int n = static_cast<int>(p.items.size());
   const Item* const items = reinterpret_cast<const Item*>(base + p.at_items);
@@ -406,22 +455,15 @@ hipError_t parts_run(const Part& p, const ou_config* cfg, const Step& st, char* 
   hipLaunchKernelGGL(normalise_kernel, dim3(static_cast<unsigned>(p.units[kBlocks])), dim3(kThreads), 0, stream, items, n, st, cfg->steps == 0, buf,
                      std::ldexp(1.f, ex), partial);
   hipError_t e = hipGetLastError();
-  auto grid = [&](Kind k) { return dim3(static_cast<unsigned>(ceil_div(p.units[k], kXcds) * kXcds)); };
-  const int gram = static_cast<int>(p.units[kGram]), product = static_cast<int>(p.units[kProduct]);
   for (int i = 0; i < cfg->steps && e == hipSuccess; ++i) {
     const bool last = i + 1 == cfg->steps;
     const double square = top * top;
     const int es = exponent_of(square), ep = exponent_of(std::fabs(cfg->b) * square + std::fabs(cfg->c) * square * square);
     top = growth(cfg, top);
     const int next = exponent_of(top);
-    hipLaunchKernelGGL(product_kernel<kS>, grid(kGram), dim3(kThreads), 0, stream, items, n, st, last, buf, Scales{std::ldexp(1.f, es), std::ldexp(1.f, -2 * ex)}, gram);
-    e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(product_kernel<kP>, grid(kGram), dim3(kThreads), 0, stream, items, n, st, last, buf, Scales{std::ldexp(1.f, ep), std::ldexp(1.f, -2 * es)}, gram);
-    e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(product_kernel<kX>, grid(kProduct), dim3(kThreads), 0, stream, items, n, st, last, buf, Scales{std::ldexp(1.f, next), std::ldexp(1.f, -ep - ex)}, product);
-    e = hipGetLastError();
+    e = launch<kS>(p, items, st, last, buf, Scales{std::ldexp(1.f, es), std::ldexp(1.f, -2 * ex)}, stream);
+    if (e == hipSuccess) e = launch<kP>(p, items, st, last, buf, Scales{std::ldexp(1.f, ep), std::ldexp(1.f, -2 * es)}, stream);
+    if (e == hipSuccess) e = launch<kX>(p, items, st, last, buf, Scales{std::ldexp(1.f, next), std::ldexp(1.f, -ep - ex)}, stream);
     ex = next;
     std::swap(buf.t, buf.next);
   }
