@@ -29,7 +29,8 @@ struct Item {
   int64_t unit[kKinds];
   int64_t x, s;            // where the tensor's X and S begin in their buffers, in elements
   int64_t px, pt, ps;      // and the parts of X, of X transposed, of S and P
-  int32_t rows, cols, dtype, pad;
+  int32_t rows, cols, dtype;
+  int32_t width;           // of a slice (ou_small.hip)
 };
 constexpr int kSent = 27;  // items of one launch's kernel arguments
 struct Sent {
@@ -95,14 +96,18 @@ __device__ __forceinline__ TA gradient(const Item& it, int64_t at) {
 
 // A finished element of X: into the update and the weight.
 template <typename TA>
+__device__ __forceinline__ void put_update(const Item& it, int64_t at, TA x) {
+  if (sizeof(TA) == 4 && it.dtype == SC_BF16) static_cast<__bf16*>(it.update)[at] = static_cast<__bf16>(static_cast<float>(x));
+  else static_cast<TA*>(it.update)[at] = x;
+}
+template <typename TA>
+__device__ __forceinline__ TA new_weight(const Item& it, const Step& st, TA w, TA x) { return static_cast<TA>(st.keep) * w - static_cast<TA>(st.rate * it.scale) * x; }
+template <typename TA>
 __device__ __forceinline__ void finish(const Item& it, const Step& st, int64_t at, TA x) {
-  if (it.update) {
-    if (sizeof(TA) == 4 && it.dtype == SC_BF16) static_cast<__bf16*>(it.update)[at] = static_cast<__bf16>(static_cast<float>(x));
-    else static_cast<TA*>(it.update)[at] = x;
-  }
+  if (it.update) put_update(it, at, x);
   if (it.weight) {
     TA* const w = static_cast<TA*>(it.weight) + at;
-    *w = static_cast<TA>(st.keep) * *w - static_cast<TA>(st.rate * it.scale) * x;
+    *w = new_weight(it, st, *w, x);
   }
 }
 
@@ -133,8 +138,12 @@ void parts_place(Part& p, Item& it, int64_t count);
 void parts_layout(Part& p, Room& room, int steps);
 hipError_t parts_run(const Part& p, const ou_config* cfg, const Step& st, char* base, hipStream_t stream);
 
-// fp32 matrices of at most 64 x 64 and 128 x 128, a workgroup each from the gradient to the weight (ou_small.hip).
-hipError_t small_run(const Part& p, const ou_config* cfg, const Step& st, bool wide, const Item* items, hipStream_t stream);
+// fp32 matrices whose shorter side is at most 64 (large: 128): those whose longer side is too, from the gradient to the weight; and wider ones, from the sums of squares
+// on (ou_small.hip).
+hipError_t whole_run(const Part& p, const ou_config* cfg, const Step& st, bool large, char* base, hipStream_t stream);
+void slice_place(Part& p, Item& it, int64_t count, bool large);
+void slice_layout(Part& p, Room& room, int steps, bool large);
+hipError_t slice_run(const Part& p, const ou_config* cfg, const Step& st, bool large, char* base, hipStream_t stream);
 
 // The power of two that brings `top` to at most 2^14 (fp16 parts).
 int exponent_of(double top);

@@ -166,7 +166,11 @@ __global__ __launch_bounds__(kThreads) void product_kernel(const Item* __restric
 
 // ---- host side
 
-enum Way { kDouble, kParts, kSmall, kMiddle, kWays };
+// The ways: fp64; products in tiles; and matrices whose shorter side is at most 64 or 128, whole or in slices.
+enum Way { kDouble, kParts, kWhole64, kWhole128, kSlices64, kSlices128, kWays };
+bool whole(int way) { return way == kWhole64 || way == kWhole128; }
+bool sliced(int way) { return way == kSlices64 || way == kSlices128; }
+bool large(int way) { return way == kWhole128 || way == kSlices128; }
 
 // The tensors by the way that their matrices take, and where everything lies in the workspace.
 struct Layout {
@@ -174,10 +178,10 @@ struct Layout {
   size_t bytes = 0;
 };
 
-// A matrix that one workgroup can hold takes one launch instead of three a step.
+// One workgroup holds what it can: one launch, or one a step, instead of three a step.
 Way way_of(const ou_tensor& t) {
-  const int l = std::max(t.rows, t.cols);
-  return t.dtype == SC_F64 ? kDouble : l <= 64 ? kSmall : l <= 128 ? kMiddle : kParts;
+  const int m = std::min(t.rows, t.cols), l = std::max(t.rows, t.cols);
+  return t.dtype == SC_F64 ? kDouble : l <= 64 ? kWhole64 : l <= 128 ? kWhole128 : m <= 64 ? kSlices64 : m <= 128 ? kSlices128 : kParts;
 }
 
 void double_place(Part& p, Item& it, int64_t count) {
@@ -215,9 +219,10 @@ Layout layout_of(int64_t n, const ou_tensor* tensors, int steps) {
     it.rows = t.rows;
     it.cols = t.cols;
     it.dtype = t.dtype;
-    if (way == kDouble || way == kParts) p.units[kChunks] += t.count * ceil_div(static_cast<int64_t>(t.rows) * t.cols, kChunk);
+    if (!whole(way)) p.units[kChunks] += t.count * ceil_div(static_cast<int64_t>(t.rows) * t.cols, kChunk);
     if (way == kDouble) double_place(p, it, t.count);
     else if (way == kParts) parts_place(p, it, t.count);
+    else if (sliced(way)) slice_place(p, it, t.count, large(way));
     else p.units[kBlocks] += t.count;
     p.items.push_back(it);
   }
@@ -229,6 +234,7 @@ Layout layout_of(int64_t n, const ou_tensor* tensors, int steps) {
     p.at_partial = room(p.units[kChunks] * sizeof(double));
     if (way == kDouble) double_layout(p, room, steps);
     else if (way == kParts) parts_layout(p, room, steps);
+    else if (sliced(way)) slice_layout(p, room, steps, large(way));
   }
   l.bytes = std::max<size_t>(room.bytes, 256);
   return l;
@@ -383,19 +389,15 @@ sc_status ou_step(const ou_config* cfg, int64_t n_tensors, const ou_tensor* tens
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     char* const base = static_cast<char*>(workspace);
     hipError_t e = hipSuccess;
-    for (const Way way : {kMiddle, kSmall}) {
+    for (int way = 0; way < kWays && e == hipSuccess; ++way) {
       const Part& p = l.part[way];
-      if (e != hipSuccess || p.items.empty()) continue;
-      e = send(p, base, stream);
-      if (e == hipSuccess) e = small_run(p, cfg, step, way == kMiddle, reinterpret_cast<const Item*>(base + p.at_items), stream);
-    }
-    if (e == hipSuccess && !l.part[kParts].items.empty()) {
-      e = begin<float>(l.part[kParts], step, base, stream);
-      if (e == hipSuccess) e = parts_run(l.part[kParts], cfg, step, base, stream);
-    }
-    if (e == hipSuccess && !l.part[kDouble].items.empty()) {
-      e = begin<double>(l.part[kDouble], step, base, stream);
-      if (e == hipSuccess) e = double_run(l.part[kDouble], cfg, step, base, stream);
+      if (p.items.empty()) continue;
+      e = way == kDouble ? begin<double>(p, step, base, stream) : whole(way) ? send(p, base, stream) : begin<float>(p, step, base, stream);
+      if (e != hipSuccess) break;
+      e = way == kDouble  ? double_run(p, cfg, step, base, stream)
+          : way == kParts ? parts_run(p, cfg, step, base, stream)
+          : whole(way)    ? whole_run(p, cfg, step, large(way), base, stream)
+                          : slice_run(p, cfg, step, large(way), base, stream);
     }
     if (e != hipSuccess) return set_error(SC_ERR_HIP, std::string("ou_step: kernel launch: ") + hipGetErrorString(e));
   } catch (const std::bad_alloc&) {
