@@ -21,9 +21,11 @@ typedef float F16 __attribute__((ext_vector_type(16)));
 
 constexpr int kSlices = 32;
 
-// The powers of two of every step: they travel as kernel arguments.
-struct Exponents {
-  int8_t x[OU_MAX_STEPS + 1], s[OU_MAX_STEPS], p[OU_MAX_STEPS];
+// Powers of two: values to parts, and sums of parts to values.  The same for all steps (what a step could gain by its own is the growth of the bound over the
+// steps, a bit or less with the usual coefficients), so that none is looked up between two products.
+struct Scales {
+  float x_up, s_up, p_up;
+  float xx_down, ss_down, px_down;
 };
 
 template <int N>
@@ -59,12 +61,6 @@ __device__ __forceinline__ void multiply(const _Float16* a, const _Float16* b, i
   constexpr int kSide = S::kSide;
   const int lane = threadIdx.x & (kLanes - 1), wave = wave_of();
   typename S::Blocks small, other;
-#pragma unroll
-  for (int e = 0; e < kSide; ++e)
-#pragma unroll
-    for (int f = 0; f < kSide; ++f)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) sum[e][f][r] = small[e][f][r] = other[e][f][r] = 0;
   const _Float16* const pa = a + (wave / 2 * 32 + (lane & 31)) * S::kPitch + lane / 32 * 8;
   const _Float16* const pb = b + (wave % 2 * 32 + (lane & 31)) * S::kPitch + lane / 32 * 8;
   bool in_row[kSide], in_col[kSide];
@@ -73,7 +69,6 @@ __device__ __forceinline__ void multiply(const _Float16* a, const _Float16* b, i
     in_row[e] = 32 * (wave / 2 + 2 * e) < rows;
     in_col[e] = 32 * (wave % 2 + 2 * e) < cols;
   }
-  if (!in_row[0] || !in_col[0]) return;
   H8 x[2][kSide][2], y[2][kSide][2];
   auto load = [&](int to, int k) {
 #pragma unroll
@@ -84,26 +79,47 @@ __device__ __forceinline__ void multiply(const _Float16* a, const _Float16* b, i
         y[to][e][q] = *reinterpret_cast<const H8*>(pb + q * S::kPart + e * 64 * S::kPitch + k);
       }
   };
-  auto mma = [&](int at, int p, int q, typename S::Blocks& to) {
+  auto mma = [&](auto first, int at, int p, int q, typename S::Blocks& to) {
+#pragma unroll
+    for (int e = 0; e < kSide; ++e)
+#pragma unroll
+      for (int f = 0; f < kSide; ++f) {
+        if constexpr (decltype(first)::value) {
+          F16 zero;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) zero[r] = 0;
+          to[e][f] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[at][e][p], y[at][f][q], zero, 0, 0, 0);
+        } else {
+          to[e][f] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[at][e][p], y[at][f][q], to[e][f], 0, 0, 0);
+        }
+      }
+  };
+  // (a block outside rows x cols is computed from whatever stands there and never used; a wave without any block inside has nothing to do)
+  if (!in_row[0] || !in_col[0]) {
 #pragma unroll
     for (int e = 0; e < kSide; ++e)
 #pragma unroll
       for (int f = 0; f < kSide; ++f)
-        if (in_row[e] && in_col[f]) to[e][f] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[at][e][p], y[at][f][q], to[e][f], 0, 0, 0);
-  };
-  auto products = [&](int at) {
-    mma(at, 1, 0, small);
-    mma(at, 0, 0, sum);
-    if constexpr (kSide == 1) mma(at, 0, 1, other);   // (one block: a sum of its own, so that no instruction waits for the one before it)
-    else mma(at, 0, 1, small);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sum[e][f][r] = 0;
+    return;
+  }
+  auto products = [&](auto first, int at) {
+    mma(first, at, 1, 0, small);
+    mma(first, at, 0, 0, sum);
+    if constexpr (kSide == 1) mma(first, at, 0, 1, other);   // (one block: a sum of its own, so that no instruction waits for the one before it)
+    else mma(std::false_type{}, at, 0, 1, small);
   };
   load(0, 0);
-  for (int k = 0; k < depth; k += 32) {
+  load(1, 16);
+  products(std::true_type{}, 0);
+  for (int k = 32; k < depth; k += 32) {
+    load(0, k);
+    products(std::false_type{}, 1);
     load(1, k + 16);
-    products(0);
-    if (k + 32 < depth) load(0, k + 32);
-    products(1);
+    products(std::false_type{}, 0);
   }
+  products(std::false_type{}, 1);
 #pragma unroll
   for (int e = 0; e < kSide; ++e)
 #pragma unroll
@@ -113,134 +129,161 @@ __device__ __forceinline__ void multiply(const _Float16* a, const _Float16* b, i
     }
 }
 
-// Parts of the wave's blocks that begin inside rows x cols, transposed: a lane's four consecutive rows are neighbours there.
-template <int N>
-__device__ __forceinline__ void put_turned(const typename Shape<N>::Blocks& v, float up, int rows, int cols, _Float16* to) {
-  using S = Shape<N>;
-  const int lane = threadIdx.x & (kLanes - 1), wave = wave_of();
-#pragma unroll
-  for (int e = 0; e < S::kSide; ++e)
-#pragma unroll
-    for (int f = 0; f < S::kSide; ++f) {
-      const int i = 32 * (wave / 2 + 2 * e), j = 32 * (wave % 2 + 2 * f);
-      if (i >= rows || j >= cols) continue;
-      _Float16* const at = to + (j + (lane & 31)) * S::kPitch + i + lane / 32 * 4;
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        H4 h, l;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          _Float16 x, y;
-          split(v[e][f][4 * g + k] * up, x, y);
-          h[k] = x;
-          l[k] = y;
-        }
-        *reinterpret_cast<H4*>(at + 8 * g) = h;
-        *reinterpret_cast<H4*>(at + S::kPart + 8 * g) = l;
-      }
-    }
+// Two values as their first parts and their second ones.
+typedef _Float16 H2 __attribute__((ext_vector_type(2)));
+typedef float F2 __attribute__((ext_vector_type(2)));
+typedef unsigned U2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ void split2(float v, float w, unsigned& h, unsigned& l) {
+  const F2 x{v, w};
+  const H2 y = __builtin_convertvector(x, H2);
+  h = __builtin_bit_cast(unsigned, y);
+  l = __builtin_bit_cast(unsigned, __builtin_convertvector(x - __builtin_convertvector(y, F2), H2));
 }
-// And as they are: neighbouring lanes (columns) exchange halves, so that each writes two columns of one of two rows.
-template <int N>
-__device__ __forceinline__ void put_straight(const typename Shape<N>::Blocks& v, float up, int rows, int cols, _Float16* to) {
+
+// Parts of the wave's blocks that begin inside rows x cols, times `up`: transposed (a lane's four consecutive rows are neighbours there), and as they are
+// (neighbouring lanes, which are columns, exchange halves, so that each writes two columns of one of two rows).
+template <int N, bool kTurned, bool kStraight>
+__device__ __forceinline__ void put(const typename Shape<N>::Blocks& v, float up, int rows, int cols, _Float16* turned, _Float16* straight) {
   using S = Shape<N>;
-  typedef _Float16 H2 __attribute__((ext_vector_type(2)));
   const int lane = threadIdx.x & (kLanes - 1), wave = wave_of();
-  const unsigned select = lane & 1 ? 0x03020706u : 0x05040100u;   // odd: upper halves of the neighbour's and its own; even: lower halves of its own and the neighbour's
+  const unsigned select = lane & 1 ? 0x03020706u : 0x05040100u;   // odd: the neighbour's upper half, its own; even: its own lower half, the neighbour's
 #pragma unroll
   for (int e = 0; e < S::kSide; ++e)
 #pragma unroll
     for (int f = 0; f < S::kSide; ++f) {
       const int i = 32 * (wave / 2 + 2 * e), j = 32 * (wave % 2 + 2 * f);
       if (i >= rows || j >= cols) continue;
-      _Float16* const at = to + (i + lane / 32 * 4 + (lane & 1)) * S::kPitch + j + (lane & 30);
+      unsigned h[8], l[8];
 #pragma unroll
-      for (int r = 0; r < 16; r += 2) {
-        _Float16 h0, l0, h1, l1;
-        split(v[e][f][r] * up, h0, l0);
-        split(v[e][f][r + 1] * up, h1, l1);
-        const unsigned h = __builtin_bit_cast(unsigned, H2{h0, h1}), l = __builtin_bit_cast(unsigned, H2{l0, l1});
-        const unsigned hn = __builtin_amdgcn_update_dpp(0u, h, 0xB1, 0xf, 0xf, true), ln = __builtin_amdgcn_update_dpp(0u, l, 0xB1, 0xf, 0xf, true);
-        _Float16* const row = at + (8 * (r / 4) + r % 4) * S::kPitch;
-        *reinterpret_cast<unsigned*>(row) = __builtin_amdgcn_perm(hn, h, select);
-        *reinterpret_cast<unsigned*>(row + S::kPart) = __builtin_amdgcn_perm(ln, l, select);
+      for (int r = 0; r < 8; ++r) split2(v[e][f][2 * r] * up, v[e][f][2 * r + 1] * up, h[r], l[r]);
+      if constexpr (kTurned) {
+        _Float16* const at = turned + (j + (lane & 31)) * S::kPitch + i + lane / 32 * 4;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          *reinterpret_cast<U2*>(at + 8 * g) = U2{h[2 * g], h[2 * g + 1]};
+          *reinterpret_cast<U2*>(at + S::kPart + 8 * g) = U2{l[2 * g], l[2 * g + 1]};
+        }
+      }
+      if constexpr (kStraight) {
+        _Float16* const at = straight + (i + lane / 32 * 4 + (lane & 1)) * S::kPitch + j + (lane & 30);
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+          const unsigned hn = __builtin_amdgcn_update_dpp(0u, h[r], 0xB1, 0xf, 0xf, true), ln = __builtin_amdgcn_update_dpp(0u, l[r], 0xB1, 0xf, 0xf, true);
+          _Float16* const row = at + (8 * (r / 2) + 2 * (r % 2)) * S::kPitch;
+          *reinterpret_cast<unsigned*>(row) = __builtin_amdgcn_perm(hn, h[r], select);
+          *reinterpret_cast<unsigned*>(row + S::kPart) = __builtin_amdgcn_perm(ln, l[r], select);
+        }
       }
     }
 }
 
-// A matrix m x l and where its element (i, j) stands in the tensor.
+// A matrix m x l of a tensor; `first` is its first element.
 struct Matrix {
   int m, l;
   bool turned;
-  int64_t first;   // of the matrix in the tensor
-  __device__ __forceinline__ int64_t at(int i, int j) const { return first + (turned ? static_cast<int64_t>(j) * m + i : static_cast<int64_t>(i) * l + j); }
+  int64_t first;
 };
 __device__ __forceinline__ Matrix matrix_of(const Item& it, int64_t index) {
   const bool turned = it.rows > it.cols;
   return {turned ? it.cols : it.rows, turned ? it.rows : it.cols, turned, index * it.rows * it.cols};
 }
 
-// U of the lane's elements of columns j0 on, zero outside.  kMomentum: the momentum takes its step too.  (All requests before the first store.)
-template <int N, bool kMomentum>
-__device__ __forceinline__ void load_direction(const Item& it, const Step& st, const Matrix& mat, int j0, typename Shape<N>::Blocks& u) {
-  typename Shape<N>::Blocks old;
-  each_result<N>([&](int e, int f, int q, int i, int j) { u[e][f][q] = i < mat.m && j0 + j < mat.l ? gradient<float>(it, mat.at(i, j0 + j)) : 0.f; });
-  if (!it.momentum) return;
-  float* const momentum = static_cast<float*>(it.momentum);
-  const float mu = static_cast<float>(st.mu);
-  each_result<N>([&](int e, int f, int q, int i, int j) { old[e][f][q] = i < mat.m && j0 + j < mat.l ? momentum[mat.at(i, j0 + j)] : 0.f; });
+// Accesses to a matrix of a tensor go through a descriptor of it: those of elements outside read zero and write nothing, without a branch for each.  (At most
+// 128 x 65536 elements: 32-bit offsets.)
+template <int N>
+struct Places {
+  unsigned at[Shape<N>::kSide][Shape<N>::kSide][16];   // elements from the first, or far beyond the last
+};
+template <int N>
+__device__ __forceinline__ void places_of(const Matrix& mat, bool turned, int j0, Places<N>& places) {
   each_result<N>([&](int e, int f, int q, int i, int j) {
-    float v = old[e][f][q];
-    if constexpr (kMomentum) {
-      v = mu * v + u[e][f][q];
-      if (i < mat.m && j0 + j < mat.l) momentum[mat.at(i, j0 + j)] = v;
-    }
-    u[e][f][q] = direction(u[e][f][q], v, mu, st.nesterov);
+    const unsigned at = turned ? (j0 + j) * mat.m + i : i * mat.l + j0 + j;
+    places.at[e][f][q] = i < mat.m && j0 + j < mat.l ? at : 0x20000000u;
+  });
+}
+template <typename T>
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t descriptor(const T* p, const Matrix& mat) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(p), 0, static_cast<int>(sizeof(T)) * mat.m * mat.l, 0x00020000);
+}
+template <int N>
+__device__ __forceinline__ void load_f32(const float* p, const Matrix& mat, const Places<N>& places, typename Shape<N>::Blocks& v) {
+  const __amdgpu_buffer_rsrc_t d = descriptor(p, mat);
+  each_result<N>([&](int e, int f, int q, int, int) {
+    v[e][f][q] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(d, static_cast<int>(places.at[e][f][q] * 4u), 0, 0));
+  });
+}
+template <int N>
+__device__ __forceinline__ void store_f32(float* p, const Matrix& mat, const Places<N>& places, const typename Shape<N>::Blocks& v) {
+  const __amdgpu_buffer_rsrc_t d = descriptor(p, mat);
+  each_result<N>([&](int e, int f, int q, int, int) {
+    __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, static_cast<float>(v[e][f][q])), d, static_cast<int>(places.at[e][f][q] * 4u), 0, 0);
   });
 }
 
-template <int N>
-__device__ __forceinline__ void store_results(const Item& it, const Step& st, const Matrix& mat, int j0, const typename Shape<N>::Blocks& x) {
-  if (it.update) {
-    each_result<N>([&](int e, int f, int q, int i, int j) {
-      if (i < mat.m && j0 + j < mat.l) put_update<float>(it, mat.at(i, j0 + j), x[e][f][q]);
+// U of the lane's elements, zero outside.  kMomentum: the momentum takes its step too.
+template <int N, bool kMomentum>
+__device__ __forceinline__ void load_direction(const Item& it, const Step& st, const Matrix& mat, const Places<N>& places, typename Shape<N>::Blocks& u) {
+  if (it.dtype == SC_BF16) {
+    const __amdgpu_buffer_rsrc_t d = descriptor(static_cast<const __bf16*>(it.grad) + mat.first, mat);
+    each_result<N>([&](int e, int f, int q, int, int) {
+      const unsigned short bits = __builtin_amdgcn_raw_buffer_load_b16(d, static_cast<int>(places.at[e][f][q] * 2u), 0, 0);
+      u[e][f][q] = __builtin_bit_cast(float, static_cast<unsigned>(bits) << 16);
     });
+  } else {
+    load_f32<N>(static_cast<const float*>(it.grad) + mat.first, mat, places, u);
+  }
+  if (!it.momentum) return;
+  typename Shape<N>::Blocks v;
+  float* const momentum = static_cast<float*>(it.momentum) + mat.first;
+  const float mu = static_cast<float>(st.mu);
+  load_f32<N>(momentum, mat, places, v);
+  if constexpr (kMomentum) {
+    each_result<N>([&](int e, int f, int q, int, int) { v[e][f][q] = mu * v[e][f][q] + u[e][f][q]; });
+    store_f32<N>(momentum, mat, places, v);
+  }
+  const bool nesterov = st.nesterov;
+  each_result<N>([&](int e, int f, int q, int, int) { u[e][f][q] = direction(u[e][f][q], static_cast<float>(v[e][f][q]), mu, nesterov); });
+}
+
+template <int N>
+__device__ __forceinline__ void store_results(const Item& it, const Step& st, const Matrix& mat, const Places<N>& places, const typename Shape<N>::Blocks& x) {
+  if (it.update) {
+    if (it.dtype == SC_BF16) {
+      const __amdgpu_buffer_rsrc_t d = descriptor(static_cast<const __bf16*>(it.update) + mat.first, mat);
+      each_result<N>([&](int e, int f, int q, int, int) {
+        const unsigned short bits = __builtin_bit_cast(unsigned short, static_cast<__bf16>(static_cast<float>(x[e][f][q])));
+        __builtin_amdgcn_raw_buffer_store_b16(bits, d, static_cast<int>(places.at[e][f][q] * 2u), 0, 0);
+      });
+    } else {
+      store_f32<N>(static_cast<float*>(it.update) + mat.first, mat, places, x);
+    }
   }
   if (it.weight) {
-    typename Shape<N>::Blocks old;
-    float* const weight = static_cast<float*>(it.weight);
-    each_result<N>([&](int e, int f, int q, int i, int j) { old[e][f][q] = i < mat.m && j0 + j < mat.l ? weight[mat.at(i, j0 + j)] : 0.f; });
-    each_result<N>([&](int e, int f, int q, int i, int j) {
-      if (i < mat.m && j0 + j < mat.l) weight[mat.at(i, j0 + j)] = new_weight(it, st, old[e][f][q], x[e][f][q]);
-    });
+    typename Shape<N>::Blocks w;
+    float* const weight = static_cast<float*>(it.weight) + mat.first;
+    load_f32<N>(weight, mat, places, w);
+    each_result<N>([&](int e, int f, int q, int, int) { w[e][f][q] = new_weight(it, st, static_cast<float>(w[e][f][q]), static_cast<float>(x[e][f][q])); });
+    store_f32<N>(weight, mat, places, w);
   }
 }
 
-// P = b S + c S S from the sums of parts in s; its parts are left in `square`.  Begins and ends with the workgroup in step.
+// P = b S + c S S; its parts are left in `square`.  Begins and ends with the workgroup in step.
 template <int N>
-__device__ __forceinline__ void make_p(const Step& st, const Exponents& ex, int step, int m, int deep, _Float16* square, typename Shape<N>::Blocks& s) {
-  constexpr int kSide = Shape<N>::kSide;
+__device__ __forceinline__ void make_p(const Step& st, const Scales& sc, int m, int deep, _Float16* square, const typename Shape<N>::Blocks& s) {
   typename Shape<N>::Blocks r;
-  put_turned<N>(s, __builtin_ldexpf(1.f, ex.s[step]), m, m, square);   // (symmetric)
+  put<N, true, false>(s, sc.s_up, m, m, square, nullptr);   // (symmetric)
   __syncthreads();
   multiply<N>(square, square, m, m, deep, r);
   __syncthreads();
-  const float cb = static_cast<float>(st.b), scale = static_cast<float>(st.c) * __builtin_ldexpf(1.f, -2 * ex.s[step]);
-#pragma unroll
-  for (int e = 0; e < kSide; ++e)
-#pragma unroll
-    for (int f = 0; f < kSide; ++f) r[e][f] = cb * s[e][f] + scale * r[e][f];
-  put_turned<N>(r, __builtin_ldexpf(1.f, ex.p[step]), m, m, square);
-  __syncthreads();
-}
-
-template <int N>
-__device__ __forceinline__ void scale_by(float v, typename Shape<N>::Blocks& s) {
+  const float cb = static_cast<float>(st.b), scale = static_cast<float>(st.c) * sc.ss_down;
 #pragma unroll
   for (int e = 0; e < Shape<N>::kSide; ++e)
 #pragma unroll
-    for (int f = 0; f < Shape<N>::kSide; ++f) s[e][f] *= v;
+    for (int f = 0; f < Shape<N>::kSide; ++f) r[e][f] = cb * s[e][f] + scale * r[e][f];
+  put<N, true, false>(r, sc.p_up, m, m, square, nullptr);
+  __syncthreads();
 }
+
 template <int N>
 __device__ __forceinline__ void next_x(float a, float scale, const typename Shape<N>::Blocks& r, typename Shape<N>::Blocks& x) {
 #pragma unroll
@@ -249,9 +292,9 @@ __device__ __forceinline__ void next_x(float a, float scale, const typename Shap
     for (int f = 0; f < Shape<N>::kSide; ++f) x[e][f] = a * x[e][f] + scale * r[e][f];
 }
 
-// A matrix of m, l <= N.  Rows and columns of parts up to the next multiple of 32 are zeros, those beyond are never read.
+// A matrix of m, l <= N.  Rows and columns of parts up to the next multiple of 32 are zeros, those beyond are never used.
 template <int N>
-__global__ __launch_bounds__(kThreads) void whole_kernel(const Item* __restrict__ items, int n, const Step st, int steps, const Exponents ex) {
+__global__ __launch_bounds__(kThreads) void whole_kernel(const Item* __restrict__ items, int n, const Step st, int steps, const Scales sc) {
   using S = Shape<N>;
   extern __shared__ __attribute__((aligned(16))) _Float16 lds[];
   _Float16* const square = lds;
@@ -260,31 +303,39 @@ __global__ __launch_bounds__(kThreads) void whole_kernel(const Item* __restrict_
   const Matrix mat = matrix_of(it, blockIdx.x - it.unit[kBlocks]);
   const int m = mat.m, l = mat.l, deep_l = (l + 31) / 32 * 32, deep_m = (m + 31) / 32 * 32;
   typename S::Blocks x, s, r;
-  load_direction<N, true>(it, st, mat, 0, x);
+  {
+    Places<N> places;
+    places_of<N>(mat, mat.turned, 0, places);
+    load_direction<N, true>(it, st, mat, places, x);
+  }
   double sum = 0;
   each_result<N>([&](int e, int f, int q, int, int) { sum = fma(static_cast<double>(x[e][f][q]), static_cast<double>(x[e][f][q]), sum); });
   const double down = 1.0 / (sqrt(workgroup_sum(sum, reinterpret_cast<double*>(lds))) + st.eps);
   each_result<N>([&](int e, int f, int q, int, int) { x[e][f][q] = static_cast<float>(static_cast<double>(x[e][f][q]) * down); });
+  const float ca = static_cast<float>(st.a);
   for (int step = 0; step < steps; ++step) {
-    const float up = __builtin_ldexpf(1.f, ex.x[step]);
-    put_straight<N>(x, up, m, l, square);
-    put_turned<N>(x, up, m, l, turned_x);
+    put<N, true, true>(x, sc.x_up, m, l, turned_x, square);
     __syncthreads();
     multiply<N>(square, square, m, m, deep_l, s);
     __syncthreads();
-    scale_by<N>(__builtin_ldexpf(1.f, -2 * ex.x[step]), s);
-    make_p<N>(st, ex, step, m, deep_m, square, s);
+#pragma unroll
+    for (int e = 0; e < S::kSide; ++e)
+#pragma unroll
+      for (int f = 0; f < S::kSide; ++f) s[e][f] *= sc.xx_down;
+    make_p<N>(st, sc, m, deep_m, square, s);
     multiply<N>(square, turned_x, m, l, deep_m, r);
-    next_x<N>(static_cast<float>(st.a), __builtin_ldexpf(1.f, -ex.p[step] - ex.x[step]), r, x);
+    next_x<N>(ca, sc.px_down, r, x);
     __syncthreads();
   }
-  store_results<N>(it, st, mat, 0, x);
+  Places<N> places;
+  places_of<N>(mat, mat.turned, 0, places);
+  store_results<N>(it, st, mat, places, x);
 }
 
 // Slices of `width` columns (a multiple of N) of a matrix of m <= N.  step 0: X from the gradient; then the step before `step` of the iteration; the last one leaves the
 // results.  partial: the slices' shares of S, in the order of the registers.
 template <int N>
-__global__ __launch_bounds__(kThreads) void slice_kernel(const Item* __restrict__ items, int n, const Step st, int step, bool last, const Exponents ex,
+__global__ __launch_bounds__(kThreads) void slice_kernel(const Item* __restrict__ items, int n, const Step st, int step, bool last, const Scales sc,
                                                          const double* __restrict__ squares, float* __restrict__ X, const float* __restrict__ partial,
                                                          float* __restrict__ next_partial) {
   using S = Shape<N>;
@@ -301,17 +352,17 @@ __global__ __launch_bounds__(kThreads) void slice_kernel(const Item* __restrict_
   float* const x_of = X + it.x + mat.first;
   typename S::Blocks x, s, r;
   double down = 0;
+#pragma unroll
+  for (int e = 0; e < kSide; ++e)
+#pragma unroll
+    for (int f = 0; f < kSide; ++f)
+#pragma unroll
+      for (int q = 0; q < 16; ++q) s[e][f][q] = 0;
   if (step == 0) {
     const int64_t per = chunks_of(static_cast<int64_t>(m) * l);
     down = down_of(squares + it.unit[kChunks] + index * per, per, st.eps, reinterpret_cast<double*>(lds));
   } else {
     const float* from = partial + (blockIdx.x - own) * static_cast<int64_t>(S::kResults) + threadIdx.x;
-#pragma unroll
-    for (int e = 0; e < kSide; ++e)
-#pragma unroll
-      for (int f = 0; f < kSide; ++f)
-#pragma unroll
-        for (int q = 0; q < 16; ++q) s[e][f][q] = 0;
 #pragma unroll 2
     for (int k = 0; k < slices; ++k, from += S::kResults) {
 #pragma unroll
@@ -321,43 +372,43 @@ __global__ __launch_bounds__(kThreads) void slice_kernel(const Item* __restrict_
 #pragma unroll
           for (int q = 0; q < 16; ++q) s[e][f][q] += from[((e * kSide + f) * 16 + q) * kThreads];
     }
-    make_p<N>(st, ex, step - 1, m, deep_m, square, s);
-  }
-#pragma unroll
-  for (int e = 0; e < kSide; ++e)
-#pragma unroll
-    for (int f = 0; f < kSide; ++f)
-#pragma unroll
-      for (int q = 0; q < 16; ++q) s[e][f][q] = 0;
-  for (int j0 = own * width; j0 < end; j0 += N) {
-    const int columns = min(l - j0, N);
-    if (step == 0) {
-      load_direction<N, false>(it, st, mat, j0, x);
-      each_result<N>([&](int e, int f, int q, int, int) { x[e][f][q] = static_cast<float>(static_cast<double>(x[e][f][q]) * down); });
-    } else {
-      each_result<N>([&](int e, int f, int q, int i, int j) { x[e][f][q] = i < m && j0 + j < l ? x_of[static_cast<int64_t>(i) * l + j0 + j] : 0.f; });
-      put_turned<N>(x, __builtin_ldexpf(1.f, ex.x[step - 1]), m, columns, slice);
-      __syncthreads();
-      multiply<N>(square, slice, m, columns, deep_m, r);
-      next_x<N>(static_cast<float>(st.a), __builtin_ldexpf(1.f, -ex.p[step - 1] - ex.x[step - 1]), r, x);
-      __syncthreads();
-    }
-    if (last) {
-      store_results<N>(it, st, mat, j0, x);
-      continue;
-    }
-    each_result<N>([&](int e, int f, int q, int i, int j) {
-      if (i < m && j0 + j < l) x_of[static_cast<int64_t>(i) * l + j0 + j] = x[e][f][q];
-    });
-    // (columns beyond the last one of the matrix hold zeros or what came of the parts' zeros; they are inside the multiple of 32 that is read)
-    put_straight<N>(x, __builtin_ldexpf(1.f, ex.x[step]), m, columns, slice);
-    __syncthreads();
-    multiply<N>(slice, slice, m, m, (columns + 31) / 32 * 32, r);
-    const float scale = __builtin_ldexpf(1.f, -2 * ex.x[step]);
+    make_p<N>(st, sc, m, deep_m, square, s);
 #pragma unroll
     for (int e = 0; e < kSide; ++e)
 #pragma unroll
-      for (int f = 0; f < kSide; ++f) s[e][f] += scale * r[e][f];
+      for (int f = 0; f < kSide; ++f)
+#pragma unroll
+        for (int q = 0; q < 16; ++q) s[e][f][q] = 0;
+  }
+  for (int j0 = own * width; j0 < end; j0 += N) {
+    const int columns = min(l - j0, N);
+    Places<N> places, in_x;   // in the tensor; in X, which is kept as m x l
+    places_of<N>(mat, mat.turned, j0, places);
+    places_of<N>(mat, false, j0, in_x);
+    if (step == 0) {
+      load_direction<N, false>(it, st, mat, places, x);
+      each_result<N>([&](int e, int f, int q, int, int) { x[e][f][q] = static_cast<float>(static_cast<double>(x[e][f][q]) * down); });
+    } else {
+      load_f32<N>(x_of, mat, in_x, x);
+      put<N, true, false>(x, sc.x_up, m, columns, slice, nullptr);
+      __syncthreads();
+      multiply<N>(square, slice, m, columns, deep_m, r);
+      next_x<N>(static_cast<float>(st.a), sc.px_down, r, x);
+      __syncthreads();
+    }
+    if (last) {
+      store_results<N>(it, st, mat, places, x);
+      continue;
+    }
+    store_f32<N>(x_of, mat, in_x, x);
+    // (the columns up to the next multiple of 32 are read too: they hold zeros, made of the parts' zeros)
+    put<N, false, true>(x, sc.x_up, m, columns, nullptr, slice);
+    __syncthreads();
+    multiply<N>(slice, slice, m, m, (columns + 31) / 32 * 32, r);
+#pragma unroll
+    for (int e = 0; e < kSide; ++e)
+#pragma unroll
+      for (int f = 0; f < kSide; ++f) s[e][f] += sc.xx_down * r[e][f];
     __syncthreads();
   }
   if (last) return;
@@ -380,28 +431,25 @@ hipError_t launch(Kernel kernel, int bytes, int64_t grid, hipStream_t stream, Ar
   return hipGetLastError();
 }
 
-Exponents exponents_of(const ou_config* cfg) {
-  Exponents ex{};
-  double top = 1;
+Scales scales_of(const ou_config* cfg) {
+  double top = 1, most = 1;
   for (int i = 0; i < cfg->steps; ++i) {
-    const double square = top * top;
-    ex.x[i] = static_cast<int8_t>(exponent_of(top));
-    ex.s[i] = static_cast<int8_t>(exponent_of(square));
-    ex.p[i] = static_cast<int8_t>(exponent_of(std::fabs(cfg->b) * square + std::fabs(cfg->c) * square * square));
     top = growth(cfg, top);
+    most = std::max(most, top);
   }
-  ex.x[cfg->steps] = static_cast<int8_t>(exponent_of(top));
-  return ex;
+  const double square = most * most;
+  const int x = exponent_of(most), s = exponent_of(square), p = exponent_of(std::fabs(cfg->b) * square + std::fabs(cfg->c) * square * square);
+  return {std::ldexp(1.f, x), std::ldexp(1.f, s), std::ldexp(1.f, p), std::ldexp(1.f, -2 * x), std::ldexp(1.f, -2 * s), std::ldexp(1.f, -p - x)};
 }
 
 template <int N>
 hipError_t slices(const Part& p, const ou_config* cfg, const Step& st, char* base, const Item* items, hipStream_t stream) {
-  const Exponents ex = exponents_of(cfg);
+  const Scales sc = scales_of(cfg);
   float* const partial[2] = {reinterpret_cast<float*>(base + p.at[0]), reinterpret_cast<float*>(base + p.at[1])};
   const double* const squares = reinterpret_cast<const double*>(base + p.at_partial);
   hipError_t e = hipSuccess;
   for (int step = 0; step <= cfg->steps && e == hipSuccess; ++step)
-    e = launch(&slice_kernel<N>, Shape<N>::kBytes, p.units[kBlocks], stream, items, static_cast<int>(p.items.size()), st, step, step == cfg->steps, ex, squares,
+    e = launch(&slice_kernel<N>, Shape<N>::kBytes, p.units[kBlocks], stream, items, static_cast<int>(p.items.size()), st, step, step == cfg->steps, sc, squares,
                reinterpret_cast<float*>(base + p.at_x), static_cast<const float*>(partial[(step + 1) & 1]), partial[step & 1]);
   return e;
 }
@@ -430,11 +478,11 @@ hipError_t slice_run(const Part& p, const ou_config* cfg, const Step& st, bool l
 }
 
 hipError_t whole_run(const Part& p, const ou_config* cfg, const Step& st, bool large, char* base, hipStream_t stream) {
-  const Exponents ex = exponents_of(cfg);
+  const Scales sc = scales_of(cfg);
   const Item* const items = reinterpret_cast<const Item*>(base + p.at_items);
   const int n = static_cast<int>(p.items.size());
-  return large ? launch(&whole_kernel<128>, Shape<128>::kBytes, p.units[kBlocks], stream, items, n, st, cfg->steps, ex)
-               : launch(&whole_kernel<64>, Shape<64>::kBytes, p.units[kBlocks], stream, items, n, st, cfg->steps, ex);
+  return large ? launch(&whole_kernel<128>, Shape<128>::kBytes, p.units[kBlocks], stream, items, n, st, cfg->steps, sc)
+               : launch(&whole_kernel<64>, Shape<64>::kBytes, p.units[kBlocks], stream, items, n, st, cfg->steps, sc);
 }
 
 }  // namespace ou
