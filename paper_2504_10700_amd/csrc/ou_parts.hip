@@ -37,7 +37,9 @@ constexpr int kXcds = 8;
 #endif
 constexpr int kFewTiles = OU_FEW;
 
-__host__ __device__ constexpr int64_t padded(int64_t n) { return (n + kPad - 1) / kPad * kPad; }
+// Columns of a row of parts in memory: an odd multiple of 32, so that the rows of a tile spread over the channels of the caches.
+__host__ __device__ constexpr int64_t padded(int64_t n) { return ((n + kPad - 1) / kPad | 1) * kPad; }
+
 
 // Buffers.  Parts: [rows][padded columns / 32][h, l][32] of each matrix: what a stage reads of a row is one line of the caches (with h and l apart, and so half
 // lines: 4096 x 4096 twice @@ms instead of 9.8).
@@ -221,59 +223,107 @@ __global__ __launch_bounds__(kThreads, kStages == 2 ? 2 : 1) void product_kernel
     const int r = half + 8 * q + lane / 8;
     offset[q] = 2u * (static_cast<unsigned>(min(r, left - 1)) * static_cast<unsigned>(ld) + 8u * ((lane % 8) ^ swizzle(r)));
   }
-  const int stages = static_cast<int>(ld / kRow);
+  const int stages = ((kPhase == kS ? l : m) + kDepth - 1) / kDepth;
   _Float16* const mine = lds + wave / 2 * kOperand + half * kRow;
   const int wi = wave / 2 * 32 * kSide, wj = wave % 2 * 32 * kSide;
 
-  F16 sum[kSide][kSide], part[kSide][kSide];
+  // (one block: each of the three products has a sum of its own, so that no instruction waits for the one before it)
+  constexpr int kSums = kSide == 1 ? 3 : 1;
+  F16 sum[kSide][kSide], part[kSums][kSide][kSide];
 #pragma unroll
   for (int x = 0; x < kSide; ++x)
 #pragma unroll
     for (int y = 0; y < kSide; ++y)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) sum[x][y][r] = part[x][y][r] = 0;
+      for (int r = 0; r < 16; ++r) sum[x][y][r] = 0;
 
-  // stage t stands in slot t % kStages; a slot is filled again once all waves have passed the barrier after its use
-  int filled = 0, slot = 0;
-  for (; filled < kStages - 1 && filled < stages; ++filled) load_rows<kLoads>(from + filled * kRow, offset, mine + filled * kStage);
-  int to = filled;   // (only used when there are stages left: then it is kStages - 1)
-  for (int t = 0; t < stages; ++t) {
-    stage_arrived<kStages - 2, kLoads>(stages - 1 - t);
-    if (filled < stages) {
-      load_rows<kLoads>(from + static_cast<int64_t>(filled) * kRow, offset, mine + to * kStage);
-      ++filled;
-      to = to + 1 == kStages ? 0 : to + 1;
-    }
-    const _Float16* const here = lds + slot * kStage;
-    slot = slot + 1 == kStages ? 0 : slot + 1;
+  struct Operands {
+    H8 x[2][kSide][2], y[2][kSide][2];   // [16 indices][block][part]
+  };
+  auto read = [&](const _Float16* here, Operands& o) {
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      H8 x[kSide][2], y[kSide][2];   // [block][part]
+    for (int s = 0; s < 2; ++s)
 #pragma unroll
       for (int e = 0; e < kSide; ++e)
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
           const int r = e * 32 + (lane & 31), piece = ((4 * q + 2 * s + lane / 32) ^ swizzle(r)) * 8;   // (wi and wj are multiples of 32)
-          x[e][q] = *reinterpret_cast<const H8*>(here + (wi + r) * kRow + piece);
-          y[e][q] = *reinterpret_cast<const H8*>(here + kOperand + (wj + r) * kRow + piece);
+          o.x[s][e][q] = *reinterpret_cast<const H8*>(here + (wi + r) * kRow + piece);
+          o.y[s][e][q] = *reinterpret_cast<const H8*>(here + kOperand + (wj + r) * kRow + piece);
         }
+  };
+  auto multiply = [&](const Operands& o, int from_s, int to_s) {
+#pragma unroll
+    for (int s = from_s; s < to_s; ++s)
 #pragma unroll
       for (int q = 0; q < 3; ++q)   // l h, h l, h h
 #pragma unroll
         for (int e = 0; e < kSide; ++e)
 #pragma unroll
-          for (int f = 0; f < kSide; ++f) part[e][f] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[e][q == 0], y[f][q == 1], part[e][f], 0, 0, 0);
-    }
-    if ((t + 1) % (kFlush / kDepth) == 0 || t + 1 == stages) {
+          for (int f = 0; f < kSide; ++f) {
+            F16& sums = part[kSums == 3 ? q : 0][e][f];
+            sums = __builtin_amdgcn_mfma_f32_32x32x16_f16(o.x[s][e][q == 0], o.y[s][f][q == 1], sums, 0, 0, 0);
+          }
+  };
+  // stage t stands in slot t % kStages
+  int filled = 0, slot = 0, to = 0;
+  auto fill = [&] {
+    load_rows<kLoads>(from + static_cast<int64_t>(filled) * kRow, offset, mine + to * kStage);
+    ++filled;
+    to = to + 1 == kStages ? 0 : to + 1;
+  };
+  auto next_slot = [&] {
+    const _Float16* const here = lds + slot * kStage;
+    slot = slot + 1 == kStages ? 0 : slot + 1;
+    return here;
+  };
+  while (filled < kStages - 1 && filled < stages) fill();
+  // One block: a stage's operands are read while the one before it is multiplied, so that neither the reads nor the barrier are waited for alone.  A slot is filled again
+  // after the barrier that follows the products of its stage.
+  constexpr bool kAhead = kSide == 1;
+  Operands operands[kAhead ? 2 : 1];
+  if constexpr (kAhead) {
+    stage_arrived<kStages - 2, kLoads>(stages - 1);
+    read(next_slot(), operands[0]);
+  }
+  for (int first = 0; first < stages; first += kFlush / kDepth) {
+#pragma unroll
+    for (int k = 0; k < kSums; ++k)
 #pragma unroll
       for (int e = 0; e < kSide; ++e)
 #pragma unroll
-        for (int f = 0; f < kSide; ++f) {
-          sum[e][f] += part[e][f];
+        for (int f = 0; f < kSide; ++f)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) part[e][f][r] = 0;
-        }
+          for (int r = 0; r < 16; ++r) part[k][e][f][r] = 0;
+    if constexpr (kAhead) {
+#pragma unroll
+      for (int u = 0; u < kFlush / kDepth; ++u) {
+        const int t = first + u;
+        if (t >= stages) break;
+        if (t + 1 < stages) stage_arrived<kStages - 3, kLoads>(stages - 2 - t);
+        read(next_slot(), operands[(u + 1) & 1]);   // (after the last stage: whatever stands in the slot, not used)
+        // (the requests go out while the matrix core works)
+        multiply(operands[u & 1], 0, 1);
+        __builtin_amdgcn_sched_barrier(0);
+        if (filled < stages && t + 1 < stages) fill();
+        multiply(operands[u & 1], 1, 2);
+      }
+    } else {
+      const int until = min(first + kFlush / kDepth, stages);
+      for (int t = first; t < until; ++t) {
+        stage_arrived<kStages - 2, kLoads>(stages - 1 - t);
+        if (filled < stages) fill();
+        read(next_slot(), operands[0]);
+        multiply(operands[0], 0, 2);
+      }
     }
+#pragma unroll
+    for (int e = 0; e < kSide; ++e)
+#pragma unroll
+      for (int f = 0; f < kSide; ++f) {
+        if constexpr (kSums == 3) sum[e][f] += part[2][e][f] + (part[0][e][f] + part[1][e][f]);
+        else sum[e][f] += part[0][e][f];
+      }
   }
 
   // results, 32 x 32 at a time through the wave's corner of LDS: row by row, then column by column
