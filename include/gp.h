@@ -44,7 +44,7 @@ extern "C" {
 #define GP_MAX_COMPONENTS 64
 #define GP_MAX_STRIDE 33554432 /* largest ld_in and ld_out                         */
 #define GP_MAX_ROWS 536870912  /* largest n_nodes * components                      */
-#define GP_UNGROUPED 32        /* batches of at most so many atoms need no grouping */
+#define GP_UNGROUPED 64        /* batches of at most so many atoms need no grouping */
 
 typedef struct {
   int32_t struct_size;  /* = sizeof(gp_config), ABI guard                          */

@@ -46,10 +46,17 @@ struct Place {
   int begin, atoms;   // positions of the bucket in the order
 };
 
-// units(atoms): of a bucket.  A bucket of several units has a slot for each of them, one of a single unit none.  The whole wave calls it; every lane sums
-// the buckets of its stretch.
+// Which unit a workgroup takes: consecutive ones go to the same XCD (workgroups are dealt out to the XCDs in turn), whose L2 then holds the weights that they share.
+constexpr int kXcds = 8;
+__device__ __forceinline__ int64_t unit_of(int64_t block, int64_t total) {
+  const int64_t per = (total + kXcds - 1) / kXcds, u = block % kXcds * per + block / kXcds;
+  return block / kXcds < per ? u : total;
+}
+
+// units(atoms): of a bucket.  A bucket of several units has a slot for each of them, one of a single unit none.  `each`: workgroups of a unit; `block` is the
+// workgroup, *which its number among the unit's.  The whole wave calls it; every lane sums the buckets of its stretch.
 template <typename U>
-__device__ __forceinline__ Place place_of(const int32_t* __restrict__ offsets, int buckets, int64_t n, int unit, U&& units) {
+__device__ __forceinline__ Place place_of(const int32_t* __restrict__ offsets, int buckets, int64_t n, int64_t block, int each, U&& units, int* which) {
   const int lane = threadIdx.x & (kLanes - 1);
   const int per = (buckets + kLanes - 1) / kLanes, first = lane * per;
   const int most = static_cast<int>(n);
@@ -74,9 +81,13 @@ __device__ __forceinline__ Place place_of(const int32_t* __restrict__ offsets, i
       s_end += b;
     }
   }
-  const unsigned long long mine = __builtin_amdgcn_ballot_w64(unit < u_end);
-  if (mine == 0) return {-1, 0, 0, 0, 0, 0};
-  const int owner = __builtin_ctzll(mine);
+  const int total = __builtin_amdgcn_readlane(u_end, kLanes - 1);
+  const int64_t mine = unit_of(block, static_cast<int64_t>(total) * each);
+  const int unit = static_cast<int>(mine / each);
+  *which = static_cast<int>(mine - static_cast<int64_t>(unit) * each);
+  const unsigned long long beyond = __builtin_amdgcn_ballot_w64(unit < u_end);
+  if (beyond == 0) return {-1, 0, 0, 0, 0, 0};
+  const int owner = __builtin_ctzll(beyond);
   int local = unit - __builtin_amdgcn_readlane(u_end - u, owner);
   int slot = __builtin_amdgcn_readlane(s_end - s, owner);
   int bucket = owner * per;
@@ -94,5 +105,57 @@ __device__ __forceinline__ Place place_of(const int32_t* __restrict__ offsets, i
   return {__builtin_amdgcn_readfirstlane(bucket), __builtin_amdgcn_readfirstlane(local), __builtin_amdgcn_readfirstlane(k),
           __builtin_amdgcn_readfirstlane(slot), __builtin_amdgcn_readfirstlane(from), __builtin_amdgcn_readfirstlane(atoms)};
 }
+
+// ---- the products' arguments
+
+struct Rows {
+  int64_t n;            // atoms
+  int64_t ld_src, ld_dst;
+  const int32_t* z;
+  Grouping group;       // offsets NULL: none
+  int elements, components;
+  int reduced, columns;
+  const void* src;
+  const void* W;        // [elements][k_in][k_out]
+  const void* residual;
+  void* dst;
+};
+
+struct Outer {
+  int64_t n;
+  int64_t ld_in, ld_out;
+  const int32_t* z;
+  Grouping group;
+  int elements, components;
+  int k_in, k_out;
+  int per;              // rows of a chunk
+  const void* X;
+  const void* dY;
+  void* dW;
+  void* partial;        // [slots][k_in][k_out]
+};
+
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Where row r of a bucket begins: component r % components of atom r / components.
+__device__ __forceinline__ int64_t row_offset(const int32_t* order, int64_t n, int begin, int r, int components, int64_t ld, int width) {
+  const int a = components == 1 ? r : static_cast<int>(static_cast<unsigned>(r) / static_cast<unsigned>(components));
+  const int64_t atom = min(static_cast<unsigned>(order[begin + a]), static_cast<unsigned>(n - 1));
+  return atom * ld + static_cast<int64_t>(r - a * components) * width;
+}
+template <typename T>
+__device__ __forceinline__ T* row_at(T* p, const int32_t* order, int64_t n, int begin, int r, int components, int64_t ld, int width) {
+  return p + row_offset(order, n, begin, r, components, ld, width);
+}
+
+// An element without rows has a chunk too, which zeroes its matrix.
+__device__ __forceinline__ int chunks_of(int rows, int per) { return max(1, static_cast<int>((static_cast<unsigned>(rows) + per - 1) / static_cast<unsigned>(per))); }
+
+// Widths that are multiples of 8, on bfloat16 parts (gp_parts.hip).  T: SC_F32 or SC_BF16 rows.
+bool parts_serve(const gp_config* c);
+hipError_t launch_rows_parts(const gp_config* c, const Rows& a, bool back, hipStream_t stream);
+hipError_t launch_outer_parts(const gp_config* c, const Outer& a, hipStream_t stream);
+// Batches without a grouping: rows (gp_few.hip).
+hipError_t launch_rows_few(const gp_config* c, const Rows& a, bool back, hipStream_t stream);
 
 }  // namespace gp

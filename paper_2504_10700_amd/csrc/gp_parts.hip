@@ -1,0 +1,368 @@
+// The products by element on the bfloat16 matrix cores, for widths that are multiples of 8.
+//
+// An fp32 value is the sum of three bfloat16 parts h + m + l (el::split_pair), a bfloat16 row its own only part.  Rows of fp32: h h' and the five products
+// h m', m h', m m', h l', l h' (what is left out is below 2^-24 of the product); rows of bfloat16 with W: three products; dW of bfloat16 rows: one.  An instruction cuts
+// off what is below the last bit of the sum it adds to, so a sum of fp32 results goes over 32 indices, smaller products first, and then joins an fp32
+// sum; results that are rounded to bfloat16 take one sum throughout.  Values that the parts do not stand for (not finite, beyond the largest bfloat16,
+// below 2^-110) are noted, and the tile is computed by the blocks of gp_blocks.h.
+//
+// A workgroup: 128 rows of a bucket x 128 columns, or 128 x 128 of an element's dW over a chunk of rows, four waves of 64 x 64.  32 reduced indices of both
+// operands are requested while the 32 before are multiplied, and pass through registers, where they are split, to LDS.  One set of LDS and two barriers a
+// stage: the two workgroups of a compute unit fill each other's waits.
+#include <algorithm>
+
+#include "gp_blocks.h"
+
+namespace gp {
+namespace {
+
+typedef __bf16 B8 __attribute__((ext_vector_type(8)));
+typedef float F16 __attribute__((ext_vector_type(16)));
+typedef float F4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef float F2 __attribute__((ext_vector_type(2), aligned(4)));
+typedef unsigned U4 __attribute__((ext_vector_type(4)));
+typedef unsigned U4Loose __attribute__((ext_vector_type(4), aligned(2)));
+typedef unsigned ULoose __attribute__((aligned(2)));
+
+constexpr int kTile = 128, kStage = 32;
+constexpr int kPlane = kTile * kStage;   // elements of one part of one operand: rows of 64 bytes
+constexpr int64_t kMaxGrid = int64_t(1) << 23;
+
+template <typename T>
+constexpr int parts() { return sizeof(T) == 2 ? 1 : 3; }
+
+// Rows 0..7, and the even and the odd ones of 16, have their four pieces at different places.
+__device__ __forceinline__ int swizzle(int row) { return ((row >> 1) & 3) ^ ((row >> 3) & 1); }
+
+__device__ __forceinline__ void barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }   // (requests to memory stay under way)
+
+// Eight reduced indices of one row of an operand: raw elements, and as its parts in LDS.
+template <typename T>
+struct Eight;
+template <>
+struct Eight<float> {
+  F4 v[2];
+  __device__ __forceinline__ void request(const float* p) {
+    v[0] = *reinterpret_cast<const F4*>(p);
+    v[1] = *reinterpret_cast<const F4*>(p + 4);
+  }
+  __device__ __forceinline__ void put(bool inside, __bf16* to, unsigned& low) const {
+    U4 p[3];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const el::SplitPair s = el::split_pair(inside ? v[i / 2][2 * (i % 2)] : 0.f, inside ? v[i / 2][2 * (i % 2) + 1] : 0.f, low);
+      p[0][i] = s.h;
+      p[1][i] = s.m;
+      p[2][i] = s.l;
+    }
+#pragma unroll
+    for (int q = 0; q < 3; ++q) *reinterpret_cast<U4*>(to + q * kPlane) = p[q];
+  }
+};
+template <>
+struct Eight<__bf16> {
+  U4 v;
+  __device__ __forceinline__ void request(const __bf16* p) { v = *reinterpret_cast<const U4Loose*>(p); }
+  __device__ __forceinline__ void put(bool inside, __bf16* to, unsigned&) const { *reinterpret_cast<U4*>(to) = inside ? v : U4{0, 0, 0, 0}; }
+};
+
+// Eight reduced indices of two neighbouring columns, from eight rows of an operand whose rows are the reduced index.
+template <typename T>
+struct TwoColumns;
+template <>
+struct TwoColumns<float> {
+  F2 v[8];
+  __device__ __forceinline__ void request(int i, const float* p) { v[i] = *reinterpret_cast<const F2*>(p); }
+  // inside: how many of the eight there are
+  __device__ __forceinline__ void put(int inside, int piece, int row, __bf16* to, unsigned& low) const {
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      U4 p[3];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const el::SplitPair s = el::split_pair(2 * i < inside ? v[2 * i][c] : 0.f, 2 * i + 1 < inside ? v[2 * i + 1][c] : 0.f, low);
+        p[0][i] = s.h;
+        p[1][i] = s.m;
+        p[2][i] = s.l;
+      }
+#pragma unroll
+      for (int q = 0; q < 3; ++q) *reinterpret_cast<U4*>(to + q * kPlane + (row + c) * kStage + (piece ^ swizzle(row + c)) * 8) = p[q];
+    }
+  }
+};
+template <>
+struct TwoColumns<__bf16> {
+  unsigned v[8];
+  __device__ __forceinline__ void request(int i, const __bf16* p) { v[i] = *reinterpret_cast<const ULoose*>(p); }
+  __device__ __forceinline__ void put(int inside, int piece, int row, __bf16* to, unsigned&) const {
+    U4 p[2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const unsigned x = 2 * i < inside ? v[2 * i] : 0u, y = 2 * i + 1 < inside ? v[2 * i + 1] : 0u;
+      p[0][i] = __builtin_amdgcn_perm(y, x, 0x05040100);
+      p[1][i] = __builtin_amdgcn_perm(y, x, 0x07060302);
+    }
+#pragma unroll
+    for (int c = 0; c < 2; ++c) *reinterpret_cast<U4*>(to + (row + c) * kStage + (piece ^ swizzle(row + c)) * 8) = p[c];
+  }
+};
+
+typedef F16 Sums[2][2];
+
+__device__ __forceinline__ void clear(Sums& s) {
+#pragma unroll
+  for (int e = 0; e < 2; ++e)
+#pragma unroll
+    for (int f = 0; f < 2; ++f)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[e][f][r] = 0;
+}
+
+// The products of a stage: a and b in LDS, NA and NB parts.
+template <int NA, int NB>
+__device__ __forceinline__ void multiply(const __bf16* a, const __bf16* b, Sums& sum) {
+  const int lane = threadIdx.x & (kLanes - 1), wave = threadIdx.x / kLanes;
+  const int wi = wave / 2 * 64 + (lane & 31), wj = wave % 2 * 64 + (lane & 31);
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    B8 x[2][NA], y[2][NB];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int i = wi + 32 * e, j = wj + 32 * e;
+#pragma unroll
+      for (int p = 0; p < NA; ++p) x[e][p] = *reinterpret_cast<const B8*>(a + p * kPlane + i * kStage + ((2 * s + lane / 32) ^ swizzle(i)) * 8);
+#pragma unroll
+      for (int p = 0; p < NB; ++p) y[e][p] = *reinterpret_cast<const B8*>(b + p * kPlane + j * kStage + ((2 * s + lane / 32) ^ swizzle(j)) * 8);
+    }
+#pragma unroll
+    for (int order = (NA > NB ? NA : NB) - 1; order >= 0; --order)   // the smallest products first; with two operands of three parts their second parts' too
+#pragma unroll
+      for (int p = NA - 1; p >= 0; --p) {
+        const int q = order - p;
+        if (q < 0 || q >= NB) continue;
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+          for (int f = 0; f < 2; ++f) sum[e][f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[e][p], y[f][q], sum[e][f], 0, 0, 0);
+      }
+  }
+}
+
+// Has a thread of the workgroup met a value that the parts do not stand for?  (One that is not finite leaves a NaN in the sums.)
+__device__ __forceinline__ bool unserved(const Sums& sum, unsigned low, unsigned* flags) {
+  float mark = 0;
+#pragma unroll
+  for (int e = 0; e < 2; ++e)
+#pragma unroll
+    for (int f = 0; f < 2; ++f)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) mark = fmaf(sum[e][f][r], 0.f, mark);
+  const bool mine = __builtin_amdgcn_ballot_w64((low & 0xffffu) != 0 || mark != 0.f) != 0;
+  __syncthreads();
+  if ((threadIdx.x & (kLanes - 1)) == 0) flags[threadIdx.x / kLanes] = mine;
+  __syncthreads();
+  return (flags[0] | flags[1] | flags[2] | flags[3]) != 0;
+}
+
+// f(row, column, value) for the lane's results.
+template <typename F>
+__device__ __forceinline__ void each_result(const Sums& sum, F&& body) {
+  const int lane = threadIdx.x & (kLanes - 1), wave = threadIdx.x / kLanes;
+#pragma unroll
+  for (int e = 0; e < 2; ++e)
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+#pragma unroll
+      for (int f = 0; f < 2; ++f)
+        body(wave / 2 * 64 + 32 * e + 8 * (r / 4) + 4 * (lane / 32) + r % 4, wave % 2 * 64 + 32 * f + (lane & 31), sum[e][f][r]);
+}
+
+template <typename T, bool kBack>
+__global__ __launch_bounds__(kThreads, 2) void rows_parts_kernel(const Rows a) {
+  constexpr int NX = parts<T>(), NW = 3;
+  constexpr bool kOneSum = NX == 1;
+  __shared__ __attribute__((aligned(16))) __bf16 lds[(NX + NW) * kPlane];
+  __shared__ int64_t offsets[kTile];
+  __shared__ unsigned flags[kWaves];
+  static_assert(sizeof(lds) >= sizeof(BlockSpace<float>), "the blocks use the same space");
+  __bf16* const xs = lds;
+  __bf16* const ws = lds + NX * kPlane;
+  const int lane = threadIdx.x & (kLanes - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
+  const int columns = (a.columns + kTile - 1) / kTile;
+  for (int64_t block = blockIdx.x;; block += gridDim.x) {
+    int which;
+    const Place p = place_of(a.group.offsets, a.elements + 1, a.n, block, columns, [&](int atoms) { return (atoms * a.components + kTile - 1) / kTile; }, &which);
+    if (p.bucket < 0) return;
+    const int rows = p.atoms * a.components, first = p.local * kTile, c0 = which * kTile;
+    __syncthreads();   // (the offsets of the tile before)
+    if (threadIdx.x < kTile) {
+      const int r = min(first + static_cast<int>(threadIdx.x), rows - 1);
+      offsets[threadIdx.x] = row_offset(a.group.order, a.n, p.begin, r, a.components, a.ld_dst, a.columns);
+    }
+    Sums sum;
+    clear(sum);
+    unsigned low = 0;
+    if (p.bucket < a.elements) {
+      const float* const W = static_cast<const float*>(a.W) + static_cast<int64_t>(p.bucket) * a.reduced * a.columns;
+      // two rows of the operand a thread, a piece of eight of each
+      const int piece = threadIdx.x % 4;
+      const T* x[2];
+      int x_to[2], w_to[2];
+      const float* w[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int r = i * 64 + threadIdx.x / 4;
+        x[i] = row_at(static_cast<const T*>(a.src), a.group.order, a.n, p.begin, min(first + r, rows - 1), a.components, a.ld_src, a.reduced);
+        x_to[i] = r * kStage + (piece ^ swizzle(r)) * 8;
+        w[i] = W + static_cast<int64_t>(min(c0 + r, a.columns - 1)) * a.reduced;   // kBack
+        w_to[i] = x_to[i];
+      }
+      const int pair = 2 * lane;                                                   // forward: columns c0 + pair, + 1 of rows 8 wave on
+      const float* const w_rows = W + min(c0 + pair, a.columns - 2);
+      Eight<T> xv[2];
+      Eight<float> wv[2];
+      TwoColumns<float> wc;
+      auto request = [&](int k) {
+        const int at = min(k + 8 * piece, a.reduced - 8);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) xv[i].request(x[i] + at);
+        if constexpr (kBack) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) wv[i].request(w[i] + at);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) wc.request(i, w_rows + static_cast<int64_t>(min(k + 8 * wave + i, a.reduced - 1)) * a.columns);
+        }
+      };
+      request(0);
+      for (int k = 0; k < a.reduced; k += kStage) {
+        if (k > 0) barrier();   // the stage before has been read
+        const bool inside = k + 8 * piece < a.reduced;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) xv[i].put(inside, xs + x_to[i], low);
+        if constexpr (kBack) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) wv[i].put(inside, ws + w_to[i], low);
+        } else {
+          wc.put(k + 8 * wave < a.reduced ? 8 : 0, wave, pair, ws, low);
+        }
+        if (k + kStage < a.reduced) request(k + kStage);
+        barrier();
+        if constexpr (kOneSum) {
+          multiply<NX, NW>(xs, ws, sum);
+        } else {
+          Sums part;
+          clear(part);
+          multiply<NX, NW>(xs, ws, part);
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int f = 0; f < 2; ++f) sum[e][f] += part[e][f];
+        }
+      }
+      if (unserved(sum, low, flags)) {
+        BlockSpace<float>& space = *reinterpret_cast<BlockSpace<float>*>(lds);
+        for (int q = 0; q < 4; ++q)
+          if (first + q / 2 * kBlock < rows && c0 + q % 2 * kBlock < a.columns)
+            rows_block<T, float, kBack>(a, p.bucket, p.begin, rows, first + q / 2 * kBlock, c0 + q % 2 * kBlock, space);
+        continue;
+      }
+    } else {
+      __syncthreads();   // the offsets
+    }
+    T* const dst = static_cast<T*>(a.dst);
+    const T* const residual = static_cast<const T*>(a.residual);
+    each_result(sum, [&](int row, int column, float v) {
+      if (first + row >= rows || c0 + column >= a.columns) return;
+      const int64_t at = offsets[row] + c0 + column;
+      dst[at] = static_cast<T>(residual ? v + static_cast<float>(residual[at]) : v);
+    });
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads, 2) void outer_parts_kernel(const Outer a) {
+  constexpr int N = parts<T>();
+  __shared__ __attribute__((aligned(16))) __bf16 lds[2 * N * kPlane < 9216 ? 9216 : 2 * N * kPlane];
+  __shared__ unsigned flags[kWaves];
+  static_assert(sizeof(lds) >= sizeof(BlockSpace<float>), "the blocks use the same space");
+  __bf16* const xs = lds;
+  __bf16* const gs = lds + N * kPlane;
+  const int lane = threadIdx.x & (kLanes - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
+  const int col_tiles = (a.k_out + kTile - 1) / kTile, tiles = (a.k_in + kTile - 1) / kTile * col_tiles;
+  for (int64_t block = blockIdx.x;; block += gridDim.x) {
+    int which;
+    Chunk c;
+    if (!chunk_of(a, block, tiles, &c, &which)) return;
+    const int k0 = which / col_tiles * kTile, c0 = which % col_tiles * kTile;
+    float* const out = static_cast<float*>(c.partial ? a.partial : a.dW) + c.matrix * a.k_in * a.k_out;
+    const int pair = 2 * lane;
+    const int x_col = min(k0 + pair, a.k_in - 2), g_col = min(c0 + pair, a.k_out - 2);
+    TwoColumns<T> xv, gv;
+    auto request = [&](int r) {   // eight rows a wave
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int row = min(r + 8 * wave + i, c.last - 1);
+        xv.request(i, row_at(static_cast<const T*>(a.X), a.group.order, a.n, c.begin, row, a.components, a.ld_in, a.k_in) + x_col);
+        gv.request(i, row_at(static_cast<const T*>(a.dY), a.group.order, a.n, c.begin, row, a.components, a.ld_out, a.k_out) + g_col);
+      }
+    };
+    Sums sum;
+    clear(sum);
+    unsigned low = 0;
+    __syncthreads();
+    if (c.first < c.last) request(c.first);
+    for (int r = c.first; r < c.last; r += kStage) {
+      if (r > c.first) barrier();
+      const int inside = c.last - r - 8 * wave;
+      xv.put(inside, wave, pair, xs, low);
+      gv.put(inside, wave, pair, gs, low);
+      if (r + kStage < c.last) request(r + kStage);
+      barrier();
+      Sums part;
+      clear(part);
+      multiply<N, N>(xs, gs, part);
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int f = 0; f < 2; ++f) sum[e][f] += part[e][f];
+    }
+    if (unserved(sum, low, flags)) {
+      BlockSpace<float>& space = *reinterpret_cast<BlockSpace<float>*>(lds);
+      for (int q = 0; q < 4; ++q)
+        if (k0 + q / 2 * kBlock < a.k_in && c0 + q % 2 * kBlock < a.k_out)
+          outer_block<T, float>(a, a.group.order, c.begin, c.first, c.last, k0 + q / 2 * kBlock, c0 + q % 2 * kBlock, out, space);
+      continue;
+    }
+    each_result(sum, [&](int k, int column, float v) {
+      if (k0 + k < a.k_in && c0 + column < a.k_out) out[static_cast<int64_t>(k0 + k) * a.k_out + c0 + column] = v;
+    });
+  }
+}
+
+}  // namespace
+
+bool parts_serve(const gp_config* c) { return c->dtype != SC_F64 && c->k_in % 8 == 0 && c->k_out % 8 == 0; }
+
+hipError_t launch_rows_parts(const gp_config* c, const Rows& a, bool back, hipStream_t stream) {
+  const int64_t tiles = ceil_div(a.n * c->components, kTile) + std::min<int64_t>(c->num_elements + 1, a.n);
+  const dim3 grid(static_cast<unsigned>(std::min(kMaxGrid, ceil_div(tiles * ceil_div(a.columns, kTile), kXcds) * kXcds)));
+  if (c->dtype == SC_F32) {
+    if (back) hipLaunchKernelGGL((rows_parts_kernel<float, true>), grid, dim3(kThreads), 0, stream, a);
+    else hipLaunchKernelGGL((rows_parts_kernel<float, false>), grid, dim3(kThreads), 0, stream, a);
+  } else {
+    if (back) hipLaunchKernelGGL((rows_parts_kernel<__bf16, true>), grid, dim3(kThreads), 0, stream, a);
+    else hipLaunchKernelGGL((rows_parts_kernel<__bf16, false>), grid, dim3(kThreads), 0, stream, a);
+  }
+  return hipGetLastError();
+}
+
+hipError_t launch_outer_parts(const gp_config* c, const Outer& a, hipStream_t stream) {
+  const int64_t chunks = c->num_elements + a.n * c->components / a.per, tiles = ceil_div(c->k_in, kTile) * ceil_div(c->k_out, kTile);
+  const dim3 grid(static_cast<unsigned>(std::min(kMaxGrid, ceil_div(chunks * tiles, kXcds) * kXcds)));
+  if (c->dtype == SC_F32) hipLaunchKernelGGL(outer_parts_kernel<float>, grid, dim3(kThreads), 0, stream, a);
+  else hipLaunchKernelGGL(outer_parts_kernel<__bf16>, grid, dim3(kThreads), 0, stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace gp

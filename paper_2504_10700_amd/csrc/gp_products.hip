@@ -1,214 +1,57 @@
-// The products by element of include/gp.h: arguments, entry points, and the kernels that serve every case.
+// The products by element of include/gp.h: arguments, entry points, and the kernels that serve every width and type (gp_parts.hip: widths that are multiples
+// of 8 in fp32 and bfloat16; gp_few.hip: the rows of batches without a grouping).
 //
 // Rows (Y, dX): a workgroup computes 64 rows of one bucket x 64 columns; the rows are gathered by the grouping's order, the reduced index goes
 // through LDS 16 at a time.  dW: a workgroup computes 64 x 64 of one element's matrix over a chunk of the element's rows; elements with several chunks leave
-// partial matrices that a second launch adds in order.  Batches without a grouping: an atom is a bucket of its own.
-// fp32 and fp64 matrix instructions (el_tile.h has their operand layout).
+// partial matrices that a second launch adds in order.
 #include <algorithm>
 #include <initializer_list>
 #include <string>
 
-#include "el_tile.h"
-#include "gp_internal.h"
+#include "gp_blocks.h"
 
 namespace gp {
 namespace {
 
-using el::Mma;
 using sc::DeviceGuard;
 using sc::misaligned;
 using sc::set_error;
 
-constexpr int kTile = 64;
-constexpr int kDepth = 16;
-constexpr int kPitch = kTile + 4;
-
-struct Rows {
-  int64_t n;            // atoms
-  int64_t ld_src, ld_dst;
-  const int32_t* z;
-  Grouping group;       // offsets NULL: none
-  int elements, components;
-  int reduced, columns;
-  const void* src;
-  const void* W;        // [elements][k_in][k_out]
-  const void* residual;
-  void* dst;
-};
-
-// The row r of a bucket: its atom, and where the row begins.
-template <typename T>
-__device__ __forceinline__ T* row_at(T* p, const int32_t* order, int64_t n, int begin, int r, int components, int64_t ld, int width) {
-  const int a = components == 1 ? r : r / components;
-  const int64_t atom = order ? min(static_cast<unsigned>(order[begin + a]), static_cast<unsigned>(n - 1)) : begin + a;
-  return p + atom * ld + static_cast<int64_t>(r - a * components) * width;
-}
-
-// kBack: dX, where W is read transposed.
 template <typename T, typename TA, bool kBack>
 __global__ __launch_bounds__(kThreads) void rows_kernel(const Rows a) {
-  __shared__ TA xs[kDepth][kPitch], ws[kDepth][kPitch];
-  typedef typename Mma<TA>::acc_t Acc;
-  const int lane = threadIdx.x & (kLanes - 1), wave = threadIdx.x / kLanes;
-  int bucket, begin, rows, first;
-  if (a.group.offsets) {
-    const Place p = place_of(a.group.offsets, a.elements + 1, a.n, blockIdx.x, [&](int atoms) { return (atoms * a.components + kTile - 1) / kTile; });
-    if (p.bucket < 0) return;
-    bucket = p.bucket;
-    begin = p.begin;
-    rows = p.atoms * a.components;
-    first = p.local * kTile;
-  } else {
-    const int z = a.z[blockIdx.x];
-    bucket = static_cast<unsigned>(z) < static_cast<unsigned>(a.elements) ? z : a.elements;
-    begin = blockIdx.x;
-    rows = a.components;
-    first = 0;
-  }
-  const int c0 = blockIdx.y * kTile;
-  Acc acc[4];
-#pragma unroll
-  for (int t = 0; t < 4; ++t) acc[t] = Acc{0, 0, 0, 0};
-  if (bucket < a.elements) {
-    const TA* const W = static_cast<const TA*>(a.W) + static_cast<int64_t>(bucket) * a.reduced * a.columns;
-    const int xr = threadIdx.x / 4, xk = threadIdx.x % 4 * 4;   // 64 rows x 4 pieces of 4
-    const T* const x = row_at(static_cast<const T*>(a.src), a.group.order, a.n, begin, min(first + xr, rows - 1), a.components, a.ld_src, a.reduced);
-    for (int k = 0; k < a.reduced; k += kDepth) {
-      TA xv[4], wv[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) xv[i] = k + xk + i < a.reduced ? static_cast<TA>(x[k + xk + i]) : TA(0);
-      if constexpr (kBack) {   // W [column][reduced]
-        const int c = min(c0 + threadIdx.x / 4, a.columns - 1);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) wv[i] = k + xk + i < a.reduced ? W[static_cast<int64_t>(c) * a.reduced + k + xk + i] : TA(0);
-      } else {                 // W [reduced][column]
-        const int r = k + threadIdx.x / 16, c = c0 + threadIdx.x % 16 * 4;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) wv[i] = r < a.reduced && c + i < a.columns ? W[static_cast<int64_t>(r) * a.columns + c + i] : TA(0);
-      }
-      __syncthreads();
-#pragma unroll
-      for (int i = 0; i < 4; ++i) xs[xk + i][xr] = xv[i];
-      if constexpr (kBack) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) ws[xk + i][threadIdx.x / 4] = wv[i];
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) ws[threadIdx.x / 16][threadIdx.x % 16 * 4 + i] = wv[i];
-      }
-      __syncthreads();
-#pragma unroll
-      for (int s = 0; s < kDepth / 4; ++s) {
-        const TA xo = xs[4 * s + lane / 16][16 * wave + (lane & 15)];
-#pragma unroll
-        for (int t = 0; t < 4; ++t) acc[t] = Mma<TA>::mma(xo, ws[4 * s + lane / 16][16 * t + (lane & 15)], acc[t]);
-      }
-    }
-  }
-#pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    const int row = first + 16 * wave + Mma<TA>::row(lane, r);
-    if (row >= rows) continue;
-    T* const y = row_at(static_cast<T*>(a.dst), a.group.order, a.n, begin, row, a.components, a.ld_dst, a.columns);
-    const T* const base = a.residual ? static_cast<const T*>(a.residual) + (y - static_cast<T*>(a.dst)) : nullptr;
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      const int c = c0 + 16 * t + (lane & 15);
-      if (c < a.columns) y[c] = static_cast<T>(base ? acc[t][r] + static_cast<TA>(base[c]) : acc[t][r]);
-    }
-  }
+  __shared__ BlockSpace<TA> space;
+  const int columns = (a.columns + kBlock - 1) / kBlock;
+  int which;
+  const Place p = place_of(a.group.offsets, a.elements + 1, a.n, blockIdx.x, columns, [&](int atoms) { return (atoms * a.components + kBlock - 1) / kBlock; },
+                           &which);
+  if (p.bucket < 0) return;
+  rows_block<T, TA, kBack>(a, p.bucket, p.begin, p.atoms * a.components, p.local * kBlock, which * kBlock, space);
 }
-
-struct Outer {
-  int64_t n;
-  int64_t ld_in, ld_out;
-  const int32_t* z;
-  Grouping group;
-  int elements, components;
-  int k_in, k_out;
-  int per;              // rows of a chunk
-  const void* X;
-  const void* dY;
-  void* dW;
-  void* partial;        // [slots][k_in][k_out]
-};
-
-// An element without rows has a chunk too, which zeroes its matrix.
-__device__ __forceinline__ int chunks_of(int rows, int per) { return max(1, static_cast<int>((static_cast<unsigned>(rows) + per - 1) / static_cast<unsigned>(per))); }
 
 template <typename T, typename TA>
 __global__ __launch_bounds__(kThreads) void outer_kernel(const Outer a) {
-  __shared__ TA xs[kDepth][kPitch], gs[kDepth][kPitch];
+  __shared__ BlockSpace<TA> space;
   __shared__ int32_t list[GP_UNGROUPED];
-  typedef typename Mma<TA>::acc_t Acc;
   const int lane = threadIdx.x & (kLanes - 1), wave = threadIdx.x / kLanes;
   const int32_t* order = a.group.order;
-  int element, begin, first, last;
-  TA* out;
   const int64_t size = static_cast<int64_t>(a.k_in) * a.k_out;
+  const int col_tiles = (a.k_out + kBlock - 1) / kBlock, tiles = (a.k_in + kBlock - 1) / kBlock * col_tiles;
+  Chunk c;
   if (a.group.offsets) {
-    const Place p = place_of(a.group.offsets, a.elements, a.n, blockIdx.x, [&](int atoms) { return chunks_of(atoms * a.components, a.per); });
-    if (p.bucket < 0) return;
-    element = p.bucket;
-    begin = p.begin;
-    first = p.local * a.per;
-    last = min(p.atoms * a.components, first + a.per);
-    const bool several = p.units > 1;
-    out = static_cast<TA*>(several ? a.partial : a.dW) + (several ? p.slots + p.local : element) * size;
+    int which;
+    if (!chunk_of(a, blockIdx.x, 1, &c, &which)) return;
   } else {   // the atoms of the element, found here
-    element = blockIdx.x;
+    static_assert(GP_UNGROUPED <= kLanes, "a lane an atom");
+    const int element = blockIdx.x;
     const unsigned long long mine = __builtin_amdgcn_ballot_w64(lane < a.n && a.z[min(static_cast<int64_t>(lane), a.n - 1)] == element);
     if (wave == 0 && (mine >> lane) & 1) list[__popcll(mine & ((1ull << lane) - 1))] = lane;
     __syncthreads();
     order = list;
-    begin = 0;
-    first = 0;
-    last = __popcll(mine) * a.components;
-    out = static_cast<TA*>(a.dW) + element * size;
+    c = {0, 0, static_cast<int>(__popcll(mine)) * a.components, element, false};
   }
-  const int col_tiles = (a.k_out + kTile - 1) / kTile;
-  const int tiles = (a.k_in + kTile - 1) / kTile * col_tiles;
-  for (int tile = blockIdx.y; tile < tiles; tile += gridDim.y) {
-  const int k0 = tile / col_tiles * kTile, c0 = tile % col_tiles * kTile;
-  Acc acc[4];
-#pragma unroll
-  for (int t = 0; t < 4; ++t) acc[t] = Acc{0, 0, 0, 0};
-  const int lr = threadIdx.x / 16, lc = threadIdx.x % 16 * 4;
-  for (int r = first; r < last; r += kDepth) {
-    const int row = min(r + lr, last - 1);
-    const bool inside = r + lr < last;
-    const T* const x = row_at(static_cast<const T*>(a.X), order, a.n, begin, row, a.components, a.ld_in, a.k_in);
-    const T* const g = row_at(static_cast<const T*>(a.dY), order, a.n, begin, row, a.components, a.ld_out, a.k_out);
-    TA xv[4], gv[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      xv[i] = inside && k0 + lc + i < a.k_in ? static_cast<TA>(x[k0 + lc + i]) : TA(0);
-      gv[i] = inside && c0 + lc + i < a.k_out ? static_cast<TA>(g[c0 + lc + i]) : TA(0);
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      xs[lr][lc + i] = xv[i];
-      gs[lr][lc + i] = gv[i];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int s = 0; s < kDepth / 4; ++s) {
-      const TA xo = xs[4 * s + lane / 16][16 * wave + (lane & 15)];
-#pragma unroll
-      for (int t = 0; t < 4; ++t) acc[t] = Mma<TA>::mma(xo, gs[4 * s + lane / 16][16 * t + (lane & 15)], acc[t]);
-    }
-  }
-#pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    const int k = k0 + 16 * wave + Mma<TA>::row(lane, r);
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      const int c = c0 + 16 * t + (lane & 15);
-      if (k < a.k_in && c < a.k_out) out[static_cast<int64_t>(k) * a.k_out + c] = acc[t][r];
-    }
-  }
-  }
+  TA* const out = static_cast<TA*>(c.partial ? a.partial : a.dW) + c.matrix * size;
+  for (int tile = blockIdx.y; tile < tiles; tile += gridDim.y)
+    outer_block<T, TA>(a, order, c.begin, c.first, c.last, tile / col_tiles * kBlock, tile % col_tiles * kBlock, out, space);
 }
 
 // Slots of the elements before this one: the lanes of a wave add up theirs.
@@ -250,13 +93,11 @@ __global__ __launch_bounds__(kThreads) void zero_kernel(TA* p, int64_t n) {
 
 // ---- host side
 
-int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-
 // Rows of a chunk of dW: enough chunks for the chip where the matrices alone do not fill it.
 int chunk_rows(const gp_config* c, int64_t n) {
-  const int64_t rows = n * c->components, tiles = ceil_div(c->k_in, kTile) * ceil_div(c->k_out, kTile);
-  const int64_t wanted = std::max<int64_t>(1, std::min<int64_t>(512, 2048 / tiles));
-  return static_cast<int>(std::min<int64_t>(std::max<int64_t>(512, ceil_div(ceil_div(rows, wanted), kTile) * kTile), int64_t(1) << 30));
+  const int64_t rows = n * c->components, side = parts_serve(c) ? 128 : kBlock, tiles = ceil_div(c->k_in, side) * ceil_div(c->k_out, side);
+  const int64_t wanted = std::max<int64_t>(1, 384 / tiles);
+  return static_cast<int>(std::min<int64_t>(std::max<int64_t>(256, ceil_div(ceil_div(rows, wanted), kBlock) * kBlock), int64_t(1) << 30));
 }
 // Chunks of the elements that have several, at most.
 int64_t slots_of(const gp_config* c, int64_t n) {
@@ -325,9 +166,10 @@ Grouping grouping_for(const gp_config* c, int64_t n, const void* grouping) {
 
 template <bool kBack>
 hipError_t launch_rows(const gp_config* c, const Rows& a, hipStream_t stream) {
-  const int64_t rows = a.n * c->components;
-  const int64_t tiles = a.group.offsets ? ceil_div(rows, kTile) + std::min<int64_t>(c->num_elements + 1, a.n) : a.n;
-  const dim3 grid(static_cast<unsigned>(tiles), static_cast<unsigned>(ceil_div(a.columns, kTile)));
+  if (!a.group.offsets) return launch_rows_few(c, a, kBack, stream);
+  if (parts_serve(c)) return launch_rows_parts(c, a, kBack, stream);
+  const int64_t tiles = ceil_div(a.n * c->components, kBlock) + std::min<int64_t>(c->num_elements + 1, a.n);
+  const dim3 grid(static_cast<unsigned>(ceil_div(tiles * ceil_div(a.columns, kBlock), kXcds) * kXcds));
   if (c->dtype == SC_F64) hipLaunchKernelGGL((rows_kernel<double, double, kBack>), grid, dim3(kThreads), 0, stream, a);
   else if (c->dtype == SC_F32) hipLaunchKernelGGL((rows_kernel<float, float, kBack>), grid, dim3(kThreads), 0, stream, a);
   else hipLaunchKernelGGL((rows_kernel<__bf16, float, kBack>), grid, dim3(kThreads), 0, stream, a);
@@ -335,13 +177,19 @@ hipError_t launch_rows(const gp_config* c, const Rows& a, hipStream_t stream) {
 }
 
 hipError_t launch_outer(const gp_config* c, const Outer& a, hipStream_t stream) {
-  const int64_t rows = a.n * c->components, col_tiles = ceil_div(c->k_out, kTile), tiles = ceil_div(c->k_in, kTile) * col_tiles;
-  const int64_t chunks = a.group.offsets ? c->num_elements + rows / a.per : c->num_elements;
-  const dim3 grid(static_cast<unsigned>(chunks), static_cast<unsigned>(std::min<int64_t>(tiles, 32768)));
-  if (c->dtype == SC_F64) hipLaunchKernelGGL((outer_kernel<double, double>), grid, dim3(kThreads), 0, stream, a);
-  else if (c->dtype == SC_F32) hipLaunchKernelGGL((outer_kernel<float, float>), grid, dim3(kThreads), 0, stream, a);
-  else hipLaunchKernelGGL((outer_kernel<__bf16, float>), grid, dim3(kThreads), 0, stream, a);
-  hipError_t e = hipGetLastError();
+  const int64_t rows = a.n * c->components;
+  hipError_t e;
+  if (a.group.offsets && parts_serve(c)) {
+    e = launch_outer_parts(c, a, stream);
+  } else {
+    const int64_t tiles = ceil_div(c->k_in, kBlock) * ceil_div(c->k_out, kBlock);
+    const int64_t chunks = a.group.offsets ? ceil_div(c->num_elements + rows / a.per, kXcds) * kXcds : c->num_elements;
+    const dim3 grid(static_cast<unsigned>(chunks), static_cast<unsigned>(std::min<int64_t>(tiles, 32768)));
+    if (c->dtype == SC_F64) hipLaunchKernelGGL((outer_kernel<double, double>), grid, dim3(kThreads), 0, stream, a);
+    else if (c->dtype == SC_F32) hipLaunchKernelGGL((outer_kernel<float, float>), grid, dim3(kThreads), 0, stream, a);
+    else hipLaunchKernelGGL((outer_kernel<__bf16, float>), grid, dim3(kThreads), 0, stream, a);
+    e = hipGetLastError();
+  }
   if (e != hipSuccess || slots_of(c, a.n) == 0) return e;
   const int64_t size = static_cast<int64_t>(c->k_in) * c->k_out;
   const dim3 join(static_cast<unsigned>(c->num_elements), static_cast<unsigned>(std::min<int64_t>(ceil_div(size, kThreads), 1024)));

@@ -6,7 +6,7 @@ import ctypes as C
 from .binding import SC_BF16, SC_F32, SC_F64, ScError, _check, _ptr, _stream, lib  # noqa: F401
 
 GP_MAX_ELEMENTS, GP_MAX_WIDTH, GP_MAX_COMPONENTS, GP_MAX_STRIDE = 1024, 65536, 64, 33554432
-GP_MAX_ROWS, GP_UNGROUPED = 536870912, 32
+GP_MAX_ROWS, GP_UNGROUPED = 536870912, 64
 
 EXPORTS = ("gp_grouping_bytes", "gp_group", "gp_workspace_bytes", "gp_forward", "gp_backward")
 

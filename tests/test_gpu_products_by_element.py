@@ -140,7 +140,7 @@ def by_elements(z, X, W, dY):
     return Y, dX, dW
 
 
-SIZES = [(1, 5, 8, 8, 1), (1, 3, 1, 1, 1), (7, 89, 128, 128, 1), (32, 4, 33, 65, 3), (33, 4, 33, 65, 3), (61, 89, 128, 128, 1), (200, 1, 64, 64, 1),
+SIZES = [(1, 5, 8, 8, 1), (1, 3, 1, 1, 1), (7, 89, 128, 128, 1), (33, 4, 33, 65, 3), (64, 4, 33, 65, 3), (65, 4, 33, 65, 3), (61, 89, 128, 128, 1), (200, 1, 64, 64, 1),
          (200, 89, 40, 24, 5), (500, 1024, 16, 16, 1), (777, 10, 96, 41, 1), (1000, 6, 128, 64, 3), (2049, 12, 7, 130, 1), (300, 5, 257, 129, 7),
          (90, 3, 31, 1, 64), (150, 7, 512, 384, 1)]
 
@@ -192,7 +192,7 @@ def test_distributions(gp, n, which):
 def test_the_grouping(gp):
     """Offsets and order are those of a stable sort, for every size of the sort."""
     import torch
-    for n, elements in ((33, 1), (64, 1024), (1000, 89), (2048, 1023), (2049, 1024), (5000, 3), (40_000, 1024), (300_000, 89)):
+    for n, elements in ((65, 1), (128, 1024), (1000, 89), (2048, 1023), (2049, 1024), (5000, 3), (40_000, 1024), (300_000, 89)):
         b = Batch(gp, n, elements, 1, 1)
         b.group()
         key = torch.where((b.z >= 0) & (b.z < elements), b.z, elements).long()
