@@ -24,6 +24,9 @@ typedef unsigned U4 __attribute__((ext_vector_type(4)));
 typedef unsigned U4Loose __attribute__((ext_vector_type(4), aligned(2)));
 typedef unsigned ULoose __attribute__((aligned(2)));
 
+#ifndef AHEAD
+#define AHEAD (sizeof(T) == 2 ? 2 : 1)
+#endif
 constexpr int kTile = 128, kStage = 32;
 constexpr int kPlane = kTile * kStage;   // elements of one part of one operand: rows of 64 bytes
 constexpr int64_t kMaxGrid = int64_t(1) << 23;
@@ -118,33 +121,70 @@ __device__ __forceinline__ void clear(Sums& s) {
       for (int r = 0; r < 16; ++r) s[e][f][r] = 0;
 }
 
-// The products of a stage: a and b in LDS, NA and NB parts.
-template <int NA, int NB>
+// Adds the products of a stage, a and b in LDS, NA and NB parts, to sum: at once (kOneSum), or, a row of blocks after the other, by a sum of the stage's own.
+template <int NA, int NB, bool kOneSum>
 __device__ __forceinline__ void multiply(const __bf16* a, const __bf16* b, Sums& sum) {
   const int lane = threadIdx.x & (kLanes - 1), wave = threadIdx.x / kLanes;
   const int wi = wave / 2 * 64 + (lane & 31), wj = wave % 2 * 64 + (lane & 31);
+  auto a_part = [&](int e, int s, int p) {
+    const int i = wi + 32 * e;
+    return *reinterpret_cast<const B8*>(a + p * kPlane + i * kStage + ((2 * s + lane / 32) ^ swizzle(i)) * 8);
+  };
+  auto b_part = [&](int f, int s, int p) {
+    const int j = wj + 32 * f;
+    return *reinterpret_cast<const B8*>(b + p * kPlane + j * kStage + ((2 * s + lane / 32) ^ swizzle(j)) * 8);
+  };
+  // the smallest products first; of two operands of three parts, their second parts' product too
+  auto products = [&](auto&& body) {
 #pragma unroll
-  for (int s = 0; s < 2; ++s) {
-    B8 x[2][NA], y[2][NB];
+    for (int order = (NA > NB ? NA : NB) - 1; order >= 0; --order)
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const int i = wi + 32 * e, j = wj + 32 * e;
+      for (int p = NA - 1; p >= 0; --p)
+        if (order - p >= 0 && order - p < NB) body(p, order - p);
+  };
+  if constexpr (kOneSum) {
 #pragma unroll
-      for (int p = 0; p < NA; ++p) x[e][p] = *reinterpret_cast<const B8*>(a + p * kPlane + i * kStage + ((2 * s + lane / 32) ^ swizzle(i)) * 8);
+    for (int s = 0; s < 2; ++s) {
+      B8 x[2][NA], y[2][NB];
 #pragma unroll
-      for (int p = 0; p < NB; ++p) y[e][p] = *reinterpret_cast<const B8*>(b + p * kPlane + j * kStage + ((2 * s + lane / 32) ^ swizzle(j)) * 8);
-    }
+      for (int e = 0; e < 2; ++e) {
 #pragma unroll
-    for (int order = (NA > NB ? NA : NB) - 1; order >= 0; --order)   // the smallest products first; with two operands of three parts their second parts' too
+        for (int p = 0; p < NA; ++p) x[e][p] = a_part(e, s, p);
 #pragma unroll
-      for (int p = NA - 1; p >= 0; --p) {
-        const int q = order - p;
-        if (q < 0 || q >= NB) continue;
+        for (int p = 0; p < NB; ++p) y[e][p] = b_part(e, s, p);
+      }
+      products([&](int p, int q) {
 #pragma unroll
         for (int e = 0; e < 2; ++e)
 #pragma unroll
           for (int f = 0; f < 2; ++f) sum[e][f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[e][p], y[f][q], sum[e][f], 0, 0, 0);
+      });
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      F16 part[2];
+#pragma unroll
+      for (int f = 0; f < 2; ++f)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) part[f][r] = 0;
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        B8 x[NA], y[2][NB];
+#pragma unroll
+        for (int p = 0; p < NA; ++p) x[p] = a_part(e, s, p);
+#pragma unroll
+        for (int f = 0; f < 2; ++f)
+#pragma unroll
+          for (int p = 0; p < NB; ++p) y[f][p] = b_part(f, s, p);
+        products([&](int p, int q) {
+#pragma unroll
+          for (int f = 0; f < 2; ++f) part[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[p], y[f][q], part[f], 0, 0, 0);
+        });
       }
+#pragma unroll
+      for (int f = 0; f < 2; ++f) sum[e][f] += part[f];
+    }
   }
 }
 
@@ -164,17 +204,19 @@ __device__ __forceinline__ bool unserved(const Sums& sum, unsigned low, unsigned
   return (flags[0] | flags[1] | flags[2] | flags[3]) != 0;
 }
 
-// f(row, column, value) for the lane's results.
-template <typename F>
-__device__ __forceinline__ void each_result(const Sums& sum, F&& body) {
+// f(row, column, value, block, i) for the lane's results, block by block; before(block) ahead of each.
+template <typename B, typename F>
+__device__ __forceinline__ void each_result(const Sums& sum, B&& before, F&& body) {
   const int lane = threadIdx.x & (kLanes - 1), wave = threadIdx.x / kLanes;
 #pragma unroll
   for (int e = 0; e < 2; ++e)
 #pragma unroll
-    for (int r = 0; r < 16; ++r)
+    for (int f = 0; f < 2; ++f) {
+      const int row = wave / 2 * 64 + 32 * e + 4 * (lane / 32), column = wave % 2 * 64 + 32 * f + (lane & 31);
+      before(row, column);
 #pragma unroll
-      for (int f = 0; f < 2; ++f)
-        body(wave / 2 * 64 + 32 * e + 8 * (r / 4) + 4 * (lane / 32) + r % 4, wave % 2 * 64 + 32 * f + (lane & 31), sum[e][f][r]);
+      for (int r = 0; r < 16; ++r) body(row + 8 * (r / 4) + r % 4, column, sum[e][f][r], r);
+    }
 }
 
 template <typename T, bool kBack>
@@ -219,14 +261,18 @@ __global__ __launch_bounds__(kThreads, 2) void rows_parts_kernel(const Rows a) {
       }
       const int pair = 2 * lane;                                                   // forward: columns c0 + pair, + 1 of rows 8 wave on
       const float* const w_rows = W + min(c0 + pair, a.columns - 2);
-      Eight<T> xv[2];
+      constexpr int kAhead = AHEAD;
+      Eight<T> xv[kAhead][2];
       Eight<float> wv[2];
       TwoColumns<float> wc;
-      auto request = [&](int k) {
+      auto request_rows = [&](int k, Eight<T> (&v)[2]) {
         const int at = min(k + 8 * piece, a.reduced - 8);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) xv[i].request(x[i] + at);
+        for (int i = 0; i < 2; ++i) v[i].request(x[i] + at);
+      };
+      auto request_weights = [&](int k) {
         if constexpr (kBack) {
+          const int at = min(k + 8 * piece, a.reduced - 8);
 #pragma unroll
           for (int i = 0; i < 2; ++i) wv[i].request(w[i] + at);
         } else {
@@ -234,31 +280,28 @@ __global__ __launch_bounds__(kThreads, 2) void rows_parts_kernel(const Rows a) {
           for (int i = 0; i < 8; ++i) wc.request(i, w_rows + static_cast<int64_t>(min(k + 8 * wave + i, a.reduced - 1)) * a.columns);
         }
       };
-      request(0);
-      for (int k = 0; k < a.reduced; k += kStage) {
+      auto stage = [&](int k, Eight<T> (&v)[2]) {
         if (k > 0) barrier();   // the stage before has been read
         const bool inside = k + 8 * piece < a.reduced;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) xv[i].put(inside, xs + x_to[i], low);
+        for (int i = 0; i < 2; ++i) v[i].put(inside, xs + x_to[i], low);
         if constexpr (kBack) {
 #pragma unroll
           for (int i = 0; i < 2; ++i) wv[i].put(inside, ws + w_to[i], low);
         } else {
           wc.put(k + 8 * wave < a.reduced ? 8 : 0, wave, pair, ws, low);
         }
-        if (k + kStage < a.reduced) request(k + kStage);
+        if (k + kStage < a.reduced) request_weights(k + kStage);
+        if (k + kAhead * kStage < a.reduced) request_rows(k + kAhead * kStage, v);
         barrier();
-        if constexpr (kOneSum) {
-          multiply<NX, NW>(xs, ws, sum);
-        } else {
-          Sums part;
-          clear(part);
-          multiply<NX, NW>(xs, ws, part);
-#pragma unroll
-          for (int e = 0; e < 2; ++e)
-#pragma unroll
-            for (int f = 0; f < 2; ++f) sum[e][f] += part[e][f];
-        }
+        multiply<NX, NW, kOneSum>(xs, ws, sum);
+      };
+      request_rows(0, xv[0]);
+      request_weights(0);
+      if (kAhead > 1 && kStage < a.reduced) request_rows(kStage, xv[kAhead - 1]);
+      for (int k = 0; k < a.reduced; k += kAhead * kStage) {
+        stage(k, xv[0]);
+        if (kAhead > 1 && k + kStage < a.reduced) stage(k + kStage, xv[kAhead - 1]);
       }
       if (unserved(sum, low, flags)) {
         BlockSpace<float>& space = *reinterpret_cast<BlockSpace<float>*>(lds);
@@ -272,11 +315,20 @@ __global__ __launch_bounds__(kThreads, 2) void rows_parts_kernel(const Rows a) {
     }
     T* const dst = static_cast<T*>(a.dst);
     const T* const residual = static_cast<const T*>(a.residual);
-    each_result(sum, [&](int row, int column, float v) {
-      if (first + row >= rows || c0 + column >= a.columns) return;
-      const int64_t at = offsets[row] + c0 + column;
-      dst[at] = static_cast<T>(residual ? v + static_cast<float>(residual[at]) : v);
-    });
+    // (sixteen rows of the residual before the first of them is written: it may be Y itself)
+    int64_t at[16];
+    float base[16];
+    each_result(sum,
+                [&](int row, int column) {
+                  const int c = min(c0 + column, a.columns - 1);
+#pragma unroll
+                  for (int r = 0; r < 16; ++r) at[r] = offsets[row + 8 * (r / 4) + r % 4] + c;
+#pragma unroll
+                  for (int r = 0; r < 16; ++r) base[r] = residual ? static_cast<float>(residual[at[r]]) : 0.f;
+                },
+                [&](int row, int column, float v, int r) {
+                  if (first + row < rows && c0 + column < a.columns) dst[at[r]] = static_cast<T>(v + base[r]);
+                });
   }
 }
 
@@ -297,35 +349,50 @@ __global__ __launch_bounds__(kThreads, 2) void outer_parts_kernel(const Outer a)
     const int k0 = which / col_tiles * kTile, c0 = which % col_tiles * kTile;
     float* const out = static_cast<float*>(c.partial ? a.partial : a.dW) + c.matrix * a.k_in * a.k_out;
     const int pair = 2 * lane;
-    const int x_col = min(k0 + pair, a.k_in - 2), g_col = min(c0 + pair, a.k_out - 2);
+    const T* const x_at = static_cast<const T*>(a.X) + min(k0 + pair, a.k_in - 2);
+    const T* const g_at = static_cast<const T*>(a.dY) + min(c0 + pair, a.k_out - 2);
     TwoColumns<T> xv, gv;
-    auto request = [&](int r) {   // eight rows a wave
+    // Lane i holds where the wave's row 8 wave + i of a stage begins (i < 8); it is looked up a stage before the row is requested.
+    int64_t x_row, g_row;
+    auto look_up = [&](int r) {
+      const int row = min(r + 8 * wave + (lane & 7), c.last - 1);
+      const int atom_of = a.components == 1 ? row : static_cast<int>(static_cast<unsigned>(row) / static_cast<unsigned>(a.components));
+      const int64_t atom = min(static_cast<unsigned>(a.group.order[c.begin + atom_of]), static_cast<unsigned>(a.n - 1));
+      const int component = row - atom_of * a.components;
+      x_row = atom * a.ld_in + static_cast<int64_t>(component) * a.k_in;
+      g_row = atom * a.ld_out + static_cast<int64_t>(component) * a.k_out;
+    };
+    auto of_lane = [](int64_t v, int i) {
+      const unsigned low_word = __builtin_amdgcn_readlane(static_cast<unsigned>(v), i), high_word = __builtin_amdgcn_readlane(static_cast<unsigned>(v >> 32), i);
+      return static_cast<int64_t>(static_cast<uint64_t>(high_word) << 32 | low_word);
+    };
+    auto request = [&] {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const int row = min(r + 8 * wave + i, c.last - 1);
-        xv.request(i, row_at(static_cast<const T*>(a.X), a.group.order, a.n, c.begin, row, a.components, a.ld_in, a.k_in) + x_col);
-        gv.request(i, row_at(static_cast<const T*>(a.dY), a.group.order, a.n, c.begin, row, a.components, a.ld_out, a.k_out) + g_col);
+        xv.request(i, x_at + of_lane(x_row, i));
+        gv.request(i, g_at + of_lane(g_row, i));
       }
     };
     Sums sum;
     clear(sum);
     unsigned low = 0;
     __syncthreads();
-    if (c.first < c.last) request(c.first);
+    if (c.first < c.last) {
+      look_up(c.first);
+      request();
+      look_up(c.first + kStage);
+    }
     for (int r = c.first; r < c.last; r += kStage) {
       if (r > c.first) barrier();
       const int inside = c.last - r - 8 * wave;
       xv.put(inside, wave, pair, xs, low);
       gv.put(inside, wave, pair, gs, low);
-      if (r + kStage < c.last) request(r + kStage);
+      if (r + kStage < c.last) {
+        request();
+        look_up(r + 2 * kStage);
+      }
       barrier();
-      Sums part;
-      clear(part);
-      multiply<N, N>(xs, gs, part);
-#pragma unroll
-      for (int e = 0; e < 2; ++e)
-#pragma unroll
-        for (int f = 0; f < 2; ++f) sum[e][f] += part[e][f];
+      multiply<N, N, false>(xs, gs, sum);
     }
     if (unserved(sum, low, flags)) {
       BlockSpace<float>& space = *reinterpret_cast<BlockSpace<float>*>(lds);
@@ -334,7 +401,7 @@ __global__ __launch_bounds__(kThreads, 2) void outer_parts_kernel(const Outer a)
           outer_block<T, float>(a, a.group.order, c.begin, c.first, c.last, k0 + q / 2 * kBlock, c0 + q % 2 * kBlock, out, space);
       continue;
     }
-    each_result(sum, [&](int k, int column, float v) {
+    each_result(sum, [](int, int) {}, [&](int k, int column, float v, int) {
       if (k0 + k < a.k_in && c0 + column < a.k_out) out[static_cast<int64_t>(k0 + k) * a.k_out + c0 + column] = v;
     });
   }

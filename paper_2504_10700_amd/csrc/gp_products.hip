@@ -81,6 +81,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const Outer a) {
   TA* const to = static_cast<TA*>(a.dW) + element * size;
   for (int64_t i = static_cast<int64_t>(blockIdx.y) * kThreads + threadIdx.x; i < size; i += static_cast<int64_t>(gridDim.y) * kThreads) {
     TA sum = 0;
+#pragma unroll 8
     for (int c = 0; c < n; ++c) sum += from[c * size + i];
     to[i] = sum;
   }
@@ -192,7 +193,7 @@ hipError_t launch_outer(const gp_config* c, const Outer& a, hipStream_t stream) 
   }
   if (e != hipSuccess || slots_of(c, a.n) == 0) return e;
   const int64_t size = static_cast<int64_t>(c->k_in) * c->k_out;
-  const dim3 join(static_cast<unsigned>(c->num_elements), static_cast<unsigned>(std::min<int64_t>(ceil_div(size, kThreads), 1024)));
+  const dim3 join(static_cast<unsigned>(c->num_elements), static_cast<unsigned>(std::min<int64_t>(ceil_div(size, kThreads), 64)));
   if (c->dtype == SC_F64) hipLaunchKernelGGL(join_kernel<double>, join, dim3(kThreads), 0, stream, a);
   else hipLaunchKernelGGL(join_kernel<float>, join, dim3(kThreads), 0, stream, a);
   return hipGetLastError();
