@@ -19,14 +19,12 @@ namespace {
 typedef __bf16 B8 __attribute__((ext_vector_type(8)));
 typedef float F16 __attribute__((ext_vector_type(16)));
 typedef float F4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef float F4Tight __attribute__((ext_vector_type(4)));
 typedef float F2 __attribute__((ext_vector_type(2), aligned(4)));
 typedef unsigned U4 __attribute__((ext_vector_type(4)));
 typedef unsigned U4Loose __attribute__((ext_vector_type(4), aligned(2)));
 typedef unsigned ULoose __attribute__((aligned(2)));
 
-#ifndef AHEAD
-#define AHEAD (sizeof(T) == 2 ? 2 : 1)
-#endif
 constexpr int kTile = 128, kStage = 32;
 constexpr int kPlane = kTile * kStage;   // elements of one part of one operand: rows of 64 bytes
 constexpr int64_t kMaxGrid = int64_t(1) << 23;
@@ -49,11 +47,12 @@ struct Eight<float> {
     v[0] = *reinterpret_cast<const F4*>(p);
     v[1] = *reinterpret_cast<const F4*>(p + 4);
   }
-  __device__ __forceinline__ void put(bool inside, __bf16* to, unsigned& low) const {
+  __device__ __forceinline__ void clear() { v[0] = v[1] = F4{0, 0, 0, 0}; }
+  __device__ __forceinline__ void put(__bf16* to, unsigned& low) const {
     U4 p[3];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const el::SplitPair s = el::split_pair(inside ? v[i / 2][2 * (i % 2)] : 0.f, inside ? v[i / 2][2 * (i % 2) + 1] : 0.f, low);
+      const el::SplitPair s = el::split_pair(v[i / 2][2 * (i % 2)], v[i / 2][2 * (i % 2) + 1], low);
       p[0][i] = s.h;
       p[1][i] = s.m;
       p[2][i] = s.l;
@@ -66,7 +65,8 @@ template <>
 struct Eight<__bf16> {
   U4 v;
   __device__ __forceinline__ void request(const __bf16* p) { v = *reinterpret_cast<const U4Loose*>(p); }
-  __device__ __forceinline__ void put(bool inside, __bf16* to, unsigned&) const { *reinterpret_cast<U4*>(to) = inside ? v : U4{0, 0, 0, 0}; }
+  __device__ __forceinline__ void clear() { v = U4{0, 0, 0, 0}; }
+  __device__ __forceinline__ void put(__bf16* to, unsigned&) const { *reinterpret_cast<U4*>(to) = v; }
 };
 
 // Eight reduced indices of two neighbouring columns, from eight rows of an operand whose rows are the reduced index.
@@ -76,14 +76,17 @@ template <>
 struct TwoColumns<float> {
   F2 v[8];
   __device__ __forceinline__ void request(int i, const float* p) { v[i] = *reinterpret_cast<const F2*>(p); }
-  // inside: how many of the eight there are
-  __device__ __forceinline__ void put(int inside, int piece, int row, __bf16* to, unsigned& low) const {
+  __device__ __forceinline__ void clear_from(int n) {   // of the eight
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i < n ? v[i] : F2{0, 0};
+  }
+  __device__ __forceinline__ void put(int piece, int row, __bf16* to, unsigned& low) const {
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
       U4 p[3];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const el::SplitPair s = el::split_pair(2 * i < inside ? v[2 * i][c] : 0.f, 2 * i + 1 < inside ? v[2 * i + 1][c] : 0.f, low);
+        const el::SplitPair s = el::split_pair(v[2 * i][c], v[2 * i + 1][c], low);
         p[0][i] = s.h;
         p[1][i] = s.m;
         p[2][i] = s.l;
@@ -97,11 +100,15 @@ template <>
 struct TwoColumns<__bf16> {
   unsigned v[8];
   __device__ __forceinline__ void request(int i, const __bf16* p) { v[i] = *reinterpret_cast<const ULoose*>(p); }
-  __device__ __forceinline__ void put(int inside, int piece, int row, __bf16* to, unsigned&) const {
+  __device__ __forceinline__ void clear_from(int n) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i < n ? v[i] : 0u;
+  }
+  __device__ __forceinline__ void put(int piece, int row, __bf16* to, unsigned&) const {
     U4 p[2];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const unsigned x = 2 * i < inside ? v[2 * i] : 0u, y = 2 * i + 1 < inside ? v[2 * i + 1] : 0u;
+      const unsigned x = v[2 * i], y = v[2 * i + 1];
       p[0][i] = __builtin_amdgcn_perm(y, x, 0x05040100);
       p[1][i] = __builtin_amdgcn_perm(y, x, 0x07060302);
     }
@@ -204,19 +211,55 @@ __device__ __forceinline__ bool unserved(const Sums& sum, unsigned low, unsigned
   return (flags[0] | flags[1] | flags[2] | flags[3]) != 0;
 }
 
-// f(row, column, value, block, i) for the lane's results, block by block; before(block) ahead of each.
-template <typename B, typename F>
-__device__ __forceinline__ void each_result(const Sums& sum, B&& before, F&& body) {
+// The results, a wave's 32 x 32 after the other through its corner of LDS, which turns them so that neighbouring lanes have the pieces of 16 bytes of a row:
+// f(row, column, values of a piece).  The workgroup has left the LDS.
+constexpr int kPitchOut = 36;   // floats
+template <typename T>
+constexpr int piece_of() { return 16 / sizeof(T); }
+template <typename T, typename F>
+__device__ __forceinline__ void each_result(const Sums& sum, float* lds, F&& body) {
+  constexpr int kN = piece_of<T>(), kLanesOfRow = 32 / kN;
   const int lane = threadIdx.x & (kLanes - 1), wave = threadIdx.x / kLanes;
+  float* const corner = lds + wave * 32 * kPitchOut;
+  const int column = lane % kLanesOfRow * kN;
 #pragma unroll
   for (int e = 0; e < 2; ++e)
 #pragma unroll
     for (int f = 0; f < 2; ++f) {
-      const int row = wave / 2 * 64 + 32 * e + 4 * (lane / 32), column = wave % 2 * 64 + 32 * f + (lane & 31);
-      before(row, column);
 #pragma unroll
-      for (int r = 0; r < 16; ++r) body(row + 8 * (r / 4) + r % 4, column, sum[e][f][r], r);
+      for (int r = 0; r < 16; ++r) corner[(8 * (r / 4) + 4 * (lane / 32) + r % 4) * kPitchOut + (lane & 31)] = sum[e][f][r];
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      float v[16 / kN][kN];
+#pragma unroll
+      for (int i = 0; i < 16 / kN; ++i)
+#pragma unroll
+        for (int k = 0; k < kN; k += 4) {
+          const F4Tight x = *reinterpret_cast<const F4Tight*>(corner + (lane / kLanesOfRow + i * (kLanes / kLanesOfRow)) * kPitchOut + column + k);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) v[i][k + j] = x[j];
+        }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+      for (int i = 0; i < 16 / kN; ++i) body(wave / 2 * 64 + 32 * e + lane / kLanesOfRow + i * (kLanes / kLanesOfRow), wave % 2 * 64 + 32 * f + column, v[i]);
     }
+}
+
+__device__ __forceinline__ void store_piece(float* p, const float (&v)[4]) { *reinterpret_cast<F4*>(p) = F4{v[0], v[1], v[2], v[3]}; }
+__device__ __forceinline__ void store_piece(__bf16* p, const float (&v)[8]) {
+  *reinterpret_cast<U4Loose*>(p) = U4Loose{el::pack_bf16(v[0], v[1]), el::pack_bf16(v[2], v[3]), el::pack_bf16(v[4], v[5]), el::pack_bf16(v[6], v[7])};
+}
+__device__ __forceinline__ void add_piece(const float* p, float (&v)[4]) {
+  const F4 x = *reinterpret_cast<const F4*>(p);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) v[k] += x[k];
+}
+__device__ __forceinline__ void add_piece(const __bf16* p, float (&v)[8]) {
+  const U4 x = *reinterpret_cast<const U4Loose*>(p);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    v[2 * k] += el::low_half(x[k]);
+    v[2 * k + 1] += el::high_half(x[k]);
+  }
 }
 
 template <typename T, bool kBack>
@@ -261,7 +304,7 @@ __global__ __launch_bounds__(kThreads, 2) void rows_parts_kernel(const Rows a) {
       }
       const int pair = 2 * lane;                                                   // forward: columns c0 + pair, + 1 of rows 8 wave on
       const float* const w_rows = W + min(c0 + pair, a.columns - 2);
-      constexpr int kAhead = AHEAD;
+      constexpr int kAhead = sizeof(T) == 2 ? 2 : 1;   // stages of rows under way (fp32: registers for one; W comes from the caches: one)
       Eight<T> xv[kAhead][2];
       Eight<float> wv[2];
       TwoColumns<float> wc;
@@ -282,14 +325,22 @@ __global__ __launch_bounds__(kThreads, 2) void rows_parts_kernel(const Rows a) {
       };
       auto stage = [&](int k, Eight<T> (&v)[2]) {
         if (k > 0) barrier();   // the stage before has been read
-        const bool inside = k + 8 * piece < a.reduced;
+        if (k + kStage > a.reduced) {
+          const bool inside = k + 8 * piece < a.reduced;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) v[i].put(inside, xs + x_to[i], low);
+          for (int i = 0; i < 2; ++i) {
+            if (!inside) v[i].clear();
+            if (kBack && !inside) wv[i].clear();
+          }
+          if (!kBack) wc.clear_from(a.reduced - k - 8 * wave);
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) v[i].put(xs + x_to[i], low);
         if constexpr (kBack) {
 #pragma unroll
-          for (int i = 0; i < 2; ++i) wv[i].put(inside, ws + w_to[i], low);
+          for (int i = 0; i < 2; ++i) wv[i].put(ws + w_to[i], low);
         } else {
-          wc.put(k + 8 * wave < a.reduced ? 8 : 0, wave, pair, ws, low);
+          wc.put(wave, pair, ws, low);
         }
         if (k + kStage < a.reduced) request_weights(k + kStage);
         if (k + kAhead * kStage < a.reduced) request_rows(k + kAhead * kStage, v);
@@ -315,20 +366,12 @@ __global__ __launch_bounds__(kThreads, 2) void rows_parts_kernel(const Rows a) {
     }
     T* const dst = static_cast<T*>(a.dst);
     const T* const residual = static_cast<const T*>(a.residual);
-    // (sixteen rows of the residual before the first of them is written: it may be Y itself)
-    int64_t at[16];
-    float base[16];
-    each_result(sum,
-                [&](int row, int column) {
-                  const int c = min(c0 + column, a.columns - 1);
-#pragma unroll
-                  for (int r = 0; r < 16; ++r) at[r] = offsets[row + 8 * (r / 4) + r % 4] + c;
-#pragma unroll
-                  for (int r = 0; r < 16; ++r) base[r] = residual ? static_cast<float>(residual[at[r]]) : 0.f;
-                },
-                [&](int row, int column, float v, int r) {
-                  if (first + row < rows && c0 + column < a.columns) dst[at[r]] = static_cast<T>(v + base[r]);
-                });
+    each_result<T>(sum, reinterpret_cast<float*>(lds), [&](int row, int column, float (&v)[piece_of<T>()]) {
+      if (first + row >= rows || c0 + column >= a.columns) return;   // (widths are multiples of a piece)
+      const int64_t at = offsets[row] + c0 + column;
+      if (residual) add_piece(residual + at, v);
+      store_piece(dst + at, v);
+    });
   }
 }
 
@@ -384,9 +427,12 @@ __global__ __launch_bounds__(kThreads, 2) void outer_parts_kernel(const Outer a)
     }
     for (int r = c.first; r < c.last; r += kStage) {
       if (r > c.first) barrier();
-      const int inside = c.last - r - 8 * wave;
-      xv.put(inside, wave, pair, xs, low);
-      gv.put(inside, wave, pair, gs, low);
+      if (r + kStage > c.last) {
+        xv.clear_from(c.last - r - 8 * wave);
+        gv.clear_from(c.last - r - 8 * wave);
+      }
+      xv.put(wave, pair, xs, low);
+      gv.put(wave, pair, gs, low);
       if (r + kStage < c.last) {
         request();
         look_up(r + 2 * kStage);
@@ -401,8 +447,8 @@ __global__ __launch_bounds__(kThreads, 2) void outer_parts_kernel(const Outer a)
           outer_block<T, float>(a, a.group.order, c.begin, c.first, c.last, k0 + q / 2 * kBlock, c0 + q % 2 * kBlock, out, space);
       continue;
     }
-    each_result(sum, [](int, int) {}, [&](int k, int column, float v, int) {
-      if (k0 + k < a.k_in && c0 + column < a.k_out) out[static_cast<int64_t>(k0 + k) * a.k_out + c0 + column] = v;
+    each_result<float>(sum, reinterpret_cast<float*>(lds), [&](int k, int column, const float (&v)[4]) {
+      if (k0 + k < a.k_in && c0 + column < a.k_out) store_piece(out + static_cast<int64_t>(k0 + k) * a.k_out + c0 + column, v);
     });
   }
 }
