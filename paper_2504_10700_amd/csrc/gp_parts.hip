@@ -10,6 +10,7 @@
 // operands are requested while the 32 before are multiplied, and pass through registers, where they are split, to LDS.  One set of LDS and two barriers a
 // stage: the two workgroups of a compute unit fill each other's waits.
 #include <algorithm>
+#include <type_traits>
 
 #include "gp_blocks.h"
 
@@ -48,7 +49,7 @@ struct Eight<float> {
     v[1] = *reinterpret_cast<const F4*>(p + 4);
   }
   __device__ __forceinline__ void clear() { v[0] = v[1] = F4{0, 0, 0, 0}; }
-  __device__ __forceinline__ void put(__bf16* to, unsigned& low) const {
+  __device__ __forceinline__ void put(__bf16* to, int plane, unsigned& low) const {
     U4 p[3];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -58,7 +59,7 @@ struct Eight<float> {
       p[2][i] = s.l;
     }
 #pragma unroll
-    for (int q = 0; q < 3; ++q) *reinterpret_cast<U4*>(to + q * kPlane) = p[q];
+    for (int q = 0; q < 3; ++q) *reinterpret_cast<U4*>(to + q * plane) = p[q];
   }
 };
 template <>
@@ -66,7 +67,7 @@ struct Eight<__bf16> {
   U4 v;
   __device__ __forceinline__ void request(const __bf16* p) { v = *reinterpret_cast<const U4Loose*>(p); }
   __device__ __forceinline__ void clear() { v = U4{0, 0, 0, 0}; }
-  __device__ __forceinline__ void put(__bf16* to, unsigned&) const { *reinterpret_cast<U4*>(to) = v; }
+  __device__ __forceinline__ void put(__bf16* to, int, unsigned&) const { *reinterpret_cast<U4*>(to) = v; }
 };
 
 // Eight reduced indices of two neighbouring columns, from eight rows of an operand whose rows are the reduced index.
@@ -117,25 +118,30 @@ struct TwoColumns<__bf16> {
   }
 };
 
-typedef F16 Sums[2][2];
+// Sums of a wave: kR x 2 blocks of 32 x 32.
+template <int kR>
+using SumsOf = F16[kR][2];
 
-__device__ __forceinline__ void clear(Sums& s) {
+template <int kR>
+__device__ __forceinline__ void clear(SumsOf<kR>& s) {
 #pragma unroll
-  for (int e = 0; e < 2; ++e)
+  for (int e = 0; e < kR; ++e)
 #pragma unroll
     for (int f = 0; f < 2; ++f)
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[e][f][r] = 0;
 }
 
-// Adds the products of a stage, a and b in LDS, NA and NB parts, to sum: at once (kOneSum), or, a row of blocks after the other, by a sum of the stage's own.
-template <int NA, int NB, bool kOneSum>
-__device__ __forceinline__ void multiply(const __bf16* a, const __bf16* b, Sums& sum) {
+// Adds the products of a stage, a and b in LDS, NA and NB parts, to sum (of the blocks that begin inside `rows`): at once (kOneSum), or, a row of blocks after the other, by a sum of the stage's own.
+template <int NA, int NB, int kR, bool kOneSum>
+__device__ __forceinline__ void multiply(const __bf16* a, const __bf16* b, int rows, SumsOf<kR>& sum) {
+  constexpr int kPlaneA = 64 * kR * kStage;
   const int lane = threadIdx.x & (kLanes - 1), wave = threadIdx.x / kLanes;
-  const int wi = wave / 2 * 64 + (lane & 31), wj = wave % 2 * 64 + (lane & 31);
+  const int first = __builtin_amdgcn_readfirstlane(wave / 2 * 32 * kR);
+  const int wi = wave / 2 * 32 * kR + (lane & 31), wj = wave % 2 * 64 + (lane & 31);
   auto a_part = [&](int e, int s, int p) {
     const int i = wi + 32 * e;
-    return *reinterpret_cast<const B8*>(a + p * kPlane + i * kStage + ((2 * s + lane / 32) ^ swizzle(i)) * 8);
+    return *reinterpret_cast<const B8*>(a + p * kPlaneA + i * kStage + ((2 * s + lane / 32) ^ swizzle(i)) * 8);
   };
   auto b_part = [&](int f, int s, int p) {
     const int j = wj + 32 * f;
@@ -152,24 +158,26 @@ __device__ __forceinline__ void multiply(const __bf16* a, const __bf16* b, Sums&
   if constexpr (kOneSum) {
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-      B8 x[2][NA], y[2][NB];
+      if (first >= rows) return;
+      B8 x[kR][NA], y[2][NB];
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
+      for (int e = 0; e < kR; ++e)
 #pragma unroll
         for (int p = 0; p < NA; ++p) x[e][p] = a_part(e, s, p);
 #pragma unroll
-        for (int p = 0; p < NB; ++p) y[e][p] = b_part(e, s, p);
-      }
+      for (int f = 0; f < 2; ++f)
+#pragma unroll
+        for (int p = 0; p < NB; ++p) y[f][p] = b_part(f, s, p);
       products([&](int p, int q) {
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
+        for (int e = 0; e < kR; ++e)
 #pragma unroll
           for (int f = 0; f < 2; ++f) sum[e][f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[e][p], y[f][q], sum[e][f], 0, 0, 0);
       });
     }
   } else {
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
+    for (int e = 0; e < kR; ++e) {
       F16 part[2];
 #pragma unroll
       for (int f = 0; f < 2; ++f)
@@ -196,10 +204,11 @@ __device__ __forceinline__ void multiply(const __bf16* a, const __bf16* b, Sums&
 }
 
 // Has a thread of the workgroup met a value that the parts do not stand for?  (One that is not finite leaves a NaN in the sums.)
-__device__ __forceinline__ bool unserved(const Sums& sum, unsigned low, unsigned* flags) {
+template <int kR>
+__device__ __forceinline__ bool unserved(const SumsOf<kR>& sum, unsigned low, unsigned* flags) {
   float mark = 0;
 #pragma unroll
-  for (int e = 0; e < 2; ++e)
+  for (int e = 0; e < kR; ++e)
 #pragma unroll
     for (int f = 0; f < 2; ++f)
 #pragma unroll
@@ -216,14 +225,14 @@ __device__ __forceinline__ bool unserved(const Sums& sum, unsigned low, unsigned
 constexpr int kPitchOut = 36;   // floats
 template <typename T>
 constexpr int piece_of() { return 16 / sizeof(T); }
-template <typename T, typename F>
-__device__ __forceinline__ void each_result(const Sums& sum, float* lds, F&& body) {
+template <typename T, int kR, typename F>
+__device__ __forceinline__ void each_result(const SumsOf<kR>& sum, float* lds, F&& body) {
   constexpr int kN = piece_of<T>(), kLanesOfRow = 32 / kN;
   const int lane = threadIdx.x & (kLanes - 1), wave = threadIdx.x / kLanes;
   float* const corner = lds + wave * 32 * kPitchOut;
   const int column = lane % kLanesOfRow * kN;
 #pragma unroll
-  for (int e = 0; e < 2; ++e)
+  for (int e = 0; e < kR; ++e)
 #pragma unroll
     for (int f = 0; f < 2; ++f) {
 #pragma unroll
@@ -240,7 +249,7 @@ __device__ __forceinline__ void each_result(const Sums& sum, float* lds, F&& bod
         }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
-      for (int i = 0; i < 16 / kN; ++i) body(wave / 2 * 64 + 32 * e + lane / kLanesOfRow + i * (kLanes / kLanesOfRow), wave % 2 * 64 + 32 * f + column, v[i]);
+      for (int i = 0; i < 16 / kN; ++i) body(wave / 2 * 32 * kR + 32 * e + lane / kLanesOfRow + i * (kLanes / kLanesOfRow), wave % 2 * 64 + 32 * f + column, v[i]);
     }
 }
 
@@ -262,56 +271,57 @@ __device__ __forceinline__ void add_piece(const __bf16* p, float (&v)[8]) {
   }
 }
 
-template <typename T, bool kBack>
-__global__ __launch_bounds__(kThreads, 2) void rows_parts_kernel(const Rows a) {
+// Tiles of 64 kR rows.
+template <typename T, bool kBack, int kR>
+__global__ __launch_bounds__(kThreads, kR == 2 || sizeof(T) == 4 ? 2 : 3) void rows_parts_kernel(const Rows a) {
+  constexpr int kTileRows = 64 * kR, kPlaneX = kTileRows * kStage;
   constexpr int NX = parts<T>(), NW = 3;
   constexpr bool kOneSum = NX == 1;
-  __shared__ __attribute__((aligned(16))) __bf16 lds[(NX + NW) * kPlane];
-  __shared__ int64_t offsets[kTile];
+  __shared__ __attribute__((aligned(16))) __bf16 lds[NX * kPlaneX + NW * kPlane];
+  __shared__ int64_t offsets[kTileRows];
   __shared__ unsigned flags[kWaves];
   static_assert(sizeof(lds) >= sizeof(BlockSpace<float>), "the blocks use the same space");
   __bf16* const xs = lds;
-  __bf16* const ws = lds + NX * kPlane;
+  __bf16* const ws = lds + NX * kPlaneX;
   const int lane = threadIdx.x & (kLanes - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
   const int columns = (a.columns + kTile - 1) / kTile;
   for (int64_t block = blockIdx.x;; block += gridDim.x) {
     int which;
-    const Place p = place_of(a.group.offsets, a.elements + 1, a.n, block, columns, [&](int atoms) { return (atoms * a.components + kTile - 1) / kTile; }, &which);
+    const Place p = place_of(a.group.offsets, a.elements + 1, a.n, block, columns, [&](int atoms) { return (atoms * a.components + kTileRows - 1) / kTileRows; }, &which);
     if (p.bucket < 0) return;
-    const int rows = p.atoms * a.components, first = p.local * kTile, c0 = which * kTile;
+    const int rows = p.atoms * a.components, first = p.local * kTileRows, c0 = which * kTile;
     __syncthreads();   // (the offsets of the tile before)
-    if (threadIdx.x < kTile) {
+    if (threadIdx.x < kTileRows) {
       const int r = min(first + static_cast<int>(threadIdx.x), rows - 1);
       offsets[threadIdx.x] = row_offset(a.group.order, a.n, p.begin, r, a.components, a.ld_dst, a.columns);
     }
-    Sums sum;
-    clear(sum);
+    SumsOf<kR> sum;
+    clear<kR>(sum);
     unsigned low = 0;
     if (p.bucket < a.elements) {
       const float* const W = static_cast<const float*>(a.W) + static_cast<int64_t>(p.bucket) * a.reduced * a.columns;
-      // two rows of the operand a thread, a piece of eight of each
+      // kR rows of X and (kBack) two of W a thread, a piece of eight of each
       const int piece = threadIdx.x % 4;
-      const T* x[2];
-      int x_to[2], w_to[2];
+      const T* x[kR];
+      int to[2];
       const float* w[2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int r = i * 64 + threadIdx.x / 4;
-        x[i] = row_at(static_cast<const T*>(a.src), a.group.order, a.n, p.begin, min(first + r, rows - 1), a.components, a.ld_src, a.reduced);
-        x_to[i] = r * kStage + (piece ^ swizzle(r)) * 8;
-        w[i] = W + static_cast<int64_t>(min(c0 + r, a.columns - 1)) * a.reduced;   // kBack
-        w_to[i] = x_to[i];
+        if (i < kR) x[i] = row_at(static_cast<const T*>(a.src), a.group.order, a.n, p.begin, min(first + r, rows - 1), a.components, a.ld_src, a.reduced);
+        to[i] = r * kStage + (piece ^ swizzle(r)) * 8;
+        w[i] = W + static_cast<int64_t>(min(c0 + r, a.columns - 1)) * a.reduced;
       }
       const int pair = 2 * lane;                                                   // forward: columns c0 + pair, + 1 of rows 8 wave on
       const float* const w_rows = W + min(c0 + pair, a.columns - 2);
-      constexpr int kAhead = sizeof(T) == 2 ? 2 : 1;   // stages of rows under way (fp32: registers for one; W comes from the caches: one)
-      Eight<T> xv[kAhead][2];
+      constexpr int kAhead = sizeof(T) == 2 || kR == 1 ? 2 : 1;   // stages of rows under way, as registers allow (of W one)
+      Eight<T> xv[kAhead][kR];
       Eight<float> wv[2];
       TwoColumns<float> wc;
-      auto request_rows = [&](int k, Eight<T> (&v)[2]) {
+      auto request_rows = [&](int k, Eight<T> (&v)[kR]) {
         const int at = min(k + 8 * piece, a.reduced - 8);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) v[i].request(x[i] + at);
+        for (int i = 0; i < kR; ++i) v[i].request(x[i] + at);
       };
       auto request_weights = [&](int k) {
         if constexpr (kBack) {
@@ -323,29 +333,29 @@ __global__ __launch_bounds__(kThreads, 2) void rows_parts_kernel(const Rows a) {
           for (int i = 0; i < 8; ++i) wc.request(i, w_rows + static_cast<int64_t>(min(k + 8 * wave + i, a.reduced - 1)) * a.columns);
         }
       };
-      auto stage = [&](int k, Eight<T> (&v)[2]) {
+      auto stage = [&](int k, Eight<T> (&v)[kR]) {
         if (k > 0) barrier();   // the stage before has been read
         if (k + kStage > a.reduced) {
           const bool inside = k + 8 * piece < a.reduced;
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            if (!inside) v[i].clear();
+            if (i < kR && !inside) v[i].clear();
             if (kBack && !inside) wv[i].clear();
           }
           if (!kBack) wc.clear_from(a.reduced - k - 8 * wave);
         }
 #pragma unroll
-        for (int i = 0; i < 2; ++i) v[i].put(xs + x_to[i], low);
+        for (int i = 0; i < kR; ++i) v[i].put(xs + to[i], kPlaneX, low);
         if constexpr (kBack) {
 #pragma unroll
-          for (int i = 0; i < 2; ++i) wv[i].put(ws + w_to[i], low);
+          for (int i = 0; i < 2; ++i) wv[i].put(ws + to[i], kPlane, low);
         } else {
           wc.put(wave, pair, ws, low);
         }
         if (k + kStage < a.reduced) request_weights(k + kStage);
         if (k + kAhead * kStage < a.reduced) request_rows(k + kAhead * kStage, v);
         barrier();
-        multiply<NX, NW, kOneSum>(xs, ws, sum);
+        multiply<NX, NW, kR, kOneSum>(xs, ws, rows - first, sum);
       };
       request_rows(0, xv[0]);
       request_weights(0);
@@ -354,9 +364,9 @@ __global__ __launch_bounds__(kThreads, 2) void rows_parts_kernel(const Rows a) {
         stage(k, xv[0]);
         if (kAhead > 1 && k + kStage < a.reduced) stage(k + kStage, xv[kAhead - 1]);
       }
-      if (unserved(sum, low, flags)) {
+      if (unserved<kR>(sum, low, flags)) {
         BlockSpace<float>& space = *reinterpret_cast<BlockSpace<float>*>(lds);
-        for (int q = 0; q < 4; ++q)
+        for (int q = 0; q < 2 * kR; ++q)
           if (first + q / 2 * kBlock < rows && c0 + q % 2 * kBlock < a.columns)
             rows_block<T, float, kBack>(a, p.bucket, p.begin, rows, first + q / 2 * kBlock, c0 + q % 2 * kBlock, space);
         continue;
@@ -366,7 +376,7 @@ __global__ __launch_bounds__(kThreads, 2) void rows_parts_kernel(const Rows a) {
     }
     T* const dst = static_cast<T*>(a.dst);
     const T* const residual = static_cast<const T*>(a.residual);
-    each_result<T>(sum, reinterpret_cast<float*>(lds), [&](int row, int column, float (&v)[piece_of<T>()]) {
+    each_result<T, kR>(sum, reinterpret_cast<float*>(lds), [&](int row, int column, float (&v)[piece_of<T>()]) {
       if (first + row >= rows || c0 + column >= a.columns) return;   // (widths are multiples of a piece)
       const int64_t at = offsets[row] + c0 + column;
       if (residual) add_piece(residual + at, v);
@@ -416,8 +426,8 @@ __global__ __launch_bounds__(kThreads, 2) void outer_parts_kernel(const Outer a)
         gv.request(i, g_at + of_lane(g_row, i));
       }
     };
-    Sums sum;
-    clear(sum);
+    SumsOf<2> sum;
+    clear<2>(sum);
     unsigned low = 0;
     __syncthreads();
     if (c.first < c.last) {
@@ -438,16 +448,16 @@ __global__ __launch_bounds__(kThreads, 2) void outer_parts_kernel(const Outer a)
         look_up(r + 2 * kStage);
       }
       barrier();
-      multiply<N, N, false>(xs, gs, sum);
+      multiply<N, N, 2, false>(xs, gs, a.k_in - k0, sum);
     }
-    if (unserved(sum, low, flags)) {
+    if (unserved<2>(sum, low, flags)) {
       BlockSpace<float>& space = *reinterpret_cast<BlockSpace<float>*>(lds);
       for (int q = 0; q < 4; ++q)
         if (k0 + q / 2 * kBlock < a.k_in && c0 + q % 2 * kBlock < a.k_out)
           outer_block<T, float>(a, a.group.order, c.begin, c.first, c.last, k0 + q / 2 * kBlock, c0 + q % 2 * kBlock, out, space);
       continue;
     }
-    each_result<float>(sum, reinterpret_cast<float*>(lds), [&](int k, int column, const float (&v)[4]) {
+    each_result<float, 2>(sum, reinterpret_cast<float*>(lds), [&](int k, int column, const float (&v)[4]) {
       if (k0 + k < a.k_in && c0 + column < a.k_out) store_piece(out + static_cast<int64_t>(k0 + k) * a.k_out + c0 + column, v);
     });
   }
@@ -457,17 +467,25 @@ __global__ __launch_bounds__(kThreads, 2) void outer_parts_kernel(const Outer a)
 
 bool parts_serve(const gp_config* c) { return c->dtype != SC_F64 && c->k_in % 8 == 0 && c->k_out % 8 == 0; }
 
-hipError_t launch_rows_parts(const gp_config* c, const Rows& a, bool back, hipStream_t stream) {
-  const int64_t tiles = ceil_div(a.n * c->components, kTile) + std::min<int64_t>(c->num_elements + 1, a.n);
+namespace {
+
+template <typename T, int kR>
+hipError_t launch_rows_of(const gp_config* c, const Rows& a, bool back, hipStream_t stream) {
+  const int64_t tiles = ceil_div(a.n * c->components, 64 * kR) + std::min<int64_t>(c->num_elements + 1, a.n);
   const dim3 grid(static_cast<unsigned>(std::min(kMaxGrid, ceil_div(tiles * ceil_div(a.columns, kTile), kXcds) * kXcds)));
-  if (c->dtype == SC_F32) {
-    if (back) hipLaunchKernelGGL((rows_parts_kernel<float, true>), grid, dim3(kThreads), 0, stream, a);
-    else hipLaunchKernelGGL((rows_parts_kernel<float, false>), grid, dim3(kThreads), 0, stream, a);
-  } else {
-    if (back) hipLaunchKernelGGL((rows_parts_kernel<__bf16, true>), grid, dim3(kThreads), 0, stream, a);
-    else hipLaunchKernelGGL((rows_parts_kernel<__bf16, false>), grid, dim3(kThreads), 0, stream, a);
-  }
+  if (back) hipLaunchKernelGGL((rows_parts_kernel<T, true, kR>), grid, dim3(kThreads), 0, stream, a);
+  else hipLaunchKernelGGL((rows_parts_kernel<T, false, kR>), grid, dim3(kThreads), 0, stream, a);
   return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_rows_parts(const gp_config* c, const Rows& a, bool back, hipStream_t stream) {
+  // Tiles of half the height where the others would not fill the compute units.
+  const int64_t tiles = (ceil_div(a.n * c->components, 128) + std::min<int64_t>(c->num_elements + 1, a.n)) * ceil_div(a.columns, kTile);
+  const bool half = tiles <= 256;
+  if (c->dtype == SC_F32) return half ? launch_rows_of<float, 1>(c, a, back, stream) : launch_rows_of<float, 2>(c, a, back, stream);
+  return half ? launch_rows_of<__bf16, 1>(c, a, back, stream) : launch_rows_of<__bf16, 2>(c, a, back, stream);
 }
 
 hipError_t launch_outer_parts(const gp_config* c, const Outer& a, hipStream_t stream) {

@@ -98,7 +98,7 @@ __global__ __launch_bounds__(kThreads) void zero_kernel(TA* p, int64_t n) {
 int chunk_rows(const gp_config* c, int64_t n) {
   const int64_t rows = n * c->components, side = parts_serve(c) ? 128 : kBlock, tiles = ceil_div(c->k_in, side) * ceil_div(c->k_out, side);
   const int64_t wanted = std::max<int64_t>(1, 384 / tiles);
-  return static_cast<int>(std::min<int64_t>(std::max<int64_t>(256, ceil_div(ceil_div(rows, wanted), kBlock) * kBlock), int64_t(1) << 30));
+  return static_cast<int>(std::min<int64_t>(std::max<int64_t>(128, ceil_div(ceil_div(rows, wanted), kBlock) * kBlock), int64_t(1) << 30));
 }
 // Chunks of the elements that have several, at most.
 int64_t slots_of(const gp_config* c, int64_t n) {
