@@ -151,7 +151,7 @@ __device__ __forceinline__ T* row_at(T* p, const int32_t* order, int64_t n, int 
 // An element without rows has a chunk too, which zeroes its matrix.
 __device__ __forceinline__ int chunks_of(int rows, int per) { return max(1, static_cast<int>((static_cast<unsigned>(rows) + per - 1) / static_cast<unsigned>(per))); }
 
-// Widths that are multiples of 8, on bfloat16 parts (gp_parts.hip).  T: SC_F32 or SC_BF16 rows.
+// Rows of fp32 and bfloat16, widths from 2 on, on bfloat16 parts (gp_parts.hip).
 bool parts_serve(const gp_config* c);
 hipError_t launch_rows_parts(const gp_config* c, const Rows& a, bool back, hipStream_t stream);
 hipError_t launch_outer_parts(const gp_config* c, const Outer& a, hipStream_t stream);

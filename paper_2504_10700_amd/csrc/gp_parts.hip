@@ -1,4 +1,4 @@
-// The products by element on the bfloat16 matrix cores, for widths that are multiples of 8.
+// The products by element on the bfloat16 matrix cores, for widths from 2 on.
 //
 // An fp32 value is the sum of three bfloat16 parts h + m + l (el::split_pair), a bfloat16 row its own only part.  Rows of fp32: h h' and the five products
 // h m', m h', m m', h l', l h' (what is left out is below 2^-24 of the product); rows of bfloat16 with W: three products; dW of bfloat16 rows: one.  An instruction cuts
@@ -38,7 +38,7 @@ __device__ __forceinline__ int swizzle(int row) { return ((row >> 1) & 3) ^ ((ro
 
 __device__ __forceinline__ void barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }   // (requests to memory stay under way)
 
-// Eight reduced indices of one row of an operand: raw elements, and as its parts in LDS.
+// Eight reduced indices of one row of an operand: raw elements (request_some: the first n, zeros behind them), and as its parts in LDS.
 template <typename T>
 struct Eight;
 template <>
@@ -49,6 +49,10 @@ struct Eight<float> {
     v[1] = *reinterpret_cast<const F4*>(p + 4);
   }
   __device__ __forceinline__ void clear() { v[0] = v[1] = F4{0, 0, 0, 0}; }
+  __device__ __forceinline__ void request_some(const float* p, int n) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i / 4][i % 4] = i < n ? p[i] : 0.f;
+  }
   __device__ __forceinline__ void put(__bf16* to, int plane, unsigned& low) const {
     U4 p[3];
 #pragma unroll
@@ -67,6 +71,14 @@ struct Eight<__bf16> {
   U4 v;
   __device__ __forceinline__ void request(const __bf16* p) { v = *reinterpret_cast<const U4Loose*>(p); }
   __device__ __forceinline__ void clear() { v = U4{0, 0, 0, 0}; }
+  __device__ __forceinline__ void request_some(const __bf16* p, int n) {
+    const unsigned short* const bits = reinterpret_cast<const unsigned short*>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const unsigned x = 2 * i < n ? bits[2 * i] : 0u, y = 2 * i + 1 < n ? bits[2 * i + 1] : 0u;
+      v[i] = x | y << 16;
+    }
+  }
   __device__ __forceinline__ void put(__bf16* to, int, unsigned&) const { *reinterpret_cast<U4*>(to) = v; }
 };
 
@@ -80,6 +92,11 @@ struct TwoColumns<float> {
   __device__ __forceinline__ void clear_from(int n) {   // of the eight
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = i < n ? v[i] : F2{0, 0};
+  }
+  // the first column where the second one was requested as the last of the row
+  __device__ __forceinline__ void shift(bool alone) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i][0] = alone ? v[i][1] : v[i][0];
   }
   __device__ __forceinline__ void put(int piece, int row, __bf16* to, unsigned& low) const {
 #pragma unroll
@@ -104,6 +121,10 @@ struct TwoColumns<__bf16> {
   __device__ __forceinline__ void clear_from(int n) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = i < n ? v[i] : 0u;
+  }
+  __device__ __forceinline__ void shift(bool alone) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = alone ? v[i] >> 16 : v[i];
   }
   __device__ __forceinline__ void put(int piece, int row, __bf16* to, unsigned&) const {
     U4 p[2];
@@ -253,26 +274,39 @@ __device__ __forceinline__ void each_result(const SumsOf<kR>& sum, float* lds, F
     }
 }
 
-__device__ __forceinline__ void store_piece(float* p, const float (&v)[4]) { *reinterpret_cast<F4*>(p) = F4{v[0], v[1], v[2], v[3]}; }
-__device__ __forceinline__ void store_piece(__bf16* p, const float (&v)[8]) {
-  *reinterpret_cast<U4Loose*>(p) = U4Loose{el::pack_bf16(v[0], v[1]), el::pack_bf16(v[2], v[3]), el::pack_bf16(v[4], v[5]), el::pack_bf16(v[6], v[7])};
-}
-__device__ __forceinline__ void add_piece(const float* p, float (&v)[4]) {
-  const F4 x = *reinterpret_cast<const F4*>(p);
+// A piece of results to p, with what stands at `residual` (NULL: nothing); `inside` of its elements are there.
+template <typename T, int kN>
+__device__ __forceinline__ void store_piece(T* p, const T* residual, int inside, float (&v)[kN]) {
+  static_assert(kN * sizeof(T) == 16, "a piece is 16 bytes");
+  if (inside >= kN) {
+    if constexpr (sizeof(T) == 4) {
+      if (residual) {
+        const F4 x = *reinterpret_cast<const F4*>(residual);
 #pragma unroll
-  for (int k = 0; k < 4; ++k) v[k] += x[k];
-}
-__device__ __forceinline__ void add_piece(const __bf16* p, float (&v)[8]) {
-  const U4 x = *reinterpret_cast<const U4Loose*>(p);
+        for (int k = 0; k < 4; ++k) v[k] += x[k];
+      }
+      *reinterpret_cast<F4*>(p) = F4{v[0], v[1], v[2], v[3]};
+    } else {
+      if (residual) {
+        const U4 x = *reinterpret_cast<const U4Loose*>(residual);
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    v[2 * k] += el::low_half(x[k]);
-    v[2 * k + 1] += el::high_half(x[k]);
+        for (int k = 0; k < 4; ++k) {
+          v[2 * k] += el::low_half(x[k]);
+          v[2 * k + 1] += el::high_half(x[k]);
+        }
+      }
+      *reinterpret_cast<U4Loose*>(p) = U4Loose{el::pack_bf16(v[0], v[1]), el::pack_bf16(v[2], v[3]), el::pack_bf16(v[4], v[5]), el::pack_bf16(v[6], v[7])};
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < kN; ++k)
+      if (k < inside) p[k] = static_cast<T>(residual ? v[k] + static_cast<float>(residual[k]) : v[k]);
   }
 }
 
-// Tiles of 64 kR rows.
-template <typename T, bool kBack, int kR>
+// Tiles of 64 kR rows.  kEights: widths are multiples of 8, so a piece is all there or not at all, and no request needs a test of its own (vectors of 128: 53 us, 58
+// with the tests).
+template <typename T, bool kBack, int kR, bool kEights>
 __global__ __launch_bounds__(kThreads, kR == 2 || sizeof(T) == 4 ? 2 : 3) void rows_parts_kernel(const Rows a) {
   constexpr int kTileRows = 64 * kR, kPlaneX = kTileRows * kStage;
   constexpr int NX = parts<T>(), NW = 3;
@@ -319,15 +353,21 @@ __global__ __launch_bounds__(kThreads, kR == 2 || sizeof(T) == 4 ? 2 : 3) void r
       Eight<float> wv[2];
       TwoColumns<float> wc;
       auto request_rows = [&](int k, Eight<T> (&v)[kR]) {
-        const int at = min(k + 8 * piece, a.reduced - 8);
+        const int at = kEights ? min(k + 8 * piece, a.reduced - 8) : k + 8 * piece;
 #pragma unroll
-        for (int i = 0; i < kR; ++i) v[i].request(x[i] + at);
+        for (int i = 0; i < kR; ++i) {
+          if (kEights || k + kStage <= a.reduced) v[i].request(x[i] + at);
+          else v[i].request_some(x[i] + at, a.reduced - at);
+        }
       };
       auto request_weights = [&](int k) {
         if constexpr (kBack) {
-          const int at = min(k + 8 * piece, a.reduced - 8);
+          const int at = kEights ? min(k + 8 * piece, a.reduced - 8) : k + 8 * piece;
 #pragma unroll
-          for (int i = 0; i < 2; ++i) wv[i].request(w[i] + at);
+          for (int i = 0; i < 2; ++i) {
+            if (kEights || k + kStage <= a.reduced) wv[i].request(w[i] + at);
+            else wv[i].request_some(w[i] + at, a.reduced - at);
+          }
         } else {
 #pragma unroll
           for (int i = 0; i < 8; ++i) wc.request(i, w_rows + static_cast<int64_t>(min(k + 8 * wave + i, a.reduced - 1)) * a.columns);
@@ -339,11 +379,12 @@ __global__ __launch_bounds__(kThreads, kR == 2 || sizeof(T) == 4 ? 2 : 3) void r
           const bool inside = k + 8 * piece < a.reduced;
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            if (i < kR && !inside) v[i].clear();
-            if (kBack && !inside) wv[i].clear();
+            if (kEights && i < kR && !inside) v[i].clear();
+            if (kEights && kBack && !inside) wv[i].clear();
           }
           if (!kBack) wc.clear_from(a.reduced - k - 8 * wave);
         }
+        if (!kEights && !kBack && a.columns % 2) wc.shift(c0 + pair == a.columns - 1);
 #pragma unroll
         for (int i = 0; i < kR; ++i) v[i].put(xs + to[i], kPlaneX, low);
         if constexpr (kBack) {
@@ -377,10 +418,9 @@ __global__ __launch_bounds__(kThreads, kR == 2 || sizeof(T) == 4 ? 2 : 3) void r
     T* const dst = static_cast<T*>(a.dst);
     const T* const residual = static_cast<const T*>(a.residual);
     each_result<T, kR>(sum, reinterpret_cast<float*>(lds), [&](int row, int column, float (&v)[piece_of<T>()]) {
-      if (first + row >= rows || c0 + column >= a.columns) return;   // (widths are multiples of a piece)
+      if (first + row >= rows || c0 + column >= a.columns) return;
       const int64_t at = offsets[row] + c0 + column;
-      if (residual) add_piece(residual + at, v);
-      store_piece(dst + at, v);
+      store_piece(dst + at, residual ? residual + at : nullptr, kEights ? 8 : a.columns - c0 - column, v);
     });
   }
 }
@@ -441,6 +481,8 @@ __global__ __launch_bounds__(kThreads, 2) void outer_parts_kernel(const Outer a)
         xv.clear_from(c.last - r - 8 * wave);
         gv.clear_from(c.last - r - 8 * wave);
       }
+      if (a.k_in % 2) xv.shift(k0 + pair == a.k_in - 1);
+      if (a.k_out % 2) gv.shift(c0 + pair == a.k_out - 1);
       xv.put(wave, pair, xs, low);
       gv.put(wave, pair, gs, low);
       if (r + kStage < c.last) {
@@ -457,15 +499,16 @@ __global__ __launch_bounds__(kThreads, 2) void outer_parts_kernel(const Outer a)
           outer_block<T, float>(a, a.group.order, c.begin, c.first, c.last, k0 + q / 2 * kBlock, c0 + q % 2 * kBlock, out, space);
       continue;
     }
-    each_result<float, 2>(sum, reinterpret_cast<float*>(lds), [&](int k, int column, const float (&v)[4]) {
-      if (k0 + k < a.k_in && c0 + column < a.k_out) store_piece(out + static_cast<int64_t>(k0 + k) * a.k_out + c0 + column, v);
+    each_result<float, 2>(sum, reinterpret_cast<float*>(lds), [&](int k, int column, float (&v)[4]) {
+      if (k0 + k < a.k_in && c0 + column < a.k_out)
+        store_piece<float>(out + static_cast<int64_t>(k0 + k) * a.k_out + c0 + column, nullptr, a.k_out - c0 - column, v);
     });
   }
 }
 
 }  // namespace
 
-bool parts_serve(const gp_config* c) { return c->dtype != SC_F64 && c->k_in % 8 == 0 && c->k_out % 8 == 0; }
+bool parts_serve(const gp_config* c) { return c->dtype != SC_F64 && c->k_in >= 2 && c->k_out >= 2; }
 
 namespace {
 
@@ -473,8 +516,10 @@ template <typename T, int kR>
 hipError_t launch_rows_of(const gp_config* c, const Rows& a, bool back, hipStream_t stream) {
   const int64_t tiles = ceil_div(a.n * c->components, 64 * kR) + std::min<int64_t>(c->num_elements + 1, a.n);
   const dim3 grid(static_cast<unsigned>(std::min(kMaxGrid, ceil_div(tiles * ceil_div(a.columns, kTile), kXcds) * kXcds)));
-  if (back) hipLaunchKernelGGL((rows_parts_kernel<T, true, kR>), grid, dim3(kThreads), 0, stream, a);
-  else hipLaunchKernelGGL((rows_parts_kernel<T, false, kR>), grid, dim3(kThreads), 0, stream, a);
+  const bool eights = a.reduced % 8 == 0 && a.columns % 8 == 0;
+  auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, stream, a); };
+  if (back) eights ? launch(&rows_parts_kernel<T, true, kR, true>) : launch(&rows_parts_kernel<T, true, kR, false>);
+  else eights ? launch(&rows_parts_kernel<T, false, kR, true>) : launch(&rows_parts_kernel<T, false, kR, false>);
   return hipGetLastError();
 }
 

@@ -1,5 +1,5 @@
-// The products by element of include/gp.h: arguments, entry points, and the kernels that serve every width and type (gp_parts.hip: widths that are multiples
-// of 8 in fp32 and bfloat16; gp_few.hip: the rows of batches without a grouping).
+// The products by element of include/gp.h: arguments, entry points, and the kernels that serve every width and type (gp_parts.hip: fp32 and
+// bfloat16 on the bfloat16 matrix cores; gp_few.hip: the rows of batches without a grouping).
 //
 // Rows (Y, dX): a workgroup computes 64 rows of one bucket x 64 columns; the rows are gathered by the grouping's order, the reduced index goes
 // through LDS 16 at a time.  dW: a workgroup computes 64 x 64 of one element's matrix over a chunk of the element's rows; elements with several chunks leave
