@@ -77,10 +77,14 @@ __device__ __forceinline__ int item_of(const Item* __restrict__ items, int n, in
 
 __device__ __forceinline__ int64_t chunks_of(int64_t elements) { return (elements + kChunk - 1) / kChunk; }
 
-// fp32 values as two fp16 parts, v = h + l.
-__device__ __forceinline__ void split(float v, _Float16& h, _Float16& l) {
-  h = static_cast<_Float16>(v);
-  l = static_cast<_Float16>(v - static_cast<float>(h));
+// Two fp32 values as two fp16 parts each, v = h + l, a 16-bit half each.
+typedef _Float16 H2 __attribute__((ext_vector_type(2)));
+typedef float F2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ void split2(float v, float w, unsigned& h, unsigned& l) {
+  const F2 x{v, w};
+  const H2 y = __builtin_convertvector(x, H2);
+  h = __builtin_bit_cast(unsigned, y);
+  l = __builtin_bit_cast(unsigned, __builtin_convertvector(x - __builtin_convertvector(y, F2), H2));
 }
 
 // U of an element from its gradient and the momentum that the step leaves.

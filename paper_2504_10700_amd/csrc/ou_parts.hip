@@ -24,6 +24,7 @@ namespace {
 
 typedef _Float16 H8 __attribute__((ext_vector_type(8)));
 typedef float F16 __attribute__((ext_vector_type(16)));
+typedef unsigned U4 __attribute__((ext_vector_type(4)));
 typedef float F4 __attribute__((ext_vector_type(4)));
 typedef float F4Loose __attribute__((ext_vector_type(4), aligned(4)));
 
@@ -59,21 +60,38 @@ struct Scales {
   float down;    // sums of parts to values
 };
 
-// Sixteen consecutive values of a row from column c (a multiple of 16) on, times `up`, to both parts; those from `inside` on are zeros.
-__device__ __forceinline__ void put_parts(const float (&v)[16], float up, int inside, _Float16* row, int c) {
-  _Float16* const to = row + 2 * (c & ~31) + (c & 31);
+// The parts of a 32 x 32 block in LDS to rows of parts that begin at `to`, `pitch` apart; the block's columns are c on, a multiple of 32.  kTurned: value (i, j) is at
+// block[j * kStep + i], otherwise at block[i * kStep + j].  Rows from `rows` on are not there, columns from `inside` on are zeros.  Eight lanes write the line of a row,
+// the first four its h, eight values each, the others its l in reverse: a lane splits four of the eight values, and its mirror image the other four.
+template <bool kTurned, int kStep>
+__device__ __forceinline__ void put_parts(const float* block, float up, int rows, int inside, _Float16* to, int64_t pitch, int c) {
+  const int lane = threadIdx.x & (kLanes - 1);
+  const bool second = lane & 4;
+  const int piece = (second ? 7 - lane % 8 : lane % 8) * 8, mine = piece + (second ? 4 : 0);
 #pragma unroll
-  for (int b = 0; b < 16; b += 8) {
-    H8 h, l;
+  for (int k = 0; k < 4; ++k) {
+    const int row = lane / 8 + 8 * k;
+    float v[4];
+    if (!kTurned && kStep % 4 == 0) {
+      const F4 x = *reinterpret_cast<const F4*>(block + row * kStep + mine);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      _Float16 x, y;
-      split(b + i < inside ? v[b + i] * up : 0.f, x, y);
-      h[i] = x;
-      l[i] = y;
+      for (int i = 0; i < 4; ++i) v[i] = x[i];
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = kTurned ? block[(mine + i) * kStep + row] : block[row * kStep + mine + i];
     }
-    *reinterpret_cast<H8*>(to + b) = h;
-    *reinterpret_cast<H8*>(to + 32 + b) = l;
+    if (inside < 32) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = mine + i < inside ? v[i] : 0.f;
+    }
+    unsigned h[2], l[2], other[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      split2(v[2 * i] * up, v[2 * i + 1] * up, h[i], l[i]);
+      other[i] = __builtin_amdgcn_update_dpp(0u, second ? h[i] : l[i], 0x141, 0xf, 0xf, true);   // (row_half_mirror)
+    }
+    const U4 parts = second ? U4{other[0], other[1], l[0], l[1]} : U4{h[0], h[1], other[0], other[1]};
+    if (row < rows) *reinterpret_cast<U4*>(to + row * pitch + 2 * c + (second ? 32 : 0) + piece) = parts;
   }
 }
 
@@ -108,19 +126,13 @@ __global__ __launch_bounds__(kThreads) void normalise_kernel(const Item* __restr
   const int i0 = turned ? c0 : r0, j0 = turned ? r0 : c0;   // of the m x l matrix
   for (int i = threadIdx.x; i < 64 * 64; i += kThreads)
     if (i0 + i / 64 < m && j0 + i % 64 < l) buf.X[it.x + matrix * size + static_cast<int64_t>(i0 + i / 64) * l + j0 + i % 64] = block[i / 64][i % 64];
+  // (a wave a quarter of the block)
   const int64_t lp = padded(l), mp = padded(m);
-  const int row = threadIdx.x / 4, from = threadIdx.x % 4 * 16;
-  float v[16];
-  if (i0 + row < m && j0 + from < lp) {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = block[row][from + i];
-    put_parts(v, up, l - j0 - from, buf.x + it.px + 2 * (matrix * m + i0 + row) * lp, j0 + from);
-  }
-  if (j0 + row < l && i0 + from < mp) {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = block[from + i][row];
-    put_parts(v, up, m - i0 - from, buf.t + it.pt + 2 * (matrix * l + j0 + row) * mp, i0 + from);
-  }
+  const int wave = threadIdx.x / kLanes, qi = wave / 2 * 32, qj = wave % 2 * 32;
+  const int ib = i0 + qi, jb = j0 + qj;
+  if (ib >= m || jb >= l) return;
+  put_parts<false, 65>(&block[qi][qj], up, m - ib, l - jb, buf.x + it.px + 2 * (matrix * m + ib) * lp, 2 * lp, jb);
+  put_parts<true, 65>(&block[qi][qj], up, l - jb, m - ib, buf.t + it.pt + 2 * (matrix * l + jb) * mp, 2 * mp, ib);
 }
 
 // Tile t of those on and below the diagonal of rows x rows tiles.  Eight rows of tiles at a time, column after column, so that what runs at the same time on
@@ -174,6 +186,24 @@ __device__ __forceinline__ void stage_arrived(int left) {
   if constexpr (kAhead == 0) arrived<0>();
   else if (left >= kAhead) arrived<kAhead * kLoads>();
   else stage_arrived<kAhead - 1, kLoads>(left);
+}
+
+// Four finished elements of X of which `inside` are there.
+__device__ __forceinline__ void finish4(const Item& it, const Step& st, int64_t at, int inside, const F4& x) {
+  if (inside >= 4 && it.dtype == SC_F32) {
+    if (it.update) *reinterpret_cast<F4Loose*>(static_cast<float*>(it.update) + at) = x;
+    if (it.weight) {
+      F4Loose* const w = reinterpret_cast<F4Loose*>(static_cast<float*>(it.weight) + at);
+      F4 v = *w;
+#pragma unroll
+      for (int n = 0; n < 4; ++n) v[n] = new_weight(it, st, static_cast<float>(v[n]), static_cast<float>(x[n]));
+      *w = v;
+    }
+    return;
+  }
+#pragma unroll
+  for (int n = 0; n < 4; ++n)
+    if (n < inside) finish(it, st, at + n, static_cast<float>(x[n]));
 }
 
 enum Phase { kS, kP, kX };
@@ -329,9 +359,10 @@ __global__ __launch_bounds__(kThreads, kStages == 2 ? 2 : 1) void product_kernel
   // results, 32 x 32 at a time through the wave's corner of LDS: row by row, then column by column
   __syncthreads();
   float* const corner = reinterpret_cast<float*>(lds) + wave * 32 * kPitch;
-  const int row = lane / 2, begin = lane % 2 * 16;
+  const int row = lane / 8, column = lane % 8 * 4;   // fp32 values: eight lanes have a line
   const bool mirrored = kPhase != kX && ti != tj;
   const int columns = kPhase == kX ? l : m;
+  const float ca = static_cast<float>(st.a), cb = static_cast<float>(st.b), cc = static_cast<float>(st.c);
 #pragma unroll
   for (int e = 0; e < kSide; ++e)
 #pragma unroll
@@ -341,91 +372,62 @@ __global__ __launch_bounds__(kThreads, kStages == 2 ? 2 : 1) void product_kernel
 #pragma unroll
       for (int r = 0; r < 16; ++r) corner[(8 * (r / 4) + 4 * (lane / 32) + r % 4) * kPitch + (lane & 31)] = sum[e][f][r] * sc.down;
       wave_sync();
-      float v[16];
+      // what the phase makes of the sums, in fp32
 #pragma unroll
-      for (int r = 0; r < 16; r += 4) {
-        const F4 x = *reinterpret_cast<const F4*>(corner + row * kPitch + begin + r);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) v[r + k] = x[k];
-      }
-      const int i = ib + row, j = jb + begin;
-      if (i < m) {
-        if constexpr (kPhase == kX) {
-          const int64_t x0 = it.x + (static_cast<int64_t>(matrix) * m + i) * l + j;
-          float x[16];
-          if (j + 16 <= l) {
-#pragma unroll
-            for (int r = 0; r < 16; r += 4) {
-              const F4 w = *reinterpret_cast<const F4Loose*>(buf.X + x0 + r);
-#pragma unroll
-              for (int k = 0; k < 4; ++k) x[r + k] = w[k];
-            }
-          } else {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) x[r] = j + r < l ? buf.X[x0 + r] : 0.f;
-          }
-          const float ca = static_cast<float>(st.a);
-#pragma unroll
-          for (int r = 0; r < 16; ++r) v[r] = ca * x[r] + v[r];
-          if (last) {
-            if (!turned) {
-#pragma unroll
-              for (int r = 0; r < 16; ++r)
-                if (j + r < l) finish(it, st, (static_cast<int64_t>(matrix) * m + i) * l + j + r, v[r]);
-            }
-          } else {
-            if (j + 16 <= l) {
-#pragma unroll
-              for (int r = 0; r < 16; r += 4) *reinterpret_cast<F4Loose*>(buf.X + x0 + r) = F4{v[r], v[r + 1], v[r + 2], v[r + 3]};
+      for (int k = 0; k < 4; ++k) {
+        const int i = ib + row + 8 * k, j = jb + column;
+        float* const here = corner + (row + 8 * k) * kPitch + column;
+        F4 v = *reinterpret_cast<const F4*>(here);
+        if (i < m) {
+          if constexpr (kPhase == kX) {
+            const int64_t at = (static_cast<int64_t>(matrix) * m + i) * l + j;
+            float* const X = buf.X + it.x + at;
+            F4 x{0, 0, 0, 0};
+            if (j + 4 <= l) {
+              x = *reinterpret_cast<const F4Loose*>(X);
             } else {
 #pragma unroll
-              for (int r = 0; r < 16; ++r)
-                if (j + r < l) buf.X[x0 + r] = v[r];
+              for (int n = 0; n < 4; ++n) x[n] = j + n < l ? X[n] : 0.f;
             }
-            put_parts(v, sc.up, l - j, buf.x + it.px + 2 * (matrix * m + i) * lp, j);
+            v = ca * x + v;
+            if (last) {
+              if (!turned) finish4(it, st, at, l - j, v);
+            } else if (j + 4 <= l) {
+              *reinterpret_cast<F4Loose*>(X) = v;
+            } else {
+#pragma unroll
+              for (int n = 0; n < 4; ++n)
+                if (j + n < l) X[n] = v[n];
+            }
+          } else {
+            F4* const S = reinterpret_cast<F4*>(buf.S + it.s + (matrix * m + i) * mp + j);
+            if constexpr (kPhase == kS) *S = v;
+            else v = cb * *S + cc * v;
+          }
+        }
+        if constexpr (kPhase != kS) *reinterpret_cast<F4*>(here) = v;
+      }
+      if constexpr (kPhase != kS) wave_sync();
+      if constexpr (kPhase == kX) {
+        if (last) {
+          if (turned) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const int j = jb + row + 8 * k, i = ib + column;
+              F4 v;
+#pragma unroll
+              for (int n = 0; n < 4; ++n) v[n] = corner[(column + n) * kPitch + row + 8 * k];
+              if (j < l && i < m) finish4(it, st, (static_cast<int64_t>(matrix) * l + j) * m + i, m - i, v);
+            }
           }
         } else {
-          float* const S = buf.S + it.s + (matrix * m + i) * mp + j;
-          if constexpr (kPhase == kS) {
-#pragma unroll
-            for (int r = 0; r < 16; r += 4) *reinterpret_cast<F4*>(S + r) = F4{v[r], v[r + 1], v[r + 2], v[r + 3]};
-          } else {
-            const float cb = static_cast<float>(st.b), cc = static_cast<float>(st.c);
-#pragma unroll
-            for (int r = 0; r < 16; r += 4) {
-              const F4 x = *reinterpret_cast<const F4*>(S + r);
-#pragma unroll
-              for (int k = 0; k < 4; ++k) v[r + k] = cb * x[k] + cc * v[r + k];
-            }
-          }
-          put_parts(v, sc.up, m - j, (kPhase == kS ? buf.s : buf.p) + it.ps + 2 * (matrix * m + i) * mp, j);
+          put_parts<false, kPitch>(corner, sc.up, m - ib, l - jb, buf.x + it.px + 2 * (matrix * m + ib) * lp, 2 * lp, jb);
+          put_parts<true, kPitch>(corner, sc.up, l - jb, m - ib, buf.next + it.pt + 2 * (matrix * l + jb) * mp, 2 * mp, ib);
         }
-      }
-      if (kPhase == kX || mirrored) {
-        if constexpr (kPhase != kS) {   // what the row pass made of the sums
-          wave_sync();
-#pragma unroll
-          for (int r = 0; r < 16; r += 4) *reinterpret_cast<F4*>(corner + row * kPitch + begin + r) = F4{v[r], v[r + 1], v[r + 2], v[r + 3]};
-          wave_sync();
-        }
-#pragma unroll
-        for (int r = 0; r < 16; ++r) v[r] = corner[(begin + r) * kPitch + row];
-        const int jc = jb + row, ic = ib + begin;
-        if (jc < columns) {
-          if constexpr (kPhase == kX) {
-            if (last) {
-              if (turned) {
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                  if (ic + r < m) finish(it, st, (static_cast<int64_t>(matrix) * l + jc) * m + ic + r, v[r]);
-              }
-            } else {
-              put_parts(v, sc.up, m - ic, buf.next + it.pt + 2 * (matrix * l + jc) * mp, ic);
-            }
-          } else {
-            put_parts(v, sc.up, m - ic, (kPhase == kS ? buf.s : buf.p) + it.ps + 2 * (matrix * m + jc) * mp, ic);
-          }
-        }
+      } else {
+        _Float16* const parts = (kPhase == kS ? buf.s : buf.p) + it.ps;
+        put_parts<false, kPitch>(corner, sc.up, m - ib, m - jb, parts + 2 * (matrix * m + ib) * mp, 2 * mp, jb);
+        if (mirrored) put_parts<true, kPitch>(corner, sc.up, m - jb, m - ib, parts + 2 * (matrix * m + jb) * mp, 2 * mp, ib);
       }
       wave_sync();
     }

@@ -129,16 +129,7 @@ __device__ __forceinline__ void multiply(const _Float16* a, const _Float16* b, i
     }
 }
 
-// Two values as their first parts and their second ones.
-typedef _Float16 H2 __attribute__((ext_vector_type(2)));
-typedef float F2 __attribute__((ext_vector_type(2)));
 typedef unsigned U2 __attribute__((ext_vector_type(2)));
-__device__ __forceinline__ void split2(float v, float w, unsigned& h, unsigned& l) {
-  const F2 x{v, w};
-  const H2 y = __builtin_convertvector(x, H2);
-  h = __builtin_bit_cast(unsigned, y);
-  l = __builtin_bit_cast(unsigned, __builtin_convertvector(x - __builtin_convertvector(y, F2), H2));
-}
 
 // Parts of the wave's blocks that begin inside rows x cols, times `up`: transposed (a lane's four consecutive rows are neighbours there), and as they are
 // (neighbouring lanes, which are columns, exchange halves, so that each writes two columns of one of two rows).
