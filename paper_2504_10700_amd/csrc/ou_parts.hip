@@ -357,17 +357,44 @@ __global__ __launch_bounds__(kThreads, kStages == 2 ? 2 : 1) void product_kernel
   }
 
   // results, 32 x 32 at a time through the wave's corner of LDS: row by row, then column by column
-  __syncthreads();
-  float* const corner = reinterpret_cast<float*>(lds) + wave * 32 * kPitch;
   const int row = lane / 8, column = lane % 8 * 4;   // fp32 values: eight lanes have a line
   const bool mirrored = kPhase != kX && ti != tj;
   const int columns = kPhase == kX ? l : m;
   const float ca = static_cast<float>(st.a), cb = static_cast<float>(st.b), cc = static_cast<float>(st.c);
+  // what stands beside a block's sums, S or X, requested a block ahead (rows beyond the last: the last one)
+  constexpr int kBlocks = kSide * kSide;
+  F4 beside[2][4];
+  auto request = [&](int block) {
+    if constexpr (kPhase == kS) return;
+    const int ib = i0 + wi + 32 * (block / kSide), jb = j0 + wj + 32 * (block % kSide);
+    if (ib >= m || jb >= columns) return;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int i = min(ib + row + 8 * k, m - 1), j = jb + column;
+      F4 x{0, 0, 0, 0};
+      if constexpr (kPhase == kP) {
+        x = *reinterpret_cast<const F4*>(buf.S + it.s + (matrix * m + i) * mp + j);
+      } else {
+        const float* const X = buf.X + it.x + (static_cast<int64_t>(matrix) * m + i) * l;
+        if (jb + 32 <= l) {
+          x = *reinterpret_cast<const F4Loose*>(X + j);
+        } else {
+#pragma unroll
+          for (int n = 0; n < 4; ++n) x[n] = X[min(j + n, l - 1)];
+        }
+      }
+      beside[block & 1][k] = x;
+    }
+  };
+  request(0);
+  __syncthreads();
+  float* const corner = reinterpret_cast<float*>(lds) + wave * 32 * kPitch;
 #pragma unroll
   for (int e = 0; e < kSide; ++e)
 #pragma unroll
     for (int f = 0; f < kSide; ++f) {
-      const int ib = i0 + wi + 32 * e, jb = j0 + wj + 32 * f;
+      const int block = e * kSide + f, ib = i0 + wi + 32 * e, jb = j0 + wj + 32 * f;
+      if (block + 1 < kBlocks) request(block + 1);
       if (ib >= m || jb >= columns) continue;
 #pragma unroll
       for (int r = 0; r < 16; ++r) corner[(8 * (r / 4) + 4 * (lane / 32) + r % 4) * kPitch + (lane & 31)] = sum[e][f][r] * sc.down;
@@ -378,18 +405,12 @@ __global__ __launch_bounds__(kThreads, kStages == 2 ? 2 : 1) void product_kernel
         const int i = ib + row + 8 * k, j = jb + column;
         float* const here = corner + (row + 8 * k) * kPitch + column;
         F4 v = *reinterpret_cast<const F4*>(here);
+        if constexpr (kPhase == kP) v = cb * beside[block & 1][k] + cc * v;
+        if constexpr (kPhase == kX) v = ca * beside[block & 1][k] + v;
         if (i < m) {
           if constexpr (kPhase == kX) {
             const int64_t at = (static_cast<int64_t>(matrix) * m + i) * l + j;
             float* const X = buf.X + it.x + at;
-            F4 x{0, 0, 0, 0};
-            if (j + 4 <= l) {
-              x = *reinterpret_cast<const F4Loose*>(X);
-            } else {
-#pragma unroll
-              for (int n = 0; n < 4; ++n) x[n] = j + n < l ? X[n] : 0.f;
-            }
-            v = ca * x + v;
             if (last) {
               if (!turned) finish4(it, st, at, l - j, v);
             } else if (j + 4 <= l) {
@@ -399,10 +420,8 @@ __global__ __launch_bounds__(kThreads, kStages == 2 ? 2 : 1) void product_kernel
               for (int n = 0; n < 4; ++n)
                 if (j + n < l) X[n] = v[n];
             }
-          } else {
-            F4* const S = reinterpret_cast<F4*>(buf.S + it.s + (matrix * m + i) * mp + j);
-            if constexpr (kPhase == kS) *S = v;
-            else v = cb * *S + cc * v;
+          } else if constexpr (kPhase == kS) {
+            *reinterpret_cast<F4*>(buf.S + it.s + (matrix * m + i) * mp + j) = v;
           }
         }
         if constexpr (kPhase != kS) *reinterpret_cast<F4*>(here) = v;
