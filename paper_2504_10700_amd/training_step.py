@@ -3,6 +3,10 @@
     element embedding -> radial network (dense layers on the edges) -> channelwise tensor product -> symmetric contraction
     -> readout (dense layers on the invariant channels) -> energies; their gradients in reverse; clipping by the global norm; update.
 
+With `self_connection` the embedded features reach the readout past the interaction too, through a matrix of their element.  With `orthogonalised` the
+matrices between features (those of the radial network, of the self connection, of the readout's first layer) take the orthogonalised update; the table, the
+contraction's weights, biases and the last layer take gradient descent, as all parameters do without it.
+
 Synthetic structures, random targets.  `python -m paper_2504_10700_amd.training_step` trains for some steps and prints the loss, the gradient's norm and
 the time of a step.  Buffers and workspaces are allocated once; a step enqueues its calls on the current stream and never synchronises.
 """
@@ -18,6 +22,8 @@ from . import binding as sc
 from . import dl_binding as dl
 from . import ee_binding as ee
 from . import gc_binding as gc
+from . import gp_binding as gp
+from . import ou_binding as ou
 from . import tp_binding as tp
 from .workloads import TPWorkload, graph_indices, make_tp_graph
 
@@ -52,7 +58,8 @@ class Dense:
 
 class Model:
     def __init__(self, num_atoms: int, mean_degree: int = 20, channels: int = 128, elements: int = 89, l_Y: int = 3, dtype: int = sc.SC_F32,
-                 max_norm: float = 10.0, learning_rate: float = 1e-2, seed: int = 7):
+                 max_norm: float = 10.0, learning_rate: float = 1e-2, seed: int = 7, self_connection: bool = False, orthogonalised: bool = False,
+                 matrix_rate: float = 1e-3):
         wl = TPWorkload("training_step", num_atoms, mean_degree, channels, l_Y, 0, l_Y, "f64" if dtype == sc.SC_F64 else "f32", seed)
         rng = np.random.default_rng(seed)
         sender, receiver = make_tp_graph(wl, rng)
@@ -90,12 +97,35 @@ class Model:
         layers = self.radial + self.readout
         self.parameters = [self.T, self.W_sc] + [p for x in layers for p in (x.W, x.b) if p is not None]
         self.gradients = [self.dT, self.dW_sc] + [p for x in layers for p in (x.dW, x.db) if p is not None]
+        needed = 0
+        self.connected = self_connection
+        if self_connection:
+            self.connection = gp.make_config(elements, channels, channels, 1, dtype)
+            self.W_own = new(elements, channels, channels, scale=channels ** -0.5)
+            self.dW_own, self.B_own, self.dh_own = torch.empty_like(self.W_own), torch.empty_like(self.B), torch.empty_like(self.h)
+            self.parameters.append(self.W_own)
+            self.gradients.append(self.dW_own)
+            # the order of the atoms by element depends on z alone: made once for the batch
+            self.grouping = torch.empty(max(gp.gp_grouping_bytes(self.connection, num_atoms), 256), dtype=torch.uint8, device="cuda")
+            gp.gp_group(self.connection, num_atoms, self.z, self.grouping, self.grouping.numel())
+            needed = gp.gp_workspace_bytes(self.connection, num_atoms)
+        self.orthogonalised = orthogonalised
+        self.descended = (self.parameters, self.gradients)
+        if orthogonalised:
+            pairs = [(x.W, x.dW) for x in self.radial + self.readout[:-1]] + ([(self.W_own, self.dW_own)] if self_connection else [])
+            matrices, of_matrices = [list(x) for x in zip(*pairs)]
+            self.momentum = [torch.zeros_like(w) for w in matrices]
+            self.update = ou.make_config(matrix_rate)
+            self.updated = ou.make_tensors(of_matrices, self.momentum, matrices, scale=[max(1.0, w.shape[-1] / w.shape[-2]) ** 0.5 for w in matrices])
+            needed = max(needed, ou.ou_workspace_bytes(self.update, self.updated))
+            others = [(p, d) for p, d in zip(self.parameters, self.gradients) if all(p is not w for w in matrices)]
+            self.descended = tuple(list(x) for x in zip(*others))
         self.clip = gc.make_config(max_norm, 1e-6, dtype)
         self.clipped = gc.make_tensors(self.gradients, self.gradients)      # in place
         self.norm = empty(2)                                                # and the coefficient
         # the contraction's workspace carries the grouping from its forward to its backward; the others share one
         self.sc_workspace = torch.empty(sc.sc_workspace_bytes(self.sc, num_atoms), dtype=torch.uint8, device="cuda")
-        self.workspace = torch.empty(max([x.workspace_bytes for x in layers] + [
+        self.workspace = torch.empty(max([needed] + [x.workspace_bytes for x in layers] + [
             ee.ee_workspace_bytes(self.embedding, num_atoms), tp.tp_workspace_bytes(self.tp, self.edges), gc.gc_workspace_bytes(self.clip, self.clipped)]),
             dtype=torch.uint8, device="cuda")
 
@@ -108,7 +138,11 @@ class Model:
         self.R = self.radial[3].forward(x)
         tp.tp_forward(self.tp, self.n, self.n, self.edges, self.Y, self.h, self.R, self.sender, self.row_ptr, self.A)
         sc.sc_forward(self.sc, self.n, self.A, self.z, self.W_sc, self.B, self.sc_workspace, self.sc_workspace.numel())
-        return self.readout[1].forward(self.readout[0].forward(self.B))
+        features = self.B
+        if self.connected:
+            features = self.B_own
+            gp.gp_forward(self.connection, self.n, self.z, self.grouping, self.h, self.W_own, self.B, features, self.workspace, self.workspace.numel())
+        return self.readout[1].forward(self.readout[0].forward(features))
 
     def loss(self):
         energy = torch.zeros_like(self.target).index_add_(0, self.structure, self.energies()[:, 0])
@@ -124,6 +158,9 @@ class Model:
                        sc.SC_REUSE_GROUPING | sc.SC_REUSE_WEIGHTS)
         tp.tp_backward(self.tp, self.n, self.n, self.edges, self.Y, self.h, self.R, self.sender, self.row_ptr, self.send_ptr, self.send_edge, self.dA,
                        self.dY, self.dh, self.dR, ws, ws.numel())
+        if self.connected:
+            gp.gp_backward(self.connection, self.n, self.z, self.grouping, self.h, self.W_own, dB, self.dh_own, self.dW_own, ws, ws.numel())
+            self.dh.add_(self.dh_own)
         ee.ee_backward(self.embedding, self.n, self.z, self.dh, self.dT, ws, ws.numel())
         dx = self.radial[3].backward(self.dR, ws)
         dx = self.radial[2].backward(dx, ws).add_(dx)        # the residual's gradient is the upstream one
@@ -131,11 +168,13 @@ class Model:
         self.radial[0].backward(dx, ws, want_dx=False)
 
     def step(self):
-        """One step of gradient descent; the loss before it, on the device."""
+        """One step of the optimizer; the loss before it, on the device."""
         loss = self.loss()
         self.backward()
         gc.gc_clip(self.clip, self.clipped, self.norm, self.workspace, self.workspace.numel())
-        torch._foreach_add_(self.parameters, self.gradients, alpha=-self.learning_rate)
+        torch._foreach_add_(*self.descended, alpha=-self.learning_rate)
+        if self.orthogonalised:
+            ou.ou_step(self.update, self.updated, self.workspace, self.workspace.numel())
         return loss
 
 
@@ -145,8 +184,10 @@ def main() -> None:
     parser.add_argument("--degree", type=int, default=20)
     parser.add_argument("--channels", type=int, default=128)
     parser.add_argument("--steps", type=int, default=20)
+    parser.add_argument("--self-connection", action="store_true", help="the embedded features reach the readout through a matrix of their element")
+    parser.add_argument("--orthogonalised", action="store_true", help="matrices take the orthogonalised update")
     args = parser.parse_args()
-    model = Model(args.atoms, args.degree, args.channels)
+    model = Model(args.atoms, args.degree, args.channels, self_connection=args.self_connection, orthogonalised=args.orthogonalised)
     print(f"{model.n} atoms, {model.edges} edges, {sum(p.numel() for p in model.parameters)} parameters", flush=True)
     for i in range(args.steps):
         torch.cuda.synchronize()
