@@ -270,3 +270,51 @@ def test_an_empty_list(ou):
     x = List(ou, [(0, 8, 8)], "float32")
     x.step()
     ou.ou_step(x.cfg, ou.make_tensors([], [], [], []), x.ws, x.nbytes)
+
+
+LONG = [(1, 3, 4500), (1, 64, 2049), (1, 5000, 100), (3, 128, 4097), (2, 2500, 33), (1, 1, 65536), (1, 1, 1), (1, 65536, 2)]
+
+
+@pytest.mark.parametrize("dtype", ["float32", "float64", "bfloat16"])
+@pytest.mark.parametrize("shape", LONG, ids=lambda s: "x".join(map(str, s)))
+def test_long_matrices(ou, shape, dtype):
+    """One side far longer than the other: more than one piece of columns to a slice."""
+    import torch
+    print(f"update long {shape} {dtype}", flush=True)
+    for skew in (0, 1):
+        x = List(ou, [shape], dtype, skew=skew)
+        before = x.host()
+        x.step()
+        torch.cuda.synchronize()
+        x.check(before, oo.iterate)
+
+
+def test_every_way_in_one_list(ou):
+    """Sizes about the limits between the kernels, of all types, in one call."""
+    import torch
+    shapes = [(n, r, c) for n, r, c in ((2, 64, 64), (1, 64, 65), (3, 65, 64), (1, 128, 128), (2, 128, 129), (1, 129, 64), (1, 129, 129), (2, 257, 130), (0, 200, 200),
+                                        (1, 2, 300), (5, 33, 31), (1, 192, 448))]
+    for types in (["float32", "bfloat16"] * 6, ["float32", "float64", "bfloat16"] * 4):
+        for skew in (0, 1):
+            x = List(ou, shapes, types, skew=skew)
+            before = x.host()
+            x.step()
+            torch.cuda.synchronize()
+            x.check(before, oo.iterate)
+
+
+def test_calls_at_the_same_time(ou):
+    """Two lists on two streams, each with its own workspace."""
+    import torch
+    shapes = [(3, 200, 300), (2, 100, 90), (1, 40, 700)]
+    want, a, b = List(ou, shapes, "float32"), List(ou, shapes, "float32"), List(ou, shapes, "float32")
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for turn in range(3):
+        want.step()
+        for s, x in zip(streams, (a, b)):
+            x.step(s)
+    torch.cuda.synchronize()
+    for x in (a, b):
+        for p, q in zip(x.momentum + x.weight + x.update, want.momentum + want.weight + want.update):
+            assert torch.equal(p, q)

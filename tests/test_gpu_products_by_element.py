@@ -52,7 +52,7 @@ class Batch:
                 z = torch.where(u < 0.05, -1 - z, torch.where(u > 0.95, elements + z, z))
         self.z = torch.as_tensor(z, device="cuda").int()
         normal = lambda *s: torch.randn(*s, generator=g, device="cuda", dtype=torch.float64)  # noqa: E731
-        self.X, self.residual, self.dY = (self.block(k, values=normal(n, components, k)) for k in (k_in, k_out, k_out))
+        self.X, self.residual, self.dY = (self.block(k, normal(n, components, k), out) for k, out in ((k_in, False), (k_out, True), (k_out, True)))
         self.W = self.skewed((elements, k_in, k_out), self.weights)
         self.W.copy_(normal(elements, k_in, k_out) * k_in ** -0.5)
         self.ws_bytes = gp.gp_workspace_bytes(self.cfg, n)
@@ -66,9 +66,9 @@ class Batch:
         n = int(np.prod(shape))
         return torch.full((n + self.skew,), fill, dtype=dtype, device="cuda")[self.skew:].view(shape)
 
-    def block(self, k, values=None):
+    def block(self, k, values=None, out=False):
         """[n][components][k] with the batch's gaps, NaN around (and in it without values)."""
-        ld = self.ld_in if k == self.k_in else self.ld_out
+        ld = self.ld_out if out or k != self.k_in else self.ld_in
         whole = self.skewed((self.n, ld), self.rows)
         view = whole[:, :self.components * k].unflatten(1, (self.components, k))
         if values is not None:
@@ -88,7 +88,7 @@ class Batch:
     def all(self, residual=True):
         import torch
         self.group()
-        Y, dX = self.block(self.k_out), self.block(self.k_in)
+        Y, dX = self.block(self.k_out, out=True), self.block(self.k_in)
         dW = self.skewed(self.W.shape, self.weights)
         self.forward(Y, self.residual if residual else None)
         self.backward(dX, dW)
@@ -363,3 +363,54 @@ def test_another_stream(gp):
     side.synchronize()
     for x, y in zip(out, want):
         assert torch.equal(x, y)
+
+
+WIDTHS = [(2, 2), (3, 5), (8, 2), (2, 200), (31, 33), (65, 8), (129, 127), (192, 66), (1, 70), (70, 1)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f64", "bf16"])
+@pytest.mark.parametrize("widths", WIDTHS, ids=lambda s: "x".join(map(str, s)))
+def test_odd_widths(gp, widths, dtype):
+    """Widths that end inside every kind of tile, dense and in wider rows that begin at any element, below and above the size that needs a grouping."""
+    for n, components, gap, skew in ((9, 3, (0, 0), 0), (64, 1, (1, 3), 1), (130, 3, (0, 0), 0), (400, 1, (7, 1), 1)):
+        print(f"products widths {widths} {dtype} {n} {components} {gap} {skew}", flush=True)
+        b = Batch(gp, n, 3, *widths, components, dtype, gap=gap, skew=skew)
+        b.check(*b.all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_calls_at_the_same_time(gp, dtype):
+    """Two calls on two streams read the same grouping and weights; each has its own workspace."""
+    import torch
+    b = Batch(gp, 5000, 7, 96, 160, 1, dtype)
+    want = b.all(residual=False)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    made = []
+    torch.cuda.synchronize()
+    for s in streams:
+        ws = torch.full((b.ws_bytes,), 255, dtype=torch.uint8, device="cuda")
+        made.append((ws, torch.full_like(want[0], NAN), torch.full_like(want[1], NAN), torch.full_like(want[2], NAN)))
+    torch.cuda.synchronize()
+    for turn in range(3):
+        for s, (ws, Y, dX, dW) in zip(streams, made):
+            gp.gp_forward(b.cfg, b.n, b.z, b.grouping, b.X, b.W, None, Y, ws, b.ws_bytes, s)
+            gp.gp_backward(b.cfg, b.n, b.z, b.grouping, b.X, b.W, b.dY, dX, dW, ws, b.ws_bytes, s)
+    torch.cuda.synchronize()
+    for _, *got in made:
+        for x, y in zip(got, want):
+            assert torch.equal(x, y)
+
+
+def test_values_beyond_the_parts_in_the_gradients(gp):
+    """Rows whose values differ by the whole range of the numbers meet in one dW; the gradients' rows too."""
+    import torch
+    for dtype in ("f32", "bf16"):
+        for n in (40, 900):
+            b = Batch(gp, n, 3, 72, 40, 2, dtype, padded=False, z=torch.arange(n) % 3)
+            up = 10.0 ** torch.linspace(-36, 30, n, dtype=torch.float64, device="cuda")[:, None, None]
+            b.X.copy_(b.X.double() * up)
+            b.dY.copy_(b.dY.double() / up.clamp(1e-34, 1e34))
+            b.W.mul_(1e-6)
+            b.residual.zero_()
+            print(f"products range {dtype} {n}", flush=True)
+            b.check(*b.all())
