@@ -18,8 +18,10 @@ namespace {
 typedef _Float16 H8 __attribute__((ext_vector_type(8)));
 typedef _Float16 H4 __attribute__((ext_vector_type(4)));
 typedef float F16 __attribute__((ext_vector_type(16)));
+typedef float F4 __attribute__((ext_vector_type(4)));
 
 constexpr int kSlices = 32;
+constexpr int kUnits = 256;   // compute units
 
 // Powers of two: values to parts, and sums of parts to values.  The same for all steps (what a step could gain by its own is the growth of the bound over the
 // steps, a bit or less with the usual coefficients), so that none is looked up between two products.
@@ -285,13 +287,13 @@ __device__ __forceinline__ void next_x(float a, float scale, const typename Shap
 
 // A matrix of m, l <= N.  Rows and columns of parts up to the next multiple of 32 are zeros, those beyond are never used.
 template <int N>
-__global__ __launch_bounds__(kThreads) void whole_kernel(const Item* __restrict__ items, int n, const Step st, int steps, const Scales sc) {
+__device__ __forceinline__ void whole(const Item* __restrict__ items, int n, int64_t unit, const Step& st, int steps, const Scales& sc) {
   using S = Shape<N>;
   extern __shared__ __attribute__((aligned(16))) _Float16 lds[];
   _Float16* const square = lds;
   _Float16* const turned_x = lds + 2 * S::kPart;
-  const Item& it = items[item_of(items, n, kBlocks, blockIdx.x)];
-  const Matrix mat = matrix_of(it, blockIdx.x - it.unit[kBlocks]);
+  const Item& it = items[item_of(items, n, kBlocks, unit)];
+  const Matrix mat = matrix_of(it, unit - it.unit[kBlocks]);
   const int m = mat.m, l = mat.l, deep_l = (l + 31) / 32 * 32, deep_m = (m + 31) / 32 * 32;
   typename S::Blocks x, s, r;
   {
@@ -321,6 +323,19 @@ __global__ __launch_bounds__(kThreads) void whole_kernel(const Item* __restrict_
   Places<N> places;
   places_of<N>(mat, mat.turned, 0, places);
   store_results<N>(it, st, mat, places, x);
+}
+
+template <int N>
+__global__ __launch_bounds__(kThreads) void whole_kernel(const Item* __restrict__ items, int n, const Step st, int steps, const Scales sc) {
+  whole<N>(items, n, blockIdx.x, st, steps, sc);
+}
+
+// Matrices of up to 128 (`large` of them) and, after them, of up to 64.
+__global__ __launch_bounds__(kThreads) void both_kernel(const Item* __restrict__ items128, int n128, int large, const Item* __restrict__ items64, int n64, const Step st,
+                                                        int steps, const Scales sc) {
+  const int unit = blockIdx.x;
+  if (unit < large) whole<128>(items128, n128, unit, st, steps, sc);
+  else whole<64>(items64, n64, unit - large, st, steps, sc);
 }
 
 // Slices of `width` columns (a multiple of N) of a matrix of m <= N.  step 0: X from the gradient; then the step before `step` of the iteration; the last one leaves the
@@ -353,15 +368,19 @@ __global__ __launch_bounds__(kThreads) void slice_kernel(const Item* __restrict_
     const int64_t per = chunks_of(static_cast<int64_t>(m) * l);
     down = down_of(squares + it.unit[kChunks] + index * per, per, st.eps, reinterpret_cast<double*>(lds));
   } else {
-    const float* from = partial + (blockIdx.x - own) * static_cast<int64_t>(S::kResults) + threadIdx.x;
-#pragma unroll 2
-    for (int k = 0; k < slices; ++k, from += S::kResults) {
+    const F4* from = reinterpret_cast<const F4*>(partial + (blockIdx.x - own) * static_cast<int64_t>(S::kResults)) + threadIdx.x;
+#pragma unroll 4 / kSide
+    for (int k = 0; k < slices; ++k, from += S::kResults / 4) {
 #pragma unroll
       for (int e = 0; e < kSide; ++e)
 #pragma unroll
         for (int f = 0; f < kSide; ++f)
 #pragma unroll
-          for (int q = 0; q < 16; ++q) s[e][f][q] += from[((e * kSide + f) * 16 + q) * kThreads];
+          for (int q = 0; q < 4; ++q) {
+            const F4 v = from[((e * kSide + f) * 4 + q) * kThreads];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[e][f][4 * q + i] += v[i];
+          }
     }
     make_p<N>(st, sc, m, deep_m, square, s);
 #pragma unroll
@@ -403,13 +422,13 @@ __global__ __launch_bounds__(kThreads) void slice_kernel(const Item* __restrict_
     __syncthreads();
   }
   if (last) return;
-  float* const to = next_partial + blockIdx.x * static_cast<int64_t>(S::kResults) + threadIdx.x;
+  F4* const to = reinterpret_cast<F4*>(next_partial + blockIdx.x * static_cast<int64_t>(S::kResults)) + threadIdx.x;
 #pragma unroll
   for (int e = 0; e < kSide; ++e)
 #pragma unroll
     for (int f = 0; f < kSide; ++f)
 #pragma unroll
-      for (int q = 0; q < 16; ++q) to[((e * kSide + f) * 16 + q) * kThreads] = s[e][f][q];
+      for (int q = 0; q < 4; ++q) to[((e * kSide + f) * 4 + q) * kThreads] = F4{s[e][f][4 * q], s[e][f][4 * q + 1], s[e][f][4 * q + 2], s[e][f][4 * q + 3]};
 }
 
 template <typename Kernel, typename... Args>
@@ -468,12 +487,19 @@ hipError_t slice_run(const Part& p, const ou_config* cfg, const Step& st, bool l
   return large ? slices<128>(p, cfg, st, base, items, stream) : slices<64>(p, cfg, st, base, items, stream);
 }
 
-hipError_t whole_run(const Part& p, const ou_config* cfg, const Step& st, bool large, char* base, hipStream_t stream) {
+// A matrix of up to 64 takes a quarter of the LDS that one of up to 128 takes, so four of them share a compute unit.  Where a unit for each
+// of both sizes is there, they have one launch (10 matrices of 128 and 6 of 64, five steps: 61 us, the launches of their own take 60 and 19).
+hipError_t whole_run(const Part& p64, const Part& p128, const ou_config* cfg, const Step& st, char* base, hipStream_t stream) {
   const Scales sc = scales_of(cfg);
-  const Item* const items = reinterpret_cast<const Item*>(base + p.at_items);
-  const int n = static_cast<int>(p.items.size());
-  return large ? launch(&whole_kernel<128>, Shape<128>::kBytes, p.units[kBlocks], stream, items, n, st, cfg->steps, sc)
-               : launch(&whole_kernel<64>, Shape<64>::kBytes, p.units[kBlocks], stream, items, n, st, cfg->steps, sc);
+  const Item* const items[2] = {reinterpret_cast<const Item*>(base + p64.at_items), reinterpret_cast<const Item*>(base + p128.at_items)};
+  const int n[2] = {static_cast<int>(p64.items.size()), static_cast<int>(p128.items.size())};
+  const int64_t units[2] = {p64.units[kBlocks], p128.units[kBlocks]};
+  if (units[0] && units[1] && units[0] + units[1] <= kUnits)
+    return launch(&both_kernel, Shape<128>::kBytes, units[0] + units[1], stream, items[1], n[1], static_cast<int>(units[1]), items[0], n[0], st, cfg->steps, sc);
+  hipError_t e = hipSuccess;
+  if (units[0]) e = launch(&whole_kernel<64>, Shape<64>::kBytes, units[0], stream, items[0], n[0], st, cfg->steps, sc);
+  if (units[1] && e == hipSuccess) e = launch(&whole_kernel<128>, Shape<128>::kBytes, units[1], stream, items[1], n[1], st, cfg->steps, sc);
+  return e;
 }
 
 }  // namespace ou

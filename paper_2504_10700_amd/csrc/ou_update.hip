@@ -1,7 +1,7 @@
 // The orthogonalised update of include/ou.h: arguments, entry points, and the kernels that serve every case.
 //
-// The list goes to the workspace once.  Then, each for all tensors of one arithmetic type together: momentum and sums of squares; X = U / norm; per
-// step S = X X^T, P = b S + c S S, X = a X + P X; the last step's results go straight into the update and the weights.
+// The list goes to the workspace once.  Then, each for all tensors of a way together: momentum and sums of squares; X = U / norm; per step S = X X^T, P = b S + c S S,
+// X = a X + P X; the last step's results go straight into the update and the weights.
 #include <algorithm>
 #include <cmath>
 #include <string>
@@ -166,8 +166,8 @@ __global__ __launch_bounds__(kThreads) void product_kernel(const Item* __restric
 
 // ---- host side
 
-// The ways: fp64; products in tiles; and matrices whose shorter side is at most 64 or 128, whole or in slices.
-enum Way { kDouble, kParts, kWhole64, kWhole128, kSlices64, kSlices128, kWays };
+// The ways: fp64; products in tiles; and matrices whose shorter side is at most 64 or 128, in slices or whole.  The three from kParts on have the first pass together.
+enum Way { kDouble, kParts, kSlices64, kSlices128, kWhole64, kWhole128, kWays };
 bool whole(int way) { return way == kWhole64 || way == kWhole128; }
 bool sliced(int way) { return way == kSlices64 || way == kSlices128; }
 bool large(int way) { return way == kWhole128 || way == kSlices128; }
@@ -175,6 +175,7 @@ bool large(int way) { return way == kWhole128 || way == kSlices128; }
 // The tensors by the way that their matrices take, and where everything lies in the workspace.
 struct Layout {
   Part part[kWays];
+  std::vector<Item> items;   // of all ways, in their order
   size_t bytes = 0;
 };
 
@@ -227,11 +228,20 @@ Layout layout_of(int64_t n, const ou_tensor* tensors, int steps) {
     p.items.push_back(it);
   }
   Room room;
+  room(n * sizeof(Item));
+  l.part[kDouble].at_partial = room(l.part[kDouble].units[kChunks] * sizeof(double));
+  int64_t chunks = 0;
+  for (int way = kParts; way <= kSlices128; ++way) {
+    for (Item& it : l.part[way].items) it.unit[kChunks] += chunks;
+    chunks += l.part[way].units[kChunks];
+  }
+  const size_t at_partial = room(chunks * sizeof(double));
   for (int way = 0; way < kWays; ++way) {
     Part& p = l.part[way];
+    p.at_items = l.items.size() * sizeof(Item);
+    l.items.insert(l.items.end(), p.items.begin(), p.items.end());
+    if (way != kDouble) p.at_partial = at_partial;
     if (p.items.empty()) continue;
-    p.at_items = room(p.items.size() * sizeof(Item));
-    p.at_partial = room(p.units[kChunks] * sizeof(double));
     if (way == kDouble) double_layout(p, room, steps);
     else if (way == kParts) parts_layout(p, room, steps);
     else if (sliced(way)) slice_layout(p, room, steps, large(way));
@@ -282,30 +292,32 @@ sc_status check(const char* fn, const ou_config* cfg, int64_t n, const ou_tensor
   return SC_OK;
 }
 
-hipError_t send(const Part& p, char* base, hipStream_t stream) {
-  const int n = static_cast<int>(p.items.size());
-  Item* const items = reinterpret_cast<Item*>(base + p.at_items);
+hipError_t send(const std::vector<Item>& items, char* base, hipStream_t stream) {
+  const int n = static_cast<int>(items.size());
   for (int first = 0; first < n; first += kSent) {
     Sent sent{};
     sent.first = first;
     sent.count = std::min(kSent, n - first);
-    std::copy_n(p.items.begin() + first, sent.count, sent.item);
-    hipLaunchKernelGGL(send_kernel, dim3(1), dim3(kLanes), 0, stream, sent, items);
+    std::copy_n(items.begin() + first, sent.count, sent.item);
+    hipLaunchKernelGGL(send_kernel, dim3(1), dim3(kLanes), 0, stream, sent, reinterpret_cast<Item*>(base));
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
 }
 
-// The items to the workspace, momentum and sums of squares.
+// Momentum and sums of squares of the ways from `way` to `end`.
 template <typename TA>
-hipError_t begin(const Part& p, const Step& st, char* base, hipStream_t stream) {
-  const hipError_t e = send(p, base, stream);
-  if (e != hipSuccess) return e;
-  const int n = static_cast<int>(p.items.size());
-  const Item* const items = reinterpret_cast<const Item*>(base + p.at_items);
-  hipLaunchKernelGGL(momentum_kernel<TA>, dim3(static_cast<unsigned>(p.units[kChunks])), dim3(kThreads), 0, stream, items, n, st,
-                     reinterpret_cast<double*>(base + p.at_partial));
+hipError_t first_pass(const Layout& l, int way, int end, const Step& st, char* base, hipStream_t stream) {
+  int n = 0;
+  int64_t chunks = 0;
+  for (int w = way; w <= end; ++w) {
+    n += static_cast<int>(l.part[w].items.size());
+    chunks += l.part[w].units[kChunks];
+  }
+  if (n == 0) return hipSuccess;
+  hipLaunchKernelGGL(momentum_kernel<TA>, dim3(static_cast<unsigned>(chunks)), dim3(kThreads), 0, stream,
+                     reinterpret_cast<const Item*>(base + l.part[way].at_items), n, st, reinterpret_cast<double*>(base + l.part[way].at_partial));
   return hipGetLastError();
 }
 
@@ -377,9 +389,7 @@ sc_status ou_step(const ou_config* cfg, int64_t n_tensors, const ou_tensor* tens
   if (st != SC_OK) return st;
   try {
     const Layout l = layout_of(n_tensors, tensors, cfg->steps);
-    bool any = false;
-    for (const Part& p : l.part) any = any || !p.items.empty();
-    if (!any) return SC_OK;
+    if (l.items.empty()) return SC_OK;
     if (!workspace || workspace_bytes < l.bytes)
       return set_error(SC_ERR_WORKSPACE, "ou_step: workspace missing or smaller than ou_workspace_bytes()");
     if (misaligned(workspace, 256)) return set_error(SC_ERR_WORKSPACE, "ou_step: workspace not 256-byte aligned");
@@ -388,16 +398,14 @@ sc_status ou_step(const ou_config* cfg, int64_t n_tensors, const ou_tensor* tens
     const Step step{cfg->a, cfg->b, cfg->c, cfg->momentum, cfg->rate, 1 - cfg->rate * cfg->decay, cfg->eps, (cfg->flags & OU_NESTEROV) != 0};
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     char* const base = static_cast<char*>(workspace);
-    hipError_t e = hipSuccess;
-    for (int way = 0; way < kWays && e == hipSuccess; ++way) {
+    hipError_t e = send(l.items, base, stream);
+    if (e == hipSuccess) e = first_pass<double>(l, kDouble, kDouble, step, base, stream);
+    if (e == hipSuccess) e = first_pass<float>(l, kParts, kSlices128, step, base, stream);
+    if (e == hipSuccess) e = whole_run(l.part[kWhole64], l.part[kWhole128], cfg, step, base, stream);
+    for (int way = kDouble; way <= kSlices128 && e == hipSuccess; ++way) {
       const Part& p = l.part[way];
       if (p.items.empty()) continue;
-      e = way == kDouble ? begin<double>(p, step, base, stream) : whole(way) ? send(p, base, stream) : begin<float>(p, step, base, stream);
-      if (e != hipSuccess) break;
-      e = way == kDouble  ? double_run(p, cfg, step, base, stream)
-          : way == kParts ? parts_run(p, cfg, step, base, stream)
-          : whole(way)    ? whole_run(p, cfg, step, large(way), base, stream)
-                          : slice_run(p, cfg, step, large(way), base, stream);
+      e = way == kDouble ? double_run(p, cfg, step, base, stream) : way == kParts ? parts_run(p, cfg, step, base, stream) : slice_run(p, cfg, step, large(way), base, stream);
     }
     if (e != hipSuccess) return set_error(SC_ERR_HIP, std::string("ou_step: kernel launch: ") + hipGetErrorString(e));
   } catch (const std::bad_alloc&) {
