@@ -4,7 +4,8 @@
 // matrix (X, S or P) in one half of its LDS and those of X transposed in the other; X and S in fp32 stay in registers, where the matrix instruction leaves its
 // results: four waves, each with every second 32 x 32 block of every second row of blocks, so that a matrix of half the size keeps all of them busy.
 //
-// Up to 64 or 128 columns (whole_kernel) everything from the gradient to the weight is one launch.  Wider matrices are cut along their columns into at most
+// Up to 64 or 128 columns (whole_kernel) everything from the gradient to the weight is one launch: 89 x 64 x 64 with five steps take 20 us, 89 x 128 x 128 64 (47 and 134
+// in slices, 95 and 146 in tiles); 19 of the 64 are matrix instructions, the rest is splitting into parts, LDS and memory.  Wider matrices are cut along their columns into at most
 // kSlices slices (slice_kernel): a launch a step, in which each workgroup adds up the slices' S in order, makes P for itself, its slice of the
 // next X, and that slice's share of the next S.
 #include <algorithm>
@@ -20,7 +21,7 @@ typedef _Float16 H4 __attribute__((ext_vector_type(4)));
 typedef float F16 __attribute__((ext_vector_type(16)));
 typedef float F4 __attribute__((ext_vector_type(4)));
 
-constexpr int kSlices = 32;
+constexpr int kSlices = 64;
 constexpr int kUnits = 256;   // compute units
 
 // Powers of two: values to parts, and sums of parts to values.  The same for all steps (what a step could gain by its own is the growth of the bound over the
@@ -466,9 +467,14 @@ hipError_t slices(const Part& p, const ou_config* cfg, const Step& st, char* bas
 
 }  // namespace
 
+// Every slice adds up the shares of all and makes P again, so a tensor of many matrices has fewer of them: as many as fill the chip, two workgroups of the smaller size a
+// compute unit (89 x 64 x 512, five steps: 106 us with five slices, 137 with eight, 116 with two; one 64 x 8192: 127 with 64, 178 with 16, one 128 x 32768: 544 and 738 with
+// 32).  With the tiles of ou_parts.hip those two take 193 and 444 us; 89 x 128 x 512 takes 239 here and 251 there, 500 x 64 x 1024 529 and 1318, one 128 x 4096 235 and 288,
+// and only a few matrices of 128 x 256 to 128 x 1024 are faster there (one 128 x 512: 135 here, 121 there).
 void slice_place(Part& p, Item& it, int64_t count, bool large) {
   const int64_t n = large ? 128 : 64, l = std::max(it.rows, it.cols);
-  it.width = static_cast<int32_t>(n * ceil_div(l, n * kSlices));
+  const int64_t slices = std::clamp<int64_t>((large ? kUnits : 2 * kUnits) / std::max<int64_t>(count, 1), 1, kSlices);
+  it.width = static_cast<int32_t>(n * ceil_div(l, n * slices));
   it.x = p.x;
   p.units[kBlocks] += count * ceil_div(l, it.width);
   p.x += count * it.rows * it.cols;
