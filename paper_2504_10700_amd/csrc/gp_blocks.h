@@ -133,7 +133,7 @@ __device__ __forceinline__ bool chunk_of(const Outer& a, int64_t block, int each
   c->last = min(p.atoms * a.components, c->first + a.per);
   c->partial = p.units > 1;
   c->matrix = c->partial ? p.slots + p.local : p.bucket;
-  return true;
+  return !c->partial || c->matrix < a.slots;   // (with a grouping of something else there can be more: they stay out of memory)
 }
 
 }  // namespace gp

@@ -21,6 +21,7 @@ constexpr int kSortThreads = 1024;
 constexpr int kSortWaves = kSortThreads / kLanes;
 constexpr int kSortGroups = 128;   // workgroups of the sort of a large batch
 constexpr int kSortAtoms = 2048;   // atoms that one workgroup sorts alone
+constexpr int64_t kMaxGrid = int64_t(1) << 23;   // workgroups of a launch; they go on to the units beyond
 
 struct Grouping {
   const int32_t* offsets;
@@ -129,6 +130,7 @@ struct Outer {
   int elements, components;
   int k_in, k_out;
   int per;              // rows of a chunk
+  int slots;            // partial matrices that the workspace holds
   const void* X;
   const void* dY;
   void* dW;

@@ -28,7 +28,6 @@ typedef unsigned ULoose __attribute__((aligned(2)));
 
 constexpr int kTile = 128, kStage = 32;
 constexpr int kPlane = kTile * kStage;   // elements of one part of one operand: rows of 64 bytes
-constexpr int64_t kMaxGrid = int64_t(1) << 23;
 
 template <typename T>
 constexpr int parts() { return sizeof(T) == 2 ? 1 : 3; }
@@ -526,7 +525,8 @@ hipError_t launch_rows_of(const gp_config* c, const Rows& a, bool back, hipStrea
 }  // namespace
 
 hipError_t launch_rows_parts(const gp_config* c, const Rows& a, bool back, hipStream_t stream) {
-  // Tiles of half the height where the others would not fill the compute units.
+  // Tiles of half the height where the others would not fill the compute units (10 000 rows, 128 x 128: 11 us instead of 14, 1000 rows, 512 x 512: 26 instead of 36;
+  // 30 000 rows, 128 x 128: 23 instead of 20).
   const int64_t tiles = (ceil_div(a.n * c->components, 128) + std::min<int64_t>(c->num_elements + 1, a.n)) * ceil_div(a.columns, kTile);
   const bool half = tiles <= 256;
   if (c->dtype == SC_F32) return half ? launch_rows_of<float, 1>(c, a, back, stream) : launch_rows_of<float, 2>(c, a, back, stream);

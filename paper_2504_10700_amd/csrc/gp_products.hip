@@ -21,11 +21,12 @@ template <typename T, typename TA, bool kBack>
 __global__ __launch_bounds__(kThreads) void rows_kernel(const Rows a) {
   __shared__ BlockSpace<TA> space;
   const int columns = (a.columns + kBlock - 1) / kBlock;
-  int which;
-  const Place p = place_of(a.group.offsets, a.elements + 1, a.n, blockIdx.x, columns, [&](int atoms) { return (atoms * a.components + kBlock - 1) / kBlock; },
-                           &which);
-  if (p.bucket < 0) return;
-  rows_block<T, TA, kBack>(a, p.bucket, p.begin, p.atoms * a.components, p.local * kBlock, which * kBlock, space);
+  for (int64_t block = blockIdx.x;; block += gridDim.x) {
+    int which;
+    const Place p = place_of(a.group.offsets, a.elements + 1, a.n, block, columns, [&](int atoms) { return (atoms * a.components + kBlock - 1) / kBlock; }, &which);
+    if (p.bucket < 0) return;
+    rows_block<T, TA, kBack>(a, p.bucket, p.begin, p.atoms * a.components, p.local * kBlock, which * kBlock, space);
+  }
 }
 
 template <typename T, typename TA>
@@ -54,12 +55,16 @@ __global__ __launch_bounds__(kThreads) void outer_kernel(const Outer a) {
     outer_block<T, TA>(a, order, c.begin, c.first, c.last, tile / col_tiles * kBlock, tile % col_tiles * kBlock, out, space);
 }
 
+__device__ __forceinline__ int atoms_of(const Outer& a, int element) {
+  auto at = [&](int e) { return min(max(a.group.offsets[e], 0), static_cast<int>(a.n)); };
+  return max(at(element + 1) - at(element), 0);
+}
+
 // Slots of the elements before this one: the lanes of a wave add up theirs.
 __device__ __forceinline__ int slots_before(const Outer& a, int element) {
-  const int most = static_cast<int>(a.n);
   int sum = 0;
   for (int e = threadIdx.x & (kLanes - 1); e < element; e += kLanes) {
-    const int atoms = max(min(a.group.offsets[e + 1], most) - min(a.group.offsets[e], most), 0);
+    const int atoms = atoms_of(a, e);
     const int k = chunks_of(atoms * a.components, a.per);
     sum += k > 1 ? k : 0;
   }
@@ -74,9 +79,8 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const Outer a) {
   const int64_t size = static_cast<int64_t>(a.k_in) * a.k_out;
   const int element = blockIdx.x;
   const int n_slots = slots_before(a, element);
-  const int atoms = max(min(a.group.offsets[element + 1], static_cast<int>(a.n)) - min(a.group.offsets[element], static_cast<int>(a.n)), 0);
-  const int n = chunks_of(atoms * a.components, a.per);
-  if (n < 2) return;
+  const int n = chunks_of(atoms_of(a, element) * a.components, a.per);
+  if (n < 2 || n_slots > a.slots - n) return;
   const TA* const from = static_cast<const TA*>(a.partial) + n_slots * size;
   TA* const to = static_cast<TA*>(a.dW) + element * size;
   for (int64_t i = static_cast<int64_t>(blockIdx.y) * kThreads + threadIdx.x; i < size; i += static_cast<int64_t>(gridDim.y) * kThreads) {
@@ -94,7 +98,8 @@ __global__ __launch_bounds__(kThreads) void zero_kernel(TA* p, int64_t n) {
 
 // ---- host side
 
-// Rows of a chunk of dW: enough chunks for the chip where the matrices alone do not fill it.
+// Rows of a chunk of dW: enough chunks for the chip where the matrices alone do not fill it (200 000 rows, 128 x 128: 79 us, with two thirds of the chunks 100, with
+// twice as many 91), none so short that adding them up costs more (6000 rows, 256 x 256: 26 us, with 256 rows at least 33; 10 000 rows, 128 x 128: 23, with 64 30).
 int chunk_rows(const gp_config* c, int64_t n) {
   const int64_t rows = n * c->components, side = parts_serve(c) ? 128 : kBlock, tiles = ceil_div(c->k_in, side) * ceil_div(c->k_out, side);
   const int64_t wanted = std::max<int64_t>(1, 384 / tiles);
@@ -170,7 +175,7 @@ hipError_t launch_rows(const gp_config* c, const Rows& a, hipStream_t stream) {
   if (!a.group.offsets) return launch_rows_few(c, a, kBack, stream);
   if (parts_serve(c)) return launch_rows_parts(c, a, kBack, stream);
   const int64_t tiles = ceil_div(a.n * c->components, kBlock) + std::min<int64_t>(c->num_elements + 1, a.n);
-  const dim3 grid(static_cast<unsigned>(ceil_div(tiles * ceil_div(a.columns, kBlock), kXcds) * kXcds));
+  const dim3 grid(static_cast<unsigned>(std::min(kMaxGrid, ceil_div(tiles * ceil_div(a.columns, kBlock), kXcds) * kXcds)));
   if (c->dtype == SC_F64) hipLaunchKernelGGL((rows_kernel<double, double, kBack>), grid, dim3(kThreads), 0, stream, a);
   else if (c->dtype == SC_F32) hipLaunchKernelGGL((rows_kernel<float, float, kBack>), grid, dim3(kThreads), 0, stream, a);
   else hipLaunchKernelGGL((rows_kernel<__bf16, float, kBack>), grid, dim3(kThreads), 0, stream, a);
@@ -290,7 +295,7 @@ sc_status gp_backward(const gp_config* cfg, int64_t n_nodes, const int32_t* z, c
   }
   if (!dW) return SC_OK;
   const Outer a{n_nodes, ld_in_of(cfg), ld_out_of(cfg), z, group, cfg->num_elements, cfg->components, cfg->k_in, cfg->k_out,
-                chunk_rows(cfg, n_nodes), X, dY, dW, workspace};
+                chunk_rows(cfg, n_nodes), static_cast<int>(slots_of(cfg, n_nodes)), X, dY, dW, workspace};
   return launched("gp_backward", launch_outer(cfg, a, stream));
 }
 
