@@ -107,17 +107,30 @@ __global__ __launch_bounds__(kThreads) void normalise_kernel(const Item* __restr
   const int b = static_cast<int>(unit % blocks), r0 = b / col_blocks * 64, c0 = b % col_blocks * 64;
   const double down = down_of(partial + it.unit[kChunks] + matrix * per, per, st.eps, slots);
   const float mu = static_cast<float>(st.mu);
-  for (int i = threadIdx.x; i < 64 * 64; i += kThreads) {
-    const int r = i / 64, c = i % 64;
-    float x = 0;
-    if (r0 + r < it.rows && c0 + c < it.cols) {
-      const int64_t at = matrix * size + static_cast<int64_t>(r0 + r) * it.cols + c0 + c;
-      float u = gradient<float>(it, at);
-      if (it.momentum) u = direction(u, static_cast<const float*>(it.momentum)[at], mu, st.nesterov);
-      x = static_cast<float>(static_cast<double>(u) * down);
-      if (last) finish(it, st, at, x);
+  // (a quarter of the block's rows after the other, each read whole before the next is asked for)
+  const int c = threadIdx.x % 64;
+  for (int r = threadIdx.x / 64; r < 64; r += 16) {
+    float u[4], v[4];
+    bool inside[4];
+    int64_t at[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      inside[k] = r0 + r + 4 * k < it.rows && c0 + c < it.cols;
+      at[k] = matrix * size + static_cast<int64_t>(r0 + r + 4 * k) * it.cols + c0 + c;
+      u[k] = inside[k] ? gradient<float>(it, at[k]) : 0.f;
     }
-    if (turned) block[c][r] = x; else block[r][c] = x;
+    if (it.momentum) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] = inside[k] ? static_cast<const float*>(it.momentum)[at[k]] : 0.f;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) u[k] = direction(u[k], v[k], mu, st.nesterov);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float x = static_cast<float>(static_cast<double>(u[k]) * down);
+      if (last && inside[k]) finish(it, st, at[k], x);
+      if (turned) block[c][r + 4 * k] = x; else block[r + 4 * k][c] = x;
+    }
   }
   if (last) return;
   __syncthreads();

@@ -24,7 +24,19 @@ __global__ __launch_bounds__(kLanes) void send_kernel(const Sent sent, Item* __r
   if (i < sent.count) items[sent.first + i] = sent.item[i];
 }
 
-// Momentum of a chunk of elements, and the sum of their U's squares.  A matrix's sum is that of its chunks.
+// Momentum of a chunk of elements, and the sum of their U's squares.  A matrix's sum is that of its chunks.  (A few elements of a thread are requested together: a store
+// between two loads would make the second wait.)
+constexpr int kAtOnce = 8;
+template <typename TA>
+__device__ __forceinline__ void gradients(const Item& it, int64_t at, int i0, int count, TA (&u)[kAtOnce]) {
+  auto read = [&](auto* g) {
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) u[k] = i0 + k * kThreads < count ? static_cast<TA>(g[at + i0 + k * kThreads]) : TA(0);
+  };
+  if constexpr (sizeof(TA) == 8) read(static_cast<const double*>(it.grad));
+  else if (it.dtype == SC_BF16) read(static_cast<const __bf16*>(it.grad));
+  else read(static_cast<const float*>(it.grad));
+}
 template <typename TA>
 __global__ __launch_bounds__(kThreads) void momentum_kernel(const Item* __restrict__ items, int n, const Step st, double* __restrict__ partial) {
   __shared__ double slots[kWaves];
@@ -33,16 +45,23 @@ __global__ __launch_bounds__(kThreads) void momentum_kernel(const Item* __restri
   const int64_t matrix = unit / per, first = unit % per * kChunk, at = matrix * size + first;
   const int count = static_cast<int>(min(size - first, static_cast<int64_t>(kChunk)));
   const TA mu = static_cast<TA>(st.mu);
+  TA* const momentum = it.momentum ? static_cast<TA*>(it.momentum) + at : nullptr;
   double sum = 0;
-  for (int i = threadIdx.x; i < count; i += kThreads) {
-    TA u = gradient<TA>(it, at + i);
-    if (it.momentum) {
-      TA* const m = static_cast<TA*>(it.momentum) + at + i;
-      const TA v = mu * *m + u;
-      *m = v;
-      u = direction(u, v, mu, st.nesterov);
+  for (int i0 = threadIdx.x; i0 < count; i0 += kAtOnce * kThreads) {
+    TA u[kAtOnce], v[kAtOnce];
+    gradients(it, at, i0, count, u);
+    if (momentum) {
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) v[k] = i0 + k * kThreads < count ? momentum[i0 + k * kThreads] : TA(0);
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) {
+        v[k] = mu * v[k] + u[k];
+        if (i0 + k * kThreads < count) momentum[i0 + k * kThreads] = v[k];
+        u[k] = direction(u[k], v[k], mu, st.nesterov);
+      }
     }
-    sum = fma(static_cast<double>(u), static_cast<double>(u), sum);
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) sum = fma(static_cast<double>(u[k]), static_cast<double>(u[k]), sum);
   }
   sum = workgroup_sum(sum, slots);
   if (threadIdx.x == 0) partial[blockIdx.x] = sum;
