@@ -145,7 +145,7 @@ hipError_t parts_run(const Part& p, const ou_config* cfg, const Step& st, char* 
 // fp32 matrices whose shorter side is at most 64 (large: 128): those whose longer side is too, from the gradient to the weight; and wider ones, from the sums of squares
 // on (ou_small.hip).
 hipError_t whole_run(const Part& p64, const Part& p128, const ou_config* cfg, const Step& st, char* base, hipStream_t stream);
-void slice_place(Part& p, Item& it, int64_t count, bool large);
+void slice_place(Part& p, Item& it, int64_t count, int64_t matrices, bool large);   // (matrices: of this way in the list)
 void slice_layout(Part& p, Room& room, int steps, bool large);
 hipError_t slice_run(const Part& p, const ou_config* cfg, const Step& st, bool large, char* base, hipStream_t stream);
 

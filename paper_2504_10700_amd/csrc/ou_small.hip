@@ -394,7 +394,7 @@ __global__ __launch_bounds__(kThreads) void slice_kernel(const Item* __restrict_
   for (int j0 = own * width; j0 < end; j0 += N) {
     const int columns = min(l - j0, N);
     Places<N> places, in_x;   // in the tensor; in X, which is kept as m x l
-    places_of<N>(mat, mat.turned, j0, places);
+    if (step == 0 || last) places_of<N>(mat, mat.turned, j0, places);
     places_of<N>(mat, false, j0, in_x);
     if (step == 0) {
       load_direction<N, false>(it, st, mat, places, x);
@@ -467,13 +467,13 @@ hipError_t slices(const Part& p, const ou_config* cfg, const Step& st, char* bas
 
 }  // namespace
 
-// Every slice adds up the shares of all and makes P again, so a tensor of many matrices has fewer of them: as many as fill the chip, two workgroups of the smaller size a
+// Every slice adds up the shares of all and makes P again, so there are fewer where a list has many matrices: as many as fill the chip, two workgroups of the smaller size a
 // compute unit (89 x 64 x 512, five steps: 106 us with five slices, 137 with eight, 116 with two; one 64 x 8192: 127 with 64, 178 with 16, one 128 x 32768: 544 and 738 with
 // 32).  With the tiles of ou_parts.hip those two take 193 and 444 us; 89 x 128 x 512 takes 239 here and 251 there, 500 x 64 x 1024 529 and 1318, one 128 x 4096 235 and 288,
 // and only a few matrices of 128 x 256 to 128 x 1024 are faster there (one 128 x 512: 135 here, 121 there).
-void slice_place(Part& p, Item& it, int64_t count, bool large) {
+void slice_place(Part& p, Item& it, int64_t count, int64_t matrices, bool large) {
   const int64_t n = large ? 128 : 64, l = std::max(it.rows, it.cols);
-  const int64_t slices = std::clamp<int64_t>((large ? kUnits : 2 * kUnits) / std::max<int64_t>(count, 1), 1, kSlices);
+  const int64_t slices = std::clamp<int64_t>((large ? kUnits : 2 * kUnits) / matrices, 1, kSlices);
   it.width = static_cast<int32_t>(n * ceil_div(l, n * slices));
   it.x = p.x;
   p.units[kBlocks] += count * ceil_div(l, it.width);

@@ -224,6 +224,8 @@ void double_layout(Part& p, Room& room, int steps) {
 
 Layout layout_of(int64_t n, const ou_tensor* tensors, int steps) {
   Layout l;
+  int64_t matrices[kWays] = {};
+  for (int64_t i = 0; i < n; ++i) matrices[way_of(tensors[i])] += tensors[i].count;
   for (int64_t i = 0; i < n; ++i) {
     const ou_tensor& t = tensors[i];
     if (t.count == 0) continue;
@@ -242,7 +244,7 @@ Layout layout_of(int64_t n, const ou_tensor* tensors, int steps) {
     if (!whole(way)) p.units[kChunks] += t.count * ceil_div(static_cast<int64_t>(t.rows) * t.cols, kChunk);
     if (way == kDouble) double_place(p, it, t.count);
     else if (way == kParts) parts_place(p, it, t.count);
-    else if (sliced(way)) slice_place(p, it, t.count, large(way));
+    else if (sliced(way)) slice_place(p, it, t.count, matrices[way], large(way));
     else p.units[kBlocks] += t.count;
     p.items.push_back(it);
   }

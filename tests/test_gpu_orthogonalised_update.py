@@ -225,7 +225,7 @@ def test_results_repeat(ou):
     b.step()
     for x, y in zip(a.momentum + a.weight + a.update, b.momentum + b.weight + b.update):
         assert torch.equal(x, y)
-    # a matrix's result does not depend on its neighbours in the list
+    # alone these sizes take the same kernels as in this list
     for i, s in enumerate(shapes):
         c = List(ou, shapes, "float32")
         c.shapes, c.scale = [s], [c.scale[i]]
