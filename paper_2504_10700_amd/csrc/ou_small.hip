@@ -5,7 +5,7 @@
 // results: four waves, each with every second 32 x 32 block of every second row of blocks, so that a matrix of half the size keeps all of them busy.
 //
 // Up to 64 or 128 columns (whole_kernel) everything from the gradient to the weight is one launch: 89 x 64 x 64 with five steps take 20 us, 89 x 128 x 128 64 (47 and 134
-// in slices, 95 and 146 in tiles); 19 of the 64 are matrix instructions, the rest is splitting into parts, LDS and memory.  Wider matrices are cut along their columns into at most
+// in slices, 91 and 140 in tiles); 19 of the 64 are matrix instructions, the rest is splitting into parts, LDS and memory.  Wider matrices are cut along their columns into at most
 // kSlices slices (slice_kernel): a launch a step, in which each workgroup adds up the slices' S in order, makes P for itself, its slice of the
 // next X, and that slice's share of the next S.
 #include <algorithm>
@@ -214,6 +214,34 @@ __device__ __forceinline__ void store_f32(float* p, const Matrix& mat, const Pla
   });
 }
 
+// A square of values in the workspace stands in the order of the registers: four values of a lane in a row.
+template <int N, typename F>
+__device__ __forceinline__ void load_square(const float* p, F&& put) {
+  constexpr int kSide = Shape<N>::kSide;
+  const F4* const from = reinterpret_cast<const F4*>(p) + threadIdx.x;
+#pragma unroll
+  for (int e = 0; e < kSide; ++e)
+#pragma unroll
+    for (int f = 0; f < kSide; ++f)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const F4 v = from[((e * kSide + f) * 4 + q) * kThreads];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) put(e, f, 4 * q + i, static_cast<float>(v[i]));
+      }
+}
+template <int N>
+__device__ __forceinline__ void store_square(float* p, const typename Shape<N>::Blocks& v) {
+  constexpr int kSide = Shape<N>::kSide;
+  F4* const to = reinterpret_cast<F4*>(p) + threadIdx.x;
+#pragma unroll
+  for (int e = 0; e < kSide; ++e)
+#pragma unroll
+    for (int f = 0; f < kSide; ++f)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) to[((e * kSide + f) * 4 + q) * kThreads] = F4{v[e][f][4 * q], v[e][f][4 * q + 1], v[e][f][4 * q + 2], v[e][f][4 * q + 3]};
+}
+
 // U of the lane's elements, zero outside.  kMomentum: the momentum takes its step too.
 template <int N, bool kMomentum>
 __device__ __forceinline__ void load_direction(const Item& it, const Step& st, const Matrix& mat, const Places<N>& places, typename Shape<N>::Blocks& u) {
@@ -340,7 +368,7 @@ __global__ __launch_bounds__(kThreads) void both_kernel(const Item* __restrict__
 }
 
 // Slices of `width` columns (a multiple of N) of a matrix of m <= N.  step 0: X from the gradient; then the step before `step` of the iteration; the last one leaves the
-// results.  partial: the slices' shares of S, in the order of the registers.
+// results.  X and the slices' shares of S (partial) are kept in the order of the registers.
 template <int N>
 __global__ __launch_bounds__(kThreads) void slice_kernel(const Item* __restrict__ items, int n, const Step st, int step, bool last, const Scales sc,
                                                          const double* __restrict__ squares, float* __restrict__ X, const float* __restrict__ partial,
@@ -356,7 +384,7 @@ __global__ __launch_bounds__(kThreads) void slice_kernel(const Item* __restrict_
   const int own = static_cast<int>(unit % slices);
   const Matrix mat = matrix_of(it, index);
   const int m = mat.m, l = mat.l, deep_m = (m + 31) / 32 * 32, end = min(l, (own + 1) * width);
-  float* const x_of = X + it.x + mat.first;
+  float* const x_of = X + it.x + index * ((l + N - 1) / N) * S::kResults;   // squares of N columns
   typename S::Blocks x, s, r;
   double down = 0;
 #pragma unroll
@@ -369,20 +397,9 @@ __global__ __launch_bounds__(kThreads) void slice_kernel(const Item* __restrict_
     const int64_t per = chunks_of(static_cast<int64_t>(m) * l);
     down = down_of(squares + it.unit[kChunks] + index * per, per, st.eps, reinterpret_cast<double*>(lds));
   } else {
-    const F4* from = reinterpret_cast<const F4*>(partial + (blockIdx.x - own) * static_cast<int64_t>(S::kResults)) + threadIdx.x;
+    const float* from = partial + (blockIdx.x - own) * static_cast<int64_t>(S::kResults);
 #pragma unroll 4 / kSide
-    for (int k = 0; k < slices; ++k, from += S::kResults / 4) {
-#pragma unroll
-      for (int e = 0; e < kSide; ++e)
-#pragma unroll
-        for (int f = 0; f < kSide; ++f)
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const F4 v = from[((e * kSide + f) * 4 + q) * kThreads];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) s[e][f][4 * q + i] += v[i];
-          }
-    }
+    for (int k = 0; k < slices; ++k, from += S::kResults) load_square<N>(from, [&](int e, int f, int q, float v) { s[e][f][q] += v; });
     make_p<N>(st, sc, m, deep_m, square, s);
 #pragma unroll
     for (int e = 0; e < kSide; ++e)
@@ -393,14 +410,14 @@ __global__ __launch_bounds__(kThreads) void slice_kernel(const Item* __restrict_
   }
   for (int j0 = own * width; j0 < end; j0 += N) {
     const int columns = min(l - j0, N);
-    Places<N> places, in_x;   // in the tensor; in X, which is kept as m x l
+    float* const x_here = x_of + static_cast<int64_t>(j0 / N) * S::kResults;
+    Places<N> places;
     if (step == 0 || last) places_of<N>(mat, mat.turned, j0, places);
-    places_of<N>(mat, false, j0, in_x);
     if (step == 0) {
       load_direction<N, false>(it, st, mat, places, x);
       each_result<N>([&](int e, int f, int q, int, int) { x[e][f][q] = static_cast<float>(static_cast<double>(x[e][f][q]) * down); });
     } else {
-      load_f32<N>(x_of, mat, in_x, x);
+      load_square<N>(x_here, [&](int e, int f, int q, float v) { x[e][f][q] = v; });
       put<N, true, false>(x, sc.x_up, m, columns, slice, nullptr);
       __syncthreads();
       multiply<N>(square, slice, m, columns, deep_m, r);
@@ -411,7 +428,7 @@ __global__ __launch_bounds__(kThreads) void slice_kernel(const Item* __restrict_
       store_results<N>(it, st, mat, places, x);
       continue;
     }
-    store_f32<N>(x_of, mat, in_x, x);
+    store_square<N>(x_here, x);   // (zeros up to the next multiples of 32, beyond whatever the products were)
     // (the columns up to the next multiple of 32 are read too: they hold zeros, made of the parts' zeros)
     put<N, false, true>(x, sc.x_up, m, columns, nullptr, slice);
     __syncthreads();
@@ -423,13 +440,7 @@ __global__ __launch_bounds__(kThreads) void slice_kernel(const Item* __restrict_
     __syncthreads();
   }
   if (last) return;
-  F4* const to = reinterpret_cast<F4*>(next_partial + blockIdx.x * static_cast<int64_t>(S::kResults)) + threadIdx.x;
-#pragma unroll
-  for (int e = 0; e < kSide; ++e)
-#pragma unroll
-    for (int f = 0; f < kSide; ++f)
-#pragma unroll
-      for (int q = 0; q < 4; ++q) to[((e * kSide + f) * 4 + q) * kThreads] = F4{s[e][f][4 * q], s[e][f][4 * q + 1], s[e][f][4 * q + 2], s[e][f][4 * q + 3]};
+  store_square<N>(next_partial + blockIdx.x * static_cast<int64_t>(S::kResults), s);
 }
 
 template <typename Kernel, typename... Args>
@@ -468,16 +479,15 @@ hipError_t slices(const Part& p, const ou_config* cfg, const Step& st, char* bas
 }  // namespace
 
 // Every slice adds up the shares of all and makes P again, so there are fewer where a list has many matrices: as many as fill the chip, two workgroups of the smaller size a
-// compute unit (89 x 64 x 512, five steps: 106 us with five slices, 137 with eight, 116 with two; one 64 x 8192: 127 with 64, 178 with 16, one 128 x 32768: 544 and 738 with
-// 32).  With the tiles of ou_parts.hip those two take 193 and 444 us; 89 x 128 x 512 takes 239 here and 251 there, 500 x 64 x 1024 529 and 1318, one 128 x 4096 235 and 288,
-// and only a few matrices of 128 x 256 to 128 x 1024 are faster there (one 128 x 512: 135 here, 121 there).
+// compute unit.  Five steps of 89 x 64 x 1024: 138 us with five slices, 159 with eleven, 164 with two; of 89 x 128 x 512: 192 with two, 271 with four; of one 64 x 8192: 117
+// with 64, 147 with 16.  In the tiles of ou_parts.hip those take 274, 247 and 437, one 128 x 512 116 (here 102), 500 x 64 x 256 385 (here 136).
 void slice_place(Part& p, Item& it, int64_t count, int64_t matrices, bool large) {
   const int64_t n = large ? 128 : 64, l = std::max(it.rows, it.cols);
   const int64_t slices = std::clamp<int64_t>((large ? kUnits : 2 * kUnits) / matrices, 1, kSlices);
   it.width = static_cast<int32_t>(n * ceil_div(l, n * slices));
   it.x = p.x;
   p.units[kBlocks] += count * ceil_div(l, it.width);
-  p.x += count * it.rows * it.cols;
+  p.x += count * ceil_div(l, n) * n * n;
 }
 
 void slice_layout(Part& p, Room& room, int steps, bool large) {
