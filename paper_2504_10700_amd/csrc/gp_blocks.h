@@ -16,6 +16,8 @@ struct BlockSpace {
   TA a[kDepth][kPitch], b[kDepth][kPitch];
 };
 
+__device__ __forceinline__ void barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }   // (requests to memory stay under way)
+
 // Rows `first` on of a bucket, columns c0 on, of Y or (kBack: W is read transposed) dX.
 template <typename T, typename TA, bool kBack>
 __device__ __forceinline__ void rows_block(const Rows& a, int bucket, int begin, int rows, int first, int c0, BlockSpace<TA>& space) {
@@ -28,8 +30,8 @@ __device__ __forceinline__ void rows_block(const Rows& a, int bucket, int begin,
     const TA* const W = static_cast<const TA*>(a.W) + static_cast<int64_t>(bucket) * a.reduced * a.columns;
     const int xr = threadIdx.x / 4, xk = threadIdx.x % 4 * 4;   // 64 rows x 4 pieces of 4
     const T* const x = row_at(static_cast<const T*>(a.src), a.group.order, a.n, begin, min(first + xr, rows - 1), a.components, a.ld_src, a.reduced);
-    for (int k = 0; k < a.reduced; k += kDepth) {
-      TA xv[4], wv[4];
+    TA xv[4], wv[4];   // 16 reduced indices, requested while the 16 before are multiplied
+    auto request = [&](int k) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) xv[i] = k + xk + i < a.reduced ? static_cast<TA>(x[k + xk + i]) : TA(0);
       if constexpr (kBack) {   // W [column][reduced]
@@ -41,7 +43,10 @@ __device__ __forceinline__ void rows_block(const Rows& a, int bucket, int begin,
 #pragma unroll
         for (int i = 0; i < 4; ++i) wv[i] = r < a.reduced && c + i < a.columns ? W[static_cast<int64_t>(r) * a.columns + c + i] : TA(0);
       }
-      __syncthreads();
+    };
+    request(0);
+    for (int k = 0; k < a.reduced; k += kDepth) {
+      barrier();
 #pragma unroll
       for (int i = 0; i < 4; ++i) space.a[xk + i][xr] = xv[i];
       if constexpr (kBack) {
@@ -51,7 +56,8 @@ __device__ __forceinline__ void rows_block(const Rows& a, int bucket, int begin,
 #pragma unroll
         for (int i = 0; i < 4; ++i) space.b[threadIdx.x / 16][threadIdx.x % 16 * 4 + i] = wv[i];
       }
-      __syncthreads();
+      if (k + kDepth < a.reduced) request(k + kDepth);
+      barrier();
 #pragma unroll
       for (int s = 0; s < kDepth / 4; ++s) {
         const TA xo = space.a[4 * s + lane / 16][16 * wave + (lane & 15)];
@@ -83,24 +89,28 @@ __device__ __forceinline__ void outer_block(const Outer& a, const int32_t* order
 #pragma unroll
   for (int t = 0; t < 4; ++t) acc[t] = Acc{0, 0, 0, 0};
   const int lr = threadIdx.x / 16, lc = threadIdx.x % 16 * 4;
-  for (int r = first; r < last; r += kDepth) {
+  TA xv[4], gv[4];   // 16 rows, requested while the 16 before are multiplied
+  auto request = [&](int r) {
     const int row = min(r + lr, last - 1);
     const bool inside = r + lr < last;
     const T* const x = row_at(static_cast<const T*>(a.X), order, a.n, begin, row, a.components, a.ld_in, a.k_in);
     const T* const g = row_at(static_cast<const T*>(a.dY), order, a.n, begin, row, a.components, a.ld_out, a.k_out);
-    TA xv[4], gv[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       xv[i] = inside && k0 + lc + i < a.k_in ? static_cast<TA>(x[k0 + lc + i]) : TA(0);
       gv[i] = inside && c0 + lc + i < a.k_out ? static_cast<TA>(g[c0 + lc + i]) : TA(0);
     }
-    __syncthreads();
+  };
+  if (first < last) request(first);
+  for (int r = first; r < last; r += kDepth) {
+    barrier();
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       space.a[lr][lc + i] = xv[i];
       space.b[lr][lc + i] = gv[i];
     }
-    __syncthreads();
+    if (r + kDepth < last) request(r + kDepth);
+    barrier();
 #pragma unroll
     for (int s = 0; s < kDepth / 4; ++s) {
       const TA xo = space.a[4 * s + lane / 16][16 * wave + (lane & 15)];

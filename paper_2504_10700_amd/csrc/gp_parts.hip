@@ -35,8 +35,6 @@ constexpr int parts() { return sizeof(T) == 2 ? 1 : 3; }
 // Rows 0..7, and the even and the odd ones of 16, have their four pieces at different places.
 __device__ __forceinline__ int swizzle(int row) { return ((row >> 1) & 3) ^ ((row >> 3) & 1); }
 
-__device__ __forceinline__ void barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }   // (requests to memory stay under way)
-
 // Eight reduced indices of one row of an operand: raw elements (request_some: the first n, zeros behind them), and as its parts in LDS.
 template <typename T>
 struct Eight;

@@ -17,7 +17,6 @@ using sc::DeviceGuard;
 using sc::misaligned;
 using sc::set_error;
 
-constexpr int kTile = 64, kDepth = 16, kPitch = kTile + 4;
 
 __global__ __launch_bounds__(kLanes) void send_kernel(const Sent sent, Item* __restrict__ items) {
   const int i = threadIdx.x;
@@ -85,6 +84,8 @@ __global__ __launch_bounds__(kThreads) void normalise_kernel(const Item* __restr
   }
 }
 
+__device__ __forceinline__ void barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }   // (requests to memory stay under way)
+
 // Element (i, k) of a matrix at p[i * ld + k * step].
 template <typename TA>
 struct View {
@@ -93,42 +94,60 @@ struct View {
   int rows, depth;
 };
 
-// acc[t] of wave's 16 rows and 64 columns: sum over k of P(i, k) Q(j, k).
-template <typename TA>
-__device__ __forceinline__ void product(const View<TA>& p, const View<TA>& q, int i0, int j0, TA (&ps)[kDepth][kPitch], TA (&qs)[kDepth][kPitch],
-                                        typename Mma<TA>::acc_t (&acc)[4]) {
-  const int lane = threadIdx.x & (kLanes - 1), wave = threadIdx.x / kLanes;
+// A tile of kTile x kTile, kDepth reduced indices at a time.  Four waves of 16 rows x 64 columns, or of 16 x 16.
+template <typename TA, int kTile>
+struct Square {
+  static constexpr int kDepth = 1024 / kTile, kPitch = kTile + 4;
+  static constexpr int kAcross = kTile == 64 ? 1 : 2;          // waves side by side
+  static constexpr int kColumns = kTile / 16 / kAcross;        // 16 x 16 of a wave
+  typedef TA Space[kDepth][kPitch];
+  typedef typename Mma<TA>::acc_t Sums[kColumns];
+};
+
+// Sums over k of P(i, k) Q(j, k) of the tile (i0, j0).
+template <typename TA, int kTile>
+__device__ __forceinline__ void product(const View<TA>& p, const View<TA>& q, int i0, int j0, typename Square<TA, kTile>::Space& ps,
+                                        typename Square<TA, kTile>::Space& qs, typename Square<TA, kTile>::Sums& acc) {
+  using S = Square<TA, kTile>;
+  constexpr int kDepth = S::kDepth;
+  const int lane = threadIdx.x & (kLanes - 1), wave = threadIdx.x / kLanes, thread = threadIdx.x;
+  const int row0 = 16 * (wave / S::kAcross), col0 = 16 * (wave % S::kAcross);
   const int depth = p.depth;
-  auto load = [&](const View<TA>& v, int r0, int k, TA (&to)[kDepth][kPitch], TA (&x)[4]) {
+  // (neighbouring threads along what is contiguous)
+  auto load = [&](const View<TA>& v, int r0, int k, TA (&x)[4]) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const int kk = v.step == 1 ? k + threadIdx.x % 16 : k + threadIdx.x / 64 + 4 * e;
-      const int r = r0 + (v.step == 1 ? static_cast<int>(threadIdx.x) / 16 + 16 * e : static_cast<int>(threadIdx.x) % 64);
+      const int kk = v.step == 1 ? k + thread % kDepth : k + thread / kTile + e * (kThreads / kTile);
+      const int r = r0 + (v.step == 1 ? thread / kDepth + e * (kThreads / kDepth) : thread % kTile);
       x[e] = kk < depth && r < v.rows ? v.p[r * v.ld + kk * v.step] : TA(0);
     }
   };
-  auto put = [&](const View<TA>& v, TA (&to)[kDepth][kPitch], const TA (&x)[4]) {
+  auto put = [&](const View<TA>& v, typename S::Space& to, const TA (&x)[4]) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      if (v.step == 1) to[threadIdx.x % 16][threadIdx.x / 16 + 16 * e] = x[e];
-      else to[threadIdx.x / 64 + 4 * e][threadIdx.x % 64] = x[e];
+      if (v.step == 1) to[thread % kDepth][thread / kDepth + e * (kThreads / kDepth)] = x[e];
+      else to[thread / kTile + e * (kThreads / kTile)][thread % kTile] = x[e];
     }
   };
 #pragma unroll
-  for (int t = 0; t < 4; ++t) acc[t] = typename Mma<TA>::acc_t{0, 0, 0, 0};
+  for (int t = 0; t < S::kColumns; ++t) acc[t] = typename Mma<TA>::acc_t{0, 0, 0, 0};
+  TA x[4], y[4];   // a stage's indices, requested while those before are multiplied
+  load(p, i0, 0, x);
+  load(q, j0, 0, y);
   for (int k = 0; k < depth; k += kDepth) {
-    TA x[4], y[4];
-    load(p, i0, k, ps, x);
-    load(q, j0, k, qs, y);
-    __syncthreads();
+    barrier();
     put(p, ps, x);
     put(q, qs, y);
-    __syncthreads();
+    if (k + kDepth < depth) {
+      load(p, i0, k + kDepth, x);
+      load(q, j0, k + kDepth, y);
+    }
+    barrier();
 #pragma unroll
     for (int s = 0; s < kDepth / 4; ++s) {
-      const TA a = ps[4 * s + lane / 16][16 * wave + (lane & 15)];
+      const TA a = ps[4 * s + lane / 16][row0 + (lane & 15)];
 #pragma unroll
-      for (int t = 0; t < 4; ++t) acc[t] = Mma<TA>::mma(a, qs[4 * s + lane / 16][16 * t + (lane & 15)], acc[t]);
+      for (int t = 0; t < S::kColumns; ++t) acc[t] = Mma<TA>::mma(a, qs[4 * s + lane / 16][col0 + 16 * t + (lane & 15)], acc[t]);
     }
   }
 }
@@ -136,11 +155,12 @@ __device__ __forceinline__ void product(const View<TA>& p, const View<TA>& q, in
 enum Phase { kS, kP, kX };
 
 // The three products of a step: S from X; P from S; the next X from P and X (last: into the results).
-template <typename TA, int kPhase>
+template <typename TA, int kPhase, int kTile>
 __global__ __launch_bounds__(kThreads) void product_kernel(const Item* __restrict__ items, int n, const Step st, bool last, const TA* __restrict__ X,
                                                            TA* __restrict__ next, TA* __restrict__ S, TA* __restrict__ P) {
-  __shared__ TA ps[kDepth][kPitch], qs[kDepth][kPitch];
-  constexpr int kind = kPhase == kX ? kProduct : kGram;
+  using Tile = Square<TA, kTile>;
+  __shared__ typename Tile::Space ps, qs;
+  constexpr int kind = kTile == 64 ? (kPhase == kX ? kProduct : kGram) : kPhase == kX ? kProductSmall : kGramSmall;
   const int lane = threadIdx.x & (kLanes - 1), wave = threadIdx.x / kLanes;
   const Item& it = items[item_of(items, n, kind, blockIdx.x)];
   const bool turned = it.rows > it.cols;
@@ -151,23 +171,23 @@ __global__ __launch_bounds__(kThreads) void product_kernel(const Item* __restric
   const int64_t unit = blockIdx.x - it.unit[kind], per = static_cast<int64_t>(row_tiles) * col_tiles, matrix = unit / per;
   const int tile = static_cast<int>(unit % per), i0 = tile / col_tiles * kTile, j0 = tile % col_tiles * kTile;
   const int64_t x0 = it.x + matrix * m * l, s0 = it.s + matrix * m * m;
-  typename Mma<TA>::acc_t acc[4];
+  typename Tile::Sums acc;
   if constexpr (kPhase == kS) {
     const View<TA> v{X + x0, si, sk, m, l};
-    product<TA>(v, v, i0, j0, ps, qs, acc);
+    product<TA, kTile>(v, v, i0, j0, ps, qs, acc);
   } else if constexpr (kPhase == kP) {
     const View<TA> v{S + s0, m, 1, m, m};
-    product<TA>(v, v, i0, j0, ps, qs, acc);
+    product<TA, kTile>(v, v, i0, j0, ps, qs, acc);
   } else {
     const View<TA> p{P + s0, m, 1, m, m}, x{X + x0, sk, si, l, m};
-    product<TA>(p, x, i0, j0, ps, qs, acc);
+    product<TA, kTile>(p, x, i0, j0, ps, qs, acc);
   }
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
-    const int i = i0 + 16 * wave + Mma<TA>::row(lane, r);
+    const int i = i0 + 16 * (wave / Tile::kAcross) + Mma<TA>::row(lane, r);
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      const int j = j0 + 16 * t + (lane & 15);
+    for (int t = 0; t < Tile::kColumns; ++t) {
+      const int j = j0 + 16 * (wave % Tile::kAcross) + 16 * t + (lane & 15);
       if (i >= m || j >= columns) continue;
       if constexpr (kPhase == kS) {
         S[s0 + static_cast<int64_t>(i) * m + j] = acc[t][r];
@@ -208,8 +228,11 @@ void double_place(Part& p, Item& it, int64_t count) {
   const int64_t m = std::min(it.rows, it.cols), l = std::max(it.rows, it.cols);
   it.x = p.x;
   it.s = p.s;
-  p.units[kGram] += count * ceil_div(m, kTile) * ceil_div(m, kTile);
-  p.units[kProduct] += count * ceil_div(m, kTile) * ceil_div(l, kTile);
+  for (const int tile : {64, 32}) {
+    const int64_t tm = ceil_div(m, tile), tl = ceil_div(l, tile);
+    p.units[tile == 64 ? kGram : kGramSmall] += count * tm * tm;
+    p.units[tile == 64 ? kProduct : kProductSmall] += count * tm * tl;
+  }
   p.x += count * m * l;
   p.s += count * m * m;
 }
@@ -306,7 +329,7 @@ sc_status check(const char* fn, const ou_config* cfg, int64_t n, const ou_tensor
       what = "pointer not aligned to its element";
     if (what) return bad(SC_ERR_INVALID_ARG, "tensor " + std::to_string(i) + ": " + what);
     if (t.rows > OU_MAX_SIDE || t.cols > OU_MAX_SIDE) return bad(SC_ERR_UNSUPPORTED, "tensor " + std::to_string(i) + ": rows or cols above OU_MAX_SIDE");
-    const int64_t tiles = ceil_div(t.rows, kTile) * ceil_div(t.cols, kTile);
+    const int64_t tiles = ceil_div(t.rows, 64) * ceil_div(t.cols, 64);
     if (t.count > (OU_MAX_TILES - total) / tiles) return bad(SC_ERR_UNSUPPORTED, "more than OU_MAX_TILES tiles");
     total += t.count * tiles;
   }
@@ -342,6 +365,19 @@ hipError_t first_pass(const Layout& l, int way, int end, const Step& st, char* b
   return hipGetLastError();
 }
 
+// Tiles of 64 that do not fill the compute units: smaller ones (five steps of one 512 x 700 295 us instead of 716, of 40 512 x 512 4.1 ms instead of 3.6).
+template <int kPhase>
+hipError_t launch(const Part& p, const Item* items, const Step& st, bool last, const double* X, double* next, double* S, double* P, hipStream_t stream) {
+  const int n = static_cast<int>(p.items.size());
+  const int64_t tiles = p.units[kPhase == kX ? kProduct : kGram];
+  if (tiles > 256)
+    hipLaunchKernelGGL((product_kernel<double, kPhase, 64>), dim3(static_cast<unsigned>(tiles)), dim3(kThreads), 0, stream, items, n, st, last, X, next, S, P);
+  else
+    hipLaunchKernelGGL((product_kernel<double, kPhase, 32>), dim3(static_cast<unsigned>(p.units[kPhase == kX ? kProductSmall : kGramSmall])), dim3(kThreads), 0, stream,
+                       items, n, st, last, X, next, S, P);
+  return hipGetLastError();
+}
+
 hipError_t double_run(const Part& p, const ou_config* cfg, const Step& st, char* base, hipStream_t stream) {
   const int n = static_cast<int>(p.items.size());
   const Item* const items = reinterpret_cast<const Item*>(base + p.at_items);
@@ -349,21 +385,15 @@ hipError_t double_run(const Part& p, const ou_config* cfg, const Step& st, char*
   double* const X[2] = {reinterpret_cast<double*>(base + p.at_x), reinterpret_cast<double*>(base + p.at[0])};
   double* const S = reinterpret_cast<double*>(base + p.at[1]);
   double* const P = reinterpret_cast<double*>(base + p.at[2]);
-  auto grid = [&](Kind k) { return dim3(static_cast<unsigned>(p.units[k])); };
-  hipLaunchKernelGGL(normalise_kernel, grid(kChunks), dim3(kThreads), 0, stream, items, n, st, cfg->steps == 0, X[0], partial);
+  hipLaunchKernelGGL(normalise_kernel, dim3(static_cast<unsigned>(p.units[kChunks])), dim3(kThreads), 0, stream, items, n, st, cfg->steps == 0, X[0], partial);
   hipError_t e = hipGetLastError();
   for (int i = 0; i < cfg->steps && e == hipSuccess; ++i) {
     const bool last = i + 1 == cfg->steps;
     const double* const x = X[i & 1];
     double* const next = X[(i + 1) & 1];
-    hipLaunchKernelGGL((product_kernel<double, kS>), grid(kGram), dim3(kThreads), 0, stream, items, n, st, last, x, next, S, P);
-    e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((product_kernel<double, kP>), grid(kGram), dim3(kThreads), 0, stream, items, n, st, last, x, next, S, P);
-    e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((product_kernel<double, kX>), grid(kProduct), dim3(kThreads), 0, stream, items, n, st, last, x, next, S, P);
-    e = hipGetLastError();
+    e = launch<kS>(p, items, st, last, x, next, S, P, stream);
+    if (e == hipSuccess) e = launch<kP>(p, items, st, last, x, next, S, P, stream);
+    if (e == hipSuccess) e = launch<kX>(p, items, st, last, x, next, S, P, stream);
   }
   return e;
 }
