@@ -23,7 +23,8 @@
  *
  * ou_tensor is a HOST array that the call reads before it returns (its contents travel to the device as kernel arguments: no copy, no
  * allocation, usable in a captured graph).  Tensors are dense, row-major, aligned to at least their element, and
- * share no memory.  Sums have a fixed order (bitwise reproducible results).  Other conventions as in sc.h.
+ * share no memory.  Sums have a fixed order: the same list gives the same bits (which kernel a matrix takes, and so its last bits, may depend on what else is in the
+ * list).  Other conventions as in sc.h.
  */
 #ifndef OU_MI355X_H
 #define OU_MI355X_H
@@ -47,7 +48,7 @@ typedef struct {
   void* momentum;   /* dev: M, updated in place; NULL: none                           */
   void* weight;     /* dev: W, updated in place; NULL: only the update is wanted      */
   void* update;     /* dev: X, overwritten; NULL: only the weight is wanted           */
-  double scale;     /* finite                                                         */
+  double scale;     /* finite, as rate * scale, rate * decay, momentum; in fp32 too but for SC_F64 */
   int64_t count;    /* matrices, 0 is valid                                           */
   int32_t rows;     /* 1..OU_MAX_SIDE                                                 */
   int32_t cols;     /* 1..OU_MAX_SIDE                                                 */

@@ -3,6 +3,7 @@
 // The list goes to the workspace once.  Then, each for all tensors of a way together: momentum and sums of squares; X = U / norm; per step S = X X^T, P = b S + c S S,
 // X = a X + P X; the last step's results go straight into the update and the weights.
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <string>
 
@@ -294,6 +295,8 @@ Layout layout_of(int64_t n, const ou_tensor* tensors, int steps) {
   return l;
 }
 
+bool representable(double v, int32_t dtype) { return std::fabs(v) <= (dtype == SC_F64 ? DBL_MAX : static_cast<double>(FLT_MAX)); }
+
 sc_status check(const char* fn, const ou_config* cfg, int64_t n, const ou_tensor* tensors) {
   auto bad = [&](sc_status st, const std::string& what) { return set_error(st, std::string(fn) + ": " + what); };
   if (!cfg) return bad(SC_ERR_INVALID_ARG, "cfg is NULL");
@@ -321,7 +324,8 @@ sc_status check(const char* fn, const ou_config* cfg, int64_t n, const ou_tensor
     else if (t.reserved != 0) what = "reserved is not 0";
     else if (t.rows < 1 || t.cols < 1) what = "rows or cols < 1";
     else if (t.count < 0) what = "count < 0";
-    else if (!std::isfinite(t.scale)) what = "scale is not finite";
+    else if (!representable(t.scale, t.dtype) || !representable(cfg->rate * t.scale, t.dtype)) what = "scale, or rate * scale, is not finite in the tensor's arithmetic";
+    else if (!representable(cfg->momentum, t.dtype) || !representable(1 - cfg->rate * cfg->decay, t.dtype)) what = "momentum or rate * decay is not finite in the tensor's arithmetic";
     else if (t.count > 0 && !t.grad) what = "grad is NULL";
     else if (t.count > 0 && !t.weight && !t.update) what = "weight and update are both NULL";
     const size_t narrow = t.dtype == SC_F64 ? 8 : t.dtype == SC_F32 ? 4 : 2, wide = t.dtype == SC_F64 ? 8 : 4;

@@ -318,3 +318,28 @@ def test_calls_at_the_same_time(ou):
     for x in (a, b):
         for p, q in zip(x.momentum + x.weight + x.update, want.momentum + want.weight + want.update):
             assert torch.equal(p, q)
+
+
+@pytest.mark.parametrize("shape", [(131_073, 128, 128), (140_001, 64, 256), (33_001, 256, 260)], ids=lambda s: "x".join(map(str, s)))
+def test_batches_past_32_bits(ou, shape):
+    """More than 2^31 elements in a tensor: the first and the last matrices."""
+    import torch
+    count, rows, cols = shape
+    g = torch.Generator(device="cuda").manual_seed(4)
+    grad = torch.zeros(shape, dtype=torch.bfloat16, device="cuda")
+    ends = [0, 1, count - 2, count - 1]
+    for i in ends:
+        grad[i] = torch.randn(rows, cols, generator=g, device="cuda") * 1e-2
+    update = torch.empty_like(grad)
+    cfg = ou.make_config(0.02, steps=2)
+    tensors = ou.make_tensors([grad], None, None, [update])
+    nbytes = ou.ou_workspace_bytes(cfg, tensors)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+    ou.ou_step(cfg, tensors, ws, nbytes)
+    torch.cuda.synchronize()
+    u = 2.0 ** -23
+    for i in ends:
+        want = oo.iterate(grad[i].double().cpu().numpy(), 2)
+        allowed = 8 * u * np.sqrt(rows * cols) * 5 + 4 * u * 16 + 2.0 ** -8 * np.sqrt((want ** 2).sum())
+        assert np.sqrt(((update[i].double().cpu().numpy() - want) ** 2).sum()) <= allowed, i
+    assert not update[2:count - 2].any()

@@ -414,3 +414,32 @@ def test_values_beyond_the_parts_in_the_gradients(gp):
             b.residual.zero_()
             print(f"products range {dtype} {n}", flush=True)
             b.check(*b.all())
+
+
+@pytest.mark.parametrize("n", [64, 70])
+def test_offsets_past_32_bits(gp, n):
+    """Blocks as far apart as they may be: the last atom's begin beyond 2^31 elements (n = 64: 2^32 bytes)."""
+    import torch
+    k, elements, ld = 64, 3, gp.GP_MAX_STRIDE
+    cfg = gp.make_config(elements, k, k, 1, gp.SC_BF16, ld_in=ld, ld_out=ld)
+    g = torch.Generator(device="cuda").manual_seed(2)
+    z = (torch.arange(n, device="cuda") % (elements + 1)).int()                  # the last of them is no element
+    far = lambda: torch.empty((n - 1) * ld + k, dtype=torch.bfloat16, device="cuda").as_strided((n, k), (ld, 1))  # noqa: E731
+    X, dY, Y, dX = far(), far(), far(), far()
+    for t in (X, dY):
+        t.copy_(torch.randn(n, k, generator=g, device="cuda"))
+    W = torch.randn(elements, k, k, generator=g, device="cuda") / 8
+    dW = torch.full_like(W, NAN)
+    nbytes, ws_bytes = gp.gp_grouping_bytes(cfg, n), gp.gp_workspace_bytes(cfg, n)
+    grouping = torch.empty(nbytes, dtype=torch.uint8, device="cuda") if nbytes else None
+    ws = torch.empty(ws_bytes, dtype=torch.uint8, device="cuda")
+    gp.gp_group(cfg, n, z, grouping, nbytes)
+    gp.gp_forward(cfg, n, z, grouping, X, W, None, Y, ws, ws_bytes)
+    gp.gp_backward(cfg, n, z, grouping, X, W, dY, dX, dW, ws, ws_bytes)
+    torch.cuda.synchronize()
+    f64 = lambda t: t.double().cpu().numpy()  # noqa: E731
+    zs, x, w, dy = z.cpu().numpy(), f64(X)[:, None], f64(W), f64(dY)[:, None]
+    wY, (wdX, wdW) = op.forward(zs, x, w, None), op.backward(zs, x, w, dy)
+    mY, (mdX, mdW) = op.forward(zs, abs(x), abs(w), None), op.backward(zs, abs(x), abs(w), abs(dy))
+    for got, want, most, terms, last in ((Y, wY[:, 0], mY[:, 0], k, 2.0 ** -8), (dX, wdX[:, 0], mdX[:, 0], k, 2.0 ** -8), (dW, wdW, mdW, n, 0.0)):
+        assert (abs(f64(got) - want) <= (terms + 4) * 2.0 ** -23 * most * (1 + last) + last * abs(want)).all()

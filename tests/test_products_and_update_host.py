@@ -126,6 +126,11 @@ def test_update_refusals():
         bad[at] = value
         refused(INVALID, ou.ou_workspace_bytes, cfg, tensors(OK, tuple(bad)))
     refused(INVALID, ou.ou_workspace_bytes, cfg, tensors((256, 512, None, None, 1.0, 2, 8, 64, 0)))    # no result
+    double = (256, 512, 1024, 2048, 1.0, 2, 8, 64, 1)
+    for kw, scale in ((dict(rate=0.02, momentum=1e39), 1.0), (dict(rate=1e30), 1e10), (dict(rate=1e30, decay=1e10), 1.0), (dict(rate=1e-9), 1e39)):
+        refused(INVALID, ou.ou_workspace_bytes, ou.make_config(**kw), tensors(OK[:4] + (scale,) + OK[5:]))   # beyond fp32
+        ou.ou_workspace_bytes(ou.make_config(**kw), tensors(double[:4] + (scale,) + double[5:]))
+    refused(INVALID, ou.ou_workspace_bytes, ou.make_config(rate=1e200), tensors(double[:4] + (1e200,) + double[5:]))
     odd = tensors(OK)
     odd[0].reserved = 1
     refused(INVALID, ou.ou_workspace_bytes, cfg, odd)
