@@ -9,6 +9,10 @@
 // A workgroup: 128 rows of a bucket x 128 columns, or 128 x 128 of an element's dW over a chunk of rows, four waves of 64 x 64.  32 reduced indices of both
 // operands are requested while the 32 before are multiplied, and pass through registers, where they are split, to LDS.  One set of LDS and two barriers a
 // stage: the two workgroups of a compute unit fill each other's waits.
+//
+// 149 997 rows of fp32, 128 x 128: Y 54 us (160 MB, 3.0 TB/s; the products are 27 at the rate of a large product), dW 62 and 15 for the chunks' sums; 200 000 of bfloat16: 47, 44
+// and 32 us.  What bounds them is the splitting beside loads and products in turn: the matrix cores work a fifth of the cycles.  16 384 rows, 64 elements,
+// 1024 x 2048: Y 321 us of bfloat16 (640 TFLOP/s), 562 of fp32 (730), matrix cores a third of the cycles.
 #include <algorithm>
 #include <type_traits>
 

@@ -3,7 +3,8 @@
 //
 // Rows (Y, dX): a workgroup computes 64 rows of one bucket x 64 columns; the rows are gathered by the grouping's order, the reduced index goes
 // through LDS 16 at a time.  dW: a workgroup computes 64 x 64 of one element's matrix over a chunk of the element's rows; elements with several chunks leave
-// partial matrices that a second launch adds in order.
+// partial matrices that a second launch adds in order.  fp64, 60 000 rows, 128 x 128: Y and dX 65 us each, where the products at the rate of a large one are 31 and the
+// memory 26, dW 124; the loads of a stage are waited for.
 #include <algorithm>
 #include <initializer_list>
 #include <string>

@@ -93,7 +93,8 @@ __device__ __forceinline__ void put_parts(const float* block, float up, int rows
   }
 }
 
-// A 64 x 64 block of X = U / (norm + eps): X, and its parts in both orientations.  last: no steps follow.
+// A 64 x 64 block of X = U / (norm + eps): X, and its parts in both orientations.  last: no steps follow.  Memory bounds it: 2 x 4096 x 4096 131 us for 268 MB read and
+// 403 written.
 __global__ __launch_bounds__(kThreads) void normalise_kernel(const Item* __restrict__ items, int n, const Step st, bool last, const Buffers buf, float up,
                                                              const double* __restrict__ partial) {
   __shared__ double slots[kWaves];

