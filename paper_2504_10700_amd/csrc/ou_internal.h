@@ -27,7 +27,7 @@ struct Item {
   void* update;
   double scale;
   int64_t unit[kKinds];
-  int64_t x, s;            // where the tensor's X and S begin in their buffers, in elements
+  int64_t x, s;            // where the tensor's X and (fp64) S begin in their buffers, in elements
   int64_t px, pt, ps;      // and the parts of X, of X transposed, of S and P
   int32_t rows, cols, dtype;
   int32_t width;           // of a slice (ou_small.hip)
@@ -52,7 +52,7 @@ struct Part {
   int64_t units[kKinds] = {};
   int64_t x = 0, s = 0, px = 0, pt = 0, ps = 0;
   size_t at_items = 0, at_partial = 0, at_x = 0;
-  size_t at[6] = {};   // the way's other buffers
+  size_t at[5] = {};   // the way's other buffers
 };
 
 // What workspace there is: room(bytes) is the offset of the next piece.

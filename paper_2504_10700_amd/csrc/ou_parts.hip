@@ -24,6 +24,7 @@ namespace ou {
 namespace {
 
 typedef _Float16 H8 __attribute__((ext_vector_type(8)));
+typedef _Float16 H4 __attribute__((ext_vector_type(4)));
 typedef float F16 __attribute__((ext_vector_type(16)));
 typedef unsigned U4 __attribute__((ext_vector_type(4)));
 typedef float F4 __attribute__((ext_vector_type(4)));
@@ -44,7 +45,6 @@ __host__ __device__ constexpr int64_t padded(int64_t n) { return ((n + kPad - 1)
 // lines: 4096 x 4096 twice 10.2 ms instead of 9.3).
 struct Buffers {
   float* X;             // [m][l]
-  float* S;             // [m][padded(m)], the tiles on and below the diagonal
   _Float16* x;          // X
   _Float16* t;          // X transposed
   _Float16* next;       // the next X transposed
@@ -56,6 +56,7 @@ struct Buffers {
 struct Scales {
   float up;      // values that the phase makes to parts
   float down;    // sums of parts to values
+  float beside;  // parts of S to values (phase P)
 };
 
 // The parts of a 32 x 32 block in LDS to rows of parts that begin at `to`, `pitch` apart; the block's columns are c on, a multiple of 32.  kTurned: value (i, j) is at
@@ -373,7 +374,7 @@ __global__ __launch_bounds__(kThreads, 2) void product_kernel(const Item* __rest
   const bool mirrored = kPhase != kX && ti != tj;
   const int columns = kPhase == kX ? l : m;
   const float ca = static_cast<float>(st.a), cb = static_cast<float>(st.b), cc = static_cast<float>(st.c);
-  // what stands beside a block's sums, S or X, requested a block ahead (rows beyond the last: the last one)
+  // what stands beside a block's sums, S (its parts) or X, requested a block ahead (rows beyond the last: the last one)
   constexpr int kBlocks = kSide * kSide;
   F4 beside[2][4];
   auto request = [&](int block) {
@@ -385,7 +386,9 @@ __global__ __launch_bounds__(kThreads, 2) void product_kernel(const Item* __rest
       const int i = min(ib + row + 8 * k, m - 1), j = jb + column;
       F4 x{0, 0, 0, 0};
       if constexpr (kPhase == kP) {
-        x = *reinterpret_cast<const F4*>(buf.S + it.s + (matrix * m + i) * mp + j);
+        const _Float16* const parts = buf.s + it.ps + 2 * ((matrix * m + i) * mp + jb) + column;   // (22 bits of S; b S has no need of more beside S S of the same parts)
+        const H4 h = *reinterpret_cast<const H4*>(parts), low = *reinterpret_cast<const H4*>(parts + 32);
+        x = (__builtin_convertvector(h, F4) + __builtin_convertvector(low, F4)) * sc.beside;
       } else {
         const float* const X = buf.X + it.x + (static_cast<int64_t>(matrix) * m + i) * l;
         if (jb + 32 <= l) {
@@ -413,14 +416,14 @@ __global__ __launch_bounds__(kThreads, 2) void product_kernel(const Item* __rest
       wave_sync();
       // what the phase makes of the sums, in fp32
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
+      for (int k = 0; k < (kPhase == kS ? 0 : 4); ++k) {
         const int i = ib + row + 8 * k, j = jb + column;
         float* const here = corner + (row + 8 * k) * kPitch + column;
         F4 v = *reinterpret_cast<const F4*>(here);
         if constexpr (kPhase == kP) v = cb * beside[block & 1][k] + cc * v;
         if constexpr (kPhase == kX) v = ca * beside[block & 1][k] + v;
-        if (i < m) {
-          if constexpr (kPhase == kX) {
+        if constexpr (kPhase == kX) {
+          if (i < m) {
             const int64_t at = (static_cast<int64_t>(matrix) * m + i) * l + j;
             float* const X = buf.X + it.x + at;
             if (last) {
@@ -432,11 +435,9 @@ __global__ __launch_bounds__(kThreads, 2) void product_kernel(const Item* __rest
               for (int n = 0; n < 4; ++n)
                 if (j + n < l) X[n] = v[n];
             }
-          } else if constexpr (kPhase == kS) {
-            *reinterpret_cast<F4*>(buf.S + it.s + (matrix * m + i) * mp + j) = v;
           }
         }
-        if constexpr (kPhase != kS) *reinterpret_cast<F4*>(here) = v;
+        *reinterpret_cast<F4*>(here) = v;
       }
       if constexpr (kPhase != kS) wave_sync();
       if constexpr (kPhase == kX) {
@@ -471,7 +472,6 @@ int exponent_of(double top) { return 14 - static_cast<int>(std::ceil(std::log2(s
 void parts_place(Part& p, Item& it, int64_t count) {
   const int64_t m = std::min(it.rows, it.cols), l = std::max(it.rows, it.cols);
   it.x = p.x;
-  it.s = p.s;
   it.px = p.px;
   it.pt = p.pt;
   it.ps = p.ps;
@@ -483,7 +483,6 @@ void parts_place(Part& p, Item& it, int64_t count) {
   }
   p.x += count * m * l;
   p.x = (p.x + 3) / 4 * 4;
-  p.s += count * m * padded(m);
   p.px += 2 * count * m * padded(l);
   p.pt += 2 * count * l * padded(m);
   p.ps += 2 * count * m * padded(m);
@@ -492,12 +491,11 @@ void parts_place(Part& p, Item& it, int64_t count) {
 void parts_layout(Part& p, Room& room, int steps) {
   if (steps == 0) return;
   p.at_x = room(p.x * sizeof(float));
-  p.at[0] = room(p.s * sizeof(float));
-  p.at[1] = room(p.px * sizeof(_Float16));
+  p.at[0] = room(p.px * sizeof(_Float16));
+  p.at[1] = room(p.pt * sizeof(_Float16));
   p.at[2] = room(p.pt * sizeof(_Float16));
-  p.at[3] = room(p.pt * sizeof(_Float16));
+  p.at[3] = room(p.ps * sizeof(_Float16));
   p.at[4] = room(p.ps * sizeof(_Float16));
-  p.at[5] = room(p.ps * sizeof(_Float16));
 }
 
 namespace {
@@ -533,7 +531,7 @@ hipError_t parts_run(const Part& p, const ou_config* cfg, const Step& st, char* 
   const Item* const items = reinterpret_cast<const Item*>(base + p.at_items);
   const double* const partial = reinterpret_cast<const double*>(base + p.at_partial);
   auto halfs = [&](int i) { return reinterpret_cast<_Float16*>(base + p.at[i]); };
-  Buffers buf{reinterpret_cast<float*>(base + p.at_x), reinterpret_cast<float*>(base + p.at[0]), halfs(1), halfs(2), halfs(3), halfs(4), halfs(5)};
+  Buffers buf{reinterpret_cast<float*>(base + p.at_x), halfs(0), halfs(1), halfs(2), halfs(3), halfs(4)};
   double top = 1;
   int ex = exponent_of(top);
   hipLaunchKernelGGL(normalise_kernel, dim3(static_cast<unsigned>(p.units[kBlocks])), dim3(kThreads), 0, stream, items, n, st, cfg->steps == 0, buf,
@@ -545,9 +543,9 @@ hipError_t parts_run(const Part& p, const ou_config* cfg, const Step& st, char* 
     const int es = exponent_of(square), ep = exponent_of(std::fabs(cfg->b) * square + std::fabs(cfg->c) * square * square);
     top = growth(cfg, top);
     const int next = exponent_of(top);
-    e = launch<kS>(p, items, st, last, buf, Scales{std::ldexp(1.f, es), std::ldexp(1.f, -2 * ex)}, stream);
-    if (e == hipSuccess) e = launch<kP>(p, items, st, last, buf, Scales{std::ldexp(1.f, ep), std::ldexp(1.f, -2 * es)}, stream);
-    if (e == hipSuccess) e = launch<kX>(p, items, st, last, buf, Scales{std::ldexp(1.f, next), std::ldexp(1.f, -ep - ex)}, stream);
+    e = launch<kS>(p, items, st, last, buf, Scales{std::ldexp(1.f, es), std::ldexp(1.f, -2 * ex), 0}, stream);
+    if (e == hipSuccess) e = launch<kP>(p, items, st, last, buf, Scales{std::ldexp(1.f, ep), std::ldexp(1.f, -2 * es), std::ldexp(1.f, -es)}, stream);
+    if (e == hipSuccess) e = launch<kX>(p, items, st, last, buf, Scales{std::ldexp(1.f, next), std::ldexp(1.f, -ep - ex), 0}, stream);
     ex = next;
     std::swap(buf.t, buf.next);
   }
