@@ -8,11 +8,12 @@
 //
 // A workgroup: 128 rows of a bucket x 128 columns, or 128 x 128 of an element's dW over a chunk of rows, four waves of 64 x 64.  32 reduced indices of both
 // operands are requested while the 32 before are multiplied, and pass through registers, where they are split, to LDS.  One set of LDS and two barriers a
-// stage: the two workgroups of a compute unit fill each other's waits.
+// stage: the two or, of bfloat16 rows, three workgroups of a compute unit fill each other's waits (200 000 rows of bfloat16, 128 x 128: 38 us with three, 43 with two
+// that request their rows two stages ahead).
 //
-// 149 997 rows of fp32, 128 x 128: Y 54 us (160 MB, 3.0 TB/s; the products are 27 at the rate of a large product), dW 62 and 15 for the chunks' sums; 200 000 of bfloat16: 47, 44
-// and 32 us.  What bounds them is the splitting beside loads and products in turn: the matrix cores work a fifth of the cycles.  16 384 rows, 64 elements,
-// 1024 x 2048: Y 321 us of bfloat16 (640 TFLOP/s), 562 of fp32 (730), matrix cores a third of the cycles.
+// 149 997 rows of fp32, 128 x 128: Y 54 us (160 MB, 3.0 TB/s; the products are 27 at the rate of a large product), dW 62 and 15 for the chunks' sums; 200 000 of bfloat16: 38, 35
+// and 30 us.  What bounds them is the splitting beside loads and products in turn: the matrix cores work a fifth of the cycles.  16 384 rows, 64 elements,
+// 1024 x 2048: Y 295 us of bfloat16 (700 TFLOP/s), 555 of fp32 (740), matrix cores a third of the cycles.
 #include <algorithm>
 #include <type_traits>
 
@@ -308,7 +309,7 @@ __device__ __forceinline__ void store_piece(T* p, const T* residual, int inside,
 // Tiles of 64 kR rows.  kEights: widths are multiples of 8, so a piece is all there or not at all, and no request needs a test of its own (vectors of 128: 53 us, 58
 // with the tests).
 template <typename T, bool kBack, int kR, bool kEights>
-__global__ __launch_bounds__(kThreads, kR == 2 || sizeof(T) == 4 ? 2 : 3) void rows_parts_kernel(const Rows a) {
+__global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 2 : 3) void rows_parts_kernel(const Rows a) {
   constexpr int kTileRows = 64 * kR, kPlaneX = kTileRows * kStage;
   constexpr int NX = parts<T>(), NW = 3;
   constexpr bool kOneSum = NX == 1;
@@ -349,7 +350,7 @@ __global__ __launch_bounds__(kThreads, kR == 2 || sizeof(T) == 4 ? 2 : 3) void r
       }
       const int pair = 2 * lane;                                                   // forward: columns c0 + pair, + 1 of rows 8 wave on
       const float* const w_rows = W + min(c0 + pair, a.columns - 2);
-      constexpr int kAhead = sizeof(T) == 2 || kR == 1 ? 2 : 1;   // stages of rows under way, as registers allow (of W one)
+      constexpr int kAhead = kR == 1 ? 2 : 1;   // stages of rows under way, as registers allow (of W one)
       Eight<T> xv[kAhead][kR];
       Eight<float> wv[2];
       TwoColumns<float> wc;
