@@ -72,7 +72,7 @@ sc_status gp_workspace_bytes(const gp_config* cfg, int64_t n_nodes, size_t* byte
 /* Forward.  z [n_nodes]; grouping: as gp_group wrote it for this z (NULL up to GP_UNGROUPED atoms); X [n_nodes][components][k_in];
  * W [num_elements][k_in][k_out]; residual [n_nodes][components][k_out] or NULL; Y [n_nodes][components][k_out].
  * workspace: device memory of at least gp_workspace_bytes().  n_nodes == 0 does nothing.
- * With the grouping of another z the results are wrong (never an access outside the buffers of this call). */
+ * With the grouping of another z for as many elements the results are wrong (never an access outside the buffers of this call). */
 sc_status gp_forward(const gp_config* cfg, int64_t n_nodes, const int32_t* z, const void* grouping, const void* X, const void* W,
                      const void* residual, void* Y, void* workspace, size_t workspace_bytes, void* hip_stream);
 

@@ -443,3 +443,26 @@ def test_offsets_past_32_bits(gp, n):
     mY, (mdX, mdW) = op.forward(zs, abs(x), abs(w), None), op.backward(zs, abs(x), abs(w), abs(dy))
     for got, want, most, terms, last in ((Y, wY[:, 0], mY[:, 0], k, 2.0 ** -8), (dX, wdX[:, 0], mdX[:, 0], k, 2.0 ** -8), (dW, wdW, mdW, n, 0.0)):
         assert (abs(f64(got) - want) <= (terms + 4) * 2.0 ** -23 * most * (1 + last) + last * abs(want)).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f64", "bf16"])
+def test_the_grouping_of_another_batch_stays_inside(gp, dtype):
+    """A larger and a smaller batch's: rows may be missing or taken twice, but what lies around the call's tensors and its workspace stays as it was."""
+    import torch
+    b = Batch(gp, 500, 6, 64, 72, 2, dtype, gap=(3, 5))
+    want = b.all()
+    for n in (70, 400, 5000):
+        other = Batch(gp, n, 6, 64, 72, 2, dtype, seed=n)
+        other.group()
+        edge = 4096
+        ws = torch.full((b.ws_bytes + 2 * edge,), 77, dtype=torch.uint8, device="cuda")
+        Y, dX, dW = b.block(72, out=True), b.block(64), b.skewed(b.W.shape, b.weights)
+        print(f"grouping of {n} atoms {dtype}", flush=True)
+        gp.gp_forward(b.cfg, b.n, b.z, other.grouping, b.X, b.W, None, Y, ws[edge:], b.ws_bytes)
+        gp.gp_backward(b.cfg, b.n, b.z, other.grouping, b.X, b.W, b.dY, dX, dW, ws[edge:], b.ws_bytes)
+        torch.cuda.synchronize()
+        assert (ws[:edge] == 77).all() and (ws[edge + b.ws_bytes:] == 77).all()
+        for t in (Y, dX):
+            assert t.whole[:, t.shape[1] * t.shape[2]:].isnan().all()
+    for x, y in zip(b.all(), want):
+        assert torch.equal(x, y)

@@ -124,3 +124,10 @@ def test_products_and_update_in_one_graph(ts):
         torch.cuda.synchronize()
         for name in ("Y", "dX", "dW", "M", "W"):
             assert torch.equal(getattr(captured, name), getattr(eager, name)), (turn, name)
+
+
+def test_the_command(ts, monkeypatch, capsys):
+    monkeypatch.setattr("sys.argv", ["training_step", "--atoms", "200", "--degree", "5", "--channels", "64", "--steps", "2", "--self-connection", "--orthogonalised"])
+    ts.main()
+    lines = capsys.readouterr().out.splitlines()
+    assert lines[0].startswith("200 atoms") and len(lines) == 3 and "nan" not in lines[2]
