@@ -26,11 +26,14 @@ typedef unsigned U4 __attribute__((ext_vector_type(4)));
 constexpr int kSlices = 64;
 constexpr int kUnits = 256;   // compute units
 
-// Powers of two: values to parts, and sums of parts to values.  The same for all steps (what a step could gain by its own is the growth of the bound over the
-// steps, a bit or less with the usual coefficients), so that none is looked up between two products.
+// Powers of two of a step: values to parts, and sums of parts to values.  Each step has its own, from the bound before it: P's goes with the fourth power of the bound, so one
+// set for all steps, from the largest bound, loses P where the coefficients make it grow ((8.28, -23.6, 17.3), two steps, 64 x 64: X off by 150%, with these by 5e-7).
 struct Scales {
   float x_up, s_up, p_up;
   float xx_down, ss_down, px_down;
+};
+struct AllScales {
+  Scales step[OU_MAX_STEPS];
 };
 
 template <int N>
@@ -355,7 +358,7 @@ __device__ __forceinline__ void next_x(float a, float scale, const typename Shap
 
 // A matrix of m, l <= N.  Rows and columns of parts up to the next multiple of 32 are zeros, those beyond are never used.
 template <int N>
-__device__ __forceinline__ void whole(const Item* __restrict__ items, int n, int64_t unit, const Step& st, int steps, const Scales& sc) {
+__device__ __forceinline__ void whole(const Item* __restrict__ items, int n, int64_t unit, const Step& st, int steps, const AllScales& all) {
   using S = Shape<N>;
   extern __shared__ __attribute__((aligned(16))) _Float16 lds[];
   _Float16* const square = lds;
@@ -376,7 +379,10 @@ __device__ __forceinline__ void whole(const Item* __restrict__ items, int n, int
   const double down = 1.0 / (sqrt(workgroup_sum(sum, reinterpret_cast<double*>(lds))) + st.eps);
   each_result<N>([&](int e, int f, int q, int, int) { x[e][f][q] = static_cast<float>(static_cast<double>(x[e][f][q]) * down); });
   const float ca = static_cast<float>(st.a);
+  Scales next = all.step[0];
   for (int step = 0; step < steps; ++step) {
+    const Scales sc = next;
+    next = all.step[min(step + 1, OU_MAX_STEPS - 1)];   // (asked for a step ahead)
     put<N, true, true>(x, sc.x_up, m, l, turned_x, square);
     __syncthreads();
     multiply<N>(square, square, m, m, deep_l, s);
@@ -397,22 +403,22 @@ __device__ __forceinline__ void whole(const Item* __restrict__ items, int n, int
 }
 
 template <int N>
-__global__ __launch_bounds__(kThreads) void whole_kernel(const Item* __restrict__ items, int n, const Step st, int steps, const Scales sc) {
+__global__ __launch_bounds__(kThreads) void whole_kernel(const Item* __restrict__ items, int n, const Step st, int steps, const AllScales sc) {
   whole<N>(items, n, blockIdx.x, st, steps, sc);
 }
 
 // Matrices of up to 128 (`large` of them) and, after them, of up to 64.
 __global__ __launch_bounds__(kThreads) void both_kernel(const Item* __restrict__ items128, int n128, int large, const Item* __restrict__ items64, int n64, const Step st,
-                                                        int steps, const Scales sc) {
+                                                        int steps, const AllScales sc) {
   const int unit = blockIdx.x;
   if (unit < large) whole<128>(items128, n128, unit, st, steps, sc);
   else whole<64>(items64, n64, unit - large, st, steps, sc);
 }
 
 // Slices of `width` columns (a multiple of N) of a matrix of m <= N.  step 0: X from the gradient; then the step before `step` of the iteration; the last one leaves the
-// results.  X and the slices' shares of S (partial) are kept in the order of the registers.
+// results.  X and the slices' shares of S (partial) are kept in the order of the registers.  sc: of that step; next_up, next_down: x_up and xx_down of the one after it.
 template <int N>
-__global__ __launch_bounds__(kThreads) void slice_kernel(const Item* __restrict__ items, int n, const Step st, int step, bool last, const Scales sc,
+__global__ __launch_bounds__(kThreads) void slice_kernel(const Item* __restrict__ items, int n, const Step st, int step, bool last, const Scales sc, float next_up, float next_down,
                                                          const double* __restrict__ squares, float* __restrict__ X, const float* __restrict__ partial,
                                                          float* __restrict__ next_partial) {
   using S = Shape<N>;
@@ -475,13 +481,13 @@ __global__ __launch_bounds__(kThreads) void slice_kernel(const Item* __restrict_
     }
     store_square<N>(x_here, x);   // (zeros up to the next multiples of 32, beyond whatever the products were)
     // (the columns up to the next multiple of 32 are read too: they hold zeros, made of the parts' zeros)
-    put<N, false, true>(x, sc.x_up, m, columns, nullptr, slice);
+    put<N, false, true>(x, next_up, m, columns, nullptr, slice);
     __syncthreads();
     multiply<N>(slice, slice, m, m, (columns + 31) / 32 * 32, r);
 #pragma unroll
     for (int e = 0; e < kSide; ++e)
 #pragma unroll
-      for (int f = 0; f < kSide; ++f) s[e][f] += sc.xx_down * r[e][f];
+      for (int f = 0; f < kSide; ++f) s[e][f] += next_down * r[e][f];
     __syncthreads();
   }
   if (last) return;
@@ -498,26 +504,30 @@ hipError_t launch(Kernel kernel, int bytes, int64_t grid, hipStream_t stream, Ar
   return hipGetLastError();
 }
 
-Scales scales_of(const ou_config* cfg) {
-  double top = 1, most = 1;
+AllScales scales_of(const ou_config* cfg) {
+  AllScales all{};
+  double top = 1;
   for (int i = 0; i < cfg->steps; ++i) {
+    const double square = top * top;
+    const int x = exponent_of(top), s = exponent_of(square), p = exponent_of(std::fabs(cfg->b) * square + std::fabs(cfg->c) * square * square);
+    all.step[i] = {std::ldexp(1.f, x), std::ldexp(1.f, s), std::ldexp(1.f, p), std::ldexp(1.f, -2 * x), std::ldexp(1.f, -2 * s), std::ldexp(1.f, -p - x)};
     top = growth(cfg, top);
-    most = std::max(most, top);
   }
-  const double square = most * most;
-  const int x = exponent_of(most), s = exponent_of(square), p = exponent_of(std::fabs(cfg->b) * square + std::fabs(cfg->c) * square * square);
-  return {std::ldexp(1.f, x), std::ldexp(1.f, s), std::ldexp(1.f, p), std::ldexp(1.f, -2 * x), std::ldexp(1.f, -2 * s), std::ldexp(1.f, -p - x)};
+  return all;
 }
 
 template <int N>
 hipError_t slices(const Part& p, const ou_config* cfg, const Step& st, char* base, const Item* items, hipStream_t stream) {
-  const Scales sc = scales_of(cfg);
+  const AllScales sc = scales_of(cfg);
   float* const partial[2] = {reinterpret_cast<float*>(base + p.at[0]), reinterpret_cast<float*>(base + p.at[1])};
   const double* const squares = reinterpret_cast<const double*>(base + p.at_partial);
   hipError_t e = hipSuccess;
-  for (int step = 0; step <= cfg->steps && e == hipSuccess; ++step)
-    e = launch(&slice_kernel<N>, Shape<N>::kBytes, p.units[kBlocks], stream, items, static_cast<int>(p.items.size()), st, step, step == cfg->steps, sc, squares,
+  for (int step = 0; step <= cfg->steps && e == hipSuccess; ++step) {
+    const Scales& next = sc.step[std::min(step, OU_MAX_STEPS - 1)];
+    e = launch(&slice_kernel<N>, Shape<N>::kBytes, p.units[kBlocks], stream, items, static_cast<int>(p.items.size()), st, step, step == cfg->steps, sc.step[std::max(step - 1, 0)],
+               next.x_up, next.xx_down, squares,
                reinterpret_cast<float*>(base + p.at_x), static_cast<const float*>(partial[(step + 1) & 1]), partial[step & 1]);
+  }
   return e;
 }
 
@@ -551,7 +561,7 @@ hipError_t slice_run(const Part& p, const ou_config* cfg, const Step& st, bool l
 // A matrix of up to 64 takes a quarter of the LDS that one of up to 128 takes, so four of them share a compute unit.  Where a unit for each
 // of both sizes is there, they have one launch (10 matrices of 128 and 6 of 64, five steps: 61 us, the launches of their own take 60 and 19).
 hipError_t whole_run(const Part& p64, const Part& p128, const ou_config* cfg, const Step& st, char* base, hipStream_t stream) {
-  const Scales sc = scales_of(cfg);
+  const AllScales sc = scales_of(cfg);
   const Item* const items[2] = {reinterpret_cast<const Item*>(base + p64.at_items), reinterpret_cast<const Item*>(base + p128.at_items)};
   const int n[2] = {static_cast<int>(p64.items.size()), static_cast<int>(p128.items.size())};
   const int64_t units[2] = {p64.units[kBlocks], p128.units[kBlocks]};

@@ -1,0 +1,72 @@
+"""How exact the orthogonalised update's products are: its results and those of the same formulas in plain fp32, both against fp64.
+
+Tolerance.  An fp32 value enters a product as two fp16 parts, off by at most half a last bit of 22, 2^-23, where fp32 arithmetic takes it as it is; the product of the two second
+parts, at most 2^-22 of the whole, is left out; so a product is off by up to 2^-21, which the rounding of an fp32 product (2^-24) is not by a factor of eight.  The sums are
+fp32 on both sides, and the steps after it carry both errors alike.  So the kernels may be off by eight times what the formulas in fp32 are, both as whole matrices
+(Frobenius norm); an fp32 result that happens to come out better than half a last bit of a step counts as that, 2^-24 of the result a step.  A product with a single part, off by 2^-12, is beyond it by a
+factor of hundreds.
+"""
+import numpy as np
+import pytest
+
+from oracle import orthogonalised_update as oo
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ou():
+    import torch
+    assert torch.cuda.is_available()
+    from paper_2504_10700_amd import ou_binding
+    return ou_binding
+
+
+def in_fp32(U, steps, coefficients, eps):
+    """The formulas in plain fp32 (the norm in fp64, as the library has it)."""
+    a, b, c = (np.float32(v) for v in coefficients)
+    X = (U / (np.sqrt((U ** 2).sum()) + eps)).astype(np.float32)
+    turned = X.shape[0] > X.shape[1]
+    X = X.T if turned else X
+    for _ in range(steps):
+        S = X @ X.T
+        X = a * X + (b * S + c * (S @ S)) @ X
+    return X.T if turned else X
+
+
+def compare(ou, shapes, steps, coefficients, eps=1e-7, make=None, dtype="float32"):
+    """One call on a list of batches [count][rows][cols] of normal numbers, or of make(generator, shape); returns the worst ratio of the errors."""
+    import torch
+    g = np.random.default_rng(11)
+    values = [(make or (lambda rng, s: rng.normal(size=s)))(g, s) for s in shapes]
+    grad = [torch.tensor(v).to(getattr(torch, dtype)).cuda() for v in values]
+    weight = [torch.zeros(s, device="cuda") for s in shapes]                     # rate -1, scale 1: the update itself, in fp32
+    cfg = ou.make_config(rate=-1.0, steps=steps, coefficients=coefficients, eps=eps)
+    tensors = ou.make_tensors(grad, None, weight, None)
+    nbytes = ou.ou_workspace_bytes(cfg, tensors)
+    ws = torch.full((nbytes,), 255, dtype=torch.uint8, device="cuda")
+    ou.ou_step(cfg, tensors, ws, nbytes)
+    torch.cuda.synchronize()
+    worst = 0.0
+    for gr, w in zip(grad, weight):
+        for U, X in zip(gr.double().cpu().numpy(), w.double().cpu().numpy()):
+            want = oo.iterate(U, steps, eps, coefficients)
+            norm = lambda x: np.sqrt((x ** 2).sum())  # noqa: E731
+            plain = max(norm(in_fp32(U, steps, coefficients, eps) - want), steps * 2.0 ** -24 * norm(want))
+            off = norm(X - want)
+            worst = max(worst, off / plain)
+            assert off <= 8 * plain, (U.shape, off / plain, off / norm(want))
+    return worst
+
+
+WAYS = [(2, 64, 64), (1, 33, 50), (2, 128, 128), (1, 100, 70), (1, 64, 1280), (1, 700, 40), (3, 128, 300), (1, 300, 90), (1, 200, 300), (1, 257, 131)]
+GROWING = [((8.28, -23.6, 17.3), 2), ((8.0, -10.0, 4.0), 2), ((30.0, -40.0, 20.0), 1), ((1000.0, -1000.0, 0.0), 1), ((0.0, 4000.0, -4000.0), 1), ((0.0, 200.0, -200.0), 1),
+           ((0.0, 1000.0, 0.0), 1), ((3.0, 0.0, 0.0), 6)]
+
+
+@pytest.mark.parametrize("coefficients,steps", GROWING, ids=str)
+def test_growing_coefficients(ou, coefficients, steps):
+    """Bounds that grow by up to 1024 over the steps: every kernel, each alone and all in one list."""
+    for shapes in [[s] for s in WAYS] + [WAYS]:
+        print(f"update growing {coefficients} {steps} {shapes}", flush=True)
+        print("times the error of fp32:", compare(ou, shapes, steps, coefficients), flush=True)
