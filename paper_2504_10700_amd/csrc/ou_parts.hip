@@ -190,9 +190,10 @@ __device__ __forceinline__ void load_rows(const _Float16* __restrict__ from, con
 
 __device__ __forceinline__ void wave_sync() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
-// Waits until at most N of the wave's requests are under way, then for the workgroup.
+// Waits until at most N of the wave's requests are under way, then for the workgroup.  Behind the barrier a slot is filled again that the waves have read before it: each waits
+// for its reads here (lgkmcnt), since the products that use them are not held before the barrier by anything else.
 template <int N>
-__device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory"); }
 // The stage that is multiplied next has arrived, of the `left` (at most kAhead) after it none has to.
 template <int kAhead, int kLoads>
 __device__ __forceinline__ void stage_arrived(int left) {
