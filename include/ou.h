@@ -18,8 +18,8 @@
  * computed element by element in fp32 (SC_F64: fp64), the norm in fp64, and the products of matrices
  * with the exactness of fp32 ones (SC_F64: fp64); an update of bfloat16 is rounded once, at the end.
  *
- * A matrix of zeros (an element that is absent) stays zero.  Where U has an element that is not finite, the matrix's X is NaN (steps 0: that
- * element is); no other matrix sees it.
+ * A matrix of zeros (an element that is absent) stays zero, for every eps.  Where U has an element that is not finite, the matrix's X is NaN (steps 0, infinite elements: these
+ * are, the others zero); no other matrix sees it.
  *
  * ou_tensor is a HOST array that the call reads before it returns (its contents travel to the device as kernel arguments: no copy, no
  * allocation, usable in a captured graph).  Tensors are dense, row-major, aligned to at least their element, and

@@ -127,11 +127,14 @@ __device__ __forceinline__ double workgroup_sum(double v, double* slots) {
   return s;
 }
 
-// 1 / (|U| + eps) of a matrix whose chunks left their sums of squares in partial[0..n).
+// 1 / (|U| + eps) of a matrix with that sum of squares.  A matrix of zeros stays zero for every eps (below 2^-1024 the quotient is beyond the largest number).
+__device__ __forceinline__ double down_from(double sum, double eps) { return sum == 0 ? 0 : 1.0 / (sqrt(sum) + eps); }
+
+// The same of a matrix whose chunks left their sums of squares in partial[0..n).
 __device__ __forceinline__ double down_of(const double* __restrict__ partial, int64_t n, double eps, double* slots) {
   double sum = 0;
   for (int64_t i = threadIdx.x; i < n; i += kThreads) sum += partial[i];
-  return 1.0 / (sqrt(workgroup_sum(sum, slots)) + eps);
+  return down_from(workgroup_sum(sum, slots), eps);
 }
 
 // The largest |a x + b x^3 + c x^5| of 0 <= x <= top: what the largest singular value can be after a step that began with top.

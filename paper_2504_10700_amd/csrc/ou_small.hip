@@ -376,7 +376,7 @@ __device__ __forceinline__ void whole(const Item* __restrict__ items, int n, int
   }
   double sum = 0;
   each_result<N>([&](int e, int f, int q, int, int) { sum = fma(static_cast<double>(x[e][f][q]), static_cast<double>(x[e][f][q]), sum); });
-  const double down = 1.0 / (sqrt(workgroup_sum(sum, reinterpret_cast<double*>(lds))) + st.eps);
+  const double down = down_from(workgroup_sum(sum, reinterpret_cast<double*>(lds)), st.eps);
   each_result<N>([&](int e, int f, int q, int, int) { x[e][f][q] = static_cast<float>(static_cast<double>(x[e][f][q]) * down); });
   const float ca = static_cast<float>(st.a);
   Scales next = all.step[0];

@@ -70,3 +70,22 @@ def test_growing_coefficients(ou, coefficients, steps):
     for shapes in [[s] for s in WAYS] + [WAYS]:
         print(f"update growing {coefficients} {steps} {shapes}", flush=True)
         print("times the error of fp32:", compare(ou, shapes, steps, coefficients), flush=True)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "float64", "bfloat16"])
+def test_zeros_stay_zero_for_every_eps(ou, dtype):
+    """Also where 1 / eps is beyond the largest number; and a mixed list keeps them apart."""
+    import torch
+    t = getattr(torch, dtype)
+    for shape in ((2, 40, 60), (2, 100, 128), (2, 64, 300), (2, 130, 140)):
+        for steps in (0, 1, 5):
+            grad = torch.zeros(shape, dtype=t, device="cuda")
+            grad[1] = torch.eye(shape[1], shape[2], dtype=t, device="cuda")
+            update = torch.full(shape, float("nan"), dtype=t, device="cuda")
+            cfg = ou.make_config(rate=0.0, steps=steps, eps=5e-324)
+            tensors = ou.make_tensors([grad], None, None, [update])
+            nbytes = ou.ou_workspace_bytes(cfg, tensors)
+            ws = torch.full((nbytes,), 255, dtype=torch.uint8, device="cuda")
+            ou.ou_step(cfg, tensors, ws, nbytes)
+            assert not update[0].any(), (shape, steps)
+            assert torch.isfinite(update[1]).all() and (update[1].diagonal() > 0).all(), (shape, steps)
