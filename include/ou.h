@@ -15,7 +15,7 @@
  * (for a matrix [k_in][k_out] usually sqrt(max(1, k_out / k_in))).
  *
  * Types.  SC_F32: everything fp32; SC_F64: everything fp64; SC_BF16: G and the update bfloat16, M and W fp32.  M, U, W are
- * computed element by element in fp32 (SC_F64: fp64), the norm in fp64, and the products of matrices
+ * computed element by element in fp32 (SC_F64: fp64), the norm in fp64 (of finite elements of any size), and the products of matrices
  * with the exactness of fp32 ones (SC_F64: fp64); an update of bfloat16 is rounded once, at the end.
  *
  * A matrix of zeros (an element that is absent) stays zero, for every eps.  Where U has an element that is not finite, the matrix's X is NaN (steps 0, infinite elements: these

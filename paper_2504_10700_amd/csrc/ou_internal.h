@@ -137,6 +137,36 @@ __device__ __forceinline__ double down_of(const double* __restrict__ partial, in
   return down_from(workgroup_sum(sum, slots), eps);
 }
 
+// fp64: squares of elements beyond 2^480 or below 2^-480 can leave the range of the numbers (or add up to more), so these have sums of their own, of the elements times 2^-600
+// and 2^600.
+struct Squares {
+  double small, middle, large;
+};
+__device__ __forceinline__ void add_square(Squares& s, double u) {
+  const double v = fabs(u);
+  if (v >= 0x1p480) s.large = fma(u * 0x1p-600, u * 0x1p-600, s.large);
+  else if (v < 0x1p-480) s.small = fma(u * 0x1p600, u * 0x1p600, s.small);
+  else s.middle = fma(u, u, s.middle);   // (NaN too)
+}
+// What an element is multiplied with, one factor after the other: together 1 / (|U| + eps).
+struct Down {
+  double first, second;
+};
+__device__ __forceinline__ Down down_of(const Squares* __restrict__ partial, int64_t n, double eps, double* slots) {
+  Squares s{0, 0, 0};
+  for (int64_t i = threadIdx.x; i < n; i += kThreads) {
+    s.small += partial[i].small;
+    s.middle += partial[i].middle;
+    s.large += partial[i].large;
+  }
+  s.small = workgroup_sum(s.small, slots);
+  s.middle = workgroup_sum(s.middle, slots);
+  s.large = workgroup_sum(s.large, slots);
+  if (s.large != 0) return {down_from(s.large + s.middle * 0x1p-600 * 0x1p-600, eps * 0x1p-600), 0x1p-600};
+  if (s.middle != 0) return {down_from(s.middle + s.small * 0x1p-600 * 0x1p-600, eps), 1.0};
+  return {0x1p600, down_from(s.small, eps * 0x1p600)};
+}
+
 // The largest |a x + b x^3 + c x^5| of 0 <= x <= top: what the largest singular value can be after a step that began with top.
 double growth(const ou_config* c, double top);
 

@@ -46,7 +46,7 @@ __global__ __launch_bounds__(kThreads) void momentum_kernel(const Item* __restri
   const int count = static_cast<int>(min(size - first, static_cast<int64_t>(kChunk)));
   const TA mu = static_cast<TA>(st.mu);
   TA* const momentum = it.momentum ? static_cast<TA*>(it.momentum) + at : nullptr;
-  double sum = 0;
+  Squares sum{0, 0, 0};   // (fp32: one sum, of squares that fp64 holds)
   for (int i0 = threadIdx.x; i0 < count; i0 += kAtOnce * kThreads) {
     TA u[kAtOnce], v[kAtOnce];
     gradients(it, at, i0, count, u);
@@ -61,27 +61,37 @@ __global__ __launch_bounds__(kThreads) void momentum_kernel(const Item* __restri
       }
     }
 #pragma unroll
-    for (int k = 0; k < kAtOnce; ++k) sum = fma(static_cast<double>(u[k]), static_cast<double>(u[k]), sum);
+    for (int k = 0; k < kAtOnce; ++k) {
+      if constexpr (sizeof(TA) == 8) add_square(sum, u[k]);
+      else sum.middle = fma(static_cast<double>(u[k]), static_cast<double>(u[k]), sum.middle);
+    }
   }
-  sum = workgroup_sum(sum, slots);
-  if (threadIdx.x == 0) partial[blockIdx.x] = sum;
+  sum.middle = workgroup_sum(sum.middle, slots);
+  if constexpr (sizeof(TA) == 8) {
+    sum.small = workgroup_sum(sum.small, slots);
+    sum.large = workgroup_sum(sum.large, slots);
+    if (threadIdx.x == 0) reinterpret_cast<Squares*>(partial)[blockIdx.x] = sum;
+  } else {
+    if (threadIdx.x == 0) partial[blockIdx.x] = sum.middle;
+  }
 }
 
 // ---- fp64: X = U / (norm + eps), in the tensor's own orientation; last: no steps follow
 
 __global__ __launch_bounds__(kThreads) void normalise_kernel(const Item* __restrict__ items, int n, const Step st, bool last, double* __restrict__ X,
-                                                             const double* __restrict__ partial) {
+                                                             const Squares* __restrict__ partial) {
   __shared__ double slots[kWaves];
   const Item& it = items[item_of(items, n, kChunks, blockIdx.x)];
   const int64_t size = static_cast<int64_t>(it.rows) * it.cols, per = chunks_of(size), unit = blockIdx.x - it.unit[kChunks];
   const int64_t matrix = unit / per, first = unit % per * kChunk;
   const int count = static_cast<int>(min(size - first, static_cast<int64_t>(kChunk)));
-  const double down = down_of(partial + it.unit[kChunks] + matrix * per, per, st.eps, slots);
+  const Down down = down_of(partial + it.unit[kChunks] + matrix * per, per, st.eps, slots);
   for (int i = threadIdx.x; i < count; i += kThreads) {
     const int64_t e = matrix * size + first + i;
     double u = gradient<double>(it, e);
     if (it.momentum) u = direction(u, static_cast<const double*>(it.momentum)[e], st.mu, st.nesterov);
-    if (last) finish(it, st, e, u * down); else X[it.x + e] = u * down;
+    u = u * down.first * down.second;
+    if (last) finish(it, st, e, u); else X[it.x + e] = u;
   }
 }
 
@@ -274,7 +284,7 @@ Layout layout_of(int64_t n, const ou_tensor* tensors, int steps) {
   }
   Room room;
   room(n * sizeof(Item));
-  l.part[kDouble].at_partial = room(l.part[kDouble].units[kChunks] * sizeof(double));
+  l.part[kDouble].at_partial = room(l.part[kDouble].units[kChunks] * sizeof(Squares));
   int64_t chunks = 0;
   for (int way = kParts; way <= kSlices128; ++way) {
     for (Item& it : l.part[way].items) it.unit[kChunks] += chunks;
@@ -385,7 +395,7 @@ hipError_t launch(const Part& p, const Item* items, const Step& st, bool last, c
 hipError_t double_run(const Part& p, const ou_config* cfg, const Step& st, char* base, hipStream_t stream) {
   const int n = static_cast<int>(p.items.size());
   const Item* const items = reinterpret_cast<const Item*>(base + p.at_items);
-  const double* const partial = reinterpret_cast<const double*>(base + p.at_partial);
+  const Squares* const partial = reinterpret_cast<const Squares*>(base + p.at_partial);
   double* const X[2] = {reinterpret_cast<double*>(base + p.at_x), reinterpret_cast<double*>(base + p.at[0])};
   double* const S = reinterpret_cast<double*>(base + p.at[1]);
   double* const P = reinterpret_cast<double*>(base + p.at[2]);

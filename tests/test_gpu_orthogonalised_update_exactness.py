@@ -72,6 +72,36 @@ def test_growing_coefficients(ou, coefficients, steps):
         print("times the error of fp32:", compare(ou, shapes, steps, coefficients), flush=True)
 
 
+@pytest.mark.parametrize("steps", [0, 1, 5])
+@pytest.mark.parametrize("size", [1e-320, 1e-300, 1e-200, 1e-150, 1e-140, 1e100, 1e140, 1e150, 1e200, 1e305])
+def test_fp64_gradients_of_every_size(ou, size, steps):
+    """The squares of such elements are not all numbers, but U / (|U| + eps) is one.  The gradient is a power of two times normal numbers (below the normal numbers: whatever is left of
+    them), so a gradient of ordinary size and an eps that goes with it have the same result but for roundings.  X has norm 1 and is off by four last bits u (2^-52: a root, a sum, a quotient and
+    two products, half a bit each, here and in the oracle); the products of a step by 8 u sqrt(n m) as the other tests of the update have it; a step makes what is before it at most 4 times as
+    large; here and in the oracle, so once more as much: less than 4 u (1 + 8 sqrt(n m) steps) 4^steps."""
+    import torch
+    g = torch.Generator().manual_seed(5)
+    up = 2.0 ** np.floor(np.log2(size))
+    for shape in ((2, 40, 70), (1, 130, 100)):
+        small = torch.randn(shape, generator=g, dtype=torch.float64)
+        grad = (small * up).cuda()
+        reference = grad.cpu().numpy() / up
+        for eps in (up * 2.0 ** -20, up):
+            if eps == 0 or not np.isfinite(eps):
+                continue
+            update = torch.full(shape, float("nan"), dtype=torch.float64, device="cuda")
+            cfg = ou.make_config(rate=0.0, steps=steps, eps=eps)
+            tensors = ou.make_tensors([grad], None, None, [update])
+            nbytes = ou.ou_workspace_bytes(cfg, tensors)
+            ws = torch.full((nbytes,), 255, dtype=torch.uint8, device="cuda")
+            ou.ou_step(cfg, tensors, ws, nbytes)
+            for U, X in zip(reference, update.cpu().numpy()):
+                want = oo.iterate(U, steps, eps / up)
+                m = min(U.shape)
+                allowed = 2.0 ** -50 * (1 + 8 * np.sqrt(max(U.shape) * m) * steps) * 4.0 ** steps
+                assert np.sqrt(((X - want) ** 2).sum()) <= allowed, (size, eps, steps, shape)
+
+
 @pytest.mark.parametrize("dtype", ["float32", "float64", "bfloat16"])
 def test_zeros_stay_zero_for_every_eps(ou, dtype):
     """Also where 1 / eps is beyond the largest number; and a mixed list keeps them apart."""
