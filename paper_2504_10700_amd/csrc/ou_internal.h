@@ -182,7 +182,8 @@ void slice_place(Part& p, Item& it, int64_t count, int64_t matrices, bool large)
 void slice_layout(Part& p, Room& room, int steps, bool large);
 hipError_t slice_run(const Part& p, const ou_config* cfg, const Step& st, bool large, char* base, hipStream_t stream);
 
-// The power of two that brings `top` to at most 2^14 (fp16 parts).
+// The power of two that brings `top` to at most 2^14 (fp16 parts); a bound below kLeastBound counts as that.
+constexpr double kLeastBound = 1e-3;
 int exponent_of(double top);
 
 }  // namespace ou

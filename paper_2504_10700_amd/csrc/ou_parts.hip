@@ -468,7 +468,7 @@ __global__ __launch_bounds__(kThreads, 2) void product_kernel(const Item* __rest
 
 }  // namespace
 
-int exponent_of(double top) { return 14 - static_cast<int>(std::ceil(std::log2(std::max(top, 1e-3)))); }
+int exponent_of(double top) { return 14 - static_cast<int>(std::ceil(std::log2(std::max(top, kLeastBound)))); }
 
 void parts_place(Part& p, Item& it, int64_t count) {
   const int64_t m = std::min(it.rows, it.cols), l = std::max(it.rows, it.cols);

@@ -6,6 +6,7 @@
 #include <cfloat>
 #include <cmath>
 #include <string>
+#include <type_traits>
 
 #include "el_tile.h"
 #include "ou_internal.h"
@@ -76,21 +77,27 @@ __global__ __launch_bounds__(kThreads) void momentum_kernel(const Item* __restri
   }
 }
 
-// ---- fp64: X = U / (norm + eps), in the tensor's own orientation; last: no steps follow
+// ---- fp64, and fp32 where parts do not hold a step (parts_hold): X = U / (norm + eps), in the tensor's own orientation; last: no steps follow
 
-__global__ __launch_bounds__(kThreads) void normalise_kernel(const Item* __restrict__ items, int n, const Step st, bool last, double* __restrict__ X,
-                                                             const Squares* __restrict__ partial) {
+template <typename TA>
+using Sum = std::conditional_t<sizeof(TA) == 8, Squares, double>;   // of a chunk
+
+template <typename TA>
+__global__ __launch_bounds__(kThreads) void normalise_kernel(const Item* __restrict__ items, int n, const Step st, bool last, TA* __restrict__ X,
+                                                             const Sum<TA>* __restrict__ partial) {
   __shared__ double slots[kWaves];
   const Item& it = items[item_of(items, n, kChunks, blockIdx.x)];
   const int64_t size = static_cast<int64_t>(it.rows) * it.cols, per = chunks_of(size), unit = blockIdx.x - it.unit[kChunks];
   const int64_t matrix = unit / per, first = unit % per * kChunk;
   const int count = static_cast<int>(min(size - first, static_cast<int64_t>(kChunk)));
-  const Down down = down_of(partial + it.unit[kChunks] + matrix * per, per, st.eps, slots);
+  const auto down = down_of(partial + it.unit[kChunks] + matrix * per, per, st.eps, slots);
+  const TA mu = static_cast<TA>(st.mu);
   for (int i = threadIdx.x; i < count; i += kThreads) {
     const int64_t e = matrix * size + first + i;
-    double u = gradient<double>(it, e);
-    if (it.momentum) u = direction(u, static_cast<const double*>(it.momentum)[e], st.mu, st.nesterov);
-    u = u * down.first * down.second;
+    TA u = gradient<TA>(it, e);
+    if (it.momentum) u = direction(u, static_cast<const TA*>(it.momentum)[e], mu, st.nesterov);
+    if constexpr (sizeof(TA) == 8) u = u * down.first * down.second;
+    else u = static_cast<TA>(static_cast<double>(u) * down);
     if (last) finish(it, st, e, u); else X[it.x + e] = u;
   }
 }
@@ -140,8 +147,12 @@ __device__ __forceinline__ void product(const View<TA>& p, const View<TA>& q, in
       else to[thread / kTile + e * (kThreads / kTile)][thread % kTile] = x[e];
     }
   };
+  // (an fp32 instruction cuts off what is below the last bit of the sum it adds to, so a sum goes no further than kFlush indices and then joins another)
+  constexpr bool kJoin = sizeof(TA) == 4;
+  constexpr int kFlush = 128;
+  typename S::Sums joined;
 #pragma unroll
-  for (int t = 0; t < S::kColumns; ++t) acc[t] = typename Mma<TA>::acc_t{0, 0, 0, 0};
+  for (int t = 0; t < S::kColumns; ++t) acc[t] = joined[t] = typename Mma<TA>::acc_t{0, 0, 0, 0};
   TA x[4], y[4];   // a stage's indices, requested while those before are multiplied
   load(p, i0, 0, x);
   load(q, j0, 0, y);
@@ -160,6 +171,17 @@ __device__ __forceinline__ void product(const View<TA>& p, const View<TA>& q, in
 #pragma unroll
       for (int t = 0; t < S::kColumns; ++t) acc[t] = Mma<TA>::mma(a, qs[4 * s + lane / 16][col0 + 16 * t + (lane & 15)], acc[t]);
     }
+    if (kJoin && (k + kDepth) % kFlush == 0) {
+#pragma unroll
+      for (int t = 0; t < S::kColumns; ++t) {
+        joined[t] += acc[t];
+        acc[t] = typename Mma<TA>::acc_t{0, 0, 0, 0};
+      }
+    }
+  }
+  if (kJoin) {
+#pragma unroll
+    for (int t = 0; t < S::kColumns; ++t) acc[t] += joined[t];
   }
 }
 
@@ -216,8 +238,9 @@ __global__ __launch_bounds__(kThreads) void product_kernel(const Item* __restric
 
 // ---- host side
 
-// The ways: fp64; products in tiles; and matrices whose shorter side is at most 64 or 128, in slices or whole.  The three from kParts on have the first pass together.
-enum Way { kDouble, kParts, kSlices64, kSlices128, kWhole64, kWhole128, kWays };
+// The ways: fp64; fp32 on fp32 instructions; products in tiles of parts; and matrices whose shorter side is at most 64 or 128, in slices or whole.  The four from kPlain on have the
+// first pass together.
+enum Way { kDouble, kPlain, kParts, kSlices64, kSlices128, kWhole64, kWhole128, kWays };
 bool whole(int way) { return way == kWhole64 || way == kWhole128; }
 bool sliced(int way) { return way == kSlices64 || way == kSlices128; }
 bool large(int way) { return way == kWhole128 || way == kSlices128; }
@@ -229,13 +252,27 @@ struct Layout {
   size_t bytes = 0;
 };
 
-// One workgroup holds what it can: one launch, or one a step, instead of three a step.
-Way way_of(const ou_tensor& t) {
-  const int m = std::min(t.rows, t.cols), l = std::max(t.rows, t.cols);
-  return t.dtype == SC_F64 ? kDouble : l <= 64 ? kWhole64 : l <= 128 ? kWhole128 : m <= 64 ? kSlices64 : m <= 128 ? kSlices128 : kParts;
+// Whether parts hold the steps as fp32 does.  A part of S, or of P = b S + c S S, is off by up to 2^-38 of what the bound `top` of the singular values allows, |b| top^2 + |c| top^4, however
+// small the matrix's own values have become; a X stands beside P X.  So relative to X a step is off by sqrt(m) 2^-38 (|b| top^2 + |c| top^4) / |a|, for m of up to 65536 and a ratio
+// of 64 by 2^-24.  The usual coefficients have 3.2; with a = 0 the values are cubed and nothing holds the small ones (three steps of X S: 64 x 64 off by 100%).
+constexpr double kMostBeside = 64;
+bool parts_hold(const ou_config* c) {
+  double top = 1;
+  for (int i = 0; i < c->steps; ++i) {
+    const double square = std::max(top * top, kLeastBound);
+    if (std::fabs(c->b) * square + std::fabs(c->c) * std::max(square * square, kLeastBound) > kMostBeside * std::fabs(c->a)) return false;
+    top = growth(c, top);
+  }
+  return true;
 }
 
-void double_place(Part& p, Item& it, int64_t count) {
+// One workgroup holds what it can: one launch, or one a step, instead of three a step.
+Way way_of(const ou_tensor& t, bool parts) {
+  const int m = std::min(t.rows, t.cols), l = std::max(t.rows, t.cols);
+  return t.dtype == SC_F64 ? kDouble : !parts ? kPlain : l <= 64 ? kWhole64 : l <= 128 ? kWhole128 : m <= 64 ? kSlices64 : m <= 128 ? kSlices128 : kParts;
+}
+
+void square_place(Part& p, Item& it, int64_t count) {
   const int64_t m = std::min(it.rows, it.cols), l = std::max(it.rows, it.cols);
   it.x = p.x;
   it.s = p.s;
@@ -248,22 +285,24 @@ void double_place(Part& p, Item& it, int64_t count) {
   p.s += count * m * m;
 }
 
-void double_layout(Part& p, Room& room, int steps) {
+void square_layout(Part& p, Room& room, int steps, size_t size) {
   if (steps == 0) return;
-  p.at_x = room(p.x * sizeof(double));
-  p.at[0] = room(p.x * sizeof(double));
-  p.at[1] = room(p.s * sizeof(double));
-  p.at[2] = room(p.s * sizeof(double));
+  p.at_x = room(p.x * size);
+  p.at[0] = room(p.x * size);
+  p.at[1] = room(p.s * size);
+  p.at[2] = room(p.s * size);
 }
 
-Layout layout_of(int64_t n, const ou_tensor* tensors, int steps) {
+Layout layout_of(const ou_config* cfg, int64_t n, const ou_tensor* tensors) {
   Layout l;
+  const int steps = cfg->steps;
+  const bool parts = parts_hold(cfg);
   int64_t matrices[kWays] = {};
-  for (int64_t i = 0; i < n; ++i) matrices[way_of(tensors[i])] += tensors[i].count;
+  for (int64_t i = 0; i < n; ++i) matrices[way_of(tensors[i], parts)] += tensors[i].count;
   for (int64_t i = 0; i < n; ++i) {
     const ou_tensor& t = tensors[i];
     if (t.count == 0) continue;
-    const Way way = way_of(t);
+    const Way way = way_of(t, parts);
     Part& p = l.part[way];
     Item it{};
     it.grad = t.grad;
@@ -276,7 +315,7 @@ Layout layout_of(int64_t n, const ou_tensor* tensors, int steps) {
     it.cols = t.cols;
     it.dtype = t.dtype;
     if (!whole(way)) p.units[kChunks] += t.count * ceil_div(static_cast<int64_t>(t.rows) * t.cols, kChunk);
-    if (way == kDouble) double_place(p, it, t.count);
+    if (way <= kPlain) square_place(p, it, t.count);
     else if (way == kParts) parts_place(p, it, t.count);
     else if (sliced(way)) slice_place(p, it, t.count, matrices[way], large(way));
     else p.units[kBlocks] += t.count;
@@ -286,7 +325,7 @@ Layout layout_of(int64_t n, const ou_tensor* tensors, int steps) {
   room(n * sizeof(Item));
   l.part[kDouble].at_partial = room(l.part[kDouble].units[kChunks] * sizeof(Squares));
   int64_t chunks = 0;
-  for (int way = kParts; way <= kSlices128; ++way) {
+  for (int way = kPlain; way <= kSlices128; ++way) {
     for (Item& it : l.part[way].items) it.unit[kChunks] += chunks;
     chunks += l.part[way].units[kChunks];
   }
@@ -297,7 +336,7 @@ Layout layout_of(int64_t n, const ou_tensor* tensors, int steps) {
     l.items.insert(l.items.end(), p.items.begin(), p.items.end());
     if (way != kDouble) p.at_partial = at_partial;
     if (p.items.empty()) continue;
-    if (way == kDouble) double_layout(p, room, steps);
+    if (way <= kPlain) square_layout(p, room, steps, way == kDouble ? sizeof(double) : sizeof(float));
     else if (way == kParts) parts_layout(p, room, steps);
     else if (sliced(way)) slice_layout(p, room, steps, large(way));
   }
@@ -380,34 +419,35 @@ hipError_t first_pass(const Layout& l, int way, int end, const Step& st, char* b
 }
 
 // Tiles of 64 that do not fill the compute units: smaller ones (five steps of one 512 x 700 295 us instead of 716, of 40 512 x 512 4.1 ms instead of 3.6).
-template <int kPhase>
-hipError_t launch(const Part& p, const Item* items, const Step& st, bool last, const double* X, double* next, double* S, double* P, hipStream_t stream) {
+template <typename TA, int kPhase>
+hipError_t launch(const Part& p, const Item* items, const Step& st, bool last, const TA* X, TA* next, TA* S, TA* P, hipStream_t stream) {
   const int n = static_cast<int>(p.items.size());
   const int64_t tiles = p.units[kPhase == kX ? kProduct : kGram];
   if (tiles > 256)
-    hipLaunchKernelGGL((product_kernel<double, kPhase, 64>), dim3(static_cast<unsigned>(tiles)), dim3(kThreads), 0, stream, items, n, st, last, X, next, S, P);
+    hipLaunchKernelGGL((product_kernel<TA, kPhase, 64>), dim3(static_cast<unsigned>(tiles)), dim3(kThreads), 0, stream, items, n, st, last, X, next, S, P);
   else
-    hipLaunchKernelGGL((product_kernel<double, kPhase, 32>), dim3(static_cast<unsigned>(p.units[kPhase == kX ? kProductSmall : kGramSmall])), dim3(kThreads), 0, stream,
+    hipLaunchKernelGGL((product_kernel<TA, kPhase, 32>), dim3(static_cast<unsigned>(p.units[kPhase == kX ? kProductSmall : kGramSmall])), dim3(kThreads), 0, stream,
                        items, n, st, last, X, next, S, P);
   return hipGetLastError();
 }
 
-hipError_t double_run(const Part& p, const ou_config* cfg, const Step& st, char* base, hipStream_t stream) {
+template <typename TA>
+hipError_t square_run(const Part& p, const ou_config* cfg, const Step& st, char* base, hipStream_t stream) {
   const int n = static_cast<int>(p.items.size());
   const Item* const items = reinterpret_cast<const Item*>(base + p.at_items);
-  const Squares* const partial = reinterpret_cast<const Squares*>(base + p.at_partial);
-  double* const X[2] = {reinterpret_cast<double*>(base + p.at_x), reinterpret_cast<double*>(base + p.at[0])};
-  double* const S = reinterpret_cast<double*>(base + p.at[1]);
-  double* const P = reinterpret_cast<double*>(base + p.at[2]);
-  hipLaunchKernelGGL(normalise_kernel, dim3(static_cast<unsigned>(p.units[kChunks])), dim3(kThreads), 0, stream, items, n, st, cfg->steps == 0, X[0], partial);
+  const Sum<TA>* const partial = reinterpret_cast<const Sum<TA>*>(base + p.at_partial);
+  TA* const X[2] = {reinterpret_cast<TA*>(base + p.at_x), reinterpret_cast<TA*>(base + p.at[0])};
+  TA* const S = reinterpret_cast<TA*>(base + p.at[1]);
+  TA* const P = reinterpret_cast<TA*>(base + p.at[2]);
+  hipLaunchKernelGGL(normalise_kernel<TA>, dim3(static_cast<unsigned>(p.units[kChunks])), dim3(kThreads), 0, stream, items, n, st, cfg->steps == 0, X[0], partial);
   hipError_t e = hipGetLastError();
   for (int i = 0; i < cfg->steps && e == hipSuccess; ++i) {
     const bool last = i + 1 == cfg->steps;
-    const double* const x = X[i & 1];
-    double* const next = X[(i + 1) & 1];
-    e = launch<kS>(p, items, st, last, x, next, S, P, stream);
-    if (e == hipSuccess) e = launch<kP>(p, items, st, last, x, next, S, P, stream);
-    if (e == hipSuccess) e = launch<kX>(p, items, st, last, x, next, S, P, stream);
+    const TA* const x = X[i & 1];
+    TA* const next = X[(i + 1) & 1];
+    e = launch<TA, kS>(p, items, st, last, x, next, S, P, stream);
+    if (e == hipSuccess) e = launch<TA, kP>(p, items, st, last, x, next, S, P, stream);
+    if (e == hipSuccess) e = launch<TA, kX>(p, items, st, last, x, next, S, P, stream);
   }
   return e;
 }
@@ -440,7 +480,7 @@ sc_status ou_workspace_bytes(const ou_config* cfg, int64_t n_tensors, const ou_t
   if (st != SC_OK) return st;
   if (!bytes) return set_error(SC_ERR_INVALID_ARG, "ou_workspace_bytes: bytes is NULL");
   try {
-    *bytes = layout_of(n_tensors, tensors, cfg->steps).bytes;
+    *bytes = layout_of(cfg, n_tensors, tensors).bytes;
   } catch (const std::bad_alloc&) {
     return set_error(SC_ERR_ALLOC, "ou_workspace_bytes: out of host memory");
   }
@@ -453,7 +493,7 @@ sc_status ou_step(const ou_config* cfg, int64_t n_tensors, const ou_tensor* tens
   const sc_status st = check("ou_step", cfg, n_tensors, tensors);
   if (st != SC_OK) return st;
   try {
-    const Layout l = layout_of(n_tensors, tensors, cfg->steps);
+    const Layout l = layout_of(cfg, n_tensors, tensors);
     if (l.items.empty()) return SC_OK;
     if (!workspace || workspace_bytes < l.bytes)
       return set_error(SC_ERR_WORKSPACE, "ou_step: workspace missing or smaller than ou_workspace_bytes()");
@@ -465,12 +505,15 @@ sc_status ou_step(const ou_config* cfg, int64_t n_tensors, const ou_tensor* tens
     char* const base = static_cast<char*>(workspace);
     hipError_t e = send(l.items, base, stream);
     if (e == hipSuccess) e = first_pass<double>(l, kDouble, kDouble, step, base, stream);
-    if (e == hipSuccess) e = first_pass<float>(l, kParts, kSlices128, step, base, stream);
+    if (e == hipSuccess) e = first_pass<float>(l, kPlain, kSlices128, step, base, stream);
     if (e == hipSuccess) e = whole_run(l.part[kWhole64], l.part[kWhole128], cfg, step, base, stream);
     for (int way = kDouble; way <= kSlices128 && e == hipSuccess; ++way) {
       const Part& p = l.part[way];
       if (p.items.empty()) continue;
-      e = way == kDouble ? double_run(p, cfg, step, base, stream) : way == kParts ? parts_run(p, cfg, step, base, stream) : slice_run(p, cfg, step, large(way), base, stream);
+      e = way == kDouble  ? square_run<double>(p, cfg, step, base, stream)
+          : way == kPlain ? square_run<float>(p, cfg, step, base, stream)
+          : way == kParts ? parts_run(p, cfg, step, base, stream)
+                          : slice_run(p, cfg, step, large(way), base, stream);
     }
     if (e != hipSuccess) return set_error(SC_ERR_HIP, std::string("ou_step: kernel launch: ") + hipGetErrorString(e));
   } catch (const std::bad_alloc&) {

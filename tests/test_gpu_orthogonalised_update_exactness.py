@@ -119,3 +119,60 @@ def test_zeros_stay_zero_for_every_eps(ou, dtype):
             ou.ou_step(cfg, tensors, ws, nbytes)
             assert not update[0].any(), (shape, steps)
             assert torch.isfinite(update[1]).all() and (update[1].diagonal() > 0).all(), (shape, steps)
+
+
+SMALL_LINEAR = [((0.0, 1.0, 0.0), 3), ((0.0, 0.1, 0.0), 3), ((0.001, 1.0, 0.0), 5), ((0.0, 2.0, -1.0), 2), ((0.0, 0.0, 1.0), 2)]
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("coefficients,steps", SMALL_LINEAR, ids=str)
+def test_coefficients_without_a_linear_term(ou, coefficients, steps, dtype):
+    """Singular values become cubes of small numbers, far below the bound of the largest there can be."""
+    for shapes in [[s] for s in WAYS] + [WAYS]:
+        print(f"update without a linear term {coefficients} {steps} {dtype} {shapes}", flush=True)
+        print("times the error of fp32:", compare(ou, shapes, steps, coefficients, dtype=dtype), flush=True)
+
+
+@pytest.mark.parametrize("coefficients,steps", [((0.05, 1.5, 1.0), 2), ((0.05, 1.5, 1.0), 3), ((0.03, 1.5, 1.0), 2), ((1.0, 30.0, -30.0), 1), ((1.0, 34.0, -34.0), 1), ((0.1, -0.1, 0.1), 9), ((0.01, 0.01, 0.0), 4)], ids=str)
+def test_coefficients_about_the_limit_of_the_parts(ou, coefficients, steps):
+    """On both sides of the ratio to which parts serve, and bounds that shrink.  (With the second, 2.55 becomes 133 and then more than OU_MAX_GROWTH: refused.)"""
+    if (coefficients, steps) == ((0.05, 1.5, 1.0), 3):
+        with pytest.raises(ou.ScError):
+            compare(ou, WAYS, steps, coefficients)
+        return
+    for scale in (1.0, 1e-9):     # the second far below eps
+        make = lambda rng, s: rng.normal(size=s) * scale  # noqa: E731
+        for shapes in [[s] for s in WAYS] + [WAYS]:
+            print(f"update about the limit {coefficients} {steps} {scale} {shapes}", flush=True)
+            print("times the error of fp32:", compare(ou, shapes, steps, coefficients, make=make), flush=True)
+
+
+def test_options_on_fp32_instructions(ou):
+    """Momentum, weights, what is left out and addresses at any element there too."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(9)
+    coefficients = (0.0, 2.0, -1.0)
+    for skew in (0, 1):
+        for nesterov in (True, False):
+            new = lambda s, t=torch.float32: torch.randn(int(np.prod(s)) + skew, generator=g, device="cuda").to(t)[skew:].view(s)  # noqa: E731
+            shapes = [(2, 64, 64), (1, 130, 260), (3, 90, 20), (0, 7, 7)]
+            types = [torch.float32, torch.bfloat16, torch.float32, torch.bfloat16]
+            grad, momentum, weight, update = [new(s, t) for s, t in zip(shapes, types)], [new(s) for s in shapes], [new(s) for s in shapes], [new(s, t) for s, t in zip(shapes, types)]
+            f64 = lambda x: x.double().cpu().numpy()  # noqa: E731
+            before = [tuple(f64(x[i]) for x in (grad, momentum, weight)) for i in range(3)]
+            cfg = ou.make_config(rate=0.5, decay=0.1, steps=2, coefficients=coefficients, nesterov=nesterov)
+            tensors = ou.make_tensors(grad, momentum, weight, update, scale=[1.0, 2.0, 3.0, 4.0])
+            nbytes = ou.ou_workspace_bytes(cfg, tensors)
+            ws = torch.full((nbytes,), 255, dtype=torch.uint8, device="cuda")
+            ou.ou_step(cfg, tensors, ws, nbytes)
+            for i, (G, M, W) in enumerate(before):
+                wM, wX, wW = oo.step(G, M, W, nesterov=nesterov, steps=2, rate=0.5, decay=0.1, scale=1.0 + i, coefficients=coefficients, form=oo.iterate)
+                assert (np.abs(f64(momentum[i]) - wM) <= 2 * 2.0 ** -23 * (np.abs(0.95 * M) + np.abs(G))).all(), i
+                U = G + 0.95 * wM if nesterov else wM
+                for k in range(G.shape[0]):
+                    norm = lambda x: np.sqrt((x ** 2).sum())  # noqa: E731
+                    # U is rounded three times (2^-23 each, of terms no larger than |G| + |M|), which two steps make 25 times as much (cubes: three times a step, and a third for X itself)
+                    plain = norm(in_fp32(U[k], 2, coefficients, 1e-7) - wX[k]) + 2.0 ** -23 * norm(wX[k])
+                    allowed = 8 * plain + 25 * 3 * 2.0 ** -23 * norm(wX[k]) * norm(np.abs(G[k]) + np.abs(M[k])) / norm(U[k])
+                    assert norm(f64(update[i])[k] - wX[k]) <= allowed + (2.0 ** -8 * norm(wX[k]) if types[i] == torch.bfloat16 else 0), (i, k)
+                    assert norm(f64(weight[i])[k] - wW[k]) <= 0.5 * (1 + i) * allowed + 4 * 2.0 ** -23 * norm(W[k]), (i, k)
