@@ -15,8 +15,10 @@
  * (for a matrix [k_in][k_out] usually sqrt(max(1, k_out / k_in))).
  *
  * Types.  SC_F32: everything fp32; SC_F64: everything fp64; SC_BF16: G and the update bfloat16, M and W fp32.  M, U, W are
- * computed element by element in fp32 (SC_F64: fp64), the norm in fp64 (of finite elements of any size), and the products of matrices
- * with the exactness of fp32 ones (SC_F64: fp64); an update of bfloat16 is rounded once, at the end.
+ * computed element by element in fp32 (SC_F64: fp64), the norm in fp64 (of finite elements of any size); an update of bfloat16 is rounded once, at the end.
+ * The products of matrices are, seen over a whole matrix (the norm of the error), as exact as fp32 ones (SC_F64: fp64).  Their operands have 22 bits relative to the largest singular value
+ * there can be after the step, and fewer below 2^-16 of it: rows or columns far smaller than the others are relatively less exact (1e-4 of them as in fp32, 1e-6 to 6e-5, 1e-8 to 6e-3 of their size).
+ * Coefficients that need more (|b| t^2 + |c| t^4 > 64 |a| in a step, t the largest singular value there can be before it) take fp32 instructions.
  *
  * A matrix of zeros (an element that is absent) stays zero, for every eps.  Where U has an element that is not finite, the matrix's X is NaN (steps 0, infinite elements: these
  * are, the others zero); no other matrix sees it.

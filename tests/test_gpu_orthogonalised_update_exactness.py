@@ -176,3 +176,58 @@ def test_options_on_fp32_instructions(ou):
                     allowed = 8 * plain + 25 * 3 * 2.0 ** -23 * norm(wX[k]) * norm(np.abs(G[k]) + np.abs(M[k])) / norm(U[k])
                     assert norm(f64(update[i])[k] - wX[k]) <= allowed + (2.0 ** -8 * norm(wX[k]) if types[i] == torch.bfloat16 else 0), (i, k)
                     assert norm(f64(weight[i])[k] - wW[k]) <= 0.5 * (1 + i) * allowed + 4 * 2.0 ** -23 * norm(W[k]), (i, k)
+
+
+LARGER = [(1, 513, 1030), (1, 700, 700), (1, 1030, 257), (1, 64, 8192), (1, 128, 20_000), (1, 260, 9000)]
+HELD = [((3.4445, -4.7750, 2.0315), 1), ((3.4445, -4.7750, 2.0315), 5), ((0.1, 4.0, -3.0), 1), ((0.1, 2.0, 1.0), 2), ((1.5, -0.5, 0.0), 8), ((2.0, -1.5, 0.5), 4)]
+
+
+def decaying(rng, s):
+    """Singular values from 1 down to 1e-6."""
+    count, rows, cols = s
+    m = min(rows, cols)
+    q = lambda n: np.linalg.qr(rng.normal(size=(n, m)))[0]  # noqa: E731
+    return np.stack([(q(rows) * np.logspace(0, -6, m)) @ q(cols).T for _ in range(count)])
+
+
+def one_direction(rng, s):
+    """Nearly of rank one: a large S off the diagonal, sums of one sign."""
+    count, rows, cols = s
+    return rng.uniform(0.5, 1.5, (count, rows, 1)) * rng.uniform(0.5, 1.5, (count, 1, cols)) + 1e-3 * rng.normal(size=s)
+
+
+@pytest.mark.parametrize("make", [None, decaying, one_direction], ids=["normal", "decaying", "one_direction"])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("coefficients,steps", HELD, ids=str)
+def test_products_as_exact_as_in_fp32(ou, coefficients, steps, dtype, make):
+    """The usual coefficients, and ones that leave most of a result to the products: a part that is lost on the way shows here."""
+    for shapes in [[s] for s in WAYS + (LARGER if make is None else [])] + [WAYS]:
+        print(f"update exactness {coefficients} {steps} {dtype} {shapes}", flush=True)
+        print("times the error of fp32:", compare(ou, shapes, steps, coefficients, make=make, dtype=dtype), flush=True)
+
+
+@pytest.mark.parametrize("shape", [(1, 64, 64), (1, 128, 100), (1, 100, 600), (1, 256, 384)], ids=lambda s: "x".join(map(str, s)))
+def test_rows_far_smaller_than_the_others(ou, shape):
+    """A row i of a step's result is a X_i + P_i X.  Elements of P are off by up to 2^-38 (|b| + |c| 1.2^2) 1.2^2, 1.2 the largest a singular value can be, and twice that as S is too; so a small row
+    by as much times sqrt(m) |X| beside eight times what fp32 does to it; what is off before a step is at most 4 times as much after it."""
+    import torch
+    a, b, c = oo.COEFFICIENTS
+    steps, m = 5, min(shape[1:])
+    for size in (1e-4, 1e-6, 1e-8):
+        U = np.random.default_rng(2).normal(size=shape)
+        U[0, 1::7] *= size
+        grad = torch.tensor(U).float().cuda()
+        update = torch.zeros(shape, device="cuda")
+        cfg = ou.make_config(rate=0.0, steps=steps)
+        tensors = ou.make_tensors([grad], None, None, [update])
+        nbytes = ou.ou_workspace_bytes(cfg, tensors)
+        ws = torch.full((nbytes,), 255, dtype=torch.uint8, device="cuda")
+        ou.ou_step(cfg, tensors, ws, nbytes)
+        U = grad[0].double().cpu().numpy()
+        want, plain = oo.iterate(U, steps), in_fp32(U, steps, oo.COEFFICIENTS, 1e-7)
+        norm = lambda x: np.sqrt((x[1::7] ** 2).sum(1))  # noqa: E731
+        off, there = norm(update[0].double().cpu().numpy() - want), norm(want)
+        worst = np.maximum(norm(plain - want).max(), steps * 2.0 ** -24 * there.max())
+        beside = 2.0 ** -38 * 3 * (abs(b) + abs(c) * 1.44) * 1.44 * np.sqrt(m) * 1.2 * sum(4.0 ** k for k in range(steps))
+        print(f"rows of {size}: relative {(off / there).max():.2e}, in fp32 {(norm(plain - want) / there).max():.2e}", flush=True)
+        assert (off <= 8 * worst + beside).all(), (size, off.max(), worst, beside)
