@@ -1,6 +1,6 @@
-// The rows of the products by element for batches without a grouping (GP_UNGROUPED atoms at most): the time is that of reading the weights once.
-// 64 atoms, 89 elements, 128 x 128: 5.0 us forward, 5.5 dX, all launch and latency, where 65 atoms in tiles take 9.6 and 9.0 and 4.6 for the grouping; 64 atoms, one
-// element, 512 x 512: 19 and 13 us, in tiles 25 and 22.  (8 elements, 1024 x 1024, bfloat16: 62 and 39, in tiles 35 and 29; in fp32 51 and 28, 46 and 41.)
+// The rows of the products by element for batches without a grouping (GP_UNGROUPED atoms at most) whose weights are read once or a few times; with more rows or wider ones
+// the call takes the tiles (gp_products.hip has the rule).  64 atoms, 89 elements, 128 x 128: 4.7 us forward, 5.3 dX, all launch and latency, where the tiles with their grouping take 14; 64 atoms,
+// one element, 512 x 512: 18 and 12 us, in tiles 25 and 23; 16 atoms, 1024 x 1024: 17 and 12 of bfloat16, in tiles 40 and 33.
 //
 // The rows of one element are taken four at a time: a workgroup's row finds, from the indices of the whole batch (a lane an atom), its rank among the rows of
 // its element; those whose rank is a multiple of four compute it and the three after it.  Forward: 32 columns a workgroup, 64 groups of eight threads along the

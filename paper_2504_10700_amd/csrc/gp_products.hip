@@ -6,6 +6,7 @@
 // partial matrices that a second launch adds in order.  fp64, 60 000 rows, 128 x 128: Y and dX 65 us each, where the products at the rate of a large one are 31 and the
 // memory 26, dW 124; the loads of a stage are waited for.
 #include <algorithm>
+#include <cmath>
 #include <initializer_list>
 #include <string>
 
@@ -106,15 +107,60 @@ int chunk_rows(const gp_config* c, int64_t n) {
   const int64_t wanted = std::max<int64_t>(1, 384 / tiles);
   return static_cast<int>(std::min<int64_t>(std::max<int64_t>(128, ceil_div(ceil_div(rows, wanted), kBlock) * kBlock), int64_t(1) << 30));
 }
+
+// Batches without a grouping.  Their own kernels read an element's weights once for every four rows of it (dW: take its rows one after the other), which is best for few rows; for more the call
+// makes a grouping itself, a launch of 5 us, and takes the tiles.  What decides is an estimate of both sides' time in us, from both measured at 600 sizes (1 to 64 atoms, 1 to 64 components, 1 to
+// 89 elements, 33 x 65 to 2048 x 1024).  E.g. own kernels and tiles, 64 atoms: fp32, 89 elements, 128 x 128: Y 4.7 and 14, dX 5.3 and 14; bfloat16, 8 elements, 1024 x 1024: Y 63 and 40, dX 39 and 33;
+// fp32, 64 components, one element, 128 x 128: Y 200 and 15, dW 218 and 24.
+struct FewCosts {
+  struct Side {
+    double weight;   // own kernel: an element of the matrices that are there
+    double again;    // the same for each row that makes it be read again
+    double group;    // a workgroup
+    double stage;    // tiles: a reduced index
+    double crowd;    // the same for each tile a compute unit
+  } side[2];         // Y, dX
+  struct {
+    double row, work;                                // own kernel: a row of an element; a product
+    double first, tile_row, partial, tile_work;      // tiles: the launches, a row of a chunk, an element of a partial matrix, a product,
+    double write;                                    // what an element of dW takes more
+  } outer;
+};
+constexpr FewCosts kFewF32{{{6.5e-7, 3.3e-7, 0.0069, 0.036, 0.020}, {3.0e-7, 2.0e-7, 0.0041, 0.030, 0.022}}, {0.041, 2.1e-8, 12, 0.071, 7.3e-6, 0.9e-8, 3.1e-7}};
+constexpr FewCosts kFewBf16{{{7.8e-7, 6.5e-7, 0.0061, 0.027, 0.008}, {5.7e-7, 4.6e-7, 0.0042, 0.020, 0.011}}, {0.068, 2.4e-8, 11, 0.038, 7.3e-6, 0.2e-8, 1.9e-7}};
+constexpr FewCosts kFewF64{{{11e-7, 5.3e-7, 0.0048, 0.064, 0.033}, {9.4e-7, 3.3e-7, 0.0140, 0.055, 0.040}}, {0.062, 3.1e-8, 9, 0.084, 0, 10.8e-8, 2.0e-7}};
+const FewCosts& few_costs(const gp_config* c) { return c->dtype == SC_F32 ? kFewF32 : c->dtype == SC_F64 ? kFewF64 : kFewBf16; }
+
+bool rows_of_few(const gp_config* c, int64_t n, bool back) {
+  if (n > GP_UNGROUPED) return false;
+  const FewCosts::Side& f = few_costs(c).side[back];
+  const int reduced = back ? c->k_out : c->k_in, columns = back ? c->k_in : c->k_out;
+  const double rows = static_cast<double>(n) * c->components, present = static_cast<double>(std::min<int64_t>(c->num_elements, n));   // (at most)
+  const double size = static_cast<double>(reduced) * columns, tiles = (rows / kBlock + present) * ceil_div(columns, 128);
+  const double own = 4.5 + f.weight * present * size + f.again * std::max(0.0, rows - 4 * present) * size + f.group * rows * ceil_div(columns, 32);
+  return own <= 9.3 + (f.stage + f.crowd * tiles / 256) * reduced;
+}
+
+bool outer_of_few(const gp_config* c, int64_t n) {
+  if (n > GP_UNGROUPED) return false;
+  const auto& f = few_costs(c).outer;
+  const double rows = static_cast<double>(n) * c->components, present = static_cast<double>(std::min<int64_t>(c->num_elements, n)), size = static_cast<double>(c->k_in) * c->k_out;
+  const double each = rows / present, per = chunk_rows(c, n), partial = each > per ? std::ceil(each / per) * present : 0;
+  return 5 + f.row * each + f.work * rows * size <=
+         f.first + f.tile_row * std::min(per, each) + f.partial * partial * size + f.tile_work * rows * size + f.write * c->num_elements * size;
+}
+
 // Chunks of the elements that have several, at most.
 int64_t slots_of(const gp_config* c, int64_t n) {
   const int64_t rows = n * c->components, per = chunk_rows(c, n);
-  return n <= GP_UNGROUPED || rows <= per ? 0 : 2 * ceil_div(rows, per);
+  return outer_of_few(c, n) || rows <= per ? 0 : 2 * ceil_div(rows, per);
 }
 size_t element_size(const gp_config* c) { return c->dtype == SC_F64 ? 8 : c->dtype == SC_F32 ? 4 : 2; }
 size_t weight_size(const gp_config* c) { return c->dtype == SC_F64 ? 8 : 4; }
+// The workspace: a grouping for batches that come without one (a workspace for a large batch has room for it too, so that it serves small ones), partial matrices.
+size_t own_grouping_bytes(const gp_config* c) { return offsets_bytes(c->num_elements) + order_bytes(GP_UNGROUPED); }
 size_t workspace_bytes(const gp_config* c, int64_t n) {
-  return align_up(std::max<size_t>(256, static_cast<size_t>(slots_of(c, n)) * c->k_in * c->k_out * weight_size(c)), 256);
+  return own_grouping_bytes(c) + align_up(static_cast<size_t>(slots_of(c, n)) * c->k_in * c->k_out * weight_size(c), 256);
 }
 
 sc_status check_config(const char* fn, const gp_config* cfg, int64_t n) {
@@ -167,8 +213,16 @@ sc_status launched(const char* fn, hipError_t e) {
 
 int64_t ld_in_of(const gp_config* c) { return c->ld_in ? c->ld_in : static_cast<int64_t>(c->components) * c->k_in; }
 int64_t ld_out_of(const gp_config* c) { return c->ld_out ? c->ld_out : static_cast<int64_t>(c->components) * c->k_out; }
-Grouping grouping_for(const gp_config* c, int64_t n, const void* grouping) {
-  return n <= GP_UNGROUPED ? Grouping{nullptr, nullptr} : grouping_of(grouping, c->num_elements);
+// The grouping that a call reads: the caller's, one that it makes itself, none.
+hipError_t grouping_for(const gp_config* c, int64_t n, const int32_t* z, const void* grouping, bool few, void* workspace, hipStream_t stream, Grouping* group) {
+  *group = Grouping{nullptr, nullptr};
+  if (n > GP_UNGROUPED) {
+    *group = grouping_of(grouping, c->num_elements);
+  } else if (!few) {
+    *group = grouping_of(workspace, c->num_elements);
+    return launch_group(c, n, z, workspace, stream);
+  }
+  return hipSuccess;
 }
 
 template <bool kBack>
@@ -253,9 +307,12 @@ sc_status gp_forward(const gp_config* cfg, int64_t n_nodes, const int32_t* z, co
   if (st != SC_OK) return st;
   DeviceGuard guard(cfg->device);
   if (!guard.ok) return set_error(SC_ERR_HIP, "gp_forward: cannot make cfg->device current");
-  const Rows a{n_nodes, ld_in_of(cfg), ld_out_of(cfg), z, grouping_for(cfg, n_nodes, grouping), cfg->num_elements, cfg->components,
-               cfg->k_in, cfg->k_out, X, W, residual, Y};
-  return launched("gp_forward", launch_rows<false>(cfg, a, static_cast<hipStream_t>(hip_stream)));
+  hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  Grouping group;
+  const hipError_t e = grouping_for(cfg, n_nodes, z, grouping, rows_of_few(cfg, n_nodes, false), workspace, stream, &group);
+  if (e != hipSuccess) return launched("gp_forward", e);
+  const Rows a{n_nodes, ld_in_of(cfg), ld_out_of(cfg), z, group, cfg->num_elements, cfg->components, cfg->k_in, cfg->k_out, X, W, residual, Y};
+  return launched("gp_forward", launch_rows<false>(cfg, a, stream));
 }
 
 sc_status gp_backward(const gp_config* cfg, int64_t n_nodes, const int32_t* z, const void* grouping, const void* X, const void* W,
@@ -288,16 +345,21 @@ sc_status gp_backward(const gp_config* cfg, int64_t n_nodes, const int32_t* z, c
     else hipLaunchKernelGGL(zero_kernel<float>, grid, dim3(kThreads), 0, stream, static_cast<float*>(dW), size);
     return launched("gp_backward", hipGetLastError());
   }
-  const Grouping group = grouping_for(cfg, n_nodes, grouping);
-  if (dX) {
-    const Rows a{n_nodes, ld_out_of(cfg), ld_in_of(cfg), z, group, cfg->num_elements, cfg->components, cfg->k_out, cfg->k_in, dY, W, nullptr, dX};
-    const hipError_t e = launch_rows<true>(cfg, a, stream);
-    if (e != hipSuccess) return launched("gp_backward", e);
+  const bool rows_few = !dX || rows_of_few(cfg, n_nodes, true), outer_few = !dW || outer_of_few(cfg, n_nodes);
+  Grouping group;
+  hipError_t e = grouping_for(cfg, n_nodes, z, grouping, rows_few && outer_few, workspace, stream, &group);
+  const bool ungrouped = n_nodes <= GP_UNGROUPED;
+  const Grouping none{nullptr, nullptr};
+  if (dX && e == hipSuccess) {
+    const Rows a{n_nodes, ld_out_of(cfg), ld_in_of(cfg), z, ungrouped && rows_few ? none : group, cfg->num_elements, cfg->components, cfg->k_out, cfg->k_in, dY, W, nullptr, dX};
+    e = launch_rows<true>(cfg, a, stream);
   }
-  if (!dW) return SC_OK;
-  const Outer a{n_nodes, ld_in_of(cfg), ld_out_of(cfg), z, group, cfg->num_elements, cfg->components, cfg->k_in, cfg->k_out,
-                chunk_rows(cfg, n_nodes), static_cast<int>(slots_of(cfg, n_nodes)), X, dY, dW, workspace};
-  return launched("gp_backward", launch_outer(cfg, a, stream));
+  if (dW && e == hipSuccess) {
+    const Outer a{n_nodes, ld_in_of(cfg), ld_out_of(cfg), z, ungrouped && outer_few ? none : group, cfg->num_elements, cfg->components, cfg->k_in, cfg->k_out,
+                  chunk_rows(cfg, n_nodes), static_cast<int>(slots_of(cfg, n_nodes)), X, dY, dW, static_cast<char*>(workspace) + own_grouping_bytes(cfg)};
+    e = launch_outer(cfg, a, stream);
+  }
+  return launched("gp_backward", e);
 }
 
 }  // extern "C"
