@@ -66,7 +66,8 @@ sc_status gp_grouping_bytes(const gp_config* cfg, int64_t n_nodes, size_t* bytes
  * data: valid until it is overwritten, read by any number of calls.  Up to GP_UNGROUPED atoms it does nothing. */
 sc_status gp_group(const gp_config* cfg, int64_t n_nodes, const int32_t* z, void* grouping, size_t grouping_bytes, void* hip_stream);
 
-/* Bytes of device workspace that gp_forward and gp_backward need.  (Batches without a grouping whose rows are many or wide are grouped by the call itself, there.) */
+/* Bytes of device workspace that gp_forward and gp_backward need.  What a batch of more than GP_UNGROUPED atoms needs is enough for every batch of up to as many.  (Batches without a grouping whose
+ * rows are many or wide are grouped by the call itself, there.) */
 sc_status gp_workspace_bytes(const gp_config* cfg, int64_t n_nodes, size_t* bytes);
 
 /* Forward.  z [n_nodes]; grouping: as gp_group wrote it for this z (NULL up to GP_UNGROUPED atoms); X [n_nodes][components][k_in];

@@ -102,10 +102,13 @@ __global__ __launch_bounds__(kThreads) void zero_kernel(TA* p, int64_t n) {
 
 // Rows of a chunk of dW: enough chunks for the chip where the matrices alone do not fill it (200 000 rows, 128 x 128: 79 us, with two thirds of the chunks 100, with
 // twice as many 91), none so short that adding them up costs more (6000 rows, 256 x 256: 26 us, with 256 rows at least 33; 10 000 rows, 128 x 128: 23, with 64 30).
+constexpr int64_t kLeastRows = 128;
+int64_t chunks_wanted(const gp_config* c) {
+  const int64_t side = parts_serve(c) ? 128 : kBlock;
+  return std::max<int64_t>(1, 384 / (ceil_div(c->k_in, side) * ceil_div(c->k_out, side)));
+}
 int chunk_rows(const gp_config* c, int64_t n) {
-  const int64_t rows = n * c->components, side = parts_serve(c) ? 128 : kBlock, tiles = ceil_div(c->k_in, side) * ceil_div(c->k_out, side);
-  const int64_t wanted = std::max<int64_t>(1, 384 / tiles);
-  return static_cast<int>(std::min<int64_t>(std::max<int64_t>(128, ceil_div(ceil_div(rows, wanted), kBlock) * kBlock), int64_t(1) << 30));
+  return static_cast<int>(std::min<int64_t>(std::max<int64_t>(kLeastRows, ceil_div(ceil_div(n * c->components, chunks_wanted(c)), kBlock) * kBlock), int64_t(1) << 30));
 }
 
 // Batches without a grouping.  Their own kernels read an element's weights once for every four rows of it (dW: take its rows one after the other), which is best for few rows; for more the call
@@ -157,10 +160,12 @@ int64_t slots_of(const gp_config* c, int64_t n) {
 }
 size_t element_size(const gp_config* c) { return c->dtype == SC_F64 ? 8 : c->dtype == SC_F32 ? 4 : 2; }
 size_t weight_size(const gp_config* c) { return c->dtype == SC_F64 ? 8 : 4; }
-// The workspace: a grouping for batches that come without one (a workspace for a large batch has room for it too, so that it serves small ones), partial matrices.
+// The workspace: a grouping for batches that come without one, partial matrices.  A workspace for a large batch serves smaller ones: it has room for the grouping too, and for the most slots that a
+// batch of so many rows can have (with the chunks' length in whole blocks, more rows may have fewer).
 size_t own_grouping_bytes(const gp_config* c) { return offsets_bytes(c->num_elements) + order_bytes(GP_UNGROUPED); }
 size_t workspace_bytes(const gp_config* c, int64_t n) {
-  return own_grouping_bytes(c) + align_up(static_cast<size_t>(slots_of(c, n)) * c->k_in * c->k_out * weight_size(c), 256);
+  const int64_t rows = n * c->components, most = outer_of_few(c, n) || rows <= kLeastRows ? 0 : 2 * std::min(ceil_div(rows, kLeastRows), chunks_wanted(c));
+  return own_grouping_bytes(c) + align_up(static_cast<size_t>(most) * c->k_in * c->k_out * weight_size(c), 256);
 }
 
 sc_status check_config(const char* fn, const gp_config* cfg, int64_t n) {
