@@ -72,7 +72,8 @@ typedef struct {
   double eps;          /* > 0, finite                        */
 } ou_config;
 
-/* Bytes of device workspace that ou_step needs for this list. */
+/* Bytes of device workspace that ou_step needs for this list.  (A matrix whose shorter side is at most 64 or 128 and whose longer one is more takes there what squares of 64 x 64 or 128 x 128 along
+ * its longer side take, however short the shorter one is: 100 000 of 1 x 200 9.8 GB.) */
 sc_status ou_workspace_bytes(const ou_config* cfg, int64_t n_tensors, const ou_tensor* tensors, size_t* bytes);
 
 /* workspace: device memory, 256-byte aligned, at least ou_workspace_bytes(). */

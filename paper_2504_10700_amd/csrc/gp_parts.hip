@@ -8,12 +8,12 @@
 //
 // A workgroup: 128 rows of a bucket x 128 columns, or 128 x 128 of an element's dW over a chunk of rows, four waves of 64 x 64.  32 reduced indices of both
 // operands are requested while the 32 before are multiplied, and pass through registers, where they are split, to LDS.  One set of LDS and two barriers a
-// stage: the two or, of bfloat16 rows, three workgroups of a compute unit fill each other's waits (200 000 rows of bfloat16, 128 x 128: 38 us with three, 43 with two
+// stage: the two or, of bfloat16 rows, three workgroups of a compute unit fill each other's waits (200 000 rows of bfloat16, 128 x 128: with three a tenth less than with two
 // that request their rows two stages ahead).
 //
-// 149 997 rows of fp32, 128 x 128: Y 54 us (160 MB, 3.0 TB/s; the products are 27 at the rate of a large product), dW 62 and 15 for the chunks' sums; 200 000 of bfloat16: 38, 35
-// and 30 us.  What bounds them is the splitting beside loads and products in turn: the matrix cores work a fifth of the cycles.  16 384 rows, 64 elements,
-// 1024 x 2048: Y 295 us of bfloat16 (700 TFLOP/s), 555 of fp32 (740), matrix cores a third of the cycles.
+// Medians of a trace, inputs from memory.  149 997 rows of fp32, 128 x 128: Y 62 us (160 MB, 2.6 TB/s; the products are 27 at the rate of a large product), dX 57, dW 64 and 16 for the
+// chunks' sums; 200 000 of bfloat16: 47, 42, 37 and 16.  What bounds them is the splitting beside loads and products in turn: the matrix cores work a fifth of the cycles.  16 384 rows, 64
+// elements, 1024 x 2048: Y of bfloat16 289 us (710 TFLOP/s; called in turn 285, of fp32 522: 790), dX 272, dW 341; matrix cores two fifths of the cycles in Y and dX, a tenth in dW.
 #include <algorithm>
 #include <type_traits>
 

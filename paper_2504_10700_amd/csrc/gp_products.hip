@@ -3,8 +3,8 @@
 //
 // Rows (Y, dX): a workgroup computes 64 rows of one bucket x 64 columns; the rows are gathered by the grouping's order, the reduced index goes
 // through LDS 16 at a time.  dW: a workgroup computes 64 x 64 of one element's matrix over a chunk of the element's rows; elements with several chunks leave
-// partial matrices that a second launch adds in order.  fp64, 60 000 rows, 128 x 128: Y and dX 65 us each, where the products at the rate of a large one are 31 and the
-// memory 26, dW 124; the loads of a stage are waited for.
+// partial matrices that a second launch adds in order.  fp64, 60 000 rows, 10 elements, 128 x 128: Y 64 us, dX 61, dW 81 with the chunks' sums, where the products at the
+// rate of a large one are 31 and the memory 26: a stage is 16 reduced indices in loads of an element each, and one stage is requested ahead.
 #include <algorithm>
 #include <cmath>
 #include <initializer_list>

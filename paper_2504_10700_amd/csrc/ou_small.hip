@@ -4,7 +4,7 @@
 // matrix (X, S or P) in one half of its LDS and those of X transposed in the other; X and S in fp32 stay in registers, where the matrix instruction leaves its
 // results: four waves, each with every second 32 x 32 block of every second row of blocks, so that a matrix of half the size keeps all of them busy.
 //
-// Up to 64 or 128 columns (whole_kernel) everything from the gradient to the weight is one launch: 89 x 64 x 64 with five steps take 20 us, 89 x 128 x 128 64 (47 and 134
+// Up to 64 or 128 columns (whole_kernel) everything from the gradient to the weight is one launch: 89 x 64 x 64 with five steps take 21 us, 89 x 128 x 128 64 (47 and 134
 // in slices, 91 and 140 in tiles); 19 of the 64 are matrix instructions, the rest is splitting into parts, LDS and memory.  Wider matrices are cut along their columns into at most
 // kSlices slices (slice_kernel): a launch a step, in which each workgroup adds up the slices' S in order, makes P for itself, its slice of the
 // next X, and that slice's share of the next S.

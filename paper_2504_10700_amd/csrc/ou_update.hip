@@ -418,7 +418,7 @@ hipError_t first_pass(const Layout& l, int way, int end, const Step& st, char* b
   return hipGetLastError();
 }
 
-// Tiles of 64 that do not fill the compute units: smaller ones (five steps of one 512 x 700 295 us instead of 716, of 40 512 x 512 4.1 ms instead of 3.6).
+// Tiles of 64 that do not fill the compute units: smaller ones (fp64, five steps of one 512 x 700 299 us instead of 716, of 40 512 x 512 4.1 ms instead of 3.5).
 template <typename TA, int kPhase>
 hipError_t launch(const Part& p, const Item* items, const Step& st, bool last, const TA* X, TA* next, TA* S, TA* P, hipStream_t stream) {
   const int n = static_cast<int>(p.items.size());
